@@ -52,7 +52,7 @@ typedef enum {
     MONE_ERR_TIMEOUT = 5,           /* a bounded device-side wait gave up (latched) */
     MONE_ERR_NONFINITE = 6,         /* an updated fast weight was NaN/Inf (latched) */
     MONE_ERR_UNSUPPORTED = 7,       /* valid request this build does not implement */
-    MONE_ERR_CHECK = 8              /* a device-side index check failed (MONE_DEBUG builds; latched) */
+    MONE_ERR_CHECK = 8              /* a device-side index check failed (the learning kernels': MONE_DEBUG builds; latched) */
 } mone_status;
 
 enum { MONE_FP32 = 0, MONE_BF16 = 1 };  /* dtype of X, K, V, Xq and generated K/V */
@@ -296,6 +296,92 @@ mone_status mone_attention(mone_mem* m, const void* Q, int n_q_heads, int Lq, co
                            const long long kv_strides[4], int n_mem, void* out, void* stream);
 
 /*
+ * Windowed attention of a prompt's tokens (mone_attention's caches and layouts, another mask).  Query token i stands at
+ * position t = n_past + i and sees the positions j <= t with
+ *     j < n_sink   (the first positions, which stay visible: the memory's tokens, say), or
+ *     j > t - window   (the last `window` positions, its own among them),
+ * each with weight softmax_j(q . k_j / sqrt(head_dim)).  A token that sees no key, or only keys of score -inf, has
+ * output 0.  What a token does not see has no effect on it, whatever it holds.
+ *   layer  MONE_ALL_LAYERS, or one layer of the handle: Q and out are then [n_ctx][n_q_heads][Lq][head_dim]
+ *   Q, K, V, kv_strides, out  as in mone_attention; the caches hold at least n_past + Lq positions
+ * Constraints: n_q_heads as in mone_attention; 1 <= Lq; n_past, n_sink, window >= 0 (a window of n_past + Lq hides
+ * nothing); n_past + Lq <= 2^20.  Errors: INVALID_ARG.  Asynchronous on stream.
+ */
+#define MONE_ALL_LAYERS (-1)
+mone_status mone_window_attention(mone_mem* m, int layer, const void* Q, int n_q_heads, int Lq, const void* K, const void* V,
+                                  const long long kv_strides[4], int n_past, int n_sink, int window, void* out, void* stream);
+
+/*
+ * A paged cache: the keys and values that a serving program keeps of its contexts (the memory's tokens among them, put
+ * there by mone_cache_append), in pages of page_size positions that any context may hold in any order.  Position p of
+ * context c is place p % page_size of page table[c * table_width + p / page_size], the same page numbers in every layer.
+ *   K, V       pools of the handle's dtype, 16-byte aligned, with element strides (layer, page, KV head, position in
+ *              the page), head_dim contiguous; a layer's pool has n_pages pages; no stride is negative
+ *   page_size  a power of two, at most 1024
+ *   lens       positions that each context holds, in device memory, so that a captured graph can serve growing contexts
+ *   score      NULL, or for every context, layer and KV head the attention weight that each position has been given
+ *              so far: [n_ctx][n_layers][n_kv_heads][table_width * page_size] fp32
+ * Contexts are the handle's n_ctx; a `layer` argument is one of its layers (the other arrays of the call then have no
+ * layer dimension) or MONE_ALL_LAYERS.  Table entries past a context's positions are not read.  An entry outside the
+ * pool, or a length outside 0 .. table_width * page_size, is latched as MONE_ERR_CHECK (mone_mem_sync) and its
+ * positions are skipped.
+ */
+typedef struct {
+    void *K, *V;
+    long long strides[4];
+    int n_pages, page_size;
+    const int* table; /* [n_ctx][table_width] */
+    int table_width;
+    const int* lens;  /* [n_ctx] */
+    float* score;
+} mone_cache;
+
+/*
+ * Write new tokens' keys and values after the positions that each context holds (lens, from before the tokens), into
+ * pages that its table already names, and set their scores to 0.
+ *   K, V     the handle's dtype, element strides (context, layer, KV head, token), head_dim contiguous: for example
+ *            the output of mone_mem_generate_kv, or a layer's projections of a prompt
+ *   n_tok    tokens of each context; counts: NULL, or how many of them to write per context (device, 0 .. n_tok)
+ *   lens_out NULL, or [n_ctx] (device, not lens itself): the lengths with the new tokens
+ * Positions past the table are not written and latch MONE_ERR_CHECK.  Errors: INVALID_ARG, UNSUPPORTED_SHAPE (page_size).
+ */
+mone_status mone_cache_append(mone_mem* m, int layer, const mone_cache* cache, const void* K, const void* V,
+                              const long long strides[4], int n_tok, const int* counts, int* lens_out, void* stream);
+
+/*
+ * Attention of the newest n_tok tokens of every context over its cache (lens counts them: they have been appended).  Token
+ * i of a context stands at position t = lens - n_tok + i and sees what mone_window_attention's would: j <= t with
+ * j < n_sink or j > t - window.  A token of a context that holds fewer than n_tok - i positions sees nothing; its
+ * output is 0.
+ *   Q, out  [n_ctx][n_layers][n_q_heads][n_tok][head_dim], dense, the handle's dtype
+ * With cache->score, the weight of every position is added to it, summed over the query heads of its KV head and the
+ * tokens (for mone_cache_evict).  The sums are in fixed order: equal calls give equal bits.
+ * Constraints: n_q_heads a multiple of n_kv_heads, n_q_heads / n_kv_heads <= 64; 1 <= n_tok <= 16; n_sink, window >= 0.
+ * The handle keeps a workspace that grows with the call's sizes (growing synchronises the stream, so a call of the
+ * largest size comes before any capture); calls of one handle that overlap on two streams share it: order them.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (page_size), OOM, CUDA.
+ */
+mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache, const void* Q, int n_q_heads, int n_tok,
+                                 int n_sink, int window, void* out, void* stream);
+
+/*
+ * Cut every context's cache down to `keep` positions, for each layer and KV head on its own: the first n_sink, the last
+ * n_recent, and of the others those with the highest scores (a NaN counts as -inf; of equal ones the lower position).
+ * A context of at most `keep` positions keeps all of them.  The survivors are written in their order to positions
+ * 0, 1, .. of the pages of to_table, with their scores; what they leave stays as it is, so pages that contexts share may
+ * be evicted from, and the caller gives the old ones back when every layer is done.
+ *   to_table  [n_ctx][to_width] pages of the same pools (device), to_width * page_size >= keep; they may hold
+ *             nothing that the call reads
+ *   to_score  [n_ctx][n_layers][n_kv_heads][to_width * page_size]; entries past the survivors keep what they hold
+ *   kept      [n_ctx][n_layers][n_kv_heads][keep] int32: the survivors' old positions, then -1
+ *   lens_out  NULL, or [n_ctx] (device, not lens itself): min(lens, keep)
+ * Constraints: cache->score given; keep >= 1; n_sink, n_recent >= 0; n_sink + n_recent <= keep.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (page_size), CUDA.  Asynchronous on stream.
+ */
+mone_status mone_cache_evict(mone_mem* m, int layer, const mone_cache* cache, int keep, int n_sink, int n_recent,
+                             const int* to_table, int to_width, float* to_score, int* kept, int* lens_out, void* stream);
+
+/*
  * Per-kernel device timing for measurement.  While enabled, the library records
  * a pair of CUDA events on the caller's stream around every kernel it launches
  * (this adds host work per launch; leave it off outside measurement).
@@ -307,7 +393,8 @@ mone_status mone_attention(mone_mem* m, const void* Q, int n_q_heads, int Lq, co
  * target, MONE_LOSS_MSE only), 6 consumer attention, 7 resident chains (the fp32 MLP
  * path when d_in + d_out <= 512: every segment of an input window in one launch,
  * forward, backward and update together), 8 host-input gathers (mone_ttl_context_host;
- * timed on the library's staging stream).  Errors: INVALID_ARG, CUDA.
+ * timed on the library's staging stream), 9 paged-cache operators (mone_cache_*).  The windowed
+ * attention counts as kind 6.  Errors: INVALID_ARG, CUDA.
  */
 mone_status mone_mem_set_timing(mone_mem* m, int enable);
 mone_status mone_mem_kernel_time(mone_mem* m, int kind, double* ms, long long* launches);

@@ -400,3 +400,41 @@ def attention(Q, K, V, n_mem: int):
             out[h, i] = (p / p.sum()) @ Vh[:vis]
     return out
 
+
+# --------------------------------------------------------------------------- cache operators
+
+def window_attention(Q, K, V, t0: int, n_sink: int, window: int):
+    """Query token i at position t = t0 + i sees the positions j <= t with j < n_sink or j > t - window, by softmax of
+    q . k_j / sqrt(d_h); a token that sees nothing (t < 0 included) has output 0.
+
+    Q [n_q, Lq, d_h]; K, V [n_kv, n, d_h], of which unseen rows may hold anything.  Returns the outputs [n_q, Lq, d_h]
+    and the weight that each position is given, summed over the tokens and the query heads of its KV head [n_kv, n]."""
+    Q, K, V = f64(Q), f64(K), f64(V)
+    n_q, Lq, dh = Q.shape
+    n_kv, n = K.shape[:2]
+    out, weight = np.zeros((n_q, Lq, dh)), np.zeros((n_kv, n))
+    j = np.arange(n)
+    for i in range(Lq):
+        t = t0 + i
+        sees = j[(j <= t) & ((j < n_sink) | (j > t - window))]
+        if len(sees) == 0:
+            continue
+        for h in range(n_q):
+            g = h // (n_q // n_kv)
+            z = K[g, sees] @ Q[h, i] / np.sqrt(dh)
+            p = np.exp(z - z.max())
+            p /= p.sum()
+            out[h, i] = p @ V[g, sees]
+            weight[g, sees] += p
+    return out, weight
+
+
+def cache_keep(score, keep: int, n_sink: int, n_recent: int):
+    """Positions that stay, in order: all of at most `keep`; else the first n_sink, the last n_recent, and of the others
+    those of the highest scores (NaN lowest, equal ones by position)."""
+    score = f64(score)
+    n = len(score)
+    if n <= keep:
+        return np.arange(n)
+    rank = sorted(range(n_sink, n - n_recent), key=lambda p: (-(-np.inf if np.isnan(score[p]) else score[p]), p))
+    return np.array(sorted([*range(n_sink), *rank[:keep - n_sink - n_recent], *range(n - n_recent, n)]), dtype=int)

@@ -24,6 +24,7 @@ MONE_LOSS_DOT, MONE_LOSS_MSE = 0, 1
 MONE_MEM_MLP, MONE_MEM_SWIGLU = 0, 1
 MONE_RENORM_ROWS, MONE_RENORM_OUT = 0, 1
 MONE_GATE_LINEAR, MONE_GATE_SILU = 0, 1
+MONE_ALL_LAYERS = -1
 
 STATUS = {0: "MONE_OK", 1: "MONE_ERR_INVALID_ARG", 2: "MONE_ERR_UNSUPPORTED_SHAPE", 3: "MONE_ERR_OOM",
           4: "MONE_ERR_CUDA", 5: "MONE_ERR_TIMEOUT", 6: "MONE_ERR_NONFINITE", 7: "MONE_ERR_UNSUPPORTED",
@@ -34,9 +35,11 @@ EXPORTS = ("mone_mem_init", "mone_ttl_segment", "mone_ttl_context", "mone_mem_ge
            "mone_mem_read_state", "mone_mem_write_state", "mone_mem_sync", "mone_mem_launch_count",
            "mone_status_string", "mone_abi_version", "mone_mem_set_timing", "mone_mem_kernel_time",
            "mone_last_error", "mone_mem_generate_kv_noalloc", "mone_attention", "mone_mem_kernel_busy",
-           "mone_ttl_context_metrics", "mone_ttl_context_host")
+           "mone_ttl_context_metrics", "mone_ttl_context_host", "mone_window_attention", "mone_cache_append",
+           "mone_cache_attention", "mone_cache_evict")
 
-KERNEL_KINDS = ("prepass", "phase_a", "phase_b", "finalize", "read", "mse", "attention", "resident", "stage")
+KERNEL_KINDS = ("prepass", "phase_a", "phase_b", "finalize", "read", "mse", "attention", "resident", "stage",
+                 "cache")
 
 
 class MoneError(RuntimeError):
@@ -56,6 +59,12 @@ class mone_config(ctypes.Structure):
 
 class mone_meta(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("alpha", "gamma", "w_eta", "b_eta", "w_beta", "b_beta", "gate")]
+
+
+class mone_cache(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("strides", ctypes.c_longlong * 4),
+                ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int), ("table", ctypes.c_void_p),
+                ("table_width", ctypes.c_int), ("lens", ctypes.c_void_p), ("score", ctypes.c_void_p)]
 
 
 _lib = None
@@ -81,6 +90,10 @@ def lib(path: Optional[str] = None) -> ctypes.CDLL:
         "mone_mem_generate_kv": ([vp, vp, i, vp, vp, ctypes.POINTER(ll), vp], i),
         "mone_mem_generate_kv_noalloc": ([vp, vp, i, vp, vp, ctypes.POINTER(ll), vp], i),
         "mone_attention": ([vp, vp, i, i, vp, vp, ctypes.POINTER(ll), i, vp, vp], i),
+        "mone_window_attention": ([vp, i, vp, i, i, vp, vp, ctypes.POINTER(ll), i, i, i, vp, vp], i),
+        "mone_cache_append": ([vp, i, ctypes.POINTER(mone_cache), vp, vp, ctypes.POINTER(ll), i, vp, vp, vp], i),
+        "mone_cache_attention": ([vp, i, ctypes.POINTER(mone_cache), vp, i, i, i, i, vp, vp], i),
+        "mone_cache_evict": ([vp, i, ctypes.POINTER(mone_cache), i, i, i, vp, i, vp, vp, vp, vp], i),
         "mone_mem_free": ([vp], i),
         "mone_mem_read_state": ([vp, vp, vp, vp, vp, vp], i),
         "mone_mem_write_state": ([vp, vp, vp, vp, vp, vp], i),
@@ -188,6 +201,51 @@ def mone_attention(h: int, Q, n_q_heads: int, Lq: int, K, V, kv_strides: Sequenc
     arr = (ctypes.c_longlong * 4)(*[int(s) for s in kv_strides])
     _check("mone_attention", lib().mone_attention(h, _ptr(Q), n_q_heads, Lq, _ptr(K), _ptr(V), arr, n_mem, _ptr(out),
                                                   _stream(stream)))
+
+
+def mone_window_attention(h: int, layer: int, Q, n_q_heads: int, Lq: int, K, V, kv_strides: Sequence[int], n_past: int,
+                          n_sink: int, window: int, out, stream=None):
+    """Attention of a prompt's tokens over the first n_sink positions and the last `window` up to their own."""
+    arr = (ctypes.c_longlong * 4)(*[int(s) for s in kv_strides])
+    _check("mone_window_attention", lib().mone_window_attention(h, layer, _ptr(Q), n_q_heads, Lq, _ptr(K), _ptr(V), arr, n_past,
+                                                                n_sink, window, _ptr(out), _stream(stream)))
+
+
+def make_cache(K, V, table, lens, score=None) -> mone_cache:
+    """A paged cache over torch tensors: K, V [layers, pages, KV heads, page_size, head_dim] of any strides with head_dim
+    contiguous (K.stride() == V.stride()), table [contexts, width] and lens [contexts] int32, score fp32.  It holds their
+    addresses, not the tensors: keep them alive."""
+    if K.stride() != V.stride() or K.shape != V.shape or K.dim() != 5 or K.stride(4) != 1:
+        raise ValueError("K and V: [layers, pages, KV heads, page_size, head_dim], the same strides, head_dim contiguous")
+    for name, t, dims in (("table", table, 2), ("lens", lens, 1), ("score", score, 4)):
+        if t is not None and (t.dim() != dims or not t.is_contiguous() or t.element_size() != 4):
+            raise ValueError(f"{name}: a contiguous tensor of {dims} dimensions and 32-bit elements")
+    return mone_cache(_ptr(K), _ptr(V), (ctypes.c_longlong * 4)(*K.stride()[:4]), K.shape[1], K.shape[3], _ptr(table),
+                      table.shape[1], _ptr(lens), _ptr(score))
+
+
+def mone_cache_append(h: int, layer: int, cache: mone_cache, K, V, strides: Sequence[int], n_tok: int, lens_out=None, counts=None,
+                      stream=None):
+    """New tokens' keys and values after each context's positions."""
+    arr = (ctypes.c_longlong * 4)(*[int(s) for s in strides])
+    _check("mone_cache_append", lib().mone_cache_append(h, layer, ctypes.byref(cache), _ptr(K), _ptr(V), arr, n_tok, _ptr(counts),
+                                                        _ptr(lens_out), _stream(stream)))
+
+
+def mone_cache_attention(h: int, layer: int, cache: mone_cache, Q, n_q_heads: int, n_tok: int, n_sink: int, window: int, out,
+                         stream=None):
+    """Attention of each context's newest n_tok tokens over its pages; with cache.score, the weights are added up there."""
+    _check("mone_cache_attention", lib().mone_cache_attention(h, layer, ctypes.byref(cache), _ptr(Q), n_q_heads, n_tok, n_sink,
+                                                              window, _ptr(out), _stream(stream)))
+
+
+def mone_cache_evict(h: int, layer: int, cache: mone_cache, keep: int, n_sink: int, n_recent: int, to_table, to_score, kept,
+                     lens_out=None, stream=None):
+    """The first n_sink positions, the last n_recent and the best scored others, `keep` in all, into the pages of to_table
+    [contexts, width]."""
+    _check("mone_cache_evict", lib().mone_cache_evict(h, layer, ctypes.byref(cache), keep, n_sink, n_recent, _ptr(to_table),
+                                                      to_table.shape[1], _ptr(to_score), _ptr(kept), _ptr(lens_out),
+                                                      _stream(stream)))
 
 
 def mone_mem_free(h: int):

@@ -14,6 +14,10 @@
 // keys l and l + 32 against every item (queries in shared memory), the chunk's max and sum
 // are reduced once per item, and the probabilities pass through shared memory into the
 // value accumulation, where a lane owns hd / 32 dimensions.
+//
+// The windowed attention (mone_window_attention) is the WIN instance of each form: of the positions up to its
+// own, a token sees the first n_sink and the last `window`.  A form then steps over the chunks that hold some
+// row's visible keys only (WinRange), and masks within them.
 #include <algorithm>
 #include <cfloat>
 #include <mutex>
@@ -39,8 +43,21 @@ struct AttnArgs {
     float scale;            // 1 / sqrt(hd)
     int tile_tok, per_block;  // decode form: tokens of a block, 16-row tiles that cut it
     int group_inv;            // decode form: 65536 / group + 1
+    int n_sink, window;     // WIN: a token at position t sees j <= t with j < n_sink or j > t - window
     int vec;                // caches 16-byte aligned (base and every stride): stage with 16-byte loads
     int* status;            // device status word (bounded waits of the prefill form)
+};
+
+// The chunks of STEP positions that hold the keys of the tokens at positions t0 .. t1: those of the first
+// positions, then those from the first token's window on.  Every position is in one chunk at most.
+struct WinRange {
+    int ns, lo, n;  // chunks of the first positions; first position after them; chunks in all
+    __device__ WinRange(const AttnArgs& a, int t0, int t1, int step) {
+        ns = (min(a.n_sink, t1 + 1) + step - 1) / step;
+        lo = max(ns * step, t0 - a.window + 1);
+        n = ns + (lo <= t1 ? (t1 - lo) / step + 1 : 0);
+    }
+    __device__ int at(int j, int step) const { return j < ns ? j * step : lo + (j - ns) * step; }
 };
 
 // Stage cache positions [j0, j0 + nk) of one head into shared memory as fp32 rows of HD
@@ -80,6 +97,30 @@ __device__ __forceinline__ void stage_rows(float* dst, const T* src, long long s
     }
 }
 
+// Output dimensions d0, d0 + STEP, .. of one row over the keys it sees and no others, by one thread.  A tile's
+// products take a key's value row times a probability of 0 for the rows that do not see it, which is NaN where the
+// value is not finite; a row of the windowed attention with such a result is computed again here.  One pass with
+// a running maximum; slow, and reached by non-finite inputs only.
+template <typename T, int HD, int N, int STEP>
+__device__ __noinline__ void row_again(const T* q, const T* K, const T* V, long long s3, int vis, const AttnArgs& a, int d0, float* o) {
+    float m = -INFINITY, l = 0.f;
+    for (int d = 0; d < N; ++d) o[d] = 0.f;
+    for (int j = min(a.n_sink, vis) > 0 ? 0 : max(0, vis - a.window); j < vis; ++j) {
+        if (j >= a.n_sink && j < vis - a.window) j = vis - a.window;
+        if (j >= vis) break;
+        float z = 0.f;
+        for (int d = 0; d < HD; ++d) z = fmaf(to_f<T>(q[d]), to_f<T>(K[(long long)j * s3 + d]), z);
+        z *= a.scale;
+        if (z == -INFINITY) continue;
+        const float mn = fmaxf(m, z), corr = __expf(m - mn), p = __expf(z - mn);
+        m = mn;
+        l = fmaf(l, corr, p);
+        for (int d = 0; d < N; ++d) o[d] = fmaf(o[d], corr, p * to_f<T>(V[(long long)j * s3 + d0 + STEP * d]));
+    }
+    const float inv = l > 0.f ? 1.f / l : l;
+    for (int d = 0; d < N; ++d) o[d] *= inv;
+}
+
 template <typename T, int HD>
 struct AttnSmem {
     // key rows padded by 4 floats: a lane reads its key row 16 bytes at a time, and the 8 lanes of a
@@ -92,7 +133,7 @@ struct AttnSmem {
     static constexpr int FLOATS = P_OFF + ATT_WARPS * MAXI * KC;
 };
 
-template <typename T, int HD>
+template <typename T, int HD, bool WIN>
 __global__ void __launch_bounds__(ATT_WARPS * 32, 2) attention_kernel(const AttnArgs a) {
     using SM = AttnSmem<T, HD>;
     constexpr int D = HD / 32;  // value / accumulator dimensions per lane
@@ -135,7 +176,10 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, 2) attention_kernel(const Attn
     }
     const int last = min(a.Lq, r0 + a.rows) - 1;
     const int keys = a.n_mem + last + 1;  // positions the tile's last token sees
-    for (int j0 = 0; j0 < keys; j0 += KC) {
+    const WinRange win(a, a.n_mem + r0, keys - 1, KC);
+    const int n_ch = WIN ? win.n : (keys + KC - 1) / KC;
+    for (int ch = 0; ch < n_ch; ++ch) {
+        const int j0 = WIN ? win.at(ch, KC) : ch * KC;
         const int nk = min(KC, keys - j0);
         __syncthreads();
         stage_rows<T, HD>(Ks, Kc, a.s3, j0, nk, a.vec, SM::KP);
@@ -164,7 +208,11 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, 2) attention_kernel(const Attn
 #pragma unroll
         for (int k = 0; k < MAXI; ++k) {
             // causal / chunk masks; an item with no visible key in this chunk keeps its state
-            const bool v0 = lane < nk && j0 + lane < vis[k], v1 = lane + 32 < nk && j0 + lane + 32 < vis[k];
+            bool v0 = lane < nk && j0 + lane < vis[k], v1 = lane + 32 < nk && j0 + lane + 32 < vis[k];
+            if constexpr (WIN) {
+                v0 = v0 && (j0 + lane < a.n_sink || j0 + lane >= vis[k] - a.window);
+                v1 = v1 && (j0 + lane + 32 < a.n_sink || j0 + lane + 32 >= vis[k] - a.window);
+            }
             const float cm = warp_max(fmaxf(v0 ? z0[k] : -INFINITY, v1 ? z1[k] : -INFINITY));
             float p0 = 0.f, p1 = 0.f;
             if (cm != -INFINITY) {
@@ -206,9 +254,24 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, 2) attention_kernel(const Attn
         const int it = warp + ATT_WARPS * k;
         const int h = g * a.group + it / a.rows, i = r0 + it % a.rows;
         T* o = static_cast<T*>(a.out) + (((size_t)c * a.n_q + h) * a.Lq + i) * HD;
-        const float inv = 1.f / sum[k];
+        if constexpr (WIN) {
+            const float inv = sum[k] > 0.f ? 1.f / sum[k] : sum[k];  // no key that counts: 0; NaN stays
+            bool bad = false;
 #pragma unroll
-        for (int d = 0; d < D; ++d) o[lane + 32 * d] = from_f<T>(acc[k][d] * inv);
+            for (int d = 0; d < D; ++d) {
+                bad |= !isfinite(acc[k][d] * inv);
+                o[lane + 32 * d] = from_f<T>(acc[k][d] * inv);
+            }
+            if (bad) {
+                float w[D];
+                row_again<T, HD, D, 32>(static_cast<const T*>(a.Q) + (o - static_cast<T*>(a.out)), Kc, Vc, a.s3, vis[k], a, lane, w);
+                for (int d = 0; d < D; ++d) o[lane + 32 * d] = from_f<T>(w[d]);
+            }
+        } else {
+            const float inv = 1.f / sum[k];
+#pragma unroll
+            for (int d = 0; d < D; ++d) o[lane + 32 * d] = from_f<T>(acc[k][d] * inv);
+        }
     }
 }
 
@@ -283,7 +346,7 @@ __device__ __forceinline__ float fa_probs(const float (&v)[N], uint64_t k2, uint
     return s.x + s.y;
 }
 
-template <int HD>
+template <int HD, bool WIN>
 __global__ void __launch_bounds__(FaSmem<HD>::THREADS, 2)
 attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                          const __grid_constant__ CUtensorMap tmV, const AttnArgs a) {
@@ -327,10 +390,14 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
 
     // token tiles: the last first (causal: it has the most keys)
     const int c = blockIdx.z, g = blockIdx.y, rt = a.rows, r0 = (gridDim.x - 1 - blockIdx.x) * rt;
-    const int keys = a.n_mem + min(a.Lq, r0 + rt), n = (keys + NK - 1) / NK;  // keys the tile's last token sees, in chunks
+    const int keys = a.n_mem + min(a.Lq, r0 + rt);  // keys the tile's last token sees
+    const WinRange win(a, a.n_mem + r0, keys - 1, NK);
+    const int n = WIN ? win.n : (keys + NK - 1) / NK;  // in chunks
+    auto pos = [&](int j) { return WIN ? win.at(j, NK) : j * NK; };  // first position of chunk j
     // The last chunk may hold later tokens' rows (past the cache's last row TMA writes zeros). No probability of theirs is
     // added up, but 0 times a non-finite value would be: their value rows are cleared.
-    const bool clear = keys < a.n_mem + a.Lq && keys < n * NK;
+    // (WIN: rows differ in what they see at both ends, and a row with a non-finite result is computed again instead.)
+    const bool clear = !WIN && keys < a.n_mem + a.Lq && keys < n * NK;
 
     if (warp == SM::LOAD_WARP) {
         bool landed = false;
@@ -351,7 +418,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
                 mbar_expect_tx(full(s), SM::TILE);
 #pragma unroll
                 for (int kb = 0; kb < HD / 64; ++kb)
-                    tma_load_5d(dst + kb * SM::SLAB, m, full(s), 64 * kb, j * NK, head, layer, ctx);
+                    tma_load_5d(dst + kb * SM::SLAB, m, full(s), 64 * kb, pos(j), head, layer, ctx);
                 if (++s == NS) {
                     s = 0;
                     ph ^= 1;
@@ -451,8 +518,16 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
                 tmem_ld48(t_s + half * NE, v);
             else
                 tmem_ld32(t_s + half * NE, v);
-            if ((j + 1) * NK > a.n_mem + r0 + 1) {      // some row does not see the whole chunk:
-                const int nv = vis - j * NK - half * NE;  // a hidden key's score of -inf gives it a probability of 0
+            if constexpr (WIN) {
+                const int p0 = pos(j);
+                // some row does not see the whole chunk (in the window of all: from the last token's first key on)
+                if (p0 + NK > a.n_mem + r0 + 1 || (p0 + NK > a.n_sink && p0 < keys - a.window)) {
+                    const int at = p0 + half * NE, nv = vis - at, nw = vis - a.window - at, ns = a.n_sink - at;
+#pragma unroll
+                    for (int u = 0; u < NE; ++u) v[u] = u < nv && (u >= nw || u < ns) ? v[u] : -INFINITY;
+                }
+            } else if ((j + 1) * NK > a.n_mem + r0 + 1) {  // some row does not see the whole chunk:
+                const int nv = vis - j * NK - half * NE;     // a hidden key's score of -inf gives it a probability of 0
 #pragma unroll
                 for (int u = 0; u < NE; ++u) v[u] = u < nv ? v[u] : -INFINITY;
             }
@@ -506,13 +581,33 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         ok = named_bar_and(1 + quarter, 64, ok);
         if (ok) {
             tc_fence_after();
-            const float inv = 1.f / (l + x[(half ^ 1) * 128 + row]);
+            const float sum = l + x[(half ^ 1) * 128 + row];
+            const float inv = WIN && sum == 0.f ? 0.f : 1.f / sum;
             bf16* orow = static_cast<bf16*>(a.out) +
                          (((size_t)c * a.n_q + g * a.group + (live ? hr : 0)) * a.Lq + (live ? i : 0)) * HD + half * (HD / 2);
 #pragma unroll
             for (int cb = 0; cb < HD / 2; cb += 32) {
                 float v[32];
+                if constexpr (WIN) __syncwarp();  // the threads of rows computed again
                 tmem_ld32(t_o + cb, v);
+                if constexpr (WIN) {
+                    bool bad = false;
+#pragma unroll
+                    for (int u = 0; u < 32; ++u) bad |= !isfinite(v[u] * inv);
+                    if (live && bad) {
+                        const long long kv_off = (long long)(c / a.L) * a.s0 + (long long)(c % a.L) * a.s1 + (long long)g * a.s2;
+                        float w[32];  // its own: the address of v would put it in local memory
+                        row_again<bf16, HD, 32, 1>(static_cast<const bf16*>(a.Q) + (orow - static_cast<bf16*>(a.out)) - half * (HD / 2),
+                                                   static_cast<const bf16*>(a.K) + kv_off, static_cast<const bf16*>(a.V) + kv_off, a.s3,
+                                                   vis, a, half * (HD / 2) + cb, w);
+#pragma unroll
+                        for (int u = 0; u < 32; u += 8)
+                            *reinterpret_cast<uint4*>(orow + cb + u) =
+                                make_uint4(pack_bf16(w[u], w[u + 1]), pack_bf16(w[u + 2], w[u + 3]), pack_bf16(w[u + 4], w[u + 5]),
+                                           pack_bf16(w[u + 6], w[u + 7]));
+                        continue;
+                    }
+                }
                 if (live) {
 #pragma unroll
                     for (int u = 0; u < 32; u += 8)
@@ -594,7 +689,7 @@ __device__ __forceinline__ float ld_cluster_f32(const float* p, uint32_t rank) {
     return v;
 }
 
-template <int HD>
+template <int HD, bool WIN>
 __global__ void __launch_bounds__(DE_WARPS * 32, HD == 64 ? 4 : 3) attention_decode_kernel(const AttnArgs a, int splits) {
     constexpr int NP = HD / 32, NV = HD / 64;  // 16-byte pieces of a key per thread; of a value
     constexpr int KB = HD == 64 ? 32 : 16;     // keys per step
@@ -628,17 +723,21 @@ __global__ void __launch_bounds__(DE_WARPS * 32, HD == 64 ? 4 : 3) attention_dec
     float o[8 * NV][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < 8 * NV; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-    const int nb = (keys + KB - 1) / KB;
+    const int t_first = WIN ? a.n_mem + __shfl_sync(0xffffffffu, tile.tok0 + DeTile::over_group(a, tile.rr0), 0) : 0;
+    const WinRange win(a, t_first, keys - 1, KB);
+    const int nb = WIN ? win.n : (keys + KB - 1) / KB;
+    // a key of a block is read if some row of the tile sees it
+    auto seen = [&](int key) { return key < keys && (!WIN || key < a.n_sink || key > t_first - a.window); };
     const int b1 = (int)((long long)nb * (rank + 1) / splits);
     for (int b = (int)((long long)nb * rank / splits) + warp; b < b1; b += DE_WARPS) {
-        const int j0 = b * KB;
+        const int j0 = WIN ? win.at(b, KB) : b * KB;
         uint4 kr[KB / 8][NP], vr[KB / 16][4][NV];
 #pragma unroll
         for (int nt = 0; nt < KB / 8; ++nt) {
             const int key = j0 + 8 * nt + gq;
 #pragma unroll
             for (int p = 0; p < NP; ++p)
-                kr[nt][p] = key < keys ? __ldg(reinterpret_cast<const uint4*>(Kc + (long long)key * a.s3 + 32 * p))
+                kr[nt][p] = seen(key) ? __ldg(reinterpret_cast<const uint4*>(Kc + (long long)key * a.s3 + 32 * p))
                                        : make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
@@ -648,8 +747,8 @@ __global__ void __launch_bounds__(DE_WARPS * 32, HD == 64 ? 4 : 3) attention_dec
                 const int key = j0 + 16 * kk + 2 * t + (u & 1) + 8 * (u >> 1);
 #pragma unroll
                 for (int p = 0; p < NV; ++p)
-                    vr[kk][u][p] = key < keys ? __ldg(reinterpret_cast<const uint4*>(Vc + (long long)key * a.s3 + 64 * p))
-                                              : make_uint4(0, 0, 0, 0);
+                    vr[kk][u][p] = seen(key) ? __ldg(reinterpret_cast<const uint4*>(Vc + (long long)key * a.s3 + 64 * p))
+                                             : make_uint4(0, 0, 0, 0);
             }
         float s[KB / 8][4];
         float cm[2] = {-INFINITY, -INFINITY};
@@ -663,7 +762,8 @@ __global__ void __launch_bounds__(DE_WARPS * 32, HD == 64 ? 4 : 3) attention_dec
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {  // e: row half e >> 1, key 2 t + (e & 1)
-                const bool in = j0 + 8 * nt + 2 * t + (e & 1) < vis[e >> 1];
+                const int key = j0 + 8 * nt + 2 * t + (e & 1);
+                const bool in = key < vis[e >> 1] && (!WIN || key < a.n_sink || key >= vis[e >> 1] - a.window);
                 cm[e >> 1] = in ? fmaxf(cm[e >> 1], s[nt][e]) : cm[e >> 1];
             }
         }
@@ -691,8 +791,10 @@ __global__ void __launch_bounds__(DE_WARPS * 32, HD == 64 ? 4 : 3) attention_dec
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int nt = 2 * kk + (q >> 1), h = q & 1, key = j0 + 8 * nt + 2 * t;
-                const float e0 = key < vis[h] ? at_exp2(fmaf(s[nt][2 * h], k2, moff[h])) : 0.f;
-                const float e1 = key + 1 < vis[h] ? at_exp2(fmaf(s[nt][2 * h + 1], k2, moff[h])) : 0.f;
+                const bool in0 = key < vis[h] && (!WIN || key < a.n_sink || key >= vis[h] - a.window);
+                const bool in1 = key + 1 < vis[h] && (!WIN || key + 1 < a.n_sink || key + 1 >= vis[h] - a.window);
+                const float e0 = in0 ? at_exp2(fmaf(s[nt][2 * h], k2, moff[h])) : 0.f;
+                const float e1 = in1 ? at_exp2(fmaf(s[nt][2 * h + 1], k2, moff[h])) : 0.f;
                 pa[q] = pack_bf16(e0, e1);
                 // the sum takes the probabilities the MMA sees
                 l[h] += __uint_as_float(pa[q] << 16) + __uint_as_float(pa[q] & 0xffff0000u);
@@ -773,28 +875,40 @@ __global__ void __launch_bounds__(DE_WARPS * 32, HD == 64 ? 4 : 3) attention_dec
             o0 = fmaf(f, ld_cluster_f32(sum + e, k), o0);
             o1 = fmaf(f, ld_cluster_f32(sum + e + 1, k), o1);
         }
-        const float inv = 1.f / lt;
-        bf16* out = static_cast<bf16*>(a.out) + (((size_t)c * a.n_q + (size_t)g * a.group + head) * a.Lq + tok) * HD + d;
-        *reinterpret_cast<uint32_t*>(out) = pack_bf16(o0 * inv, o1 * inv);
+        const float inv = WIN && lt == 0.f ? 0.f : 1.f / lt;
+        const size_t row = ((size_t)c * a.n_q + (size_t)g * a.group + head) * a.Lq + tok;
+        bf16* out = static_cast<bf16*>(a.out) + row * HD + d;
+        o0 *= inv;
+        o1 *= inv;
+        if constexpr (WIN) {
+            if (!isfinite(o0) || !isfinite(o1)) {
+                float w[2];
+                row_again<bf16, HD, 2, 1>(static_cast<const bf16*>(a.Q) + row * HD, static_cast<const bf16*>(a.K) + kv_off,
+                                          static_cast<const bf16*>(a.V) + kv_off, a.s3, a.n_mem + tok + 1, a, d, w);
+                o0 = w[0];
+                o1 = w[1];
+            }
+        }
+        *reinterpret_cast<uint32_t*>(out) = pack_bf16(o0, o1);
     }
     if (splits > 1) cluster_sync();  // no CTA leaves while another reads its shared memory
 }
 
-template <typename T, int HD>
+template <typename T, int HD, bool WIN>
 cudaError_t launch_t(const AttnArgs& a, int C, cudaStream_t st) {
     const size_t smem = AttnSmem<T, HD>::FLOATS * sizeof(float);
     static PerDevice<SmemOptIn> once;
-    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(attention_kernel<T, HD>), smem, once);
+    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(attention_kernel<T, HD, WIN>), smem, once);
     if (e != cudaSuccess) return e;
     dim3 grid((a.Lq + a.rows - 1) / a.rows, a.n_kv, C);
-    attention_kernel<T, HD><<<grid, ATT_WARPS * 32, smem, st>>>(a);
+    attention_kernel<T, HD, WIN><<<grid, ATT_WARPS * 32, smem, st>>>(a);
     return cudaGetLastError();
 }
 
-template <int HD>
+template <int HD, bool WIN>
 cudaError_t launch_prefill(AttnArgs a, int n_ctx, int C, cudaStream_t st) {
     static PerDevice<SmemOptIn> once;
-    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(attention_prefill_kernel<HD>), FaSmem<HD>::DYN, once);
+    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(attention_prefill_kernel<HD, WIN>), FaSmem<HD>::DYN, once);
     if (e != cudaSuccess) return e;
     // The maps of the last call's shape, of which a call only sets the addresses: three maps encoded anew are 0.5 us of
     // the 9 us that a short call takes on the host
@@ -816,31 +930,32 @@ cudaError_t launch_prefill(AttnArgs a, int n_ctx, int C, cudaStream_t st) {
         const uint32_t kb[5] = {64, FaSmem<HD>::NK, 1, 1, 1};
         plan.key[0] = 0;
         if (!encode_map_bf16_4d(&plan.q, a.Q, qd, qs, qb) || !encode_map_bf16_5d(&plan.kv, a.K, kd, ks, kb))
-            return launch_t<bf16, HD>(a, C, st);  // strides past a tensor map's range (2^40 bytes): the CUDA-core form
+            return launch_t<bf16, HD, WIN>(a, C, st);  // strides past a tensor map's range (2^40 bytes): the CUDA-core form
         std::copy(key, key + 10, plan.key);
     }
     CUtensorMap mq = plan.q, mk = plan.kv, mv = plan.kv;
     if (!retarget_map(&mq, a.Q) || !retarget_map(&mk, a.K) || !retarget_map(&mv, a.V)) return cudaErrorInvalidValue;
     a.rows = rows;
     dim3 grid((a.Lq + a.rows - 1) / a.rows, a.n_kv, C);
-    attention_prefill_kernel<HD><<<grid, FaSmem<HD>::THREADS, FaSmem<HD>::DYN, st>>>(mq, mk, mv, a);
+    attention_prefill_kernel<HD, WIN><<<grid, FaSmem<HD>::THREADS, FaSmem<HD>::DYN, st>>>(mq, mk, mv, a);
     return cudaGetLastError();
 }
 
-template <int HD>
+template <int HD, bool WIN>
 cudaError_t launch_decode(AttnArgs a, int C, int sms, cudaStream_t st) {
     a.tile_tok = 128 / a.group;
     a.per_block = (a.tile_tok * a.group + DE_ROWS - 1) / DE_ROWS;
     a.group_inv = 65536 / a.group + 1;
     static PerDevice<SmemOptIn> once;
     constexpr size_t smem = DeSmem<HD>::FLOATS * sizeof(float);
-    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(attention_decode_kernel<HD>), smem, once);
+    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(attention_decode_kernel<HD, WIN>), smem, once);
     if (e != cudaSuccess) return e;
     const int row_tiles = DeTile::count(a.group, a.Lq);
     // split the keys over a cluster until the grid fills the SMs' CTA slots, or a CTA's warps would
     // have no block of keys each
     const long long ctas = (long long)row_tiles * a.n_kv * C;
-    const int blocks = (a.n_mem + a.Lq + 31) / 32;
+    const long long all = (long long)a.n_mem + a.Lq;
+    const int blocks = (int)((WIN ? std::min(all, (long long)a.n_sink + a.window + std::min(a.Lq, a.tile_tok)) : all) + 31) / 32;
     const int slots = (HD == 64 ? 4 : 3) * sms;
     const int splits = (int)std::max(1ll, std::min({8ll, slots / ctas, (long long)blocks / DE_WARPS}));
     cudaLaunchConfig_t cfg = {};
@@ -855,7 +970,31 @@ cudaError_t launch_decode(AttnArgs a, int C, int sms, cudaStream_t st) {
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attention_decode_kernel<HD>, a, splits);
+    return cudaLaunchKernelEx(&cfg, attention_decode_kernel<HD, WIN>, a, splits);
+}
+
+template <bool WIN>
+cudaError_t launch(const DevState& s, AttnArgs a, int n_ctx, cudaStream_t st) {
+    const int C = n_ctx * a.L;
+    a.n_kv = s.n_kv;
+    a.group = a.n_q / s.n_kv;
+    a.rows = std::max(1, ATT_ITEMS / a.group);
+    a.scale = 1.0f / sqrtf((float)s.hd);
+    const long long el = s.dtype == 0 ? 4 : 2;
+    a.vec = ((reinterpret_cast<uintptr_t>(a.K) | reinterpret_cast<uintptr_t>(a.V)) & 15u) == 0 && (a.s0 * el) % 16 == 0 &&
+            (a.s1 * el) % 16 == 0 && (a.s2 * el) % 16 == 0 && (a.s3 * el) % 16 == 0;
+    a.status = s.status;
+    if (s.dtype == 0)
+        return s.hd == 64 ? launch_t<float, 64, WIN>(a, C, st) : launch_t<float, 128, WIN>(a, C, st);
+    // bf16 on the tensor cores when every row it stages is 16-byte aligned (the queries and the
+    // output are dense rows of hd elements); other cache layouts take the CUDA-core kernel
+    if (a.vec && ((reinterpret_cast<uintptr_t>(a.Q) | reinterpret_cast<uintptr_t>(a.out)) & 15u) == 0) {
+        const long long row_tiles = ((long long)a.group * a.Lq + DE_ROWS - 1) / DE_ROWS;
+        if (row_tiles == 1 || row_tiles * a.n_kv * C <= DE_MAX_TILES)
+            return s.hd == 64 ? launch_decode<64, WIN>(a, C, s.sms, st) : launch_decode<128, WIN>(a, C, s.sms, st);
+        return s.hd == 64 ? launch_prefill<64, WIN>(a, n_ctx, C, st) : launch_prefill<128, WIN>(a, n_ctx, C, st);
+    }
+    return s.hd == 64 ? launch_t<bf16, 64, WIN>(a, C, st) : launch_t<bf16, 128, WIN>(a, C, st);
 }
 
 }  // namespace
@@ -865,24 +1004,23 @@ cudaError_t launch_attention(const DevState& s, int n_layers, const void* Q, int
     AttnArgs a{};
     a.Q = Q; a.K = K; a.V = V; a.out = out;
     a.s0 = strides[0]; a.s1 = strides[1]; a.s2 = strides[2]; a.s3 = strides[3];
-    a.L = n_layers; a.n_q = n_q; a.n_kv = s.n_kv; a.group = n_q / s.n_kv; a.Lq = Lq; a.n_mem = n_mem;
-    a.rows = std::max(1, ATT_ITEMS / a.group);
-    a.scale = 1.0f / sqrtf((float)s.hd);
-    const long long el = s.dtype == 0 ? 4 : 2;
-    a.vec = ((reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) & 15u) == 0 && (a.s0 * el) % 16 == 0 &&
-            (a.s1 * el) % 16 == 0 && (a.s2 * el) % 16 == 0 && (a.s3 * el) % 16 == 0;
-    a.status = s.status;
-    if (s.dtype == 0)
-        return s.hd == 64 ? launch_t<float, 64>(a, s.C, st) : launch_t<float, 128>(a, s.C, st);
-    // bf16 on the tensor cores when every row it stages is 16-byte aligned (the queries and the
-    // output are dense rows of hd elements); other cache layouts take the CUDA-core kernel
-    if (a.vec && ((reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(out)) & 15u) == 0) {
-        const long long row_tiles = ((long long)a.group * Lq + DE_ROWS - 1) / DE_ROWS;
-        if (row_tiles == 1 || row_tiles * a.n_kv * s.C <= DE_MAX_TILES)
-            return s.hd == 64 ? launch_decode<64>(a, s.C, s.sms, st) : launch_decode<128>(a, s.C, s.sms, st);
-        return s.hd == 64 ? launch_prefill<64>(a, s.C / n_layers, s.C, st) : launch_prefill<128>(a, s.C / n_layers, s.C, st);
-    }
-    return s.hd == 64 ? launch_t<bf16, 64>(a, s.C, st) : launch_t<bf16, 128>(a, s.C, st);
+    a.L = n_layers; a.n_q = n_q; a.Lq = Lq; a.n_mem = n_mem;
+    return launch<false>(s, a, s.C / n_layers, st);
+}
+
+cudaError_t launch_window_attention(const DevState& s, int n_ctx, int n_layers, const void* Q, int n_q, int Lq, const void* K,
+                                    const void* V, const long long* strides, int n_past, int n_sink, int window, void* out,
+                                    cudaStream_t st) {
+    AttnArgs a{};
+    a.Q = Q; a.K = K; a.V = V; a.out = out;
+    a.s0 = strides[0]; a.s1 = strides[1]; a.s2 = strides[2]; a.s3 = strides[3];
+    a.L = n_layers; a.n_q = n_q; a.Lq = Lq; a.n_mem = n_past;
+    // no more than there is: what a window or a number of first positions past the last one adds is nothing
+    a.n_sink = std::min(n_sink, n_past + Lq);
+    a.window = std::min(window, n_past + Lq);
+    if (a.n_sink == 0 && a.window == 0)  // nobody sees anything
+        return cudaMemsetAsync(out, 0, (size_t)n_ctx * n_layers * n_q * Lq * s.hd * (s.dtype == 0 ? 4 : 2), st);
+    return launch<true>(s, a, n_ctx, st);
 }
 
 }  // namespace mone

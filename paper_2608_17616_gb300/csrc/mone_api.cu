@@ -19,7 +19,7 @@ using namespace mone;
 
 // Kernel kinds of the per-kernel timing (mone_mem_kernel_time).
 enum { K_PREPASS = 0, K_PHASE_A = 1, K_PHASE_B = 2, K_FINALIZE = 3, K_READ = 4, K_MSE = 5, K_ATTN = 6,
-       K_RESIDENT = 7, K_STAGE = 8, K_KINDS = 9 };
+       K_RESIDENT = 7, K_STAGE = 8, K_CACHE = 9, K_KINDS = 10 };
 
 // Optional per-kernel device timing (mone_mem_set_timing).
 struct KernelTiming {
@@ -112,6 +112,9 @@ struct mone_mem {
     size_t hwin_bytes;
     cudaStream_t hstream;
     cudaEvent_t hstart, hstaged[2], hfree[2];
+    // workspace of mone_cache_attention, grown on demand
+    void* cws;
+    size_t cws_bytes;
 };
 
 namespace {
@@ -216,6 +219,9 @@ void destroy_host_pipeline(mone_mem* m) {
 
 void destroy_streams(mone_mem* m) {
     destroy_host_pipeline(m);
+    if (m->cws) cudaFree(m->cws);
+    m->cws = nullptr;
+    m->cws_bytes = 0;
     if (m->rg) {
         if (m->rg->exec) cudaGraphExecDestroy(m->rg->exec);
         delete m->rg;
@@ -1004,6 +1010,121 @@ mone_status mone_attention(mone_mem* m, const void* Q, int n_q_heads, int Lq, co
     });
 }
 
+mone_status mone_window_attention(mone_mem* m, int layer, const void* Q, int n_q_heads, int Lq, const void* K, const void* V,
+                                  const long long kv_strides[4], int n_past, int n_sink, int window, void* out, void* stream) {
+    if (!is_live(m)) return MONE_ERR_INVALID_ARG;
+    const DevState& s = m->s;
+    if (layer != MONE_ALL_LAYERS && (layer < 0 || layer >= m->cfg.n_layers)) return MONE_ERR_INVALID_ARG;
+    if (!Q || !K || !V || !out || !kv_strides) return MONE_ERR_INVALID_ARG;
+    if (n_q_heads < s.n_kv || n_q_heads % s.n_kv || n_q_heads / s.n_kv > 64) return MONE_ERR_INVALID_ARG;
+    if (Lq < 1 || n_past < 0 || n_sink < 0 || window < 0 || (long long)n_past + Lq > (1ll << 20)) return MONE_ERR_INVALID_ARG;
+    for (int i = 0; i < 4; ++i)
+        if (kv_strides[i] < 0) return MONE_ERR_INVALID_ARG;
+    if (kv_strides[3] < s.hd) return MONE_ERR_INVALID_ARG;  // positions hold head_dim contiguous elements
+    const size_t el = elsize(s.dtype);
+    if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)out) % el) return MONE_ERR_INVALID_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const bool one = layer != MONE_ALL_LAYERS;
+    const size_t off = one ? (size_t)layer * kv_strides[1] * el : 0;
+    return timed(m, K_ATTN, st, 1, [&] {
+        return launch_window_attention(s, m->cfg.n_ctx, one ? 1 : m->cfg.n_layers, Q, n_q_heads, Lq, (const char*)K + off,
+                                       (const char*)V + off, kv_strides, n_past, n_sink, window, out, st);
+    });
+}
+
+// A cache and a layer argument, checked, as the kernels take them.
+static mone_status cache_view(const mone_mem* m, int layer, const mone_cache* c, CacheView* v) {
+    if (!is_live(m) || !c) return MONE_ERR_INVALID_ARG;
+    const DevState& s = m->s;
+    if (layer != MONE_ALL_LAYERS && (layer < 0 || layer >= m->cfg.n_layers)) return MONE_ERR_INVALID_ARG;
+    if (!c->K || !c->V || !aligned16(c->K) || !aligned16(c->V) || !c->table || !c->lens) return MONE_ERR_INVALID_ARG;
+    if (((uintptr_t)c->table | (uintptr_t)c->lens | (uintptr_t)c->score) & 3u) return MONE_ERR_INVALID_ARG;
+    if (c->n_pages < 1 || c->page_size < 1 || c->table_width < 1) return MONE_ERR_INVALID_ARG;
+    if ((c->page_size & (c->page_size - 1)) || c->page_size > 1024) return MONE_ERR_UNSUPPORTED_SHAPE;
+    for (int i = 0; i < 4; ++i)
+        if (c->strides[i] < 0) return MONE_ERR_INVALID_ARG;
+    // a page's positions hold head_dim elements each, and pages are apart
+    if ((c->page_size > 1 && c->strides[3] < s.hd) || (c->n_pages > 1 && c->strides[1] < s.hd)) return MONE_ERR_INVALID_ARG;
+    if ((long long)c->table_width * c->page_size > (1ll << 30)) return MONE_ERR_INVALID_ARG;
+    const bool one = layer != MONE_ALL_LAYERS;
+    const long long off = one ? layer : 0;
+    const size_t el = elsize(s.dtype);
+    v->K = (char*)c->K + off * c->strides[0] * el;
+    v->V = (char*)c->V + off * c->strides[0] * el;
+    v->s_layer = c->strides[0]; v->s_page = c->strides[1]; v->s_head = c->strides[2]; v->s_pos = c->strides[3];
+    v->n_pages = c->n_pages;
+    v->page_log2 = 0;
+    while ((1 << v->page_log2) < c->page_size) ++v->page_log2;
+    v->table = c->table;
+    v->width = c->table_width;
+    v->lens = c->lens;
+    v->cap = (long long)c->table_width * c->page_size;
+    v->score = c->score ? c->score + off * s.n_kv * v->cap : nullptr;
+    v->n_ctx = m->cfg.n_ctx;
+    v->L = one ? 1 : m->cfg.n_layers;
+    v->Lh = m->cfg.n_layers;
+    v->n_kv = s.n_kv;
+    v->status = s.status;
+    return MONE_OK;
+}
+
+mone_status mone_cache_append(mone_mem* m, int layer, const mone_cache* cache, const void* K, const void* V,
+                              const long long strides[4], int n_tok, const int* counts, int* lens_out, void* stream) {
+    CacheView v;
+    MONE_TRY(cache_view(m, layer, cache, &v));
+    const DevState& s = m->s;
+    if (!K || !V || !strides || n_tok < 1 || n_tok > (1 << 20)) return MONE_ERR_INVALID_ARG;
+    if (((uintptr_t)K | (uintptr_t)V) % elsize(s.dtype) || (((uintptr_t)counts | (uintptr_t)lens_out) & 3u)) return MONE_ERR_INVALID_ARG;
+    for (int i = 0; i < 4; ++i)
+        if (strides[i] < 0) return MONE_ERR_INVALID_ARG;
+    if (lens_out && lens_out == cache->lens) return MONE_ERR_INVALID_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    return timed(m, K_CACHE, st, 1, [&] { return launch_cache_append(s, v, K, V, strides, n_tok, counts, lens_out, st); });
+}
+
+mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache, const void* Q, int n_q_heads, int n_tok,
+                                 int n_sink, int window, void* out, void* stream) {
+    CacheView v;
+    MONE_TRY(cache_view(m, layer, cache, &v));
+    const DevState& s = m->s;
+    if (!Q || !out || !aligned16(Q) || !aligned16(out)) return MONE_ERR_INVALID_ARG;
+    if (n_q_heads < s.n_kv || n_q_heads % s.n_kv || n_q_heads / s.n_kv > 64) return MONE_ERR_INVALID_ARG;
+    if (n_tok < 1 || n_tok > 16 || n_sink < 0 || window < 0) return MONE_ERR_INVALID_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const size_t need = cache_attention_workspace(s, v, n_q_heads, n_tok);
+    if (need > m->cws_bytes) {
+        MONE_CUDA(cudaStreamSynchronize(st));
+        if (m->cws) cudaFree(m->cws);
+        m->cws = nullptr;
+        m->cws_bytes = 0;
+        char* p = nullptr;
+        MONE_TRY(dalloc(&p, need));
+        m->cws = p;
+        MONE_CUDA(cudaMemsetAsync(p, 0, kCacheCounters * sizeof(int), st));
+        m->cws_bytes = need;
+    }
+    return timed(m, K_CACHE, st, cache_attention_kernels(v), [&] {
+        return launch_cache_attention(s, v, Q, n_q_heads, n_tok, n_sink, window, out, m->cws, st);
+    });
+}
+
+mone_status mone_cache_evict(mone_mem* m, int layer, const mone_cache* cache, int keep, int n_sink, int n_recent,
+                             const int* to_table, int to_width, float* to_score, int* kept, int* lens_out, void* stream) {
+    CacheView v;
+    MONE_TRY(cache_view(m, layer, cache, &v));
+    const DevState& s = m->s;
+    if (!cache->score || !to_table || !to_score || !kept || to_width < 1) return MONE_ERR_INVALID_ARG;
+    if (((uintptr_t)to_table | (uintptr_t)to_score | (uintptr_t)kept | (uintptr_t)lens_out) & 3u) return MONE_ERR_INVALID_ARG;
+    if (keep < 1 || n_sink < 0 || n_recent < 0 || (long long)n_sink + n_recent > keep) return MONE_ERR_INVALID_ARG;
+    if ((long long)to_width * cache->page_size < keep || (long long)to_width * cache->page_size > (1ll << 30)) return MONE_ERR_INVALID_ARG;
+    if (to_table == cache->table || to_score == cache->score || (lens_out && lens_out == cache->lens)) return MONE_ERR_INVALID_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const size_t off = layer == MONE_ALL_LAYERS ? 0 : (size_t)layer * s.n_kv * to_width * cache->page_size;
+    return timed(m, K_CACHE, st, 2, [&] {
+        return launch_cache_evict(s, v, keep, n_sink, n_recent, to_table, to_width, to_score + off, kept, lens_out, st);
+    });
+}
+
 mone_status mone_mem_free(mone_mem* m) {
     {
         std::lock_guard<std::mutex> lk(g_live_mu);
@@ -1065,8 +1186,8 @@ mone_status mone_mem_sync(mone_mem* m, void* stream) {
     if (flag) MONE_CUDA(cudaMemset(m->s.status, 0, sizeof(word)));
     if (flag & DEV_CHECK) {
         static const char* const sites[] = {"?", "phase A tile", "phase B tile", "read tile", "resident rows",
-                                            "TMA x coordinate"};
-        const int site = word[1] >= 1 && word[1] <= 5 ? word[1] : 0;
+                                            "TMA x coordinate", "cache page number", "cache length"};
+        const int site = word[1] >= 1 && word[1] <= 7 ? word[1] : 0;
         std::snprintf(g_last_error, sizeof(g_last_error), "device index check failed: %s", sites[site]);
         return MONE_ERR_CHECK;
     }

@@ -18,7 +18,9 @@ enum : int { DEV_TIMEOUT = 1, DEV_NONFINITE = 2, DEV_CHECK = 4 };
 // Sites of the device-side index checks of a MONE_DEBUG build; the first failing site is kept
 // in status[1] (the word after the status flags) and named by mone_mem_sync's error text.
 enum : int { DS_PHASE_A_TILE = 1, DS_PHASE_B_TILE = 2, DS_READ_TILE = 3, DS_RESIDENT_ROWS = 4,
-             DS_TMA_X = 5 };
+             DS_TMA_X = 5,
+             // the cache operators check these in every build: they come from device memory
+             DS_CACHE_PAGE = 6, DS_CACHE_LEN = 7 };
 
 // Device-resident state of all chains (see mone_mem_init).
 struct TcDevice;  // what the tensor-core launches need to know of a device
@@ -188,6 +190,38 @@ int stage_sms();
 // ---- kernels in attention.cu
 cudaError_t launch_attention(const DevState& s, int n_layers, const void* Q, int n_q, int Lq, const void* K,
                              const void* V, const long long* strides, int n_mem, void* out, cudaStream_t st);
+// The windowed form over n_ctx x n_layers chains (all layers, or one: K, V then point at it).
+cudaError_t launch_window_attention(const DevState& s, int n_ctx, int n_layers, const void* Q, int n_q, int Lq, const void* K,
+                                    const void* V, const long long* strides, int n_past, int n_sink, int window, void* out,
+                                    cudaStream_t st);
+
+// ---- kernels in cache.cu and cache_attention.cu (paged cache)
+// A mone_cache as the kernels take it, with the contexts and layers of the call: chain c = context * L + l is layer
+// layer0 + l of its context, and chain c of what the call's other arrays hold.
+struct CacheView {
+    void *K, *V;                           // pools of the call's first layer
+    long long s_layer, s_page, s_head, s_pos;
+    int n_pages, page_log2;
+    const int* table;                      // [n_ctx][width]
+    int width;
+    const int* lens;                       // [n_ctx]
+    float* score;                          // [n_ctx][Lh][n_kv][cap], at the call's first layer
+    long long cap;                         // positions a context's table covers
+    int n_ctx, L, Lh, n_kv;                // contexts, layers of the call, layers of the handle, KV heads
+    int* status;
+};
+cudaError_t launch_cache_append(const DevState& s, const CacheView& v, const void* K, const void* V, const long long* strides,
+                                int n_tok, const int* counts, int* lens_out, cudaStream_t st);
+cudaError_t launch_cache_evict(const DevState& s, const CacheView& v, int keep, int n_sink, int n_recent, const int* to, int to_width,
+                               float* to_score, int* kept, int* lens_out, cudaStream_t st);
+// Workspace of launch_cache_attention in bytes for this call, and the call.  It begins with kCacheCounters ints that are
+// zero where it is allocated and that the kernels leave at zero.
+constexpr int kCacheCounters = 4096;
+size_t cache_attention_workspace(const DevState& s, const CacheView& v, int n_q, int n_tok);
+cudaError_t launch_cache_attention(const DevState& s, const CacheView& v, const void* Q, int n_q, int n_tok, int n_sink, int window,
+                                   void* out, void* ws, cudaStream_t st);
+// Kernels of one launch_cache_attention.
+inline int cache_attention_kernels(const CacheView& v) { return v.score ? 2 : 1; }
 
 // ---- kernels in ttl_tc.cu (bf16 tcgen05 path)
 struct TcMaps {

@@ -1,0 +1,191 @@
+"""GPU parity of the windowed attention against the oracle's definition in 64 bits, in each of its forms: many rows on the
+tensor cores (128-row tiles, chunks of 96 keys, 64 at hd 128), few rows (16-row tiles, the keys split), and the CUDA cores
+(fp32, and bf16 rows that are not aligned).
+
+Tolerances (relative 2-norm).  bf16 5e-3: probabilities and outputs are rounded to 8 bits once each, at most 2^-9 of
+themselves and 2^-9 / sqrt(3) in the mean, 1.6e-3 together, times three.  fp32 1e-5: the score of a key is a sum of up to
+128 products in 32 bits, off by about 2^-24 sqrt(128) |z| with |z| up to 15.
+"""
+import pytest
+import torch
+
+import oracle as O
+import paper_2608_17616_gb300 as mone
+import workloads as wk
+from harness import DeviceRun, record, rel_fro
+
+pytestmark = pytest.mark.gpu
+ALL = 1 << 30
+TOL = {torch.bfloat16: 5e-3, torch.float32: 1e-5}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    from paper_2608_17616_gb300 import build
+    build.build()
+    assert torch.cuda.is_available()
+    mone.lib()
+
+
+def handle(n_layers, n_kv, hd, dtype, n_ctx=1):
+    return DeviceRun(wk.Workload("window", 51, n_ctx, n_layers, 256, 256, 2 * n_kv * hd, n_kv, hd, 128, 128, 8,
+                                 "f32" if dtype is torch.float32 else "bf16", wk.PLAIN))
+
+
+def case(group, Lq, n_past, n_sink, window, hd=64, n_layers=2, dtype=torch.bfloat16, pad=0, layer=-1, n_ctx=1, late=1.0, kind=None):
+    n_kv = 2
+    run = handle(n_layers, n_kv, hd, dtype, n_ctx)
+    g = torch.Generator(device="cuda").manual_seed(group * 1000 + Lq + n_past + window % 97)
+    rn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    S = n_past + Lq
+    K, V = (rn(n_ctx, n_layers, n_kv, S + 5, hd + pad) for _ in range(2))  # spare rows that nobody may read
+    K[..., 2 * S // 3:, :] *= late
+    K[..., S:, :], V[..., S:, :] = float("nan"), float("nan")
+    K, V = (x.to(dtype)[..., :hd] for x in (K, V))
+    if kind == "heads inner":
+        K, V = (x.transpose(2, 3).contiguous().transpose(2, 3) for x in (K, V))
+    layers = list(range(n_layers)) if layer < 0 else [layer]
+    Q = rn(n_ctx, len(layers), group * n_kv, Lq, hd).to(dtype)
+    out = torch.full_like(Q, 7.0)
+    mone.mone_window_attention(run.h, layer, Q, group * n_kv, Lq, K, V, K.stride()[:4], n_past, n_sink, window, out)
+    mone.mone_mem_sync(run.h)
+    run.close()
+    for c in sorted({0, n_ctx - 1}):
+        for a in sorted({0, len(layers) - 1}):
+            ref, _ = O.window_attention(Q[c, a].float().cpu(), K[c, layers[a], :, :S].float().cpu(), V[c, layers[a], :, :S].float().cpu(),
+                                        n_past, n_sink, window)
+            got = out[c, a].float().cpu()
+            if not ref.any():
+                assert not got.any()
+            else:
+                assert record("window attention", f"out {str(dtype)[6:]}", rel_fro(got, ref), TOL[dtype]) <= TOL[dtype], (c, a)
+
+
+MANY = [  # rows past the few-rows form: 20 layers x 2 KV heads
+    (4, 200, 70, 64, 40, 64),      # first positions, then a gap that grows along the tile
+    (4, 200, 70, 0, 40, 64),       # a window alone
+    (4, 200, 70, 0, ALL, 64),      # everything
+    (1, 300, 0, 0, 1, 64),         # a window of one
+    (1, 300, 0, 4, 1, 64),
+    (1, 300, 513, 100, 96, 64),    # a window of a chunk, first positions past a chunk
+    (2, 133, 1000, 96, 192, 64),   # whole chunks exactly
+    (2, 133, 1000, 97, 193, 64),   # one past
+    (2, 133, 1000, 5000, 7, 64),   # more first positions than there are
+    (2, 133, 100, 150, 30, 64),    # first positions that reach into the prompt
+    (64, 3, 94, 10, 20, 64),       # the most heads a KV head has
+    (3, 150, 0, 2, 64, 128),       # padded rows
+    (4, 129, 383, 64, 64, 128),
+    (4, 129, 383, 65, 129, 128),
+    (2, 140, 200, 9, 0, 128),      # first positions alone
+    (5, 77, 20, 0, 0, 64),         # nothing to see
+]
+
+
+@pytest.mark.parametrize("group,Lq,n_past,n_sink,window,hd", MANY)
+def test_many_rows(group, Lq, n_past, n_sink, window, hd):
+    case(group, Lq, n_past, n_sink, window, hd, n_layers=20)
+
+
+@pytest.mark.parametrize("group,Lq,n_past,n_sink,window,hd", MANY)
+@pytest.mark.parametrize("dtype,pad", [(torch.float32, 0), (torch.float32, 1), (torch.bfloat16, 4)])
+def test_cuda_cores(group, Lq, n_past, n_sink, window, hd, dtype, pad):
+    case(group, Lq, n_past, n_sink, window, hd, n_layers=2, dtype=dtype, pad=pad)
+
+
+@pytest.mark.parametrize("group,Lq,n_past,n_sink,window,hd", [
+    (1, 1, 0, 0, 1, 64),
+    (1, 1, 0, 1, 0, 64),
+    (4, 1, 31, 0, 32, 64),
+    (4, 1, 32, 0, 32, 64),
+    (4, 1, 500, 4, 100, 64),
+    (7, 2, 5000, 64, 1000, 64),
+    (8, 3, 700, 33, 40, 64),
+    (16, 32, 100, 20, 30, 64),     # 32 row tiles of two heads
+    (4, 1, 15, 3, 5, 128),
+    (5, 5, 3000, 100, 200, 128),
+    (5, 5, 3000, 0, ALL, 128),
+    (1, 90, 50, 7, 3, 64),         # row tiles of 16 tokens with windows of 3
+])
+def test_few_rows(group, Lq, n_past, n_sink, window, hd):
+    case(group, Lq, n_past, n_sink, window, hd, n_layers=1, late=3.0)
+
+
+def test_the_row_max_grows_late():
+    case(4, 100, 300, 16, 250, n_layers=20, late=9.0)
+    case(2, 140, 200, 16, 250, hd=128, n_layers=20, late=9.0)
+
+
+@pytest.mark.parametrize("layer", [0, 7, 19])
+def test_one_layer_of_a_cache(layer):
+    case(4, 400, 70, 64, 40, n_layers=20, layer=layer, n_ctx=3)
+
+
+@pytest.mark.parametrize("Lq", [1, 150])
+def test_heads_inside_the_positions(Lq):
+    case(4, Lq, 70, 64, 40, n_layers=20, n_ctx=2, kind="heads inner")
+
+
+@pytest.mark.parametrize("group,Lq,n_past,hd,n_layers,dtype,pad", [
+    (4, 200, 70, 64, 20, torch.bfloat16, 0),     # many rows
+    (3, 150, 0, 128, 20, torch.bfloat16, 0),
+    (4, 20, 300, 64, 1, torch.bfloat16, 0),      # few rows
+    (3, 50, 70, 64, 2, torch.float32, 0),        # CUDA cores
+    (3, 50, 70, 64, 2, torch.bfloat16, 4),
+])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_non_finite_values_reach_only_the_tokens_that_see_them(group, Lq, n_past, hd, n_layers, dtype, pad, bad):
+    n_kv, n_sink, window = 2, 2, 30
+    run = handle(n_layers, n_kv, hd, dtype)
+    g = torch.Generator(device="cuda").manual_seed(Lq)
+    rn = lambda *s: torch.randn(*s, generator=g, device="cuda").to(dtype)  # noqa: E731
+    S = n_past + Lq
+    K, V = (rn(1, n_layers, n_kv, S, hd + pad)[..., :hd] for _ in range(2))
+    Q = rn(1, n_layers, group * n_kv, Lq, hd)
+    V[..., n_past + Lq // 2, :] = bad
+    K[..., S - 1, ::2] = bad
+    V[..., S - 1, :] = bad
+    out = torch.full_like(Q, 7.0)
+    mone.mone_window_attention(run.h, -1, Q, group * n_kv, Lq, K, V, K.stride()[:4], n_past, n_sink, window, out)
+    mone.mone_mem_sync(run.h)
+    run.close()
+    ok = torch.ones(Lq, dtype=torch.bool)
+    ok[Lq // 2:Lq // 2 + window] = False
+    ok[-1] = False
+    for layer in {0, n_layers - 1}:
+        ref, _ = O.window_attention(Q[0, layer, :, :-1].float().cpu(), K[0, layer, :, :-1].float().cpu(), V[0, layer, :, :-1].float().cpu(),
+                                    n_past, n_sink, window)
+        got = out[0, layer].float().cpu()
+        assert not got[:, ~ok].isfinite().any()
+        assert rel_fro(got[:, :-1][:, ok[:-1]], ref[:, ok[:-1].numpy()]) <= TOL[dtype]
+
+
+def test_keys_at_minus_infinity_count_for_nothing():
+    for L, Lq in ((20, 150), (1, 4)):
+        run = handle(L, 2, 64, torch.bfloat16)
+        g = torch.Generator(device="cuda").manual_seed(Lq)
+        rn = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+        n_past = 200
+        K, V, Q = rn(1, L, 2, n_past + Lq, 64), rn(1, L, 2, n_past + Lq, 64), rn(1, L, 4, Lq, 64)
+        K[..., 0] = 0
+        K[..., :n_past, 0] = -1e25
+        Q[..., 0] = 1e25
+        out = torch.full_like(Q, 7.0)
+        mone.mone_window_attention(run.h, -1, Q, 4, Lq, K, V, K.stride()[:4], n_past, 50, 100, out)
+        mone.mone_mem_sync(run.h)
+        run.close()
+        ref, _ = O.window_attention(Q[0, 0].float().cpu(), K[0, 0].float().cpu(), V[0, 0].float().cpu(), n_past, 50, 100)
+        assert rel_fro(out[0, 0].float().cpu(), ref) <= 5e-3
+
+
+def test_many_tiles_repeat_bit_for_bit():
+    n_kv, group, hd, Lq, n_past, L = 8, 4, 128, 400, 64, 16
+    run = handle(L, n_kv, hd, torch.bfloat16)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    K, V = (torch.randn(1, L, n_kv, n_past + Lq, hd, generator=g, device="cuda").bfloat16() for _ in range(2))
+    Q = torch.randn(1, L, group * n_kv, Lq, hd, generator=g, device="cuda").bfloat16()
+    outs = [torch.full_like(Q, 7.0) for _ in range(2)]
+    for i in range(40):
+        mone.mone_window_attention(run.h, -1, Q, group * n_kv, Lq, K, V, K.stride()[:4], n_past, 64, 100, outs[i % 2])
+    mone.mone_mem_sync(run.h)
+    run.close()
+    assert torch.equal(*outs)
