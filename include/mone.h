@@ -356,7 +356,9 @@ mone_status mone_cache_append(mone_mem* m, int layer, const mone_cache* cache, c
  *   Q, out  [n_ctx][n_layers][n_q_heads][n_tok][head_dim], dense, the handle's dtype
  * With cache->score, the weight of every position is added to it, summed over the query heads of its KV head and the
  * tokens (for mone_cache_evict).  The sums are in fixed order: equal calls give equal bits.
- * Constraints: n_q_heads a multiple of n_kv_heads, n_q_heads / n_kv_heads <= 64; 1 <= n_tok <= 16; n_sink, window >= 0.
+ * Constraints: n_q_heads a multiple of n_kv_heads, n_q_heads / n_kv_heads <= 64; 1 <= n_tok <= 16; n_sink, window >= 0;
+ * KV heads x contexts x layers of the call x ceil(n_tok n_q_heads / (4 n_kv_heads)) x blocks of 32 positions that a
+ * table covers below 2^30.
  * The handle keeps a workspace that grows with the call's sizes (growing synchronises the stream, so a call of the
  * largest size comes before any capture); calls of one handle that overlap on two streams share it: order them.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (page_size), OOM, CUDA.

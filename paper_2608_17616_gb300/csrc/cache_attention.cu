@@ -2,14 +2,15 @@
 // positions are given by it.
 //
 // Every context's visible positions are cut into blocks of 32, and the blocks of all (context, layer, KV head, row tile)
-// items, one item after the other, are dealt out evenly to a grid that fills the GPU once: however unequal the contexts
-// are, every CTA reads as much as any other, and nothing of it has to be known on the host.  A CTA's warps take an item's
-// blocks in turn, each with a softmax of its own, and meet in shared memory.  An item that one CTA has whole is
-// written at once; the parts of others go to the workspace, and the CTA that finishes an item's last part joins
-// them in order, so the result does not depend on who comes last.
+// items, one item after the other, are dealt out evenly to the CTAs of a grid that fills the GPU once, and those of a CTA
+// to its warps: however unequal the contexts are, every warp reads as much as any other, and nothing of it has to be known on
+// the host.  A warp works alone to the end of its share: it keeps an item's softmax and output in registers, and writes the
+// rows of an item that it has whole.  Of the others it leaves parts (max, sums and unnormalised output), which the CTA joins
+// when its warps are done, to the item's rows if it has the item whole, else to a part that the second kernel
+// joins.  Parts are joined in order, so equal calls give equal bits.
 //
-// For the weights the scores go to the workspace as well, and a second kernel turns them into exp(z - max) / sum,
-// summed over the rows of a KV head: 4 bytes a row and position beside the 4 head_dim (bf16) of its key and value.
+// For the weights the scores go to the workspace as well (4 bytes a row and position beside the 4 head_dim, in bf16, of its
+// key and value), and the second kernel adds exp(z - max) / sum over the rows of a KV head.
 #include <algorithm>
 #include <climits>
 
@@ -22,20 +23,22 @@ namespace {
 
 constexpr int CA_WARPS = 4, CA_THREADS = CA_WARPS * 32;
 constexpr int KB = 32;         // positions of a block
-constexpr int CA_CTAS = 4;     // CTAs an SM at most
-constexpr int CA_WHOLE = 8;    // items of up to so many blocks are not split
+constexpr int CA_WHOLE = 16;   // items of up to so many blocks are not split over CTAs
+constexpr int CA_SHARE = 4;    // blocks of a CTA, at least
+constexpr int CA_SM_ROWS = 32; // rows of an SM's CTAs, at most
+constexpr int FIN_ROWS = 64;   // rows whose weights are added at a time
 
 struct CaArgs {
     CacheView v;
     const void* Q;             // [chains][n_q][n_tok][hd]: the rows (head of the group, token) of a KV head are contiguous
     void* out;
     int n_tok, R, RT, n_sink, window;  // rows and row tiles of a KV head
-    long long per;             // items of a context
+    int per;                   // items of a context
     int vec;                   // 16-byte aligned rows
     float scale;
-    int* count;                // [grid] parts done of the item that is split from this CTA on; zero between calls
-    float* part;               // [2 grid][ROWS][hd + 3]
-    float* lse;                // [chains][n_kv][R] log2 of the sum of exp, with the weights
+    int ctas;                  // that the blocks are dealt out to
+    float* part;               // [ctas + 4 ctas][2][ROWS][hd + 3]: the CTAs' parts, and those that their warps put here
+    float* lse;                // [chains][n_kv][R] log2 of the sum of exp of items that one CTA has whole, with the weights
     float* z2;                 // [chains][n_kv][R][pitch] scores in base 2, -inf where not seen
     long long pitch;
 };
@@ -62,51 +65,109 @@ struct CaRange {
     __device__ int units() const { return max(nb, 1); }  // an item without a block still writes its zeros
 };
 
-// The share of a CTA: units [begin, end), from unit `at0` of context `c` on
-struct CaShare {
-    long long share, begin, end, ctx0;  // ctx0: first unit of context c
-    int c;
-    // where unit u lies: the first unit of its context, and the context
-    static __device__ void locate(const CaArgs& a, long long u, long long& base, int& c) {
+// How the units of all items, one item after the other, are dealt out: `share` to each CTA.  A boundary within an item of
+// up to CA_WHOLE units moves to the item's start.
+struct CaDeal {
+    int total, share;
+    int mine, incl;  // units of context c0 + lane and those up to it, of the contexts scanned last
+    __device__ CaDeal(const CaArgs& a) {
+        total = 0;
+        for (int c0 = 0; c0 < a.v.n_ctx; c0 += 32) total = scan(a, c0, total);
+        share = max((total + a.ctas - 1) / a.ctas, CA_SHARE);
+    }
+    // with `before` units ahead of them; returns the units up to the last
+    __device__ int scan(const CaArgs& a, int c0, int before) {
         const int lane = threadIdx.x & 31;
-        base = 0;
-        for (int c0 = 0;; c0 += 32) {
-            const long long mine = c0 + lane < a.v.n_ctx ? CaRange(a, c0 + lane).units() * a.per : 0;
-            long long incl = mine;
+        mine = c0 + lane < a.v.n_ctx ? CaRange(a, c0 + lane).units() * a.per : 0;
+        incl = mine;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long up = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += up;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += up;
+        }
+        incl += before;
+        return __shfl_sync(0xffffffffu, incl, 31);
+    }
+    // where unit u < total lies: its context and the context's first unit; returns the units of its items
+    __device__ int locate(const CaArgs& a, int u, int& base, int& c) {
+        int c0 = 0;
+        if (a.v.n_ctx > 32)
+            for (int before = scan(a, 0, 0); before <= u; before = scan(a, c0, before)) c0 += 32;
+        const int k = __ffs(__ballot_sync(0xffffffffu, incl > u)) - 1;
+        c = c0 + k;
+        base = __shfl_sync(0xffffffffu, incl - mine, k);
+        return __shfl_sync(0xffffffffu, mine, k) / a.per;
+    }
+    // the first unit of context c
+    __device__ int first_unit(const CaArgs& a, int c) {
+        if (a.v.n_ctx > 32) {
+            int before = 0;
+            for (int c0 = 0;; c0 += 32) {
+                const int up_to = scan(a, c0, before);
+                if (c < c0 + 32) break;
+                before = up_to;
             }
-            const uint32_t past = __ballot_sync(0xffffffffu, base + incl > u);
-            if (past || c0 + 32 >= a.v.n_ctx) {
-                const int k = past ? __ffs(past) - 1 : 31;
-                c = c0 + k;
-                base += __shfl_sync(0xffffffffu, incl - mine, k);
-                return;
-            }
-            base += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        return __shfl_sync(0xffffffffu, incl - mine, c & 31);
+    }
+    // the first unit of CTA w
+    __device__ int start(const CaArgs& a, int w) {
+        const long long at = (long long)w * share;
+        if (at >= total) return total;
+        int base, c;
+        const int u = (int)at, units = locate(a, u, base, c);
+        return units <= CA_WHOLE ? base + (u - base) / units * units : u;
+    }
+    // the parts of the item of units [u, u + units): from CTA `first`, 1 where it stays whole
+    __device__ int parts(int u, int units, int& first) const {
+        first = u / share;
+        return units <= CA_WHOLE ? 1 : (u + units - 1) / share - first + 1;
+    }
+};
+
+// The pieces of a warp, one after the other: blocks [b0, b1) of an item
+struct CaWalk {
+    int u, end, ctx0, c, units;
+    CaRange r;
+    int l, g, rt, b0, b1;
+    bool whole, cta_whole;    // the warp has the item whole, the CTA has
+    bool first, last;         // the item begins in the CTA's share; the warp's last piece
+    int cta0, cta1;           // the CTA's units
+    __device__ CaWalk(const CaArgs& a) {
+        CaDeal deal(a);
+        cta0 = deal.start(a, blockIdx.x);
+        cta1 = deal.start(a, blockIdx.x + 1);
+        const int warp = threadIdx.x >> 5, n = cta1 - cta0;
+        u = cta0 + (int)((long long)n * warp / CA_WARPS);
+        end = cta0 + (int)((long long)n * (warp + 1) / CA_WARPS);
+        if (u < end) {
+            units = deal.locate(a, u, ctx0, c);
+            r = CaRange(a, c);
         }
     }
-    // a boundary between CTAs: in an item that stays whole, its start
-    static __device__ long long snap(const CaArgs& a, long long u, long long total) {
-        if (u >= total) return total;
-        long long base;
-        int c;
-        locate(a, u, base, c);
-        const int un = CaRange(a, c).units();
-        return un <= CA_WHOLE ? base + (u - base) / un * un : u;
+    __device__ bool next(const CaArgs& a) {
+        if (u >= end) return false;
+        while (u - ctx0 >= units * a.per) {
+            ctx0 += units * a.per;
+            r = CaRange(a, ++c);
+            units = r.units();
+        }
+        const int in_ctx = (u - ctx0) / units, lg = in_ctx / a.RT;
+        b0 = u - ctx0 - in_ctx * units;
+        const int e = min(units, b0 + end - u);
+        whole = b0 == 0 && e == units;
+        cta_whole = u - b0 >= cta0 && u - b0 + units <= cta1;
+        first = u - b0 >= cta0;
+        b1 = min(e, r.nb);
+        u += e - b0;
+        last = u >= end;
+        rt = in_ctx - lg * a.RT;
+        l = lg / a.v.n_kv;
+        g = lg - l * a.v.n_kv;
+        return true;
     }
-    __device__ CaShare(const CaArgs& a) {
-        long long total = 0;
-        for (int c0 = threadIdx.x & 31; c0 < a.v.n_ctx; c0 += 32) total += CaRange(a, c0).units() * a.per;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-        share = max((total + gridDim.x - 1) / gridDim.x, (long long)CA_WARPS);
-        begin = snap(a, share * blockIdx.x, total);
-        end = snap(a, share * (blockIdx.x + 1), total);
-        if (begin < end) locate(a, begin, ctx0, c);
-    }
+    // index of its KV head's rows, in units of R
+    __device__ size_t kv(const CaArgs& a) const { return ((size_t)c * a.v.L + l) * a.v.n_kv + g; }
 };
 
 // A row of Q over the positions it sees and no others, by one thread: dimensions d0, d0 + 1.  A block's products take a
@@ -142,115 +203,110 @@ template <> __device__ __forceinline__ void store2<float>(float* p, float x, flo
 template <> __device__ __forceinline__ void store2<bf16>(bf16* p, float x, float y) { *reinterpret_cast<uint32_t*>(p) = pack_bf16(x, y); }
 
 // A part of an item: O [ROWS][HD], then per row the max (of raw scores), the sum that goes with O, and the sum of the
-// probabilities before their rounding (for the weights).
+// probabilities before their rounding (for the weights).  A CTA has two that are not whole, one of the item that it begins
+// with in the middle, one of the item that it ends with before its end; a warp the same.
 template <int HD, int ROWS>
 struct Part {
-    static constexpr int FLOATS = ROWS * (HD + 3);
+    static constexpr int FLOATS = ROWS * (HD + 3), M = ROWS * HD, L = M + ROWS, LX = L + ROWS;
+    static __device__ float* of_cta(const CaArgs& a, int cta, bool first) { return a.part + (2ll * cta + first) * FLOATS; }
+    // of a warp of this CTA
+    static __device__ float* of_warp(const CaArgs& a, bool first) {
+        return a.part + (2ll * (a.ctas + blockIdx.x * CA_WARPS + (threadIdx.x >> 5)) + first) * FLOATS;
+    }
 };
 
-// An item's rows in the workspace or, joined from `n` parts, in `out`: read(k, i) is element i of part k.
-template <typename T, int HD, int ROWS, typename Read>
-__device__ __forceinline__ void finish_rows(const CaArgs& a, int n, Read&& read, float* to_part, int rows, float k2, int c, size_t kv, int row0,
-                                            const CaRange& r, const T* Kp, const T* Vp) {
-    constexpr int ST = ROWS * HD;
-    for (int e = 2 * threadIdx.x; e < rows * HD; e += 2 * CA_THREADS) {
-        const int row = e / HD, d = e - row * HD;
-        float mx = -INFINITY, l = 0.f, lx = 0.f, o0 = 0.f, o1 = 0.f;
-        for (int k = 0; k < n; ++k) mx = fmaxf(mx, read(k, ST + row));
-#pragma unroll 4
-        for (int k = 0; k < n; ++k) {
-            const float mk = read(k, ST + row);
-            const float f = mk == -INFINITY ? 0.f : ca_exp2((mk - mx) * k2);
-            l = fmaf(f, read(k, ST + ROWS + row), l);
-            lx = fmaf(f, read(k, ST + 2 * ROWS + row), lx);
-            o0 = fmaf(f, read(k, e), o0);
-            o1 = fmaf(f, read(k, e + 1), o1);
-        }
-        if (to_part) {
-            __stcg(reinterpret_cast<float2*>(to_part + e), make_float2(o0, o1));
-            if (d == 0) {
-                __stcg(to_part + ST + row, mx);
-                __stcg(to_part + ST + ROWS + row, l);
-                __stcg(to_part + ST + 2 * ROWS + row, lx);
-            }
-            continue;
-        }
-        const float inv = l == 0.f ? 0.f : 1.f / l;  // no key that counts: 0
-        o0 *= inv;
-        o1 *= inv;
-        const size_t at = kv * a.R + row0 + row;
-        if (a.n_tok > 1 && (!isfinite(o0) || !isfinite(o1))) {
-            float w[2];
-            row_again<T, HD>(a, static_cast<const T*>(a.Q) + at * HD, Kp, Vp, a.v.table + (size_t)c * a.v.width,
-                             r.n - a.n_tok + (row0 + row) % a.n_tok + 1, d, w);
-            o0 = w[0];
-            o1 = w[1];
-        }
-        store2<T>(static_cast<T*>(a.out) + at * HD + d, o0, o1);
-        if (d == 0 && a.lse) a.lse[at] = l == 0.f ? INFINITY : fmaf(mx, k2, log2f(lx));
+// What a warp says of its parts, in the order of their blocks: the piece it begins with, the piece it ends with
+struct CaNote {
+    const float* part;  // null: no such part
+    int c, l, g, rt, n, first, whole;  // the item; positions held; whether the CTA has its first part, all of them
+};
+
+// Dimensions d, d + 1 of a row from its O and sum.  (The pools' pointers are their layer's and head's.)
+template <typename T, int HD>
+__device__ __forceinline__ void write_row(const CaArgs& a, size_t kv, int c, int n, int row, int d, const T* K, const T* V, float o0,
+                                          float o1, float l) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;  // no key that counts: 0
+    o0 *= inv;
+    o1 *= inv;
+    const size_t at = kv * a.R + row;
+    if (a.n_tok > 1 && (!isfinite(o0) || !isfinite(o1))) {
+        float w[2];
+        row_again<T, HD>(a, static_cast<const T*>(a.Q) + at * HD, K, V, a.v.table + (size_t)c * a.v.width, n - a.n_tok + row % a.n_tok + 1, d, w);
+        o0 = w[0];
+        o1 = w[1];
     }
+    store2<T>(static_cast<T*>(a.out) + at * HD + d, o0, o1);
 }
 
-// One CTA's share of the work; Form::piece computes blocks [b0, b1) of an item into the warps' parts.
+// log2 of the sum of exp of a row, +inf where nothing counts (its weights are then 0)
+__device__ __forceinline__ float row_lse(float m, float lx, float k2) { return lx == 0.f ? INFINITY : fmaf(m, k2, log2f(lx)); }
+
 template <typename Form>
 __global__ void __launch_bounds__(CA_THREADS, Form::CTAS)
 cache_attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const CaArgs a) {
     using T = typename Form::T;
-    constexpr int HD = Form::HD, ROWS = Form::ROWS, PART = Form::WARP_BYTES / 4;
+    constexpr int HD = Form::HD, ROWS = Form::ROWS;
+    using P = Part<HD, ROWS>;
     extern __shared__ uint8_t ca_raw[];
-    float* ca_smem = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(ca_raw) + 1023) & ~uintptr_t(1023));
-    __shared__ int last;
-    const CaShare sh(a);
-    if (sh.begin >= sh.end) return;
-    Form form(tmK, tmV, a, ca_smem + (threadIdx.x >> 5) * PART);
+    __shared__ CaNote notes[2 * CA_WARPS];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ca_raw) + 1023) & ~uintptr_t(1023));
+    pdl_trigger();  // the second kernel waits for the end of this one
+    const int warp = threadIdx.x >> 5;
+    if ((threadIdx.x & 31) < 2) notes[2 * warp + (threadIdx.x & 31)].part = nullptr;
+    __syncwarp();
+    {
+        Form form(tmK, tmV, smem + warp * Form::WARP_BYTES);
+        form.run(a, notes + 2 * warp);
+    }
+    __syncthreads();
+    // the warps' parts, item by item
     const float k2 = a.scale * 1.4426950408889634f;
-    long long u = sh.begin, ctx0 = sh.ctx0;
-    int c = sh.c;
-    CaRange r(a, c);
-    while (u < sh.end) {
-        const int units = r.units();
-        if (u - ctx0 >= units * a.per) {
-            ctx0 += units * a.per;
-            r = CaRange(a, ++c);
+    for (int i = 0; i < 2 * CA_WARPS;) {
+        const CaNote it = notes[i];
+        if (!it.part) {
+            ++i;
             continue;
         }
-        const long long in_ctx = (u - ctx0) / units, item0 = ctx0 + in_ctx * units;
-        const int b0 = (int)(u - item0), b1 = (int)min((long long)units, b0 + sh.end - u);
-        const int rt = (int)(in_ctx % a.RT);
-        const int lg = (int)(in_ctx / a.RT), l = lg / a.v.n_kv, g = lg - l * a.v.n_kv;
-        const size_t kv = ((size_t)c * a.v.L + l) * a.v.n_kv + g;
-        const int row0 = rt * ROWS, rows = min(ROWS, a.R - row0);
-        const T* Kp = static_cast<const T*>(a.v.K) + l * a.v.s_layer + g * a.v.s_head;
-        const T* Vp = static_cast<const T*>(a.v.V) + l * a.v.s_layer + g * a.v.s_head;
-        form.piece(a, r, c, l, g, kv, row0, rows, Kp, Vp, b0, min(b1, r.nb), k2, ca_smem + (threadIdx.x >> 5) * PART);
-        __syncthreads();
-        auto mine = [&](int k, int i) { return ca_smem[k * PART + i]; };
-        if (b0 == 0 && b1 == units) {
-            finish_rows<T, HD, ROWS>(a, CA_WARPS, mine, nullptr, rows, k2, c, kv, row0, r, Kp, Vp);
-        } else {
-            // slot 1 of a CTA: the first part of an item, which the next CTAs go on with; slot 0: the part it begins with
-            float* slot = a.part + (2ll * blockIdx.x + (b0 == 0)) * Part<HD, ROWS>::FLOATS;
-            finish_rows<T, HD, ROWS>(a, CA_WARPS, mine, slot, rows, k2, c, kv, row0, r, Kp, Vp);
-            const long long first = item0 / sh.share, parts = (item0 + units - 1) / sh.share - first + 1;
-            __threadfence();
-            __syncthreads();
-            int* count = a.count + first;
-            if (threadIdx.x == 0) {
-                last = atomicAdd(count, 1) == (int)parts - 1;
-                if (last) *count = 0;  // for the next call
+        const float* ps[CA_WARPS] = {};
+        for (int n = 0; i < 2 * CA_WARPS; ++i) {  // an item's, a warp at most one each
+            const CaNote& x = notes[i];
+            if (!x.part) continue;
+            if (x.c != it.c || x.l != it.l || x.g != it.g || x.rt != it.rt) break;
+#pragma unroll
+            for (int k = 0; k < CA_WARPS; ++k) ps[k] = k == n ? x.part : ps[k];
+            ++n;
+        }
+        const int row0 = it.rt * ROWS, rows = min(ROWS, a.R - row0);
+        const size_t kv = ((size_t)it.c * a.v.L + it.l) * a.v.n_kv + it.g;
+        const long long head = it.l * a.v.s_layer + it.g * a.v.s_head;
+        float* to = it.whole ? nullptr : P::of_cta(a, blockIdx.x, it.first);
+        for (int e = 2 * threadIdx.x; e < rows * HD; e += 2 * CA_THREADS) {
+            const int row = e / HD, d = e - row * HD;
+            float mk[CA_WARPS], mx = -INFINITY, l = 0.f, lx = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll
+            for (int k = 0; k < CA_WARPS; ++k) {
+                mk[k] = ps[k] ? ps[k][P::M + row] : -INFINITY;
+                mx = fmaxf(mx, mk[k]);
             }
-            __syncthreads();
-            if (last) {
-                __threadfence();
-                const float* p0 = a.part + 2ll * first * Part<HD, ROWS>::FLOATS;
-                auto theirs = [&](int k, int i) { return __ldcg(p0 + (2ll * k + (k == 0)) * Part<HD, ROWS>::FLOATS + i); };
-                finish_rows<T, HD, ROWS>(a, (int)parts, theirs, nullptr, rows, k2, c, kv, row0, r, Kp, Vp);
+#pragma unroll
+            for (int k = 0; k < CA_WARPS; ++k) {
+                if (!ps[k]) continue;
+                const float f = mk[k] == -INFINITY ? 0.f : ca_exp2((mk[k] - mx) * k2);
+                const float2 o = *reinterpret_cast<const float2*>(ps[k] + e);
+                l = fmaf(f, ps[k][P::L + row], l);
+                lx = fmaf(f, ps[k][P::LX + row], lx);
+                o0 = fmaf(f, o.x, o0);
+                o1 = fmaf(f, o.y, o1);
+            }
+            if (to) {
+                *reinterpret_cast<float2*>(to + e) = make_float2(o0, o1);
+                if (d == 0) to[P::M + row] = mx, to[P::L + row] = l, to[P::LX + row] = lx;
+            } else {
+                write_row<T, HD>(a, kv, it.c, it.n, row0 + row, d, static_cast<const T*>(a.v.K) + head, static_cast<const T*>(a.v.V) + head, o0, o1, l);
+                if (d == 0 && a.lse) a.lse[kv * a.R + row0 + row] = row_lse(mx, lx, k2);
             }
         }
-        __syncthreads();  // the warps' parts have been read
-        u += b1 - b0;
     }
-    form.done();
 }
 
 // ---------------------------------------------------------------- CUDA cores: fp32, and rows that are not aligned
@@ -262,10 +318,16 @@ struct CaCores {
     static constexpr int HD = HD_, ROWS = 4, CTAS = HD == 64 ? 3 : 2;
     static constexpr int VE = 16 / sizeof(T), D = HD / 8, NP = D / VE;  // elements of 16 bytes; dimensions and 16-byte pieces of a lane
     static constexpr int U = 2;                                         // keys of a lane group at a time
-    static constexpr int WARP_BYTES = Part<HD, ROWS>::FLOATS * 4;
+    static constexpr int WARP_BYTES = 2 * Part<HD, ROWS>::FLOATS * 4;
 
-    __device__ CaCores(const CUtensorMap&, const CUtensorMap&, const CaArgs&, float*) {}
-    __device__ void done() {}
+    float* parts;
+
+    __device__ CaCores(const CUtensorMap&, const CUtensorMap&, uint8_t* smem) : parts(reinterpret_cast<float*>(smem)) {}
+
+    __device__ __forceinline__ void run(const CaArgs& a, CaNote* notes) {
+        CaWalk walk(a);
+        while (walk.next(a)) piece(a, walk, notes);
+    }
 
     static __device__ __forceinline__ void load(const T* row, bool vec, bool in, int l8, float (&f)[D]) {
 #pragma unroll
@@ -286,9 +348,14 @@ struct CaCores {
         }
     }
 
-    __device__ __forceinline__ void piece(const CaArgs& a, const CaRange& r, int c, int, int, size_t kv, int row0, int rows, const T* Kp,
-                                          const T* Vp, int b0, int b1, float k2, float* part) {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane >> 3, l8 = lane & 7;
+    __device__ __forceinline__ void piece(const CaArgs& a, const CaWalk& walk, CaNote* notes) {
+        const CaRange& r = walk.r;
+        const int c = walk.c, row0 = walk.rt * ROWS, rows = min(ROWS, a.R - row0);
+        const size_t kv = walk.kv(a);
+        const long long head = walk.l * a.v.s_layer + walk.g * a.v.s_head;
+        const T *Kp = static_cast<const T*>(a.v.K) + head, *Vp = static_cast<const T*>(a.v.V) + head;
+        const float k2 = a.scale * 1.4426950408889634f;
+        const int lane = threadIdx.x & 31, grp = lane >> 3, l8 = lane & 7;
         const int* table = a.v.table + (size_t)c * a.v.width;
         const int mask = (1 << a.v.page_log2) - 1;
         float q[ROWS][D], o[ROWS][D], m[ROWS], l[ROWS];
@@ -303,7 +370,7 @@ struct CaCores {
 #pragma unroll
             for (int d = 0; d < D; ++d) o[i][d] = 0.f;
         }
-        for (int b = b0 + warp; b < b1; b += CA_WARPS) {
+        for (int b = walk.b0; b < walk.b1; ++b) {
             const int j0 = r.at(b);
 #pragma unroll 1
             for (int it = 0; it < KB / 4; it += U) {
@@ -368,7 +435,10 @@ struct CaCores {
                 }
             }
         }
-        // the lane groups' softmaxes into one
+        // the lane groups' softmaxes into one; lane group i writes row i
+        using P = Part<HD, ROWS>;
+        float* part = parts + (walk.b0 == 0) * P::FLOATS;
+        if (!walk.whole && lane == 0) notes[walk.b0 == 0] = {part, c, walk.l, walk.g, walk.rt, r.n, walk.first, walk.cta_whole};
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
             float mx = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], 8));
@@ -377,16 +447,28 @@ struct CaCores {
             l[i] *= f;
             l[i] += __shfl_xor_sync(0xffffffffu, l[i], 8);
             l[i] += __shfl_xor_sync(0xffffffffu, l[i], 16);
+            if (i >= rows) break;
 #pragma unroll
-            for (int d = 0; d < D; ++d) {
-                float x = o[i][d] * f;
-                x += __shfl_xor_sync(0xffffffffu, x, 8);
-                x += __shfl_xor_sync(0xffffffffu, x, 16);
-                if (grp == i) part[i * HD + d / VE * 8 * VE + l8 * VE + d % VE] = x;
+            for (int d = 0; d < D; d += 2) {
+                float x[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    x[e] = o[i][d + e] * f;
+                    x[e] += __shfl_xor_sync(0xffffffffu, x[e], 8);
+                    x[e] += __shfl_xor_sync(0xffffffffu, x[e], 16);
+                }
+                const int dim = d / VE * 8 * VE + l8 * VE + d % VE;
+                if (grp != i) continue;
+                if (walk.whole)
+                    write_row<T, HD>(a, kv, c, r.n, row0 + i, dim, Kp, Vp, x[0], x[1], l[i]);
+                else
+                    *reinterpret_cast<float2*>(part + i * HD + dim) = make_float2(x[0], x[1]);
             }
             if (lane == 0) {
-                part[ROWS * HD + i] = mx;
-                part[ROWS * (HD + 1) + i] = part[ROWS * (HD + 2) + i] = l[i];
+                if (!walk.whole)
+                    part[P::M + i] = mx, part[P::L + i] = part[P::LX + i] = l[i];
+                else if (a.lse)
+                    a.lse[kv * a.R + row0 + i] = row_lse(mx, l[i], k2);
             }
         }
     }
@@ -424,256 +506,392 @@ struct CaTensor {
     static constexpr int SK = HD == 64 ? 32 : 16, SPB = KB / SK;  // keys of a stage, stages of a block
     static constexpr int SLAB = SK * 128, TILE = HD / 64 * SLAB, STAGE = 2 * TILE;  // 64 dimensions of the keys; keys; both
     static constexpr int NS = 3;
-    static constexpr int BAR = NS * STAGE, WARP_BYTES = BAR + 1024;  // the ring (at a piece's end: its part), its barriers
+    static constexpr int BAR = NS * STAGE, WARP_BYTES = BAR + 1024;  // the ring, its barriers
+    static_assert(CTAS * (CA_WARPS * WARP_BYTES + 3072) <= 228 * 1024, "CTAs an SM");
     static_assert(Part<HD, ROWS>::FLOATS * 4 <= BAR, "a part fits in the ring");
-    static_assert(CTAS * (CA_WARPS * WARP_BYTES + 2048) <= 228 * 1024, "CTAs an SM");
 
     const CUtensorMap &tmK, &tmV;
     uint32_t ring, bars;
-    int slot = 0, phase = 0;   // of the stage to be read next
-    bool ok = true;
+    float* ring_part;  // the ring as the place of the warp's last part
 
-    __device__ CaTensor(const CUtensorMap& k, const CUtensorMap& v, const CaArgs&, float* smem) : tmK(k), tmV(v) {
+    __device__ CaTensor(const CUtensorMap& k, const CUtensorMap& v, uint8_t* smem) : tmK(k), tmV(v) {
         ring = smem_u32(smem);
+        ring_part = reinterpret_cast<float*>(smem);
         bars = ring + BAR;
         if ((threadIdx.x & 31) == 0) {
             for (int s = 0; s < NS; ++s) mbar_init(bars + 8 * s, 1);
             fence_mbar_init();
+            fence_proxy_async_smem();
             tma_prefetch_map(&tmK);
             tma_prefetch_map(&tmV);
         }
         __syncwarp();
-    }
-    __device__ void done() {
-        if (!ok) drain_copies();
     }
 
     // row of a slab, 16-byte chunk of it, under the 128-byte swizzle
     static __device__ __forceinline__ uint32_t at(int row, int chunk) {
         return (chunk >> 3) * SLAB + row * 128 + (((chunk ^ row) & 7) << 4);
     }
+    // stages of a piece, and the first key of one (the last block may end in its first half)
+    static __device__ __forceinline__ int stages(const CaWalk& w) {
+        const int n = (w.b1 - w.b0) * SPB;
+        return SPB == 2 && n && w.r.at(w.b1 - 1) + SK >= w.r.n ? n - 1 : n;
+    }
+    static __device__ __forceinline__ int key0(const CaWalk& w, int i) { return w.r.at(w.b0 + i / SPB) + i % SPB * SK; }
 
-    __device__ __forceinline__ void piece(const CaArgs& a, const CaRange& r, int c, int l, int g, size_t kv, int row0, int rows, const T*,
-                                          const T*, int b0, int b1, float k2, float* part) {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, t = lane & 3;
-        const int* table = a.v.table + (size_t)c * a.v.width;
-        const int mask = (1 << a.v.page_log2) - 1, box = min(mask + 1, SK);  // positions that one copy brings
-        const int cl = a.v.s_layer ? l : 0, cg = a.v.s_head ? g : 0;  // a dimension that is shared has one element in the maps
-        const int first = b0 + warp, stages = first < b1 ? ((b1 - first + CA_WARPS - 1) / CA_WARPS) * SPB : 0;
-        auto key0 = [&](int i) { return r.at(first + i / SPB * CA_WARPS) + i % SPB * SK; };
-        auto issue = [&](int i, int s) {
-            const int j = key0(i) + lane * box;
-            const bool mine = lane * box < SK && j < r.n;
-            const uint32_t who = __ballot_sync(0xffffffffu, mine);
-            if (lane == 0) mbar_expect_tx(bars + 8 * s, __popc(who) * box * HD * 4);
-            __syncwarp();
-            if (mine) {
-                const int page = max(0, cache_page(a.v, table, j >> a.v.page_log2));  // a wrong one is latched
-                const uint32_t dst = ring + s * STAGE + lane * box * 128;
-#pragma unroll
-                for (int kb = 0; kb < HD / 64; ++kb) {
-                    tma_load_5d(dst + kb * SLAB, &tmK, bars + 8 * s, 64 * kb, j & mask, cg, page, cl);
-                    tma_load_5d(dst + TILE + kb * SLAB, &tmV, bars + 8 * s, 64 * kb, j & mask, cg, page, cl);
-                }
-            }
-        };
-        // rows gq and gq + 8 of the tile
-        uint32_t qa[HD / 16][4];
-        int vis[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int row = row0 + min(gq + 8 * h, rows - 1);
-            const bool live = gq + 8 * h < rows;
-            vis[h] = live ? r.n - a.n_tok + row % a.n_tok + 1 : 0;
-            const uint32_t* q = reinterpret_cast<const uint32_t*>(static_cast<const bf16*>(a.Q) + (kv * a.R + row) * HD) + t;
-#pragma unroll
-            for (int k = 0; k < HD / 16; ++k) {
-                qa[k][h] = live ? __ldg(q + 8 * k) : 0;
-                qa[k][2 + h] = live ? __ldg(q + 8 * k + 4) : 0;
-            }
+    // The copies of a warp's stages, ahead of their reading and on through the pieces.  Lane n holds the page of copy n of the
+    // piece's next 32.
+    struct Feed {
+        CaWalk w;
+        int i = 0, n = 0, batch = 0, page = 0;
+        bool more = true;
+        __device__ Feed(const CaArgs& a) : w(a) {}
+    };
+    __device__ __forceinline__ bool feed(const CaArgs& a, Feed& f, int s) {
+        const int lane = threadIdx.x & 31, mask = (1 << a.v.page_log2) - 1;
+        const int box = min(mask + 1, SK), copies = SK / box, copies_log2 = 31 - __clz(copies);  // positions of a copy; of a stage
+        while (f.i == f.n) {
+            if (!f.more || !(f.more = f.w.next(a))) return false;
+            f.i = 0;
+            f.n = stages(f.w);
+            f.batch = INT_MIN;
         }
-        float o[HD / 8][4], m[2] = {-INFINITY, -INFINITY}, lr[2] = {0.f, 0.f}, lx[2] = {0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < HD / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-        // the part that the ring's bytes held before has been read: by everybody (the CTA's barrier), and for the copies
-        fence_proxy_async_smem();
+        if (f.batch == INT_MIN || f.i - f.batch == 32 >> copies_log2) {
+            f.batch = f.i;
+            const int i = f.i + (lane >> copies_log2), j = i < f.n ? key0(f.w, i) + (lane & (copies - 1)) * box : INT_MAX;
+            f.page = j < f.w.r.n ? __ldg(a.v.table + (size_t)f.w.c * a.v.width + (j >> a.v.page_log2)) : 0;
+        }
+        int page = __shfl_sync(0xffffffffu, f.page, ((f.i - f.batch) << copies_log2) + (lane & (copies - 1)));
+        const int j = key0(f.w, f.i) + lane * box;
+        const bool mine = lane < copies && j < f.w.r.n;
+        const uint32_t who = __ballot_sync(0xffffffffu, mine);
+        if (lane == 0) mbar_expect_tx(bars + 8 * s, __popc(who) * box * HD * 4);
         __syncwarp();
-        int ahead = 0;  // stages asked for; their slots follow `slot`
-        for (int s = slot; ok && ahead < min(NS - 1, stages) && key0(ahead) < r.n; ++ahead) {
-            issue(ahead, s);
-            s = s + 1 == NS ? 0 : s + 1;
+        if (mine) {
+            if ((unsigned)page >= (unsigned)a.v.n_pages) {  // some page instead: what comes of it is an error's
+                cache_fail(a.v.status, DS_CACHE_PAGE);
+                page = 0;
+            }
+            const uint32_t dst = ring + s * STAGE + lane * box * 128;
+            const int l = a.v.s_layer ? f.w.l : 0, g = a.v.s_head ? f.w.g : 0;  // what is shared has one element in the maps
+#pragma unroll
+            for (int kb = 0; kb < HD / 64; ++kb) {
+                tma_load_5d(dst + kb * SLAB, &tmK, bars + 8 * s, 64 * kb, j & mask, g, page, l);
+                tma_load_5d(dst + TILE + kb * SLAB, &tmV, bars + 8 * s, 64 * kb, j & mask, g, page, l);
+            }
         }
-        for (int i = 0; ok && i < stages && key0(i) < r.n; ++i) {
-            if (ahead < stages && key0(ahead) < r.n) {  // into the slot that was read last
-                int s = slot + NS - 1;
-                issue(ahead++, s >= NS ? s - NS : s);
-            }
-            ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * slot, phase, a.v.status));
-            if (!ok) break;
-            const int j0 = key0(i);
-            const uint32_t ks = ring + slot * STAGE, vs = ks + TILE;
-            const bool whole = j0 + SK <= r.n - a.n_tok + 1 && (j0 + SK <= a.n_sink || j0 >= r.n - a.window);
-            if (!whole) {  // values that no row sees are not to meet a probability of 0
-                for (int e = lane; e < SK * 8; e += 32) {
-                    const int key = j0 + (e >> 3);
-                    if (key < r.n && (key < a.n_sink || key > r.t0 - a.window)) continue;
-#pragma unroll
-                    for (int kb = 0; kb < HD / 64; ++kb)
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(vs + kb * SLAB + e * 16), "r"(0) : "memory");
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-            }
-            float s[SK / 8][4];
-#pragma unroll
-            for (int nt = 0; nt < SK / 8; ++nt) {
-                s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
-#pragma unroll
-                for (int k = 0; k < HD / 32; ++k) {
-                    uint32_t b[4];
-                    ca_ldmatrix<false>(b, ks + at(8 * nt + (lane & 7), 4 * k + (lane >> 3)));
-                    ca_mma(s[nt], qa[2 * k], b[0], b[1]);
-                    ca_mma(s[nt], qa[2 * k + 1], b[2], b[3]);
-                }
-            }
-            if (!whole) {
-#pragma unroll
-                for (int nt = 0; nt < SK / 8; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = j0 + 8 * nt + 2 * t + (e & 1), h = e >> 1;
-                        s[nt][e] = key < vis[h] && (key < a.n_sink || key >= vis[h] - a.window) ? s[nt][e] : -INFINITY;
-                    }
-            }
-            if (a.z2) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (gq + 8 * h < rows) {
-                        float* z = a.z2 + (kv * a.R + row0 + gq + 8 * h) * a.pitch + j0 + 2 * t;
-#pragma unroll
-                        for (int nt = 0; nt < SK / 8; ++nt)
-                            *reinterpret_cast<float2*>(z + 8 * nt) = make_float2(s[nt][2 * h] * k2, s[nt][2 * h + 1] * k2);
-                    }
-            }
-            float moff[2], corr[2];
+        ++f.i;
+        return true;
+    }
+
+    __device__ __forceinline__ void run(const CaArgs& a, CaNote* notes) {
+        using P = Part<HD, ROWS>;
+        const int lane = threadIdx.x & 31, gq = lane >> 2, t = lane & 3;
+        const float k2 = a.scale * 1.4426950408889634f;
+        Feed ahead(a);
+        CaWalk w = ahead.w;
+        int slot = 0, phase = 0;  // of the stage to be read next
+        for (int s = 0; s < NS - 1; ++s)
+            if (!feed(a, ahead, s)) break;
+        bool ok = true;
+        while (ok && w.next(a)) {
+            const CaRange& r = w.r;
+            const int row0 = w.rt * ROWS, rows = min(ROWS, a.R - row0), n = stages(w);
+            const size_t kv = w.kv(a);
+            // rows gq and gq + 8 of the tile
+            uint32_t qa[HD / 16][4];
+            int vis[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                float cm = fmaxf(s[0][2 * h], s[0][2 * h + 1]);
+                const int row = row0 + min(gq + 8 * h, rows - 1);
+                const bool live = gq + 8 * h < rows;
+                vis[h] = live ? r.n - a.n_tok + row % a.n_tok + 1 : 0;
+                const uint32_t* q = reinterpret_cast<const uint32_t*>(static_cast<const bf16*>(a.Q) + (kv * a.R + row) * HD) + t;
 #pragma unroll
-                for (int nt = 1; nt < SK / 8; ++nt) cm = fmaxf(cm, fmaxf(s[nt][2 * h], s[nt][2 * h + 1]));
-                cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, 1));
-                cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, 2));
-                const float mn = fmaxf(m[h], cm);
-                corr[h] = mn == m[h] ? 1.f : ca_exp2((m[h] - mn) * k2);
-                moff[h] = mn == -INFINITY ? 0.f : -mn * k2;
-                m[h] = mn;
-            }
-            if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    lr[h] *= corr[h];
-                    lx[h] *= corr[h];
-                }
-#pragma unroll
-                for (int j = 0; j < HD / 8; ++j) {
-                    o[j][0] *= corr[0];
-                    o[j][1] *= corr[0];
-                    o[j][2] *= corr[1];
-                    o[j][3] *= corr[1];
+                for (int k = 0; k < HD / 16; ++k) {
+                    qa[k][h] = live ? __ldg(q + 8 * k) : 0;
+                    qa[k][2 + h] = live ? __ldg(q + 8 * k + 4) : 0;
                 }
             }
+            float o[HD / 8][4], m[2] = {-INFINITY, -INFINITY}, lr[2] = {0.f, 0.f}, lx[2] = {0.f, 0.f};
 #pragma unroll
-            for (int kk = 0; kk < SK / 16; ++kk) {
-                uint32_t pa[4];  // rows gq, gq + 8 x keys (2 t, 2 t + 1), then the same of the next eight keys
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int nt = 2 * kk + (q >> 1), h = q & 1;
-                    const float e0 = ca_exp2(fmaf(s[nt][2 * h], k2, moff[h])), e1 = ca_exp2(fmaf(s[nt][2 * h + 1], k2, moff[h]));
-                    pa[q] = pack_bf16(e0, e1);
-                    // O's sum takes the probabilities the MMA sees, the weights' the exact ones
-                    lr[h] += __uint_as_float(pa[q] << 16) + __uint_as_float(pa[q] & 0xffff0000u);
-                    lx[h] += e0 + e1;
-                }
-#pragma unroll
-                for (int d = 0; d < HD / 16; ++d) {
-                    uint32_t b[4];
-                    ca_ldmatrix<true>(b, vs + at(16 * kk + (lane & 15), 2 * d + (lane >> 4)));
-                    ca_mma(o[2 * d], pa, b[0], b[1]);
-                    ca_mma(o[2 * d + 1], pa, b[2], b[3]);
+            for (int j = 0; j < HD / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+            for (int i = 0; i < n; ++i) {
+                feed(a, ahead, slot == 0 ? NS - 1 : slot - 1);  // the slot that was read last
+                ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * slot, phase, a.v.status));
+                if (!ok) break;
+                step(a, r, key0(w, i), ring + slot * STAGE, kv, row0, rows, vis, k2, qa, o, m, lr, lx);
+                __syncwarp();  // the stage has been read
+                if (++slot == NS) {
+                    slot = 0;
+                    phase ^= 1;
                 }
             }
-            __syncwarp();  // the stage has been read
-            if (++slot == NS) {
-                slot = 0;
-                phase ^= 1;
+            // a part goes to the workspace while the ring is in use
+            float* part = w.last && ok ? ring_part : P::of_warp(a, w.b0 == 0);
+            if (!w.whole && lane == 0) notes[w.b0 == 0] = {part, w.c, w.l, w.g, w.rt, r.n, w.first, w.cta_whole};
+            const long long head = w.l * a.v.s_layer + w.g * a.v.s_head;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int x = 1; x < 4; x <<= 1) {
+                    lr[h] += __shfl_xor_sync(0xffffffffu, lr[h], x);
+                    lx[h] += __shfl_xor_sync(0xffffffffu, lx[h], x);
+                }
+                const int row = gq + 8 * h;
+                if (row >= rows) continue;
+                if (w.whole) {
+#pragma unroll
+                    for (int j = 0; j < HD / 8; ++j)
+                        write_row<bf16, HD>(a, kv, w.c, r.n, row0 + row, 8 * j + 2 * t, static_cast<const bf16*>(a.v.K) + head,
+                                            static_cast<const bf16*>(a.v.V) + head, o[j][2 * h], o[j][2 * h + 1], lr[h]);
+                    if (t == 0 && a.lse) a.lse[kv * a.R + row0 + row] = row_lse(m[h], lx[h], k2);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < HD / 8; ++j)
+                        *reinterpret_cast<float2*>(part + row * HD + 8 * j + 2 * t) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
+                    if (t == 0) {
+                        part[P::M + row] = m[h];
+                        part[P::L + row] = lr[h];
+                        part[P::LX + row] = lx[h];
+                    }
+                }
+            }
+            __syncwarp();
+        }
+        if (!ok) drain_copies();
+    }
+
+    // One stage's keys
+    __device__ __forceinline__ void step(const CaArgs& a, const CaRange& r, int j0, uint32_t ks, size_t kv, int row0, int rows, const int (&vis)[2],
+                                         float k2, const uint32_t (&qa)[HD / 16][4], float (&o)[HD / 8][4], float (&m)[2], float (&lr)[2],
+                                         float (&lx)[2]) {
+        const int lane = threadIdx.x & 31, gq = lane >> 2, t = lane & 3;
+        const uint32_t vs = ks + TILE;
+        const bool whole = j0 + SK <= r.n - a.n_tok + 1 && (j0 + SK <= a.n_sink || j0 >= r.n - a.window);
+        if (!whole) {  // values that no row sees are not to meet a probability of 0
+            for (int e = lane; e < SK * 8; e += 32) {
+                const int key = j0 + (e >> 3);
+                if (key < r.n && (key < a.n_sink || key > r.t0 - a.window)) continue;
+#pragma unroll
+                for (int kb = 0; kb < HD / 64; ++kb)
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(vs + kb * SLAB + e * 16), "r"(0) : "memory");
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+        }
+        float s[SK / 8][4];
+#pragma unroll
+        for (int nt = 0; nt < SK / 8; ++nt) {
+            s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+#pragma unroll
+            for (int k = 0; k < HD / 32; ++k) {
+                uint32_t b[4];
+                ca_ldmatrix<false>(b, ks + at(8 * nt + (lane & 7), 4 * k + (lane >> 3)));
+                ca_mma(s[nt], qa[2 * k], b[0], b[1]);
+                ca_mma(s[nt], qa[2 * k + 1], b[2], b[3]);
+            }
+        }
+        if (!whole) {
+#pragma unroll
+            for (int nt = 0; nt < SK / 8; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int key = j0 + 8 * nt + 2 * t + (e & 1), h = e >> 1;
+                    s[nt][e] = key < vis[h] && (key < a.n_sink || key >= vis[h] - a.window) ? s[nt][e] : -INFINITY;
+                }
+        }
+        if (a.z2) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (gq + 8 * h < rows) {
+                    float* z = a.z2 + (kv * a.R + row0 + gq + 8 * h) * a.pitch + j0 + 2 * t;
+#pragma unroll
+                    for (int nt = 0; nt < SK / 8; ++nt)
+                        *reinterpret_cast<float2*>(z + 8 * nt) = make_float2(s[nt][2 * h] * k2, s[nt][2 * h + 1] * k2);
+                }
+        }
+        float moff[2], corr[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float cm = fmaxf(s[0][2 * h], s[0][2 * h + 1]);
+#pragma unroll
+            for (int nt = 1; nt < SK / 8; ++nt) cm = fmaxf(cm, fmaxf(s[nt][2 * h], s[nt][2 * h + 1]));
+            cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, 1));
+            cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, 2));
+            const float mn = fmaxf(m[h], cm);
+            corr[h] = mn == m[h] ? 1.f : ca_exp2((m[h] - mn) * k2);
+            moff[h] = mn == -INFINITY ? 0.f : -mn * k2;
+            m[h] = mn;
+        }
+        if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                lr[h] *= corr[h];
+                lx[h] *= corr[h];
+            }
+#pragma unroll
+            for (int j = 0; j < HD / 8; ++j) {
+                o[j][0] *= corr[0];
+                o[j][1] *= corr[0];
+                o[j][2] *= corr[1];
+                o[j][3] *= corr[1];
             }
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int kk = 0; kk < SK / 16; ++kk) {
+            uint32_t pa[4];  // rows gq, gq + 8 x keys (2 t, 2 t + 1), then the same of the next eight keys
 #pragma unroll
-            for (int x = 1; x < 4; x <<= 1) {
-                lr[h] += __shfl_xor_sync(0xffffffffu, lr[h], x);
-                lx[h] += __shfl_xor_sync(0xffffffffu, lx[h], x);
+            for (int q = 0; q < 4; ++q) {
+                const int nt = 2 * kk + (q >> 1), h = q & 1;
+                const float e0 = ca_exp2(fmaf(s[nt][2 * h], k2, moff[h])), e1 = ca_exp2(fmaf(s[nt][2 * h + 1], k2, moff[h]));
+                pa[q] = pack_bf16(e0, e1);
+                // O's sum takes the probabilities the MMA sees, the weights' the exact ones
+                lr[h] += __uint_as_float(pa[q] << 16) + __uint_as_float(pa[q] & 0xffff0000u);
+                lx[h] += e0 + e1;
             }
-            const int row = gq + 8 * h;
-            if (t == 0) {
-                part[ROWS * HD + row] = m[h];
-                part[ROWS * (HD + 1) + row] = lr[h];
-                part[ROWS * (HD + 2) + row] = lx[h];
-            }
-            if (row < rows)
 #pragma unroll
-                for (int j = 0; j < HD / 8; ++j) *reinterpret_cast<float2*>(part + row * HD + 8 * j + 2 * t) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
+            for (int d = 0; d < HD / 16; ++d) {
+                uint32_t b[4];
+                ca_ldmatrix<true>(b, vs + at(16 * kk + (lane & 15), 2 * d + (lane >> 4)));
+                ca_mma(o[2 * d], pa, b[0], b[1]);
+                ca_mma(o[2 * d + 1], pa, b[2], b[3]);
+            }
         }
     }
 };
 
-// ---------------------------------------------------------------- weights
-constexpr int SC_THREADS = 256, SC_POS = 4 * SC_THREADS;
+// ---------------------------------------------------------------- joining the parts, and the weights
+constexpr int FIN_THREADS = 256, FIN_WARPS = FIN_THREADS / 32, FIN_POS = 4 * FIN_THREADS;
 
-// A thread adds the weights of four positions over the KV head's rows.
-__global__ void __launch_bounds__(SC_THREADS) cache_weights_kernel(const CaArgs a) {
-    const int chain = blockIdx.z, g = blockIdx.y, c = chain / a.v.L, l = chain % a.v.L;
-    const int n = cache_len(a.v, c), p0 = blockIdx.x * SC_POS + 4 * threadIdx.x;
-    if (p0 >= n) return;
-    const long long t0 = max(0, n - a.n_tok);
-    if (p0 >= a.n_sink && p0 + 4 <= t0 - a.window + 1) return;  // nobody sees them
-    const size_t kv = (size_t)chain * a.v.n_kv + g;
-    float w[4] = {0.f, 0.f, 0.f, 0.f};
-    const float* z = a.z2 + kv * a.R * a.pitch + p0;
-    const float* lse = a.lse + kv * a.R;
-#pragma unroll 4
-    for (int row = 0; row < a.R; ++row) {
-        const float4 x = __ldcs(reinterpret_cast<const float4*>(z + row * a.pitch));
-        const float s = __ldg(lse + row);
-        w[0] += ca_exp2(x.x - s);
-        w[1] += ca_exp2(x.y - s);
-        w[2] += ca_exp2(x.z - s);
-        w[3] += ca_exp2(x.w - s);
+// One row of a split item from its parts, of CTAs first .. first + n - 1.  A thread has two dimensions of every G-th part;
+// the G sums are added in order.
+template <typename T, int HD, int ROWS>
+__device__ __forceinline__ void join_row(const CaArgs& a, int c, int row, size_t kv, const T* K, const T* V, int n_pos, int first, int n, float k2) {
+    using P = Part<HD, ROWS>;
+    constexpr int COLS = HD / 2, G = FIN_THREADS / COLS;
+    __shared__ float2 os[G][COLS];
+    __shared__ float ls[G];
+    const int col = threadIdx.x % COLS, grp = threadIdx.x / COLS, in = row % ROWS;
+    auto part = [&](int k) { return P::of_cta(a, first + k, k == 0); };
+    float mx = -INFINITY;
+    for (int k = threadIdx.x & 31; k < n; k += 32) mx = fmaxf(mx, part(k)[P::M + in]);
+    mx = warp_max(mx);
+    float2 o = make_float2(0.f, 0.f);
+    float l = 0.f;
+#pragma unroll 8
+    for (int k = grp; k < n; k += G) {
+        const float* p = part(k);
+        const float2 x = *reinterpret_cast<const float2*>(p + in * HD + 2 * col);
+        const float mk = p[P::M + in], f = mk == -INFINITY ? 0.f : ca_exp2((mk - mx) * k2);
+        l = fmaf(f, p[P::L + in], l);
+        o.x = fmaf(f, x.x, o.x);
+        o.y = fmaf(f, x.y, o.y);
     }
+    os[grp][col] = o;
+    if (col == 0) ls[grp] = l;
+    __syncthreads();
+    if (grp) return;
+    for (int k = 1; k < G; ++k) {
+        l += ls[k];
+        o.x += os[k][col].x;
+        o.y += os[k][col].y;
+    }
+    write_row<T, HD>(a, kv, c, n_pos, row, 2 * col, K, V, o.x, o.y, l);
+}
+
+// The first R blocks of a KV head join its rows' parts; the others, if the cache has weights, add those of FIN_POS positions
+// each, four a thread.
+template <typename Form>
+__global__ void __launch_bounds__(FIN_THREADS, 5) cache_finish_kernel(const CaArgs a) {
+    using T = typename Form::T;
+    constexpr int HD = Form::HD, ROWS = Form::ROWS;
+    __shared__ float lse[FIN_ROWS];
+    const int chain = blockIdx.z, g = blockIdx.y, c = chain / a.v.L, l = chain % a.v.L;
+    const float k2 = a.scale * 1.4426950408889634f;
+    const size_t kv = (size_t)chain * a.v.n_kv + g;
+    const CaRange r(a, c);
+    const int tile0 = ((int)blockIdx.x - a.R) * FIN_POS, p0 = tile0 + 4 * threadIdx.x;
+    if (tile0 >= r.n || (tile0 >= a.n_sink && tile0 + FIN_POS <= r.t0 - a.window + 1)) return;  // nobody sees them
+    CaDeal deal(a);
+    const int units = r.units(), item0 = deal.first_unit(a, c) + (l * a.v.n_kv + g) * a.RT * units;
+    pdl_wait();  // what is above reads only what the call was given
+    if ((int)blockIdx.x < a.R) {
+        int first;
+        const int row = blockIdx.x, n = deal.parts(item0 + row / ROWS * units, units, first);
+        if (n == 1) return;
+        const long long head = l * a.v.s_layer + g * a.v.s_head;
+        join_row<T, HD, ROWS>(a, c, row, kv, static_cast<const T*>(a.v.K) + head, static_cast<const T*>(a.v.V) + head, r.n, first, n, k2);
+        return;
+    }
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
+    const bool any = p0 < r.n && !(p0 >= a.n_sink && p0 + 4 <= r.t0 - a.window + 1);
+    for (int row0 = 0; row0 < a.R; row0 += FIN_ROWS) {
+        const int rows = min(FIN_ROWS, a.R - row0);
+        __syncthreads();
+        for (int row = threadIdx.x >> 5; row < rows; row += FIN_WARPS) {  // a warp a row
+            const int lane = threadIdx.x & 31, rt = (row0 + row) / ROWS, in = (row0 + row) % ROWS;
+            int first;
+            const int n = deal.parts(item0 + rt * units, units, first);
+            float m = -INFINITY, lx = 0.f;
+            if (n == 1) {
+                m = a.lse[kv * a.R + row0 + row];
+            } else {
+                for (int k = lane; k < n; k += 32) {
+                    using P = Part<HD, ROWS>;
+                    const float* p = P::of_cta(a, first + k, k == 0) + in;
+                    const float mk = p[P::M], lk = p[P::LX], mn = fmaxf(m, mk);
+                    if (mk == -INFINITY) continue;
+                    lx = fmaf(lx, ca_exp2((m - mn) * k2), lk * ca_exp2((mk - mn) * k2));
+                    m = mn;
+                }
+                const float mx = warp_max(m);
+                lx = warp_sum(m == -INFINITY ? 0.f : lx * ca_exp2((m - mx) * k2));
+                m = row_lse(mx, lx, k2);
+            }
+            if (lane == 0) lse[row] = m;
+        }
+        __syncthreads();
+        if (!any) continue;
+        const float* z = a.z2 + (kv * a.R + row0) * a.pitch + p0;
+#pragma unroll 4
+        for (int row = 0; row < rows; ++row) {
+            const float4 x = __ldcs(reinterpret_cast<const float4*>(z + row * a.pitch));
+            const float s = lse[row];
+            w[0] += ca_exp2(x.x - s);
+            w[1] += ca_exp2(x.y - s);
+            w[2] += ca_exp2(x.z - s);
+            w[3] += ca_exp2(x.w - s);
+        }
+    }
+    if (!any) return;
     float* score = a.v.score + (((size_t)c * a.v.Lh + l) * a.v.n_kv + g) * a.v.cap;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int p = p0 + i;
-        if (p < n && (p < a.n_sink || p > t0 - a.window)) score[p] += w[i];
+        if (p < r.n && (p < a.n_sink || p > r.t0 - a.window)) score[p] += w[i];
     }
 }
 
+// Blocks of an item, at most: a context as long as its table, first positions and window in blocks of their own
+long long max_blocks(const CacheView& v) { return (v.cap + KB - 1) / KB + 1; }
+// Whether a call has a second kernel
+bool has_finish(const CacheView& v) { return v.score || max_blocks(v) > CA_WHOLE; }
+
 template <typename Form>
 cudaError_t launch(CaArgs a, const CUtensorMap& tmK, const CUtensorMap& tmV, int sms, cudaStream_t st) {
-    static_assert(Form::CTAS <= CA_CTAS, "the workspace holds the parts of CA_CTAS CTAs an SM");
-    if (Form::CTAS * sms > kCacheCounters) return cudaErrorInvalidConfiguration;
+    static_assert(Form::CTAS * Form::ROWS <= CA_SM_ROWS, "the workspace's parts");
     constexpr size_t smem = CA_WARPS * Form::WARP_BYTES + 1024;
     static PerDevice<SmemOptIn> once;
     cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(cache_attention_kernel<Form>), smem, once);
     if (e != cudaSuccess) return e;
     a.RT = (a.R + Form::ROWS - 1) / Form::ROWS;
-    a.per = (long long)a.v.L * a.v.n_kv * a.RT;
-    cache_attention_kernel<Form><<<Form::CTAS * sms, CA_THREADS, smem, st>>>(tmK, tmV, a);
-    if ((e = cudaGetLastError()) != cudaSuccess || !a.v.score) return e;
-    const dim3 grid((unsigned)((a.v.cap + SC_POS - 1) / SC_POS), a.v.n_kv, a.v.n_ctx * a.v.L);
-    cache_weights_kernel<<<grid, SC_THREADS, 0, st>>>(a);
-    return cudaGetLastError();
+    a.per = a.v.L * a.v.n_kv * a.RT;
+    a.ctas = Form::CTAS * sms;
+    cache_attention_kernel<Form><<<a.ctas, CA_THREADS, smem, st>>>(tmK, tmV, a);
+    if ((e = cudaGetLastError()) != cudaSuccess || !has_finish(a.v)) return e;
+    const dim3 grid((unsigned)(a.R + (a.v.score ? (a.v.cap + FIN_POS - 1) / FIN_POS : 0)), a.v.n_kv, a.v.n_ctx * a.v.L);
+    return launch_kernel(cache_finish_kernel<Form>, grid, dim3(FIN_THREADS), 0, st, true, 1, a);
 }
 
 // The pools as (head_dim, position, KV head, page, layer), a box the positions of a page that a stage holds.
@@ -711,15 +929,13 @@ cudaError_t launch_bf16(const CaArgs& a, int sms, cudaStream_t st) {
     return launch<CaCores<bf16, HD>>(a, mk, mv, sms, st);
 }
 
-// The workspace: the counters in the same place whatever the call's sizes, then what a call needs beside them.
 struct Layout {
-    size_t part, lse, z2, bytes;
+    size_t lse, z2, bytes;
     long long pitch;
     Layout(const DevState& s, const CacheView& v, int n_q, int n_tok) {
         const size_t kv = (size_t)v.n_ctx * v.L * v.n_kv, R = (size_t)n_q / v.n_kv * n_tok;
         auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-        part = kCacheCounters * sizeof(int);
-        lse = part + up((size_t)2 * CA_CTAS * s.sms * Part<128, 16>::FLOATS * sizeof(float));
+        lse = up((size_t)2 * (1 + CA_WARPS) * CA_SM_ROWS * s.sms * (s.hd + 3) * sizeof(float));  // after the parts
         z2 = lse + (v.score ? up(kv * R * sizeof(float)) : 0);
         pitch = (v.cap + KB - 1) / KB * KB;
         bytes = z2 + (v.score ? up(kv * R * pitch * sizeof(float)) : 0);
@@ -728,7 +944,14 @@ struct Layout {
 
 }  // namespace
 
-size_t cache_attention_workspace(const DevState& s, const CacheView& v, int n_q, int n_tok) { return Layout(s, v, n_q, n_tok).bytes; }
+size_t cache_attention_workspace(const DevState& s, const CacheView& v, int n_q, int n_tok) {
+    // blocks are counted in 31 bits; the CUDA-core form has the most row tiles
+    const long long tiles = (n_q / v.n_kv * n_tok + CaCores<float, 64>::ROWS - 1) / CaCores<float, 64>::ROWS;
+    if (max_blocks(v) * v.n_ctx * v.L * v.n_kv * tiles >= 1 << 30) return 0;
+    return Layout(s, v, n_q, n_tok).bytes;
+}
+
+int cache_attention_kernels(const CacheView& v) { return has_finish(v) ? 2 : 1; }
 
 cudaError_t launch_cache_attention(const DevState& s, const CacheView& v, const void* Q, int n_q, int n_tok, int n_sink, int window,
                                    void* out, void* ws, cudaStream_t st) {
@@ -742,8 +965,7 @@ cudaError_t launch_cache_attention(const DevState& s, const CacheView& v, const 
     a.vec = cache_vec(v, s.dtype == 0 ? 4 : 2);
     a.scale = 1.0f / sqrtf((float)s.hd);
     char* b = static_cast<char*>(ws);
-    a.count = reinterpret_cast<int*>(b);
-    a.part = reinterpret_cast<float*>(b + w.part);
+    a.part = reinterpret_cast<float*>(b);
     a.lse = v.score ? reinterpret_cast<float*>(b + w.lse) : nullptr;
     a.z2 = v.score ? reinterpret_cast<float*>(b + w.z2) : nullptr;
     a.pitch = w.pitch;

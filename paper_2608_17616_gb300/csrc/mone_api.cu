@@ -1092,6 +1092,7 @@ mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache
     if (n_tok < 1 || n_tok > 16 || n_sink < 0 || window < 0) return MONE_ERR_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const size_t need = cache_attention_workspace(s, v, n_q_heads, n_tok);
+    if (need == 0) return MONE_ERR_UNSUPPORTED_SHAPE;
     if (need > m->cws_bytes) {
         MONE_CUDA(cudaStreamSynchronize(st));
         if (m->cws) cudaFree(m->cws);
@@ -1100,7 +1101,6 @@ mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache
         char* p = nullptr;
         MONE_TRY(dalloc(&p, need));
         m->cws = p;
-        MONE_CUDA(cudaMemsetAsync(p, 0, kCacheCounters * sizeof(int), st));
         m->cws_bytes = need;
     }
     return timed(m, K_CACHE, st, cache_attention_kernels(v), [&] {

@@ -166,7 +166,7 @@ def test_launches_on_either_device(fake, dtype):
             launches, _ = fake.drain()
             assert {x["dev"] for x in launches} == {dev}
             assert [x["grid"][0] % sms for x in launches if "attention_kernel" in x["name"]] == [0, 0]
-            assert sum("weights_kernel" in x["name"] for x in launches) == 1
+            assert sum("finish_kernel" in x["name"] for x in launches) == 1
         mone.mone_mem_free(h)
 
 
