@@ -65,20 +65,23 @@ struct CaRange {
     __device__ int units() const { return max(nb, 1); }  // an item without a block still writes its zeros
 };
 
+__device__ __forceinline__ int udiv(int a, int b) { return (int)((unsigned)a / (unsigned)b); }
+
 // How the units of all items, one item after the other, are dealt out: `share` to each CTA.  A boundary within an item of
 // up to CA_WHOLE units moves to the item's start.
 struct CaDeal {
     int total, share;
-    int mine, incl;  // units of context c0 + lane and those up to it, of the contexts scanned last
+    int units, mine, incl;  // of context c0 + lane, of those scanned last: units of an item, of its items, up to its last
     __device__ CaDeal(const CaArgs& a) {
         total = 0;
         for (int c0 = 0; c0 < a.v.n_ctx; c0 += 32) total = scan(a, c0, total);
-        share = max((total + a.ctas - 1) / a.ctas, CA_SHARE);
+        share = max(udiv(total + a.ctas - 1, a.ctas), CA_SHARE);
     }
     // with `before` units ahead of them; returns the units up to the last
     __device__ int scan(const CaArgs& a, int c0, int before) {
         const int lane = threadIdx.x & 31;
-        mine = c0 + lane < a.v.n_ctx ? CaRange(a, c0 + lane).units() * a.per : 0;
+        units = c0 + lane < a.v.n_ctx ? CaRange(a, c0 + lane).units() : 0;
+        mine = units * a.per;
         incl = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -88,7 +91,7 @@ struct CaDeal {
         incl += before;
         return __shfl_sync(0xffffffffu, incl, 31);
     }
-    // where unit u < total lies: its context and the context's first unit; returns the units of its items
+    // where unit u < total lies: its context, the context's first unit and the units of its items
     __device__ int locate(const CaArgs& a, int u, int& base, int& c) {
         int c0 = 0;
         if (a.v.n_ctx > 32)
@@ -96,7 +99,7 @@ struct CaDeal {
         const int k = __ffs(__ballot_sync(0xffffffffu, incl > u)) - 1;
         c = c0 + k;
         base = __shfl_sync(0xffffffffu, incl - mine, k);
-        return __shfl_sync(0xffffffffu, mine, k) / a.per;
+        return __shfl_sync(0xffffffffu, units, k);
     }
     // the first unit of context c
     __device__ int first_unit(const CaArgs& a, int c) {
@@ -112,16 +115,16 @@ struct CaDeal {
     }
     // the first unit of CTA w
     __device__ int start(const CaArgs& a, int w) {
-        const long long at = (long long)w * share;
-        if (at >= total) return total;
+        const int u = w * share;  // below 2^30 + ctas share
+        if (u >= total) return total;
         int base, c;
-        const int u = (int)at, units = locate(a, u, base, c);
-        return units <= CA_WHOLE ? base + (u - base) / units * units : u;
+        const int n = locate(a, u, base, c);
+        return n <= CA_WHOLE ? base + udiv(u - base, n) * n : u;
     }
-    // the parts of the item of units [u, u + units): from CTA `first`, 1 where it stays whole
-    __device__ int parts(int u, int units, int& first) const {
-        first = u / share;
-        return units <= CA_WHOLE ? 1 : (u + units - 1) / share - first + 1;
+    // the parts of the item of units [u, u + n): from CTA `first`, 1 where it stays whole
+    __device__ int parts(int u, int n, int& first) const {
+        first = udiv(u, share);
+        return n <= CA_WHOLE ? 1 : udiv(u + n - 1, share) - first + 1;
     }
 };
 
@@ -138,8 +141,8 @@ struct CaWalk {
         cta0 = deal.start(a, blockIdx.x);
         cta1 = deal.start(a, blockIdx.x + 1);
         const int warp = threadIdx.x >> 5, n = cta1 - cta0;
-        u = cta0 + (int)((long long)n * warp / CA_WARPS);
-        end = cta0 + (int)((long long)n * (warp + 1) / CA_WARPS);
+        u = cta0 + n / CA_WARPS * warp + n % CA_WARPS * warp / CA_WARPS;
+        end = cta0 + n / CA_WARPS * (warp + 1) + n % CA_WARPS * (warp + 1) / CA_WARPS;
         if (u < end) {
             units = deal.locate(a, u, ctx0, c);
             r = CaRange(a, c);
@@ -152,7 +155,7 @@ struct CaWalk {
             r = CaRange(a, ++c);
             units = r.units();
         }
-        const int in_ctx = (u - ctx0) / units, lg = in_ctx / a.RT;
+        const int in_ctx = udiv(u - ctx0, units), lg = a.RT == 1 ? in_ctx : udiv(in_ctx, a.RT);
         b0 = u - ctx0 - in_ctx * units;
         const int e = min(units, b0 + end - u);
         whole = b0 == 0 && e == units;
@@ -162,7 +165,7 @@ struct CaWalk {
         u += e - b0;
         last = u >= end;
         rt = in_ctx - lg * a.RT;
-        l = lg / a.v.n_kv;
+        l = a.v.L == 1 ? 0 : udiv(lg, a.v.n_kv);
         g = lg - l * a.v.n_kv;
         return true;
     }
@@ -170,13 +173,13 @@ struct CaWalk {
     __device__ size_t kv(const CaArgs& a) const { return ((size_t)c * a.v.L + l) * a.v.n_kv + g; }
 };
 
-// A row of Q over the positions it sees and no others, by one thread: dimensions d0, d0 + 1.  A block's products take a
+// A row of Q over the positions it sees and no others, by one thread: N dimensions from d0.  A block's products take a
 // value row times a probability of 0 for the rows that do not see it, which is NaN where the value is not finite; only
 // with several tokens do the rows of an item differ in what they see.  Reached by non-finite inputs only.
-template <typename T, int HD>
+template <typename T, int HD, int N>
 __device__ __noinline__ void row_again(const CaArgs& a, const T* q, const T* K, const T* V, const int* table, int vis, int d0, float* o) {
     float m = -INFINITY, l = 0.f;
-    o[0] = o[1] = 0.f;
+    for (int d = 0; d < N; ++d) o[d] = 0.f;
     for (int j = a.n_sink > 0 ? 0 : max(0, vis - a.window); j < vis; ++j) {
         if (j >= a.n_sink && j < vis - a.window) j = vis - a.window;
         if (j >= vis) break;
@@ -190,12 +193,10 @@ __device__ __noinline__ void row_again(const CaArgs& a, const T* q, const T* K, 
         const float mn = fmaxf(m, z), corr = __expf(m - mn), p = __expf(z - mn);
         m = mn;
         l = fmaf(l, corr, p);
-        o[0] = fmaf(o[0], corr, p * to_f<T>(V[off + d0]));
-        o[1] = fmaf(o[1], corr, p * to_f<T>(V[off + d0 + 1]));
+        for (int d = 0; d < N; ++d) o[d] = fmaf(o[d], corr, p * to_f<T>(V[off + d0 + d]));
     }
     const float inv = l > 0.f ? 1.f / l : l;
-    o[0] *= inv;
-    o[1] *= inv;
+    for (int d = 0; d < N; ++d) o[d] *= inv;
 }
 
 template <typename T> __device__ __forceinline__ void store2(T* p, float x, float y);
@@ -221,21 +222,30 @@ struct CaNote {
     int c, l, g, rt, n, first, whole;  // the item; positions held; whether the CTA has its first part, all of them
 };
 
-// Dimensions d, d + 1 of a row from its O and sum.  (The pools' pointers are their layer's and head's.)
+// N dimensions from d of a row, from its O and sum, ready to be stored.  (The pools' pointers are their layer's and head's.)
+template <typename T, int HD, int N>
+__device__ __forceinline__ void finish_row(const CaArgs& a, size_t kv, int c, int n, int row, int d, const T* K, const T* V, float (&o)[N], float l) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;  // no key that counts: 0
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        o[i] *= inv;
+        bad |= !isfinite(o[i]);
+    }
+    if (a.n_tok > 1 && bad) {
+        float w[N];
+        row_again<T, HD, N>(a, static_cast<const T*>(a.Q) + (kv * a.R + row) * HD, K, V, a.v.table + (size_t)c * a.v.width,
+                            n - a.n_tok + row % a.n_tok + 1, d, w);
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] = w[i];
+    }
+}
 template <typename T, int HD>
 __device__ __forceinline__ void write_row(const CaArgs& a, size_t kv, int c, int n, int row, int d, const T* K, const T* V, float o0,
                                           float o1, float l) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;  // no key that counts: 0
-    o0 *= inv;
-    o1 *= inv;
-    const size_t at = kv * a.R + row;
-    if (a.n_tok > 1 && (!isfinite(o0) || !isfinite(o1))) {
-        float w[2];
-        row_again<T, HD>(a, static_cast<const T*>(a.Q) + at * HD, K, V, a.v.table + (size_t)c * a.v.width, n - a.n_tok + row % a.n_tok + 1, d, w);
-        o0 = w[0];
-        o1 = w[1];
-    }
-    store2<T>(static_cast<T*>(a.out) + at * HD + d, o0, o1);
+    float o[2] = {o0, o1};
+    finish_row<T, HD, 2>(a, kv, c, n, row, d, K, V, o, l);
+    store2<T>(static_cast<T*>(a.out) + (kv * a.R + row) * HD + d, o[0], o[1]);
 }
 
 // log2 of the sum of exp of a row, +inf where nothing counts (its weights are then 0)
@@ -477,9 +487,10 @@ struct CaCores {
 // ---------------------------------------------------------------- tensor cores: bf16
 // A block's keys and values come by TMA, whose box is the positions of a page in the block (a swizzled row of 64 dimensions
 // each), into a ring that belongs to one warp: a lane looks up a page and starts its copies, the warp waits for the
-// stage, and what it has read is free for the next copy without another warp's say.  16 rows (a row tile) are the M of
-// m16n8k16: S = Q K^T by ldmatrix from the key rows, P from S's registers, O += P V by transposed ldmatrix.  A 128-row
-// tcgen05 tile would be 1/32 full for the four heads that usually share a KV head; what bounds this kernel is the bytes.
+// stage, and what it has read is free for the next copy without another warp's say.  The keys are the M of m16n8k16 and
+// the rows its N, 8 or 16 of them: S^T = K Q^T by ldmatrix from the key rows, P^T turned in registers (movmatrix), and
+// O^T += V^T P^T by transposed ldmatrix.  (The rows as M would have 12 of 16 unused where four heads share a KV head, and a
+// 128-row tcgen05 tile 124; what bounds this kernel is the bytes, and at short contexts the chain of a block's steps.)
 __device__ __forceinline__ void ca_mma(float (&d)[4], const uint32_t (&A)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -498,11 +509,17 @@ __device__ __forceinline__ void ca_ldmatrix(uint32_t (&r)[4], uint32_t addr) {
                      : "r"(addr)
                      : "memory");
 }
+// an 8 x 8 matrix of 16-bit elements, two of a row a lane, transposed
+__device__ __forceinline__ uint32_t ca_transpose(uint32_t x) {
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
 
-template <int HD_>
+template <int HD_, int NT>
 struct CaTensor {
     using T = bf16;
-    static constexpr int HD = HD_, ROWS = 16, CTAS = 2;
+    static constexpr int HD = HD_, ROWS = 8 * NT, CTAS = 2;
     static constexpr int SK = HD == 64 ? 32 : 16, SPB = KB / SK;  // keys of a stage, stages of a block
     static constexpr int SLAB = SK * 128, TILE = HD / 64 * SLAB, STAGE = 2 * TILE;  // 64 dimensions of the keys; keys; both
     static constexpr int NS = 3;
@@ -543,46 +560,57 @@ struct CaTensor {
     // piece's next 32.
     struct Feed {
         CaWalk w;
+        int box_log2, copies;  // positions of a copy, copies of a stage
         int i = 0, n = 0, batch = 0, page = 0;
-        bool more = true;
-        __device__ Feed(const CaArgs& a) : w(a) {}
+        __device__ Feed(const CaArgs& a) : w(a) {
+            box_log2 = min(a.v.page_log2, SK == 32 ? 5 : 4);
+            copies = SK >> box_log2;
+        }
     };
-    __device__ __forceinline__ bool feed(const CaArgs& a, Feed& f, int s) {
-        const int lane = threadIdx.x & 31, mask = (1 << a.v.page_log2) - 1;
-        const int box = min(mask + 1, SK), copies = SK / box, copies_log2 = 31 - __clz(copies);  // positions of a copy; of a stage
+    __device__ __forceinline__ void feed(const CaArgs& a, Feed& f, int s) {
+        const int lane = threadIdx.x & 31;
         while (f.i == f.n) {
-            if (!f.more || !(f.more = f.w.next(a))) return false;
+            if (!f.w.next(a)) return;
             f.i = 0;
             f.n = stages(f.w);
-            f.batch = INT_MIN;
+            f.batch = f.i - 32;
         }
-        if (f.batch == INT_MIN || f.i - f.batch == 32 >> copies_log2) {
+        if ((f.i - f.batch) * f.copies >= 32) {
             f.batch = f.i;
-            const int i = f.i + (lane >> copies_log2), j = i < f.n ? key0(f.w, i) + (lane & (copies - 1)) * box : INT_MAX;
+            const int copies_log2 = (SK == 32 ? 5 : 4) - f.box_log2, i = f.i + (lane >> copies_log2);
+            const int j = i < f.n ? key0(f.w, i) + ((lane & (f.copies - 1)) << f.box_log2) : INT_MAX;
             f.page = j < f.w.r.n ? __ldg(a.v.table + (size_t)f.w.c * a.v.width + (j >> a.v.page_log2)) : 0;
         }
-        int page = __shfl_sync(0xffffffffu, f.page, ((f.i - f.batch) << copies_log2) + (lane & (copies - 1)));
-        const int j = key0(f.w, f.i) + lane * box;
-        const bool mine = lane < copies && j < f.w.r.n;
-        const uint32_t who = __ballot_sync(0xffffffffu, mine);
-        if (lane == 0) mbar_expect_tx(bars + 8 * s, __popc(who) * box * HD * 4);
-        __syncwarp();
-        if (mine) {
+        const int j0 = key0(f.w, f.i), box = 1 << f.box_log2, live = min(f.copies, (f.w.r.n - j0 + box - 1) >> f.box_log2);
+        int page = __shfl_sync(0xffffffffu, f.page, (f.i - f.batch) * f.copies + lane);
+        if (lane == 0) mbar_expect_tx(bars + 8 * s, live * box * HD * 4);
+        if (f.copies > 1) __syncwarp();
+        if (lane < live) {
             if ((unsigned)page >= (unsigned)a.v.n_pages) {  // some page instead: what comes of it is an error's
                 cache_fail(a.v.status, DS_CACHE_PAGE);
                 page = 0;
             }
             const uint32_t dst = ring + s * STAGE + lane * box * 128;
+            const int at = (j0 + lane * box) & ((1 << a.v.page_log2) - 1);
             const int l = a.v.s_layer ? f.w.l : 0, g = a.v.s_head ? f.w.g : 0;  // what is shared has one element in the maps
 #pragma unroll
             for (int kb = 0; kb < HD / 64; ++kb) {
-                tma_load_5d(dst + kb * SLAB, &tmK, bars + 8 * s, 64 * kb, j & mask, g, page, l);
-                tma_load_5d(dst + TILE + kb * SLAB, &tmV, bars + 8 * s, 64 * kb, j & mask, g, page, l);
+                tma_load_5d(dst + kb * SLAB, &tmK, bars + 8 * s, 64 * kb, at, g, page, l);
+                tma_load_5d(dst + TILE + kb * SLAB, &tmV, bars + 8 * s, 64 * kb, at, g, page, l);
             }
         }
+        __syncwarp();
         ++f.i;
-        return true;
     }
+
+    // A warp's rows of an item and what it has of them.  Lane 4 gq + t has Q of row 8 i + gq, and S, O and the sums of rows
+    // 8 i + 2 t and + 1.
+    struct Rows {
+        uint32_t q[NT][HD / 16][2];
+        float o[NT][HD / 16][4];
+        float m[NT][2], l[NT][2], lx[NT][2];
+        int vis[NT][2];
+    };
 
     __device__ __forceinline__ void run(const CaArgs& a, CaNote* notes) {
         using P = Part<HD, ROWS>;
@@ -591,36 +619,37 @@ struct CaTensor {
         Feed ahead(a);
         CaWalk w = ahead.w;
         int slot = 0, phase = 0;  // of the stage to be read next
-        for (int s = 0; s < NS - 1; ++s)
-            if (!feed(a, ahead, s)) break;
+        for (int s = 0; s < NS - 1; ++s) feed(a, ahead, s);
         bool ok = true;
         while (ok && w.next(a)) {
             const CaRange& r = w.r;
             const int row0 = w.rt * ROWS, rows = min(ROWS, a.R - row0), n = stages(w);
             const size_t kv = w.kv(a);
-            // rows gq and gq + 8 of the tile
-            uint32_t qa[HD / 16][4];
-            int vis[2];
+            Rows x;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int row = row0 + min(gq + 8 * h, rows - 1);
-                const bool live = gq + 8 * h < rows;
-                vis[h] = live ? r.n - a.n_tok + row % a.n_tok + 1 : 0;
-                const uint32_t* q = reinterpret_cast<const uint32_t*>(static_cast<const bf16*>(a.Q) + (kv * a.R + row) * HD) + t;
+            for (int i = 0; i < NT; ++i) {
+                const bool live = 8 * i + gq < rows;
+                const uint32_t* q =
+                    reinterpret_cast<const uint32_t*>(static_cast<const bf16*>(a.Q) + (kv * a.R + row0 + (live ? 8 * i + gq : 0)) * HD) + t;
 #pragma unroll
                 for (int k = 0; k < HD / 16; ++k) {
-                    qa[k][h] = live ? __ldg(q + 8 * k) : 0;
-                    qa[k][2 + h] = live ? __ldg(q + 8 * k + 4) : 0;
+                    x.q[i][k][0] = live ? __ldg(q + 8 * k) : 0;
+                    x.q[i][k][1] = live ? __ldg(q + 8 * k + 4) : 0;
+                    x.o[i][k][0] = x.o[i][k][1] = x.o[i][k][2] = x.o[i][k][3] = 0.f;
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int row = 8 * i + 2 * t + h;
+                    x.m[i][h] = -INFINITY;
+                    x.l[i][h] = x.lx[i][h] = 0.f;
+                    x.vis[i][h] = row < rows ? r.n - a.n_tok + (a.n_tok == 1 ? 0 : (row0 + row) % a.n_tok) + 1 : 0;
                 }
             }
-            float o[HD / 8][4], m[2] = {-INFINITY, -INFINITY}, lr[2] = {0.f, 0.f}, lx[2] = {0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < HD / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
             for (int i = 0; i < n; ++i) {
                 feed(a, ahead, slot == 0 ? NS - 1 : slot - 1);  // the slot that was read last
                 ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * slot, phase, a.v.status));
                 if (!ok) break;
-                step(a, r, key0(w, i), ring + slot * STAGE, kv, row0, rows, vis, k2, qa, o, m, lr, lx);
+                step(a, r, key0(w, i), ring + slot * STAGE, kv, row0, rows, k2, x);
                 __syncwarp();  // the stage has been read
                 if (++slot == NS) {
                     slot = 0;
@@ -632,40 +661,44 @@ struct CaTensor {
             if (!w.whole && lane == 0) notes[w.b0 == 0] = {part, w.c, w.l, w.g, w.rt, r.n, w.first, w.cta_whole};
             const long long head = w.l * a.v.s_layer + w.g * a.v.s_head;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int i = 0; i < NT; ++i)
 #pragma unroll
-                for (int x = 1; x < 4; x <<= 1) {
-                    lr[h] += __shfl_xor_sync(0xffffffffu, lr[h], x);
-                    lx[h] += __shfl_xor_sync(0xffffffffu, lx[h], x);
-                }
-                const int row = gq + 8 * h;
-                if (row >= rows) continue;
-                if (w.whole) {
+                for (int h = 0; h < 2; ++h) {
+                    float l = x.l[i][h], lx = x.lx[i][h];
 #pragma unroll
-                    for (int j = 0; j < HD / 8; ++j)
-                        write_row<bf16, HD>(a, kv, w.c, r.n, row0 + row, 8 * j + 2 * t, static_cast<const bf16*>(a.v.K) + head,
-                                            static_cast<const bf16*>(a.v.V) + head, o[j][2 * h], o[j][2 * h + 1], lr[h]);
-                    if (t == 0 && a.lse) a.lse[kv * a.R + row0 + row] = row_lse(m[h], lx[h], k2);
-                } else {
+                    for (int y = 4; y < 32; y <<= 1) {
+                        l += __shfl_xor_sync(0xffffffffu, l, y);
+                        lx += __shfl_xor_sync(0xffffffffu, lx, y);
+                    }
+                    const int row = 8 * i + 2 * t + h;
+                    if (row >= rows) continue;
+                    if (w.whole) {
+                        bf16* out = static_cast<bf16*>(a.out) + (kv * a.R + row0 + row) * HD;
 #pragma unroll
-                    for (int j = 0; j < HD / 8; ++j)
-                        *reinterpret_cast<float2*>(part + row * HD + 8 * j + 2 * t) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
-                    if (t == 0) {
-                        part[P::M + row] = m[h];
-                        part[P::L + row] = lr[h];
-                        part[P::LX + row] = lx[h];
+                        for (int d = 0; d < HD / 8; ++d) {
+                            float v[1] = {x.o[i][d / 2][d % 2 * 2 + h]};
+                            finish_row<bf16, HD, 1>(a, kv, w.c, r.n, row0 + row, 8 * d + gq, static_cast<const bf16*>(a.v.K) + head,
+                                                    static_cast<const bf16*>(a.v.V) + head, v, l);
+                            out[8 * d + gq] = __float2bfloat16_rn(v[0]);
+                        }
+                        if (gq == 0 && a.lse) a.lse[kv * a.R + row0 + row] = row_lse(x.m[i][h], lx, k2);
+                    } else {
+#pragma unroll
+                        for (int d = 0; d < HD / 8; ++d) part[row * HD + 8 * d + gq] = x.o[i][d / 2][d % 2 * 2 + h];
+                        if (gq == 0) {
+                            part[P::M + row] = x.m[i][h];
+                            part[P::L + row] = l;
+                            part[P::LX + row] = lx;
+                        }
                     }
                 }
-            }
             __syncwarp();
         }
         if (!ok) drain_copies();
     }
 
     // One stage's keys
-    __device__ __forceinline__ void step(const CaArgs& a, const CaRange& r, int j0, uint32_t ks, size_t kv, int row0, int rows, const int (&vis)[2],
-                                         float k2, const uint32_t (&qa)[HD / 16][4], float (&o)[HD / 8][4], float (&m)[2], float (&lr)[2],
-                                         float (&lx)[2]) {
+    __device__ __forceinline__ void step(const CaArgs& a, const CaRange& r, int j0, uint32_t ks, size_t kv, int row0, int rows, float k2, Rows& x) {
         const int lane = threadIdx.x & 31, gq = lane >> 2, t = lane & 3;
         const uint32_t vs = ks + TILE;
         const bool whole = j0 + SK <= r.n - a.n_tok + 1 && (j0 + SK <= a.n_sink || j0 >= r.n - a.window);
@@ -680,89 +713,98 @@ struct CaTensor {
             fence_proxy_async_smem();
             __syncwarp();
         }
-        float s[SK / 8][4];
+        float s[NT][SK / 16][4];  // of keys 16 u + gq (0, 1) and + 8 (2, 3), rows 2 t and + 1
 #pragma unroll
-        for (int nt = 0; nt < SK / 8; ++nt) {
-            s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+        for (int u = 0; u < SK / 16; ++u)
 #pragma unroll
-            for (int k = 0; k < HD / 32; ++k) {
-                uint32_t b[4];
-                ca_ldmatrix<false>(b, ks + at(8 * nt + (lane & 7), 4 * k + (lane >> 3)));
-                ca_mma(s[nt], qa[2 * k], b[0], b[1]);
-                ca_mma(s[nt], qa[2 * k + 1], b[2], b[3]);
+            for (int i = 0; i < NT; ++i) s[i][u][0] = s[i][u][1] = s[i][u][2] = s[i][u][3] = 0.f;
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k)
+#pragma unroll
+            for (int u = 0; u < SK / 16; ++u) {
+                uint32_t A[4];
+                ca_ldmatrix<false>(A, ks + at(16 * u + (lane & 15), 2 * k + (lane >> 4)));
+#pragma unroll
+                for (int i = 0; i < NT; ++i) ca_mma(s[i][u], A, x.q[i][k][0], x.q[i][k][1]);
             }
-        }
-        if (!whole) {
+        uint32_t pb[NT][SK / 16][2];  // P^T: keys 16 u + 2 t, + 1 (and + 8) of row gq
 #pragma unroll
-            for (int nt = 0; nt < SK / 8; ++nt)
+        for (int i = 0; i < NT; ++i) {
+            if (!whole) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int key = j0 + 8 * nt + 2 * t + (e & 1), h = e >> 1;
-                    s[nt][e] = key < vis[h] && (key < a.n_sink || key >= vis[h] - a.window) ? s[nt][e] : -INFINITY;
-                }
-        }
-        if (a.z2) {
+                for (int u = 0; u < SK / 16; ++u)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (gq + 8 * h < rows) {
-                    float* z = a.z2 + (kv * a.R + row0 + gq + 8 * h) * a.pitch + j0 + 2 * t;
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = j0 + 16 * u + gq + 8 * (e >> 1), v = x.vis[i][e & 1];
+                        s[i][u][e] = key < v && (key < a.n_sink || key >= v - a.window) ? s[i][u][e] : -INFINITY;
+                    }
+            }
+            if (a.z2) {
 #pragma unroll
-                    for (int nt = 0; nt < SK / 8; ++nt)
-                        *reinterpret_cast<float2*>(z + 8 * nt) = make_float2(s[nt][2 * h] * k2, s[nt][2 * h + 1] * k2);
-                }
-        }
-        float moff[2], corr[2];
+                for (int h = 0; h < 2; ++h)
+                    if (8 * i + 2 * t + h < rows) {
+                        float* z = a.z2 + (kv * a.R + row0 + 8 * i + 2 * t + h) * a.pitch + j0 + gq;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float cm = fmaxf(s[0][2 * h], s[0][2 * h + 1]);
-#pragma unroll
-            for (int nt = 1; nt < SK / 8; ++nt) cm = fmaxf(cm, fmaxf(s[nt][2 * h], s[nt][2 * h + 1]));
-            cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, 1));
-            cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, 2));
-            const float mn = fmaxf(m[h], cm);
-            corr[h] = mn == m[h] ? 1.f : ca_exp2((m[h] - mn) * k2);
-            moff[h] = mn == -INFINITY ? 0.f : -mn * k2;
-            m[h] = mn;
-        }
-        if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+                        for (int u = 0; u < SK / 16; ++u) {
+                            z[16 * u] = s[i][u][h] * k2;
+                            z[16 * u + 8] = s[i][u][2 + h] * k2;
+                        }
+                    }
+            }
+            float moff[2], corr[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                lr[h] *= corr[h];
-                lx[h] *= corr[h];
+                float cm = fmaxf(s[i][0][h], s[i][0][2 + h]);
+#pragma unroll
+                for (int u = 1; u < SK / 16; ++u) cm = fmaxf(cm, fmaxf(s[i][u][h], s[i][u][2 + h]));
+#pragma unroll
+                for (int y = 4; y < 32; y <<= 1) cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, y));
+                const float mn = fmaxf(x.m[i][h], cm);
+                corr[h] = mn == x.m[i][h] ? 1.f : ca_exp2((x.m[i][h] - mn) * k2);
+                moff[h] = mn == -INFINITY ? 0.f : -mn * k2;
+                x.m[i][h] = mn;
+            }
+            if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    x.l[i][h] *= corr[h];
+                    x.lx[i][h] *= corr[h];
+#pragma unroll
+                    for (int d = 0; d < HD / 16; ++d) {
+                        x.o[i][d][h] *= corr[h];
+                        x.o[i][d][2 + h] *= corr[h];
+                    }
+                }
             }
 #pragma unroll
-            for (int j = 0; j < HD / 8; ++j) {
-                o[j][0] *= corr[0];
-                o[j][1] *= corr[0];
-                o[j][2] *= corr[1];
-                o[j][3] *= corr[1];
-            }
+            for (int u = 0; u < SK / 16; ++u)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const float e0 = ca_exp2(fmaf(s[i][u][2 * half], k2, moff[0])), e1 = ca_exp2(fmaf(s[i][u][2 * half + 1], k2, moff[1]));
+                    const uint32_t p = pack_bf16(e0, e1);
+                    // O's sums take the probabilities that the MMA sees, the weights' the exact ones
+                    x.l[i][0] += __uint_as_float(p << 16);
+                    x.l[i][1] += __uint_as_float(p & 0xffff0000u);
+                    x.lx[i][0] += e0;
+                    x.lx[i][1] += e1;
+                    pb[i][u][half] = ca_transpose(p);
+                }
         }
 #pragma unroll
-        for (int kk = 0; kk < SK / 16; ++kk) {
-            uint32_t pa[4];  // rows gq, gq + 8 x keys (2 t, 2 t + 1), then the same of the next eight keys
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int nt = 2 * kk + (q >> 1), h = q & 1;
-                const float e0 = ca_exp2(fmaf(s[nt][2 * h], k2, moff[h])), e1 = ca_exp2(fmaf(s[nt][2 * h + 1], k2, moff[h]));
-                pa[q] = pack_bf16(e0, e1);
-                // O's sum takes the probabilities the MMA sees, the weights' the exact ones
-                lr[h] += __uint_as_float(pa[q] << 16) + __uint_as_float(pa[q] & 0xffff0000u);
-                lx[h] += e0 + e1;
-            }
+        for (int u = 0; u < SK / 16; ++u)
 #pragma unroll
             for (int d = 0; d < HD / 16; ++d) {
-                uint32_t b[4];
-                ca_ldmatrix<true>(b, vs + at(16 * kk + (lane & 15), 2 * d + (lane >> 4)));
-                ca_mma(o[2 * d], pa, b[0], b[1]);
-                ca_mma(o[2 * d + 1], pa, b[2], b[3]);
+                uint32_t A[4];
+                ca_ldmatrix<true>(A, vs + at(16 * u + (lane & 7) + ((lane >> 4) << 3), 2 * d + ((lane >> 3) & 1)));
+#pragma unroll
+                for (int i = 0; i < NT; ++i) ca_mma(x.o[i][d], A, pb[i][u][0], pb[i][u][1]);
             }
-        }
     }
 };
 
 // ---------------------------------------------------------------- joining the parts, and the weights
-constexpr int FIN_THREADS = 256, FIN_WARPS = FIN_THREADS / 32, FIN_POS = 4 * FIN_THREADS;
+constexpr int FIN_THREADS = 256, FIN_WARPS = FIN_THREADS / 32;
+constexpr int FIN_TILE = 4 * FIN_THREADS, FIN_TILES = 4, FIN_POS = FIN_TILES * FIN_TILE;  // positions at a time, times, of a block
 
 // One row of a split item from its parts, of CTAs first .. first + n - 1.  A thread has two dimensions of every G-th part;
 // the G sums are added in order.
@@ -801,7 +843,7 @@ __device__ __forceinline__ void join_row(const CaArgs& a, int c, int row, size_t
 }
 
 // The first R blocks of a KV head join its rows' parts; the others, if the cache has weights, add those of FIN_POS positions
-// each, four a thread.
+// each, four a thread at a time.
 template <typename Form>
 __global__ void __launch_bounds__(FIN_THREADS, 5) cache_finish_kernel(const CaArgs a) {
     using T = typename Form::T;
@@ -824,8 +866,7 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) cache_finish_kernel(const CaAr
         join_row<T, HD, ROWS>(a, c, row, kv, static_cast<const T*>(a.v.K) + head, static_cast<const T*>(a.v.V) + head, r.n, first, n, k2);
         return;
     }
-    float w[4] = {0.f, 0.f, 0.f, 0.f};
-    const bool any = p0 < r.n && !(p0 >= a.n_sink && p0 + 4 <= r.t0 - a.window + 1);
+    float* score = a.v.score + (((size_t)c * a.v.Lh + l) * a.v.n_kv + g) * a.v.cap;
     for (int row0 = 0; row0 < a.R; row0 += FIN_ROWS) {
         const int rows = min(FIN_ROWS, a.R - row0);
         __syncthreads();
@@ -852,24 +893,25 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) cache_finish_kernel(const CaAr
             if (lane == 0) lse[row] = m;
         }
         __syncthreads();
-        if (!any) continue;
-        const float* z = a.z2 + (kv * a.R + row0) * a.pitch + p0;
+#pragma unroll 2
+        for (int tile = 0; tile < FIN_TILES; ++tile) {
+            const int p = p0 + tile * FIN_TILE;
+            if (p >= r.n || (p >= a.n_sink && p + 4 <= r.t0 - a.window + 1)) continue;
+            float w[4] = {0.f, 0.f, 0.f, 0.f};
+            const float* z = a.z2 + (kv * a.R + row0) * a.pitch + p;
 #pragma unroll 4
-        for (int row = 0; row < rows; ++row) {
-            const float4 x = __ldcs(reinterpret_cast<const float4*>(z + row * a.pitch));
-            const float s = lse[row];
-            w[0] += ca_exp2(x.x - s);
-            w[1] += ca_exp2(x.y - s);
-            w[2] += ca_exp2(x.z - s);
-            w[3] += ca_exp2(x.w - s);
-        }
-    }
-    if (!any) return;
-    float* score = a.v.score + (((size_t)c * a.v.Lh + l) * a.v.n_kv + g) * a.v.cap;
+            for (int row = 0; row < rows; ++row) {
+                const float4 x = __ldcs(reinterpret_cast<const float4*>(z + row * a.pitch));
+                const float s = lse[row];
+                w[0] += ca_exp2(x.x - s);
+                w[1] += ca_exp2(x.y - s);
+                w[2] += ca_exp2(x.z - s);
+                w[3] += ca_exp2(x.w - s);
+            }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int p = p0 + i;
-        if (p < r.n && (p < a.n_sink || p > r.t0 - a.window)) score[p] += w[i];
+            for (int i = 0; i < 4; ++i)
+                if (p + i < r.n && (p + i < a.n_sink || p + i > r.t0 - a.window)) score[p + i] += w[i];
+        }
     }
 }
 
@@ -911,7 +953,7 @@ bool pool_maps(const CacheView& v, CUtensorMap* mk, CUtensorMap* mv) {
         const uint64_t d[5] = {HD, page, v.s_head ? (uint64_t)v.n_kv : 1, (uint64_t)v.n_pages, v.s_layer ? (uint64_t)v.L : 1};
         const uint64_t s3 = v.s_pos * 2;
         const uint64_t s[4] = {s3, d[2] > 1 ? v.s_head * 2 : s3, d[3] > 1 ? v.s_page * 2 : s3, d[4] > 1 ? v.s_layer * 2 : s3};
-        const uint32_t b[5] = {64, (uint32_t)std::min<uint64_t>(page, CaTensor<HD>::SK), 1, 1, 1};
+        const uint32_t b[5] = {64, (uint32_t)std::min<uint64_t>(page, CaTensor<HD, 1>::SK), 1, 1, 1};
         plan.key[0] = 0;
         if (!encode_map_bf16_5d(&plan.m, v.K, d, s, b)) return false;  // strides past a tensor map's range (2^40 bytes)
         std::copy(key, key + 8, plan.key);
@@ -925,7 +967,7 @@ template <int HD>
 cudaError_t launch_bf16(const CaArgs& a, int sms, cudaStream_t st) {
     CUtensorMap mk = {}, mv = {};
     // pages of fewer than 8 positions would need copies of less than a swizzle's rows
-    if (a.vec && a.v.page_log2 >= 3 && pool_maps<HD>(a.v, &mk, &mv)) return launch<CaTensor<HD>>(a, mk, mv, sms, st);
+    if (a.vec && a.v.page_log2 >= 3 && pool_maps<HD>(a.v, &mk, &mv)) return a.R <= 8 ? launch<CaTensor<HD, 1>>(a, mk, mv, sms, st) : launch<CaTensor<HD, 2>>(a, mk, mv, sms, st);
     return launch<CaCores<bf16, HD>>(a, mk, mv, sms, st);
 }
 
