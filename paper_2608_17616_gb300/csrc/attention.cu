@@ -15,14 +15,14 @@
 // are reduced once per item, and the probabilities pass through shared memory into the
 // value accumulation, where a lane owns hd / 32 dimensions.
 //
-// The windowed attention (mone_window_attention) is the WIN instance of each form: of the positions up to its
-// own, a token sees the first n_sink and the last `window`.  A form then steps over the chunks that hold some
-// row's visible keys only (WinRange), and masks within them.
+// The windowed attention (mone_window_attention) is the WIN instance of the decode and CUDA-core forms, and a prefill
+// form of its own in attention_window.cu: of the positions up to its own, a token sees the first n_sink and the last
+// `window`.  A form then steps over the chunks that hold some row's visible keys only (WinRange), and masks within them.
 #include <algorithm>
 #include <cfloat>
 #include <mutex>
 
-#include "mone_common.cuh"
+#include "attention_common.cuh"
 #include "per_device.h"
 
 namespace mone {
@@ -33,32 +33,6 @@ constexpr int ATT_WARPS = 8;
 constexpr int ATT_ITEMS = 64;                 // (query head, token) items per CTA
 constexpr int MAXI = ATT_ITEMS / ATT_WARPS;   // items per warp
 constexpr int KC = 64;                        // cache positions per shared-memory chunk
-
-struct AttnArgs {
-    const void* Q;          // [C][n_q][Lq][hd]
-    const void *K, *V;      // caches, element strides s0 (context), s1 (layer), s2 (head), s3 (position)
-    void* out;              // [C][n_q][Lq][hd]
-    long long s0, s1, s2, s3;
-    int L, n_q, n_kv, group, Lq, n_mem, rows;  // rows: query tokens per CTA (group * rows <= ATT_ITEMS)
-    float scale;            // 1 / sqrt(hd)
-    int tile_tok, per_block;  // decode form: tokens of a block, 16-row tiles that cut it
-    int group_inv;            // decode form: 65536 / group + 1
-    int n_sink, window;     // WIN: a token at position t sees j <= t with j < n_sink or j > t - window
-    int vec;                // caches 16-byte aligned (base and every stride): stage with 16-byte loads
-    int* status;            // device status word (bounded waits of the prefill form)
-};
-
-// The chunks of STEP positions that hold the keys of the tokens at positions t0 .. t1: those of the first
-// positions, then those from the first token's window on.  Every position is in one chunk at most.
-struct WinRange {
-    int ns, lo, n;  // chunks of the first positions; first position after them; chunks in all
-    __device__ WinRange(const AttnArgs& a, int t0, int t1, int step) {
-        ns = (min(a.n_sink, t1 + 1) + step - 1) / step;
-        lo = max(ns * step, t0 - a.window + 1);
-        n = ns + (lo <= t1 ? (t1 - lo) / step + 1 : 0);
-    }
-    __device__ int at(int j, int step) const { return j < ns ? j * step : lo + (j - ns) * step; }
-};
 
 // Stage cache positions [j0, j0 + nk) of one head into shared memory as fp32 rows of HD
 // values, `pitch` floats apart.
@@ -95,30 +69,6 @@ __device__ __forceinline__ void stage_rows(float* dst, const T* src, long long s
             dst[j * pitch + d] = to_f<T>(src[(long long)(j0 + j) * s3 + d]);
         }
     }
-}
-
-// Output dimensions d0, d0 + STEP, .. of one row over the keys it sees and no others, by one thread.  A tile's
-// products take a key's value row times a probability of 0 for the rows that do not see it, which is NaN where the
-// value is not finite; a row of the windowed attention with such a result is computed again here.  One pass with
-// a running maximum; slow, and reached by non-finite inputs only.
-template <typename T, int HD, int N, int STEP>
-__device__ __noinline__ void row_again(const T* q, const T* K, const T* V, long long s3, int vis, const AttnArgs& a, int d0, float* o) {
-    float m = -INFINITY, l = 0.f;
-    for (int d = 0; d < N; ++d) o[d] = 0.f;
-    for (int j = min(a.n_sink, vis) > 0 ? 0 : max(0, vis - a.window); j < vis; ++j) {
-        if (j >= a.n_sink && j < vis - a.window) j = vis - a.window;
-        if (j >= vis) break;
-        float z = 0.f;
-        for (int d = 0; d < HD; ++d) z = fmaf(to_f<T>(q[d]), to_f<T>(K[(long long)j * s3 + d]), z);
-        z *= a.scale;
-        if (z == -INFINITY) continue;
-        const float mn = fmaxf(m, z), corr = __expf(m - mn), p = __expf(z - mn);
-        m = mn;
-        l = fmaf(l, corr, p);
-        for (int d = 0; d < N; ++d) o[d] = fmaf(o[d], corr, p * to_f<T>(V[(long long)j * s3 + d0 + STEP * d]));
-    }
-    const float inv = l > 0.f ? 1.f / l : l;
-    for (int d = 0; d < N; ++d) o[d] *= inv;
 }
 
 template <typename T, int HD>
@@ -275,14 +225,6 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, 2) attention_kernel(const Attn
     }
 }
 
-// 2^x on the special-function unit (PTX ex2.approx), whose error is far below the bf16
-// rounding of the probabilities it feeds (the parity tests bound the result at 1e-2).
-__device__ __forceinline__ float at_exp2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 // ---------------------------------------------------------------- prefill form (bf16, tcgen05)
 // One CTA per (chain, key/value head, tile of query tokens), two CTAs an SM.  A tile's 128 MMA rows are
 // (query head of the group, token) pairs, rt = 128 / group tokens of each of the group's heads, so
@@ -346,7 +288,7 @@ __device__ __forceinline__ float fa_probs(const float (&v)[N], uint64_t k2, uint
     return s.x + s.y;
 }
 
-template <int HD, bool WIN>
+template <int HD>
 __global__ void __launch_bounds__(FaSmem<HD>::THREADS, 2)
 attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                          const __grid_constant__ CUtensorMap tmV, const AttnArgs a) {
@@ -390,14 +332,10 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
 
     // token tiles: the last first (causal: it has the most keys)
     const int c = blockIdx.z, g = blockIdx.y, rt = a.rows, r0 = (gridDim.x - 1 - blockIdx.x) * rt;
-    const int keys = a.n_mem + min(a.Lq, r0 + rt);  // keys the tile's last token sees
-    const WinRange win(a, a.n_mem + r0, keys - 1, NK);
-    const int n = WIN ? win.n : (keys + NK - 1) / NK;  // in chunks
-    auto pos = [&](int j) { return WIN ? win.at(j, NK) : j * NK; };  // first position of chunk j
+    const int keys = a.n_mem + min(a.Lq, r0 + rt), n = (keys + NK - 1) / NK;  // keys the tile's last token sees, in chunks
     // The last chunk may hold later tokens' rows (past the cache's last row TMA writes zeros). No probability of theirs is
     // added up, but 0 times a non-finite value would be: their value rows are cleared.
-    // (WIN: rows differ in what they see at both ends, and a row with a non-finite result is computed again instead.)
-    const bool clear = !WIN && keys < a.n_mem + a.Lq && keys < n * NK;
+    const bool clear = keys < a.n_mem + a.Lq && keys < n * NK;
 
     if (warp == SM::LOAD_WARP) {
         bool landed = false;
@@ -418,7 +356,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
                 mbar_expect_tx(full(s), SM::TILE);
 #pragma unroll
                 for (int kb = 0; kb < HD / 64; ++kb)
-                    tma_load_5d(dst + kb * SM::SLAB, m, full(s), 64 * kb, pos(j), head, layer, ctx);
+                    tma_load_5d(dst + kb * SM::SLAB, m, full(s), 64 * kb, j * NK, head, layer, ctx);
                 if (++s == NS) {
                     s = 0;
                     ph ^= 1;
@@ -518,16 +456,8 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
                 tmem_ld48(t_s + half * NE, v);
             else
                 tmem_ld32(t_s + half * NE, v);
-            if constexpr (WIN) {
-                const int p0 = pos(j);
-                // some row does not see the whole chunk (in the window of all: from the last token's first key on)
-                if (p0 + NK > a.n_mem + r0 + 1 || (p0 + NK > a.n_sink && p0 < keys - a.window)) {
-                    const int at = p0 + half * NE, nv = vis - at, nw = vis - a.window - at, ns = a.n_sink - at;
-#pragma unroll
-                    for (int u = 0; u < NE; ++u) v[u] = u < nv && (u >= nw || u < ns) ? v[u] : -INFINITY;
-                }
-            } else if ((j + 1) * NK > a.n_mem + r0 + 1) {  // some row does not see the whole chunk:
-                const int nv = vis - j * NK - half * NE;     // a hidden key's score of -inf gives it a probability of 0
+            if ((j + 1) * NK > a.n_mem + r0 + 1) {      // some row does not see the whole chunk:
+                const int nv = vis - j * NK - half * NE;  // a hidden key's score of -inf gives it a probability of 0
 #pragma unroll
                 for (int u = 0; u < NE; ++u) v[u] = u < nv ? v[u] : -INFINITY;
             }
@@ -581,33 +511,13 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         ok = named_bar_and(1 + quarter, 64, ok);
         if (ok) {
             tc_fence_after();
-            const float sum = l + x[(half ^ 1) * 128 + row];
-            const float inv = WIN && sum == 0.f ? 0.f : 1.f / sum;
+            const float inv = 1.f / (l + x[(half ^ 1) * 128 + row]);
             bf16* orow = static_cast<bf16*>(a.out) +
                          (((size_t)c * a.n_q + g * a.group + (live ? hr : 0)) * a.Lq + (live ? i : 0)) * HD + half * (HD / 2);
 #pragma unroll
             for (int cb = 0; cb < HD / 2; cb += 32) {
                 float v[32];
-                if constexpr (WIN) __syncwarp();  // the threads of rows computed again
                 tmem_ld32(t_o + cb, v);
-                if constexpr (WIN) {
-                    bool bad = false;
-#pragma unroll
-                    for (int u = 0; u < 32; ++u) bad |= !isfinite(v[u] * inv);
-                    if (live && bad) {
-                        const long long kv_off = (long long)(c / a.L) * a.s0 + (long long)(c % a.L) * a.s1 + (long long)g * a.s2;
-                        float w[32];  // its own: the address of v would put it in local memory
-                        row_again<bf16, HD, 32, 1>(static_cast<const bf16*>(a.Q) + (orow - static_cast<bf16*>(a.out)) - half * (HD / 2),
-                                                   static_cast<const bf16*>(a.K) + kv_off, static_cast<const bf16*>(a.V) + kv_off, a.s3,
-                                                   vis, a, half * (HD / 2) + cb, w);
-#pragma unroll
-                        for (int u = 0; u < 32; u += 8)
-                            *reinterpret_cast<uint4*>(orow + cb + u) =
-                                make_uint4(pack_bf16(w[u], w[u + 1]), pack_bf16(w[u + 2], w[u + 3]), pack_bf16(w[u + 4], w[u + 5]),
-                                           pack_bf16(w[u + 6], w[u + 7]));
-                        continue;
-                    }
-                }
                 if (live) {
 #pragma unroll
                     for (int u = 0; u < 32; u += 8)
@@ -905,10 +815,10 @@ cudaError_t launch_t(const AttnArgs& a, int C, cudaStream_t st) {
     return cudaGetLastError();
 }
 
-template <int HD, bool WIN>
+template <int HD>
 cudaError_t launch_prefill(AttnArgs a, int n_ctx, int C, cudaStream_t st) {
     static PerDevice<SmemOptIn> once;
-    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(attention_prefill_kernel<HD, WIN>), FaSmem<HD>::DYN, once);
+    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(attention_prefill_kernel<HD>), FaSmem<HD>::DYN, once);
     if (e != cudaSuccess) return e;
     // The maps of the last call's shape, of which a call only sets the addresses: three maps encoded anew are 0.5 us of
     // the 9 us that a short call takes on the host
@@ -930,14 +840,14 @@ cudaError_t launch_prefill(AttnArgs a, int n_ctx, int C, cudaStream_t st) {
         const uint32_t kb[5] = {64, FaSmem<HD>::NK, 1, 1, 1};
         plan.key[0] = 0;
         if (!encode_map_bf16_4d(&plan.q, a.Q, qd, qs, qb) || !encode_map_bf16_5d(&plan.kv, a.K, kd, ks, kb))
-            return launch_t<bf16, HD, WIN>(a, C, st);  // strides past a tensor map's range (2^40 bytes): the CUDA-core form
+            return launch_t<bf16, HD, false>(a, C, st);  // strides past a tensor map's range (2^40 bytes): the CUDA-core form
         std::copy(key, key + 10, plan.key);
     }
     CUtensorMap mq = plan.q, mk = plan.kv, mv = plan.kv;
     if (!retarget_map(&mq, a.Q) || !retarget_map(&mk, a.K) || !retarget_map(&mv, a.V)) return cudaErrorInvalidValue;
     a.rows = rows;
     dim3 grid((a.Lq + a.rows - 1) / a.rows, a.n_kv, C);
-    attention_prefill_kernel<HD, WIN><<<grid, FaSmem<HD>::THREADS, FaSmem<HD>::DYN, st>>>(mq, mk, mv, a);
+    attention_prefill_kernel<HD><<<grid, FaSmem<HD>::THREADS, FaSmem<HD>::DYN, st>>>(mq, mk, mv, a);
     return cudaGetLastError();
 }
 
@@ -992,7 +902,12 @@ cudaError_t launch(const DevState& s, AttnArgs a, int n_ctx, cudaStream_t st) {
         const long long row_tiles = ((long long)a.group * a.Lq + DE_ROWS - 1) / DE_ROWS;
         if (row_tiles == 1 || row_tiles * a.n_kv * C <= DE_MAX_TILES)
             return s.hd == 64 ? launch_decode<64, WIN>(a, C, s.sms, st) : launch_decode<128, WIN>(a, C, s.sms, st);
-        return s.hd == 64 ? launch_prefill<64, WIN>(a, n_ctx, C, st) : launch_prefill<128, WIN>(a, n_ctx, C, st);
+        if constexpr (WIN) {
+            const cudaError_t e = launch_window_prefill(a, s.hd, n_ctx, C, s.sms, st);
+            if (e != cudaErrorNotSupported) return e;
+        } else {
+            return s.hd == 64 ? launch_prefill<64>(a, n_ctx, C, st) : launch_prefill<128>(a, n_ctx, C, st);
+        }
     }
     return s.hd == 64 ? launch_t<bf16, 64, WIN>(a, C, st) : launch_t<bf16, 128, WIN>(a, C, st);
 }

@@ -177,15 +177,20 @@ def test_keys_at_minus_infinity_count_for_nothing():
         assert rel_fro(out[0, 0].float().cpu(), ref) <= 5e-3
 
 
-def test_many_tiles_repeat_bit_for_bit():
-    n_kv, group, hd, Lq, n_past, L = 8, 4, 128, 400, 64, 16
+@pytest.mark.parametrize("hd,n_sink,window", [(64, 64, 100), (128, 64, 100), (64, 0, 7), (128, 130, 300)])
+def test_many_tiles_of_a_cta(hd, n_sink, window):
+    """Five tiles and more for each CTA of the many-rows form: right, and the same bits again."""
+    n_kv, group, Lq, n_past, L = 8, 4, 400, 64, 16
     run = handle(L, n_kv, hd, torch.bfloat16)
     g = torch.Generator(device="cuda").manual_seed(3)
     K, V = (torch.randn(1, L, n_kv, n_past + Lq, hd, generator=g, device="cuda").bfloat16() for _ in range(2))
     Q = torch.randn(1, L, group * n_kv, Lq, hd, generator=g, device="cuda").bfloat16()
     outs = [torch.full_like(Q, 7.0) for _ in range(2)]
     for i in range(40):
-        mone.mone_window_attention(run.h, -1, Q, group * n_kv, Lq, K, V, K.stride()[:4], n_past, 64, 100, outs[i % 2])
+        mone.mone_window_attention(run.h, -1, Q, group * n_kv, Lq, K, V, K.stride()[:4], n_past, n_sink, window, outs[i % 2])
     mone.mone_mem_sync(run.h)
     run.close()
     assert torch.equal(*outs)
+    for layer in (0, 9, L - 1):
+        ref, _ = O.window_attention(Q[0, layer].float().cpu(), K[0, layer].float().cpu(), V[0, layer].float().cpu(), n_past, n_sink, window)
+        assert rel_fro(outs[0][0, layer].float().cpu(), ref) <= 5e-3, layer
