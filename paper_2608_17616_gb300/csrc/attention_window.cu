@@ -2,11 +2,17 @@
 //
 // A tile is 128 MMA rows: rt = 128 / group tokens of each of a KV head's `group` query heads, which share every staged key
 // and value row.  A CTA, two an SM, takes one tile after another.  Per chunk of NK keys: S = Q K^T into one of two TMEM
-// buffers, the softmax by one thread a row, whose bf16 probabilities go over the scores as the A operand of O += P V, O in TMEM.
-// Warps 0-3: the softmax, row = thread = TMEM lane, and the output.  Warp 4: the loader; keys and values by TMA with the caller's
-// strides through a ring of NS slots, the queries into a buffer of their own.  Warp 5: the MMA issuer, two chunks of S ahead of
-// P V.  Loads and S run on over the end of a tile (a window has few chunks, so a tile's first loads and last output would
-// otherwise cost as much as its chunks): the chunks of all tiles of a CTA are one sequence.
+// buffers, the softmax, whose bf16 probabilities go over the scores as the A operand of O += P V, O in TMEM.
+// Warps 0-7: the softmax and the output, two threads a row (= TMEM lane), one for each half of a chunk's keys and of the head's
+// dimensions.  Warp 8: the loader; keys and values by TMA with the caller's strides through a ring each, the queries into a
+// buffer of their own.  Warps 9 and 10: the MMA issuers, of S, two chunks ahead, and of P V.  Loads and S run on over the end of a
+// tile (a window has few chunks, so a tile's first loads and last output would otherwise cost as much as its
+// chunks): the chunks of all tiles of a CTA are one sequence.
+//
+// The softmax's instructions bound it, so it does without a maximum for each chunk: the scale of a row is the max of its
+// first chunk with a key that counts, and floating point does not mind later scores above it.  A row whose sum has passed 2^20
+// is scaled down two chunks later (its two threads and the P V behind agree by then); one that overflows before, by
+// scores 70 above its scale within two chunks, is computed again at the end like one that met a value that is not finite.
 #include <algorithm>
 #include <cfloat>
 
@@ -19,16 +25,19 @@ namespace {
 
 template <int HD>
 struct WinSmem {
-    static constexpr int LOAD_WARP = 4, MMA_WARP = 5, THREADS = 6 * 32;
+    static constexpr int LOAD_WARP = 8, S_WARP = 9, PV_WARP = 10, THREADS = 11 * 32;
     static constexpr int NK = HD == 64 ? 96 : 64;          // key positions per chunk: 2 NK + HD TMEM columns
     static constexpr int TMEM = 256;                       // two CTAs an SM
     static constexpr int QB = HD == 64 ? 2 : 1;            // query buffers
     static constexpr int Q_SLAB = 128 * 128, Q_TILE = (HD / 64) * Q_SLAB;  // 128 query rows x 64 bf16; x HD
     static constexpr int SLAB = NK * 128, TILE = (HD / 64) * SLAB;         // NK keys x 64 bf16; x HD
-    static constexpr int NS = HD == 64 ? 6 : 4;            // ring slots, one K or V chunk each
-    static constexpr int KV_OFF = QB * Q_TILE;
-    static constexpr int BAR_OFF = KV_OFF + NS * TILE;     // qfull[QB] qempty[QB] full[NS] empty[NS] sfull[2] odone[2] pready[2] oempty
-    static constexpr int SLOT_OFF = BAR_OFF + (2 * QB + 2 * NS + 7) * 8;
+    static constexpr int NS = HD == 64 ? 3 : 2;            // slots of the ring of keys and of that of values, a chunk each
+    static constexpr int K_OFF = QB * Q_TILE, V_OFF = K_OFF + NS * TILE;
+    static constexpr int X_OFF = V_OFF + NS * TILE;       // [2][2][128] floats that a row's two threads exchange
+    static constexpr int FLAG_OFF = X_OFF + 2 * 2 * 128 * 4;  // [4][2] chunk in which a sum of a quarter's rows passed 2^20
+    static constexpr int BAR_OFF = FLAG_OFF + 4 * 2 * 4;   // qfull[QB] qempty[QB] kfull[NS] kempty[NS] vfull[NS] vempty[NS]
+                                                           // sfull[2] odone[2] pready[2] oempty pair[4]
+    static constexpr int SLOT_OFF = BAR_OFF + (2 * QB + 4 * NS + 11) * 8;
     static constexpr int DYN = SLOT_OFF + 16 + 1024;       // + TMEM slot, + alignment slack
 };
 static_assert(2 * (WinSmem<64>::DYN + 1024) <= 228 * 1024 && 2 * (WinSmem<128>::DYN + 1024) <= 228 * 1024, "two CTAs an SM");
@@ -37,6 +46,56 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
+}
+
+// The same, NaN if one is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
+__device__ __forceinline__ float sum_f32x4(const uint64_t (&x)[2]) {
+    const float2 s = unpack_f32x2(add_f32x2(x[0], x[1]));
+    return s.x + s.y;
+}
+
+// The MMA warp runs its loop as a whole, so that the compiler keeps descriptors and addresses in uniform registers, where
+// the instruction wants them; the lane with `me` issues.  (With the loop in one lane's branch, each of the dozen small
+// MMAs of a chunk came with a handful of moves into them, and the issuer, which shares its scheduler with softmax warps, was
+// the slowest part of the chain.)
+__device__ __forceinline__ void win_mma(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate, uint32_t me) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 e, %5, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(me)
+        : "memory");
+}
+// The same with A in TMEM.
+__device__ __forceinline__ void win_mma_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate, uint32_t me) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 e, %5, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(me)
+        : "memory");
+}
+__device__ __forceinline__ void win_commit(uint32_t bar, uint32_t me) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\t"
+        "setp.ne.b32 e, %1, 0;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+        "r"(me)
+        : "memory");
+}
+
+// mbar_wait by a whole warp, with one answer
+__device__ __forceinline__ bool win_wait(uint32_t bar, uint32_t parity, int* status) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, status));
 }
 
 // The tiles of a CTA and their chunks, as its warps step through them
@@ -69,69 +128,81 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     const uint32_t bars = smem_u32(base + SM::BAR_OFF);
     auto qfull = [&](int i) { return bars + 8 * (i % QB); };  // of the CTA's tile i, phase i / QB
     auto qempty = [&](int i) { return bars + 8 * (QB + i % QB); };
-    auto full = [&](int s) { return bars + 8 * (2 * QB + s); };
-    auto empty = [&](int s) { return bars + 8 * (2 * QB + NS + s); };
+    constexpr int KB0 = 2 * QB, VB0 = KB0 + 2 * NS, SB0 = VB0 + 2 * NS;
+    auto kfull = [&](int s) { return bars + 8 * (KB0 + s); };
+    auto kempty = [&](int s) { return bars + 8 * (KB0 + NS + s); };
+    auto vfull = [&](int s) { return bars + 8 * (VB0 + s); };
+    auto vempty = [&](int s) { return bars + 8 * (VB0 + NS + s); };
     // of chunk j of all the CTA's, phase j >> 1
-    auto sfull = [&](int j) { return bars + 8 * (2 * QB + 2 * NS + (j & 1)); };
-    auto odone = [&](int j) { return bars + 8 * (2 * QB + 2 * NS + 2 + (j & 1)); };
-    auto pready = [&](int j) { return bars + 8 * (2 * QB + 2 * NS + 4 + (j & 1)); };
-    const uint32_t oempty = bars + 8 * (2 * QB + 2 * NS + 6);  // of a tile
+    auto sfull = [&](int j) { return bars + 8 * (SB0 + (j & 1)); };
+    auto odone = [&](int j) { return bars + 8 * (SB0 + 2 + (j & 1)); };
+    auto pready = [&](int j) { return bars + 8 * (SB0 + 4 + (j & 1)); };
+    const uint32_t oempty = bars + 8 * (SB0 + 6);              // of a tile
+    auto pair = [&](int q) { return bars + 8 * (SB0 + 7 + q); };  // of the two warps of a quarter of the rows
+    volatile int* flag = reinterpret_cast<int*>(base + SM::FLAG_OFF);
     uint32_t* slot = reinterpret_cast<uint32_t*>(base + SM::SLOT_OFF);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    // the warp's number from one lane, and below the TMEM address: the compiler then knows them to be the same in all
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     if (tid == 0) {
         for (int i = 0; i < QB; ++i) {
             mbar_init(qfull(i), 1);
             mbar_init(qempty(i), 1);
         }
         for (int s = 0; s < NS; ++s) {
-            mbar_init(full(s), 1);
-            mbar_init(empty(s), 1);
+            mbar_init(kfull(s), 1);
+            mbar_init(kempty(s), 1);
+            mbar_init(vfull(s), 1);
+            mbar_init(vempty(s), 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(sfull(b), 1);
             mbar_init(odone(b), 1);
-            mbar_init(pready(b), 4);  // the softmax warps
+            mbar_init(pready(b), 8);  // the softmax warps
         }
-        mbar_init(oempty, 4);
+        mbar_init(oempty, 8);
+        for (int q = 0; q < 4; ++q) {
+            mbar_init(pair(q), 2);
+            flag[2 * q] = flag[2 * q + 1] = -8;
+        }
         fence_mbar_init();
     }
-    if (warp == SM::MMA_WARP) {
+    if (warp == SM::S_WARP) {
         tmem_alloc(smem_u32(slot), SM::TMEM);
         tmem_relinquish();
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *slot, t_out = tmem + 2 * NK;  // two S (and P) buffers, then O
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *slot, 0), t_out = tmem + 2 * NK;  // two S (and P) buffers, then O
     const int rt = a.rows;
     WinTiles tl(a, C);
     // a tile's chunks: of the keys that its tokens r0 .. see
     auto range = [&](int r0) { return WinRange(a, a.n_mem + r0, a.n_mem + min(a.Lq, r0 + rt) - 1, NK); };
+    // keys of a chunk up to the last that some token sees, in sixteens: what S, the softmax and P V go over
+    auto width = [&](const WinRange& w, int r0, int j) {
+        return (w.count(a, a.n_mem + r0, a.n_mem + min(a.Lq, r0 + rt) - 1, j, NK) + 15) & ~15;
+    };
 
     if (warp == SM::LOAD_WARP) {
         if (lane == 0) {
             tma_prefetch_map(&tmQ);
             tma_prefetch_map(&tmK);
             tma_prefetch_map(&tmV);
-            int s = 0, ph = 1;  // slot, and the phase of its release (the first round passes)
             bool ok = true;
-            auto load = [&](const CUtensorMap* m, int pos, int c, int g) {
-                ok = ok && mbar_wait(empty(s), ph, a.status);
+            // chunk j of all to its ring's slot j % NS, whose release of before is phase j / NS - 1 (the first passes)
+            auto load = [&](const CUtensorMap* m, uint32_t full, uint32_t empty, uint32_t dst, int j, int pos, int c, int g) {
+                ok = ok && mbar_wait(empty, (j / NS & 1) ^ 1, a.status);
                 if (!ok) return;
-                const uint32_t dst = smem_u32(base + SM::KV_OFF + s * SM::TILE);
                 // a dimension that the caches share (stride 0) has one element in the maps
                 const int ctx = a.s0 ? c / a.L : 0, layer = a.s1 ? c % a.L : 0, head = a.s2 ? g : 0;
-                mbar_expect_tx(full(s), SM::TILE);
+                mbar_expect_tx(full, SM::TILE);
 #pragma unroll
-                for (int kb = 0; kb < HD / 64; ++kb)
-                    tma_load_5d(dst + kb * SM::SLAB, m, full(s), 64 * kb, pos, head, layer, ctx);
-                if (++s == NS) {
-                    s = 0;
-                    ph ^= 1;
-                }
+                for (int kb = 0; kb < HD / 64; ++kb) tma_load_5d(dst + kb * SM::SLAB, m, full, 64 * kb, pos, head, layer, ctx);
             };
+            const uint32_t k0 = smem_u32(base + SM::K_OFF), v0 = smem_u32(base + SM::V_OFF);
             // K0 K1 V0 K2 V1 .. over all chunks of all tiles: the keys of a chunk, then the values of the chunk before
-            int vp = -1, vc = 0, vg = 0;
+            int J = 0, vp = 0, vc = 0, vg = 0;
+            auto load_v = [&](int j) { load(&tmV, vfull(j % NS), vempty(j % NS), v0 + j % NS * SM::TILE, j, vp, vc, vg); };
             for (int i = 0; ok && tl.more(); ++i, tl.next()) {
                 int c, g, r0;
                 tl.where(a, c, g, r0);
@@ -142,105 +213,105 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
 #pragma unroll
                 for (int kb = 0; kb < HD / 64; ++kb)  // the query rows, [head of the group][token]
                     tma_load_4d(smem_u32(base + (i % QB) * SM::Q_TILE) + kb * SM::Q_SLAB, &tmQ, qfull(i), 64 * kb, r0, g * a.group, c);
-                for (int j = 0; ok && j < w.n; ++j) {
-                    load(&tmK, w.at(j, NK), c, g);
-                    if (vp >= 0) load(&tmV, vp, vc, vg);
+                for (int j = 0; ok && j < w.n; ++j, ++J) {
+                    load(&tmK, kfull(J % NS), kempty(J % NS), k0 + J % NS * SM::TILE, J, w.at(j, NK), c, g);
+                    if (J > 0) load_v(J - 1);
                     vp = w.at(j, NK);
                     vc = c;
                     vg = g;
                 }
             }
-            if (vp >= 0) load(&tmV, vp, vc, vg);
+            if (J > 0) load_v(J - 1);
             if (!ok) drain_copies();
         }
         __syncwarp();
-    } else if (warp == SM::MMA_WARP) {
-        if (lane == 0) {
-            const uint32_t id_s = idesc_bf16_f32(128, NK, false, false), id_o = idesc_bf16_f32(128, HD, false, true);
-            // descriptors of the queries and of the ring's first slot as K and as V
-            const uint64_t dq0 = sdesc_sw128(smem_u32(base), 16), dk0 = sdesc_sw128(smem_u32(base + SM::KV_OFF), 16),
-                           dv0 = sdesc_sw128(smem_u32(base + SM::KV_OFF), SM::SLAB);
-            int s = 0, ph = 0;  // the ring's next slot and its phase
-            bool ok = true;
-            auto next = [&]() {
-                if (++s == NS) {
-                    s = 0;
-                    ph ^= 1;
-                }
-            };
-            // S runs two chunks ahead of P V, on into the CTA's next tile
-            int si = 0, sj = 0, sn = 0, SJ = 0;  // S: tile, chunk in it, its chunks, chunk of all
-            auto open = [&]() {
-                int c, g, r0;
-                tl.where(a, c, g, r0);
-                sn = range(r0).n;
-                sj = 0;
-            };
-            auto issue_s = [&]() {  // S = Q K^T over HD (K-major both)
-                if (!ok || !tl.more()) return;
-                if (sj == 0) {
-                    open();
-                    ok = mbar_wait(qfull(si), si / QB & 1, a.status);
-                }
-                ok = ok && mbar_wait(full(s), ph, a.status);
-                if (!ok) return;
+    } else if (warp == SM::S_WARP) {
+        // S = Q K^T over HD (K-major both)
+        const uint32_t me = lane == 0;
+        const uint64_t dq0 = sdesc_sw128(smem_u32(base), 16), dk0 = sdesc_sw128(smem_u32(base + SM::K_OFF), 16);
+        bool ok = true;
+        int s = 0, ph = 0, J = 0;  // the ring's next slot and its phase; chunk of all
+        for (int i = 0; ok && tl.more(); ++i, tl.next()) {
+            int c, g, r0;
+            tl.where(a, c, g, r0);
+            const WinRange w = range(r0);
+            ok = win_wait(qfull(i), i / QB & 1, a.status);
+            for (int j = 0; ok && j < w.n; ++j, ++J) {
+                const uint32_t id_s = idesc_bf16_f32(128, width(w, r0, j), false, false);
+                const uint64_t dk = sdesc_step(dk0, s * SM::TILE), dq = sdesc_step(dq0, i % QB * SM::Q_TILE);
+                ok = win_wait(kfull(s), ph, a.status);
+                if (J >= 2) ok = ok && win_wait(odone(J), ((J >> 1) & 1) ^ 1, a.status);  // P V of chunk J - 2 has read its P, where S goes
+                if (!ok) break;
                 tc_fence_after();
-                const uint64_t dk = sdesc_step(dk0, s * SM::TILE), dq = sdesc_step(dq0, si % QB * SM::Q_TILE);
 #pragma unroll
                 for (int kb = 0; kb < HD / 64; ++kb)
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        umma_bf16(tmem + (SJ & 1) * NK, sdesc_step(dq, kb * SM::Q_SLAB + u * 32), sdesc_step(dk, kb * SM::SLAB + u * 32), id_s,
-                                  (kb | u) ? 1u : 0u);
-                umma_commit(sfull(SJ));
-                umma_commit(empty(s));
-                next();
-                ++SJ;
-                if (++sj == sn) {
-                    umma_commit(qempty(si));  // the queries have been read
-                    ++si;
-                    sj = 0;
-                    tl.next();
-                }
-            };
-            issue_s();
-            issue_s();
-            WinTiles pt(a, C);
-            int J = 0;
-            for (int i = 0; ok && pt.more(); ++i, pt.next()) {
-                int c, g, r0;
-                pt.where(a, c, g, r0);
-                const int n = range(r0).n;
-                for (int j = 0; ok && j < n; ++j, ++J) {
-                    ok = mbar_wait(full(s), ph, a.status) && mbar_wait(pready(J), (J >> 1) & 1, a.status);  // P of chunk J is in TMEM
-                    if (j == 0) ok = ok && mbar_wait(oempty, (i & 1) ^ 1, a.status);  // the last tile's O has been read
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint64_t dv = sdesc_step(dv0, s * SM::TILE);
-#pragma unroll
-                    for (int kk = 0; kk < NK / 16; ++kk)  // O += P V over the chunk's keys (P in TMEM, V MN-major)
-                        umma_bf16_ta(t_out, tmem + (J & 1) * NK + kk * 8, sdesc_step(dv, kk * 16 * 128), id_o, (j | kk) ? 1u : 0u);
-                    umma_commit(odone(J));
-                    umma_commit(empty(s));
-                    next();
-                    // the next S goes over the P that P V has to have read
-                    if (tl.more()) {
-                        ok = mbar_wait(odone(J), (J >> 1) & 1, a.status);
-                        issue_s();
-                    }
+                        win_mma(tmem + (J & 1) * NK, sdesc_step(dq, kb * SM::Q_SLAB + u * 32), sdesc_step(dk, kb * SM::SLAB + u * 32), id_s,
+                                (kb | u) ? 1u : 0u, me);
+                win_commit(sfull(J), me);
+                win_commit(kempty(s), me);
+                if (++s == NS) {
+                    s = 0;
+                    ph ^= 1;
                 }
             }
-            if (!ok) drain_copies();
+            win_commit(qempty(i), me);  // the queries have been read
         }
+        if (!ok) drain_copies();
+        __syncwarp();
+    } else if (warp == SM::PV_WARP) {
+        // O += P V over the chunk's keys (P in TMEM, that of a half over its own scores; V MN-major)
+        const uint32_t me = lane == 0, id_o = idesc_bf16_f32(128, HD, false, true);
+        const uint64_t dv0 = sdesc_sw128(smem_u32(base + SM::V_OFF), SM::SLAB);
+        bool ok = true;
+        int s = 0, ph = 0, J = 0;
+        for (int i = 0; ok && tl.more(); ++i, tl.next()) {
+            int c, g, r0;
+            tl.where(a, c, g, r0);
+            const WinRange w = range(r0);
+            for (int j = 0; ok && j < w.n; ++j, ++J) {
+                const int wd = width(w, r0, j);
+                const uint64_t dv = sdesc_step(dv0, s * SM::TILE);
+                ok = win_wait(vfull(s), ph, a.status);
+                if (j == 0) ok = ok && win_wait(oempty, (i & 1) ^ 1, a.status);  // the last tile's O has been read
+                ok = ok && win_wait(pready(J), (J >> 1) & 1, a.status);          // P of chunk J is in TMEM
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int kk = 0; kk < NK / 16; ++kk)
+                    if (kk * 16 < wd)
+                        win_mma_ta(t_out, tmem + (J & 1) * NK + kk * 8 + (kk * 16 >= NK / 2 ? NK / 4 : 0), sdesc_step(dv, kk * 16 * 128), id_o,
+                                   (j | kk) ? 1u : 0u, me);
+                win_commit(odone(J), me);
+                win_commit(vempty(s), me);
+                if (++s == NS) {
+                    s = 0;
+                    ph ^= 1;
+                }
+            }
+        }
+        if (!ok) drain_copies();
         __syncwarp();
     } else {
-        // ---- softmax: row = thread = TMEM lane
-        const int row = tid, hr = row / rt;
+        // ---- softmax: row = TMEM lane, half = keys NE half .. of every chunk, dimensions HD / 2 half ..
+        constexpr int NE = NK / 2;
+        const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane, hr = row / rt;
         const float k2 = a.scale * 1.4426950408889634f;  // softmax scale in base 2: exp(s x) = 2^(s log2(e) x)
-        const float grow = 8.f / k2;
-        const uint32_t lane_off = (uint32_t)(warp * 32) << 16, t_o = t_out + lane_off;
+        const uint32_t lane_off = (uint32_t)(quarter * 32) << 16, t_o = t_out + lane_off + half * (HD / 2);
+        float* xch = reinterpret_cast<float*>(base + SM::X_OFF);
         bool ok = true;
-        int J = 0;
+        int J = 0, met = 0;  // chunks of all tiles; exchanges
+        // the other thread's value of the row
+        auto exchange = [&](float x) {
+            float* p = xch + (met & 1) * 256;
+            p[half * 128 + row] = x;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(pair(quarter));
+            ok = win_wait(pair(quarter), met & 1, a.status) && ok;
+            ++met;
+            return p[(half ^ 1) * 128 + row];
+        };
         for (int i = 0; ok && tl.more(); ++i, tl.next()) {
             int c, g, r0;
             tl.where(a, c, g, r0);
@@ -249,90 +320,125 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             const int tok = r0 + row - hr * rt;
             const bool live = hr < a.group && tok < a.Lq;
             const int vis = a.n_mem + (live ? tok : r0) + 1;  // the row sees keys before it (a row of padding: any)
-            float m_run = 0.f;
+            float m_run = -FLT_MAX;  // the row's scale; that: no key counted so far
             uint64_t l2[2] = {0, 0};
             for (int j = 0; j < win.n; ++j, ++J) {
                 const uint32_t t_s = tmem + lane_off + (J & 1) * NK;
-                ok = __all_sync(0xffffffffu, mbar_wait(sfull(J), (J >> 1) & 1, a.status));
+                const int at = win.at(j, NK) + half * NE;
+                const int wd = width(win, r0, j) - half * NE;  // of the half's keys, if positive
+                ok = win_wait(sfull(J), (J >> 1) & 1, a.status);
                 if (!ok) break;
                 tc_fence_after();
-                float v[NK];
-                if constexpr (NK == 96)
-                    tmem_ld96(t_s, v);
-                else
-                    tmem_ld64(t_s, v);
-                const int p0 = win.at(j, NK);
-                // some row does not see the whole chunk (in the window of all: from the last token's first key on)
-                if (p0 + NK > a.n_mem + r0 + 1 || (p0 + NK > a.n_sink && p0 < keys - a.window)) {
-                    const int nv = vis - p0, nw = vis - a.window - p0, ns = a.n_sink - p0;
-#pragma unroll
-                    for (int u = 0; u < NK; ++u) v[u] = u < nv && (u >= nw || u < ns) ? v[u] : -INFINITY;
-                }
-                float c4[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-                for (int u = 4; u < NK; u += 8)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) c4[k] = u + 4 < NK ? max3(c4[k], v[u + k], v[u + 4 + k]) : fmaxf(c4[k], v[u + k]);
-                const float cm = max3(fmaxf(c4[0], c4[1]), c4[2], c4[3]);
-                // The scale is the max of the first chunk, and of a later one where that is over 2^8 times it (probabilities
-                // of up to 2^8 lose nothing in bf16 or the sums): O is hardly ever rescaled
-                if (j == 0) {
-                    m_run = fmaxf(cm, -FLT_MAX);  // finite: where every key so far scores -inf, probabilities of 0
-                } else {
-                    const bool grown = cm > m_run + grow;
-                    if (__any_sync(0xffffffffu, grown)) {
-                        const bool in = __all_sync(0xffffffffu, mbar_wait(odone(J - 1), ((J - 1) >> 1) & 1, a.status));  // O up to the last chunk
-                        tc_fence_after();
-                        const float corr = grown ? at_exp2((m_run - cm) * k2) : 1.f;
-                        if (grown) m_run = cm;
-                        l2[0] = mul_f32x2(l2[0], pack_f32x2(corr, corr));
-                        l2[1] = mul_f32x2(l2[1], pack_f32x2(corr, corr));
+                // Hidden keys get scores of -inf, written back: few chunks have any, and the loop over all of them stays short (its
+                // instructions, unrolled with masks, did not fit the instruction caches)
+                if (at + NE > a.n_mem + r0 + 1 || (at + NE > a.n_sink && at < keys - a.window)) {
 #pragma unroll 1
-                        for (int cb = 0; in && cb < HD; cb += 16) {
-                            float ov[16];
-                            uint32_t on[16];
-                            tmem_ld16(t_o + cb, ov);
+                    for (int b = 0; b < NE && b < wd; b += 16) {
+                        // sixteen of which some row does not see all (in the window of all: from the last token's first key on)
+                        const int p = at + b;
+                        if (p + 16 <= a.n_mem + r0 + 1 && (p + 16 <= a.n_sink || p >= keys - a.window)) continue;
+                        const int nv = vis - p, nw = nv - a.window, ns = a.n_sink - p;
+                        float v[16];
+                        uint32_t hid[16];
+                        tmem_ld16(t_s + half * NE + b, v);
 #pragma unroll
-                            for (int u = 0; u < 16; ++u) on[u] = __float_as_uint(ov[u] * corr);
-                            tmem_st16(t_o + cb, on);
-                        }
+                        for (int u = 0; u < 16; ++u) hid[u] = u < nv && (u >= nw || u < ns) ? __float_as_uint(v[u]) : 0xff800000u;
+                        tmem_st16(t_s + half * NE + b, hid);
+                    }
+                    tmem_wait_st();
+                }
+                if (j == 0 || __any_sync(0xffffffffu, m_run == -FLT_MAX)) {  // the same in both warps
+                    float cm = -INFINITY;
+#pragma unroll 1
+                    for (int b = 0; b < NE && b < wd; b += 16) {
+                        float v[16];
+                        tmem_ld16(t_s + half * NE + b, v);
+#pragma unroll
+                        for (int u = 0; u < 16; u += 2) cm = max3(cm, v[u], v[u + 1]);
+                    }
+                    cm = fmaxf(cm, exchange(cm));
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (m_run == -FLT_MAX) m_run = fmaxf(cm, -FLT_MAX);  // sums and O are 0 so far
+                } else if (flag[2 * quarter + (J & 1)] == J - 2) {
+                    float l = sum_f32x4(l2);
+                    l += exchange(l);
+                    const bool in = win_wait(odone(J - 1), ((J - 1) >> 1) & 1, a.status);  // O up to the last chunk
+                    ok = ok && in;
+                    if (!ok) break;
+                    tc_fence_after();
+                    const int e = l > 0x1p20f && l <= FLT_MAX ? ilogbf(l) : 0;  // by a power of two
+                    const float corr = ldexpf(1.f, -e);
+                    m_run += e / k2;
+                    l2[0] = mul_f32x2(l2[0], pack_f32x2(corr, corr));
+                    l2[1] = mul_f32x2(l2[1], pack_f32x2(corr, corr));
+#pragma unroll 1
+                    for (int cb = 0; cb < HD / 2; cb += 16) {
+                        float ov[16];
+                        uint32_t on[16];
+                        tmem_ld16(t_o + cb, ov);
+#pragma unroll
+                        for (int u = 0; u < 16; ++u) on[u] = __float_as_uint(ov[u] * corr);
+                        tmem_st16(t_o + cb, on);
                     }
                 }
                 const float moff = -m_run * k2;
                 const uint64_t kk2 = pack_f32x2(k2, k2), mm2 = pack_f32x2(moff, moff);
+                auto probs = [&](auto& v, int b, int n) {
 #pragma unroll
-                for (int b = 0; b < NK; b += 32) {
-                    uint32_t pk[16];
+                    for (int h = 0; h < n; h += 16) {
+                        uint32_t pk[8];
 #pragma unroll
-                    for (int u = 0; u < 16; ++u) {
-                        const float2 x = unpack_f32x2(fma_f32x2(pack_f32x2(v[b + 2 * u], v[b + 2 * u + 1]), kk2, mm2));
-                        const float e0 = at_exp2(x.x), e1 = at_exp2(x.y);
-                        pk[u] = pack_bf16(e0, e1);
-                        l2[u & 1] = add_f32x2(l2[u & 1], pack_f32x2(e0, e1));
+                        for (int u = 0; u < 8; ++u) {
+                            const float2 x = unpack_f32x2(fma_f32x2(pack_f32x2(v[h + 2 * u], v[h + 2 * u + 1]), kk2, mm2));
+                            const float e0 = at_exp2(x.x), e1 = at_exp2(x.y);
+                            pk[u] = pack_bf16(e0, e1);
+                            l2[u & 1] = add_f32x2(l2[u & 1], pack_f32x2(e0, e1));
+                        }
+                        tmem_st8(t_s + half * NE + (b + h) / 2, pk);
                     }
-                    tmem_st16(t_s + b / 2, pk);
+                };
+                if (wd > 0) {
+                    if (wd > 16) {
+                        float v[32];
+                        tmem_ld32(t_s + half * NE, v);
+                        probs(v, 0, 32);
+                    } else {
+                        float v[16];
+                        tmem_ld16(t_s + half * NE, v);
+                        probs(v, 0, 16);
+                    }
+                    if (NE == 48 && wd > 32) {
+                        float v[16];
+                        tmem_ld16(t_s + half * NE + 32, v);
+                        probs(v, 32, 16);
+                    }
+                    if (__any_sync(0xffffffffu, sum_f32x4(l2) > 0x1p20f) && lane == 0) flag[2 * quarter + (J & 1)] = J;
                 }
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(pready(J));
             }
-            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(odone(J - 1), ((J - 1) >> 1) & 1, a.status));
+            if (!ok) break;
+            float sum = sum_f32x4(l2);
+            sum += exchange(sum);
+            ok = win_wait(odone(J - 1), ((J - 1) >> 1) & 1, a.status) && ok;
             if (!ok) break;
             tc_fence_after();
-            const float2 ls = unpack_f32x2(add_f32x2(l2[0], l2[1]));
-            const float sum = ls.x + ls.y, inv = sum == 0.f ? 0.f : 1.f / sum;  // no key that counts: 0
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no key that counts: 0
             const size_t at = (((size_t)c * a.n_q + g * a.group + (live ? hr : 0)) * a.Lq + (live ? tok : 0)) * HD;
-            bf16* orow = static_cast<bf16*>(a.out) + at;
-            bool bad = false;
+            bf16* orow = static_cast<bf16*>(a.out) + at + half * (HD / 2);
+            float top = 0.f;  // of the row's magnitudes, NaN if one is
 #pragma unroll
-            for (int cb = 0; cb < HD; cb += 32) {
+            for (int cb = 0; cb < HD / 2; cb += 32) {
                 float v[32];
                 tmem_ld32(t_o + cb, v);
 #pragma unroll
-                for (int u = 0; u < 32; ++u) {
+                for (int u = 0; u < 32; u += 2) {
                     v[u] *= inv;
-                    bad |= !isfinite(v[u]);
+                    v[u + 1] *= inv;
+                    top = max3_nan(top, fabsf(v[u]), fabsf(v[u + 1]));
                 }
                 if (live) {
 #pragma unroll
@@ -345,13 +451,13 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(oempty);
-            if (live && bad) {
+            if (live && !(top <= FLT_MAX)) {
                 const long long kv_off = (long long)(c / a.L) * a.s0 + (long long)(c % a.L) * a.s1 + (long long)g * a.s2;
 #pragma unroll 1
-                for (int cb = 0; cb < HD; cb += 32) {
+                for (int cb = 0; cb < HD / 2; cb += 32) {
                     float w[32];
                     row_again<bf16, HD, 32, 1>(static_cast<const bf16*>(a.Q) + at, static_cast<const bf16*>(a.K) + kv_off,
-                                               static_cast<const bf16*>(a.V) + kv_off, a.s3, vis, a, cb, w);
+                                               static_cast<const bf16*>(a.V) + kv_off, a.s3, vis, a, half * (HD / 2) + cb, w);
                     for (int u = 0; u < 32; ++u) orow[cb + u] = __float2bfloat16_rn(w[u]);
                 }
             }
@@ -361,7 +467,7 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == SM::MMA_WARP) tmem_dealloc(tmem, SM::TMEM);
+    if (warp == SM::S_WARP) tmem_dealloc(tmem, SM::TMEM);
 }
 
 template <int HD>
