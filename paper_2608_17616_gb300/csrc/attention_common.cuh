@@ -29,11 +29,6 @@ struct WinRange {
         n = ns + (lo <= t1 ? (t1 - lo) / step + 1 : 0);
     }
     __device__ int at(int j, int step) const { return j < ns ? j * step : lo + (j - ns) * step; }
-    // positions of chunk j up to the last that some token sees
-    __device__ int count(const AttnArgs& a, int t0, int t1, int j, int step) const {
-        const bool first_only = j < ns && t0 - a.window + 1 >= (j + 1) * step;
-        return min(step, (first_only ? min(a.n_sink, t1 + 1) : t1 + 1) - at(j, step));
-    }
 };
 
 // Output dimensions d0, d0 + STEP, .. of one row over the keys it sees and no others, by one thread.  A tile's

@@ -1,11 +1,13 @@
 // Windowed attention of many query rows (mone_window_attention, bf16 with 16-byte-aligned rows) on the tensor cores.
 //
 // A tile is 128 MMA rows: rt = 128 / group tokens of each of a KV head's `group` query heads, which share every staged key
-// and value row.  A CTA, two an SM, takes one tile after another.  Per chunk of NK keys: S = Q K^T into one of two TMEM
+// and value row.  A CTA takes one tile after another (hd 64, two CTAs an SM), or one pair of tiles of consecutive tokens
+// after another, which share the staged keys and values (hd 128, one CTA an SM: with two, the rings had room for two chunks
+// each, and S and P V waited for loads for a third of the time).  Per chunk of NK keys: S = Q K^T into one of two TMEM
 // buffers, the softmax, whose bf16 probabilities go over the scores as the A operand of O += P V, O in TMEM.
-// Warps 0-7: the softmax and the output, two threads a row (= TMEM lane), one for each half of a chunk's keys and of the head's
-// dimensions.  Warp 8: the loader; keys and values by TMA with the caller's strides through a ring each, the queries into a
-// buffer of their own.  Warps 9 and 10: the MMA issuers, of S, two chunks ahead, and of P V.  Loads and S run on over the end of a
+// Eight warps for each of the tiles: the softmax and the output, two threads a row (= TMEM lane), one for each half of a chunk's keys and of the head's
+// dimensions.  Then the loader; keys and values by TMA with the caller's strides through a ring each, the queries into a
+// buffer of their own.  Then the MMA issuers, of S, two chunks ahead, one for each tile, and of P V.  Loads and S run on over the end of a
 // tile (a window has few chunks, so a tile's first loads and last output would otherwise cost as much as its
 // chunks): the chunks of all tiles of a CTA are one sequence.
 //
@@ -23,24 +25,26 @@ namespace mone {
 
 namespace {
 
-template <int HD>
+// TP: tiles at a time
+template <int HD, int TP>
 struct WinSmem {
-    static constexpr int LOAD_WARP = 8, S_WARP = 9, PV_WARP = 10, THREADS = 11 * 32;
-    static constexpr int NK = HD == 64 ? 96 : 64;          // key positions per chunk: 2 NK + HD TMEM columns
-    static constexpr int TMEM = 256;                       // two CTAs an SM
+    static constexpr int CTAS = HD == 64 ? 2 / TP : 1;     // CTAs an SM
+    static constexpr int LOAD_WARP = 8 * TP, S_WARP = LOAD_WARP + 1, PV_WARP = S_WARP + TP, THREADS = (PV_WARP + 1) * 32;
+    static constexpr int NK = HD == 64 ? 96 : 64;          // key positions per chunk: 2 NK + HD TMEM columns for each tile
+    static constexpr int TILE_COLS = 256, TMEM = TP * TILE_COLS;
     static constexpr int QB = HD == 64 ? 2 : 1;            // query buffers
     static constexpr int Q_SLAB = 128 * 128, Q_TILE = (HD / 64) * Q_SLAB;  // 128 query rows x 64 bf16; x HD
     static constexpr int SLAB = NK * 128, TILE = (HD / 64) * SLAB;         // NK keys x 64 bf16; x HD
-    static constexpr int NS = HD == 64 ? 3 : 2;            // slots of the ring of keys and of that of values, a chunk each
-    static constexpr int K_OFF = QB * Q_TILE, V_OFF = K_OFF + NS * TILE;
-    static constexpr int X_OFF = V_OFF + NS * TILE;       // [2][2][128] floats that a row's two threads exchange
-    static constexpr int FLAG_OFF = X_OFF + 2 * 2 * 128 * 4;  // [4][2] chunk in which a sum of a quarter's rows passed 2^20
-    static constexpr int BAR_OFF = FLAG_OFF + 4 * 2 * 4;   // qfull[QB] qempty[QB] kfull[NS] kempty[NS] vfull[NS] vempty[NS]
-                                                           // sfull[2] odone[2] pready[2] oempty pair[4]
-    static constexpr int SLOT_OFF = BAR_OFF + (2 * QB + 4 * NS + 11) * 8;
+    static constexpr int NS = CTAS == 2 ? 3 : 4;           // slots of the ring of keys and of that of values, a chunk each
+    static constexpr int K_OFF = QB * TP * Q_TILE, V_OFF = K_OFF + NS * TILE;
+    static constexpr int X_OFF = V_OFF + NS * TILE;        // [tile][2][2][128] floats that a row's two threads exchange
+    static constexpr int FLAG_OFF = X_OFF + TP * 2 * 2 * 128 * 4;  // [tile][4][2] chunk in which a sum of a quarter's rows passed 2^20
+    // qfull[QB] qempty[QB] kfull[NS] kempty[NS] vfull[NS] vempty[NS], and for each tile sfull[2] odone[2] pready[2] oempty pair[4]
+    static constexpr int BAR_OFF = FLAG_OFF + TP * 4 * 2 * 4, TILE_BARS = 11;
+    static constexpr int SLOT_OFF = BAR_OFF + (2 * QB + 4 * NS + TP * TILE_BARS) * 8;
     static constexpr int DYN = SLOT_OFF + 16 + 1024;       // + TMEM slot, + alignment slack
+    static_assert(2 * NK + HD <= TILE_COLS && CTAS * TMEM <= 512 && CTAS * (DYN + 1024) <= 228 * 1024, "CTAs an SM");
 };
-static_assert(2 * (WinSmem<64>::DYN + 1024) <= 228 * 1024 && 2 * (WinSmem<128>::DYN + 1024) <= 228 * 1024, "two CTAs an SM");
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
@@ -60,10 +64,27 @@ __device__ __forceinline__ float sum_f32x4(const uint64_t (&x)[2]) {
     return s.x + s.y;
 }
 
-// The MMA warp runs its loop as a whole, so that the compiler keeps descriptors and addresses in uniform registers, where
-// the instruction wants them; the lane with `me` issues.  (With the loop in one lane's branch, each of the dozen small
-// MMAs of a chunk came with a handful of moves into them, and the issuer, which shares its scheduler with softmax warps, was
-// the slowest part of the chain.)
+// The loader and the MMA issuers run their loops as whole warps, so that the compiler keeps descriptors, coordinates and
+// addresses in uniform registers, where the instructions want them; the lane with `me` issues.  (With the loop in one lane's
+// branch, each of the dozen small MMAs and copies of a chunk came with a handful of moves into them, and these warps, which
+// share their schedulers with softmax warps, were the slowest part of the chain.)
+__device__ __forceinline__ void win_load_5d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y, int z, int w, int v, uint32_t me) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\t"
+        "setp.ne.b32 e, %8, 0;\n\t"
+        "@e cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4, %5, %6, %7}], [%2];\n\t}" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v), "r"(me)
+        : "memory");
+}
+__device__ __forceinline__ void win_expect(uint32_t bar, uint32_t bytes, uint32_t me) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\t"
+        "setp.ne.b32 e, %2, 0;\n\t"
+        "@e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar),
+        "r"(bytes), "r"(me)
+        : "memory");
+}
 __device__ __forceinline__ void win_mma(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate, uint32_t me) {
     asm volatile(
         "{\n\t.reg .pred p, e;\n\t"
@@ -98,30 +119,46 @@ __device__ __forceinline__ bool win_wait(uint32_t bar, uint32_t parity, int* sta
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, status));
 }
 
-// The tiles of a CTA and their chunks, as its warps step through them
+// The tiles (pairs of tiles) of a CTA, as its warps step through them
+template <int TP, int NK>
 struct WinTiles {
     int tile, step, count, nt;  // this tile, distance to the CTA's next, tiles in all, of a KV head
+    int c, g, r0, t0, t1;       // chain, KV head, first token; positions of its first and last
+    int ns, lo, n, wf, wl;      // chunks of the first positions; first position after them; chunks in all; widths of the last ones
     __device__ WinTiles(const AttnArgs& a, int C) {
-        nt = (a.Lq + a.rows - 1) / a.rows;
+        nt = (a.Lq + TP * a.rows - 1) / (TP * a.rows);
         tile = blockIdx.x;
         step = gridDim.x;
         count = nt * a.n_kv * C;
     }
     __device__ bool more() const { return tile < count; }
     __device__ void next() { tile += step; }
-    __device__ void where(const AttnArgs& a, int& c, int& g, int& r0) const {
+    __device__ void open(const AttnArgs& a) {
         const int cg = tile / nt;
-        r0 = (tile - cg * nt) * a.rows;
+        r0 = (tile - cg * nt) * TP * a.rows;
         c = cg / a.n_kv;
         g = cg - c * a.n_kv;
+        t0 = a.n_mem + r0;
+        t1 = a.n_mem + min(a.Lq, r0 + TP * a.rows) - 1;
+        const WinRange w(a, t0, t1, NK);
+        ns = w.ns;
+        lo = w.lo;
+        n = w.n;
+        // the last chunk of the first positions may go on into the window
+        const int first_end = t0 - a.window + 1 >= ns * NK ? min(a.n_sink, t1 + 1) : t1 + 1;
+        wf = (min(NK, first_end - (ns - 1) * NK) + 15) & ~15;
+        wl = n > ns ? (min(NK, t1 + 1 - (lo + (n - 1 - ns) * NK)) + 15) & ~15 : wf;
     }
+    __device__ int at(int j) const { return j < ns ? j * NK : lo + (j - ns) * NK; }
+    // keys of a chunk up to the last that some token sees, in sixteens: what S, the softmax and P V go over
+    __device__ int width(int j) const { return j == n - 1 ? wl : j == ns - 1 ? wf : NK; }
 };
 
-template <int HD>
-__global__ void __launch_bounds__(WinSmem<HD>::THREADS, 2)
+template <int HD, int TP>
+__global__ void __launch_bounds__(WinSmem<HD, TP>::THREADS, WinSmem<HD, TP>::CTAS)
 window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                       const AttnArgs a, int C) {
-    using SM = WinSmem<HD>;
+    using SM = WinSmem<HD, TP>;
     constexpr int NS = SM::NS, NK = SM::NK, QB = SM::QB;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -133,37 +170,37 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     auto kempty = [&](int s) { return bars + 8 * (KB0 + NS + s); };
     auto vfull = [&](int s) { return bars + 8 * (VB0 + s); };
     auto vempty = [&](int s) { return bars + 8 * (VB0 + NS + s); };
-    // of chunk j of all the CTA's, phase j >> 1
-    auto sfull = [&](int j) { return bars + 8 * (SB0 + (j & 1)); };
-    auto odone = [&](int j) { return bars + 8 * (SB0 + 2 + (j & 1)); };
-    auto pready = [&](int j) { return bars + 8 * (SB0 + 4 + (j & 1)); };
-    const uint32_t oempty = bars + 8 * (SB0 + 6);              // of a tile
-    auto pair = [&](int q) { return bars + 8 * (SB0 + 7 + q); };  // of the two warps of a quarter of the rows
-    volatile int* flag = reinterpret_cast<int*>(base + SM::FLAG_OFF);
+    // of tile x (of a pair) and chunk j of all the CTA's, phase j >> 1
+    auto sfull = [&](int x, int j) { return bars + 8 * (SB0 + x * SM::TILE_BARS + (j & 1)); };
+    auto odone = [&](int x, int j) { return bars + 8 * (SB0 + x * SM::TILE_BARS + 2 + (j & 1)); };
+    auto pready = [&](int x, int j) { return bars + 8 * (SB0 + x * SM::TILE_BARS + 4 + (j & 1)); };
+    auto oempty = [&](int x) { return bars + 8 * (SB0 + x * SM::TILE_BARS + 6); };           // of a tile
+    auto pair = [&](int x, int q) { return bars + 8 * (SB0 + x * SM::TILE_BARS + 7 + q); };  // of the two warps of a quarter of the rows
+    volatile int* flags = reinterpret_cast<int*>(base + SM::FLAG_OFF);
     uint32_t* slot = reinterpret_cast<uint32_t*>(base + SM::SLOT_OFF);
     // the warp's number from one lane, and below the TMEM address: the compiler then knows them to be the same in all
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     if (tid == 0) {
         for (int i = 0; i < QB; ++i) {
             mbar_init(qfull(i), 1);
-            mbar_init(qempty(i), 1);
+            mbar_init(qempty(i), TP);
         }
         for (int s = 0; s < NS; ++s) {
             mbar_init(kfull(s), 1);
-            mbar_init(kempty(s), 1);
+            mbar_init(kempty(s), TP);
             mbar_init(vfull(s), 1);
             mbar_init(vempty(s), 1);
         }
-        for (int b = 0; b < 2; ++b) {
-            mbar_init(sfull(b), 1);
-            mbar_init(odone(b), 1);
-            mbar_init(pready(b), 8);  // the softmax warps
+        for (int x = 0; x < TP; ++x) {
+            for (int b = 0; b < 2; ++b) {
+                mbar_init(sfull(x, b), 1);
+                mbar_init(odone(x, b), 1);
+                mbar_init(pready(x, b), 8);  // the tile's softmax warps
+            }
+            mbar_init(oempty(x), 8);
+            for (int q = 0; q < 4; ++q) mbar_init(pair(x, q), 2);
         }
-        mbar_init(oempty, 8);
-        for (int q = 0; q < 4; ++q) {
-            mbar_init(pair(q), 2);
-            flag[2 * q] = flag[2 * q + 1] = -8;
-        }
+        for (int i = 0; i < TP * 8; ++i) flags[i] = -8;
         fence_mbar_init();
     }
     if (warp == SM::S_WARP) {
@@ -173,83 +210,98 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = __shfl_sync(0xffffffffu, *slot, 0), t_out = tmem + 2 * NK;  // two S (and P) buffers, then O
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *slot, 0);  // of a tile: two S (and P) buffers, then O
     const int rt = a.rows;
-    WinTiles tl(a, C);
-    // a tile's chunks: of the keys that its tokens r0 .. see
-    auto range = [&](int r0) { return WinRange(a, a.n_mem + r0, a.n_mem + min(a.Lq, r0 + rt) - 1, NK); };
-    // keys of a chunk up to the last that some token sees, in sixteens: what S, the softmax and P V go over
-    auto width = [&](const WinRange& w, int r0, int j) {
-        return (w.count(a, a.n_mem + r0, a.n_mem + min(a.Lq, r0 + rt) - 1, j, NK) + 15) & ~15;
-    };
+    WinTiles<TP, NK> tl(a, C);
 
     if (warp == SM::LOAD_WARP) {
-        if (lane == 0) {
+        const uint32_t me = lane == 0;
+        if (me) {
             tma_prefetch_map(&tmQ);
             tma_prefetch_map(&tmK);
             tma_prefetch_map(&tmV);
-            bool ok = true;
-            // chunk j of all to its ring's slot j % NS, whose release of before is phase j / NS - 1 (the first passes)
-            auto load = [&](const CUtensorMap* m, uint32_t full, uint32_t empty, uint32_t dst, int j, int pos, int c, int g) {
-                ok = ok && mbar_wait(empty, (j / NS & 1) ^ 1, a.status);
-                if (!ok) return;
-                // a dimension that the caches share (stride 0) has one element in the maps
-                const int ctx = a.s0 ? c / a.L : 0, layer = a.s1 ? c % a.L : 0, head = a.s2 ? g : 0;
-                mbar_expect_tx(full, SM::TILE);
-#pragma unroll
-                for (int kb = 0; kb < HD / 64; ++kb) tma_load_5d(dst + kb * SM::SLAB, m, full, 64 * kb, pos, head, layer, ctx);
-            };
-            const uint32_t k0 = smem_u32(base + SM::K_OFF), v0 = smem_u32(base + SM::V_OFF);
-            // K0 K1 V0 K2 V1 .. over all chunks of all tiles: the keys of a chunk, then the values of the chunk before
-            int J = 0, vp = 0, vc = 0, vg = 0;
-            auto load_v = [&](int j) { load(&tmV, vfull(j % NS), vempty(j % NS), v0 + j % NS * SM::TILE, j, vp, vc, vg); };
-            for (int i = 0; ok && tl.more(); ++i, tl.next()) {
-                int c, g, r0;
-                tl.where(a, c, g, r0);
-                const WinRange w = range(r0);
-                ok = mbar_wait(qempty(i), (i / QB & 1) ^ 1, a.status);
-                if (!ok) break;
-                mbar_expect_tx(qfull(i), (HD / 64) * a.group * rt * 128);
-#pragma unroll
-                for (int kb = 0; kb < HD / 64; ++kb)  // the query rows, [head of the group][token]
-                    tma_load_4d(smem_u32(base + (i % QB) * SM::Q_TILE) + kb * SM::Q_SLAB, &tmQ, qfull(i), 64 * kb, r0, g * a.group, c);
-                for (int j = 0; ok && j < w.n; ++j, ++J) {
-                    load(&tmK, kfull(J % NS), kempty(J % NS), k0 + J % NS * SM::TILE, J, w.at(j, NK), c, g);
-                    if (J > 0) load_v(J - 1);
-                    vp = w.at(j, NK);
-                    vc = c;
-                    vg = g;
+        }
+        bool ok = true;
+        // K0 K1 V0 K2 V1 .. over all chunks of all tiles: the keys of a chunk, then the values of the chunk before
+        struct Ring {
+            int s = 0, ph = 1;  // slot, and the phase of its release (the first round passes)
+            __device__ void next() {
+                if (++s == NS) {
+                    s = 0;
+                    ph ^= 1;
                 }
             }
-            if (J > 0) load_v(J - 1);
-            if (!ok) drain_copies();
+        } rk, rv;
+        const uint32_t k0 = smem_u32(base + SM::K_OFF), v0 = smem_u32(base + SM::V_OFF);
+        int vp = -1, vctx = 0, vlayer = 0, vhead = 0;
+        auto load_v = [&]() {
+            ok = ok && win_wait(vempty(rv.s), rv.ph, a.status);
+            if (!ok) return;
+            win_expect(vfull(rv.s), SM::TILE, me);
+#pragma unroll
+            for (int kb = 0; kb < HD / 64; ++kb)
+                win_load_5d(v0 + rv.s * SM::TILE + kb * SM::SLAB, &tmV, vfull(rv.s), 64 * kb, vp, vhead, vlayer, vctx, me);
+            rv.next();
+        };
+        for (int i = 0; ok && tl.more(); ++i, tl.next()) {
+            tl.open(a);
+            // a dimension that the caches share (stride 0) has one element in the maps
+            const int tctx = tl.c / a.L, ctx = a.s0 ? tctx : 0, layer = a.s1 ? tl.c - tctx * a.L : 0, head = a.s2 ? tl.g : 0;
+            ok = win_wait(qempty(i), (i / QB & 1) ^ 1, a.status);
+            if (!ok) break;
+            if (me) {
+                mbar_expect_tx(qfull(i), TP * (HD / 64) * a.group * rt * 128);
+#pragma unroll
+                for (int x = 0; x < TP; ++x)
+#pragma unroll
+                    for (int kb = 0; kb < HD / 64; ++kb)  // the query rows, [head of the group][token]
+                        tma_load_4d(smem_u32(base + (i % QB * TP + x) * SM::Q_TILE) + kb * SM::Q_SLAB, &tmQ, qfull(i), 64 * kb, tl.r0 + x * rt,
+                                    tl.g * a.group, tl.c);
+            }
+            __syncwarp();
+            for (int j = 0; ok && j < tl.n; ++j) {
+                const int pos = tl.at(j);
+                ok = win_wait(kempty(rk.s), rk.ph, a.status);
+                if (!ok) break;
+                win_expect(kfull(rk.s), SM::TILE, me);
+#pragma unroll
+                for (int kb = 0; kb < HD / 64; ++kb)
+                    win_load_5d(k0 + rk.s * SM::TILE + kb * SM::SLAB, &tmK, kfull(rk.s), 64 * kb, pos, head, layer, ctx, me);
+                rk.next();
+                if (vp >= 0) load_v();
+                vp = pos;
+                vctx = ctx;
+                vlayer = layer;
+                vhead = head;
+            }
         }
+        if (vp >= 0) load_v();
+        if (!ok) drain_copies();
         __syncwarp();
-    } else if (warp == SM::S_WARP) {
+    } else if (warp >= SM::S_WARP && warp < SM::PV_WARP) {
         // S = Q K^T over HD (K-major both)
-        const uint32_t me = lane == 0;
-        const uint64_t dq0 = sdesc_sw128(smem_u32(base), 16), dk0 = sdesc_sw128(smem_u32(base + SM::K_OFF), 16);
+        const uint32_t me = lane == 0, x = warp - SM::S_WARP, t_s = tmem + x * SM::TILE_COLS;
+        const uint64_t dq0 = sdesc_sw128(smem_u32(base + x * SM::Q_TILE), 16), dk0 = sdesc_sw128(smem_u32(base + SM::K_OFF), 16);
         bool ok = true;
         int s = 0, ph = 0, J = 0;  // the ring's next slot and its phase; chunk of all
         for (int i = 0; ok && tl.more(); ++i, tl.next()) {
-            int c, g, r0;
-            tl.where(a, c, g, r0);
-            const WinRange w = range(r0);
+            tl.open(a);
             ok = win_wait(qfull(i), i / QB & 1, a.status);
-            for (int j = 0; ok && j < w.n; ++j, ++J) {
-                const uint32_t id_s = idesc_bf16_f32(128, width(w, r0, j), false, false);
-                const uint64_t dk = sdesc_step(dk0, s * SM::TILE), dq = sdesc_step(dq0, i % QB * SM::Q_TILE);
+            const uint64_t dq = sdesc_step(dq0, i % QB * TP * SM::Q_TILE);
+            for (int j = 0; ok && j < tl.n; ++j, ++J) {
+                const uint32_t id_s = idesc_bf16_f32(128, tl.width(j), false, false);
+                const uint64_t dk = sdesc_step(dk0, s * SM::TILE);
                 ok = win_wait(kfull(s), ph, a.status);
-                if (J >= 2) ok = ok && win_wait(odone(J), ((J >> 1) & 1) ^ 1, a.status);  // P V of chunk J - 2 has read its P, where S goes
+                if (J >= 2) ok = ok && win_wait(odone(x, J), ((J >> 1) & 1) ^ 1, a.status);  // P V of chunk J - 2 has read its P, where S goes
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
                 for (int kb = 0; kb < HD / 64; ++kb)
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        win_mma(tmem + (J & 1) * NK, sdesc_step(dq, kb * SM::Q_SLAB + u * 32), sdesc_step(dk, kb * SM::SLAB + u * 32), id_s,
+                        win_mma(t_s + (J & 1) * NK, sdesc_step(dq, kb * SM::Q_SLAB + u * 32), sdesc_step(dk, kb * SM::SLAB + u * 32), id_s,
                                 (kb | u) ? 1u : 0u, me);
-                win_commit(sfull(J), me);
+                win_commit(sfull(x, J), me);
                 win_commit(kempty(s), me);
                 if (++s == NS) {
                     s = 0;
@@ -267,23 +319,25 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         bool ok = true;
         int s = 0, ph = 0, J = 0;
         for (int i = 0; ok && tl.more(); ++i, tl.next()) {
-            int c, g, r0;
-            tl.where(a, c, g, r0);
-            const WinRange w = range(r0);
-            for (int j = 0; ok && j < w.n; ++j, ++J) {
-                const int wd = width(w, r0, j);
+            tl.open(a);
+            for (int j = 0; ok && j < tl.n; ++j, ++J) {
+                const int wd = tl.width(j);
                 const uint64_t dv = sdesc_step(dv0, s * SM::TILE);
                 ok = win_wait(vfull(s), ph, a.status);
-                if (j == 0) ok = ok && win_wait(oempty, (i & 1) ^ 1, a.status);  // the last tile's O has been read
-                ok = ok && win_wait(pready(J), (J >> 1) & 1, a.status);          // P of chunk J is in TMEM
-                if (!ok) break;
-                tc_fence_after();
 #pragma unroll
-                for (int kk = 0; kk < NK / 16; ++kk)
-                    if (kk * 16 < wd)
-                        win_mma_ta(t_out, tmem + (J & 1) * NK + kk * 8 + (kk * 16 >= NK / 2 ? NK / 4 : 0), sdesc_step(dv, kk * 16 * 128), id_o,
-                                   (j | kk) ? 1u : 0u, me);
-                win_commit(odone(J), me);
+                for (int x = 0; x < TP; ++x) {
+                    const uint32_t t_p = tmem + x * SM::TILE_COLS + (J & 1) * NK, t_o = tmem + x * SM::TILE_COLS + 2 * NK;
+                    if (j == 0) ok = ok && win_wait(oempty(x), (i & 1) ^ 1, a.status);  // the last tile's O has been read
+                    ok = ok && win_wait(pready(x, J), (J >> 1) & 1, a.status);          // P of chunk J is in TMEM
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int kk = 0; kk < NK / 16; ++kk)
+                        if (kk * 16 < wd)
+                            win_mma_ta(t_o, t_p + kk * 8 + (kk * 16 >= NK / 2 ? NK / 4 : 0), sdesc_step(dv, kk * 16 * 128), id_o, (j | kk) ? 1u : 0u, me);
+                    win_commit(odone(x, J), me);
+                }
+                if (!ok) break;
                 win_commit(vempty(s), me);
                 if (++s == NS) {
                     s = 0;
@@ -296,47 +350,48 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     } else {
         // ---- softmax: row = TMEM lane, half = keys NE half .. of every chunk, dimensions HD / 2 half ..
         constexpr int NE = NK / 2;
-        const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane, hr = row / rt;
+        const int x = warp >> 3, quarter = warp & 3, half = (warp >> 2) & 1, row = quarter * 32 + lane, hr = row / rt;
+        volatile int* flag = flags + x * 8 + 2 * quarter;
         const float k2 = a.scale * 1.4426950408889634f;  // softmax scale in base 2: exp(s x) = 2^(s log2(e) x)
-        const uint32_t lane_off = (uint32_t)(quarter * 32) << 16, t_o = t_out + lane_off + half * (HD / 2);
-        float* xch = reinterpret_cast<float*>(base + SM::X_OFF);
+        const uint32_t t_x = tmem + x * SM::TILE_COLS + ((uint32_t)(quarter * 32) << 16), t_o = t_x + 2 * NK + half * (HD / 2);
+        float* xch = reinterpret_cast<float*>(base + SM::X_OFF) + x * 512;
         bool ok = true;
         int J = 0, met = 0;  // chunks of all tiles; exchanges
         // the other thread's value of the row
-        auto exchange = [&](float x) {
+        auto exchange = [&](float mine) {
             float* p = xch + (met & 1) * 256;
-            p[half * 128 + row] = x;
+            p[half * 128 + row] = mine;
             __syncwarp();
-            if (lane == 0) mbar_arrive(pair(quarter));
-            ok = win_wait(pair(quarter), met & 1, a.status) && ok;
+            if (lane == 0) mbar_arrive(pair(x, quarter));
+            ok = win_wait(pair(x, quarter), met & 1, a.status) && ok;
             ++met;
             return p[(half ^ 1) * 128 + row];
         };
         for (int i = 0; ok && tl.more(); ++i, tl.next()) {
-            int c, g, r0;
-            tl.where(a, c, g, r0);
-            const WinRange win = range(r0);
-            const int keys = a.n_mem + min(a.Lq, r0 + rt);  // keys the tile's last token sees
-            const int tok = r0 + row - hr * rt;
+            tl.open(a);
+            const int c = tl.c, g = tl.g, r0 = min(tl.r0 + x * rt, a.Lq - 1);  // of a pair's second tile that is not there: any
+            const int first = a.n_mem + r0 + 1;                       // keys that the tile's first token sees
+            const int keys = a.n_mem + min(a.Lq, r0 + rt);            // its last
+            const int tok = tl.r0 + x * rt + row - hr * rt;
             const bool live = hr < a.group && tok < a.Lq;
-            const int vis = a.n_mem + (live ? tok : r0) + 1;  // the row sees keys before it (a row of padding: any)
+            const int vis = live ? a.n_mem + tok + 1 : first;         // the row sees keys before it (a row of padding: any)
             float m_run = -FLT_MAX;  // the row's scale; that: no key counted so far
             uint64_t l2[2] = {0, 0};
-            for (int j = 0; j < win.n; ++j, ++J) {
-                const uint32_t t_s = tmem + lane_off + (J & 1) * NK;
-                const int at = win.at(j, NK) + half * NE;
-                const int wd = width(win, r0, j) - half * NE;  // of the half's keys, if positive
-                ok = win_wait(sfull(J), (J >> 1) & 1, a.status);
+            for (int j = 0; j < tl.n; ++j, ++J) {
+                const uint32_t t_s = t_x + (J & 1) * NK;
+                const int at = tl.at(j) + half * NE;
+                const int wd = tl.width(j) - half * NE;  // of the half's keys, if positive
+                ok = win_wait(sfull(x, J), (J >> 1) & 1, a.status);
                 if (!ok) break;
                 tc_fence_after();
                 // Hidden keys get scores of -inf, written back: few chunks have any, and the loop over all of them stays short (its
                 // instructions, unrolled with masks, did not fit the instruction caches)
-                if (at + NE > a.n_mem + r0 + 1 || (at + NE > a.n_sink && at < keys - a.window)) {
+                if (at + NE > first || (at + NE > a.n_sink && at < keys - a.window)) {
 #pragma unroll 1
                     for (int b = 0; b < NE && b < wd; b += 16) {
                         // sixteen of which some row does not see all (in the window of all: from the last token's first key on)
                         const int p = at + b;
-                        if (p + 16 <= a.n_mem + r0 + 1 && (p + 16 <= a.n_sink || p >= keys - a.window)) continue;
+                        if (p + 16 <= first && (p + 16 <= a.n_sink || p >= keys - a.window)) continue;
                         const int nv = vis - p, nw = nv - a.window, ns = a.n_sink - p;
                         float v[16];
                         uint32_t hid[16];
@@ -360,10 +415,10 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                     if (!ok) break;
                     tc_fence_after();
                     if (m_run == -FLT_MAX) m_run = fmaxf(cm, -FLT_MAX);  // sums and O are 0 so far
-                } else if (flag[2 * quarter + (J & 1)] == J - 2) {
+                } else if (flag[J & 1] == J - 2) {
                     float l = sum_f32x4(l2);
                     l += exchange(l);
-                    const bool in = win_wait(odone(J - 1), ((J - 1) >> 1) & 1, a.status);  // O up to the last chunk
+                    const bool in = win_wait(odone(x, J - 1), ((J - 1) >> 1) & 1, a.status);  // O up to the last chunk
                     ok = ok && in;
                     if (!ok) break;
                     tc_fence_after();
@@ -390,8 +445,8 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                         uint32_t pk[8];
 #pragma unroll
                         for (int u = 0; u < 8; ++u) {
-                            const float2 x = unpack_f32x2(fma_f32x2(pack_f32x2(v[h + 2 * u], v[h + 2 * u + 1]), kk2, mm2));
-                            const float e0 = at_exp2(x.x), e1 = at_exp2(x.y);
+                            const float2 z = unpack_f32x2(fma_f32x2(pack_f32x2(v[h + 2 * u], v[h + 2 * u + 1]), kk2, mm2));
+                            const float e0 = at_exp2(z.x), e1 = at_exp2(z.y);
                             pk[u] = pack_bf16(e0, e1);
                             l2[u & 1] = add_f32x2(l2[u & 1], pack_f32x2(e0, e1));
                         }
@@ -413,17 +468,17 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                         tmem_ld16(t_s + half * NE + 32, v);
                         probs(v, 32, 16);
                     }
-                    if (__any_sync(0xffffffffu, sum_f32x4(l2) > 0x1p20f) && lane == 0) flag[2 * quarter + (J & 1)] = J;
+                    if (__any_sync(0xffffffffu, sum_f32x4(l2) > 0x1p20f) && lane == 0) flag[J & 1] = J;
                 }
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(pready(J));
+                if (lane == 0) mbar_arrive(pready(x, J));
             }
             if (!ok) break;
             float sum = sum_f32x4(l2);
             sum += exchange(sum);
-            ok = win_wait(odone(J - 1), ((J - 1) >> 1) & 1, a.status) && ok;
+            ok = win_wait(odone(x, J - 1), ((J - 1) >> 1) & 1, a.status) && ok;
             if (!ok) break;
             tc_fence_after();
             const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no key that counts: 0
@@ -450,7 +505,7 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(oempty);
+            if (lane == 0) mbar_arrive(oempty(x));
             if (live && !(top <= FLT_MAX)) {
                 const long long kv_off = (long long)(c / a.L) * a.s0 + (long long)(c % a.L) * a.s1 + (long long)g * a.s2;
 #pragma unroll 1
@@ -470,10 +525,10 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     if (warp == SM::S_WARP) tmem_dealloc(tmem, SM::TMEM);
 }
 
-template <int HD>
+template <int HD, int TP>
 cudaError_t launch(AttnArgs a, int n_ctx, int C, int sms, cudaStream_t st) {
     static PerDevice<SmemOptIn> once;
-    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(window_prefill_kernel<HD>), WinSmem<HD>::DYN, once);
+    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(window_prefill_kernel<HD, TP>), WinSmem<HD, TP>::DYN, once);
     if (e != cudaSuccess) return e;
     // The maps of the last call's shape, of which a call only sets the addresses
     struct Plan {
@@ -491,7 +546,7 @@ cudaError_t launch(AttnArgs a, int n_ctx, int C, int sms, cudaStream_t st) {
         const uint64_t kd[5] = {HD, keys, a.s2 ? (uint64_t)a.n_kv : 1, a.s1 ? (uint64_t)a.L : 1, a.s0 ? (uint64_t)n_ctx : 1};
         const uint64_t s3 = a.s3 * 2;
         const uint64_t ks[4] = {s3, kd[2] > 1 ? a.s2 * 2 : s3, kd[3] > 1 ? a.s1 * 2 : s3, kd[4] > 1 ? a.s0 * 2 : s3};
-        const uint32_t kb[5] = {64, WinSmem<HD>::NK, 1, 1, 1};
+        const uint32_t kb[5] = {64, WinSmem<HD, TP>::NK, 1, 1, 1};
         plan.key[0] = 0;
         if (!encode_map_bf16_4d(&plan.q, a.Q, qd, qs, qb) || !encode_map_bf16_5d(&plan.kv, a.K, kd, ks, kb)) return cudaErrorNotSupported;
         std::copy(key, key + 10, plan.key);
@@ -499,16 +554,19 @@ cudaError_t launch(AttnArgs a, int n_ctx, int C, int sms, cudaStream_t st) {
     CUtensorMap mq = plan.q, mk = plan.kv, mv = plan.kv;
     if (!retarget_map(&mq, a.Q) || !retarget_map(&mk, a.K) || !retarget_map(&mv, a.V)) return cudaErrorInvalidValue;
     a.rows = rows;
-    const long long tiles = (long long)((a.Lq + rows - 1) / rows) * a.n_kv * C;
+    const long long tiles = (long long)((a.Lq + TP * rows - 1) / (TP * rows)) * a.n_kv * C;
     if (tiles >= 1ll << 30) return cudaErrorNotSupported;
-    window_prefill_kernel<HD><<<(unsigned)std::min(tiles, 2ll * sms), WinSmem<HD>::THREADS, WinSmem<HD>::DYN, st>>>(mq, mk, mv, a, C);
+    window_prefill_kernel<HD, TP><<<(unsigned)std::min(tiles, (long long)WinSmem<HD, TP>::CTAS * sms), WinSmem<HD, TP>::THREADS, WinSmem<HD, TP>::DYN, st>>>(mq, mk, mv, a, C);
     return cudaGetLastError();
 }
 
 }  // namespace
 
 cudaError_t launch_window_prefill(const AttnArgs& a, int hd, int n_ctx, int C, int sms, cudaStream_t st) {
-    return hd == 64 ? launch<64>(a, n_ctx, C, sms, st) : launch<128>(a, n_ctx, C, sms, st);
+    if (hd == 64) return launch<64, 1>(a, n_ctx, C, sms, st);
+    // pairs of tiles, unless there is an SM for every tile
+    const long long tiles = (long long)((a.Lq + 128 / a.group - 1) / (128 / a.group)) * a.n_kv * C;
+    return tiles <= sms ? launch<128, 1>(a, n_ctx, C, sms, st) : launch<128, 2>(a, n_ctx, C, sms, st);
 }
 
 }  // namespace mone
