@@ -38,6 +38,7 @@ struct CaArgs {
     float scale;
     int ctas;                  // that the blocks are dealt out to
     float* part;               // [ctas + 4 ctas][2][ROWS][hd + 3]: the CTAs' parts, and those that their warps put here
+    int* info;                 // [chains][n_kv][RT] of an item, the CTA that has its first part and their number (<< 16)
     float* lse;                // [chains][n_kv][R] log2 of the sum of exp of items that one CTA has whole, with the weights
     float* z2;                 // [chains][n_kv][R][pitch] scores in base 2, -inf where not seen
     long long pitch;
@@ -101,18 +102,6 @@ struct CaDeal {
         base = __shfl_sync(0xffffffffu, incl - mine, k);
         return __shfl_sync(0xffffffffu, units, k);
     }
-    // the first unit of context c
-    __device__ int first_unit(const CaArgs& a, int c) {
-        if (a.v.n_ctx > 32) {
-            int before = 0;
-            for (int c0 = 0;; c0 += 32) {
-                const int up_to = scan(a, c0, before);
-                if (c < c0 + 32) break;
-                before = up_to;
-            }
-        }
-        return __shfl_sync(0xffffffffu, incl - mine, c & 31);
-    }
     // the first unit of CTA w
     __device__ int start(const CaArgs& a, int w) {
         const int u = w * share;  // below 2^30 + ctas share
@@ -121,11 +110,6 @@ struct CaDeal {
         const int n = locate(a, u, base, c);
         return n <= CA_WHOLE ? base + udiv(u - base, n) * n : u;
     }
-    // the parts of the item of units [u, u + n): from CTA `first`, 1 where it stays whole
-    __device__ int parts(int u, int n, int& first) const {
-        first = udiv(u, share);
-        return n <= CA_WHOLE ? 1 : udiv(u + n - 1, share) - first + 1;
-    }
 };
 
 // The pieces of a warp, one after the other: blocks [b0, b1) of an item
@@ -133,11 +117,13 @@ struct CaWalk {
     int u, end, ctx0, c, units;
     CaRange r;
     int l, g, rt, b0, b1;
+    int share, parts;         // of a CTA; CTAs that have a part of the item
     bool whole, cta_whole;    // the warp has the item whole, the CTA has
     bool first, last;         // the item begins in the CTA's share; the warp's last piece
     int cta0, cta1;           // the CTA's units
     __device__ CaWalk(const CaArgs& a) {
         CaDeal deal(a);
+        share = deal.share;
         cta0 = deal.start(a, blockIdx.x);
         cta1 = deal.start(a, blockIdx.x + 1);
         const int warp = threadIdx.x >> 5, n = cta1 - cta0;
@@ -159,8 +145,10 @@ struct CaWalk {
         b0 = u - ctx0 - in_ctx * units;
         const int e = min(units, b0 + end - u);
         whole = b0 == 0 && e == units;
-        cta_whole = u - b0 >= cta0 && u - b0 + units <= cta1;
-        first = u - b0 >= cta0;
+        const int u0 = u - b0;
+        cta_whole = u0 >= cta0 && u0 + units <= cta1;
+        first = u0 >= cta0;
+        parts = cta_whole || !first ? 1 : udiv(u0 + units - 1, share) - udiv(u0, share) + 1;
         b1 = min(e, r.nb);
         u += e - b0;
         last = u >= end;
@@ -220,6 +208,7 @@ struct Part {
 struct CaNote {
     const float* part;  // null: no such part
     int c, l, g, rt, n, first, whole;  // the item; positions held; whether the CTA has its first part, all of them
+    int parts;                         // of the item, one a CTA
 };
 
 // N dimensions from d of a row, from its O and sum, ready to be stored.  (The pools' pointers are their layer's and head's.)
@@ -289,6 +278,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
         const int row0 = it.rt * ROWS, rows = min(ROWS, a.R - row0);
         const size_t kv = ((size_t)it.c * a.v.L + it.l) * a.v.n_kv + it.g;
         const long long head = it.l * a.v.s_layer + it.g * a.v.s_head;
+        if (threadIdx.x == 0 && it.first) a.info[kv * a.RT + it.rt] = blockIdx.x | it.parts << 16;
         float* to = it.whole ? nullptr : P::of_cta(a, blockIdx.x, it.first);
         for (int e = 2 * threadIdx.x; e < rows * HD; e += 2 * CA_THREADS) {
             const int row = e / HD, d = e - row * HD;
@@ -448,7 +438,8 @@ struct CaCores {
         // the lane groups' softmaxes into one; lane group i writes row i
         using P = Part<HD, ROWS>;
         float* part = parts + (walk.b0 == 0) * P::FLOATS;
-        if (!walk.whole && lane == 0) notes[walk.b0 == 0] = {part, c, walk.l, walk.g, walk.rt, r.n, walk.first, walk.cta_whole};
+        if (walk.whole && lane == 0) a.info[kv * a.RT + walk.rt] = 1 << 16;
+        if (!walk.whole && lane == 0) notes[walk.b0 == 0] = {part, c, walk.l, walk.g, walk.rt, r.n, walk.first, walk.cta_whole, walk.parts};
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
             float mx = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], 8));
@@ -646,10 +637,9 @@ struct CaTensor {
                 }
             }
             for (int i = 0; i < n; ++i) {
-                feed(a, ahead, slot == 0 ? NS - 1 : slot - 1);  // the slot that was read last
                 ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * slot, phase, a.v.status));
                 if (!ok) break;
-                step(a, r, key0(w, i), ring + slot * STAGE, kv, row0, rows, k2, x);
+                step(a, ahead, r, key0(w, i), slot, kv, row0, rows, k2, x);
                 __syncwarp();  // the stage has been read
                 if (++slot == NS) {
                     slot = 0;
@@ -658,7 +648,8 @@ struct CaTensor {
             }
             // a part goes to the workspace while the ring is in use
             float* part = w.last && ok ? ring_part : P::of_warp(a, w.b0 == 0);
-            if (!w.whole && lane == 0) notes[w.b0 == 0] = {part, w.c, w.l, w.g, w.rt, r.n, w.first, w.cta_whole};
+            if (w.whole && lane == 0) a.info[kv * a.RT + w.rt] = 1 << 16;
+            if (!w.whole && lane == 0) notes[w.b0 == 0] = {part, w.c, w.l, w.g, w.rt, r.n, w.first, w.cta_whole, w.parts};
             const long long head = w.l * a.v.s_layer + w.g * a.v.s_head;
 #pragma unroll
             for (int i = 0; i < NT; ++i)
@@ -698,9 +689,10 @@ struct CaTensor {
     }
 
     // One stage's keys
-    __device__ __forceinline__ void step(const CaArgs& a, const CaRange& r, int j0, uint32_t ks, size_t kv, int row0, int rows, float k2, Rows& x) {
+    __device__ __forceinline__ void step(const CaArgs& a, Feed& ahead, const CaRange& r, int j0, int slot, size_t kv, int row0, int rows, float k2,
+                                         Rows& x) {
         const int lane = threadIdx.x & 31, gq = lane >> 2, t = lane & 3;
-        const uint32_t vs = ks + TILE;
+        const uint32_t ks = ring + slot * STAGE, vs = ks + TILE;
         const bool whole = j0 + SK <= r.n - a.n_tok + 1 && (j0 + SK <= a.n_sink || j0 >= r.n - a.window);
         if (!whole) {  // values that no row sees are not to meet a probability of 0
             for (int e = lane; e < SK * 8; e += 32) {
@@ -727,6 +719,7 @@ struct CaTensor {
 #pragma unroll
                 for (int i = 0; i < NT; ++i) ca_mma(s[i][u], A, x.q[i][k][0], x.q[i][k][1]);
             }
+        feed(a, ahead, slot == 0 ? NS - 1 : slot - 1);  // into the slot that was read last, while the products are under way
         uint32_t pb[NT][SK / 16][2];  // P^T: keys 16 u + 2 t, + 1 (and + 8) of row gq
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
@@ -855,12 +848,9 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) cache_finish_kernel(const CaAr
     const CaRange r(a, c);
     const int tile0 = ((int)blockIdx.x - a.R) * FIN_POS, p0 = tile0 + 4 * threadIdx.x;
     if (tile0 >= r.n || (tile0 >= a.n_sink && tile0 + FIN_POS <= r.t0 - a.window + 1)) return;  // nobody sees them
-    CaDeal deal(a);
-    const int units = r.units(), item0 = deal.first_unit(a, c) + (l * a.v.n_kv + g) * a.RT * units;
     pdl_wait();  // what is above reads only what the call was given
     if ((int)blockIdx.x < a.R) {
-        int first;
-        const int row = blockIdx.x, n = deal.parts(item0 + row / ROWS * units, units, first);
+        const int row = blockIdx.x, info = a.info[kv * a.RT + row / ROWS], first = info & 0xffff, n = info >> 16;
         if (n == 1) return;
         const long long head = l * a.v.s_layer + g * a.v.s_head;
         join_row<T, HD, ROWS>(a, c, row, kv, static_cast<const T*>(a.v.K) + head, static_cast<const T*>(a.v.V) + head, r.n, first, n, k2);
@@ -871,9 +861,8 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) cache_finish_kernel(const CaAr
         const int rows = min(FIN_ROWS, a.R - row0);
         __syncthreads();
         for (int row = threadIdx.x >> 5; row < rows; row += FIN_WARPS) {  // a warp a row
-            const int lane = threadIdx.x & 31, rt = (row0 + row) / ROWS, in = (row0 + row) % ROWS;
-            int first;
-            const int n = deal.parts(item0 + rt * units, units, first);
+            const int lane = threadIdx.x & 31, in = (row0 + row) % ROWS, info = a.info[kv * a.RT + (row0 + row) / ROWS];
+            const int first = info & 0xffff, n = info >> 16;
             float m = -INFINITY, lx = 0.f;
             if (n == 1) {
                 m = a.lse[kv * a.R + row0 + row];
@@ -972,12 +961,13 @@ cudaError_t launch_bf16(const CaArgs& a, int sms, cudaStream_t st) {
 }
 
 struct Layout {
-    size_t lse, z2, bytes;
+    size_t info, lse, z2, bytes;
     long long pitch;
     Layout(const DevState& s, const CacheView& v, int n_q, int n_tok) {
         const size_t kv = (size_t)v.n_ctx * v.L * v.n_kv, R = (size_t)n_q / v.n_kv * n_tok;
         auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-        lse = up((size_t)2 * (1 + CA_WARPS) * CA_SM_ROWS * s.sms * (s.hd + 3) * sizeof(float));  // after the parts
+        info = up((size_t)2 * (1 + CA_WARPS) * CA_SM_ROWS * s.sms * (s.hd + 3) * sizeof(float));  // after the parts
+        lse = info + up(kv * ((R + 3) / 4) * sizeof(int));  // items, at most
         z2 = lse + (v.score ? up(kv * R * sizeof(float)) : 0);
         pitch = (v.cap + KB - 1) / KB * KB;
         bytes = z2 + (v.score ? up(kv * R * pitch * sizeof(float)) : 0);
@@ -1008,6 +998,7 @@ cudaError_t launch_cache_attention(const DevState& s, const CacheView& v, const 
     a.scale = 1.0f / sqrtf((float)s.hd);
     char* b = static_cast<char*>(ws);
     a.part = reinterpret_cast<float*>(b);
+    a.info = reinterpret_cast<int*>(b + w.info);
     a.lse = v.score ? reinterpret_cast<float*>(b + w.lse) : nullptr;
     a.z2 = v.score ? reinterpret_cast<float*>(b + w.z2) : nullptr;
     a.pitch = w.pitch;
