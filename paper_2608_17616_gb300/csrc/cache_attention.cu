@@ -254,7 +254,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
     if ((threadIdx.x & 31) < 2) notes[2 * warp + (threadIdx.x & 31)].part = nullptr;
     __syncwarp();
     {
-        Form form(tmK, tmV, smem + warp * Form::WARP_BYTES);
+        Form form(tmK, tmV, smem + warp * Form::WARP_BYTES, a.RT);
         form.run(a, notes + 2 * warp);
     }
     __syncthreads();
@@ -322,7 +322,7 @@ struct CaCores {
 
     float* parts;
 
-    __device__ CaCores(const CUtensorMap&, const CUtensorMap&, uint8_t* smem) : parts(reinterpret_cast<float*>(smem)) {}
+    __device__ CaCores(const CUtensorMap&, const CUtensorMap&, uint8_t* smem, int) : parts(reinterpret_cast<float*>(smem)) {}
 
     __device__ __forceinline__ void run(const CaArgs& a, CaNote* notes) {
         CaWalk walk(a);
@@ -507,6 +507,15 @@ __device__ __forceinline__ uint32_t ca_transpose(uint32_t x) {
     return y;
 }
 
+// tma_load_5d with an L2 policy
+__device__ __forceinline__ void ca_load(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y, int z, int w, int v, uint64_t pol) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
+        " [%0], [%1, {%3, %4, %5, %6, %7}], [%2], %8;" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v), "l"(pol)
+        : "memory");
+}
+
 template <int HD_, int NT>
 struct CaTensor {
     using T = bf16;
@@ -521,8 +530,16 @@ struct CaTensor {
     const CUtensorMap &tmK, &tmV;
     uint32_t ring, bars;
     float* ring_part;  // the ring as the place of the warp's last part
+    uint64_t policy;
 
-    __device__ CaTensor(const CUtensorMap& k, const CUtensorMap& v, uint8_t* smem) : tmK(k), tmV(v) {
+    __device__ CaTensor(const CUtensorMap& k, const CUtensorMap& v, uint8_t* smem, int row_tiles) : tmK(k), tmV(v) {
+        // Keys and values that one row tile reads are read once: the first to leave L2, before the scores that the second kernel
+        // comes back for and what the program's other kernels keep there (16 contexts of up to 32K: 128 us for 133, with weights
+        // 142 for 156)
+        if (row_tiles == 1)
+            asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+        else
+            asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
         ring = smem_u32(smem);
         ring_part = reinterpret_cast<float*>(smem);
         bars = ring + BAR;
@@ -586,8 +603,8 @@ struct CaTensor {
             const int l = a.v.s_layer ? f.w.l : 0, g = a.v.s_head ? f.w.g : 0;  // what is shared has one element in the maps
 #pragma unroll
             for (int kb = 0; kb < HD / 64; ++kb) {
-                tma_load_5d(dst + kb * SLAB, &tmK, bars + 8 * s, 64 * kb, at, g, page, l);
-                tma_load_5d(dst + TILE + kb * SLAB, &tmV, bars + 8 * s, 64 * kb, at, g, page, l);
+                ca_load(dst + kb * SLAB, &tmK, bars + 8 * s, 64 * kb, at, g, page, l, policy);
+                ca_load(dst + TILE + kb * SLAB, &tmV, bars + 8 * s, 64 * kb, at, g, page, l, policy);
             }
         }
         __syncwarp();
