@@ -15,7 +15,7 @@
 // are reduced once per item, and the probabilities pass through shared memory into the
 // value accumulation, where a lane owns hd / 32 dimensions.
 //
-// The windowed attention (mone_window_attention) is the WIN instance of the decode and CUDA-core forms, and a prefill
+// The windowed attention (mone_window_attention) is the WIN instance of the decode form, and a prefill and a CUDA-core
 // form of its own in attention_window.cu: of the positions up to its own, a token sees the first n_sink and the last
 // `window`.  A form then steps over the chunks that hold some row's visible keys only (WinRange), and masks within them.
 #include <algorithm>
@@ -83,7 +83,7 @@ struct AttnSmem {
     static constexpr int FLOATS = P_OFF + ATT_WARPS * MAXI * KC;
 };
 
-template <typename T, int HD, bool WIN>
+template <typename T, int HD>
 __global__ void __launch_bounds__(ATT_WARPS * 32, 2) attention_kernel(const AttnArgs a) {
     using SM = AttnSmem<T, HD>;
     constexpr int D = HD / 32;  // value / accumulator dimensions per lane
@@ -126,10 +126,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, 2) attention_kernel(const Attn
     }
     const int last = min(a.Lq, r0 + a.rows) - 1;
     const int keys = a.n_mem + last + 1;  // positions the tile's last token sees
-    const WinRange win(a, a.n_mem + r0, keys - 1, KC);
-    const int n_ch = WIN ? win.n : (keys + KC - 1) / KC;
-    for (int ch = 0; ch < n_ch; ++ch) {
-        const int j0 = WIN ? win.at(ch, KC) : ch * KC;
+    for (int j0 = 0; j0 < keys; j0 += KC) {
         const int nk = min(KC, keys - j0);
         __syncthreads();
         stage_rows<T, HD>(Ks, Kc, a.s3, j0, nk, a.vec, SM::KP);
@@ -158,11 +155,7 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, 2) attention_kernel(const Attn
 #pragma unroll
         for (int k = 0; k < MAXI; ++k) {
             // causal / chunk masks; an item with no visible key in this chunk keeps its state
-            bool v0 = lane < nk && j0 + lane < vis[k], v1 = lane + 32 < nk && j0 + lane + 32 < vis[k];
-            if constexpr (WIN) {
-                v0 = v0 && (j0 + lane < a.n_sink || j0 + lane >= vis[k] - a.window);
-                v1 = v1 && (j0 + lane + 32 < a.n_sink || j0 + lane + 32 >= vis[k] - a.window);
-            }
+            const bool v0 = lane < nk && j0 + lane < vis[k], v1 = lane + 32 < nk && j0 + lane + 32 < vis[k];
             const float cm = warp_max(fmaxf(v0 ? z0[k] : -INFINITY, v1 ? z1[k] : -INFINITY));
             float p0 = 0.f, p1 = 0.f;
             if (cm != -INFINITY) {
@@ -204,24 +197,9 @@ __global__ void __launch_bounds__(ATT_WARPS * 32, 2) attention_kernel(const Attn
         const int it = warp + ATT_WARPS * k;
         const int h = g * a.group + it / a.rows, i = r0 + it % a.rows;
         T* o = static_cast<T*>(a.out) + (((size_t)c * a.n_q + h) * a.Lq + i) * HD;
-        if constexpr (WIN) {
-            const float inv = sum[k] > 0.f ? 1.f / sum[k] : sum[k];  // no key that counts: 0; NaN stays
-            bool bad = false;
+        const float inv = 1.f / sum[k];
 #pragma unroll
-            for (int d = 0; d < D; ++d) {
-                bad |= !isfinite(acc[k][d] * inv);
-                o[lane + 32 * d] = from_f<T>(acc[k][d] * inv);
-            }
-            if (bad) {
-                float w[D];
-                row_again<T, HD, D, 32>(static_cast<const T*>(a.Q) + (o - static_cast<T*>(a.out)), Kc, Vc, a.s3, vis[k], a, lane, w);
-                for (int d = 0; d < D; ++d) o[lane + 32 * d] = from_f<T>(w[d]);
-            }
-        } else {
-            const float inv = 1.f / sum[k];
-#pragma unroll
-            for (int d = 0; d < D; ++d) o[lane + 32 * d] = from_f<T>(acc[k][d] * inv);
-        }
+        for (int d = 0; d < D; ++d) o[lane + 32 * d] = from_f<T>(acc[k][d] * inv);
     }
 }
 
@@ -804,14 +782,14 @@ __global__ void __launch_bounds__(DE_WARPS * 32, HD == 64 ? 4 : 3) attention_dec
     if (splits > 1) cluster_sync();  // no CTA leaves while another reads its shared memory
 }
 
-template <typename T, int HD, bool WIN>
+template <typename T, int HD>
 cudaError_t launch_t(const AttnArgs& a, int C, cudaStream_t st) {
     const size_t smem = AttnSmem<T, HD>::FLOATS * sizeof(float);
     static PerDevice<SmemOptIn> once;
-    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(attention_kernel<T, HD, WIN>), smem, once);
+    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(attention_kernel<T, HD>), smem, once);
     if (e != cudaSuccess) return e;
     dim3 grid((a.Lq + a.rows - 1) / a.rows, a.n_kv, C);
-    attention_kernel<T, HD, WIN><<<grid, ATT_WARPS * 32, smem, st>>>(a);
+    attention_kernel<T, HD><<<grid, ATT_WARPS * 32, smem, st>>>(a);
     return cudaGetLastError();
 }
 
@@ -840,7 +818,7 @@ cudaError_t launch_prefill(AttnArgs a, int n_ctx, int C, cudaStream_t st) {
         const uint32_t kb[5] = {64, FaSmem<HD>::NK, 1, 1, 1};
         plan.key[0] = 0;
         if (!encode_map_bf16_4d(&plan.q, a.Q, qd, qs, qb) || !encode_map_bf16_5d(&plan.kv, a.K, kd, ks, kb))
-            return launch_t<bf16, HD, false>(a, C, st);  // strides past a tensor map's range (2^40 bytes): the CUDA-core form
+            return launch_t<bf16, HD>(a, C, st);  // strides past a tensor map's range (2^40 bytes): the CUDA-core form
         std::copy(key, key + 10, plan.key);
     }
     CUtensorMap mq = plan.q, mk = plan.kv, mv = plan.kv;
@@ -894,11 +872,9 @@ cudaError_t launch(const DevState& s, AttnArgs a, int n_ctx, cudaStream_t st) {
     a.vec = ((reinterpret_cast<uintptr_t>(a.K) | reinterpret_cast<uintptr_t>(a.V)) & 15u) == 0 && (a.s0 * el) % 16 == 0 &&
             (a.s1 * el) % 16 == 0 && (a.s2 * el) % 16 == 0 && (a.s3 * el) % 16 == 0;
     a.status = s.status;
-    if (s.dtype == 0)
-        return s.hd == 64 ? launch_t<float, 64, WIN>(a, C, st) : launch_t<float, 128, WIN>(a, C, st);
     // bf16 on the tensor cores when every row it stages is 16-byte aligned (the queries and the
-    // output are dense rows of hd elements); other cache layouts take the CUDA-core kernel
-    if (a.vec && ((reinterpret_cast<uintptr_t>(a.Q) | reinterpret_cast<uintptr_t>(a.out)) & 15u) == 0) {
+    // output are dense rows of hd elements); fp32 and other cache layouts take a CUDA-core kernel
+    if (s.dtype != 0 && a.vec && ((reinterpret_cast<uintptr_t>(a.Q) | reinterpret_cast<uintptr_t>(a.out)) & 15u) == 0) {
         const long long row_tiles = ((long long)a.group * a.Lq + DE_ROWS - 1) / DE_ROWS;
         if (row_tiles == 1 || row_tiles * a.n_kv * C <= DE_MAX_TILES)
             return s.hd == 64 ? launch_decode<64, WIN>(a, C, s.sms, st) : launch_decode<128, WIN>(a, C, s.sms, st);
@@ -909,7 +885,9 @@ cudaError_t launch(const DevState& s, AttnArgs a, int n_ctx, cudaStream_t st) {
             return s.hd == 64 ? launch_prefill<64>(a, n_ctx, C, st) : launch_prefill<128>(a, n_ctx, C, st);
         }
     }
-    return s.hd == 64 ? launch_t<bf16, 64, WIN>(a, C, st) : launch_t<bf16, 128, WIN>(a, C, st);
+    if constexpr (WIN) return launch_window_cores(a, s.dtype, s.hd, C, st);
+    if (s.dtype == 0) return s.hd == 64 ? launch_t<float, 64>(a, C, st) : launch_t<float, 128>(a, C, st);
+    return s.hd == 64 ? launch_t<bf16, 64>(a, C, st) : launch_t<bf16, 128>(a, C, st);
 }
 
 }  // namespace

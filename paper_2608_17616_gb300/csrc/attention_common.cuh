@@ -65,5 +65,7 @@ __device__ __forceinline__ float at_exp2(float x) {
 
 // The windowed prefill form (bf16, 16-byte-aligned rows), in attention_window.cu.  cudaErrorNotSupported: strides past a tensor map's range.
 cudaError_t launch_window_prefill(const AttnArgs& a, int hd, int n_ctx, int C, int sms, cudaStream_t st);
+// Its CUDA-core form: fp32 (dtype 0), and bf16 rows of any alignment.
+cudaError_t launch_window_cores(AttnArgs a, int dtype, int hd, int C, cudaStream_t st);
 
 }  // namespace mone

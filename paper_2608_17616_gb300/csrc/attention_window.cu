@@ -1,6 +1,7 @@
-// Windowed attention of many query rows (mone_window_attention, bf16 with 16-byte-aligned rows) on the tensor cores.
+// Windowed attention (mone_window_attention): many query rows on the tensor cores (bf16 with 16-byte-aligned rows), and
+// the CUDA-core form.  (Few rows on the tensor cores: attention.cu's decode form.)
 //
-// A tile is 128 MMA rows: rt = 128 / group tokens of each of a KV head's `group` query heads, which share every staged key
+// On the tensor cores, a tile is 128 MMA rows: rt = 128 / group tokens of each of a KV head's `group` query heads, which share every staged key
 // and value row.  A CTA takes one tile after another (hd 64, two CTAs an SM), or one pair of tiles of consecutive tokens
 // after another, which share the staged keys and values (hd 128, one CTA an SM: with two, the rings had room for two chunks
 // each, and S and P V waited for loads for a third of the time).  Per chunk of NK keys: S = Q K^T into one of two TMEM
@@ -525,6 +526,178 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     if (warp == SM::S_WARP) tmem_dealloc(tmem, SM::TMEM);
 }
 
+// ---------------------------------------------------------------- CUDA cores: fp32, and bf16 rows that are not aligned
+// 32 rows (query heads x tokens of a KV head) a CTA, chunks of 64 keys as fp32 in shared memory.  Both products are tiled in
+// registers: a thread has 4 rows x 4 keys of S (keys 16 apart), then 4 rows x 4 dimensions (twice at hd 128) of O, eight
+// 16-byte loads for 64 multiply-adds each.  A row's 64 scores lie in 16 lanes, which take its max by shuffles; each thread adds
+// up the probabilities that it made itself, and the sums meet at the end.
+constexpr int WC_THREADS = 128, WC_ROWS = 32, WC_KEYS = 64;
+
+template <int HD>
+struct WcSmem {
+    static constexpr int P = HD + 4;          // floats between rows: 16 lanes' 16-byte loads of a column fall on different banks
+    static constexpr int PP = WC_KEYS + 4;
+    static constexpr int K = WC_ROWS * P, V = K + WC_KEYS * P, PR = V + WC_KEYS * P, FLOATS = PR + WC_ROWS * PP;
+};
+
+// Row i of `n` (n: the rows that are there) of HD elements from `row(i)`, as fp32 times `scale`; zeros after the last.
+template <typename T, int HD, int ROWS, typename Row>
+__device__ __forceinline__ void wc_stage(float* dst, int n, bool vec, float scale, Row&& row) {
+    constexpr int PER = 16 / sizeof(T), VPR = HD / PER;
+    if (vec) {
+#pragma unroll 4
+        for (int e = threadIdx.x; e < ROWS * VPR; e += WC_THREADS) {
+            const int i = e / VPR, u = e % VPR;
+            const uint4 r = i < n ? __ldg(reinterpret_cast<const uint4*>(row(i)) + u) : make_uint4(0, 0, 0, 0);
+            const T* t = reinterpret_cast<const T*>(&r);
+#pragma unroll
+            for (int k = 0; k < PER; k += 4)
+                *reinterpret_cast<float4*>(dst + i * WcSmem<HD>::P + u * PER + k) =
+                    make_float4(to_f<T>(t[k]) * scale, to_f<T>(t[k + 1]) * scale, to_f<T>(t[k + 2]) * scale, to_f<T>(t[k + 3]) * scale);
+        }
+    } else {
+        for (int e = threadIdx.x; e < ROWS * HD; e += WC_THREADS) {
+            const int i = e / HD, d = e % HD;
+            dst[i * WcSmem<HD>::P + d] = i < n ? to_f<T>(row(i)[d]) * scale : 0.f;
+        }
+    }
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(WC_THREADS) window_cores_kernel(const AttnArgs a, int hb, int head_blocks, bool vec_q) {
+    using SM = WcSmem<HD>;
+    constexpr int DB = HD / 64;  // blocks of 64 dimensions
+    extern __shared__ float sh[];
+    float *Qs = sh, *Ks = sh + SM::K, *Vs = sh + SM::V, *Ps = sh + SM::PR;
+    const int c = blockIdx.z, g = blockIdx.y, tb = blockIdx.x / head_blocks, h0 = (blockIdx.x - tb * head_blocks) * hb;
+    const int r0 = tb * a.rows, heads = min(hb, a.group - h0), toks = min(a.rows, a.Lq - r0), rows = heads * toks;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const long long kv_off = (long long)(c / a.L) * a.s0 + (long long)(c % a.L) * a.s1 + (long long)g * a.s2;
+    const T* Kc = static_cast<const T*>(a.K) + kv_off;
+    const T* Vc = static_cast<const T*>(a.V) + kv_off;
+    // row i of the tile: head h0 + i / toks, token r0 + i % toks
+    auto q_at = [&](int i) { return (((size_t)c * a.n_q + (size_t)g * a.group + h0 + i / toks) * a.Lq + r0 + i % toks) * HD; };
+    wc_stage<T, HD, WC_ROWS>(Qs, rows, vec_q, a.scale, [&](int i) { return static_cast<const T*>(a.Q) + q_at(i); });
+    float o[4][4 * DB], m[4], l[4];
+    int vis[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = 4 * ty + i;
+        vis[i] = row < rows ? a.n_mem + r0 + row % toks + 1 : 0;
+        m[i] = -INFINITY;
+        l[i] = 0.f;
+#pragma unroll
+        for (int d = 0; d < 4 * DB; ++d) o[i][d] = 0.f;
+    }
+    const int keys = a.n_mem + r0 + toks;
+    const WinRange win(a, a.n_mem + r0, keys - 1, WC_KEYS);
+    for (int ch = 0; ch < win.n; ++ch) {
+        const int j0 = win.at(ch, WC_KEYS), nk = min(WC_KEYS, keys - j0);
+        __syncthreads();
+        wc_stage<T, HD, WC_KEYS>(Ks, nk, a.vec, 1.f, [&](int i) { return Kc + (long long)(j0 + i) * a.s3; });
+        wc_stage<T, HD, WC_KEYS>(Vs, nk, a.vec, 1.f, [&](int i) { return Vc + (long long)(j0 + i) * a.s3; });
+        __syncthreads();
+        float s[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+        for (int d = 0; d < HD; d += 4) {
+            float4 q[4], k[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = *reinterpret_cast<const float4*>(Qs + (4 * ty + i) * SM::P + d);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const float4*>(Ks + (tx + 16 * j) * SM::P + d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    s[i][j] = fmaf(q[i].x, k[j].x, fmaf(q[i].y, k[j].y, fmaf(q[i].z, k[j].z, fmaf(q[i].w, k[j].w, s[i][j]))));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float mn = m[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int p = j0 + tx + 16 * j;
+                s[i][j] = p < vis[i] && (p < a.n_sink || p >= vis[i] - a.window) ? s[i][j] : -INFINITY;
+                mn = fmaxf(mn, s[i][j]);
+            }
+#pragma unroll
+            for (int x = 1; x < 16; x <<= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, x));
+            const float corr = mn == m[i] ? 1.f : __expf(m[i] - mn), off = mn == -INFINITY ? 0.f : mn;
+            m[i] = mn;
+            l[i] *= corr;
+#pragma unroll
+            for (int d = 0; d < 4 * DB; ++d) o[i][d] *= corr;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float p = __expf(s[i][j] - off);
+                l[i] += p;
+                Ps[(4 * ty + i) * SM::PP + tx + 16 * j] = p;
+            }
+        }
+        __syncwarp();  // a row's probabilities are its own half-warp's
+#pragma unroll 4
+        for (int k = 0; k < WC_KEYS; k += 4) {
+            float4 p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const float4*>(Ps + (4 * ty + i) * SM::PP + k);
+#pragma unroll
+            for (int b = 0; b < DB; ++b) {
+                float4 v[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const float4*>(Vs + (k + u) * SM::P + 64 * b + 4 * tx);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float* x = o[i] + 4 * b;
+                    x[0] = fmaf(p[i].x, v[0].x, fmaf(p[i].y, v[1].x, fmaf(p[i].z, v[2].x, fmaf(p[i].w, v[3].x, x[0]))));
+                    x[1] = fmaf(p[i].x, v[0].y, fmaf(p[i].y, v[1].y, fmaf(p[i].z, v[2].y, fmaf(p[i].w, v[3].y, x[1]))));
+                    x[2] = fmaf(p[i].x, v[0].z, fmaf(p[i].y, v[1].z, fmaf(p[i].z, v[2].z, fmaf(p[i].w, v[3].z, x[2]))));
+                    x[3] = fmaf(p[i].x, v[0].w, fmaf(p[i].y, v[1].w, fmaf(p[i].z, v[2].w, fmaf(p[i].w, v[3].w, x[3]))));
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = 4 * ty + i;
+#pragma unroll
+        for (int x = 1; x < 16; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+        if (row >= rows) continue;
+        const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];  // no key that counts: 0
+        const size_t at = q_at(row);
+#pragma unroll
+        for (int b = 0; b < DB; ++b) {
+            T* out = static_cast<T*>(a.out) + at + 64 * b + 4 * tx;
+            float w[4];
+            bool bad = false;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                w[d] = o[i][4 * b + d] * inv;
+                bad |= !isfinite(w[d]);
+            }
+            if (bad) row_again<T, HD, 4, 1>(static_cast<const T*>(a.Q) + at, Kc, Vc, a.s3, vis[i], a, 64 * b + 4 * tx, w);
+            for (int d = 0; d < 4; ++d) out[d] = from_f<T>(w[d]);
+        }
+    }
+}
+
+template <typename T, int HD>
+cudaError_t launch_cores(AttnArgs a, int C, cudaStream_t st) {
+    constexpr size_t smem = WcSmem<HD>::FLOATS * sizeof(float);
+    static PerDevice<SmemOptIn> once;
+    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(window_cores_kernel<T, HD>), smem, once);
+    if (e != cudaSuccess) return e;
+    const int hb = std::min(a.group, WC_ROWS), head_blocks = (a.group + hb - 1) / hb;
+    a.rows = WC_ROWS / hb;  // tokens of a tile
+    const long long blocks = (long long)((a.Lq + a.rows - 1) / a.rows) * head_blocks;
+    window_cores_kernel<T, HD><<<dim3((unsigned)blocks, a.n_kv, C), WC_THREADS, smem, st>>>(
+        a, hb, head_blocks, (reinterpret_cast<uintptr_t>(a.Q) & 15u) == 0);
+    return cudaGetLastError();
+}
+
 template <int HD, int TP>
 cudaError_t launch(AttnArgs a, int n_ctx, int C, int sms, cudaStream_t st) {
     static PerDevice<SmemOptIn> once;
@@ -561,6 +734,11 @@ cudaError_t launch(AttnArgs a, int n_ctx, int C, int sms, cudaStream_t st) {
 }
 
 }  // namespace
+
+cudaError_t launch_window_cores(AttnArgs a, int dtype, int hd, int C, cudaStream_t st) {
+    if (dtype == 0) return hd == 64 ? launch_cores<float, 64>(a, C, st) : launch_cores<float, 128>(a, C, st);
+    return hd == 64 ? launch_cores<bf16, 64>(a, C, st) : launch_cores<bf16, 128>(a, C, st);
+}
 
 cudaError_t launch_window_prefill(const AttnArgs& a, int hd, int n_ctx, int C, int sms, cudaStream_t st) {
     if (hd == 64) return launch<64, 1>(a, n_ctx, C, sms, st);
