@@ -18,6 +18,7 @@
 // scores 70 above its scale within two chunks, is computed again at the end like one that met a value that is not finite.
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 #include "attention_common.cuh"
 #include "per_device.h"
@@ -531,7 +532,7 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
 // registers: a thread has 4 rows x 4 keys of S (keys 16 apart), then 4 rows x 4 dimensions (twice at hd 128) of O, eight
 // 16-byte loads for 64 multiply-adds each.  A row's 64 scores lie in 16 lanes, which take its max by shuffles; each thread adds
 // up the probabilities that it made itself, and the sums meet at the end.
-constexpr int WC_THREADS = 128, WC_ROWS = 32, WC_KEYS = 64;
+constexpr int WC_R = 4, WC_ROWS = 32, WC_KEYS = 64, WC_THREADS = 16 * WC_ROWS / WC_R;  // WC_R: rows of a thread
 
 template <int HD>
 struct WcSmem {
@@ -545,7 +546,7 @@ template <typename T, int HD, int ROWS, typename Row>
 __device__ __forceinline__ void wc_stage(float* dst, int n, bool vec, float scale, Row&& row) {
     constexpr int PER = 16 / sizeof(T), VPR = HD / PER;
     if (vec) {
-#pragma unroll 4
+#pragma unroll 8
         for (int e = threadIdx.x; e < ROWS * VPR; e += WC_THREADS) {
             const int i = e / VPR, u = e % VPR;
             const uint4 r = i < n ? __ldg(reinterpret_cast<const uint4*>(row(i)) + u) : make_uint4(0, 0, 0, 0);
@@ -578,11 +579,11 @@ __global__ void __launch_bounds__(WC_THREADS) window_cores_kernel(const AttnArgs
     // row i of the tile: head h0 + i / toks, token r0 + i % toks
     auto q_at = [&](int i) { return (((size_t)c * a.n_q + (size_t)g * a.group + h0 + i / toks) * a.Lq + r0 + i % toks) * HD; };
     wc_stage<T, HD, WC_ROWS>(Qs, rows, vec_q, a.scale, [&](int i) { return static_cast<const T*>(a.Q) + q_at(i); });
-    float o[4][4 * DB], m[4], l[4];
-    int vis[4];
+    float o[WC_R][4 * DB], m[WC_R], l[WC_R];
+    int vis[WC_R];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = 4 * ty + i;
+    for (int i = 0; i < WC_R; ++i) {
+        const int row = WC_R * ty + i;
         vis[i] = row < rows ? a.n_mem + r0 + row % toks + 1 : 0;
         m[i] = -INFINITY;
         l[i] = 0.f;
@@ -592,36 +593,46 @@ __global__ void __launch_bounds__(WC_THREADS) window_cores_kernel(const AttnArgs
     const int keys = a.n_mem + r0 + toks;
     const WinRange win(a, a.n_mem + r0, keys - 1, WC_KEYS);
     for (int ch = 0; ch < win.n; ++ch) {
-        const int j0 = win.at(ch, WC_KEYS), nk = min(WC_KEYS, keys - j0);
+        const int j0 = win.at(ch, WC_KEYS);
+        // keys up to the last that some row sees, and the sixteens of them
+        const bool first_only = ch < win.ns && a.n_mem + r0 - a.window + 1 >= (ch + 1) * WC_KEYS;
+        const int nk = min(WC_KEYS, (first_only ? min(a.n_sink, keys) : keys) - j0), nj = (nk + 15) / 16;
         __syncthreads();
         wc_stage<T, HD, WC_KEYS>(Ks, nk, a.vec, 1.f, [&](int i) { return Kc + (long long)(j0 + i) * a.s3; });
         wc_stage<T, HD, WC_KEYS>(Vs, nk, a.vec, 1.f, [&](int i) { return Vc + (long long)(j0 + i) * a.s3; });
         __syncthreads();
-        float s[4][4];
+        float s[WC_R][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < WC_R; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+        auto scores = [&](auto all) {  // all: of the four sixteens
 #pragma unroll 4
-        for (int d = 0; d < HD; d += 4) {
-            float4 q[4], k[4];
+            for (int d = 0; d < HD; d += 4) {
+                float4 q[WC_R];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = *reinterpret_cast<const float4*>(Qs + (4 * ty + i) * SM::P + d);
+                for (int i = 0; i < WC_R; ++i) q[i] = *reinterpret_cast<const float4*>(Qs + (WC_R * ty + i) * SM::P + d);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const float4*>(Ks + (tx + 16 * j) * SM::P + d);
+                for (int j = 0; j < 4; ++j) {
+                    if (!decltype(all)::value && j >= nj) break;
+                    const float4 k = *reinterpret_cast<const float4*>(Ks + (tx + 16 * j) * SM::P + d);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < WC_R; ++i)
+                        s[i][j] = fmaf(q[i].x, k.x, fmaf(q[i].y, k.y, fmaf(q[i].z, k.z, fmaf(q[i].w, k.w, s[i][j]))));
+                }
+            }
+        };
+        if (nj == 4)
+            scores(std::true_type());
+        else
+            scores(std::false_type());
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    s[i][j] = fmaf(q[i].x, k[j].x, fmaf(q[i].y, k[j].y, fmaf(q[i].z, k[j].z, fmaf(q[i].w, k[j].w, s[i][j]))));
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < WC_R; ++i) {
             float mn = m[i];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int p = j0 + tx + 16 * j;
-                s[i][j] = p < vis[i] && (p < a.n_sink || p >= vis[i] - a.window) ? s[i][j] : -INFINITY;
+                s[i][j] = p < j0 + nk && p < vis[i] && (p < a.n_sink || p >= vis[i] - a.window) ? s[i][j] : -INFINITY;
                 mn = fmaxf(mn, s[i][j]);
             }
 #pragma unroll
@@ -635,22 +646,22 @@ __global__ void __launch_bounds__(WC_THREADS) window_cores_kernel(const AttnArgs
             for (int j = 0; j < 4; ++j) {
                 const float p = __expf(s[i][j] - off);
                 l[i] += p;
-                Ps[(4 * ty + i) * SM::PP + tx + 16 * j] = p;
+                Ps[(WC_R * ty + i) * SM::PP + tx + 16 * j] = p;
             }
         }
         __syncwarp();  // a row's probabilities are its own half-warp's
 #pragma unroll 4
-        for (int k = 0; k < WC_KEYS; k += 4) {
-            float4 p[4];
+        for (int k = 0; k < nk; k += 4) {  // to a multiple of 4: zeros
+            float4 p[WC_R];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const float4*>(Ps + (4 * ty + i) * SM::PP + k);
+            for (int i = 0; i < WC_R; ++i) p[i] = *reinterpret_cast<const float4*>(Ps + (WC_R * ty + i) * SM::PP + k);
 #pragma unroll
             for (int b = 0; b < DB; ++b) {
                 float4 v[4];
 #pragma unroll
                 for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const float4*>(Vs + (k + u) * SM::P + 64 * b + 4 * tx);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < WC_R; ++i) {
                     float* x = o[i] + 4 * b;
                     x[0] = fmaf(p[i].x, v[0].x, fmaf(p[i].y, v[1].x, fmaf(p[i].z, v[2].x, fmaf(p[i].w, v[3].x, x[0]))));
                     x[1] = fmaf(p[i].x, v[0].y, fmaf(p[i].y, v[1].y, fmaf(p[i].z, v[2].y, fmaf(p[i].w, v[3].y, x[1]))));
@@ -661,8 +672,8 @@ __global__ void __launch_bounds__(WC_THREADS) window_cores_kernel(const AttnArgs
         }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = 4 * ty + i;
+    for (int i = 0; i < WC_R; ++i) {
+        const int row = WC_R * ty + i;
 #pragma unroll
         for (int x = 1; x < 16; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
         if (row >= rows) continue;
