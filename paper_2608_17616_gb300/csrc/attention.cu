@@ -876,7 +876,13 @@ cudaError_t launch(const DevState& s, AttnArgs a, int n_ctx, cudaStream_t st) {
     // output are dense rows of hd elements); fp32 and other cache layouts take a CUDA-core kernel
     if (s.dtype != 0 && a.vec && ((reinterpret_cast<uintptr_t>(a.Q) | reinterpret_cast<uintptr_t>(a.out)) & 15u) == 0) {
         const long long row_tiles = ((long long)a.group * a.Lq + DE_ROWS - 1) / DE_ROWS;
-        if (row_tiles == 1 || row_tiles * a.n_kv * C <= DE_MAX_TILES)
+        bool few = row_tiles == 1 || row_tiles * a.n_kv * C <= DE_MAX_TILES;
+        // The windowed prefill form splits no keys either, but starts in less time than the decode form of hd 128 (1 chain x 8
+        // heads x 4: 64 + 64 tokens, 6.8 us there and 10.1 here; 1 + 1000 at a window of 512, 9.1 and 9.8; 1 token of 16 chains, 9.6 and
+        // 13.7; but 4 + 1000 at 1024, 12.6 and 9.5; 16 + 4000 at 4096, 36.0 and 22.2).  At hd 64 the rule above holds for both.
+        if (WIN && s.hd == 128)
+            few = row_tiles * a.n_kv * C <= DE_MAX_TILES / 2 && std::min((long long)a.n_mem + a.Lq, (long long)a.n_sink + a.window + a.Lq) >= 800;
+        if (few)
             return s.hd == 64 ? launch_decode<64, WIN>(a, C, s.sms, st) : launch_decode<128, WIN>(a, C, s.sms, st);
         if constexpr (WIN) {
             const cudaError_t e = launch_window_prefill(a, s.hd, n_ctx, C, s.sms, st);
