@@ -398,3 +398,35 @@ def test_on_another_stream():
     s.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(s):
         attend(x, 4, 1, 0, ALL)
+
+
+# ----------------------------------------------------------------- offsets past 32 bits
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_pools_and_offsets_past_32_bits(dtype):
+    """Pages whose elements lie more than 2^31 from the pool's first, in a cache longer than its heads' first 2^31 bytes."""
+    hd, page, n_kv, n_pages = 64, 64, 2, (1 << 31) // (64 * 64 * 2) + 40
+    K, V = (torch.empty(1, n_pages, n_kv, page, hd, dtype=dtype, device="cuda") for _ in range(2))
+    x = Cache([1], n_layers=1, page=page, dtype=dtype)  # a handle
+    g = torch.Generator(device="cuda").manual_seed(5)
+    n, extra = 300, 20
+    far = torch.tensor([[n_pages - 1, n_pages - 2, n_pages - 30, 3, n_pages - 7, n_pages - 9]], dtype=torch.int32, device="cuda")
+    lens, out_lens = torch.tensor([0], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    score = torch.zeros(1, 1, n_kv, 6 * page, device="cuda")
+    k, v = (torch.randn(1, 1, n_kv, n, hd, generator=g, device="cuda").to(dtype) for _ in range(2))
+    mone.mone_cache_append(x.h, -1, mone.make_cache(K, V, far, lens, score), k, v, k.stride()[:4], n, out_lens)
+    q = torch.randn(1, 1, 4 * n_kv, 1, hd, generator=g, device="cuda").to(dtype)
+    out, c = torch.empty_like(q), mone.make_cache(K, V, far, out_lens, score)
+    mone.mone_cache_attention(x.h, -1, c, q, 4 * n_kv, 1, 0, ALL, out)
+    ref, w = O.window_attention(q[0, 0].float().cpu(), k[0, 0].float().cpu(), v[0, 0].float().cpu(), n - 1, 0, ALL)
+    to = torch.tensor([[n_pages - 3, n_pages - 5]], dtype=torch.int32, device="cuda")
+    to_score, kept = torch.zeros(1, 1, n_kv, 2 * page, device="cuda"), torch.empty(1, 1, n_kv, 100, dtype=torch.int32, device="cuda")
+    mone.mone_cache_evict(x.h, -1, c, 100, 4, extra, to, to_score, kept)
+    x.done()
+    assert rel_fro(out[0, 0].float().cpu(), ref) <= TOL[dtype]
+    assert rel_fro(score[0, 0, :, :n].cpu(), w) <= 1e-5
+    for h in range(n_kv):
+        at = O.cache_keep(score[0, 0, h, :n].cpu(), 100, 4, extra)
+        assert kept[0, 0, h].tolist() == at.tolist()
+        got = torch.cat([K[0, p, h] for p in to[0].tolist()])[:100]
+        assert torch.equal(got, k[0, 0, h, at])

@@ -194,3 +194,26 @@ def test_many_tiles_of_a_cta(hd, n_sink, window):
     for layer in (0, 9, L - 1):
         ref, _ = O.window_attention(Q[0, layer].float().cpu(), K[0, layer].float().cpu(), V[0, layer].float().cpu(), n_past, n_sink, window)
         assert rel_fro(outs[0][0, layer].float().cpu(), ref) <= 5e-3, layer
+
+
+@pytest.mark.parametrize("Lq", [3, 140])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_offsets_past_32_bits(Lq, dtype):
+    """A cache whose second layer and later positions lie more than 2^31 elements from its first."""
+    L, n_kv, hd, group, n_past = 20, 2, 64, 2, 500
+    run = handle(L, n_kv, hd, dtype)
+    g = torch.Generator(device="cuda").manual_seed(Lq)
+    S, pos = n_past + Lq, 1 << 16
+    size = L * n_kv * hd + (S - 1) * (1 << 22) + pos
+    buf = [torch.empty(size, dtype=dtype, device="cuda") for _ in range(2)]
+    K, V = (b.as_strided((1, L, n_kv, S, hd), (0, n_kv * hd, hd, 1 << 22, 1)) for b in buf)
+    for x in (K, V):
+        x.copy_(torch.randn(x.shape, generator=g, device="cuda"))
+    Q = torch.randn(1, L, group * n_kv, Lq, hd, generator=g, device="cuda").to(dtype)
+    out = torch.full_like(Q, 7.0)
+    mone.mone_window_attention(run.h, -1, Q, group * n_kv, Lq, K, V, K.stride()[:4], n_past, 10, 490, out)
+    mone.mone_mem_sync(run.h)
+    run.close()
+    for layer in (0, L - 1):
+        ref, _ = O.window_attention(Q[0, layer].float().cpu(), K[0, layer].float().cpu(), V[0, layer].float().cpu(), n_past, 10, 490)
+        assert rel_fro(out[0, layer].float().cpu(), ref) <= TOL[dtype], layer
