@@ -1,21 +1,22 @@
 // Windowed attention (mone_window_attention): many query rows on the tensor cores (bf16 with 16-byte-aligned rows), and
 // the CUDA-core form.  (Few rows on the tensor cores: attention.cu's decode form.)
 //
-// On the tensor cores, a tile is 128 MMA rows: rt = 128 / group tokens of each of a KV head's `group` query heads, which share every staged key
-// and value row.  A CTA takes one tile after another (hd 64, two CTAs an SM), or one pair of tiles of consecutive tokens
-// after another, which share the staged keys and values (hd 128, one CTA an SM: with two, the rings had room for two chunks
-// each, and S and P V waited for loads for a third of the time).  Per chunk of NK keys: S = Q K^T into one of two TMEM
-// buffers, the softmax, whose bf16 probabilities go over the scores as the A operand of O += P V, O in TMEM.
-// Eight warps for each of the tiles: the softmax and the output, two threads a row (= TMEM lane), one for each half of a chunk's keys and of the head's
-// dimensions.  Then the loader; keys and values by TMA with the caller's strides through a ring each, the queries into a
-// buffer of their own.  Then the MMA issuers, of S, two chunks ahead, one for each tile, and of P V.  Loads and S run on over the end of a
-// tile (a window has few chunks, so a tile's first loads and last output would otherwise cost as much as its
-// chunks): the chunks of all tiles of a CTA are one sequence.
+// On the tensor cores, a tile is 128 MMA rows: rt = 128 / group tokens of each of a KV head's `group` query heads, which share
+// every staged key and value row.  A CTA takes pairs of tiles of consecutive tokens, which share the staged keys and values too,
+// one after another (hd 64: two CTAs an SM, hd 128: one; TMEM holds no more).  Per chunk of 64 keys and tile: S = Q K^T into
+// TMEM, the softmax, whose bf16 probabilities go over the scores as the A operand of O += P V, O in TMEM.  A tile has two S
+// buffers at hd 128, one at hd 64, where the other three tiles of the SM fill the wait.
+// Four warps for each tile do the softmax and the output, a thread a row (= TMEM lane).  (Two threads a row, one tile at a time
+// at hd 64 and two at hd 128: 282 us for 223 at 16 layers of 32 heads over 8, 2048 tokens, window 512, hd 64, and 755 for 700 at
+// 16001 tokens, window 4096, hd 128.)  Then the loader: keys and values by TMA with the caller's strides through a ring each,
+// the queries into a buffer of their own.  Then the MMA issuers, of each tile's S, NB chunks ahead, and of P V.  Loads and S run on
+// over the end of a tile (a window has few chunks, so a tile's first loads and last output would otherwise cost as much as
+// its chunks): the chunks of all tiles of a CTA are one sequence.
 //
-// The softmax's instructions bound it, so it does without a maximum for each chunk: the scale of a row is the max of its
-// first chunk with a key that counts, and floating point does not mind later scores above it.  A row whose sum has passed 2^20
-// is scaled down two chunks later (its two threads and the P V behind agree by then); one that overflows before, by
-// scores 70 above its scale within two chunks, is computed again at the end like one that met a value that is not finite.
+// The softmax does without a maximum for each chunk: the scale of a row is the max of its first chunk with a key that counts,
+// and floating point does not mind later scores above it.  A row whose sum has passed 2^20 is scaled down before the next chunk;
+// one that overflows within a chunk, by scores 70 above its scale, is computed again at the end like one that met a value
+// that is not finite.
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>
@@ -27,25 +28,23 @@ namespace mone {
 
 namespace {
 
-// TP: tiles at a time
-template <int HD, int TP>
+template <int HD>
 struct WinSmem {
-    static constexpr int CTAS = HD == 64 ? 2 / TP : 1;     // CTAs an SM
-    static constexpr int LOAD_WARP = 8 * TP, S_WARP = LOAD_WARP + 1, PV_WARP = S_WARP + TP, THREADS = (PV_WARP + 1) * 32;
-    static constexpr int NK = HD == 64 ? 96 : 64;          // key positions per chunk: 2 NK + HD TMEM columns for each tile
-    static constexpr int TILE_COLS = 256, TMEM = TP * TILE_COLS;
-    static constexpr int QB = HD == 64 ? 2 : 1;            // query buffers
+    static constexpr int CTAS = HD == 64 ? 2 : 1;          // CTAs an SM
+    static constexpr int NK = 64;                          // key positions per chunk
+    static constexpr int NB = HD == 64 ? 1 : 2;            // S (and P) buffers of a tile: NB NK + HD TMEM columns
+    static constexpr int LOAD_WARP = 8, S_WARP = LOAD_WARP + 1, PV_WARP = S_WARP + 2, THREADS = (PV_WARP + 1) * 32;
+    static constexpr int TILE_COLS = HD == 64 ? 128 : 256, TMEM = 2 * TILE_COLS;
+    static constexpr int QB = HD == 64 ? 2 : 1;            // query buffers, of a pair each
     static constexpr int Q_SLAB = 128 * 128, Q_TILE = (HD / 64) * Q_SLAB;  // 128 query rows x 64 bf16; x HD
     static constexpr int SLAB = NK * 128, TILE = (HD / 64) * SLAB;         // NK keys x 64 bf16; x HD
-    static constexpr int NS = CTAS == 2 ? 3 : 4;           // slots of the ring of keys and of that of values, a chunk each
-    static constexpr int K_OFF = QB * TP * Q_TILE, V_OFF = K_OFF + NS * TILE;
-    static constexpr int X_OFF = V_OFF + NS * TILE;        // [tile][2][2][128] floats that a row's two threads exchange
-    static constexpr int FLAG_OFF = X_OFF + TP * 2 * 2 * 128 * 4;  // [tile][4][2] chunk in which a sum of a quarter's rows passed 2^20
-    // qfull[QB] qempty[QB] kfull[NS] kempty[NS] vfull[NS] vempty[NS], and for each tile sfull[2] odone[2] pready[2] oempty pair[4]
-    static constexpr int BAR_OFF = FLAG_OFF + TP * 4 * 2 * 4, TILE_BARS = 11;
-    static constexpr int SLOT_OFF = BAR_OFF + (2 * QB + 4 * NS + TP * TILE_BARS) * 8;
+    static constexpr int NS = HD == 64 ? 2 : 4;            // slots of the ring of keys and of that of values, a chunk each
+    static constexpr int K_OFF = QB * 2 * Q_TILE, V_OFF = K_OFF + NS * TILE;
+    // qfull[QB] qempty[QB] kfull[NS] kempty[NS] vfull[NS] vempty[NS], and for each tile sfull[NB] odone[NB] pready[NB] oempty
+    static constexpr int BAR_OFF = V_OFF + NS * TILE, TILE_BARS = 3 * NB + 1;
+    static constexpr int SLOT_OFF = BAR_OFF + (2 * QB + 4 * NS + 2 * TILE_BARS) * 8;
     static constexpr int DYN = SLOT_OFF + 16 + 1024;       // + TMEM slot, + alignment slack
-    static_assert(2 * NK + HD <= TILE_COLS && CTAS * TMEM <= 512 && CTAS * (DYN + 1024) <= 228 * 1024, "CTAs an SM");
+    static_assert(NB * NK + HD <= TILE_COLS && CTAS * TMEM <= 512 && CTAS * (DYN + 1024) <= 228 * 1024, "CTAs an SM");
 };
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -121,27 +120,55 @@ __device__ __forceinline__ bool win_wait(uint32_t bar, uint32_t parity, int* sta
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, status));
 }
 
-// The tiles (pairs of tiles) of a CTA, as its warps step through them
-template <int TP, int NK>
+
+// The lowest n bits (n <= 0: none; n >= 32: all)
+__device__ __forceinline__ uint32_t low_bits(int n) {
+    uint32_t r;
+    asm("shl.b32 %0, -1, %1;" : "=r"(r) : "r"(max(n, 0)));  // a shift by 32 or more leaves 0
+    return ~r;
+}
+
+// The tiles of a CTA, as its warps step through them, pair by pair: the last tokens' come first, of all chains and heads, since
+// the first ones see fewer keys, and the CTAs take them in turn, to and fro.  (In the order of the tokens, a CTA's pairs could
+// all lie at the same place of their prompts: 223 us for 207 at 16 layers of 32 heads, 2048 tokens, window 512, hd 64.)  What is
+// left of the pairs goes by single tiles if there is a CTA for each.
+template <int NK>
 struct WinTiles {
-    int tile, step, count, nt;  // this tile, distance to the CTA's next, tiles in all, of a KV head
+    int item, step, turn;       // this item, distance to the CTA's next and to the one after that
+    int count, whole;           // items in all; those that are pairs
+    int np, heads, odd;         // pairs of a KV head; KV heads in all; whether the last pair of a head is one tile
     int c, g, r0, t0, t1;       // chain, KV head, first token; positions of its first and last
     int ns, lo, n, wf, wl;      // chunks of the first positions; first position after them; chunks in all; widths of the last ones
+    bool two;
     __device__ WinTiles(const AttnArgs& a, int C) {
-        nt = (a.Lq + TP * a.rows - 1) / (TP * a.rows);
-        tile = blockIdx.x;
-        step = gridDim.x;
-        count = nt * a.n_kv * C;
+        const int nt = (a.Lq + a.rows - 1) / a.rows, grid = gridDim.x, b = blockIdx.x;
+        np = (nt + 1) / 2;
+        odd = nt & 1;
+        heads = a.n_kv * C;
+        const int pairs = np * heads, rest = pairs % grid;
+        whole = 2 * rest <= grid ? pairs - rest : pairs;
+        count = whole + 2 * (pairs - whole);
+        item = b;
+        step = 2 * (grid - 1 - b) + 1;
+        turn = 2 * b + 1;
     }
-    __device__ bool more() const { return tile < count; }
-    __device__ void next() { tile += step; }
+    // (the second tile of a head's last pair may not be there; single tiles are a CTA's last)
+    __device__ bool more() const { return item < count && !(odd && item >= whole && ((item - whole) & 1) && whole + (item - whole) / 2 < heads); }
+    __device__ void next() {
+        item += step;
+        const int s = step;
+        step = turn;
+        turn = s;
+    }
+    __device__ bool has(int x) const { return x == 0 || two; }
     __device__ void open(const AttnArgs& a) {
-        const int cg = tile / nt;
-        r0 = (tile - cg * nt) * TP * a.rows;
+        const int single = item >= whole, p = single ? whole + (item - whole) / 2 : item, rank = p / heads, cg = p - rank * heads;
+        two = !single && !(odd && rank == 0);
+        r0 = (2 * (np - 1 - rank) + (single ? (item - whole) & 1 : 0)) * a.rows;
         c = cg / a.n_kv;
         g = cg - c * a.n_kv;
         t0 = a.n_mem + r0;
-        t1 = a.n_mem + min(a.Lq, r0 + TP * a.rows) - 1;
+        t1 = a.n_mem + min(a.Lq, r0 + (two ? 2 : 1) * a.rows) - 1;
         const WinRange w(a, t0, t1, NK);
         ns = w.ns;
         lo = w.lo;
@@ -156,12 +183,12 @@ struct WinTiles {
     __device__ int width(int j) const { return j == n - 1 ? wl : j == ns - 1 ? wf : NK; }
 };
 
-template <int HD, int TP>
-__global__ void __launch_bounds__(WinSmem<HD, TP>::THREADS, WinSmem<HD, TP>::CTAS)
+template <int HD>
+__global__ void __launch_bounds__(WinSmem<HD>::THREADS, WinSmem<HD>::CTAS)
 window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                       const AttnArgs a, int C) {
-    using SM = WinSmem<HD, TP>;
-    constexpr int NS = SM::NS, NK = SM::NK, QB = SM::QB;
+    using SM = WinSmem<HD>;
+    constexpr int NS = SM::NS, NK = SM::NK, QB = SM::QB, NB = SM::NB;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t bars = smem_u32(base + SM::BAR_OFF);
@@ -172,37 +199,33 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     auto kempty = [&](int s) { return bars + 8 * (KB0 + NS + s); };
     auto vfull = [&](int s) { return bars + 8 * (VB0 + s); };
     auto vempty = [&](int s) { return bars + 8 * (VB0 + NS + s); };
-    // of tile x (of a pair) and chunk j of all the CTA's, phase j >> 1
-    auto sfull = [&](int x, int j) { return bars + 8 * (SB0 + x * SM::TILE_BARS + (j & 1)); };
-    auto odone = [&](int x, int j) { return bars + 8 * (SB0 + x * SM::TILE_BARS + 2 + (j & 1)); };
-    auto pready = [&](int x, int j) { return bars + 8 * (SB0 + x * SM::TILE_BARS + 4 + (j & 1)); };
-    auto oempty = [&](int x) { return bars + 8 * (SB0 + x * SM::TILE_BARS + 6); };           // of a tile
-    auto pair = [&](int x, int q) { return bars + 8 * (SB0 + x * SM::TILE_BARS + 7 + q); };  // of the two warps of a quarter of the rows
-    volatile int* flags = reinterpret_cast<int*>(base + SM::FLAG_OFF);
+    // of tile x (of a pair) and chunk j of all the CTA's, phase j / NB
+    auto sfull = [&](int x, int j) { return bars + 8 * (SB0 + x * SM::TILE_BARS + j % NB); };
+    auto odone = [&](int x, int j) { return bars + 8 * (SB0 + x * SM::TILE_BARS + NB + j % NB); };
+    auto pready = [&](int x, int j) { return bars + 8 * (SB0 + x * SM::TILE_BARS + 2 * NB + j % NB); };
+    auto oempty = [&](int x) { return bars + 8 * (SB0 + x * SM::TILE_BARS + 3 * NB); };  // of a tile
     uint32_t* slot = reinterpret_cast<uint32_t*>(base + SM::SLOT_OFF);
     // the warp's number from one lane, and below the TMEM address: the compiler then knows them to be the same in all
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     if (tid == 0) {
         for (int i = 0; i < QB; ++i) {
             mbar_init(qfull(i), 1);
-            mbar_init(qempty(i), TP);
+            mbar_init(qempty(i), 2);
         }
         for (int s = 0; s < NS; ++s) {
             mbar_init(kfull(s), 1);
-            mbar_init(kempty(s), TP);
+            mbar_init(kempty(s), 2);
             mbar_init(vfull(s), 1);
             mbar_init(vempty(s), 1);
         }
-        for (int x = 0; x < TP; ++x) {
-            for (int b = 0; b < 2; ++b) {
+        for (int x = 0; x < 2; ++x) {
+            for (int b = 0; b < NB; ++b) {
                 mbar_init(sfull(x, b), 1);
                 mbar_init(odone(x, b), 1);
-                mbar_init(pready(x, b), 8);  // the tile's softmax warps
+                mbar_init(pready(x, b), 4);
             }
-            mbar_init(oempty(x), 8);
-            for (int q = 0; q < 4; ++q) mbar_init(pair(x, q), 2);
+            mbar_init(oempty(x), 4);
         }
-        for (int i = 0; i < TP * 8; ++i) flags[i] = -8;
         fence_mbar_init();
     }
     if (warp == SM::S_WARP) {
@@ -212,9 +235,9 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = __shfl_sync(0xffffffffu, *slot, 0);  // of a tile: two S (and P) buffers, then O
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *slot, 0);  // of a tile: the S (and P) buffers, then O
     const int rt = a.rows;
-    WinTiles<TP, NK> tl(a, C);
+    WinTiles<NK> tl(a, C);
 
     if (warp == SM::LOAD_WARP) {
         const uint32_t me = lane == 0;
@@ -252,12 +275,12 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             ok = win_wait(qempty(i), (i / QB & 1) ^ 1, a.status);
             if (!ok) break;
             if (me) {
-                mbar_expect_tx(qfull(i), TP * (HD / 64) * a.group * rt * 128);
+                mbar_expect_tx(qfull(i), (tl.two ? 2 : 1) * (HD / 64) * a.group * rt * 128);
 #pragma unroll
-                for (int x = 0; x < TP; ++x)
+                for (int x = 0; x < 2; ++x)
 #pragma unroll
-                    for (int kb = 0; kb < HD / 64; ++kb)  // the query rows, [head of the group][token]
-                        tma_load_4d(smem_u32(base + (i % QB * TP + x) * SM::Q_TILE) + kb * SM::Q_SLAB, &tmQ, qfull(i), 64 * kb, tl.r0 + x * rt,
+                    for (int kb = 0; kb < HD / 64 && tl.has(x); ++kb)  // the query rows, [head of the group][token]
+                        tma_load_4d(smem_u32(base + (i % QB * 2 + x) * SM::Q_TILE) + kb * SM::Q_SLAB, &tmQ, qfull(i), 64 * kb, tl.r0 + x * rt,
                                     tl.g * a.group, tl.c);
             }
             __syncwarp();
@@ -281,29 +304,32 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         if (!ok) drain_copies();
         __syncwarp();
     } else if (warp >= SM::S_WARP && warp < SM::PV_WARP) {
-        // S = Q K^T over HD (K-major both)
+        // S = Q K^T over HD (K-major both), of one of the tiles
         const uint32_t me = lane == 0, x = warp - SM::S_WARP, t_s = tmem + x * SM::TILE_COLS;
         const uint64_t dq0 = sdesc_sw128(smem_u32(base + x * SM::Q_TILE), 16), dk0 = sdesc_sw128(smem_u32(base + SM::K_OFF), 16);
         bool ok = true;
-        int s = 0, ph = 0, J = 0;  // the ring's next slot and its phase; chunk of all
+        int s = 0, ph = 0, J = 0;  // the ring's next slot and its phase; chunk of all the tile's
         for (int i = 0; ok && tl.more(); ++i, tl.next()) {
             tl.open(a);
             ok = win_wait(qfull(i), i / QB & 1, a.status);
-            const uint64_t dq = sdesc_step(dq0, i % QB * TP * SM::Q_TILE);
-            for (int j = 0; ok && j < tl.n; ++j, ++J) {
+            const uint64_t dq = sdesc_step(dq0, i % QB * 2 * SM::Q_TILE);
+            for (int j = 0; ok && j < tl.n; ++j) {
                 const uint32_t id_s = idesc_bf16_f32(128, tl.width(j), false, false);
                 const uint64_t dk = sdesc_step(dk0, s * SM::TILE);
                 ok = win_wait(kfull(s), ph, a.status);
-                if (J >= 2) ok = ok && win_wait(odone(x, J), ((J >> 1) & 1) ^ 1, a.status);  // P V of chunk J - 2 has read its P, where S goes
-                if (!ok) break;
-                tc_fence_after();
+                if (tl.has(x)) {
+                    if (J >= NB) ok = ok && win_wait(odone(x, J), (J / NB & 1) ^ 1, a.status);  // P V of chunk J - NB has read its P, where S goes
+                    if (!ok) break;
+                    tc_fence_after();
 #pragma unroll
-                for (int kb = 0; kb < HD / 64; ++kb)
+                    for (int kb = 0; kb < HD / 64; ++kb)
 #pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        win_mma(t_s + (J & 1) * NK, sdesc_step(dq, kb * SM::Q_SLAB + u * 32), sdesc_step(dk, kb * SM::SLAB + u * 32), id_s,
-                                (kb | u) ? 1u : 0u, me);
-                win_commit(sfull(x, J), me);
+                        for (int u = 0; u < 4; ++u)
+                            win_mma(t_s + J % NB * NK, sdesc_step(dq, kb * SM::Q_SLAB + u * 32), sdesc_step(dk, kb * SM::SLAB + u * 32), id_s,
+                                    (kb | u) ? 1u : 0u, me);
+                    win_commit(sfull(x, J), me);
+                    ++J;
+                }
                 win_commit(kempty(s), me);
                 if (++s == NS) {
                     s = 0;
@@ -315,28 +341,30 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         if (!ok) drain_copies();
         __syncwarp();
     } else if (warp == SM::PV_WARP) {
-        // O += P V over the chunk's keys (P in TMEM, that of a half over its own scores; V MN-major)
+        // O += P V over the chunk's keys (P in TMEM, over the scores; V MN-major)
         const uint32_t me = lane == 0, id_o = idesc_bf16_f32(128, HD, false, true);
         const uint64_t dv0 = sdesc_sw128(smem_u32(base + SM::V_OFF), SM::SLAB);
         bool ok = true;
-        int s = 0, ph = 0, J = 0;
-        for (int i = 0; ok && tl.more(); ++i, tl.next()) {
+        int s = 0, ph = 0, count[2] = {}, chunk[2] = {};  // ring; items and chunks of each tile
+        for (; ok && tl.more(); tl.next()) {
             tl.open(a);
-            for (int j = 0; ok && j < tl.n; ++j, ++J) {
+            for (int j = 0; ok && j < tl.n; ++j) {
                 const int wd = tl.width(j);
                 const uint64_t dv = sdesc_step(dv0, s * SM::TILE);
                 ok = win_wait(vfull(s), ph, a.status);
 #pragma unroll
-                for (int x = 0; x < TP; ++x) {
-                    const uint32_t t_p = tmem + x * SM::TILE_COLS + (J & 1) * NK, t_o = tmem + x * SM::TILE_COLS + 2 * NK;
-                    if (j == 0) ok = ok && win_wait(oempty(x), (i & 1) ^ 1, a.status);  // the last tile's O has been read
-                    ok = ok && win_wait(pready(x, J), (J >> 1) & 1, a.status);          // P of chunk J is in TMEM
+                for (int x = 0; x < 2; ++x) {
+                    if (!tl.has(x)) continue;
+                    const int J = chunk[x]++;
+                    const uint32_t t_p = tmem + x * SM::TILE_COLS + J % NB * NK, t_o = tmem + x * SM::TILE_COLS + NB * NK;
+                    if (j == 0) ok = ok && win_wait(oempty(x), (count[x]++ & 1) ^ 1, a.status);  // the last tile's O has been read
+                    ok = ok && win_wait(pready(x, J), J / NB & 1, a.status);          // P of chunk J is in TMEM
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll
                     for (int kk = 0; kk < NK / 16; ++kk)
                         if (kk * 16 < wd)
-                            win_mma_ta(t_o, t_p + kk * 8 + (kk * 16 >= NK / 2 ? NK / 4 : 0), sdesc_step(dv, kk * 16 * 128), id_o, (j | kk) ? 1u : 0u, me);
+                            win_mma_ta(t_o, t_p + kk * 8, sdesc_step(dv, kk * 16 * 128), id_o, (j | kk) ? 1u : 0u, me);
                     win_commit(odone(x, J), me);
                 }
                 if (!ok) break;
@@ -350,28 +378,16 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         if (!ok) drain_copies();
         __syncwarp();
     } else {
-        // ---- softmax: row = TMEM lane, half = keys NE half .. of every chunk, dimensions HD / 2 half ..
-        constexpr int NE = NK / 2;
-        const int x = warp >> 3, quarter = warp & 3, half = (warp >> 2) & 1, row = quarter * 32 + lane, hr = row / rt;
-        volatile int* flag = flags + x * 8 + 2 * quarter;
+        // ---- softmax: row = TMEM lane
+        const int x = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane, hr = row / rt;
         const float k2 = a.scale * 1.4426950408889634f;  // softmax scale in base 2: exp(s x) = 2^(s log2(e) x)
-        const uint32_t t_x = tmem + x * SM::TILE_COLS + ((uint32_t)(quarter * 32) << 16), t_o = t_x + 2 * NK + half * (HD / 2);
-        float* xch = reinterpret_cast<float*>(base + SM::X_OFF) + x * 512;
+        const uint32_t t_x = tmem + x * SM::TILE_COLS + ((uint32_t)(quarter * 32) << 16), t_o = t_x + NB * NK;
         bool ok = true;
-        int J = 0, met = 0;  // chunks of all tiles; exchanges
-        // the other thread's value of the row
-        auto exchange = [&](float mine) {
-            float* p = xch + (met & 1) * 256;
-            p[half * 128 + row] = mine;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(pair(x, quarter));
-            ok = win_wait(pair(x, quarter), met & 1, a.status) && ok;
-            ++met;
-            return p[(half ^ 1) * 128 + row];
-        };
-        for (int i = 0; ok && tl.more(); ++i, tl.next()) {
+        int J = 0;  // chunk of all the tile's
+        for (; ok && tl.more(); tl.next()) {
             tl.open(a);
-            const int c = tl.c, g = tl.g, r0 = min(tl.r0 + x * rt, a.Lq - 1);  // of a pair's second tile that is not there: any
+            if (!tl.has(x)) continue;
+            const int c = tl.c, g = tl.g, r0 = tl.r0 + x * rt;
             const int first = a.n_mem + r0 + 1;                       // keys that the tile's first token sees
             const int keys = a.n_mem + min(a.Lq, r0 + rt);            // its last
             const int tok = tl.r0 + x * rt + row - hr * rt;
@@ -380,48 +396,43 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             float m_run = -FLT_MAX;  // the row's scale; that: no key counted so far
             uint64_t l2[2] = {0, 0};
             for (int j = 0; j < tl.n; ++j, ++J) {
-                const uint32_t t_s = t_x + (J & 1) * NK;
-                const int at = tl.at(j) + half * NE;
-                const int wd = tl.width(j) - half * NE;  // of the half's keys, if positive
-                ok = win_wait(sfull(x, J), (J >> 1) & 1, a.status);
+                const uint32_t t_s = t_x + J % NB * NK;
+                const int at = tl.at(j), wd = tl.width(j);
+                ok = win_wait(sfull(x, J), J / NB & 1, a.status);
                 if (!ok) break;
                 tc_fence_after();
                 // Hidden keys get scores of -inf, written back: few chunks have any, and the loop over all of them stays short (its
                 // instructions, unrolled with masks, did not fit the instruction caches)
-                if (at + NE > first || (at + NE > a.n_sink && at < keys - a.window)) {
+                if (at + NK > first || (at + NK > a.n_sink && at < keys - a.window)) {
 #pragma unroll 1
-                    for (int b = 0; b < NE && b < wd; b += 16) {
+                    for (int b = 0; b < NK && b < wd; b += 16) {
                         // sixteen of which some row does not see all (in the window of all: from the last token's first key on)
                         const int p = at + b;
                         if (p + 16 <= first && (p + 16 <= a.n_sink || p >= keys - a.window)) continue;
-                        const int nv = vis - p, nw = nv - a.window, ns = a.n_sink - p;
+                        const int nv = vis - p;
+                        const uint32_t sees = low_bits(nv) & (~low_bits(nv - a.window) | low_bits(a.n_sink - p));
                         float v[16];
                         uint32_t hid[16];
-                        tmem_ld16(t_s + half * NE + b, v);
+                        tmem_ld16(t_s + b, v);
 #pragma unroll
-                        for (int u = 0; u < 16; ++u) hid[u] = u < nv && (u >= nw || u < ns) ? __float_as_uint(v[u]) : 0xff800000u;
-                        tmem_st16(t_s + half * NE + b, hid);
+                        for (int u = 0; u < 16; ++u) hid[u] = sees >> u & 1 ? __float_as_uint(v[u]) : 0xff800000u;
+                        tmem_st16(t_s + b, hid);
                     }
                     tmem_wait_st();
                 }
-                if (j == 0 || __any_sync(0xffffffffu, m_run == -FLT_MAX)) {  // the same in both warps
+                if (__any_sync(0xffffffffu, m_run == -FLT_MAX)) {
                     float cm = -INFINITY;
 #pragma unroll 1
-                    for (int b = 0; b < NE && b < wd; b += 16) {
+                    for (int b = 0; b < NK && b < wd; b += 16) {
                         float v[16];
-                        tmem_ld16(t_s + half * NE + b, v);
+                        tmem_ld16(t_s + b, v);
 #pragma unroll
                         for (int u = 0; u < 16; u += 2) cm = max3(cm, v[u], v[u + 1]);
                     }
-                    cm = fmaxf(cm, exchange(cm));
-                    if (!ok) break;
-                    tc_fence_after();
                     if (m_run == -FLT_MAX) m_run = fmaxf(cm, -FLT_MAX);  // sums and O are 0 so far
-                } else if (flag[J & 1] == J - 2) {
-                    float l = sum_f32x4(l2);
-                    l += exchange(l);
-                    const bool in = win_wait(odone(x, J - 1), ((J - 1) >> 1) & 1, a.status);  // O up to the last chunk
-                    ok = ok && in;
+                } else if (__any_sync(0xffffffffu, sum_f32x4(l2) > 0x1p20f)) {
+                    const float l = sum_f32x4(l2);
+                    ok = win_wait(odone(x, J - 1), (J - 1) / NB & 1, a.status);  // O up to the last chunk
                     if (!ok) break;
                     tc_fence_after();
                     const int e = l > 0x1p20f && l <= FLT_MAX ? ilogbf(l) : 0;  // by a power of two
@@ -430,7 +441,7 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                     l2[0] = mul_f32x2(l2[0], pack_f32x2(corr, corr));
                     l2[1] = mul_f32x2(l2[1], pack_f32x2(corr, corr));
 #pragma unroll 1
-                    for (int cb = 0; cb < HD / 2; cb += 16) {
+                    for (int cb = 0; cb < HD; cb += 16) {
                         float ov[16];
                         uint32_t on[16];
                         tmem_ld16(t_o + cb, ov);
@@ -452,25 +463,23 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                             pk[u] = pack_bf16(e0, e1);
                             l2[u & 1] = add_f32x2(l2[u & 1], pack_f32x2(e0, e1));
                         }
-                        tmem_st8(t_s + half * NE + (b + h) / 2, pk);
+                        tmem_st8(t_s + (b + h) / 2, pk);
                     }
                 };
-                if (wd > 0) {
-                    if (wd > 16) {
+                if (wd == NK) {
+#pragma unroll
+                    for (int b = 0; b < NK; b += 32) {
                         float v[32];
-                        tmem_ld32(t_s + half * NE, v);
-                        probs(v, 0, 32);
-                    } else {
-                        float v[16];
-                        tmem_ld16(t_s + half * NE, v);
-                        probs(v, 0, 16);
+                        tmem_ld32(t_s + b, v);
+                        probs(v, b, 32);
                     }
-                    if (NE == 48 && wd > 32) {
+                } else {
+#pragma unroll 1
+                    for (int b = 0; b < wd; b += 16) {
                         float v[16];
-                        tmem_ld16(t_s + half * NE + 32, v);
-                        probs(v, 32, 16);
+                        tmem_ld16(t_s + b, v);
+                        probs(v, b, 16);
                     }
-                    if (__any_sync(0xffffffffu, sum_f32x4(l2) > 0x1p20f) && lane == 0) flag[J & 1] = J;
                 }
                 tmem_wait_st();
                 tc_fence_before();
@@ -478,17 +487,16 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 if (lane == 0) mbar_arrive(pready(x, J));
             }
             if (!ok) break;
-            float sum = sum_f32x4(l2);
-            sum += exchange(sum);
-            ok = win_wait(odone(x, J - 1), ((J - 1) >> 1) & 1, a.status) && ok;
+            const float sum = sum_f32x4(l2);
+            ok = win_wait(odone(x, J - 1), (J - 1) / NB & 1, a.status);
             if (!ok) break;
             tc_fence_after();
             const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no key that counts: 0
             const size_t at = (((size_t)c * a.n_q + g * a.group + (live ? hr : 0)) * a.Lq + (live ? tok : 0)) * HD;
-            bf16* orow = static_cast<bf16*>(a.out) + at + half * (HD / 2);
+            bf16* orow = static_cast<bf16*>(a.out) + at;
             float top = 0.f;  // of the row's magnitudes, NaN if one is
 #pragma unroll
-            for (int cb = 0; cb < HD / 2; cb += 32) {
+            for (int cb = 0; cb < HD; cb += 32) {
                 float v[32];
                 tmem_ld32(t_o + cb, v);
 #pragma unroll
@@ -511,10 +519,10 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             if (live && !(top <= FLT_MAX)) {
                 const long long kv_off = (long long)(c / a.L) * a.s0 + (long long)(c % a.L) * a.s1 + (long long)g * a.s2;
 #pragma unroll 1
-                for (int cb = 0; cb < HD / 2; cb += 32) {
+                for (int cb = 0; cb < HD; cb += 32) {
                     float w[32];
                     row_again<bf16, HD, 32, 1>(static_cast<const bf16*>(a.Q) + at, static_cast<const bf16*>(a.K) + kv_off,
-                                               static_cast<const bf16*>(a.V) + kv_off, a.s3, vis, a, half * (HD / 2) + cb, w);
+                                               static_cast<const bf16*>(a.V) + kv_off, a.s3, vis, a, cb, w);
                     for (int u = 0; u < 32; ++u) orow[cb + u] = __float2bfloat16_rn(w[u]);
                 }
             }
@@ -709,10 +717,10 @@ cudaError_t launch_cores(AttnArgs a, int C, cudaStream_t st) {
     return cudaGetLastError();
 }
 
-template <int HD, int TP>
+template <int HD>
 cudaError_t launch(AttnArgs a, int n_ctx, int C, int sms, cudaStream_t st) {
     static PerDevice<SmemOptIn> once;
-    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(window_prefill_kernel<HD, TP>), WinSmem<HD, TP>::DYN, once);
+    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(window_prefill_kernel<HD>), WinSmem<HD>::DYN, once);
     if (e != cudaSuccess) return e;
     // The maps of the last call's shape, of which a call only sets the addresses
     struct Plan {
@@ -730,7 +738,7 @@ cudaError_t launch(AttnArgs a, int n_ctx, int C, int sms, cudaStream_t st) {
         const uint64_t kd[5] = {HD, keys, a.s2 ? (uint64_t)a.n_kv : 1, a.s1 ? (uint64_t)a.L : 1, a.s0 ? (uint64_t)n_ctx : 1};
         const uint64_t s3 = a.s3 * 2;
         const uint64_t ks[4] = {s3, kd[2] > 1 ? a.s2 * 2 : s3, kd[3] > 1 ? a.s1 * 2 : s3, kd[4] > 1 ? a.s0 * 2 : s3};
-        const uint32_t kb[5] = {64, WinSmem<HD, TP>::NK, 1, 1, 1};
+        const uint32_t kb[5] = {64, WinSmem<HD>::NK, 1, 1, 1};
         plan.key[0] = 0;
         if (!encode_map_bf16_4d(&plan.q, a.Q, qd, qs, qb) || !encode_map_bf16_5d(&plan.kv, a.K, kd, ks, kb)) return cudaErrorNotSupported;
         std::copy(key, key + 10, plan.key);
@@ -738,9 +746,10 @@ cudaError_t launch(AttnArgs a, int n_ctx, int C, int sms, cudaStream_t st) {
     CUtensorMap mq = plan.q, mk = plan.kv, mv = plan.kv;
     if (!retarget_map(&mq, a.Q) || !retarget_map(&mk, a.K) || !retarget_map(&mv, a.V)) return cudaErrorInvalidValue;
     a.rows = rows;
-    const long long tiles = (long long)((a.Lq + TP * rows - 1) / (TP * rows)) * a.n_kv * C;
-    if (tiles >= 1ll << 30) return cudaErrorNotSupported;
-    window_prefill_kernel<HD, TP><<<(unsigned)std::min(tiles, (long long)WinSmem<HD, TP>::CTAS * sms), WinSmem<HD, TP>::THREADS, WinSmem<HD, TP>::DYN, st>>>(mq, mk, mv, a, C);
+    const long long nt = (a.Lq + rows - 1) / rows, pairs = (nt + 1) / 2 * a.n_kv * C, ctas = (long long)WinSmem<HD>::CTAS * sms;
+    if (pairs >= 1ll << 29) return cudaErrorNotSupported;
+    const long long grid = 2 * pairs <= ctas ? 2 * pairs : std::min(pairs, ctas);  // single tiles if there is a CTA for each
+    window_prefill_kernel<HD><<<(unsigned)grid, WinSmem<HD>::THREADS, WinSmem<HD>::DYN, st>>>(mq, mk, mv, a, C);
     return cudaGetLastError();
 }
 
@@ -752,10 +761,7 @@ cudaError_t launch_window_cores(AttnArgs a, int dtype, int hd, int C, cudaStream
 }
 
 cudaError_t launch_window_prefill(const AttnArgs& a, int hd, int n_ctx, int C, int sms, cudaStream_t st) {
-    if (hd == 64) return launch<64, 1>(a, n_ctx, C, sms, st);
-    // pairs of tiles, unless there is an SM for every tile
-    const long long tiles = (long long)((a.Lq + 128 / a.group - 1) / (128 / a.group)) * a.n_kv * C;
-    return tiles <= sms ? launch<128, 1>(a, n_ctx, C, sms, st) : launch<128, 2>(a, n_ctx, C, sms, st);
+    return hd == 64 ? launch<64>(a, n_ctx, C, sms, st) : launch<128>(a, n_ctx, C, sms, st);
 }
 
 }  // namespace mone
