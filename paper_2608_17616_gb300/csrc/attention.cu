@@ -589,6 +589,12 @@ __global__ void __launch_bounds__(DE_WARPS * 32, HD == 64 ? 4 : 3) attention_dec
     const long long kv_off = (long long)(c / a.L) * a.s0 + (long long)(c % a.L) * a.s1 + (long long)g * a.s2;
     const bf16* Kc = static_cast<const bf16*>(a.K) + kv_off + 8 * t;
     const bf16* Vc = static_cast<const bf16*>(a.V) + kv_off + 8 * gq;
+    // the windowed form starts ahead of the end of the kernel before it
+    auto load = [](const bf16* p) { return WIN ? *reinterpret_cast<const uint4*>(p) : __ldg(reinterpret_cast<const uint4*>(p)); };
+    if constexpr (WIN) {
+        pdl_wait();
+        pdl_trigger();
+    }
     // rows gq and gq + 8 of the tile
     uint32_t qa[HD / 16][4];
     int vis[2];
@@ -625,8 +631,7 @@ __global__ void __launch_bounds__(DE_WARPS * 32, HD == 64 ? 4 : 3) attention_dec
             const int key = j0 + 8 * nt + gq;
 #pragma unroll
             for (int p = 0; p < NP; ++p)
-                kr[nt][p] = seen(key) ? __ldg(reinterpret_cast<const uint4*>(Kc + (long long)key * a.s3 + 32 * p))
-                                       : make_uint4(0, 0, 0, 0);
+                kr[nt][p] = seen(key) ? load(Kc + (long long)key * a.s3 + 32 * p) : make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
         for (int kk = 0; kk < KB / 16; ++kk)
@@ -635,8 +640,7 @@ __global__ void __launch_bounds__(DE_WARPS * 32, HD == 64 ? 4 : 3) attention_dec
                 const int key = j0 + 16 * kk + 2 * t + (u & 1) + 8 * (u >> 1);
 #pragma unroll
                 for (int p = 0; p < NV; ++p)
-                    vr[kk][u][p] = seen(key) ? __ldg(reinterpret_cast<const uint4*>(Vc + (long long)key * a.s3 + 64 * p))
-                                             : make_uint4(0, 0, 0, 0);
+                    vr[kk][u][p] = seen(key) ? load(Vc + (long long)key * a.s3 + 64 * p) : make_uint4(0, 0, 0, 0);
             }
         float s[KB / 8][4];
         float cm[2] = {-INFINITY, -INFINITY};
@@ -847,17 +851,19 @@ cudaError_t launch_decode(AttnArgs a, int C, int sms, cudaStream_t st) {
     const int slots = (HD == 64 ? 4 : 3) * sms;
     const int splits = (int)std::max(1ll, std::min({8ll, slots / ctas, (long long)blocks / DE_WARPS}));
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = splits;
     at[0].val.clusterDim.y = 1;
     at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3(splits * row_tiles, a.n_kv, C);
     cfg.blockDim = dim3(DE_WARPS * 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = WIN ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, attention_decode_kernel<HD, WIN>, a, splits);
 }
 
@@ -878,8 +884,9 @@ cudaError_t launch(const DevState& s, AttnArgs a, int n_ctx, cudaStream_t st) {
         const long long row_tiles = ((long long)a.group * a.Lq + DE_ROWS - 1) / DE_ROWS;
         bool few = row_tiles == 1 || row_tiles * a.n_kv * C <= DE_MAX_TILES;
         // The windowed prefill form splits no keys either, but starts in less time than the decode form of hd 128 (1 chain x 8
-        // heads x 4: 64 + 64 tokens, 6.8 us there and 10.1 here; 1 + 1000 at a window of 512, 9.1 and 9.8; 1 token of 16 chains, 9.6 and
-        // 13.7; but 4 + 1000 at 1024, 12.6 and 9.5; 16 + 4000 at 4096, 36.0 and 22.2).  At hd 64 the rule above holds for both.
+        // heads x 4: 64 + 64 tokens, 5.5 us there and 9.1 here; 1 + 1000 at a window of 512, 7.8 and 8.8; 1 token of 16 chains, 8.7 and
+        // 14.3; but 4 + 1000 at 1024, 11.2 and 8.6; 16 + 4000 at 4096, 33.0 and 25.6).  At hd 64 the rule above holds for both (1 + 1000
+        // at 512, 10.2 and 6.7; 64 + 1000 at 1064, 16.9 and 13.5; 64 + 64, 5.4 and 5.5).
         if (WIN && s.hd == 128)
             few = row_tiles * a.n_kv * C <= DE_MAX_TILES / 2 && std::min((long long)a.n_mem + a.Lq, (long long)a.n_sink + a.window + a.Lq) >= 800;
         if (few)

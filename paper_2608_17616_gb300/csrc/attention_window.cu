@@ -235,6 +235,8 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    pdl_wait();
+    pdl_trigger();
     const uint32_t tmem = __shfl_sync(0xffffffffu, *slot, 0);  // of a tile: the S (and P) buffers, then O
     const int rt = a.rows;
     WinTiles<NK> tl(a, C);
@@ -749,8 +751,7 @@ cudaError_t launch(AttnArgs a, int n_ctx, int C, int sms, cudaStream_t st) {
     const long long nt = (a.Lq + rows - 1) / rows, pairs = (nt + 1) / 2 * a.n_kv * C, ctas = (long long)WinSmem<HD>::CTAS * sms;
     if (pairs >= 1ll << 29) return cudaErrorNotSupported;
     const long long grid = 2 * pairs <= ctas ? 2 * pairs : std::min(pairs, ctas);  // single tiles if there is a CTA for each
-    window_prefill_kernel<HD><<<(unsigned)grid, WinSmem<HD>::THREADS, WinSmem<HD>::DYN, st>>>(mq, mk, mv, a, C);
-    return cudaGetLastError();
+    return launch_kernel(window_prefill_kernel<HD>, dim3((unsigned)grid), dim3(WinSmem<HD>::THREADS), WinSmem<HD>::DYN, st, true, 1, mq, mk, mv, a, C);
 }
 
 }  // namespace

@@ -27,8 +27,10 @@ struct AppendArgs {
 template <typename U>
 __global__ void __launch_bounds__(CP_THREADS) cache_append_kernel(const AppendArgs a) {
     const int chain = blockIdx.z, g = blockIdx.y, c = chain / a.v.L, l = chain % a.v.L;
+    pdl_wait();
+    pdl_trigger();
     const int len = cache_len(a.v, c);
-    const int n = a.counts ? min(max(__ldg(a.counts + c), 0), a.n_tok) : a.n_tok;
+    const int n = a.counts ? min(max(a.counts[c], 0), a.n_tok) : a.n_tok;
     if (a.lens_out && blockIdx.x == 0 && g == 0 && l == 0 && threadIdx.x == 0)
         a.lens_out[c] = (int)min((long long)len + n, a.v.cap);
     const long long e = (long long)blockIdx.x * CP_THREADS + threadIdx.x;
@@ -60,8 +62,7 @@ void in_units(CacheView& v, int per) {
 template <typename U>
 cudaError_t append(AppendArgs a, cudaStream_t st) {
     const dim3 grid((unsigned)(((long long)a.n_tok * a.units + CP_THREADS - 1) / CP_THREADS), a.v.n_kv, a.v.n_ctx * a.v.L);
-    cache_append_kernel<U><<<grid, CP_THREADS, 0, st>>>(a);
-    return cudaGetLastError();
+    return launch_kernel(cache_append_kernel<U>, grid, dim3(CP_THREADS), 0, st, true, 1, a);
 }
 
 // ---------------------------------------------------------------- eviction: which positions stay
@@ -108,6 +109,7 @@ __global__ void __launch_bounds__(SEL_THREADS) cache_select_kernel(const EvictAr
     __shared__ int found[2];
     const int chain = blockIdx.z, g = blockIdx.y, c = chain / a.v.L, l = chain % a.v.L, rank = (int)cluster_ctarank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    pdl_wait();
     pdl_trigger();
     const int N = cache_len(a.v, c);
     int* kept = a.kept + ((size_t)chain * a.v.n_kv + g) * a.keep;
@@ -295,9 +297,8 @@ cudaError_t launch_cache_evict(const DevState& s, const CacheView& v, int keep, 
     constexpr size_t smem = SEL_KEYS * sizeof(uint32_t);
     cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(cache_select_kernel), smem, once);
     if (e != cudaSuccess) return e;
-    // (no programmatic launch of its own: what it reads may come from the kernel ahead)
     e = launch_kernel(cache_select_kernel, dim3(slices, v.n_kv, v.n_ctx * v.L), dim3(SEL_THREADS),
-                      std::min<size_t>(smem, (v.cap + slices - 1) / slices * sizeof(uint32_t)), st, false, slices, a, slices);
+                      std::min<size_t>(smem, (v.cap + slices - 1) / slices * sizeof(uint32_t)), st, true, slices, a, slices);
     if (e != cudaSuccess) return e;
     if (!cache_vec(v, el)) return s.dtype == 0 ? compact<uint32_t>(a, st) : compact<uint16_t>(a, st);
     in_units(a.v, 16 / el);

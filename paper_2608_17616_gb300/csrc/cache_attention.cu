@@ -249,12 +249,13 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
     extern __shared__ uint8_t ca_raw[];
     __shared__ CaNote notes[2 * CA_WARPS];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ca_raw) + 1023) & ~uintptr_t(1023));
-    pdl_trigger();  // the second kernel waits for the end of this one
     const int warp = threadIdx.x >> 5;
     if ((threadIdx.x & 31) < 2) notes[2 * warp + (threadIdx.x & 31)].part = nullptr;
     __syncwarp();
     {
         Form form(tmK, tmV, smem + warp * Form::WARP_BYTES, a.RT);
+        pdl_wait();
+        pdl_trigger();  // the second kernel waits for the end of this one
         form.run(a, notes + 2 * warp);
     }
     __syncthreads();
@@ -337,7 +338,7 @@ struct CaCores {
 #pragma unroll
                 for (int e = 0; e < VE; ++e) f[p * VE + e] = 0.f;
             } else if (vec) {
-                const uint4 x = __ldg(reinterpret_cast<const uint4*>(s));
+                const uint4 x = *reinterpret_cast<const uint4*>(s);
                 const T* t = reinterpret_cast<const T*>(&x);
 #pragma unroll
                 for (int e = 0; e < VE; ++e) f[p * VE + e] = to_f<T>(t[e]);
@@ -587,7 +588,7 @@ struct CaTensor {
             f.batch = f.i;
             const int copies_log2 = (SK == 32 ? 5 : 4) - f.box_log2, i = f.i + (lane >> copies_log2);
             const int j = i < f.n ? key0(f.w, i) + ((lane & (f.copies - 1)) << f.box_log2) : INT_MAX;
-            f.page = j < f.w.r.n ? __ldg(a.v.table + (size_t)f.w.c * a.v.width + (j >> a.v.page_log2)) : 0;
+            f.page = j < f.w.r.n ? a.v.table[(size_t)f.w.c * a.v.width + (j >> a.v.page_log2)] : 0;
         }
         const int j0 = key0(f.w, f.i), box = 1 << f.box_log2, live = min(f.copies, (f.w.r.n - j0 + box - 1) >> f.box_log2);
         int page = __shfl_sync(0xffffffffu, f.page, (f.i - f.batch) * f.copies + lane);
@@ -641,8 +642,8 @@ struct CaTensor {
                     reinterpret_cast<const uint32_t*>(static_cast<const bf16*>(a.Q) + (kv * a.R + row0 + (live ? 8 * i + gq : 0)) * HD) + t;
 #pragma unroll
                 for (int k = 0; k < HD / 16; ++k) {
-                    x.q[i][k][0] = live ? __ldg(q + 8 * k) : 0;
-                    x.q[i][k][1] = live ? __ldg(q + 8 * k + 4) : 0;
+                    x.q[i][k][0] = live ? q[8 * k] : 0;
+                    x.q[i][k][1] = live ? q[8 * k + 4] : 0;
                     x.o[i][k][0] = x.o[i][k][1] = x.o[i][k][2] = x.o[i][k][3] = 0.f;
                 }
 #pragma unroll
@@ -865,7 +866,7 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) cache_finish_kernel(const CaAr
     const CaRange r(a, c);
     const int tile0 = ((int)blockIdx.x - a.R) * FIN_POS, p0 = tile0 + 4 * threadIdx.x;
     if (tile0 >= r.n || (tile0 >= a.n_sink && tile0 + FIN_POS <= r.t0 - a.window + 1)) return;  // nobody sees them
-    pdl_wait();  // what is above reads only what the call was given
+    pdl_wait();  // above, only the lengths are read, which were there before the first kernel triggered
     if ((int)blockIdx.x < a.R) {
         const int row = blockIdx.x, info = a.info[kv * a.RT + row / ROWS], first = info & 0xffff, n = info >> 16;
         if (n == 1) return;
@@ -936,8 +937,8 @@ cudaError_t launch(CaArgs a, const CUtensorMap& tmK, const CUtensorMap& tmV, int
     a.RT = (a.R + Form::ROWS - 1) / Form::ROWS;
     a.per = a.v.L * a.v.n_kv * a.RT;
     a.ctas = Form::CTAS * sms;
-    cache_attention_kernel<Form><<<a.ctas, CA_THREADS, smem, st>>>(tmK, tmV, a);
-    if ((e = cudaGetLastError()) != cudaSuccess || !has_finish(a.v)) return e;
+    e = launch_kernel(cache_attention_kernel<Form>, dim3(a.ctas), dim3(CA_THREADS), smem, st, true, 1, tmK, tmV, a);
+    if (e != cudaSuccess || !has_finish(a.v)) return e;
     const dim3 grid((unsigned)(a.R + (a.v.score ? (a.v.cap + FIN_POS - 1) / FIN_POS : 0)), a.v.n_kv, a.v.n_ctx * a.v.L);
     return launch_kernel(cache_finish_kernel<Form>, grid, dim3(FIN_THREADS), 0, st, true, 1, a);
 }

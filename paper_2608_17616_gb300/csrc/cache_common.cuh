@@ -13,7 +13,7 @@ __device__ __forceinline__ void cache_fail(int* status, int site) {
 
 // Positions that context c holds; a length that its table cannot cover counts as what it covers.
 __device__ __forceinline__ int cache_len(const CacheView& v, int c) {
-    const int n = __ldg(v.lens + c);
+    const int n = v.lens[c];
     if (n < 0 || n > v.cap) {
         cache_fail(v.status, DS_CACHE_LEN);
         return n < 0 ? 0 : (int)v.cap;
@@ -23,7 +23,7 @@ __device__ __forceinline__ int cache_len(const CacheView& v, int c) {
 
 // Page of a table entry, -1 (and an error latched) where it is outside the pool.
 __device__ __forceinline__ int cache_page(const CacheView& v, const int* table, int block) {
-    const int p = __ldg(table + block);
+    const int p = table[block];
     if ((unsigned)p < (unsigned)v.n_pages) return p;
     cache_fail(v.status, DS_CACHE_PAGE);
     return -1;
