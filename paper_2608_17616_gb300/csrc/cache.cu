@@ -70,6 +70,9 @@ constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32, SEL_BINS = 2048;
 constexpr int SEL_KEYS = 16384;  // keys that a CTA keeps on chip; of a longer slice it reads the others' scores again in each pass
 constexpr int SEL_SLICE = 2048;  // positions of a CTA's slice at least, where a row is split
 
+// Positions of a CTA's slice, in fours
+__host__ __device__ inline int sel_slice(long long n, int slices) { return (int)(((n + slices - 1) / slices + 3) & ~3ll); }
+
 struct EvictArgs {
     CacheView v;
     int keep, n_sink, n_recent, units;
@@ -87,26 +90,52 @@ __device__ __forceinline__ uint32_t score_key(float f) {
     const uint32_t u = __float_as_uint(f);
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
-constexpr uint32_t KEY_STAYS = 0xffffffffu;  // of the first and the last positions: above every score's (+inf: 0xff800000)
+constexpr uint32_t KEY_STAYS = 0xffffffffu;  // of the first and the last positions: above every score's (+inf: 0xff800000; none is 0)
 
-// int of CTA `rank` of the cluster at the place of `p` in this one
-__device__ __forceinline__ int ld_cluster(const int* p, uint32_t rank) {
-    int v;
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(map_to_cta(smem_u32(p), rank)) : "memory");
+__device__ __forceinline__ int2 ld_cluster(const int* p, uint32_t rank) {
+    int2 v;
+    asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(map_to_cta(smem_u32(p), rank)) : "memory");
     return v;
 }
+// The sums of p[0] and p[1] over the cluster's CTAs, each of which has them at the same place
+template <int SLICES>
+__device__ __forceinline__ int2 cluster_total(const int* p, int rank) {
+    int2 sum = *reinterpret_cast<const int2*>(p), v[SLICES];
+#pragma unroll
+    for (int r = 1; r < SLICES; ++r) v[r] = ld_cluster(p, (rank + r) & (SLICES - 1));  // all under way at once
+#pragma unroll
+    for (int r = 1; r < SLICES; ++r) {
+        sum.x += v[r].x;
+        sum.y += v[r].y;
+    }
+    return sum;
+}
+// Sum of x over the lanes up to this one
+__device__ __forceinline__ int scan_up(int x) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += up;
+    }
+    return x;
+}
 
-// A cluster takes a (chain, head), each CTA a slice of its positions, whose keys stay in shared memory.  The least key that
-// stays is found by its digits, highest first (11, 11 and 10 bits): histograms of the candidates that share the digits so
-// far, added up over the cluster, and the bin in which the wanted rank falls.  Then the positions above it, and of those equal
-// to it the lowest, are written in order: each warp has a contiguous part of the slice, whose place in the list follows from
-// the counts of the parts before it.  What bounds it is the chain of passes, each a shared-memory histogram, a cluster barrier and a scan:
-// 64 rows of up to 32K take 13 us (one CTA a row, scores read again in each pass: 37).
-__global__ void __launch_bounds__(SEL_THREADS) cache_select_kernel(const EvictArgs a, int slices) {
-    extern __shared__ uint32_t keys[];
-    __shared__ int hist[2][SEL_BINS];
-    __shared__ int part[2][SEL_WARPS], total[2];
-    __shared__ int found[2];
+// A cluster takes a (chain, head), each CTA a slice of its positions, whose keys stay in shared memory, and of which a thread takes four
+// neighbours at a time.  The least key that stays is found by its digits, highest first (11, 11 and 10 bits): histograms of the
+// candidates that share the digits so far, and the bin in which the wanted rank falls: a warp looks for it among the sums of 32 bins
+// each, then within one such group, both added up over the cluster.  Then the positions above the least key, and of those equal to it the lowest, are
+// written in order: each warp has a contiguous part of the slice, whose place in the list follows from the counts of
+// the parts before it.  What bounds it is the chain of these steps,
+// the loads of the scores among them: 64 rows of 32K take 13.5 us on four CTAs each, 128 rows of 2K 8 us on one.  (With the bins'
+// counts added up by all threads, 32 positions a warp at a time and the list written from there, 20 and 8.6.)
+template <int SLICES>
+__global__ void __launch_bounds__(SEL_THREADS, 2) cache_select_kernel(const EvictArgs a) {
+    extern __shared__ __align__(16) uint32_t keys[];
+    __shared__ __align__(8) int hist[2][SEL_BINS], group[2][SEL_BINS / 32];
+    __shared__ int part[2][SEL_WARPS];
+    __shared__ __align__(8) int total[2];
+    __shared__ int found[3];
     const int chain = blockIdx.z, g = blockIdx.y, c = chain / a.v.L, l = chain % a.v.L, rank = (int)cluster_ctarank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_wait();
@@ -115,71 +144,90 @@ __global__ void __launch_bounds__(SEL_THREADS) cache_select_kernel(const EvictAr
     int* kept = a.kept + ((size_t)chain * a.v.n_kv + g) * a.keep;
     if (a.lens_out && g == 0 && l == 0 && rank == 0 && tid == 0) a.lens_out[c] = min(N, a.keep);
     if (N <= a.keep) {  // the whole cluster
-        for (int i = rank * SEL_THREADS + tid; i < a.keep; i += slices * SEL_THREADS) kept[i] = i < N ? i : -1;
+        for (int i = rank * SEL_THREADS + tid; i < a.keep; i += SLICES * SEL_THREADS) kept[i] = i < N ? i : -1;
         return;
     }
     const float* score = a.v.score + (((size_t)c * a.v.Lh + l) * a.v.n_kv + g) * a.v.cap;
     const int lo = a.n_sink, hi = N - a.n_recent;  // candidates
-    const int per = (N + slices - 1) / slices, s0 = min(N, rank * per), n = min(N, s0 + per) - s0;
-    auto make = [&](int i) { return s0 + i < lo || s0 + i >= hi ? KEY_STAYS : score_key(score[s0 + i]); };
-    for (int i = tid; i < min(n, SEL_KEYS); i += SEL_THREADS) keys[i] = make(i);
-    auto key = [&](int i) { return i < SEL_KEYS ? keys[i] : make(i); };
-    for (int i = tid; i < SEL_BINS; i += SEL_THREADS) hist[0][i] = 0;
-    __syncthreads();
-    int need = a.keep - a.n_sink - a.n_recent;  // of the candidates to keep, then of those equal to the least
-    uint32_t prefix = need ? 0 : KEY_STAYS - 1;
-    int shift = 32, pass = 0;
-    while (need > 0 && shift > 0) {
-        const int bits = shift > 10 ? 11 : 10, low = shift - bits;
-        int* h = hist[pass & 1];
-        for (int i = tid; i < n; i += SEL_THREADS) {
-            const uint32_t k = key(i);
-            if (k != KEY_STAYS && (shift == 32 || (k >> shift) == prefix)) atomicAdd(&h[(k >> low) & ((1u << bits) - 1)], 1);
-        }
-        if (slices > 1)
+    const int per = sel_slice(N, SLICES), s0 = min(N, rank * per), n = min(N, s0 + per) - s0;
+    auto key = [&](int i, float x) { return i >= n ? 0u : s0 + i < lo || s0 + i >= hi ? KEY_STAYS : score_key(x); };
+    auto make = [&](int i) { return key(i, i < n ? score[s0 + i] : 0.f); };
+    auto sync = [&]() {
+        if constexpr (SLICES > 1)
             cluster_sync();
         else
             __syncthreads();
-        for (int i = tid; i < SEL_BINS; i += SEL_THREADS) hist[(pass & 1) ^ 1][i] = 0;  // read by all before the barrier above
-        // candidates in the bins from a thread's pair up, counted from the top
-        const int b1 = SEL_BINS - 1 - 2 * tid;
-        int h1 = h[b1], h0 = h[b1 - 1];
-        for (int r = 1; r < slices; ++r) {
-            const int other = rank + r < slices ? rank + r : rank + r - slices;
-            h1 += ld_cluster(h + b1, other);
-            h0 += ld_cluster(h + b1 - 1, other);
-        }
-        int sum = h1 + h0;
+    };
+    for (int i0 = tid; i0 < min((n + 3) & ~3, SEL_KEYS); i0 += 4 * SEL_THREADS) {
+        float x[4];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int up = __shfl_up_sync(0xffffffffu, sum, o);
-            if (lane >= o) sum += up;
+        for (int u = 0; u < 4; ++u) x[u] = i0 + u * SEL_THREADS < n ? score[s0 + i0 + u * SEL_THREADS] : 0.f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (const int i = i0 + u * SEL_THREADS; i < min((n + 3) & ~3, SEL_KEYS)) keys[i] = key(i, x[u]);
+    }
+    auto four = [&](int i) { return i < SEL_KEYS ? *reinterpret_cast<const uint4*>(keys + i) : make_uint4(make(i), make(i + 1), make(i + 2), make(i + 3)); };
+    for (int i = tid; i < SEL_BINS; i += SEL_THREADS) hist[0][i] = 0;
+    __syncthreads();
+    int need = a.keep - a.n_sink - a.n_recent;  // of the candidates to keep, then of those equal to the least
+    uint32_t least = need ? 0 : KEY_STAYS - 1;  // its digits so far
+    int shift = 32;
+    for (int pass = 0; need > 0 && shift > 0; ++pass) {
+        const int bits = shift > 10 ? 11 : 10, low = shift - bits;
+        int *h = hist[pass & 1], *gs = group[pass & 1];
+        for (int i = 4 * tid; i < n; i += 4 * SEL_THREADS) {
+            const uint4 k4 = four(i);
+            const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (k[u] - 1u < KEY_STAYS - 1u && (shift == 32 || (k[u] >> shift) == least)) atomicAdd(&h[(k[u] >> low) & ((1u << bits) - 1)], 1);
         }
-        if (lane == 31) part[0][warp] = sum;
         __syncthreads();
-        const int mine = part[0][lane];
-        const int above = __reduce_add_sync(0xffffffffu, lane < warp ? mine : 0) + sum - h1 - h0;  // in the bins over the pair
-        if (above < need && need <= above + h1) {
-            found[0] = b1;
-            found[1] = need - above;
-        } else if (above + h1 < need && need <= above + h1 + h0) {
-            found[0] = b1 - 1;
-            found[1] = need - above - h1;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int sum = __reduce_add_sync(0xffffffffu, h[64 * warp + 32 * b + lane]);
+            if (lane == 0) gs[2 * warp + b] = sum;
+        }
+        sync();
+        for (int i = tid; i < SEL_BINS; i += SEL_THREADS) hist[(pass & 1) ^ 1][i] = 0;  // read by all before the barrier above
+        if (warp == 0) {  // from the top down: which group, then which bin, a lane has two of the former, half the lanes two of the latter
+            int b = 0, above = 0, count = 0;
+            auto look = [&](const int* at, int n_at) {
+                const int2 v = 2 * lane < n_at ? cluster_total<SLICES>(at + n_at - 2 - 2 * lane, rank) : make_int2(0, 0);
+                const int upto = above + scan_up(v.x + v.y);
+                const int k = __ffs(__ballot_sync(0xffffffffu, upto >= need)) - 1;
+                const bool lower = __shfl_sync(0xffffffffu, upto - v.x < need, k);  // in the second of the lane's two
+                count = __shfl_sync(0xffffffffu, lower ? v.x : v.y, k);
+                above = __shfl_sync(0xffffffffu, lower ? upto - v.x : upto - v.x - v.y, k);
+                return n_at - 1 - 2 * k - lower;
+            };
+            b = look(gs, SEL_BINS / 32);
+            b = 32 * b + look(h + 32 * b, 32);
+            if (lane == 0) {
+                found[0] = b;
+                found[1] = need - above;
+                found[2] = count;
+            }
         }
         __syncthreads();
-        prefix = (prefix << bits) | (uint32_t)found[0];
+        least = (least << bits) | (uint32_t)found[0];
         need = found[1];
         shift = low;
-        ++pass;
+        if (need == found[2] && low) {  // the whole bin stays: all above the key below it
+            least = (least << low) - 1;
+            need = 0;
+        }
     }
-    const int wper = (n + SEL_THREADS - 1) / SEL_THREADS * 32;  // positions of a warp's part
+    const int wper = (n + 4 * SEL_THREADS - 1) / (4 * SEL_THREADS) * 128;  // positions of a warp's part
     const int w0 = warp * wper, w1 = min(n, w0 + wper);
     int over = 0, equal = 0;
-    for (int i = w0 + lane; i - lane < w1; i += 32) {
-        const uint32_t k = i < w1 ? key(i) : 0;
-        over += __popc(__ballot_sync(0xffffffffu, i < w1 && k > prefix));
-        equal += __popc(__ballot_sync(0xffffffffu, i < w1 && k == prefix));
+    for (int i = w0 + 4 * lane; i < w1; i += 128) {
+        const uint4 k = four(i);
+        over += (k.x > least) + (k.y > least) + (k.z > least) + (k.w > least);
+        equal += (k.x == least) + (k.y == least) + (k.z == least) + (k.w == least);
     }
+    over = __reduce_add_sync(0xffffffffu, over);
+    equal = __reduce_add_sync(0xffffffffu, equal);
     if (lane == 0) {
         part[0][warp] = over;
         part[1][warp] = equal;
@@ -189,33 +237,80 @@ __global__ void __launch_bounds__(SEL_THREADS) cache_select_kernel(const EvictAr
         const int sum = __reduce_add_sync(0xffffffffu, part[warp][lane]);
         if (lane == 0) total[warp] = sum;
     }
-    if (slices > 1)
-        cluster_sync();
-    else
-        __syncthreads();
     over = __reduce_add_sync(0xffffffffu, lane < warp ? part[0][lane] : 0);
     equal = __reduce_add_sync(0xffffffffu, lane < warp ? part[1][lane] : 0);
-    if (slices > 1) {
-        over += __reduce_add_sync(0xffffffffu, lane < rank ? ld_cluster(total, lane) : 0);
-        equal += __reduce_add_sync(0xffffffffu, lane < rank ? ld_cluster(total + 1, lane) : 0);
-        cluster_sync();  // no CTA leaves while another reads its shared memory
+    if constexpr (SLICES > 1) {
+        cluster_sync();
+        const int2 v = lane < rank ? ld_cluster(total, lane) : make_int2(0, 0);
+        over += __reduce_add_sync(0xffffffffu, v.x);
+        equal += __reduce_add_sync(0xffffffffu, v.y);
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     }
-    for (int i = w0 + lane; i - lane < w1; i += 32) {
-        const uint32_t k = i < w1 ? key(i) : 0;
-        const bool up = i < w1 && k > prefix, eq = i < w1 && k == prefix;
-        const uint32_t ups = __ballot_sync(0xffffffffu, up), eqs = __ballot_sync(0xffffffffu, eq), below = (1u << lane) - 1;
-        const int e = equal + __popc(eqs & below), at = over + __popc(ups & below) + min(e, need);
-        if ((up || (eq && e < need)) && at < a.keep) kept[at] = s0 + i;
-        over += __popc(ups);
-        equal += __popc(eqs);
+    // The positions of a part that stay are neighbours in the list: they go where their keys were, then out
+    const int first = over + min(equal, need);
+    int n_out = 0;
+    for (int i = w0 + 4 * lane; i - 4 * lane < w1; i += 128) {
+        const uint4 k4 = i < w1 ? four(i) : make_uint4(0, 0, 0, 0);
+        const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
+        const bool some = need && __any_sync(0xffffffffu, k[0] == least || k[1] == least || k[2] == least || k[3] == least);
+        if (w1 <= SEL_KEYS && !some) {  // most of the time
+            const int mine = (k[0] > least) + (k[1] > least) + (k[2] > least) + (k[3] > least), upto = scan_up(mine);
+            uint32_t* to = keys + w0 + n_out + upto - mine;
+            __syncwarp();
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (k[u] > least) *to++ = s0 + i + u;
+            const int all = __shfl_sync(0xffffffffu, upto, 31);
+            over += all;
+            n_out += all;
+        } else {
+            int mine = 0;  // above, and equal << 16
+#pragma unroll
+            for (int u = 0; u < 4; ++u) mine += (k[u] > least) + ((k[u] == least) << 16);
+            const int upto = scan_up(mine), ahead = upto - mine, all = __shfl_sync(0xffffffffu, upto, 31);
+            int o = over + (ahead & 0xffff), e = equal + (ahead >> 16);
+#pragma unroll 1
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t ku = u == 0 ? k[0] : u == 1 ? k[1] : u == 2 ? k[2] : k[3];
+                const bool up = ku > least, eq = ku == least;
+                const int at = o + min(e, need);
+                if (up || (eq && e < need)) {
+                    if (w1 <= SEL_KEYS)
+                        keys[w0 + at - first] = s0 + i + u;
+                    else if (at < a.keep)
+                        kept[at] = s0 + i + u;
+                }
+                o += up;
+                e += eq;
+            }
+            over += all & 0xffff;
+            equal += all >> 16;
+            if (w1 <= SEL_KEYS) n_out = over + min(equal, need) - first;
+        }
+        __syncwarp();
     }
+    for (int i = lane; i < n_out; i += 32)
+        if (first + i < a.keep) kept[first + i] = keys[w0 + i];
+    if constexpr (SLICES > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // no CTA leaves while another reads its shared memory
+}
+
+template <int SLICES>
+cudaError_t select(const EvictArgs& a, cudaStream_t st) {
+    static PerDevice<SmemOptIn> once;
+    constexpr size_t smem = SEL_KEYS * sizeof(uint32_t);
+    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(cache_select_kernel<SLICES>), smem, once);
+    if (e != cudaSuccess) return e;
+    return launch_kernel(cache_select_kernel<SLICES>, dim3(SLICES, a.v.n_kv, a.v.n_ctx * a.v.L), dim3(SEL_THREADS),
+                         std::min<size_t>(smem, sel_slice(a.v.cap, SLICES) * sizeof(uint32_t)), st, true, SLICES, a);
 }
 
 // ---------------------------------------------------------------- eviction: their rows
 constexpr int CM_SLOTS = 8, CM_WAY = 2;
 
 // A warp takes CM_SLOTS survivors: a lane looks up where one comes from and goes to, then all move units of their key and value
-// rows, CM_WAY under way in each lane.
+// rows, CM_WAY under way in each lane.  Bound by HBM, whose reads come row by row: 64 x 8192 rows of 2 x 256 bytes take 65 us, 8.2 TB/s
+// read and written (part of it in L2), 128 x 1024 of 2 x 128 bytes 13.  (With the select: 8 slots, 2 under way 14.5 and 88.7
+// us; 4 under way 16.1 and 99.6; 8 under way 19.6 and 121: fewer loads a warp and more warps.)
 template <typename U>
 __global__ void __launch_bounds__(CP_THREADS) cache_compact_kernel(const EvictArgs a) {
     const int chain = blockIdx.z, g = blockIdx.y, c = chain / a.v.L, l = chain % a.v.L, lane = threadIdx.x & 31;
@@ -288,17 +383,13 @@ cudaError_t launch_cache_evict(const DevState& s, const CacheView& v, int keep, 
                                float* to_score, int* kept, int* lens_out, cudaStream_t st) {
     const int el = s.dtype == 0 ? 4 : 2;
     EvictArgs a{v, keep, n_sink, n_recent, s.hd, to, to_width, (long long)to_width << v.page_log2, to_score, kept, lens_out};
-    // A row over as many CTAs of a cluster as the SMs hold, two each, and slices of SEL_SLICE positions.  (8 rows of 2K take 8.5 us
-    // with their compaction on one CTA each, 11.0 on two; 64 rows of up to 32K 88.7 on two, 85.4 on four, 126 on eight.)
+    // A row over as many CTAs of a cluster as the SMs hold, two each, and slices of SEL_SLICE positions.  (128 rows of 2K take
+    // 14.1 us with their compaction on one CTA each, 17.8 on two; 64 rows of 32K 99, 84, 80 and 82 on one, two, four and eight; 8
+    // rows of 120000 202 on one and 98 on eight.)
     const long long rows = (long long)v.n_ctx * v.L * v.n_kv;
     int slices = 1;
     while (slices < 8 && 2 * slices * rows <= 2 * s.sms && v.cap / (2 * slices) >= SEL_SLICE) slices *= 2;
-    static PerDevice<SmemOptIn> once;
-    constexpr size_t smem = SEL_KEYS * sizeof(uint32_t);
-    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(cache_select_kernel), smem, once);
-    if (e != cudaSuccess) return e;
-    e = launch_kernel(cache_select_kernel, dim3(slices, v.n_kv, v.n_ctx * v.L), dim3(SEL_THREADS),
-                      std::min<size_t>(smem, (v.cap + slices - 1) / slices * sizeof(uint32_t)), st, true, slices, a, slices);
+    cudaError_t e = slices == 1 ? select<1>(a, st) : slices == 2 ? select<2>(a, st) : slices == 4 ? select<4>(a, st) : select<8>(a, st);
     if (e != cudaSuccess) return e;
     if (!cache_vec(v, el)) return s.dtype == 0 ? compact<uint32_t>(a, st) : compact<uint16_t>(a, st);
     in_units(a.v, 16 / el);
