@@ -321,10 +321,12 @@ mone_status mone_window_attention(mone_mem* m, int layer, const void* Q, int n_q
  *   lens       positions that each context holds, in device memory, so that a captured graph can serve growing contexts
  *   score      NULL, or for every context, layer and KV head the attention weight that each position has been given
  *              so far: [n_ctx][n_layers][n_kv_heads][table_width * page_size] fp32
- * Contexts are the handle's n_ctx; a `layer` argument is one of its layers (the other arrays of the call then have no
- * layer dimension) or MONE_ALL_LAYERS.  Table entries past a context's positions are not read.  An entry outside the
- * pool, or a length outside 0 .. table_width * page_size, is latched as MONE_ERR_CHECK (mone_mem_sync) and its
- * positions are skipped.
+ * Contexts are the handle's n_ctx; a `layer` argument is MONE_ALL_LAYERS or one of its layers: the call's queries, outputs,
+ * new keys and values and `kept` then have no layer dimension, what belongs to a cache (pools, score, to_score) keeps it.
+ * Table entries past a context's positions are not read.  An entry outside the pool, or a length outside
+ * 0 .. table_width * page_size, is latched as MONE_ERR_CHECK (mone_mem_sync), and what the call then gives for that
+ * context is not defined; nothing outside the pools, tables and outputs is read or written.  No output of a call may overlap
+ * what it reads.
  */
 typedef struct {
     void *K, *V;
@@ -359,8 +361,9 @@ mone_status mone_cache_append(mone_mem* m, int layer, const mone_cache* cache, c
  * Constraints: n_q_heads a multiple of n_kv_heads, n_q_heads / n_kv_heads <= 64; 1 <= n_tok <= 16; n_sink, window >= 0;
  * KV heads x contexts x layers of the call x ceil(n_tok n_q_heads / (4 n_kv_heads)) x blocks of 32 positions that a
  * table covers below 2^30.
- * The handle keeps a workspace that grows with the call's sizes (growing synchronises the stream, so a call of the
- * largest size comes before any capture); calls of one handle that overlap on two streams share it: order them.
+ * The handle keeps a workspace that grows with the call's sizes (with scores, 4 bytes for every query row and position that
+ * a table covers; growing synchronises the stream, so a call of the largest size comes before any capture); calls of one
+ * handle that overlap on two streams share it: order them.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (page_size), OOM, CUDA.
  */
 mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache, const void* Q, int n_q_heads, int n_tok,

@@ -308,9 +308,9 @@ cudaError_t select(const EvictArgs& a, cudaStream_t st) {
 constexpr int CM_SLOTS = 8, CM_WAY = 2;
 
 // A warp takes CM_SLOTS survivors: a lane looks up where one comes from and goes to, then all move units of their key and value
-// rows, CM_WAY under way in each lane.  Bound by HBM, whose reads come row by row: 64 x 8192 rows of 2 x 256 bytes take 65 us, 8.2 TB/s
-// read and written (part of it in L2), 128 x 1024 of 2 x 128 bytes 13.  (With the select: 8 slots, 2 under way 14.5 and 88.7
-// us; 4 under way 16.1 and 99.6; 8 under way 19.6 and 121: fewer loads a warp and more warps.)
+// rows, CM_WAY under way in each lane.  Bound by HBM, whose reads come row by row: 203 MB in rows of 256 bytes, read and written, take
+// 65 us, 6.2 TB/s, 128 x 1024 rows of 2 x 128 bytes 13 us.  (The two with their select: 2 under way 88.7 and 14.5 us, 4 under way
+// 99.6 and 16.1, 8 under way 121 and 19.6: few loads a warp and many warps.)
 template <typename U>
 __global__ void __launch_bounds__(CP_THREADS) cache_compact_kernel(const EvictArgs a) {
     const int chain = blockIdx.z, g = blockIdx.y, c = chain / a.v.L, l = chain % a.v.L, lane = threadIdx.x & 31;
