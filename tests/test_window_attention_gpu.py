@@ -104,6 +104,9 @@ def test_cuda_cores(group, Lq, n_past, n_sink, window, hd, dtype, pad):
     (4, 1, 15, 3, 5, 128),
     (5, 5, 3000, 100, 200, 128),
     (5, 5, 3000, 0, ALL, 128),
+    (5, 5, 3000, 100, 900, 128),   # few rows over many keys, hidden ones between
+    (4, 3, 2000, 4, 801, 128),
+    (1, 16, 1500, 700, 130, 128),
     (1, 90, 50, 7, 3, 64),         # row tiles of 16 tokens with windows of 3
 ])
 def test_few_rows(group, Lq, n_past, n_sink, window, hd):
@@ -194,6 +197,29 @@ def test_many_tiles_of_a_cta(hd, n_sink, window):
     for layer in (0, 9, L - 1):
         ref, _ = O.window_attention(Q[0, layer].float().cpu(), K[0, layer].float().cpu(), V[0, layer].float().cpu(), n_past, n_sink, window)
         assert rel_fro(outs[0][0, layer].float().cpu(), ref) <= 5e-3, layer
+
+
+@pytest.mark.parametrize("L,Lq", [(1, 280), (2, 280), (5, 280), (8, 280), (20, 90), (7, 500), (19, 33)])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_every_tile_of_uneven_shares(L, Lq, hd):
+    """Odd numbers of tiles of 32 tokens, over fewer CTAs than there are, over all, and with some left over: every row."""
+    n_kv, group, n_past, n_sink, window = 8, 4, 20, 9, 50
+    run = handle(L, n_kv, hd, torch.bfloat16)
+    g = torch.Generator(device="cuda").manual_seed(L)
+    K, V = (torch.randn(1, L, n_kv, n_past + Lq, hd, generator=g, device="cuda").bfloat16() for _ in range(2))
+    Q = torch.randn(1, L, group * n_kv, Lq, hd, generator=g, device="cuda").bfloat16()
+    out = torch.full_like(Q, 7.0)
+    mone.mone_window_attention(run.h, -1, Q, group * n_kv, Lq, K, V, K.stride()[:4], n_past, n_sink, window, out)
+    mone.mone_mem_sync(run.h)
+    run.close()
+    t, j = n_past + torch.arange(Lq, device="cuda")[:, None], torch.arange(n_past + Lq, device="cuda")[None]
+    hidden = (j > t) | ((j >= n_sink) & (j <= t - window))
+    k, v = (x.repeat_interleave(group, 2).double() for x in (K, V))
+    z = (Q.double() @ k.transpose(-1, -2) / hd ** 0.5).masked_fill(hidden, float("-inf"))
+    ref = torch.softmax(z, -1) @ v
+    far = (out.double() - ref).norm(dim=-1) / ref.norm(dim=-1)
+    assert (out.double() - ref).norm() / ref.norm() <= 5e-3
+    assert far.max() <= 2e-2  # no row is another's: the rounding of one row's probabilities, at most 2^-8 of each, and the output's
 
 
 @pytest.mark.parametrize("Lq", [3, 140])
