@@ -392,6 +392,52 @@ def test_append_attend_evict_attend():
                 assert rel_fro(res[c, l, g * group:(g + 1) * group].float().cpu(), one) <= 5e-3
 
 
+@pytest.mark.parametrize("hd,dtype", [(64, torch.bfloat16), (128, torch.bfloat16), (64, torch.float32)])
+def test_calls_in_a_row_read_what_the_kernels_ahead_wrote(hd, dtype):
+    """Nothing between the calls waits: the same bits as with a synchronisation after each, whatever runs ahead of what."""
+    n_kv, group, steps, keep = 2, 4, 24, 40
+    results = []
+    for wait in (True, False, False):
+        x = Cache([70, 0, 33], n_layers=2, n_kv=n_kv, hd=hd, page=16, dtype=dtype, spare=4, seed=5)
+        B, L = len(x.lens), x.L
+        g = torch.Generator(device="cuda").manual_seed(9)
+        rn = lambda *s: torch.randn(*s, generator=g, device="cuda").to(dtype)  # noqa: E731
+        Q, K, V = rn(steps, B, L, group * n_kv, 1, hd), rn(steps, B, L, n_kv, 1, hd), rn(steps, B, L, n_kv, 1, hd)
+        WQ, WK, WV = rn(steps, B, L, group * n_kv, 40, hd), rn(steps, B, L, n_kv, 90, hd), rn(steps, B, L, n_kv, 90, hd)
+        q, k, v, wq, wk, wv = (torch.zeros_like(t[0]) for t in (Q, K, V, WQ, WK, WV))
+        out, few, w_out, longer = torch.zeros_like(q), torch.zeros_like(q), torch.zeros_like(wq), torch.zeros_like(x.len_t)
+        got = []
+        x.tbl.copy_(x.table)
+        sync = torch.cuda.synchronize if wait else lambda: None
+        sync()
+        for i in range(steps):
+            for t, bank in ((q, Q), (k, K), (v, V), (wq, WQ), (wk, WK), (wv, WV)):
+                t.copy_(bank[i])
+            mone.mone_cache_append(x.h, -1, x.c, k, v, k.stride()[:4], 1, longer)
+            sync()
+            x.len_t.copy_(longer)
+            mone.mone_cache_attention(x.h, -1, x.c, q, group * n_kv, 1, 3, 50, out)
+            sync()
+            mone.mone_window_attention(x.h, -1, wq, group * n_kv, 40, wk, wv, wk.stride()[:4], 50, 4, 30, w_out)  # many rows
+            sync()
+            mone.mone_window_attention(x.h, -1, out, group * n_kv, 1, wk, wv, wk.stride()[:4], 50, 4, 30, few)
+            sync()
+            got += [out.clone(), w_out.clone(), few.clone()]
+        to_score = torch.zeros(B, L, n_kv, x.fresh.shape[1] * x.page, device="cuda")
+        kept = torch.zeros(B, L, n_kv, keep, dtype=torch.int32, device="cuda")
+        mone.mone_cache_evict(x.h, -1, x.c, keep, 4, 8, x.fresh, to_score, kept, longer)
+        sync()
+        x.len_t.copy_(longer)
+        x.tbl[:, :x.fresh.shape[1]].copy_(x.fresh)
+        x.score.copy_(to_score)
+        mone.mone_cache_attention(x.h, -1, x.c, q, group * n_kv, 1, 0, ALL, out)
+        got += [out.clone(), kept, to_score, x.score.clone()]
+        x.done()
+        results.append(got)
+    for other in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(results[0], other))
+
+
 def test_on_another_stream():
     x = Cache([900, 40])
     s = torch.cuda.Stream()
