@@ -9,8 +9,12 @@
 // when its warps are done, to the item's rows if it has the item whole, else to a part that the second kernel
 // joins.  Parts are joined in order, so equal calls give equal bits.
 //
+// Where the items are few and short enough (item_ctas), a cluster takes each of them instead: its CTAs and their warps have equal
+// shares of the item's blocks, and at the end they join their parts through distributed shared memory, without a second
+// kernel.
+//
 // For the weights the scores go to the workspace as well (4 bytes a row and position beside the 4 head_dim, in bf16, of its
-// key and value), and the second kernel adds exp(z - max) / sum over the rows of a KV head.
+// key and value), and the second kernel, or the cluster's end, adds exp(z - max) / sum over the rows of a KV head.
 #include <algorithm>
 #include <climits>
 
@@ -37,6 +41,7 @@ struct CaArgs {
     int vec;                   // 16-byte aligned rows
     float scale;
     int ctas;                  // that the blocks are dealt out to
+    int split;                 // CTAs of an item, or 0: dealt out
     float* part;               // [ctas + 4 ctas][2][ROWS][hd + 3]: the CTAs' parts, and those that their warps put here
     int* info;                 // [chains][n_kv][RT] of an item, the CTA that has its first part and their number (<< 16)
     float* lse;                // [chains][n_kv][R] log2 of the sum of exp of items that one CTA has whole, with the weights
@@ -122,13 +127,30 @@ struct CaWalk {
     bool first, last;         // the item begins in the CTA's share; the warp's last piece
     int cta0, cta1;           // the CTA's units
     __device__ CaWalk(const CaArgs& a) {
+        const int warp = threadIdx.x >> 5;
+        auto share_out = [&]() {
+            const int n = cta1 - cta0;
+            u = cta0 + n / CA_WARPS * warp + n % CA_WARPS * warp / CA_WARPS;
+            end = cta0 + n / CA_WARPS * (warp + 1) + n % CA_WARPS * (warp + 1) / CA_WARPS;
+        };
+        if (a.split) {  // units as if the item's context were the only one
+            const int item = udiv(blockIdx.x, a.split), rank = blockIdx.x - item * a.split;
+            c = a.v.n_ctx == 1 ? 0 : udiv(item, a.per);
+            r = CaRange(a, c);
+            units = r.units();
+            ctx0 = 0;
+            share = 1;
+            const int u0 = (item - c * a.per) * units;
+            cta0 = u0 + units * rank / a.split;
+            cta1 = u0 + units * (rank + 1) / a.split;
+            share_out();
+            return;
+        }
         CaDeal deal(a);
         share = deal.share;
         cta0 = deal.start(a, blockIdx.x);
         cta1 = deal.start(a, blockIdx.x + 1);
-        const int warp = threadIdx.x >> 5, n = cta1 - cta0;
-        u = cta0 + n / CA_WARPS * warp + n % CA_WARPS * warp / CA_WARPS;
-        end = cta0 + n / CA_WARPS * (warp + 1) + n % CA_WARPS * (warp + 1) / CA_WARPS;
+        share_out();
         if (u < end) {
             units = deal.locate(a, u, ctx0, c);
             r = CaRange(a, c);
@@ -240,7 +262,141 @@ __device__ __forceinline__ void write_row(const CaArgs& a, size_t kv, int c, int
 // log2 of the sum of exp of a row, +inf where nothing counts (its weights are then 0)
 __device__ __forceinline__ float row_lse(float m, float lx, float k2) { return lx == 0.f ? INFINITY : fmaf(m, k2, log2f(lx)); }
 
+// What the warps of a CTA have of a row's dimensions d and d + 1 (e: their place in a part), in the warps' order
+struct CaJoined {
+    float mx, l, lx, o0, o1;
+    template <typename P>
+    static __device__ __forceinline__ CaJoined of(const float* const (&ps)[CA_WARPS], int e, int row, float k2) {
+        CaJoined x{-INFINITY, 0.f, 0.f, 0.f, 0.f};
+        float mk[CA_WARPS];
+#pragma unroll
+        for (int k = 0; k < CA_WARPS; ++k) {
+            mk[k] = ps[k] ? ps[k][P::M + row] : -INFINITY;
+            x.mx = fmaxf(x.mx, mk[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < CA_WARPS; ++k) {
+            if (!ps[k]) continue;
+            const float f = mk[k] == -INFINITY ? 0.f : ca_exp2((mk[k] - x.mx) * k2);
+            const float2 o = *reinterpret_cast<const float2*>(ps[k] + e);
+            x.l = fmaf(f, ps[k][P::L + row], x.l);
+            x.lx = fmaf(f, ps[k][P::LX + row], x.lx);
+            x.o0 = fmaf(f, o.x, x.o0);
+            x.o1 = fmaf(f, o.y, x.o1);
+        }
+        return x;
+    }
+};
+
+// float (floats) of CTA `rank` of the cluster at the place of `p` in this one
+__device__ __forceinline__ float ca_remote(const float* p, uint32_t rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(map_to_cta(smem_u32(p), rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 ca_remote2(const float* p, uint32_t rank) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(map_to_cta(smem_u32(p), rank)) : "memory");
+    return v;
+}
+
+// An item's end where a cluster has it: the CTAs' parts, `mine` in each one's shared memory, are joined through it, each CTA some
+// of the dimensions, and each adds its positions' weights.
 template <typename Form>
+__device__ __forceinline__ void cluster_end(const CaArgs& a, const CaNote* notes, float* mine) {
+    using T = typename Form::T;
+    constexpr int HD = Form::HD, ROWS = Form::ROWS;
+    using P = Part<HD, ROWS>;
+    __shared__ float lse[ROWS];
+    const float k2 = a.scale * 1.4426950408889634f;
+    const int S = a.split, item = udiv(blockIdx.x, S), rank = blockIdx.x - item * S, tid = threadIdx.x;
+    const int c = a.v.n_ctx == 1 ? 0 : udiv(item, a.per), in_ctx = item - c * a.per, lg = a.RT == 1 ? in_ctx : udiv(in_ctx, a.RT);
+    const int l = a.v.L == 1 ? 0 : udiv(lg, a.v.n_kv), g = lg - l * a.v.n_kv, row0 = (in_ctx - lg * a.RT) * ROWS, rows = min(ROWS, a.R - row0);
+    const size_t kv = ((size_t)c * a.v.L + l) * a.v.n_kv + g;
+    const CaRange r(a, c);
+    const int units = r.units();
+    const bool split = S > 1 && units > 1;
+    if (units > 1) {  // else one warp has written the item
+        const long long head = l * a.v.s_layer + g * a.v.s_head;
+        auto write = [&](int row, int d, float o0, float o1, float l) {
+            write_row<T, HD>(a, kv, c, r.n, row0 + row, d, static_cast<const T*>(a.v.K) + head, static_cast<const T*>(a.v.V) + head, o0, o1, l);
+        };
+        const float* ps[CA_WARPS];
+#pragma unroll
+        for (int k = 0; k < CA_WARPS; ++k) ps[k] = notes[2 * k].part ? notes[2 * k].part : notes[2 * k + 1].part;
+        for (int e = 2 * tid; e < rows * HD; e += 2 * CA_THREADS) {
+            const int row = e / HD, d = e - row * HD;
+            const auto x = CaJoined::of<P>(ps, e, row, k2);
+            if (split) {
+                *reinterpret_cast<float2*>(mine + e) = make_float2(x.o0, x.o1);
+                if (d == 0) mine[P::M + row] = x.mx, mine[P::L + row] = x.l, mine[P::LX + row] = x.lx;
+            } else {
+                write(row, d, x.o0, x.o1, x.l);
+                if (d == 0) lse[row] = row_lse(x.mx, x.lx, k2);
+            }
+        }
+        if (split) {
+            cluster_sync();
+            // its max over the CTAs, and their factors
+            auto factors = [&](int row, float (&f)[8]) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) f[k] = k < S ? ca_remote(mine + P::M + row, k) : -INFINITY;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) mx = fmaxf(mx, f[k]);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) f[k] = f[k] == -INFINITY ? 0.f : ca_exp2((f[k] - mx) * k2);
+                return mx;
+            };
+            for (int e = 2 * (tid + rank * CA_THREADS); e < rows * HD; e += 2 * CA_THREADS * S) {
+                const int row = e / HD, d = e - row * HD;
+                float f[8], lk[8], sum = 0.f, o0 = 0.f, o1 = 0.f;
+                float2 o[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    o[k] = k < S ? ca_remote2(mine + e, k) : make_float2(0.f, 0.f);
+                    lk[k] = k < S ? ca_remote(mine + P::L + row, k) : 0.f;
+                }
+                factors(row, f);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    sum = fmaf(f[k], lk[k], sum);
+                    o0 = fmaf(f[k], o[k].x, o0);
+                    o1 = fmaf(f[k], o[k].y, o1);
+                }
+                write(row, d, o0, o1, sum);
+            }
+            if (a.z2 && tid < rows) {
+                float f[8], lx = 0.f;
+                const float mx = factors(tid, f);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < S) lx = fmaf(f[k], ca_remote(mine + P::LX + tid, k), lx);
+                lse[tid] = row_lse(mx, lx, k2);
+            }
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        }
+    } else if (a.z2 && tid < rows) {
+        lse[tid] = a.lse[kv * a.R + row0 + tid];
+    }
+    if (a.z2) {
+        __syncthreads();
+        const int b0 = units * rank / S, b1 = min(units * (rank + 1) / S, r.nb);
+        float* score = a.v.score + (((size_t)c * a.v.Lh + l) * a.v.n_kv + g) * a.v.cap;
+        const float* z = a.z2 + (kv * a.R + row0) * a.pitch;
+        for (int i = tid; i < (b1 - b0) * KB; i += CA_THREADS) {
+            const int p = r.at(b0 + i / KB) + i % KB;
+            if (p >= r.n || (p >= a.n_sink && p <= r.t0 - a.window)) continue;
+            float w = 0.f;
+#pragma unroll 4
+            for (int row = 0; row < rows; ++row) w += ca_exp2(z[row * a.pitch + p] - lse[row]);
+            score[p] += w;
+        }
+    }
+    if (split) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // nobody leaves while another reads its part
+}
+
+template <typename Form, bool ITEMS>
 __global__ void __launch_bounds__(CA_THREADS, Form::CTAS)
 cache_attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const CaArgs a) {
     using T = typename Form::T;
@@ -259,6 +415,10 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
         form.run(a, notes + 2 * warp);
     }
     __syncthreads();
+    if constexpr (ITEMS) {
+        cluster_end<Form>(a, notes, reinterpret_cast<float*>(smem + CA_WARPS * Form::WARP_BYTES));
+        return;
+    }
     // the warps' parts, item by item
     const float k2 = a.scale * 1.4426950408889634f;
     for (int i = 0; i < 2 * CA_WARPS;) {
@@ -283,28 +443,14 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
         float* to = it.whole ? nullptr : P::of_cta(a, blockIdx.x, it.first);
         for (int e = 2 * threadIdx.x; e < rows * HD; e += 2 * CA_THREADS) {
             const int row = e / HD, d = e - row * HD;
-            float mk[CA_WARPS], mx = -INFINITY, l = 0.f, lx = 0.f, o0 = 0.f, o1 = 0.f;
-#pragma unroll
-            for (int k = 0; k < CA_WARPS; ++k) {
-                mk[k] = ps[k] ? ps[k][P::M + row] : -INFINITY;
-                mx = fmaxf(mx, mk[k]);
-            }
-#pragma unroll
-            for (int k = 0; k < CA_WARPS; ++k) {
-                if (!ps[k]) continue;
-                const float f = mk[k] == -INFINITY ? 0.f : ca_exp2((mk[k] - mx) * k2);
-                const float2 o = *reinterpret_cast<const float2*>(ps[k] + e);
-                l = fmaf(f, ps[k][P::L + row], l);
-                lx = fmaf(f, ps[k][P::LX + row], lx);
-                o0 = fmaf(f, o.x, o0);
-                o1 = fmaf(f, o.y, o1);
-            }
+            const auto x = CaJoined::of<P>(ps, e, row, k2);
             if (to) {
-                *reinterpret_cast<float2*>(to + e) = make_float2(o0, o1);
-                if (d == 0) to[P::M + row] = mx, to[P::L + row] = l, to[P::LX + row] = lx;
+                *reinterpret_cast<float2*>(to + e) = make_float2(x.o0, x.o1);
+                if (d == 0) to[P::M + row] = x.mx, to[P::L + row] = x.l, to[P::LX + row] = x.lx;
             } else {
-                write_row<T, HD>(a, kv, it.c, it.n, row0 + row, d, static_cast<const T*>(a.v.K) + head, static_cast<const T*>(a.v.V) + head, o0, o1, l);
-                if (d == 0 && a.lse) a.lse[kv * a.R + row0 + row] = row_lse(mx, lx, k2);
+                write_row<T, HD>(a, kv, it.c, it.n, row0 + row, d, static_cast<const T*>(a.v.K) + head, static_cast<const T*>(a.v.V) + head, x.o0, x.o1,
+                                 x.l);
+                if (d == 0 && a.lse) a.lse[kv * a.R + row0 + row] = row_lse(x.mx, x.lx, k2);
             }
         }
     }
@@ -319,6 +465,7 @@ struct CaCores {
     static constexpr int HD = HD_, ROWS = 4, CTAS = HD == 64 ? 3 : 2;
     static constexpr int VE = 16 / sizeof(T), D = HD / 8, NP = D / VE;  // elements of 16 bytes; dimensions and 16-byte pieces of a lane
     static constexpr int U = 2;                                         // keys of a lane group at a time
+    static constexpr int ONE = 1, EACH = 1, FULL = 1, FEW = 1;          // blocks of a warp, see item_ctas
     static constexpr int WARP_BYTES = 2 * Part<HD, ROWS>::FLOATS * 4;
 
     float* parts;
@@ -522,6 +669,7 @@ struct CaTensor {
     using T = bf16;
     static constexpr int HD = HD_, ROWS = 8 * NT, CTAS = 2;
     static constexpr int SK = HD == 64 ? 32 : 16, SPB = KB / SK;  // keys of a stage, stages of a block
+    static constexpr int ONE = 3, EACH = 2, FULL = 16, FEW = 6 / SPB;                // blocks of a warp, see item_ctas
     static constexpr int SLAB = SK * 128, TILE = HD / 64 * SLAB, STAGE = 2 * TILE;  // 64 dimensions of the keys; keys; both
     static constexpr int NS = 3;
     static constexpr int BAR = NS * STAGE, WARP_BYTES = BAR + 1024;  // the ring, its barriers
@@ -924,21 +1072,49 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) cache_finish_kernel(const CaAr
 
 // Blocks of an item, at most: a context as long as its table, first positions and window in blocks of their own
 long long max_blocks(const CacheView& v) { return (v.cap + KB - 1) / KB + 1; }
-// Whether a call has a second kernel
-bool has_finish(const CacheView& v) { return v.score || max_blocks(v) > CA_WHOLE; }
+long long seen_blocks(const CaArgs& a) {
+    return std::min(max_blocks(a.v), ((long long)a.n_sink + KB - 1) / KB + ((long long)a.window + a.n_tok + KB - 1) / KB + 1);
+}
+
+// CTAs (a cluster) of each item, or 0: the blocks are dealt out and a second kernel follows.  While all items fit on the GPU at once, a cluster an
+// item saves the second kernel and the dealing.  It takes one CTA up to ONE blocks a warp, then as many as leave EACH.  Where a
+// warp would have more than FULL blocks, or more than FEW and half of the GPU nothing to do, dealing is faster, and contexts may
+// be unequal.  (32 heads over 8, pages of 64, without and with weights, us here and dealt.  hd 64: 1 layer of 150 positions 5.1, 6.4 and
+// 6.3, 8.9; 500: 5.7, 6.8 and 9.4, 10.7; 4500: 8.6, 11.9 and 10.4, 14.3; 9000: 11.5, 17.2 and 11.3, 15.6; 16 layers of 1151: 9.7, 14.2
+// and 12.5, 15.4; 4500: 26.2, 39.0 and 30.5, 37.2; 32 of 1151: 15.7, 22.0 and 22.6, 25.5.  hd 128, 4500: 13.7, 17.6 and 12.2, 15.7.
+// The CUDA cores take 6 us a block, so it is theirs for one a warp: fp32, 500: 11.6, 13.3 and 27.8, 30.8; 1151: 17.5, 20.0
+// and 14.7, 17.1.)
+template <typename Form>
+int item_ctas(const CaArgs& a, int sms) {
+    const long long items = (long long)a.per * a.v.n_ctx, blocks = seen_blocks(a), slots = (long long)Form::CTAS * sms;
+    if (items > slots || (a.v.score && a.RT > 1)) return 0;  // (row tiles of a head add to the same weights)
+    int S = 1;
+    if (blocks > Form::ONE * CA_WARPS)
+        while (S < 8 && 2 * S * items <= slots && blocks > Form::EACH * S * CA_WARPS) S *= 2;
+    return blocks <= S * CA_WARPS * (2 * S * items > slots ? Form::FULL : Form::FEW) ? S : 0;
+}
 
 template <typename Form>
-cudaError_t launch(CaArgs a, const CUtensorMap& tmK, const CUtensorMap& tmV, int sms, cudaStream_t st) {
+cudaError_t launch(CaArgs a, const CUtensorMap& tmK, const CUtensorMap& tmV, int sms, int* kernels, cudaStream_t st) {
     static_assert(Form::CTAS * Form::ROWS <= CA_SM_ROWS, "the workspace's parts");
-    constexpr size_t smem = CA_WARPS * Form::WARP_BYTES + 1024;
-    static PerDevice<SmemOptIn> once;
-    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(cache_attention_kernel<Form>), smem, once);
-    if (e != cudaSuccess) return e;
+    constexpr size_t smem = CA_WARPS * Form::WARP_BYTES + 1024, smem_items = smem + Part<Form::HD, Form::ROWS>::FLOATS * sizeof(float);
+    static PerDevice<SmemOptIn> once, once_items;
     a.RT = (a.R + Form::ROWS - 1) / Form::ROWS;
     a.per = a.v.L * a.v.n_kv * a.RT;
     a.ctas = Form::CTAS * sms;
-    e = launch_kernel(cache_attention_kernel<Form>, dim3(a.ctas), dim3(CA_THREADS), smem, st, true, 1, tmK, tmV, a);
-    if (e != cudaSuccess || !has_finish(a.v)) return e;
+    a.split = item_ctas<Form>(a, sms);
+    if (a.split) {
+        *kernels = 1;
+        a.ctas = a.split * a.per * a.v.n_ctx;
+        cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(cache_attention_kernel<Form, true>), smem_items, once_items);
+        if (e != cudaSuccess) return e;
+        return launch_kernel(cache_attention_kernel<Form, true>, dim3(a.ctas), dim3(CA_THREADS), smem_items, st, true, a.split, tmK, tmV, a);
+    }
+    cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(cache_attention_kernel<Form, false>), smem, once);
+    if (e != cudaSuccess) return e;
+    e = launch_kernel(cache_attention_kernel<Form, false>, dim3(a.ctas), dim3(CA_THREADS), smem, st, true, 1, tmK, tmV, a);
+    // without weights, no item is split over CTAs if none is long
+    if (e != cudaSuccess || (*kernels = a.v.score || max_blocks(a.v) > CA_WHOLE ? 2 : 1) == 1) return e;
     const dim3 grid((unsigned)(a.R + (a.v.score ? (a.v.cap + FIN_POS - 1) / FIN_POS : 0)), a.v.n_kv, a.v.n_ctx * a.v.L);
     return launch_kernel(cache_finish_kernel<Form>, grid, dim3(FIN_THREADS), 0, st, true, 1, a);
 }
@@ -971,11 +1147,11 @@ bool pool_maps(const CacheView& v, CUtensorMap* mk, CUtensorMap* mv) {
 }
 
 template <int HD>
-cudaError_t launch_bf16(const CaArgs& a, int sms, cudaStream_t st) {
+cudaError_t launch_bf16(const CaArgs& a, int sms, int* kernels, cudaStream_t st) {
     CUtensorMap mk = {}, mv = {};
     // pages of fewer than 8 positions would need copies of less than a swizzle's rows
-    if (a.vec && a.v.page_log2 >= 3 && pool_maps<HD>(a.v, &mk, &mv)) return a.R <= 8 ? launch<CaTensor<HD, 1>>(a, mk, mv, sms, st) : launch<CaTensor<HD, 2>>(a, mk, mv, sms, st);
-    return launch<CaCores<bf16, HD>>(a, mk, mv, sms, st);
+    if (a.vec && a.v.page_log2 >= 3 && pool_maps<HD>(a.v, &mk, &mv)) return a.R <= 8 ? launch<CaTensor<HD, 1>>(a, mk, mv, sms, kernels, st) : launch<CaTensor<HD, 2>>(a, mk, mv, sms, kernels, st);
+    return launch<CaCores<bf16, HD>>(a, mk, mv, sms, kernels, st);
 }
 
 struct Layout {
@@ -1001,10 +1177,8 @@ size_t cache_attention_workspace(const DevState& s, const CacheView& v, int n_q,
     return Layout(s, v, n_q, n_tok).bytes;
 }
 
-int cache_attention_kernels(const CacheView& v) { return has_finish(v) ? 2 : 1; }
-
 cudaError_t launch_cache_attention(const DevState& s, const CacheView& v, const void* Q, int n_q, int n_tok, int n_sink, int window,
-                                   void* out, void* ws, cudaStream_t st) {
+                                   void* out, void* ws, int* kernels, cudaStream_t st) {
     const Layout w(s, v, n_q, n_tok);
     CaArgs a{};
     a.v = v;
@@ -1020,9 +1194,9 @@ cudaError_t launch_cache_attention(const DevState& s, const CacheView& v, const 
     a.lse = v.score ? reinterpret_cast<float*>(b + w.lse) : nullptr;
     a.z2 = v.score ? reinterpret_cast<float*>(b + w.z2) : nullptr;
     a.pitch = w.pitch;
-    if (s.dtype != 0) return s.hd == 64 ? launch_bf16<64>(a, s.sms, st) : launch_bf16<128>(a, s.sms, st);
+    if (s.dtype != 0) return s.hd == 64 ? launch_bf16<64>(a, s.sms, kernels, st) : launch_bf16<128>(a, s.sms, kernels, st);
     const CUtensorMap none = {};
-    return s.hd == 64 ? launch<CaCores<float, 64>>(a, none, none, s.sms, st) : launch<CaCores<float, 128>>(a, none, none, s.sms, st);
+    return s.hd == 64 ? launch<CaCores<float, 64>>(a, none, none, s.sms, kernels, st) : launch<CaCores<float, 128>>(a, none, none, s.sms, kernels, st);
 }
 
 }  // namespace mone

@@ -1103,9 +1103,12 @@ mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache
         m->cws = p;
         m->cws_bytes = need;
     }
-    return timed(m, K_CACHE, st, cache_attention_kernels(v), [&] {
-        return launch_cache_attention(s, v, Q, n_q_heads, n_tok, n_sink, window, out, m->cws, st);
-    });
+    int kernels = 0;
+    MONE_TRY(timed(m, K_CACHE, st, 0, [&] {
+        return launch_cache_attention(s, v, Q, n_q_heads, n_tok, n_sink, window, out, m->cws, &kernels, st);
+    }));
+    m->launches += kernels;
+    return MONE_OK;
 }
 
 mone_status mone_cache_evict(mone_mem* m, int layer, const mone_cache* cache, int keep, int n_sink, int n_recent,

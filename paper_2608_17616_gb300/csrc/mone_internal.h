@@ -214,12 +214,11 @@ cudaError_t launch_cache_append(const DevState& s, const CacheView& v, const voi
                                 int n_tok, const int* counts, int* lens_out, cudaStream_t st);
 cudaError_t launch_cache_evict(const DevState& s, const CacheView& v, int keep, int n_sink, int n_recent, const int* to, int to_width,
                                float* to_score, int* kept, int* lens_out, cudaStream_t st);
-// Workspace of launch_cache_attention in bytes for this call (0: more blocks than it counts), and the call.
+// Workspace of launch_cache_attention in bytes for this call (0: more blocks than it counts), and the call, which says how many
+// kernels it launched.
 size_t cache_attention_workspace(const DevState& s, const CacheView& v, int n_q, int n_tok);
 cudaError_t launch_cache_attention(const DevState& s, const CacheView& v, const void* Q, int n_q, int n_tok, int n_sink, int window,
-                                   void* out, void* ws, cudaStream_t st);
-// Kernels of one launch_cache_attention.
-int cache_attention_kernels(const CacheView& v);
+                                   void* out, void* ws, int* kernels, cudaStream_t st);
 
 // ---- kernels in ttl_tc.cu (bf16 tcgen05 path)
 struct TcMaps {

@@ -154,29 +154,48 @@ def test_launches_on_either_device(fake, dtype):
     for dev, sms in ((0, 152), (1, 100), (0, 152)):
         fake.device(dev)
         h, c = init(dtype=dtype), cache()
+        c.table_width = 2000  # more than a cluster takes
         fake.drain()
         for layer in (-1, 2):
             mone.mone_cache_append(h, layer, c, P, P, ST, 3, stream=0)
             for score in (P, None):
                 c.score = score
-                mone.mone_cache_attention(h, layer, c, P, 4, 2, 1, 100, P, stream=0)
+                mone.mone_cache_attention(h, layer, c, P, 4, 2, 1, 1 << 30, P, stream=0)
             c.score = P
             to = type("T", (), dict(shape=(2, 10), data_ptr=lambda self: P + 64))()
             mone.mone_cache_evict(h, layer, c, 50, 2, 3, to, P + 128, P, stream=0)
             launches, _ = fake.drain()
             assert {x["dev"] for x in launches} == {dev}
             assert [x["grid"][0] % sms for x in launches if "attention_kernel" in x["name"]] == [0, 0]
-            assert sum("finish_kernel" in x["name"] for x in launches) == 1
+            assert sum("finish_kernel" in x["name"] for x in launches) == 2
         mone.mone_mem_free(h)
+
+
+@pytest.mark.parametrize("width,window,ctas", [(10, 1 << 30, 1), (22, 1 << 30, 1), (23, 1 << 30, 2), (50, 1 << 30, 4), (128, 1 << 30, 8),
+                                               (382, 1 << 30, 8), (383, 1 << 30, 0), (5000, 300, 1), (5000, 400, 2)])
+def test_few_and_short_items_take_a_cluster_each(fake, width, window, ctas):
+    """Pages of 16: blocks of 32 positions, one more for the window's start, over warps with at most three of them, or two, or six."""
+    h, c = init(), cache()
+    c.table_width, c.score = width, None
+    fake.drain()
+    mone.mone_cache_attention(h, 0, c, P, 4, 1, 0, window, P, stream=0)
+    (x, *more), _ = fake.drain()
+    if ctas:
+        assert not more and x["grid"][0] % ctas == 0 and x["grid"][0] // ctas < 20 and max(x["cluster"], 1) == ctas
+    else:
+        assert len(more) == 1 and x["grid"][0] % 152 == 0
 
 
 def test_launch_counts_are_the_kernels_launched(fake):
     h, c = init(), cache()
+    wide = cache()
+    wide.table_width = 2000
     fake.drain()
     n0 = mone.mone_mem_launch_count(h)
     to = type("T", (), dict(shape=(2, 10), data_ptr=lambda self: P + 64))()
     for call in (lambda: mone.mone_cache_append(h, 0, c, P, P, ST, 3, stream=0),
                  lambda: mone.mone_cache_attention(h, 0, c, P, 4, 2, 1, 100, P, stream=0),
+                 lambda: mone.mone_cache_attention(h, 0, wide, P, 4, 2, 1, 1 << 30, P, stream=0),
                  lambda: mone.mone_cache_evict(h, 0, c, 50, 2, 3, to, P + 128, P, stream=0),
                  lambda: mone.mone_window_attention(h, 0, P, 4, 10, P, P, ST, 5, 2, 3, P, stream=0)):
         call()

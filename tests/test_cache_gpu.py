@@ -140,6 +140,32 @@ def test_attention(lens, group, n_tok, hd, page, n_sink, window, dtype):
     attend(x, group, n_tok, n_sink, window, scale=4.0)  # again on the same workspace, with steeper softmaxes
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lens,group,n_tok,hd,page,n_sink,window", [
+    ([0, 1, 2, 0, 300], 4, 1, 64, 16, 0, ALL),
+    ([31, 32, 33, 63, 64, 65], 4, 1, 64, 32, 0, ALL),
+    ([255, 256, 257, 600], 2, 1, 128, 64, 0, ALL),
+    ([4000], 8, 1, 64, 16, 0, ALL),
+    ([3001, 17, 900], 5, 3, 128, 8, 0, ALL),
+    ([400, 90], 7, 16, 64, 16, 0, ALL),
+    ([9000, 30], 4, 1, 64, 16, 100, 7000),
+    ([9000, 500, 6700], 4, 3, 128, 64, 33, 6500),
+    ([300, 77], 4, 1, 64, 1, 0, ALL),
+])
+def test_attention_where_tables_could_hold_much(lens, group, n_tok, hd, page, n_sink, window, dtype):
+    """A call goes by what its tables and its window allow: dealt out here, though the contexts are short."""
+    x = Cache(lens, hd=hd, page=page, dtype=dtype, seed=sum(lens) + group, spare=16384 // page)
+    attend(x, group, n_tok, n_sink, window)
+    attend(x, group, n_tok, n_sink, window, scale=4.0)
+
+
+@pytest.mark.parametrize("n_layers,lens", [
+    (10, [700, 1500, 90]), (20, [700, 1500, 90]), (20, [300, 0, 77, 130, 1, 200]), (1, [1000]), (20, [33, 32, 31, 64, 65, 1])])
+@pytest.mark.parametrize("group,n_tok,hd,n_sink,window", [(4, 1, 64, 0, ALL), (4, 1, 128, 40, 300), (3, 5, 64, 0, ALL), (2, 4, 64, 3, 33)])
+def test_attention_by_clusters_of_every_size(n_layers, lens, group, n_tok, hd, n_sink, window):
+    attend(Cache(lens, n_layers=n_layers, hd=hd, page=32, seed=n_layers), group, n_tok, n_sink, window)
+
+
 @pytest.mark.parametrize("order,pad", [("position", 0), ("layers inner", 0), ("head", 8), ("head", 3), ("position", 1)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("hd", [64, 128])
