@@ -384,13 +384,27 @@ __device__ __forceinline__ void cluster_end(const CaArgs& a, const CaNote* notes
         const int b0 = units * rank / S, b1 = min(units * (rank + 1) / S, r.nb);
         float* score = a.v.score + (((size_t)c * a.v.Lh + l) * a.v.n_kv + g) * a.v.cap;
         const float* z = a.z2 + (kv * a.R + row0) * a.pitch;
-        for (int i = tid; i < (b1 - b0) * KB; i += CA_THREADS) {
-            const int p = r.at(b0 + i / KB) + i % KB;
-            if (p >= r.n || (p >= a.n_sink && p <= r.t0 - a.window)) continue;
-            float w = 0.f;
+        for (int i = tid; i < (b1 - b0) * (KB / 4); i += CA_THREADS) {  // four positions a thread
+            const int p = r.at(b0 + i / (KB / 4)) + i % (KB / 4) * 4;
+            bool seen[4];
+            float w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                seen[k] = p + k < r.n && (p + k < a.n_sink || p + k > r.t0 - a.window);
+                w[k] = seen[k] ? score[p + k] : 0.f;
+            }
+            float add[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-            for (int row = 0; row < rows; ++row) w += ca_exp2(z[row * a.pitch + p] - lse[row]);
-            score[p] += w;
+            for (int row = 0; row < rows; ++row) {
+                const float4 x = *reinterpret_cast<const float4*>(z + row * a.pitch + p);
+                add[0] += ca_exp2(x.x - lse[row]);
+                add[1] += ca_exp2(x.y - lse[row]);
+                add[2] += ca_exp2(x.z - lse[row]);
+                add[3] += ca_exp2(x.w - lse[row]);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (seen[k]) score[p + k] = w[k] + add[k];
         }
     }
     if (split) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // nobody leaves while another reads its part
@@ -1077,21 +1091,28 @@ long long seen_blocks(const CaArgs& a) {
 }
 
 // CTAs (a cluster) of each item, or 0: the blocks are dealt out and a second kernel follows.  While all items fit on the GPU at once, a cluster an
-// item saves the second kernel and the dealing.  It takes one CTA up to ONE blocks a warp, then as many as leave EACH.  Where a
-// warp would have more than FULL blocks, or more than FEW and half of the GPU nothing to do, dealing is faster, and contexts may
-// be unequal.  (32 heads over 8, pages of 64, without and with weights, us here and dealt.  hd 64: 1 layer of 150 positions 5.1, 6.4 and
-// 6.3, 8.9; 500: 5.7, 6.8 and 9.4, 10.7; 4500: 8.6, 11.9 and 10.4, 14.3; 9000: 11.5, 17.2 and 11.3, 15.6; 16 layers of 1151: 9.7, 14.2
-// and 12.5, 15.4; 4500: 26.2, 39.0 and 30.5, 37.2; 32 of 1151: 15.7, 22.0 and 22.6, 25.5.  hd 128, 4500: 13.7, 17.6 and 12.2, 15.7.
-// The CUDA cores take 6 us a block, so it is theirs for one a warp: fp32, 500: 11.6, 13.3 and 27.8, 30.8; 1151: 17.5, 20.0
-// and 14.7, 17.1.)
+// item saves the second kernel and the dealing.  It takes one CTA up to ONE blocks a warp, then as many as leave EACH.  Dealing is
+// faster where a warp would have more than FEW blocks with half of the GPU idle, or more than FULL blocks of contexts that
+// may be unequal.  (32 heads over 8, pages of 64, without and with weights, us here and dealt.  hd 64: 1 layer of 150 positions 5.2, 5.8
+// and 6.3, 8.9; 500: 5.7, 6.8 and 9.4, 10.7; 4500: 8.6, 10.5 and 10.4, 14.3; 9000: 11.5, 17.2 and 11.3, 15.6; 16 layers of 1151:
+// 9.8, 12.1 and 12.5, 15.4; 20000: 97, 121 and 106, 124; 32 of 1151: 15.6, 17.5 and 22.6, 25.5.  hd 128, 4 layers of 131072, two tokens:
+// 297 and 318; 1 of 4500: 13.7, 17.6 and 12.2, 15.7.  The CUDA cores take 6 us a block, so it is theirs for one a warp: fp32, 500: 12.0,
+// 13.7 and 27.8, 30.8; 1151: 17.5, 20.0 and 14.7, 17.1.)
 template <typename Form>
 int item_ctas(const CaArgs& a, int sms) {
     const long long items = (long long)a.per * a.v.n_ctx, blocks = seen_blocks(a), slots = (long long)Form::CTAS * sms;
     if (items > slots || (a.v.score && a.RT > 1)) return 0;  // (row tiles of a head add to the same weights)
     int S = 1;
     if (blocks > Form::ONE * CA_WARPS)
-        while (S < 8 && 2 * S * items <= slots && blocks > Form::EACH * S * CA_WARPS) S *= 2;
-    return blocks <= S * CA_WARPS * (2 * S * items > slots ? Form::FULL : Form::FEW) ? S : 0;
+        while (S < 8 && 2 * S * items <= slots && blocks > Form::EACH * S * CA_WARPS) {
+            // clusters of eight that fill the GPU make way for the next call's late (4 layers of 1151, hd 64, with weights: 8.8 us on four CTAs
+            // each, 10.7 on eight; of 9000 24.5 and 21.0)
+            if (S == 4 && a.v.score && 8 * items > slots * 3 / 4 && blocks <= 5 * S * CA_WARPS) break;
+            S *= 2;
+        }
+    const bool full = 2 * S * items > slots;
+    if (full && a.v.n_ctx == 1 && Form::FULL > 1) return S;
+    return blocks <= S * CA_WARPS * (full ? Form::FULL : Form::FEW) ? S : 0;
 }
 
 template <typename Form>
