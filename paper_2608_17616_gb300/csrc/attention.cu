@@ -593,7 +593,6 @@ __global__ void __launch_bounds__(DE_WARPS * 32, HD == 64 ? 4 : 3) attention_dec
     auto load = [](const bf16* p) { return WIN ? *reinterpret_cast<const uint4*>(p) : __ldg(reinterpret_cast<const uint4*>(p)); };
     if constexpr (WIN) {
         pdl_wait();
-        pdl_trigger();
     }
     // rows gq and gq + 8 of the tile
     uint32_t qa[HD / 16][4];

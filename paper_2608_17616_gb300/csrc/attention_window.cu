@@ -237,7 +237,6 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     __syncthreads();
     tc_fence_after();
     pdl_wait();
-    pdl_trigger();
     const uint32_t tmem = __shfl_sync(0xffffffffu, *slot, 0);  // of a tile: the S (and P) buffers, then O
     const int rt = a.rows;
     WinTiles<NK> tl(a, C);
@@ -564,7 +563,9 @@ __device__ __forceinline__ void wc_stage(float* dst, int n, bool vec, float scal
 #pragma unroll 8
         for (int e = threadIdx.x; e < ROWS * VPR; e += WC_THREADS) {
             const int i = e / VPR, u = e % VPR;
-            const uint4 r = i < n ? __ldg(reinterpret_cast<const uint4*>(row(i)) + u) : make_uint4(0, 0, 0, 0);
+            // (fp32: after the wait for the kernel ahead)
+            const uint4* p = i < n ? reinterpret_cast<const uint4*>(row(i)) + u : nullptr;
+            const uint4 r = !p ? make_uint4(0, 0, 0, 0) : sizeof(T) == 4 ? *p : __ldg(p);
             const T* t = reinterpret_cast<const T*>(&r);
 #pragma unroll
             for (int k = 0; k < PER; k += 4)
@@ -611,6 +612,9 @@ __global__ void __launch_bounds__(WC_THREADS) window_cores_kernel(const AttnArgs
     const long long kv_off = (long long)(c / a.L) * a.s0 + (long long)(c % a.L) * a.s1 + (long long)g * a.s2;
     const T* Kc = static_cast<const T*>(a.K) + kv_off;
     const T* Vc = static_cast<const T*>(a.V) + kv_off;
+    if constexpr (sizeof(T) == 4) {
+        pdl_wait();
+        }
     // row i of the tile: head h0 + i / toks, token r0 + i % toks
     auto q_at = [&](int i) { return (((size_t)c * a.n_q + (size_t)g * a.group + h0 + i / toks) * a.Lq + r0 + i % toks) * HD; };
     wc_stage<T, HD, WC_ROWS>(Qs, rows, vec_q, a.scale, [&](int i) { return static_cast<const T*>(a.Q) + q_at(i); });
@@ -760,8 +764,9 @@ cudaError_t launch_cores(AttnArgs a, int C, cudaStream_t st) {
     a.rows = WC_ROWS / hb;  // tokens of a tile
     const long long blocks = (long long)((a.Lq + a.rows - 1) / a.rows) * head_blocks * a.n_kv * C;
     if (blocks > INT_MAX) return cudaErrorInvalidConfiguration;
-    window_cores_kernel<T, HD><<<(unsigned)blocks, WC_THREADS, smem, st>>>(a, hb, head_blocks, C, (reinterpret_cast<uintptr_t>(a.Q) & 15u) == 0);
-    return cudaGetLastError();
+    // (programmatic: fp32, whose keys and values come by asynchronous copies)
+    return launch_kernel(window_cores_kernel<T, HD>, dim3((unsigned)blocks), dim3(WC_THREADS), smem, st, sizeof(T) == 4, 1, a, hb, head_blocks, C,
+                         (reinterpret_cast<uintptr_t>(a.Q) & 15u) == 0);
 }
 
 template <int HD>

@@ -28,7 +28,6 @@ template <typename U>
 __global__ void __launch_bounds__(CP_THREADS) cache_append_kernel(const AppendArgs a) {
     const int chain = blockIdx.z, g = blockIdx.y, c = chain / a.v.L, l = chain % a.v.L;
     pdl_wait();
-    pdl_trigger();
     const int len = cache_len(a.v, c);
     const int n = a.counts ? min(max(a.counts[c], 0), a.n_tok) : a.n_tok;
     if (a.lens_out && blockIdx.x == 0 && g == 0 && l == 0 && threadIdx.x == 0)
@@ -139,7 +138,6 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) cache_select_kernel(const Evic
     const int chain = blockIdx.z, g = blockIdx.y, c = chain / a.v.L, l = chain % a.v.L, rank = (int)cluster_ctarank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_wait();
-    pdl_trigger();
     const int N = cache_len(a.v, c);
     int* kept = a.kept + ((size_t)chain * a.v.n_kv + g) * a.keep;
     if (a.lens_out && g == 0 && l == 0 && rank == 0 && tid == 0) a.lens_out[c] = min(N, a.keep);

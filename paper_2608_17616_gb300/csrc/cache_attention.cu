@@ -425,7 +425,6 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_con
     {
         Form form(tmK, tmV, smem + warp * Form::WARP_BYTES, a.RT);
         pdl_wait();
-        pdl_trigger();  // the second kernel waits for the end of this one
         form.run(a, notes + 2 * warp);
     }
     __syncthreads();
@@ -1028,7 +1027,7 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) cache_finish_kernel(const CaAr
     const CaRange r(a, c);
     const int tile0 = ((int)blockIdx.x - a.R) * FIN_POS, p0 = tile0 + 4 * threadIdx.x;
     if (tile0 >= r.n || (tile0 >= a.n_sink && tile0 + FIN_POS <= r.t0 - a.window + 1)) return;  // nobody sees them
-    pdl_wait();  // above, only the lengths are read, which were there before the first kernel triggered
+    pdl_wait();  // above, only the lengths are read, which were there before the first kernel began
     if ((int)blockIdx.x < a.R) {
         const int row = blockIdx.x, info = a.info[kv * a.RT + row / ROWS], first = info & 0xffff, n = info >> 16;
         if (n == 1) return;
@@ -1104,12 +1103,7 @@ int item_ctas(const CaArgs& a, int sms) {
     if (items > slots || (a.v.score && a.RT > 1)) return 0;  // (row tiles of a head add to the same weights)
     int S = 1;
     if (blocks > Form::ONE * CA_WARPS)
-        while (S < 8 && 2 * S * items <= slots && blocks > Form::EACH * S * CA_WARPS) {
-            // clusters of eight that fill the GPU make way for the next call's late (4 layers of 1151, hd 64, with weights: 8.8 us on four CTAs
-            // each, 10.7 on eight; of 9000 24.5 and 21.0)
-            if (S == 4 && a.v.score && 8 * items > slots * 3 / 4 && blocks <= 5 * S * CA_WARPS) break;
-            S *= 2;
-        }
+        while (S < 8 && 2 * S * items <= slots && blocks > Form::EACH * S * CA_WARPS) S *= 2;
     const bool full = 2 * S * items > slots;
     if (full && a.v.n_ctx == 1 && Form::FULL > 1) return S;
     return blocks <= S * CA_WARPS * (full ? Form::FULL : Form::FEW) ? S : 0;

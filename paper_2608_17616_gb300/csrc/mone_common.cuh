@@ -242,10 +242,12 @@ __device__ __forceinline__ void fence_proxy_async_smem() {
 // their wait; chained behind them are each other and kernels that begin with their wait.  The first learning kernel of a call
 // is launched without the attribute and starts when all before it is complete.
 //
-// The cache's kernels, and the windowed attention's on the tensor cores, wait before they read or write anything of a caller's,
-// and trigger, if at all, after that.  They may start next to any kernel, and read what it wrote, so they do it with plain
-// loads: a load through the read-only path, which the compiler may move, could pass the wait.  (A token of one context
-// behind its append, in a stream: 9.2 us the pair for 12.3.)
+// The cache's kernels, and the windowed attention's on the tensor cores and in fp32, wait before they read or write anything of a
+// caller's (but the lengths, where a call's second kernel follows its first), and read what the kernel ahead may have written with
+// plain loads: a load through the read-only path, which the compiler may move, could pass the wait.  (A token of one
+// context behind its append, in a stream: 9.2 us the pair for 12.3.)  They trigger at their end: with a trigger after the wait, the
+// next kernel's CTAs took what slots were left on some SMs and came out unevenly (fp32 windowed attention in a stream 39 us for 27,
+// 64 tokens over 128 6.5 for 5.7, a token of 16 layers over 1151 13.4 for 12.8).
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
