@@ -13,10 +13,12 @@
 // over the end of a tile (a window has few chunks, so a tile's first loads and last output would otherwise cost as much as
 // its chunks): the chunks of all tiles of a CTA are one sequence.
 //
-// The softmax does without a maximum for each chunk: the scale of a row is the max of its first chunk with a key that counts,
+// The softmax does without a maximum for each chunk: the scale of a row is the max of its first sixteen keys of which one counts,
 // and floating point does not mind later scores above it.  A row whose sum has passed 2^20 is scaled down before the next chunk;
 // one that overflows within a chunk, by scores 70 above its scale, is computed again at the end like one that met a value
 // that is not finite.
+// At hd 64 the warps' latencies and issue bound it (16 softmax warps an SM: 183 us, 750 TFLOP/s of what the tokens see, at the sizes above,
+// 1080 over all of 8000 tokens), at hd 128 the tensor pipe, 76% active (690 us, 1560 TFLOP/s).
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -140,6 +142,7 @@ struct WinTiles {
     int np, heads, odd;         // pairs of a KV head; KV heads in all; whether the last pair of a head is one tile
     int c, g, r0, t0, t1;       // chain, KV head, first token; positions of its first and last
     int ns, lo, n, wf, wl;      // chunks of the first positions; first position after them; chunks in all; widths of the last ones
+    int wl0;                    // of the last, for the first of two tiles
     bool two;
     __device__ WinTiles(const AttnArgs& a, int C) {
         const int nt = (a.Lq + a.rows - 1) / a.rows, grid = gridDim.x, b = blockIdx.x;
@@ -178,10 +181,11 @@ struct WinTiles {
         const int first_end = t0 - a.window + 1 >= ns * NK ? min(a.n_sink, t1 + 1) : t1 + 1;
         wf = (min(NK, first_end - (ns - 1) * NK) + 15) & ~15;
         wl = n > ns ? (min(NK, t1 + 1 - (lo + (n - 1 - ns) * NK)) + 15) & ~15 : wf;
+        wl0 = two && n > ns ? max(16, (min(NK, t0 + a.rows - (lo + (n - 1 - ns) * NK)) + 15) & ~15) : wl;
     }
     __device__ int at(int j) const { return j < ns ? j * NK : lo + (j - ns) * NK; }
-    // keys of a chunk up to the last that some token sees, in sixteens: what S, the softmax and P V go over
-    __device__ int width(int j) const { return j == n - 1 ? wl : j == ns - 1 ? wf : NK; }
+    // keys of a chunk up to the last that some token of a tile sees, in sixteens: what S, the softmax and P V go over
+    __device__ int width(int j, int x) const { return j == n - 1 ? (x ? wl : wl0) : j == ns - 1 ? wf : NK; }
 };
 
 template <int HD>
@@ -316,7 +320,7 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             ok = win_wait(qfull(i), i / QB & 1, a.status);
             const uint64_t dq = sdesc_step(dq0, i % QB * 2 * SM::Q_TILE);
             for (int j = 0; ok && j < tl.n; ++j) {
-                const uint32_t id_s = idesc_bf16_f32(128, tl.width(j), false, false);
+                const uint32_t id_s = idesc_bf16_f32(128, tl.width(j, x), false, false);
                 const uint64_t dk = sdesc_step(dk0, s * SM::TILE);
                 ok = win_wait(kfull(s), ph, a.status);
                 if (tl.has(x)) {
@@ -351,13 +355,12 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         for (; ok && tl.more(); tl.next()) {
             tl.open(a);
             for (int j = 0; ok && j < tl.n; ++j) {
-                const int wd = tl.width(j);
                 const uint64_t dv = sdesc_step(dv0, s * SM::TILE);
                 ok = win_wait(vfull(s), ph, a.status);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     if (!tl.has(x)) continue;
-                    const int J = chunk[x]++;
+                    const int J = chunk[x]++, wd = tl.width(j, x);
                     const uint32_t t_p = tmem + x * SM::TILE_COLS + J % NB * NK, t_o = tmem + x * SM::TILE_COLS + NB * NK;
                     if (j == 0) ok = ok && win_wait(oempty(x), (count[x]++ & 1) ^ 1, a.status);  // the last tile's O has been read
                     ok = ok && win_wait(pready(x, J), J / NB & 1, a.status);          // P of chunk J is in TMEM
@@ -399,7 +402,7 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             uint64_t l2[2] = {0, 0};
             for (int j = 0; j < tl.n; ++j, ++J) {
                 const uint32_t t_s = t_x + J % NB * NK;
-                const int at = tl.at(j), wd = tl.width(j);
+                const int at = tl.at(j), wd = tl.width(j, x);
                 ok = win_wait(sfull(x, J), J / NB & 1, a.status);
                 if (!ok) break;
                 tc_fence_after();
@@ -425,7 +428,7 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 if (__any_sync(0xffffffffu, m_run == -FLT_MAX)) {
                     float cm = -INFINITY;
 #pragma unroll 1
-                    for (int b = 0; b < NK && b < wd; b += 16) {
+                    for (int b = 0; b < NK && b < wd && __any_sync(0xffffffffu, m_run == -FLT_MAX && cm == -INFINITY); b += 16) {
                         float v[16];
                         tmem_ld16(t_s + b, v);
 #pragma unroll
