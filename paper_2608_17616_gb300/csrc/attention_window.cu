@@ -14,9 +14,9 @@
 // its chunks): the chunks of all tiles of a CTA are one sequence.
 //
 // The softmax does without a maximum for each chunk: the scale of a row is the max of its first sixteen keys of which one counts,
-// and floating point does not mind later scores above it.  A row whose sum has passed 2^20 is scaled down before the next chunk;
-// one that overflows within a chunk, by scores 70 above its scale, is computed again at the end like one that met a value
-// that is not finite.
+// and floating point does not mind later scores above it.  A row whose sum has passed SUM_MOST is scaled down before the next chunk;
+// one that overflows within a chunk, by scores some 46 above all before, is computed again at the end, by its warp, like one that met
+// a value that is not finite.
 // At hd 64 the warps' latencies and issue bound it (16 softmax warps an SM: 183 us, 750 TFLOP/s of what the tokens see, at the sizes above,
 // 1080 over all of 8000 tokens), at hd 128 the tensor pipe, 76% active (690 us, 1560 TFLOP/s).
 #include <algorithm>
@@ -49,6 +49,10 @@ struct WinSmem {
     static constexpr int DYN = SLOT_OFF + 16 + 1024;       // + TMEM slot, + alignment slack
     static_assert(NB * NK + HD <= TILE_COLS && CTAS * TMEM <= 512 && CTAS * (DYN + 1024) <= 228 * 1024, "CTAs an SM");
 };
+
+// A row's sum is scaled down when it has passed this: far enough above 1 to be rare (with 2^20, scores of standard deviation 4 took
+// 904 us for 658 at 16001 tokens, window 4096, hd 128), far enough below FLT_MAX that a chunk seldom gets from there to it
+constexpr float SUM_MOST = 0x1p60f;
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
@@ -123,6 +127,40 @@ __device__ __forceinline__ bool win_wait(uint32_t bar, uint32_t parity, int* sta
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, status));
 }
 
+
+// row_again by a warp, which has HD / 32 dimensions a lane: a row of 4096 keys takes some 0.1 ms
+template <int HD>
+__device__ __noinline__ void row_by_warp(const bf16* q, const bf16* K, const bf16* V, int vis, const AttnArgs& a, bf16* out) {
+    constexpr int D = HD / 32;
+    const int d0 = D * (threadIdx.x & 31);
+    float qf[D], o[D] = {}, m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int d = 0; d < D; ++d) qf[d] = __bfloat162float(q[d0 + d]) * a.scale;
+    auto keys = [&](int j0, int j1) {
+#pragma unroll 4
+        for (int j = j0; j < j1; ++j) {
+            float z = 0.f, v[D];
+#pragma unroll
+            for (int d = 0; d < D; ++d) {
+                z = fmaf(qf[d], __bfloat162float(K[(long long)j * a.s3 + d0 + d]), z);
+                v[d] = __bfloat162float(V[(long long)j * a.s3 + d0 + d]);
+            }
+            z = warp_sum(z);
+            if (z == -INFINITY) continue;
+            const float mn = fmaxf(m, z), corr = __expf(m - mn), p = __expf(z - mn);
+            m = mn;
+            l = fmaf(l, corr, p);
+#pragma unroll
+            for (int d = 0; d < D; ++d) o[d] = fmaf(o[d], corr, p * v[d]);
+        }
+    };
+    const int first = min(a.n_sink, vis);
+    keys(0, first);
+    keys(max(first, vis - a.window), vis);
+    const float inv = l > 0.f ? 1.f / l : l;
+#pragma unroll
+    for (int d = 0; d < D; ++d) out[d0 + d] = __float2bfloat16_rn(o[d] * inv);
+}
 
 // The lowest n bits (n <= 0: none; n >= 32: all)
 __device__ __forceinline__ uint32_t low_bits(int n) {
@@ -435,12 +473,12 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                         for (int u = 0; u < 16; u += 2) cm = max3(cm, v[u], v[u + 1]);
                     }
                     if (m_run == -FLT_MAX) m_run = fmaxf(cm, -FLT_MAX);  // sums and O are 0 so far
-                } else if (__any_sync(0xffffffffu, sum_f32x4(l2) > 0x1p20f)) {
+                } else if (__any_sync(0xffffffffu, sum_f32x4(l2) > SUM_MOST)) {
                     const float l = sum_f32x4(l2);
                     ok = win_wait(odone(x, J - 1), (J - 1) / NB & 1, a.status);  // O up to the last chunk
                     if (!ok) break;
                     tc_fence_after();
-                    const int e = l > 0x1p20f && l <= FLT_MAX ? ilogbf(l) : 0;  // by a power of two
+                    const int e = l > SUM_MOST && l <= FLT_MAX ? ilogbf(l) : 0;  // by a power of two
                     const float corr = ldexpf(1.f, -e);
                     m_run += e / k2;
                     l2[0] = mul_f32x2(l2[0], pack_f32x2(corr, corr));
@@ -496,7 +534,8 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             ok = win_wait(odone(x, J - 1), (J - 1) / NB & 1, a.status);
             if (!ok) break;
             tc_fence_after();
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no key that counts: 0
+            // no key that counts: 0; a sum that has overflowed: NaN, and the row again
+            const float inv = sum == 0.f ? 0.f : sum <= FLT_MAX ? 1.f / sum : NAN;
             const size_t at = (((size_t)c * a.n_q + g * a.group + (live ? hr : 0)) * a.Lq + (live ? tok : 0)) * HD;
             bf16* orow = static_cast<bf16*>(a.out) + at;
             float top = 0.f;  // of the row's magnitudes, NaN if one is
@@ -521,15 +560,12 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(oempty(x));
-            if (live && !(top <= FLT_MAX)) {
-                const long long kv_off = (long long)(c / a.L) * a.s0 + (long long)(c % a.L) * a.s1 + (long long)g * a.s2;
-#pragma unroll 1
-                for (int cb = 0; cb < HD; cb += 32) {
-                    float w[32];
-                    row_again<bf16, HD, 32, 1>(static_cast<const bf16*>(a.Q) + at, static_cast<const bf16*>(a.K) + kv_off,
-                                               static_cast<const bf16*>(a.V) + kv_off, a.s3, vis, a, cb, w);
-                    for (int u = 0; u < 32; ++u) orow[cb + u] = __float2bfloat16_rn(w[u]);
-                }
+            const long long kv_off = (long long)(c / a.L) * a.s0 + (long long)(c % a.L) * a.s1 + (long long)g * a.s2;
+            for (uint32_t bad = __ballot_sync(0xffffffffu, live && !(top <= FLT_MAX)); bad; bad &= bad - 1) {
+                const int src = __ffs(bad) - 1;
+                const size_t of = __shfl_sync(0xffffffffu, at, src);
+                row_by_warp<HD>(static_cast<const bf16*>(a.Q) + of, static_cast<const bf16*>(a.K) + kv_off, static_cast<const bf16*>(a.V) + kv_off,
+                                __shfl_sync(0xffffffffu, vis, src), a, static_cast<bf16*>(a.out) + of);
             }
             __syncwarp();
         }

@@ -118,6 +118,27 @@ def test_the_row_max_grows_late():
     case(2, 140, 200, 16, 250, hd=128, n_layers=20, late=9.0)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("top,size", [(88.5, 1.0), (88.5, 2.0 ** -10), (60.0, 1.0), (200.0, 1.0)])
+def test_scores_far_above_the_first_keys(hd, top, size):
+    """Two keys in the middle whose exponentials, against the first keys', add up past 32 bits, or are past them."""
+    L, group, Lq, n_past = 20, 4, 150, 300
+    run = handle(L, 2, hd, torch.bfloat16)
+    g = torch.Generator(device="cuda").manual_seed(hd)
+    rn = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    K, V, Q = rn(1, L, 2, n_past + Lq, hd), size * rn(1, L, 2, n_past + Lq, hd), rn(1, L, 2 * group, Lq, hd)
+    Q[..., 0], K[..., 0] = hd ** 0.5 if hd == 64 else 11.3125, 0
+    Q[..., 1:] *= 0.5
+    K[..., 200, 0] = K[..., 203, 0] = top
+    out = torch.full_like(Q, 7.0)
+    mone.mone_window_attention(run.h, -1, Q, 2 * group, Lq, K, V, K.stride()[:4], n_past, 16, ALL, out)
+    mone.mone_mem_sync(run.h)
+    run.close()
+    for layer in (0, L - 1):
+        ref, _ = O.window_attention(Q[0, layer].float().cpu(), K[0, layer].float().cpu(), V[0, layer].float().cpu(), n_past, 16, ALL)
+        assert rel_fro(out[0, layer].float().cpu(), ref) <= 5e-3
+
+
 @pytest.mark.parametrize("layer", [0, 7, 19])
 def test_one_layer_of_a_cache(layer):
     case(4, 400, 70, 64, 40, n_layers=20, layer=layer, n_ctx=3)
