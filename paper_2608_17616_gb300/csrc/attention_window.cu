@@ -128,30 +128,48 @@ __device__ __forceinline__ bool win_wait(uint32_t bar, uint32_t parity, int* sta
 }
 
 
-// row_again by a warp, which has HD / 32 dimensions a lane: a row of 4096 keys takes some 0.1 ms
+// row_again by a warp, which has HD / 32 dimensions a lane; eight keys' loads under way
 template <int HD>
 __device__ __noinline__ void row_by_warp(const bf16* q, const bf16* K, const bf16* V, int vis, const AttnArgs& a, bf16* out) {
-    constexpr int D = HD / 32;
+    constexpr int D = HD / 32, U = 8;
     const int d0 = D * (threadIdx.x & 31);
     float qf[D], o[D] = {}, m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int d = 0; d < D; ++d) qf[d] = __bfloat162float(q[d0 + d]) * a.scale;
     auto keys = [&](int j0, int j1) {
-#pragma unroll 4
-        for (int j = j0; j < j1; ++j) {
-            float z = 0.f, v[D];
+        for (int j = j0; j < j1; j += U) {
+            bf16 k[U][D], v[U][D];
 #pragma unroll
-            for (int d = 0; d < D; ++d) {
-                z = fmaf(qf[d], __bfloat162float(K[(long long)j * a.s3 + d0 + d]), z);
-                v[d] = __bfloat162float(V[(long long)j * a.s3 + d0 + d]);
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int d = 0; d < D; ++d) {
+                    const long long at = (long long)min(j + u, j1 - 1) * a.s3 + d0 + d;
+                    k[u][d] = K[at];
+                    v[u][d] = V[at];
+                }
+            float z[U], mn = m;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float x = 0.f;
+#pragma unroll
+                for (int d = 0; d < D; ++d) x = fmaf(qf[d], __bfloat162float(k[u][d]), x);
+                z[u] = warp_sum(x);
+                if (j + u >= j1) z[u] = -INFINITY;
+                mn = fmaxf(mn, z[u]);
             }
-            z = warp_sum(z);
-            if (z == -INFINITY) continue;
-            const float mn = fmaxf(m, z), corr = __expf(m - mn), p = __expf(z - mn);
+            const float corr = m == mn ? 1.f : __expf(m - mn);
             m = mn;
-            l = fmaf(l, corr, p);
+            l *= corr;
 #pragma unroll
-            for (int d = 0; d < D; ++d) o[d] = fmaf(o[d], corr, p * v[d]);
+            for (int d = 0; d < D; ++d) o[d] *= corr;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (z[u] == -INFINITY) continue;
+                const float p = __expf(z[u] - mn);
+                l += p;
+#pragma unroll
+                for (int d = 0; d < D; ++d) o[d] = fmaf(p, __bfloat162float(v[u][d]), o[d]);
+            }
         }
     };
     const int first = min(a.n_sink, vis);
