@@ -18,7 +18,7 @@
 // one that overflows within a chunk, by scores some 46 above all before, is computed again at the end, by its warp, like one that met
 // a value that is not finite.
 // At hd 64 the warps' latencies and issue bound it (16 softmax warps an SM: 183 us, 750 TFLOP/s of what the tokens see, at the sizes above,
-// 1080 over all of 8000 tokens), at hd 128 the tensor pipe, 76% active (690 us, 1560 TFLOP/s).
+// 1080 over all of 8000 tokens), at hd 128 the tensor pipe, 75% active (655 us, 1640 TFLOP/s; 710, 1510, at the power cap).
 #include <algorithm>
 #include <cfloat>
 #include <climits>

@@ -1165,7 +1165,8 @@ template <int HD>
 cudaError_t launch_bf16(const CaArgs& a, int sms, int* kernels, cudaStream_t st) {
     CUtensorMap mk = {}, mv = {};
     // pages of fewer than 8 positions would need copies of less than a swizzle's rows
-    if (a.vec && a.v.page_log2 >= 3 && pool_maps<HD>(a.v, &mk, &mv)) return a.R <= 8 ? launch<CaTensor<HD, 1>>(a, mk, mv, sms, kernels, st) : launch<CaTensor<HD, 2>>(a, mk, mv, sms, kernels, st);
+    if (a.vec && a.v.page_log2 >= 3 && pool_maps<HD>(a.v, &mk, &mv))
+        return a.R <= 8 ? launch<CaTensor<HD, 1>>(a, mk, mv, sms, kernels, st) : launch<CaTensor<HD, 2>>(a, mk, mv, sms, kernels, st);
     return launch<CaCores<bf16, HD>>(a, mk, mv, sms, kernels, st);
 }
 
