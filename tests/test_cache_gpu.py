@@ -464,6 +464,44 @@ def test_calls_in_a_row_read_what_the_kernels_ahead_wrote(hd, dtype):
         assert all(torch.equal(a, b) for a, b in zip(results[0], other))
 
 
+@pytest.mark.parametrize("hd,spare", [(64, 4), (128, 4), (64, 1024)])
+def test_a_captured_step_serves_growing_contexts(hd, spare):
+    """A graph of append and attention, replayed, gives the bits of the calls; lengths grow over pages' ends in device memory."""
+    n_kv, group, steps = 2, 4, 40
+    results = []
+    for graph in (False, True):
+        x = Cache([30, 0, 500], n_kv=n_kv, hd=hd, page=16, spare=spare, seed=3)
+        B, L = len(x.lens), x.L
+        g = torch.Generator(device="cuda").manual_seed(4)
+        Q, K, V = (torch.randn(steps, B, L, n, 1, hd, generator=g, device="cuda").bfloat16() for n in (group * n_kv, n_kv, n_kv))
+        q, k, v = Q[0].clone(), K[0].clone(), V[0].clone()
+        out, longer, got = torch.zeros_like(q), torch.zeros_like(x.len_t), []
+        x.tbl.copy_(x.table)
+
+        def step():
+            mone.mone_cache_append(x.h, -1, x.c, k, v, k.stride()[:4], 1, longer)
+            x.len_t.copy_(longer)
+            mone.mone_cache_attention(x.h, -1, x.c, q, group * n_kv, 1, 2, 200, out)
+
+        lens, score = x.len_t.clone(), x.score.clone()
+        step()  # the workspace, before a capture
+        x.len_t.copy_(lens)
+        x.score.copy_(score)
+        torch.cuda.synchronize()
+        if graph:
+            G = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(G):
+                step()
+        for i in range(steps):
+            q.copy_(Q[i]), k.copy_(K[i]), v.copy_(V[i])
+            G.replay() if graph else step()
+            got.append(out.clone())
+        x.done()
+        assert x.len_t.tolist() == [n + steps for n in x.lens]
+        results.append(got + [x.score.clone()])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
 def test_on_another_stream():
     x = Cache([900, 40])
     s = torch.cuda.Stream()
