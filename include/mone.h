@@ -376,7 +376,7 @@ mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache
  * 0, 1, .. of the pages of to_table, with their scores; what they leave stays as it is, so pages that contexts share may
  * be evicted from, and the caller gives the old ones back when every layer is done.
  *   to_table  [n_ctx][to_width] pages of the same pools (device), to_width * page_size >= keep; they may hold
- *             nothing that the call reads
+ *             nothing that the call reads; a context's entries past its survivors are not read
  *   to_score  [n_ctx][n_layers][n_kv_heads][to_width * page_size]; entries past the survivors keep what they hold
  *   kept      [n_ctx][n_layers][n_kv_heads][keep] int32: the survivors' old positions, then -1
  *   lens_out  NULL, or [n_ctx] (device, not lens itself): min(lens, keep)

@@ -319,8 +319,8 @@ __global__ void __launch_bounds__(CP_THREADS) cache_compact_kernel(const EvictAr
     const int i = i0 + lane;
     if (lane < CM_SLOTS && i < a.keep) {
         const int mask = (1 << a.v.page_log2) - 1, from = a.kept[((size_t)chain * a.v.n_kv + g) * a.keep + i];
-        const int p1 = cache_page(a.v, a.to + (size_t)c * a.to_width, i >> a.v.page_log2);
-        if (from >= 0) {
+        if (from >= 0) {  // (past the survivors, an entry of the target's table need not name a page)
+            const int p1 = cache_page(a.v, a.to + (size_t)c * a.to_width, i >> a.v.page_log2);
             const size_t row = ((size_t)c * a.v.Lh + l) * a.v.n_kv + g;
             const int p0 = cache_page(a.v, a.v.table + (size_t)c * a.v.width, from >> a.v.page_log2);
             a.to_score[row * a.to_cap + i] = a.v.score[row * a.v.cap + from];

@@ -384,6 +384,14 @@ def test_evict_one_layer():
     evict(Cache([300, 90], n_layers=3), 80, 4, 8, layer=1)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_evict_reads_the_target_pages_of_survivors_only(dtype):
+    """Contexts that hold fewer positions than are kept have target pages for what they hold; the entries past them name no page."""
+    x = Cache([300, 20, 0, 90, 80, 81], dtype=dtype)
+    x.trim(x.fresh, [min(n, 80) for n in x.lens])
+    evict(x, 80, 4, 8)
+
+
 # ----------------------------------------------------------------- together, as a serving program uses them
 
 def test_append_attend_evict_attend():
