@@ -392,6 +392,35 @@ def test_evict_reads_the_target_pages_of_survivors_only(dtype):
     evict(x, 80, 4, 8)
 
 
+@pytest.mark.parametrize("lens,n_layers,n_kv,keep", [
+    ([16385, 20001, 40000], 14, 4, 9001),     # more rows than the SMs hold twice: a CTA has a row, past what it keeps on chip
+    ([140001, 131080], 1, 1, 50000),          # eight CTAs a row, whose slices are longer than that too
+])
+@pytest.mark.parametrize("levels", [None, 7])  # scores that differ, and ties at every value
+def test_evict_from_slices_longer_than_a_cta_holds(lens, n_layers, n_kv, keep, levels):
+    n_sink, n_recent, page, B = 5, 300, 64, len(lens)
+    x = Cache(lens, n_layers=n_layers, n_kv=n_kv, page=page, seed=7)
+    if levels:
+        x.score.mul_(levels).floor_()
+    n_to = -(-keep // page)
+    to = x.fresh[:, :n_to].contiguous()
+    to_score = torch.zeros(B, n_layers, n_kv, n_to * page, device="cuda")
+    kept = torch.full((B, n_layers, n_kv, keep), -9, dtype=torch.int32, device="cuda")
+    mone.mone_cache_evict(x.h, -1, x.c, keep, n_sink, n_recent, to, to_score, kept)
+    x.done()
+    for c, n in enumerate(lens):
+        score = x.score[c, :, :, :n].cpu()
+        newK = x.held(x.K, c, keep, to)
+        for l in range(n_layers):
+            for g in range(n_kv):
+                mid = score[l, g, n_sink:n - n_recent]
+                best = torch.sort(mid, descending=True, stable=True).indices[:keep - n_sink - n_recent]  # ties by position
+                at = torch.cat([torch.arange(n_sink), n_sink + best.sort().values, torch.arange(n - n_recent, n)])
+                assert torch.equal(kept[c, l, g].cpu().long(), at), (c, l, g)
+                assert torch.equal(to_score[c, l, g, :keep].cpu(), score[l, g, at])
+                assert torch.equal(newK[l, g], x.k[c][l, g, at.cuda()])
+
+
 # ----------------------------------------------------------------- together, as a serving program uses them
 
 def test_append_attend_evict_attend():
