@@ -362,8 +362,9 @@ mone_status mone_cache_append(mone_mem* m, int layer, const mone_cache* cache, c
  * KV heads x contexts x layers of the call x ceil(n_tok n_q_heads / (4 n_kv_heads)) x blocks of 32 positions that a
  * table covers below 2^30.
  * The handle keeps a workspace that grows with the call's sizes (with scores, 4 bytes for every query row and position that
- * a table covers; growing synchronises the stream, so a call of the largest size comes before any capture); calls of one
- * handle that overlap on two streams share it: order them.
+ * a table covers).  Growing synchronises the stream and is refused (OOM) while it is captured: a call of the largest size
+ * comes before a capture.  A workspace that a capture has seen stays until mone_mem_free, so graphs can be replayed after
+ * larger calls.  Calls and replays of one handle that overlap on two streams share a workspace: order them.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (page_size), OOM, CUDA.
  */
 mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache, const void* Q, int n_q_heads, int n_tok,

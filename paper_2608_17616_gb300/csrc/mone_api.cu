@@ -94,6 +94,12 @@ struct ReadGraph {
     long long strides[4] = {0, 0, 0, 0};
 };
 
+// A workspace that has been outgrown and that a captured graph may still use
+struct Outgrown {
+    void* p;
+    Outgrown* next;
+};
+
 struct mone_mem {
     mone_config cfg;
     DevState s;
@@ -112,9 +118,11 @@ struct mone_mem {
     size_t hwin_bytes;
     cudaStream_t hstream;
     cudaEvent_t hstart, hstaged[2], hfree[2];
-    // workspace of mone_cache_attention, grown on demand
+    // workspace of mone_cache_attention, grown on demand; whether a capture has seen it; those that captures have seen before
     void* cws;
     size_t cws_bytes;
+    bool cws_captured;
+    Outgrown* cws_old;
 };
 
 namespace {
@@ -222,6 +230,11 @@ void destroy_streams(mone_mem* m) {
     if (m->cws) cudaFree(m->cws);
     m->cws = nullptr;
     m->cws_bytes = 0;
+    while (Outgrown* o = m->cws_old) {
+        m->cws_old = o->next;
+        cudaFree(o->p);
+        delete o;
+    }
     if (m->rg) {
         if (m->rg->exec) cudaGraphExecDestroy(m->rg->exec);
         delete m->rg;
@@ -1093,9 +1106,31 @@ mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const size_t need = cache_attention_workspace(s, v, n_q_heads, n_tok);
     if (need == 0) return MONE_ERR_UNSUPPORTED_SHAPE;
-    if (need > m->cws_bytes) {
-        MONE_CUDA(cudaStreamSynchronize(st));
-        if (m->cws) cudaFree(m->cws);
+    const bool grow = need > m->cws_bytes;
+    if (grow || !m->cws_captured) {
+        cudaStreamCaptureStatus capture;
+        MONE_CUDA(cudaStreamIsCapturing(st, &capture));
+        if (capture != cudaStreamCaptureStatusNone) {
+            if (grow) {
+                std::snprintf(g_last_error, sizeof(g_last_error),
+                              "mone_cache_attention: a workspace of %zu bytes cannot be made during a capture; make a call of "
+                              "this size before it",
+                              need);
+                return MONE_ERR_OOM;
+            }
+            m->cws_captured = true;
+        }
+    }
+    if (grow) {
+        if (m->cws && m->cws_captured) {  // its address is in a graph, which may be replayed until the handle is freed
+            Outgrown* o = new (std::nothrow) Outgrown{m->cws, m->cws_old};
+            if (!o) return MONE_ERR_OOM;
+            m->cws_old = o;
+            m->cws_captured = false;
+        } else if (m->cws) {
+            MONE_CUDA(cudaStreamSynchronize(st));
+            cudaFree(m->cws);
+        }
         m->cws = nullptr;
         m->cws_bytes = 0;
         char* p = nullptr;

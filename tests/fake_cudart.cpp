@@ -19,6 +19,8 @@ std::map<const void*, std::string> g_names;
 std::map<std::pair<int, const void*>, int> g_smem;
 std::string g_log;
 int g_fail_opt_ins = 0;
+int g_capturing = 0;  // of every stream
+std::string g_frees;
 uintptr_t g_next = 1ull << 40;
 thread_local struct { dim3 grid, block; size_t smem; cudaStream_t st; } g_cfg;
 
@@ -65,6 +67,9 @@ void fake_set_device(int d) { g_dev = d; }
 void fake_fail_opt_ins(int n) { g_fail_opt_ins = n; }  // the next n opt-ins fail
 const char* fake_log() { return g_log.c_str(); }
 void fake_clear() { g_log.clear(); }
+void fake_set_capturing(int on) { g_capturing = on; }
+const char* fake_frees() { return g_frees.c_str(); }  // sizes freed and waits for a stream since the last call of fake_clear_frees
+void fake_clear_frees() { g_frees.clear(); }
 
 void** __cudaRegisterFatBinary(void*) { static void* h; return &h; }
 void __cudaRegisterFatBinaryEnd(void**) {}
@@ -105,8 +110,9 @@ cudaError_t cudaOccupancyMaxActiveClusters(int* n, const void*, const cudaLaunch
         if (c->attrs[i].id == cudaLaunchAttributeClusterDimension) *n = kSms[g_dev] / (int)c->attrs[i].val.clusterDim.x;
     return cudaSuccess;
 }
-cudaError_t cudaMalloc(void** p, size_t n) { *p = (void*)g_next; g_next += (n + 255) / 256 * 256; return cudaSuccess; }
-cudaError_t cudaFree(void*) { return cudaSuccess; }
+std::map<void*, size_t> g_sizes;
+cudaError_t cudaMalloc(void** p, size_t n) { *p = (void*)g_next; g_next += (n + 255) / 256 * 256; g_sizes[*p] = n; return cudaSuccess; }
+cudaError_t cudaFree(void* p) { if (p) g_frees += std::to_string(g_sizes.at(p)) + "\n"; return cudaSuccess; }
 cudaError_t cudaMemcpy(void* d, const void*, size_t n, cudaMemcpyKind k) { if (k == cudaMemcpyDeviceToHost) std::memset(d, 0, n); return cudaSuccess; }
 cudaError_t cudaMemcpyAsync(void* d, const void* s, size_t n, cudaMemcpyKind k, cudaStream_t) { return cudaMemcpy(d, s, n, k); }
 cudaError_t cudaMemset(void*, int, size_t) { return cudaSuccess; }
@@ -124,7 +130,11 @@ cudaError_t cudaPointerGetAttributes(cudaPointerAttributes* a, const void* p) { 
 const char* cudaGetErrorName(cudaError_t) { return "fake"; }
 const char* cudaGetErrorString(cudaError_t) { return "fake"; }
 cudaError_t cudaDeviceSynchronize() { return cudaSuccess; }
-cudaError_t cudaStreamSynchronize(cudaStream_t) { return cudaSuccess; }
+cudaError_t cudaStreamSynchronize(cudaStream_t) { g_frees += "wait\n"; return cudaSuccess; }
+cudaError_t cudaStreamIsCapturing(cudaStream_t, cudaStreamCaptureStatus* s) {
+    *s = g_capturing ? cudaStreamCaptureStatusActive : cudaStreamCaptureStatusNone;
+    return cudaSuccess;
+}
 cudaError_t cudaStreamCreateWithFlags(cudaStream_t* s, unsigned) { *s = (cudaStream_t)(g_next += 16); return cudaSuccess; }
 cudaError_t cudaStreamDestroy(cudaStream_t) { return cudaSuccess; }
 cudaError_t cudaStreamWaitEvent(cudaStream_t, cudaEvent_t, unsigned) { return cudaSuccess; }

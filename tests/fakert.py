@@ -15,13 +15,22 @@ class Fake:
     def __init__(self, path):
         self.path = path
         self.raw = ctypes.CDLL(path)
-        self.raw.fake_log.restype = ctypes.c_char_p
+        self.raw.fake_log.restype = self.raw.fake_frees.restype = ctypes.c_char_p
 
     def device(self, d):
         self.raw.fake_set_device(d)
 
     def fail_opt_ins(self, n):
         self.raw.fake_fail_opt_ins(n)
+
+    def capturing(self, on):
+        self.raw.fake_set_capturing(int(on))
+
+    def frees(self):
+        """Sizes freed since the last call, and "wait" for each wait for a stream."""
+        out = [f if f == "wait" else int(f) for f in self.raw.fake_frees().decode().split()]
+        self.raw.fake_clear_frees()
+        return out
 
     def drain(self):
         """The log since the last call: launches as dicts, tensor maps as (base, [(dim, stride, box), ..]) each time their

@@ -204,6 +204,54 @@ def test_launch_counts_are_the_kernels_launched(fake):
         n0 = n
 
 
+def attend(h, n_tok, layer=0, score=P):
+    c = cache(score=score)
+    mone.mone_cache_attention(h, layer, c, P, 4, n_tok, 1, 100, P, stream=0)
+
+
+def test_a_workspace_that_a_capture_has_seen_outlives_larger_calls(fake):
+    h = init()
+    fake.frees()
+    attend(h, 1)
+    assert fake.frees() == []
+    attend(h, 2)  # no graph can hold the first
+    first, = [f for f in fake.frees() if f != "wait"]
+    fake.capturing(True)
+    attend(h, 2)
+    attend(h, 1)
+    fake.capturing(False)
+    attend(h, 8)  # a graph holds the last one: it stays
+    assert fake.frees() == []
+    attend(h, 8, layer=-1)  # no graph holds this one
+    grown, = [f for f in fake.frees() if f != "wait"]
+    assert grown > first
+    fake.capturing(True)
+    attend(h, 8, layer=-1)
+    fake.capturing(False)
+    attend(h, 16, layer=-1)
+    assert fake.frees() == []
+    mone.mone_mem_free(h)
+    last = [f for f in fake.frees() if f != "wait"]
+    assert first not in last and grown not in last
+    assert sum(f > grown for f in last) == 2 and sum(first < f < grown for f in last) == 1  # the two that graphs held, and the newest
+
+
+def test_a_workspace_does_not_grow_during_a_capture(fake):
+    h = init()
+    attend(h, 1)
+    fake.frees()
+    n0 = mone.mone_mem_launch_count(h)
+    fake.capturing(True)
+    with pytest.raises(mone.MoneError) as e:
+        attend(h, 16, layer=-1)
+    assert e.value.code == 3 and "capture" in str(e.value)
+    assert fake.frees() == [] and mone.mone_mem_launch_count(h) == n0
+    attend(h, 1)  # what fits goes on
+    fake.capturing(False)
+    attend(h, 16, layer=-1)
+    mone.mone_mem_free(h)
+
+
 def test_make_cache_takes_the_tensors_strides():
     import torch
     K, V = torch.zeros(2, 3, 16, 4, 64).transpose(2, 3), torch.zeros(2, 3, 16, 4, 64).transpose(2, 3)

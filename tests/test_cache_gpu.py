@@ -539,6 +539,32 @@ def test_a_captured_step_serves_growing_contexts(hd, spare):
     assert all(torch.equal(a, b) for a, b in zip(*results))
 
 
+def test_a_graph_is_replayed_after_larger_calls():
+    """The workspace that a graph holds stays when the handle's grows, which it does not during a capture."""
+    x = Cache([300, 40], spare=40, seed=6)
+    n_kv, group = x.n_kv, 4
+    rn = lambda n_tok: torch.randn(2, 2, group * n_kv, n_tok, 64, generator=x.g, device="cuda").bfloat16()  # noqa: E731
+    q, big = rn(1), rn(16)
+    out, want, score = torch.empty_like(q), torch.empty_like(q), x.score.clone()
+    mone.mone_cache_attention(x.h, -1, x.c, q, group * n_kv, 1, 2, 100, want)
+    want_score = x.score.clone()
+    torch.cuda.synchronize()
+    G = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(G):
+        with pytest.raises(mone.MoneError) as e:
+            mone.mone_cache_attention(x.h, -1, x.c, big, group * n_kv, 16, 2, 100, torch.empty_like(big))
+        mone.mone_cache_attention(x.h, -1, x.c, q, group * n_kv, 1, 2, 100, out)
+    assert e.value.code == 3 and "capture" in str(e.value)
+    mone.mone_cache_attention(x.h, -1, x.c, big, group * n_kv, 16, 2, 100, torch.empty_like(big))
+    junk = [torch.full((1 << 22,), float("nan"), device="cuda") for _ in range(8)]  # what would lie where the old one was
+    for _ in range(3):
+        x.score.copy_(score)
+        out.zero_()
+        G.replay()
+    x.done()
+    assert torch.equal(out, want) and torch.equal(x.score, want_score) and all(j.isnan().all() for j in junk)
+
+
 def test_on_another_stream():
     x = Cache([900, 40])
     s = torch.cuda.Stream()
