@@ -454,7 +454,9 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             const int tok = tl.r0 + x * rt + row - hr * rt;
             const bool live = hr < a.group && tok < a.Lq;
             const int vis = live ? a.n_mem + tok + 1 : first;         // the row sees keys before it (a row of padding: any)
-            float m_run = -FLT_MAX;  // the row's scale; that: no key counted so far
+            // The row's scale; -FLT_MAX: no key counted so far.  A row of padding holds whatever shared memory did (a group that does
+            // not divide 128): its sum stays 0 or becomes NaN, and it has no say in the votes below
+            float m_run = live ? -FLT_MAX : INFINITY;
             uint64_t l2[2] = {0, 0};
             for (int j = 0; j < tl.n; ++j, ++J) {
                 const uint32_t t_s = t_x + J % NB * NK;

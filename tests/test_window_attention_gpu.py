@@ -264,3 +264,33 @@ def test_offsets_past_32_bits(Lq, dtype):
     for layer in (0, L - 1):
         ref, _ = O.window_attention(Q[0, layer].float().cpu(), K[0, layer].float().cpu(), V[0, layer].float().cpu(), n_past, 10, 490)
         assert rel_fro(out[0, layer].float().cpu(), ref) <= TOL[dtype], layer
+
+
+# ----------------------------------------------------------------- what rows of padding, equal values and long recomputations show
+
+@pytest.mark.parametrize("group,hd", [(7, 64), (7, 128), (3, 64), (5, 128)])
+def test_rows_of_padding_have_no_say(group, hd):
+    """A group that does not divide the tile's 128 rows leaves some that no copy fills: what a kernel before left in shared memory
+    there changes no bit.  Scores grow by half a unit a position, so that every row is rescaled several times."""
+    n_kv, L, n_past, Lq = 2, 20, 300, 150
+    runs = handle(L, n_kv, hd, torch.bfloat16)
+    g = torch.Generator(device="cuda").manual_seed(group)
+    rn = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    K, V, Q = rn(1, L, n_kv, n_past + Lq, hd), rn(1, L, n_kv, n_past + Lq, hd), rn(1, L, group * n_kv, Lq, hd)
+    Q[..., 0] = hd ** 0.5 if hd == 64 else 11.3125
+    K[..., 0] = torch.arange(n_past + Lq, device="cuda") * 0.5
+    K2, V2 = rn(1, L, n_kv, 2000, hd), rn(1, L, n_kv, 2000, hd)
+    outs = []
+    for left in (0.0, float("nan"), 1e30, float("inf")):  # queries of a call that fills all rows of every tile
+        q2 = torch.full((1, L, 4 * n_kv, 2000, hd), left, dtype=torch.bfloat16, device="cuda")
+        mone.mone_window_attention(runs.h, -1, q2, 4 * n_kv, 2000, K2, V2, K2.stride()[:4], 0, 0, 64, torch.empty_like(q2))
+        torch.cuda.synchronize()
+        out = torch.full_like(Q, 7.0)
+        mone.mone_window_attention(runs.h, -1, Q, group * n_kv, Lq, K, V, K.stride()[:4], n_past, 16, ALL, out)
+        outs.append(out)
+    mone.mone_mem_sync(runs.h)
+    runs.close()
+    ref, _ = O.window_attention(Q[0, 3].float().cpu(), K[0, 3].float().cpu(), V[0, 3].float().cpu(), n_past, 16, ALL)
+    assert rel_fro(outs[0][0, 3].float().cpu(), ref) <= 5e-3
+    for out in outs[1:]:
+        assert torch.equal(outs[0], out)
