@@ -487,13 +487,16 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                     float cm = -INFINITY;
 #pragma unroll 1
                     for (int b = 0; b < NK && b < wd && __any_sync(0xffffffffu, m_run == -FLT_MAX && cm == -INFINITY); b += 16) {
-                        float v[16];
+                        float v[16], c16 = -INFINITY;
                         tmem_ld16(t_s + b, v);
 #pragma unroll
-                        for (int u = 0; u < 16; u += 2) cm = max3(cm, v[u], v[u + 1]);
+                        for (int u = 0; u < 16; u += 2) c16 = max3(c16, v[u], v[u + 1]);
+                        if (cm == -INFINITY) cm = c16;  // (others may look on: a row's scale is its own)
                     }
                     if (m_run == -FLT_MAX) m_run = fmaxf(cm, -FLT_MAX);  // sums and O are 0 so far
-                } else if (__any_sync(0xffffffffu, sum_f32x4(l2) > SUM_MOST)) {
+                }
+                // (whether or not a row has no scale yet: one whose scores are all NaN never gets one)
+                if (__any_sync(0xffffffffu, sum_f32x4(l2) > SUM_MOST)) {
                     const float l = sum_f32x4(l2);
                     ok = win_wait(odone(x, J - 1), (J - 1) / NB & 1, a.status);  // O up to the last chunk
                     if (!ok) break;

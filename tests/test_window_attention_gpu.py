@@ -294,3 +294,24 @@ def test_rows_of_padding_have_no_say(group, hd):
     assert rel_fro(outs[0][0, 3].float().cpu(), ref) <= 5e-3
     for out in outs[1:]:
         assert torch.equal(outs[0], out)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_a_token_that_is_not_a_number_leaves_the_others_as_they_are(hd):
+    """Its row shares a warp with other tokens', which are rescaled, as above, whatever it holds: not a bit of theirs changes."""
+    n_kv, group, L, n_past, Lq = 2, 4, 20, 300, 150
+    run = handle(L, n_kv, hd, torch.bfloat16)
+    g = torch.Generator(device="cuda").manual_seed(hd)
+    rn = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    K, V, Q = rn(1, L, n_kv, n_past + Lq, hd), rn(1, L, n_kv, n_past + Lq, hd), rn(1, L, group * n_kv, Lq, hd)
+    Q[..., 0] = hd ** 0.5 if hd == 64 else 11.3125
+    K[..., 0] = torch.arange(n_past + Lq, device="cuda") * 0.5
+    outs = [torch.full_like(Q, 7.0) for _ in range(2)]
+    for out in outs:
+        mone.mone_window_attention(run.h, -1, Q, group * n_kv, Lq, K, V, K.stride()[:4], n_past, 16, ALL, out)
+        Q[..., 40, :] = float("nan")
+    mone.mone_mem_sync(run.h)
+    run.close()
+    assert outs[1][..., 40, :].isnan().all()
+    outs[1][..., 40, :] = outs[0][..., 40, :]
+    assert torch.equal(*outs)
