@@ -67,6 +67,16 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
     return d;
 }
 
+// The two bf16 of p to the two sums of l, in 32 bits
+__device__ __forceinline__ void add_bf16x2(uint64_t& l, uint32_t p) {
+    asm("{\n\t.reg .b16 lo, hi;\n\t.reg .f32 a, b;\n\t"
+        "mov.b32 {lo, hi}, %1;\n\tmov.b64 {a, b}, %0;\n\t"
+        "add.f32.bf16 a, lo, a;\n\tadd.f32.bf16 b, hi, b;\n\t"
+        "mov.b64 %0, {a, b};\n\t}"
+        : "+l"(l)
+        : "r"(p));
+}
+
 __device__ __forceinline__ float sum_f32x4(const uint64_t (&x)[2]) {
     const float2 s = unpack_f32x2(add_f32x2(x[0], x[1]));
     return s.x + s.y;
@@ -527,7 +537,10 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                             const float2 z = unpack_f32x2(fma_f32x2(pack_f32x2(v[h + 2 * u], v[h + 2 * u + 1]), kk2, mm2));
                             const float e0 = at_exp2(z.x), e1 = at_exp2(z.y);
                             pk[u] = pack_bf16(e0, e1);
-                            l2[u & 1] = add_f32x2(l2[u & 1], pack_f32x2(e0, e1));
+                            // The sums take the probabilities that the MMA sees, so that a row's weights add up to 1.  (Sums of
+                            // e0 and e1: error 2.3e-3 of the output for 2.1e-3, the mean of equal values is not that value; 182 us
+                            // for 172 at 16 layers of 2048 tokens, hd 64, and 710 for 740 at 16001, hd 128.)
+                            add_bf16x2(l2[u & 1], pk[u]);
                         }
                         tmem_st8(t_s + (b + h) / 2, pk);
                     }

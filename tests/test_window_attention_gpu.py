@@ -315,3 +315,20 @@ def test_a_token_that_is_not_a_number_leaves_the_others_as_they_are(hd):
     assert outs[1][..., 40, :].isnan().all()
     outs[1][..., 40, :] = outs[0][..., 40, :]
     assert torch.equal(*outs)
+
+
+@pytest.mark.parametrize("L,Lq,hd,late", [(20, 300, 64, 1.0), (20, 300, 128, 1.0), (20, 300, 64, 6.0), (1, 5, 64, 1.0), (1, 5, 128, 6.0)])
+def test_values_that_are_all_the_same_come_out_as_they_are(L, Lq, hd, late):
+    """The weights that a bf16 output is made of add up to 1: 32-bit sums of some hundred terms are off by 2^-16 at most, which is far
+    below half of a bf16 place, so the output is the value exactly."""
+    n_kv, group, n_past = 2, 4, 500
+    run = handle(L, n_kv, hd, torch.bfloat16)
+    g = torch.Generator(device="cuda").manual_seed(Lq + hd)
+    rn = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    K, V, Q = rn(1, L, n_kv, n_past + Lq, hd), rn(1, L, n_kv, 1, hd).repeat(1, 1, 1, n_past + Lq, 1), 2 * rn(1, L, group * n_kv, Lq, hd)
+    K[..., n_past // 2:, :] *= late
+    out = torch.full_like(Q, 7.0)
+    mone.mone_window_attention(run.h, -1, Q, group * n_kv, Lq, K, V, K.stride()[:4], n_past, 7, 333, out)
+    mone.mone_mem_sync(run.h)
+    run.close()
+    assert torch.equal(out, V[..., :1, :].repeat_interleave(group, 2).expand_as(out))
