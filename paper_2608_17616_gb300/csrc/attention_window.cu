@@ -46,7 +46,7 @@ struct WinSmem {
     // qfull[QB] qempty[QB] kfull[NS] kempty[NS] vfull[NS] vempty[NS], and for each tile sfull[NB] odone[NB] pready[NB] oempty
     static constexpr int BAR_OFF = V_OFF + NS * TILE, TILE_BARS = 3 * NB + 1;
     static constexpr int SLOT_OFF = BAR_OFF + (2 * QB + 4 * NS + 2 * TILE_BARS) * 8;
-    static constexpr int DYN = SLOT_OFF + 16 + 1024;       // + TMEM slot, + alignment slack
+    static constexpr int DYN = SLOT_OFF + 16 + 1024;       // + TMEM slot and count of rows, + alignment slack
     static_assert(NB * NK + HD <= TILE_COLS && CTAS * TMEM <= 512 && CTAS * (DYN + 1024) <= 228 * 1024, "CTAs an SM");
 };
 
@@ -131,12 +131,27 @@ __device__ __forceinline__ void win_commit(uint32_t bar, uint32_t me) {
         : "memory");
 }
 
-// mbar_wait by a whole warp, with one answer
-__device__ __forceinline__ bool win_wait(uint32_t bar, uint32_t parity, int* status) {
+// mbar_wait by a whole warp, with one answer.  It gives up when neither the barrier's phase nor the count of rows computed again has
+// moved for the limit: a warp may have 32 such rows between two tiles, each over up to 2^20 positions (0.2 s).
+__device__ __forceinline__ bool win_wait(uint32_t bar, uint32_t parity, int* status, const volatile uint32_t* again) {
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    return __all_sync(0xffffffffu, mbar_wait(bar, parity, status));
+    uint32_t rows = __shfl_sync(0xffffffffu, *again, 0);
+    uint64_t t0 = globaltimer_ns();
+    while (true) {
+#pragma unroll 1
+        for (int i = 0; i < 32; ++i)
+            if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+        if (__any_sync(0xffffffffu, globaltimer_ns() - t0 > kWaitLimitNs)) {
+            const uint32_t now = __shfl_sync(0xffffffffu, *again, 0);
+            if (now == rows) {
+                atomicOr(status, DEV_TIMEOUT);
+                return false;
+            }
+            rows = now;
+            t0 = globaltimer_ns();
+        }
+    }
 }
-
 
 // row_again by a warp, which has HD / 32 dimensions a lane; eight keys' loads under way
 template <int HD>
@@ -276,9 +291,12 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     auto pready = [&](int x, int j) { return bars + 8 * (SB0 + x * SM::TILE_BARS + 2 * NB + j % NB); };
     auto oempty = [&](int x) { return bars + 8 * (SB0 + x * SM::TILE_BARS + 3 * NB); };  // of a tile
     uint32_t* slot = reinterpret_cast<uint32_t*>(base + SM::SLOT_OFF);
+    uint32_t* again = slot + 1;  // rows computed again
+    auto wait = [&](uint32_t bar, uint32_t parity) { return win_wait(bar, parity, a.status, again); };
     // the warp's number from one lane, and below the TMEM address: the compiler then knows them to be the same in all
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     if (tid == 0) {
+        *again = 0;
         for (int i = 0; i < QB; ++i) {
             mbar_init(qfull(i), 1);
             mbar_init(qempty(i), 2);
@@ -332,7 +350,7 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         const uint32_t k0 = smem_u32(base + SM::K_OFF), v0 = smem_u32(base + SM::V_OFF);
         int vp = -1, vctx = 0, vlayer = 0, vhead = 0;
         auto load_v = [&]() {
-            ok = ok && win_wait(vempty(rv.s), rv.ph, a.status);
+            ok = ok && wait(vempty(rv.s), rv.ph);
             if (!ok) return;
             win_expect(vfull(rv.s), SM::TILE, me);
 #pragma unroll
@@ -344,7 +362,7 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             tl.open(a);
             // a dimension that the caches share (stride 0) has one element in the maps
             const int tctx = tl.c / a.L, ctx = a.s0 ? tctx : 0, layer = a.s1 ? tl.c - tctx * a.L : 0, head = a.s2 ? tl.g : 0;
-            ok = win_wait(qempty(i), (i / QB & 1) ^ 1, a.status);
+            ok = wait(qempty(i), (i / QB & 1) ^ 1);
             if (!ok) break;
             if (me) {
                 mbar_expect_tx(qfull(i), (tl.two ? 2 : 1) * (HD / 64) * a.group * rt * 128);
@@ -358,7 +376,7 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             __syncwarp();
             for (int j = 0; ok && j < tl.n; ++j) {
                 const int pos = tl.at(j);
-                ok = win_wait(kempty(rk.s), rk.ph, a.status);
+                ok = wait(kempty(rk.s), rk.ph);
                 if (!ok) break;
                 win_expect(kfull(rk.s), SM::TILE, me);
 #pragma unroll
@@ -383,14 +401,14 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         int s = 0, ph = 0, J = 0;  // the ring's next slot and its phase; chunk of all the tile's
         for (int i = 0; ok && tl.more(); ++i, tl.next()) {
             tl.open(a);
-            ok = win_wait(qfull(i), i / QB & 1, a.status);
+            ok = wait(qfull(i), i / QB & 1);
             const uint64_t dq = sdesc_step(dq0, i % QB * 2 * SM::Q_TILE);
             for (int j = 0; ok && j < tl.n; ++j) {
                 const uint32_t id_s = idesc_bf16_f32(128, tl.width(j, x), false, false);
                 const uint64_t dk = sdesc_step(dk0, s * SM::TILE);
-                ok = win_wait(kfull(s), ph, a.status);
+                ok = wait(kfull(s), ph);
                 if (tl.has(x)) {
-                    if (J >= NB) ok = ok && win_wait(odone(x, J), (J / NB & 1) ^ 1, a.status);  // P V of chunk J - NB has read its P, where S goes
+                    if (J >= NB) ok = ok && wait(odone(x, J), (J / NB & 1) ^ 1);  // P V of chunk J - NB has read its P, where S goes
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll
@@ -422,14 +440,14 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             tl.open(a);
             for (int j = 0; ok && j < tl.n; ++j) {
                 const uint64_t dv = sdesc_step(dv0, s * SM::TILE);
-                ok = win_wait(vfull(s), ph, a.status);
+                ok = wait(vfull(s), ph);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     if (!tl.has(x)) continue;
                     const int J = chunk[x]++, wd = tl.width(j, x);
                     const uint32_t t_p = tmem + x * SM::TILE_COLS + J % NB * NK, t_o = tmem + x * SM::TILE_COLS + NB * NK;
-                    if (j == 0) ok = ok && win_wait(oempty(x), (count[x]++ & 1) ^ 1, a.status);  // the last tile's O has been read
-                    ok = ok && win_wait(pready(x, J), J / NB & 1, a.status);          // P of chunk J is in TMEM
+                    if (j == 0) ok = ok && wait(oempty(x), (count[x]++ & 1) ^ 1);  // the last tile's O has been read
+                    ok = ok && wait(pready(x, J), J / NB & 1);          // P of chunk J is in TMEM
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll
@@ -471,7 +489,7 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             for (int j = 0; j < tl.n; ++j, ++J) {
                 const uint32_t t_s = t_x + J % NB * NK;
                 const int at = tl.at(j), wd = tl.width(j, x);
-                ok = win_wait(sfull(x, J), J / NB & 1, a.status);
+                ok = wait(sfull(x, J), J / NB & 1);
                 if (!ok) break;
                 tc_fence_after();
                 // Hidden keys get scores of -inf, written back: few chunks have any, and the loop over all of them stays short (its
@@ -508,7 +526,7 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 // (whether or not a row has no scale yet: one whose scores are all NaN never gets one)
                 if (__any_sync(0xffffffffu, sum_f32x4(l2) > SUM_MOST)) {
                     const float l = sum_f32x4(l2);
-                    ok = win_wait(odone(x, J - 1), (J - 1) / NB & 1, a.status);  // O up to the last chunk
+                    ok = wait(odone(x, J - 1), (J - 1) / NB & 1);  // O up to the last chunk
                     if (!ok) break;
                     tc_fence_after();
                     const int e = l > SUM_MOST && l <= FLT_MAX ? ilogbf(l) : 0;  // by a power of two
@@ -567,7 +585,7 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             }
             if (!ok) break;
             const float sum = sum_f32x4(l2);
-            ok = win_wait(odone(x, J - 1), (J - 1) / NB & 1, a.status);
+            ok = wait(odone(x, J - 1), (J - 1) / NB & 1);
             if (!ok) break;
             tc_fence_after();
             // no key that counts: 0; a sum that has overflowed: NaN, and the row again
@@ -602,6 +620,7 @@ window_prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 const size_t of = __shfl_sync(0xffffffffu, at, src);
                 row_by_warp<HD>(static_cast<const bf16*>(a.Q) + of, static_cast<const bf16*>(a.K) + kv_off, static_cast<const bf16*>(a.V) + kv_off,
                                 __shfl_sync(0xffffffffu, vis, src), a, static_cast<bf16*>(a.out) + of);
+                if (lane == 0) atomicAdd(again, 1u);
             }
             __syncwarp();
         }

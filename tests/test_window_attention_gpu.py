@@ -332,3 +332,25 @@ def test_values_that_are_all_the_same_come_out_as_they_are(L, Lq, hd, late):
     mone.mone_mem_sync(run.h)
     run.close()
     assert torch.equal(out, V[..., :1, :].repeat_interleave(group, 2).expand_as(out))
+
+
+def test_rows_that_take_seconds_to_compute_again_do_not_time_out():
+    """A value of the first position is infinite in one dimension: every row is computed again over all of its 450,000 positions, which
+    takes a warp more than the 2 s of a wait for its 32, while the others wait for its next tile."""
+    group, hd, Lq, S = 4, 128, 6000, 450000  # more pairs of tiles than CTAs
+    run = handle(1, 2, hd, torch.bfloat16)
+    g = torch.Generator(device="cuda").manual_seed(hd)
+    rn = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    K, V, Q = rn(1, 1, 1, S, hd), rn(1, 1, 1, S, hd), rn(1, 1, 2 * group, Lq, hd)  # both KV heads read the same: stride 0
+    V[0, 0, 0, 0, 5] = float("inf")
+    out = torch.full_like(Q, 7.0)
+    mone.mone_window_attention(run.h, -1, Q, 2 * group, Lq, K, V, (S * hd, S * hd, 0, hd), S - Lq, 0, ALL, out)
+    mone.mone_mem_sync(run.h)
+    run.close()
+    assert out[..., 5].isposinf().all()
+    rest = [d for d in range(hd) if d != 5]
+    k, v = K[0, 0, 0].float(), V[0, 0, 0, :, rest].double()
+    for i in (0, 1, 37, Lq // 2, Lq - 1):
+        n = S - Lq + i + 1
+        ref = torch.softmax((Q[0, 0, :, i].float() @ k[:n].T).double() / hd ** 0.5, -1) @ v[:n]
+        assert rel_fro(out[0, 0, :, i][:, rest].double().cpu(), ref.cpu()) <= 5e-3, i
