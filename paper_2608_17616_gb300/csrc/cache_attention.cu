@@ -17,6 +17,7 @@
 // key and value), and the second kernel, or the cluster's end, adds exp(z - max) / sum over the rows of a KV head.
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "cache_common.cuh"
 #include "per_device.h"
@@ -262,6 +263,11 @@ __device__ __forceinline__ void write_row(const CaArgs& a, size_t kv, int c, int
 // log2 of the sum of exp of a row, +inf where nothing counts (its weights are then 0)
 __device__ __forceinline__ float row_lse(float m, float lx, float k2) { return lx == 0.f ? INFINITY : fmaf(m, k2, log2f(lx)); }
 
+// A position's weight from a row.  NANS: some row's sum is not a number; such a row adds nothing where it does not see.  (The
+// comparison everywhere: 13.4 us for 12.9 at 16 layers of 1151 positions.)
+template <bool NANS>
+__device__ __forceinline__ float ca_weight(float z2, float lse) { return NANS && z2 == -INFINITY ? 0.f : ca_exp2(z2 - lse); }
+
 // What the warps of a CTA have of a row's dimensions d and d + 1 (e: their place in a part), in the warps' order
 struct CaJoined {
     float mx, l, lx, o0, o1;
@@ -316,7 +322,8 @@ __device__ __forceinline__ void cluster_end(const CaArgs& a, const CaNote* notes
     const CaRange r(a, c);
     const int units = r.units();
     const bool split = S > 1 && units > 1;
-    if (units > 1) {  // else one warp has written the item
+    bool nans = false;  // some row's sum
+    if (units > 1) {    // else one warp has written the item
         const long long head = l * a.v.s_layer + g * a.v.s_head;
         auto write = [&](int row, int d, float o0, float o1, float l) {
             write_row<T, HD>(a, kv, c, r.n, row0 + row, d, static_cast<const T*>(a.v.K) + head, static_cast<const T*>(a.v.V) + head, o0, o1, l);
@@ -332,7 +339,10 @@ __device__ __forceinline__ void cluster_end(const CaArgs& a, const CaNote* notes
                 if (d == 0) mine[P::M + row] = x.mx, mine[P::L + row] = x.l, mine[P::LX + row] = x.lx;
             } else {
                 write(row, d, x.o0, x.o1, x.l);
-                if (d == 0) lse[row] = row_lse(x.mx, x.lx, k2);
+                if (d == 0) {
+                    lse[row] = row_lse(x.mx, x.lx, k2);
+                    nans |= isnan(x.lx);
+                }
             }
         }
         if (split) {
@@ -373,14 +383,16 @@ __device__ __forceinline__ void cluster_end(const CaArgs& a, const CaNote* notes
                 for (int k = 0; k < 8; ++k)
                     if (k < S) lx = fmaf(f[k], ca_remote(mine + P::LX + tid, k), lx);
                 lse[tid] = row_lse(mx, lx, k2);
+                nans = isnan(lx);
             }
             asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         }
     } else if (a.z2 && tid < rows) {
         lse[tid] = a.lse[kv * a.R + row0 + tid];
+        nans = isnan(lse[tid]);
     }
     if (a.z2) {
-        __syncthreads();
+        nans = __syncthreads_or(nans);
         const int b0 = units * rank / S, b1 = min(units * (rank + 1) / S, r.nb);
         float* score = a.v.score + (((size_t)c * a.v.Lh + l) * a.v.n_kv + g) * a.v.cap;
         const float* z = a.z2 + (kv * a.R + row0) * a.pitch;
@@ -394,14 +406,18 @@ __device__ __forceinline__ void cluster_end(const CaArgs& a, const CaNote* notes
                 w[k] = seen[k] ? score[p + k] : 0.f;
             }
             float add[4] = {0.f, 0.f, 0.f, 0.f};
+            auto sum = [&](auto check) {
+                constexpr bool N = decltype(check)::value;
 #pragma unroll 4
-            for (int row = 0; row < rows; ++row) {
-                const float4 x = *reinterpret_cast<const float4*>(z + row * a.pitch + p);
-                add[0] += ca_exp2(x.x - lse[row]);
-                add[1] += ca_exp2(x.y - lse[row]);
-                add[2] += ca_exp2(x.z - lse[row]);
-                add[3] += ca_exp2(x.w - lse[row]);
-            }
+                for (int row = 0; row < rows; ++row) {
+                    const float4 x = *reinterpret_cast<const float4*>(z + row * a.pitch + p);
+                    add[0] += ca_weight<N>(x.x, lse[row]);
+                    add[1] += ca_weight<N>(x.y, lse[row]);
+                    add[2] += ca_weight<N>(x.z, lse[row]);
+                    add[3] += ca_weight<N>(x.w, lse[row]);
+                }
+            };
+            nans ? sum(std::true_type()) : sum(std::false_type());
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (seen[k]) score[p + k] = w[k] + add[k];
@@ -1038,6 +1054,7 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) cache_finish_kernel(const CaAr
     float* score = a.v.score + (((size_t)c * a.v.Lh + l) * a.v.n_kv + g) * a.v.cap;
     for (int row0 = 0; row0 < a.R; row0 += FIN_ROWS) {
         const int rows = min(FIN_ROWS, a.R - row0);
+        bool nans = false;  // some row's sum
         __syncthreads();
         for (int row = threadIdx.x >> 5; row < rows; row += FIN_WARPS) {  // a warp a row
             const int lane = threadIdx.x & 31, in = (row0 + row) % ROWS, info = a.info[kv * a.RT + (row0 + row) / ROWS];
@@ -1049,33 +1066,38 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) cache_finish_kernel(const CaAr
                 for (int k = lane; k < n; k += 32) {
                     using P = Part<HD, ROWS>;
                     const float* p = P::of_cta(a, first + k, k == 0) + in;
+                    // (a part of max -inf has the sum 0, or NaN, which stays)
                     const float mk = p[P::M], lk = p[P::LX], mn = fmaxf(m, mk);
-                    if (mk == -INFINITY) continue;
-                    lx = fmaf(lx, ca_exp2((m - mn) * k2), lk * ca_exp2((mk - mn) * k2));
+                    lx = fmaf(lx, m == -INFINITY ? 1.f : ca_exp2((m - mn) * k2), mk == -INFINITY ? lk : lk * ca_exp2((mk - mn) * k2));
                     m = mn;
                 }
                 const float mx = warp_max(m);
-                lx = warp_sum(m == -INFINITY ? 0.f : lx * ca_exp2((m - mx) * k2));
+                lx = warp_sum(m == -INFINITY ? lx : lx * ca_exp2((m - mx) * k2));
                 m = row_lse(mx, lx, k2);
             }
             if (lane == 0) lse[row] = m;
+            nans |= isnan(m);
         }
-        __syncthreads();
+        nans = __syncthreads_or(nans);
 #pragma unroll 2
         for (int tile = 0; tile < FIN_TILES; ++tile) {
             const int p = p0 + tile * FIN_TILE;
             if (p >= r.n || (p >= a.n_sink && p + 4 <= r.t0 - a.window + 1)) continue;
             float w[4] = {0.f, 0.f, 0.f, 0.f};
             const float* z = a.z2 + (kv * a.R + row0) * a.pitch + p;
+            auto sum = [&](auto check) {
+                constexpr bool N = decltype(check)::value;
 #pragma unroll 4
-            for (int row = 0; row < rows; ++row) {
-                const float4 x = __ldcs(reinterpret_cast<const float4*>(z + row * a.pitch));
-                const float s = lse[row];
-                w[0] += ca_exp2(x.x - s);
-                w[1] += ca_exp2(x.y - s);
-                w[2] += ca_exp2(x.z - s);
-                w[3] += ca_exp2(x.w - s);
-            }
+                for (int row = 0; row < rows; ++row) {
+                    const float4 x = __ldcs(reinterpret_cast<const float4*>(z + row * a.pitch));
+                    const float s = lse[row];
+                    w[0] += ca_weight<N>(x.x, s);
+                    w[1] += ca_weight<N>(x.y, s);
+                    w[2] += ca_weight<N>(x.z, s);
+                    w[3] += ca_weight<N>(x.w, s);
+                }
+            };
+            nans ? sum(std::true_type()) : sum(std::false_type());
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (p + i < r.n && (p + i < a.n_sink || p + i > r.t0 - a.window)) score[p + i] += w[i];

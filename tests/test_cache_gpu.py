@@ -275,6 +275,34 @@ def test_pages_and_lengths_out_of_range_are_latched_and_skipped():
     assert e.value.code == 8 and "length" in str(e.value)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lens,spare,n_tok,bad", [
+    ([200], 3, 4, slice(199, 200)),        # the newest token's key alone: the older tokens' windows begin where its own does not
+    ([300, 40], 3, 3, slice(2, 3)),        # one that all see
+    ([9000], 1024, 1, slice(1024, 8064)),   # dealt out: parts of 128 positions that hold no other score
+    ([9000], 1024, 4, slice(8999, 9000)),
+    ([900], 3, 1, slice(100, 800)),        # a cluster's
+])
+def test_weights_of_tokens_whose_scores_are_not_numbers(lens, spare, n_tok, bad, dtype):
+    """Such a token's weights are not numbers where it sees, and nothing where it does not."""
+    x = Cache(lens, dtype=dtype, spare=spare, seed=len(lens))
+    window = 50 if n_tok > 1 else ALL
+    x.k[0][:, :, bad] = float("nan")
+    x.put(x.K, 0, x.k[0])
+    Q = torch.randn(len(lens), 2, 8, n_tok, 64, generator=x.g, device="cuda").to(dtype)
+    out, want = torch.full_like(Q, 7.0), x.score.double().cpu()
+    mone.mone_cache_attention(x.h, -1, x.c, Q, 8, n_tok, 3, window, out)
+    x.done()
+    for c, n in enumerate(lens):
+        for l in range(2):
+            ref, w = O.window_attention(Q[c, l].float().cpu(), x.k[c][l].float().cpu(), x.v[c][l].float().cpu(), n - n_tok, 3, window)
+            want[c, l, :, :n] += torch.from_numpy(w)
+            assert torch.equal(out[c, l].isnan().cpu(), torch.from_numpy(ref).isnan())
+    got = x.score.cpu()
+    assert torch.equal(got.isnan(), want.isnan()) and want.isnan().any()
+    assert rel_fro(got.nan_to_num(), want.nan_to_num()) <= 1e-5
+
+
 # ----------------------------------------------------------------- append
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
