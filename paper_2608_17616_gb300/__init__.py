@@ -68,9 +68,13 @@ class mone_cache(ctypes.Structure):
     _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("strides", _LL4),
                 ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int), ("table", ctypes.c_void_p),
                 ("table_width", ctypes.c_int), ("lens", ctypes.c_void_p), ("score", ctypes.c_void_p)]
+    _of = None  # make_cache's: its tensors' layers, contexts, KV heads, head_dim, dtype; layers and KV heads of its score
+    _fits = None  # the handle's that they were found to do for
 
 
 _lib = None
+_types = {}  # torch's, by name
+_handles = {}  # a live handle's layers, contexts, KV heads, head_dim and dtype
 
 
 def lib(path: Optional[str] = None) -> ctypes.CDLL:
@@ -191,6 +195,7 @@ def mone_mem_init(cfg: mone_config, W1_0, W2_0, meta=None, stream=None) -> int:
     rc = lib().mone_mem_init(ctypes.byref(cfg), _ptr(W1_0), _ptr(W2_0), ctypes.byref(m) if m is not None else None,
                              _stream(stream), ctypes.byref(h))
     _check("mone_mem_init", rc)
+    _handles[h.value] = (cfg.n_layers, cfg.n_ctx, cfg.n_kv_heads, cfg.head_dim, cfg.dtype)
     return h.value
 
 
@@ -245,45 +250,89 @@ def mone_window_attention(h: int, layer: int, Q, n_q_heads: int, Lq: int, K, V, 
                                                                 n_sink, window, _ptr(out), _stream(stream)))
 
 
+def _buffer(name: str, t, dtype: str, at_least: int, shape: str):
+    """Refuses a tensor of another type, with gaps or too small (an address is taken as it is)."""
+    if not hasattr(t, "is_contiguous"):
+        return
+    want = _types.get(dtype)
+    if want is None:
+        import torch
+        want = _types[dtype] = getattr(torch, dtype)
+    if t.dtype is not want or not t.is_contiguous() or t.numel() < at_least:
+        raise ValueError(f"{name}: a contiguous {dtype} tensor {shape}, not {tuple(t.shape)}, {t.dtype}")
+
+
 def make_cache(K, V, table, lens, score=None) -> mone_cache:
     """A paged cache over torch tensors: K, V [layers, pages, KV heads, page_size, head_dim] of any strides with head_dim
-    contiguous (K.stride() == V.stride()), table [contexts, width] and lens [contexts] int32, score fp32.  It holds their
-    addresses, not the tensors: keep them alive."""
-    if K.stride() != V.stride() or K.shape != V.shape or K.dim() != 5 or K.stride(4) != 1:
+    contiguous (K.stride() == V.stride()), table [contexts, width] and lens [contexts] int32, score
+    [contexts, layers, KV heads, width * page_size] fp32.  It holds their addresses, not the tensors: keep them alive."""
+    if K.stride() != V.stride() or K.shape != V.shape or K.dtype != V.dtype or K.dim() != 5 or K.stride(4) != 1:
         raise ValueError("K and V: [layers, pages, KV heads, page_size, head_dim], the same strides, head_dim contiguous")
+    dtype = {"torch.float32": MONE_FP32, "torch.bfloat16": MONE_BF16}.get(str(K.dtype))
+    if dtype is None:
+        raise ValueError("K and V: float32 or bfloat16")
     for name, t, dims in (("table", table, 2), ("lens", lens, 1), ("score", score, 4)):
-        if t is not None and (t.dim() != dims or not t.is_contiguous() or t.element_size() != 4):
-            raise ValueError(f"{name}: a contiguous tensor of {dims} dimensions and 32-bit elements")
-    return mone_cache(_ptr(K), _ptr(V), _LL4(*K.stride()[:4]), K.shape[1], K.shape[3], _ptr(table),
-                      table.shape[1], _ptr(lens), _ptr(score))
+        if t is not None and t.dim() != dims:
+            raise ValueError(f"{name}: a tensor of {dims} dimensions")
+    n_layers, n_pages, n_kv, page, hd = K.shape
+    n_ctx, width = table.shape
+    _buffer("table", table, "int32", 1, "[contexts, width]")
+    _buffer("lens", lens, "int32", n_ctx, "[contexts]")
+    if score is not None:
+        _buffer("score", score, "float32", 1, "[contexts, layers, KV heads, width * page_size]")
+        if score.shape[0] < n_ctx or score.shape[3] != width * page:
+            raise ValueError(f"score: [{n_ctx} contexts, layers, KV heads, {width} * {page}], not {tuple(score.shape)}")
+    c = mone_cache(_ptr(K), _ptr(V), _LL4(*K.stride()[:4]), n_pages, page, _ptr(table), width, _ptr(lens), _ptr(score))
+    c._of = (n_layers, n_ctx, n_kv, hd, dtype, None if score is None else tuple(score.shape[1:3]))
+    return c
+
+
+def _cache(h: int, cache: mone_cache):
+    need = _handles.get(h)
+    if cache._fits is not need:
+        of = cache._of
+        if None not in (of, need) and (of[4] != need[4] or any(a < b for a, b in zip(of[:4], need)) or of[5] not in (None, need[0:3:2])):
+            raise ValueError(f"the cache's layers, contexts, KV heads, head_dim, dtype (and its score's layers and KV heads) are {of}, "
+                             f"the handle's {need}")
+        cache._fits = need
+    return ctypes.byref(cache)
 
 
 def mone_cache_append(h: int, layer: int, cache: mone_cache, K, V, strides: Sequence[int], n_tok: int, lens_out=None, counts=None,
                       stream=None):
     """New tokens' keys and values after each context's positions."""
     arr = _strides(strides)
-    _check("mone_cache_append", lib().mone_cache_append(h, layer, ctypes.byref(cache), _ptr(K), _ptr(V), arr, n_tok, _ptr(counts),
+    _check("mone_cache_append", lib().mone_cache_append(h, layer, _cache(h, cache), _ptr(K), _ptr(V), arr, n_tok, _ptr(counts),
                                                         _ptr(lens_out), _stream(stream)))
 
 
 def mone_cache_attention(h: int, layer: int, cache: mone_cache, Q, n_q_heads: int, n_tok: int, n_sink: int, window: int, out,
                          stream=None):
     """Attention of each context's newest n_tok tokens over its pages; with cache.score, the weights are added up there."""
-    _check("mone_cache_attention", lib().mone_cache_attention(h, layer, ctypes.byref(cache), _ptr(Q), n_q_heads, n_tok, n_sink,
+    _check("mone_cache_attention", lib().mone_cache_attention(h, layer, _cache(h, cache), _ptr(Q), n_q_heads, n_tok, n_sink,
                                                               window, _ptr(out), _stream(stream)))
 
 
 def mone_cache_evict(h: int, layer: int, cache: mone_cache, keep: int, n_sink: int, n_recent: int, to_table, to_score, kept,
                      lens_out=None, stream=None):
     """The first n_sink positions, the last n_recent and the best scored others, `keep` in all, into the pages of to_table
-    [contexts, width]."""
-    _check("mone_cache_evict", lib().mone_cache_evict(h, layer, ctypes.byref(cache), keep, n_sink, n_recent, _ptr(to_table),
-                                                      to_table.shape[1], _ptr(to_score), _ptr(kept), _ptr(lens_out),
-                                                      _stream(stream)))
+    [contexts, width]; to_score and kept as in the header."""
+    width, need = to_table.shape[1], _handles.get(h)
+    if need is not None:
+        n_layers, n_ctx, n_kv = need[:3]
+        per, rows = width * cache.page_size, n_ctx * n_kv
+        _buffer("to_table", to_table, "int32", n_ctx * width, "[contexts, width]")
+        _buffer("to_score", to_score, "float32", rows * n_layers * per, "[contexts, layers, KV heads, width * page_size]")
+        _buffer("kept", kept, "int32", rows * (n_layers if layer == MONE_ALL_LAYERS else 1) * keep, "[contexts, layers, KV heads, keep]")
+        if getattr(to_score, "ndim", 0) == 4 and to_score.shape[1:] != (n_layers, n_kv, per):
+            raise ValueError(f"to_score: [contexts, {n_layers}, {n_kv}, {per}], not {tuple(to_score.shape)}")
+    _check("mone_cache_evict", lib().mone_cache_evict(h, layer, _cache(h, cache), keep, n_sink, n_recent, _ptr(to_table), width,
+                                                      _ptr(to_score), _ptr(kept), _ptr(lens_out), _stream(stream)))
 
 
 def mone_mem_free(h: int):
     _check("mone_mem_free", lib().mone_mem_free(h))
+    _handles.pop(h, None)
 
 
 def mone_mem_read_state(h: int, W1=None, W2=None, mu1=None, mu2=None, stream=None):

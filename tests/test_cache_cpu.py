@@ -263,3 +263,67 @@ def test_make_cache_takes_the_tensors_strides():
                 lambda: mone.make_cache(K, V, t.T, n), lambda: mone.make_cache(K.transpose(3, 4), V.transpose(3, 4), t, n)):
         with pytest.raises(ValueError):
             bad()
+
+
+def tensors(L=3, n_ctx=2, n_kv=2, hd=64, page=16, width=10, dtype="bfloat16", score=True):
+    import torch
+    pool = [torch.zeros(L, 40, n_kv, page, hd, dtype=getattr(torch, dtype)) for _ in range(2)]
+    return [*pool, torch.zeros(n_ctx, width, dtype=torch.int32), torch.zeros(n_ctx, dtype=torch.int32),
+            torch.zeros(n_ctx, L, n_kv, width * page) if score else None]
+
+
+def test_make_cache_refuses_tensors_that_do_not_go_together():
+    import torch
+    good = tensors()
+    mone.make_cache(*good)
+    for i, bad in ((2, torch.zeros(2, 10)), (2, torch.zeros(2, 10, dtype=torch.uint32)), (2, torch.zeros(3, 10, dtype=torch.int32)),
+                   (3, torch.zeros(1, dtype=torch.int32)), (3, torch.zeros(2)), (4, torch.zeros(2, 3, 2, 159)), (4, torch.zeros(2, 3, 2, 161)),
+                   (4, torch.zeros(1, 3, 2, 160)), (4, torch.zeros(2, 3, 2, 160, dtype=torch.int32)), (4, torch.zeros(2, 3, 2, 320)[..., ::2]),
+                   (1, good[0].half()), (1, good[0].float())):
+        with pytest.raises(ValueError):
+            mone.make_cache(*[bad if k == i else x for k, x in enumerate(good)])
+    with pytest.raises(ValueError):
+        mone.make_cache(*[x.half() for x in good[:2]], *good[2:])
+
+
+@pytest.mark.parametrize("kw", [dict(L=2), dict(n_ctx=1), dict(n_kv=1), dict(hd=32), dict(dtype="float32"), dict(L=4), dict(n_kv=4)])
+def test_a_cache_of_another_handle_is_refused(fake, kw):
+    """Too little of anything, and scores that lie otherwise."""
+    h, keep = init(), tensors(**kw)
+    n0 = mone.mone_mem_launch_count(h)
+    c, to = mone.make_cache(*keep), tensors()[2]
+    for call in (lambda: mone.mone_cache_append(h, -1, c, P, P, ST, 3, stream=0),
+                 lambda: mone.mone_cache_attention(h, -1, c, P, 4, 1, 0, 100, P, stream=0),
+                 lambda: mone.mone_cache_evict(h, -1, c, 50, 2, 3, to, P + 128, P, stream=0)):
+        with pytest.raises(ValueError):
+            call()
+    assert mone.mone_mem_launch_count(h) == n0
+
+
+def test_a_cache_with_room_for_more_than_the_handle_has_is_taken(fake):
+    h, keep, exact = init(), tensors(L=4, n_ctx=3, n_kv=4, score=False), tensors()
+    for t in (keep, exact):
+        c = mone.make_cache(*t)
+        for _ in range(2):
+            mone.mone_cache_attention(h, -1, c, P, 4, 1, 0, 100, P, stream=0)
+    mone.mone_mem_free(h)
+    refused(1, mone.mone_cache_attention, h, -1, c, P, 4, 1, 0, 100, P)
+    h = init(n_ctx=3)  # perhaps at the same address
+    with pytest.raises(ValueError):
+        mone.mone_cache_attention(h, -1, c, P, 4, 1, 0, 100, P, stream=0)
+
+
+def test_evict_refuses_targets_that_are_too_small_or_lie_otherwise(fake):
+    import torch
+    h, keep = init(), tensors()
+    c = mone.make_cache(*keep)
+    good = [torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, 3, 2, 64), torch.zeros(2, 3, 2, 50, dtype=torch.int32)]
+    mone.mone_cache_evict(h, -1, c, 50, 2, 3, *good, stream=0)
+    mone.mone_cache_evict(h, 1, c, 50, 2, 3, *good[:2], good[2][:, 0].contiguous(), stream=0)
+    n0 = mone.mone_mem_launch_count(h)
+    for i, bad in ((0, torch.zeros(2, 8, dtype=torch.int32)[:, :4]), (0, good[0].long()), (0, good[0][:1]), (1, torch.zeros(2, 3, 2, 63)),
+                   (1, torch.zeros(2, 3, 2, 160)), (1, good[1].double()), (1, good[1][:1]), (2, torch.zeros(2, 3, 2, 49, dtype=torch.int32)),
+                   (2, good[2].long()), (2, good[2].transpose(1, 2))):
+        with pytest.raises(ValueError):
+            mone.mone_cache_evict(h, -1, c, 50, 2, 3, *[bad if k == i else x for k, x in enumerate(good)], stream=0)
+    assert mone.mone_mem_launch_count(h) == n0
