@@ -1,6 +1,6 @@
 """GPU parity of the windowed attention against the oracle's definition in 64 bits, in each of its forms: many rows on the
-tensor cores (128-row tiles, chunks of 96 keys, 64 at hd 128), few rows (16-row tiles, the keys split), and the CUDA cores
-(fp32, and bf16 rows that are not aligned).
+tensor cores (128-row tiles, chunks of 64 keys), few rows (16-row tiles, the keys split), and the CUDA cores (fp32, and bf16
+rows that are not aligned).
 
 Tolerances (relative 2-norm).  bf16 5e-3: probabilities and outputs are rounded to 8 bits once each, at most 2^-9 of
 themselves and 2^-9 / sqrt(3) in the mean, 1.6e-3 together, times three.  fp32 1e-5: the score of a key is a sum of up to
@@ -354,3 +354,19 @@ def test_rows_that_take_seconds_to_compute_again_do_not_time_out():
         n = S - Lq + i + 1
         ref = torch.softmax((Q[0, 0, :, i].float() @ k[:n].T).double() / hd ** 0.5, -1) @ v[:n]
         assert rel_fro(out[0, 0, :, i][:, rest].double().cpu(), ref.cpu()) <= 5e-3, i
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n_past", [0, 1, 15, 16, 17, 31, 32, 33, 47, 48, 49, 63, 65])
+def test_last_chunks_of_every_width(n_past, hd):
+    """Chunks of 64 keys, tiles of 32 tokens: a pair of tiles whose last chunk ends with n_past % 64 of its keys in the second tile and
+    with half a chunk less or more in the first, in sixteens and one more or less."""
+    case(4, 64, n_past, 0, ALL, hd, n_layers=20)
+    case(4, 41, n_past, 3, 70, hd, n_layers=20)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n_sink,window", [(0, 63), (0, 64), (0, 65), (63, 64), (64, 63), (64, 64), (65, 65), (127, 64), (128, 128),
+                                           (129, 127), (64, 129), (65, 1), (128, 0), (127, 0)])
+def test_first_positions_and_windows_at_the_ends_of_chunks(n_sink, window, hd):
+    case(4, 133, 300, n_sink, window, hd, n_layers=20)
