@@ -16,9 +16,9 @@
 // The softmax does without a maximum for each chunk: the scale of a row is the max of its first sixteen keys of which one counts,
 // and floating point does not mind later scores above it.  A row whose sum has passed SUM_MOST is scaled down before the next chunk;
 // one that overflows within a chunk, by scores some 46 above all before, is computed again at the end, by its warp, like one that met
-// a value that is not finite.
-// At hd 64 the warps' latencies and issue bound it (16 softmax warps an SM: 183 us, 750 TFLOP/s of what the tokens see, at the sizes above,
-// 1080 over all of 8000 tokens), at hd 128 the tensor pipe, 75% active (655 us, 1640 TFLOP/s; 710, 1510, at the power cap).
+// a value that is not finite (0.3 to 0.8 ms a row and 4096 positions; a tile that sees such a value has 128 of them).
+// At hd 64 the warps' latencies and issue bound it (16 softmax warps an SM: 174 us, 785 TFLOP/s of what the tokens see, at the sizes above,
+// 1080 over all of 8000 tokens), at hd 128 the tensor pipe, 70% active (692 us, 1550 TFLOP/s; 740, 1450, at the power cap).
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -706,9 +706,7 @@ __global__ void __launch_bounds__(WC_THREADS) window_cores_kernel(const AttnArgs
     const long long kv_off = (long long)(c / a.L) * a.s0 + (long long)(c % a.L) * a.s1 + (long long)g * a.s2;
     const T* Kc = static_cast<const T*>(a.K) + kv_off;
     const T* Vc = static_cast<const T*>(a.V) + kv_off;
-    if constexpr (sizeof(T) == 4) {
-        pdl_wait();
-        }
+    if constexpr (sizeof(T) == 4) pdl_wait();
     // row i of the tile: head h0 + i / toks, token r0 + i % toks
     auto q_at = [&](int i) { return (((size_t)c * a.n_q + (size_t)g * a.group + h0 + i / toks) * a.Lq + r0 + i % toks) * HD; };
     wc_stage<T, HD, WC_ROWS>(Qs, rows, vec_q, a.scale, [&](int i) { return static_cast<const T*>(a.Q) + q_at(i); });

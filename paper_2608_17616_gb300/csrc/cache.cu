@@ -381,7 +381,8 @@ cudaError_t launch_cache_evict(const DevState& s, const CacheView& v, int keep, 
                                float* to_score, int* kept, int* lens_out, cudaStream_t st) {
     const int el = s.dtype == 0 ? 4 : 2;
     EvictArgs a{v, keep, n_sink, n_recent, s.hd, to, to_width, (long long)to_width << v.page_log2, to_score, kept, lens_out};
-    // A row over as many CTAs of a cluster as the SMs hold, two each, and slices of SEL_SLICE positions.  (128 rows of 2K take
+    // A row over as many CTAs of a cluster as the SMs hold, two each, and slices of SEL_SLICE positions of what the table covers (the
+    // lengths are on the device).  (128 rows of 2K take
     // 14.1 us with their compaction on one CTA each, 17.8 on two; 64 rows of 32K 99, 84, 80 and 82 on one, two, four and eight; 8
     // rows of 120000 202 on one and 98 on eight.)
     const long long rows = (long long)v.n_ctx * v.L * v.n_kv;
