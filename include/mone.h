@@ -388,6 +388,147 @@ mone_status mone_cache_evict(mone_mem* m, int layer, const mone_cache* cache, in
                              const int* to_table, int to_width, float* to_score, int* kept, int* lens_out, void* stream);
 
 /*
+ * A paged cache held in 4 bits: mone_cache's, whose rows are cut into groups of 16 values.  An element is
+ *     2^exp * scale * code,
+ * the scale an unsigned e4m3 number of its group (0 .. 448), the code an e2m1 number: 0, 0.5, 1, 1.5, 2, 3, 4 or 6 and a sign.  A row takes
+ * head_dim / 2 + head_dim / 16 bytes, 3.6 times less than in bf16; every element is exact in bf16.
+ *   K, V              codes, two to a byte, the even element in the low half; 16-byte aligned, element strides (layer, page, KV head, position
+ *                     in the page) in bytes, multiples of 16, the head_dim / 2 bytes of a row contiguous
+ *   K_scale, V_scale  scales, scale_strides likewise, multiples of head_dim / 16 as are the addresses, the head_dim / 16 bytes of
+ *                     a row contiguous
+ *   k_exp, v_exp      -64 .. 64: powers of two that bring keys and values to the range that codes and scales have
+ *                     (2688 at most, 2^-10 at least)
+ * and the rest as in mone_cache.
+ */
+typedef struct {
+    void *K, *V, *K_scale, *V_scale;
+    long long strides[4], scale_strides[4];
+    int k_exp, v_exp;
+    int n_pages, page_size;
+    const int* table; /* [n_ctx][table_width] */
+    int table_width;
+    const int* lens;  /* [n_ctx] */
+    float* score;
+} mone_cache4;
+
+/*
+ * mone_cache_append into a 4-bit cache: the same arguments.  Of a group's 16 values x the scale is max |x| / 6 / 2^exp, rounded to e4m3, and an
+ * element's code x / (2^exp scale), rounded to e2m1: both to the nearest, ties to even, the largest for what is larger.  A
+ * group that holds a NaN becomes NaN; an infinity counts as the largest element (2688 * 2^exp).
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (page_size).
+ */
+mone_status mone_cache4_append(mone_mem* m, int layer, const mone_cache4* cache, const void* K, const void* V,
+                               const long long strides[4], int n_tok, const int* counts, int* lens_out, void* stream);
+
+/*
+ * A context's positions as dense keys and values of the handle's type: positions from[c] .. from[c] + n_pos - 1 of every context to places
+ * 0 .. n_pos - 1, for mone_window_attention of a prompt's next tokens, say.  Places of positions that the context does not hold stay
+ * as they are.
+ *   from   NULL (0), or [n_ctx] (device, >= 0): each context's first position
+ *   K, V   element strides (context, layer, KV head, place), head_dim contiguous
+ * Constraints: 1 <= n_pos <= 2^20.  Errors: INVALID_ARG, UNSUPPORTED_SHAPE (page_size).
+ */
+mone_status mone_cache4_read(mone_mem* m, int layer, const mone_cache4* cache, const int* from, int n_pos, void* K, void* V,
+                             const long long strides[4], void* stream);
+
+/*
+ * mone_cache_attention over a 4-bit cache: the same arguments, masks, weights, workspace and constraints, errors too.  Sums and
+ * softmax are held in 32 bits; with a bf16 handle the probabilities are rounded to 11 bits for their product with the values, with an
+ * fp32 handle queries and probabilities to 22.
+ */
+mone_status mone_cache4_attention(mone_mem* m, int layer, const mone_cache4* cache, const void* Q, int n_q_heads, int n_tok,
+                                  int n_sink, int window, void* out, void* stream);
+
+/* mone_cache_evict of a 4-bit cache: the same arguments, rows moved as they are. */
+mone_status mone_cache4_evict(mone_mem* m, int layer, const mone_cache4* cache, int keep, int n_sink, int n_recent,
+                              const int* to_table, int to_width, float* to_score, int* kept, int* lens_out, void* stream);
+
+/*
+ * The pages of a pool that nobody holds, and the tables that hold the others, all in device memory, so that a captured graph
+ * can serve contexts that grow into new pages.
+ *   free    [n_pages] (room for every page): the free pages are its first *n_free entries
+ *   table   [n_ctx][table_width] as in mone_cache, for every layer; n_pages and page_size too
+ *   lens    [n_ctx] positions that each context holds: it has the pages of those
+ * Calls that share a list or a table are ordered by the caller (one stream, say).
+ */
+typedef struct {
+    int* free;
+    const int* n_free; /* [1] */
+    int n_pages, page_size;
+    int* table;
+    int table_width;
+    const int* lens;
+} mone_pages;
+
+/*
+ * Pages for each context's next tokens: the entries of its table that lens + counts positions need beyond those of its lens positions
+ * are taken from the end of the free list, context after context in the list's order.  A context is served in full or not at
+ * all: it gets its pages and tokens if it needs no page, or if the pages that it and all contexts before it need are
+ * there.  One whose table is too narrow gets nothing, and its pages do not count.
+ *   n_tok      tokens of each context; counts: NULL, or how many of them (device, 0 .. n_tok)
+ *   granted    NULL, or [n_ctx] (not counts itself): the context's tokens, or 0; mone_cache_append's counts
+ *   slots      NULL, or [n_ctx][n_tok]: where token i of a context goes, page * page_size + place; -1 past the granted ones
+ *   lens_out   NULL, or [n_ctx] (not lens itself): the lengths with the granted tokens
+ *   n_free_out [1] (not n_free itself): the free pages left
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE (page_size).  A length, count of free pages or page outside its range is latched as
+ * MONE_ERR_CHECK; nothing outside the lists and tables is read or written.
+ */
+mone_status mone_cache_reserve(mone_mem* m, const mone_pages* pages, int n_tok, const int* counts, int* granted, long long* slots,
+                               int* lens_out, int* n_free_out, void* stream);
+
+/*
+ * Pages given back: those that hold no position below `keep` any more go to the end of the free list, context after context, and
+ * their table entries become -1.  (A request has ended, drafted tokens were rejected, a cache has been evicted to other
+ * pages.)  After a mone_cache_reserve of the same contexts, with its lens_out as lens and its lens as keep, list and tables are as before it.
+ *   keep       NULL (0), or [n_ctx] (device): positions that each context keeps, its length at most
+ *   lens_out   NULL, or [n_ctx] (not lens itself): min(lens, keep); n_free_out [1] (not n_free itself)
+ * Errors as above.
+ */
+mone_status mone_cache_release(mone_mem* m, const mone_pages* pages, const int* keep, int* lens_out, int* n_free_out, void* stream);
+
+/*
+ * Queries and keys of new tokens, each head divided by its root mean square and scaled, then rotated by its position, in one pass.
+ * For a row x of a head: with a weight w, x_d becomes x_d w_d / sqrt(mean(x^2) + eps); then pair i of its first rot_dim elements, (a, b),
+ * becomes (a cos f - b sin f, b cos f + a sin f) with f = p freq_i at position p, or p mod period (the segment-local positions of the
+ * paper's keys).  MONE_ROTATE_HALVES: pair i is elements i and i + rot_dim / 2; MONE_ROTATE_NEIGHBOURS: 2 i and 2 i + 1.
+ *
+ * mone_rotary is made once, on the host, by mone_rotary_make, from the frequencies freq[rot_dim / 2] in radians per position, or where
+ * freq is NULL from freq_i = base^(-2 i / rot_dim).  It holds each as a 64-bit fraction of a turn, so that an angle is a product of whole numbers
+ * whose overflow is its reduction, exact at any position; the table goes with each launch, so the struct may go after the call.
+ * Constraints: rot_dim a multiple of 16, 0 .. 128; |freq_i| < 2^31; period >= 0 (0: none); eps >= 0.  Errors: INVALID_ARG.
+ */
+enum { MONE_ROTATE_HALVES = 0, MONE_ROTATE_NEIGHBOURS = 1 };
+typedef struct {
+    int rot_dim, pairing, period;
+    float eps;
+    unsigned long long turns[64];
+} mone_rotary;
+mone_status mone_rotary_make(mone_rotary* r, int rot_dim, int pairing, const double* freq, double base, int period, float eps);
+
+/*
+ * The rows of one side, queries or keys.
+ *   x, out  the call's layers of the handle's dtype, element strides (context, layer, head, token), head_dim contiguous; out may be x
+ *           with the same strides, and overlaps it in no other way
+ *   weight  NULL (rows are rotated as they are), or [n_layers][head_dim] fp32, the handle's layers
+ */
+typedef struct {
+    const void* x;
+    void* out;
+    const float* weight;
+    long long strides[4], out_strides[4];
+    int n_heads;
+} mone_heads;
+
+/*
+ *   q, k    one of them may be NULL
+ *   first   NULL (0), or [n_ctx] (device, >= 0): the position of each context's first token (its length in a cache, say)
+ * Sums of squares and rotations are in 32 bits and rounded once.  Constraints: rot_dim <= head_dim; 1 <= n_tok <= 2^24; n_heads <= 4096.
+ * Errors: INVALID_ARG.  Asynchronous on stream.
+ */
+mone_status mone_norm_rotate(mone_mem* m, int layer, const mone_rotary* rotary, const int* first, int n_tok, const mone_heads* q,
+                             const mone_heads* k, void* stream);
+
+/*
  * Per-kernel device timing for measurement.  While enabled, the library records
  * a pair of CUDA events on the caller's stream around every kernel it launches
  * (this adds host work per launch; leave it off outside measurement).
@@ -399,7 +540,8 @@ mone_status mone_cache_evict(mone_mem* m, int layer, const mone_cache* cache, in
  * target, MONE_LOSS_MSE only), 6 consumer attention, 7 resident chains (the fp32 MLP
  * path when d_in + d_out <= 512: every segment of an input window in one launch,
  * forward, backward and update together), 8 host-input gathers (mone_ttl_context_host;
- * timed on the library's staging stream), 9 paged-cache operators (mone_cache_*).  The windowed
+ * timed on the library's staging stream), 9 paged-cache operators (mone_cache_*,
+ * mone_cache4_*, mone_norm_rotate).  The windowed
  * attention counts as kind 6.  Errors: INVALID_ARG, CUDA.
  */
 mone_status mone_mem_set_timing(mone_mem* m, int enable);

@@ -78,6 +78,8 @@ them).
 from __future__ import annotations
 
 import dataclasses
+import functools
+from fractions import Fraction
 from typing import Optional
 
 import numpy as np
@@ -438,3 +440,92 @@ def cache_keep(score, keep: int, n_sink: int, n_recent: int):
         return np.arange(n)
     rank = sorted(range(n_sink, n - n_recent), key=lambda p: (-(-np.inf if np.isnan(score[p]) else score[p]), p))
     return np.array(sorted([*range(n_sink), *rank[:keep - n_sink - n_recent], *range(n - n_recent, n)]), dtype=int)
+
+
+# --------------------------------------------------------------------------- rows in 4 bits
+
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+E4M3 = np.array([m / 512 for m in range(8)] + [(8 + m) * 2.0 ** (e - 10) for e in range(1, 16) for m in range(8)][:119])
+
+
+def _nearest_even(x, numbers):
+    """Index of the number nearest to x >= 0, ties to the even index, the last one from there on."""
+    mid = (numbers[1:] + numbers[:-1]) / 2
+    below, upto = np.searchsorted(mid, x, side="left"), np.searchsorted(mid, x, side="right")
+    return np.where((below != upto) & (below % 2 == 1), upto, below)
+
+
+def four_bits(x, exp: int = 0):
+    """Rows x [.., d] as codes [.., d] (0 .. 15) and e4m3 scales [.., d / 16] (0 .. 127) of groups of 16: the scale max |x| / 6 / 2^exp, a
+    code x / (2^exp scale), each to the nearest, ties to even, saturating; a group that holds a NaN has the NaN scale 127."""
+    x = f64(x)
+    g = x.reshape(*x.shape[:-1], x.shape[-1] // 16, 16) * 2.0 ** -exp
+    bad = np.isnan(g).any(-1)
+    g = np.where(bad[..., None], 0.0, g)
+    scale = _nearest_even(np.abs(g).max(-1) / 6, E4M3)
+    s = E4M3[scale][..., None]
+    code = _nearest_even(np.divide(np.minimum(np.abs(g), 1e9), s, out=np.zeros_like(g), where=s > 0), E2M1)
+    code = np.where(s > 0, code + 8 * np.signbit(g), 0)
+    return code.reshape(x.shape).astype(np.uint8), np.where(bad, 127, scale).astype(np.uint8)
+
+
+def four_bit_values(code, scale, exp: int = 0):
+    """The values [.., d] of codes [.., d] and scales [.., d / 16]; the scale 127 is NaN."""
+    code, scale = np.asarray(code), np.asarray(scale)
+    s = np.where(scale == 127, np.nan, E4M3[np.minimum(scale, 126)])
+    return np.where(code >= 8, -1.0, 1.0) * E2M1[code & 7] * np.repeat(s, 16, -1) * 2.0 ** exp
+
+
+# --------------------------------------------------------------------------- heads normalised and rotated
+
+@functools.lru_cache(maxsize=64)
+def _angles(positions, freq):
+    """positions x freq without their whole turns, [positions, len(freq)]: a product past 2^53 has lost its place in the turn."""
+    pi = Fraction(314159265358979323846264338327950288419716939937510582097494459230781640628620899, 10 ** 80)
+    turns = [int(Fraction(q) / (2 * pi) * 2 ** 160) for q in freq]
+    return np.array([[(p * t % 2 ** 160) / 2 ** 160 * 2 * np.pi for t in turns] for p in positions]).reshape(len(positions), len(freq))
+
+
+def norm_rotate(x, weight, positions, freq, halves: bool, eps: float):
+    """Rows x [n, d_h] at positions [n]: with a weight [d_h], x w / sqrt(mean(x^2) + eps); then pair i of the first 2 len(freq) elements,
+    (a, b), turned by positions * freq[i].  halves: pair i is elements i and i + len(freq), else 2 i and 2 i + 1."""
+    y = f64(x).copy()
+    if weight is not None:
+        y = y / np.sqrt((y * y).mean(-1, keepdims=True) + eps) * f64(weight)
+    n = len(freq)
+    a, b = (slice(0, n), slice(n, 2 * n)) if halves else (slice(0, 2 * n, 2), slice(1, 2 * n, 2))
+    f = _angles(tuple(int(p) for p in positions), tuple(float(q) for q in freq))
+    y[:, a], y[:, b] = y[:, a] * np.cos(f) - y[:, b] * np.sin(f), y[:, b] * np.cos(f) + y[:, a] * np.sin(f)
+    return y
+
+
+# --------------------------------------------------------------------------- pages
+
+def cache_reserve(free, table, lens, counts, page: int, width: int):
+    """Pages for counts[c] more positions of each context, from the end of the list `free`: context after context, each in full or not at
+    all, as long as the pages that it and those before it need are there (a context whose table would be too wide needs none).  Returns
+    the list, the tables (lists of pages), the granted counts and each granted token's slot."""
+    need = [0 if n + k > width * page else -(-(n + k) // page) - -(-n // page) for n, k in zip(lens, counts)]
+    granted, new, asked = [], [], 0
+    for n, k, m in zip(lens, counts, need):
+        asked += m
+        ok = n + k <= width * page and (m == 0 or asked <= len(free))
+        granted.append(k if ok else 0)
+        new.append(m if ok and k else 0)
+    top = len(free) - sum(new)
+    taken, tables = top, []
+    for t, m in zip(table, new):
+        tables.append(list(t) + list(free[taken:taken + m]))
+        taken += m
+    slots = [[t[p // page] * page + p % page for p in range(n, n + k)] for t, n, k in zip(tables, lens, granted)]
+    return list(free[:top]), tables, granted, slots
+
+
+def cache_release(free, table, lens, keep, page: int):
+    """The list and the tables after the pages without a position below min(keep, lens) have gone back, context after context."""
+    free, tables = list(free), []
+    for t, n, k in zip(table, lens, keep):
+        stay = -(-min(max(k, 0), n) // page)
+        tables.append(list(t[:stay]))
+        free += t[stay:-(-n // page)]
+    return free, tables

@@ -24,6 +24,7 @@ MONE_LOSS_DOT, MONE_LOSS_MSE = 0, 1
 MONE_MEM_MLP, MONE_MEM_SWIGLU = 0, 1
 MONE_RENORM_ROWS, MONE_RENORM_OUT = 0, 1
 MONE_GATE_LINEAR, MONE_GATE_SILU = 0, 1
+MONE_ROTATE_HALVES, MONE_ROTATE_NEIGHBOURS = 0, 1
 MONE_ALL_LAYERS = -1
 
 STATUS = {0: "MONE_OK", 1: "MONE_ERR_INVALID_ARG", 2: "MONE_ERR_UNSUPPORTED_SHAPE", 3: "MONE_ERR_OOM",
@@ -36,7 +37,8 @@ EXPORTS = ("mone_mem_init", "mone_ttl_segment", "mone_ttl_context", "mone_mem_ge
            "mone_status_string", "mone_abi_version", "mone_mem_set_timing", "mone_mem_kernel_time",
            "mone_last_error", "mone_mem_generate_kv_noalloc", "mone_attention", "mone_mem_kernel_busy",
            "mone_ttl_context_metrics", "mone_ttl_context_host", "mone_window_attention", "mone_cache_append",
-           "mone_cache_attention", "mone_cache_evict")
+           "mone_cache_attention", "mone_cache_evict", "mone_cache4_append", "mone_cache4_read", "mone_cache4_attention",
+           "mone_cache4_evict", "mone_cache_reserve", "mone_cache_release", "mone_rotary_make", "mone_norm_rotate")
 
 KERNEL_KINDS = ("prepass", "phase_a", "phase_b", "finalize", "read", "mse", "attention", "resident", "stage",
                  "cache")
@@ -72,6 +74,32 @@ class mone_cache(ctypes.Structure):
     _fits = None  # the handle's that they were found to do for
 
 
+class mone_cache4(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("K_scale", ctypes.c_void_p), ("V_scale", ctypes.c_void_p),
+                ("strides", _LL4), ("scale_strides", _LL4), ("k_exp", ctypes.c_int), ("v_exp", ctypes.c_int),
+                ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int), ("table", ctypes.c_void_p),
+                ("table_width", ctypes.c_int), ("lens", ctypes.c_void_p), ("score", ctypes.c_void_p)]
+    _of = None  # make_cache4's, as mone_cache's (no dtype)
+    _fits = None
+
+
+class mone_pages(ctypes.Structure):
+    _fields_ = [("free", ctypes.c_void_p), ("n_free", ctypes.c_void_p), ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("table", ctypes.c_void_p), ("table_width", ctypes.c_int), ("lens", ctypes.c_void_p)]
+    _of = None  # make_pages': its contexts
+
+
+class mone_rotary(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int), ("pairing", ctypes.c_int), ("period", ctypes.c_int), ("eps", ctypes.c_float),
+                ("turns", ctypes.c_ulonglong * 64)]
+
+
+class mone_heads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("strides", _LL4),
+                ("out_strides", _LL4), ("n_heads", ctypes.c_int)]
+    _of = None  # make_heads': contexts, layers, tokens, head_dim, dtype, layers of its weight
+
+
 _lib = None
 _types = {}  # torch's, by name
 _handles = {}  # a live handle's layers, contexts, KV heads, head_dim and dtype
@@ -101,6 +129,14 @@ def lib(path: Optional[str] = None) -> ctypes.CDLL:
         "mone_cache_append": ([vp, i, ctypes.POINTER(mone_cache), vp, vp, ctypes.POINTER(ll), i, vp, vp, vp], i),
         "mone_cache_attention": ([vp, i, ctypes.POINTER(mone_cache), vp, i, i, i, i, vp, vp], i),
         "mone_cache_evict": ([vp, i, ctypes.POINTER(mone_cache), i, i, i, vp, i, vp, vp, vp, vp], i),
+        "mone_cache4_append": ([vp, i, ctypes.POINTER(mone_cache4), vp, vp, ctypes.POINTER(ll), i, vp, vp, vp], i),
+        "mone_cache4_read": ([vp, i, ctypes.POINTER(mone_cache4), vp, i, vp, vp, ctypes.POINTER(ll), vp], i),
+        "mone_cache4_attention": ([vp, i, ctypes.POINTER(mone_cache4), vp, i, i, i, i, vp, vp], i),
+        "mone_cache4_evict": ([vp, i, ctypes.POINTER(mone_cache4), i, i, i, vp, i, vp, vp, vp, vp], i),
+        "mone_cache_reserve": ([vp, ctypes.POINTER(mone_pages), i, vp, vp, vp, vp, vp, vp], i),
+        "mone_cache_release": ([vp, ctypes.POINTER(mone_pages), vp, vp, vp, vp], i),
+        "mone_rotary_make": ([ctypes.POINTER(mone_rotary), i, i, ctypes.POINTER(ctypes.c_double), ctypes.c_double, i, f], i),
+        "mone_norm_rotate": ([vp, i, ctypes.POINTER(mone_rotary), vp, i, ctypes.POINTER(mone_heads), ctypes.POINTER(mone_heads), vp], i),
         "mone_mem_free": ([vp], i),
         "mone_mem_read_state": ([vp, vp, vp, vp, vp, vp], i),
         "mone_mem_write_state": ([vp, vp, vp, vp, vp, vp], i),
@@ -262,6 +298,21 @@ def _buffer(name: str, t, dtype: str, at_least: int, shape: str):
         raise ValueError(f"{name}: a contiguous {dtype} tensor {shape}, not {tuple(t.shape)}, {t.dtype}")
 
 
+def _tables(table, lens, score, page: int):
+    """Checks a cache's table, lengths and scores; contexts and entries of the table."""
+    for name, t, dims in (("table", table, 2), ("lens", lens, 1), ("score", score, 4)):
+        if t is not None and t.dim() != dims:
+            raise ValueError(f"{name}: a tensor of {dims} dimensions")
+    n_ctx, width = table.shape
+    _buffer("table", table, "int32", 1, "[contexts, width]")
+    _buffer("lens", lens, "int32", n_ctx, "[contexts]")
+    if score is not None:
+        _buffer("score", score, "float32", 1, "[contexts, layers, KV heads, width * page_size]")
+        if score.shape[0] < n_ctx or score.shape[3] != width * page:
+            raise ValueError(f"score: [{n_ctx} contexts, layers, KV heads, {width} * {page}], not {tuple(score.shape)}")
+    return n_ctx, width
+
+
 def make_cache(K, V, table, lens, score=None) -> mone_cache:
     """A paged cache over torch tensors: K, V [layers, pages, KV heads, page_size, head_dim] of any strides with head_dim
     contiguous (K.stride() == V.stride()), table [contexts, width] and lens [contexts] int32, score
@@ -271,27 +322,18 @@ def make_cache(K, V, table, lens, score=None) -> mone_cache:
     dtype = {"torch.float32": MONE_FP32, "torch.bfloat16": MONE_BF16}.get(str(K.dtype))
     if dtype is None:
         raise ValueError("K and V: float32 or bfloat16")
-    for name, t, dims in (("table", table, 2), ("lens", lens, 1), ("score", score, 4)):
-        if t is not None and t.dim() != dims:
-            raise ValueError(f"{name}: a tensor of {dims} dimensions")
     n_layers, n_pages, n_kv, page, hd = K.shape
-    n_ctx, width = table.shape
-    _buffer("table", table, "int32", 1, "[contexts, width]")
-    _buffer("lens", lens, "int32", n_ctx, "[contexts]")
-    if score is not None:
-        _buffer("score", score, "float32", 1, "[contexts, layers, KV heads, width * page_size]")
-        if score.shape[0] < n_ctx or score.shape[3] != width * page:
-            raise ValueError(f"score: [{n_ctx} contexts, layers, KV heads, {width} * {page}], not {tuple(score.shape)}")
+    n_ctx, width = _tables(table, lens, score, page)
     c = mone_cache(_ptr(K), _ptr(V), _LL4(*K.stride()[:4]), n_pages, page, _ptr(table), width, _ptr(lens), _ptr(score))
     c._of = (n_layers, n_ctx, n_kv, hd, dtype, None if score is None else tuple(score.shape[1:3]))
     return c
 
 
-def _cache(h: int, cache: mone_cache):
+def _cache(h: int, cache):
     need = _handles.get(h)
     if cache._fits is not need:
         of = cache._of
-        if None not in (of, need) and (of[4] != need[4] or any(a < b for a, b in zip(of[:4], need)) or of[5] not in (None, need[0:3:2])):
+        if None not in (of, need) and (of[4] not in (None, need[4]) or any(a < b for a, b in zip(of[:4], need)) or of[5] not in (None, need[0:3:2])):
             raise ValueError(f"the cache's layers, contexts, KV heads, head_dim, dtype (and its score's layers and KV heads) are {of}, "
                              f"the handle's {need}")
         cache._fits = need
@@ -313,21 +355,167 @@ def mone_cache_attention(h: int, layer: int, cache: mone_cache, Q, n_q_heads: in
                                                               window, _ptr(out), _stream(stream)))
 
 
-def mone_cache_evict(h: int, layer: int, cache: mone_cache, keep: int, n_sink: int, n_recent: int, to_table, to_score, kept,
-                     lens_out=None, stream=None):
-    """The first n_sink positions, the last n_recent and the best scored others, `keep` in all, into the pages of to_table
-    [contexts, width]; to_score and kept as in the header."""
+def _targets(h: int, layer: int, page: int, keep: int, to_table, to_score, kept) -> int:
+    """Checks an eviction's targets; entries of their table."""
     width, need = to_table.shape[1], _handles.get(h)
     if need is not None:
         n_layers, n_ctx, n_kv = need[:3]
-        per, rows = width * cache.page_size, n_ctx * n_kv
+        per, rows = width * page, n_ctx * n_kv
         _buffer("to_table", to_table, "int32", n_ctx * width, "[contexts, width]")
         _buffer("to_score", to_score, "float32", rows * n_layers * per, "[contexts, layers, KV heads, width * page_size]")
         _buffer("kept", kept, "int32", rows * (n_layers if layer == MONE_ALL_LAYERS else 1) * keep, "[contexts, layers, KV heads, keep]")
         if getattr(to_score, "ndim", 0) == 4 and to_score.shape[1:] != (n_layers, n_kv, per):
             raise ValueError(f"to_score: [contexts, {n_layers}, {n_kv}, {per}], not {tuple(to_score.shape)}")
+    return width
+
+
+def mone_cache_evict(h: int, layer: int, cache: mone_cache, keep: int, n_sink: int, n_recent: int, to_table, to_score, kept,
+                     lens_out=None, stream=None):
+    """The first n_sink positions, the last n_recent and the best scored others, `keep` in all, into the pages of to_table
+    [contexts, width]; to_score and kept as in the header."""
+    width = _targets(h, layer, cache.page_size, keep, to_table, to_score, kept)
     _check("mone_cache_evict", lib().mone_cache_evict(h, layer, _cache(h, cache), keep, n_sink, n_recent, _ptr(to_table), width,
                                                       _ptr(to_score), _ptr(kept), _ptr(lens_out), _stream(stream)))
+
+
+def make_cache4(K, V, K_scale, V_scale, table, lens, score=None, k_exp=0, v_exp=0) -> mone_cache4:
+    """A paged cache in 4 bits over torch tensors: K, V [layers, pages, KV heads, page_size, head_dim / 2] uint8 of any strides
+    with the last dimension contiguous (K.stride() == V.stride()), K_scale, V_scale [.., head_dim / 16] likewise, uint8 or
+    float8_e4m3fn; the rest as for make_cache.  It holds their addresses, not the tensors: keep them alive."""
+    for x, y in ((K, V), (K_scale, V_scale)):
+        if x.stride() != y.stride() or x.shape != y.shape or x.dtype != y.dtype or x.dim() != 5 or x.stride(4) != 1:
+            raise ValueError("K and V, and their scales: [layers, pages, KV heads, page_size, head_dim / 2 (/ 16)], the same strides, the "
+                             "last dimension contiguous")
+    if str(K.dtype) != "torch.uint8" or str(K_scale.dtype) not in ("torch.uint8", "torch.float8_e4m3fn"):
+        raise ValueError("codes: uint8; scales: uint8 or float8_e4m3fn")
+    n_layers, n_pages, n_kv, page, half = K.shape
+    if K_scale.shape[:4] != K.shape[:4] or 8 * K_scale.shape[4] != half:
+        raise ValueError(f"scales: {(*K.shape[:4], half // 8)}, not {tuple(K_scale.shape)}")
+    n_ctx, width = _tables(table, lens, score, page)
+    c = mone_cache4(_ptr(K), _ptr(V), _ptr(K_scale), _ptr(V_scale), _LL4(*K.stride()[:4]), _LL4(*K_scale.stride()[:4]), k_exp, v_exp,
+                    n_pages, page, _ptr(table), width, _ptr(lens), _ptr(score))
+    c._of = (n_layers, n_ctx, n_kv, 2 * half, None, None if score is None else tuple(score.shape[1:3]))
+    return c
+
+
+def mone_cache4_append(h: int, layer: int, cache: mone_cache4, K, V, strides: Sequence[int], n_tok: int, lens_out=None, counts=None,
+                       stream=None):
+    """New tokens' keys and values, rounded to 4 bits, after each context's positions."""
+    arr = _strides(strides)
+    _check("mone_cache4_append", lib().mone_cache4_append(h, layer, _cache(h, cache), _ptr(K), _ptr(V), arr, n_tok, _ptr(counts),
+                                                          _ptr(lens_out), _stream(stream)))
+
+
+def mone_cache4_read(h: int, layer: int, cache: mone_cache4, first, n_pos: int, K, V, strides: Sequence[int], stream=None):
+    """Positions first[c] .. first[c] + n_pos - 1 (None: from 0) of each context as dense keys and values."""
+    arr = _strides(strides)
+    _check("mone_cache4_read", lib().mone_cache4_read(h, layer, _cache(h, cache), _ptr(first), n_pos, _ptr(K), _ptr(V), arr,
+                                                      _stream(stream)))
+
+
+def mone_cache4_attention(h: int, layer: int, cache: mone_cache4, Q, n_q_heads: int, n_tok: int, n_sink: int, window: int, out,
+                          stream=None):
+    """mone_cache_attention over a 4-bit cache."""
+    _check("mone_cache4_attention", lib().mone_cache4_attention(h, layer, _cache(h, cache), _ptr(Q), n_q_heads, n_tok, n_sink,
+                                                                window, _ptr(out), _stream(stream)))
+
+
+def mone_cache4_evict(h: int, layer: int, cache: mone_cache4, keep: int, n_sink: int, n_recent: int, to_table, to_score, kept,
+                      lens_out=None, stream=None):
+    """mone_cache_evict of a 4-bit cache."""
+    width = _targets(h, layer, cache.page_size, keep, to_table, to_score, kept)
+    _check("mone_cache4_evict", lib().mone_cache4_evict(h, layer, _cache(h, cache), keep, n_sink, n_recent, _ptr(to_table), width,
+                                                        _ptr(to_score), _ptr(kept), _ptr(lens_out), _stream(stream)))
+
+
+def make_pages(free, n_free, table, lens, page_size: int) -> mone_pages:
+    """The free pages of a pool of free.numel() pages and the contexts' tables, int32: free [pages], n_free [1], table
+    [contexts, width], lens [contexts].  It holds their addresses, not the tensors: keep them alive."""
+    for name, t, dims in (("free", free, 1), ("n_free", n_free, 1), ("table", table, 2), ("lens", lens, 1)):
+        if t.dim() != dims:
+            raise ValueError(f"{name}: a tensor of {dims} dimensions")
+        _buffer(name, t, "int32", 1, f"of {dims} dimensions")
+    n_ctx, width = table.shape
+    _buffer("lens", lens, "int32", n_ctx, "[contexts]")
+    p = mone_pages(_ptr(free), _ptr(n_free), free.numel(), page_size, _ptr(table), width, _ptr(lens))
+    p._of = n_ctx
+    return p
+
+
+def _pages(h: int, pages: mone_pages):
+    need = _handles.get(h)
+    if None not in (pages._of, need) and pages._of < need[1]:
+        raise ValueError(f"pages of {pages._of} contexts, the handle has {need[1]}")
+    return ctypes.byref(pages), need[1] if need else 1
+
+
+def mone_cache_reserve(h: int, pages: mone_pages, n_tok: int, n_free_out, lens_out=None, granted=None, slots=None, counts=None,
+                       stream=None):
+    """Pages for each context's next n_tok (or counts) tokens from the free list, and the tokens' slots [contexts, n_tok] int64."""
+    ref, n_ctx = _pages(h, pages)
+    for name, t, dtype, n, shape in (("n_free_out", n_free_out, "int32", 1, "[1]"), ("lens_out", lens_out, "int32", n_ctx, "[contexts]"),
+                                     ("granted", granted, "int32", n_ctx, "[contexts]"), ("counts", counts, "int32", n_ctx, "[contexts]"),
+                                     ("slots", slots, "int64", n_ctx * n_tok, "[contexts, n_tok]")):
+        if t is not None:
+            _buffer(name, t, dtype, n, shape)
+    _check("mone_cache_reserve", lib().mone_cache_reserve(h, ref, n_tok, _ptr(counts), _ptr(granted), _ptr(slots), _ptr(lens_out),
+                                                          _ptr(n_free_out), _stream(stream)))
+
+
+def mone_cache_release(h: int, pages: mone_pages, n_free_out, keep=None, lens_out=None, stream=None):
+    """The pages that hold no position below keep (None: 0) back to the free list."""
+    ref, n_ctx = _pages(h, pages)
+    for name, t, n, shape in (("n_free_out", n_free_out, 1, "[1]"), ("lens_out", lens_out, n_ctx, "[contexts]"),
+                              ("keep", keep, n_ctx, "[contexts]")):
+        if t is not None:
+            _buffer(name, t, "int32", n, shape)
+    _check("mone_cache_release", lib().mone_cache_release(h, ref, _ptr(keep), _ptr(lens_out), _ptr(n_free_out), _stream(stream)))
+
+
+def make_rotary(rot_dim: int, pairing: int = MONE_ROTATE_HALVES, base: float = 10000.0, freq: Optional[Sequence[float]] = None,
+                period: int = 0, eps: float = 1e-6) -> mone_rotary:
+    """The rotation of mone_norm_rotate: frequencies freq [rot_dim / 2] in radians per position, or base^(-2 i / rot_dim)."""
+    r = mone_rotary()
+    if freq is not None and len(freq) != rot_dim // 2:
+        raise ValueError(f"freq: {rot_dim // 2} frequencies, not {len(freq)}")
+    arr = None if freq is None else (ctypes.c_double * max(len(freq), 1))(*[float(x) for x in freq])
+    _check("mone_rotary_make", lib().mone_rotary_make(ctypes.byref(r), rot_dim, pairing, arr, base, period, eps))
+    return r
+
+
+def make_heads(x, out, weight=None) -> mone_heads:
+    """One side of mone_norm_rotate: x, out [contexts, the call's layers, heads, tokens, head_dim] of any strides with head_dim contiguous,
+    weight [the handle's layers, head_dim] fp32 or None.  It holds their addresses, not the tensors: keep them alive."""
+    if x.shape != out.shape or x.dtype != out.dtype or x.dim() != 5 or x.stride(4) != 1 or out.stride(4) != 1:
+        raise ValueError("x and out: [contexts, layers, heads, tokens, head_dim], the same type, head_dim contiguous")
+    dtype = {"torch.float32": MONE_FP32, "torch.bfloat16": MONE_BF16}.get(str(x.dtype))
+    if dtype is None:
+        raise ValueError("x and out: float32 or bfloat16")
+    if weight is not None:
+        _buffer("weight", weight, "float32", 1, "[layers, head_dim]")
+        if weight.dim() != 2 or weight.shape[1] != x.shape[4]:
+            raise ValueError(f"weight: [layers, {x.shape[4]}], not {tuple(weight.shape)}")
+    s = mone_heads(_ptr(x), _ptr(out), _ptr(weight), _LL4(*x.stride()[:4]), _LL4(*out.stride()[:4]), x.shape[2])
+    s._of = (x.shape[0], x.shape[1], x.shape[3], x.shape[4], dtype, None if weight is None else weight.shape[0])
+    return s
+
+
+def mone_norm_rotate(h: int, layer: int, rotary: mone_rotary, first, n_tok: int, q: Optional[mone_heads], k: Optional[mone_heads],
+                     stream=None):
+    """Queries and keys normalised by head and rotated by position; first [contexts] int32: the first token's (None: 0)."""
+    need = _handles.get(h)
+    if need is not None:
+        for side in (q, k):
+            of = side._of if side is not None else None
+            if of is not None and (of[0] < need[1] or of[1] < (need[0] if layer == MONE_ALL_LAYERS else 1) or of[2] < n_tok or
+                                   of[3:5] != need[3:5] or (of[5] is not None and of[5] < need[0])):
+                raise ValueError(f"contexts, layers, tokens, head_dim, dtype (and the weight's layers) are {of}, the handle's layers, contexts, "
+                                 f"KV heads, head_dim, dtype {need}")
+        if first is not None:
+            _buffer("first", first, "int32", need[1], "[contexts]")
+    _check("mone_norm_rotate", lib().mone_norm_rotate(h, layer, ctypes.byref(rotary), _ptr(first), n_tok,
+                                                      None if q is None else ctypes.byref(q), None if k is None else ctypes.byref(k),
+                                                      _stream(stream)))
 
 
 def mone_mem_free(h: int):

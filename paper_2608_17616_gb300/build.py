@@ -19,7 +19,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmone.so")
 SOURCES = ["mone_api.cu", "ttl_prepass.cu", "ttl_simt.cu", "ttl_tc.cu", "attention.cu", "swiglu_tc.cu", "host_stage.cu",
-           "cache.cu", "cache_attention.cu", "attention_window.cu"]
+           "cache.cu", "cache_attention.cu", "attention_window.cu", "cache4.cu", "cache4_attention.cu", "pages.cu", "norm_rotate.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -377,10 +377,12 @@ cudaError_t launch_cache_append(const DevState& s, const CacheView& v, const voi
     return append<uint4>(a, st);
 }
 
-cudaError_t launch_cache_evict(const DevState& s, const CacheView& v, int keep, int n_sink, int n_recent, const int* to, int to_width,
-                               float* to_score, int* kept, int* lens_out, cudaStream_t st) {
-    const int el = s.dtype == 0 ? 4 : 2;
-    EvictArgs a{v, keep, n_sink, n_recent, s.hd, to, to_width, (long long)to_width << v.page_log2, to_score, kept, lens_out};
+cudaError_t launch_cache_select(const DevState& s, const CacheView& v, int keep, int n_sink, int n_recent, int* kept, int* lens_out,
+                                cudaStream_t st) {
+    EvictArgs a{};
+    a.v = v;
+    a.keep = keep; a.n_sink = n_sink; a.n_recent = n_recent;
+    a.kept = kept; a.lens_out = lens_out;
     // A row over as many CTAs of a cluster as the SMs hold, two each, and slices of SEL_SLICE positions of what the table covers (the
     // lengths are on the device).  (128 rows of 2K take
     // 14.1 us with their compaction on one CTA each, 17.8 on two; 64 rows of 32K 99, 84, 80 and 82 on one, two, four and eight; 8
@@ -388,7 +390,14 @@ cudaError_t launch_cache_evict(const DevState& s, const CacheView& v, int keep, 
     const long long rows = (long long)v.n_ctx * v.L * v.n_kv;
     int slices = 1;
     while (slices < 8 && 2 * slices * rows <= 2 * s.sms && v.cap / (2 * slices) >= SEL_SLICE) slices *= 2;
-    cudaError_t e = slices == 1 ? select<1>(a, st) : slices == 2 ? select<2>(a, st) : slices == 4 ? select<4>(a, st) : select<8>(a, st);
+    return slices == 1 ? select<1>(a, st) : slices == 2 ? select<2>(a, st) : slices == 4 ? select<4>(a, st) : select<8>(a, st);
+}
+
+cudaError_t launch_cache_evict(const DevState& s, const CacheView& v, int keep, int n_sink, int n_recent, const int* to, int to_width,
+                               float* to_score, int* kept, int* lens_out, cudaStream_t st) {
+    const int el = s.dtype == 0 ? 4 : 2;
+    EvictArgs a{v, keep, n_sink, n_recent, s.hd, to, to_width, (long long)to_width << v.page_log2, to_score, kept, lens_out};
+    const cudaError_t e = launch_cache_select(s, v, keep, n_sink, n_recent, kept, lens_out, st);
     if (e != cudaSuccess) return e;
     if (!cache_vec(v, el)) return s.dtype == 0 ? compact<uint32_t>(a, st) : compact<uint16_t>(a, st);
     in_units(a.v, 16 / el);

@@ -1045,8 +1045,8 @@ mone_status mone_window_attention(mone_mem* m, int layer, const void* Q, int n_q
     });
 }
 
-// A cache and a layer argument, checked, as the kernels take them.
-static mone_status cache_view(const mone_mem* m, int layer, const mone_cache* c, CacheView* v) {
+// A cache and a layer argument, checked, as the kernels take them; a row is `row` units (of the strides) of el bytes.
+static mone_status pool_view(const mone_mem* m, int layer, const mone_cache* c, int row, size_t el, CacheView* v) {
     if (!is_live(m) || !c) return MONE_ERR_INVALID_ARG;
     const DevState& s = m->s;
     if (layer != MONE_ALL_LAYERS && (layer < 0 || layer >= m->cfg.n_layers)) return MONE_ERR_INVALID_ARG;
@@ -1056,12 +1056,11 @@ static mone_status cache_view(const mone_mem* m, int layer, const mone_cache* c,
     if ((c->page_size & (c->page_size - 1)) || c->page_size > 1024) return MONE_ERR_UNSUPPORTED_SHAPE;
     for (int i = 0; i < 4; ++i)
         if (c->strides[i] < 0) return MONE_ERR_INVALID_ARG;
-    // a page's positions hold head_dim elements each, and pages are apart
-    if ((c->page_size > 1 && c->strides[3] < s.hd) || (c->n_pages > 1 && c->strides[1] < s.hd)) return MONE_ERR_INVALID_ARG;
+    // a page's positions hold a row each, and pages are apart
+    if ((c->page_size > 1 && c->strides[3] < row) || (c->n_pages > 1 && c->strides[1] < row)) return MONE_ERR_INVALID_ARG;
     if ((long long)c->table_width * c->page_size > (1ll << 30)) return MONE_ERR_INVALID_ARG;
     const bool one = layer != MONE_ALL_LAYERS;
     const long long off = one ? layer : 0;
-    const size_t el = elsize(s.dtype);
     v->K = (char*)c->K + off * c->strides[0] * el;
     v->V = (char*)c->V + off * c->strides[0] * el;
     v->s_layer = c->strides[0]; v->s_page = c->strides[1]; v->s_head = c->strides[2]; v->s_pos = c->strides[3];
@@ -1081,6 +1080,11 @@ static mone_status cache_view(const mone_mem* m, int layer, const mone_cache* c,
     return MONE_OK;
 }
 
+static mone_status cache_view(const mone_mem* m, int layer, const mone_cache* c, CacheView* v) {
+    if (!is_live(m)) return MONE_ERR_INVALID_ARG;
+    return pool_view(m, layer, c, m->s.hd, elsize(m->s.dtype), v);
+}
+
 mone_status mone_cache_append(mone_mem* m, int layer, const mone_cache* cache, const void* K, const void* V,
                               const long long strides[4], int n_tok, const int* counts, int* lens_out, void* stream) {
     CacheView v;
@@ -1095,17 +1099,8 @@ mone_status mone_cache_append(mone_mem* m, int layer, const mone_cache* cache, c
     return timed(m, K_CACHE, st, 1, [&] { return launch_cache_append(s, v, K, V, strides, n_tok, counts, lens_out, st); });
 }
 
-mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache, const void* Q, int n_q_heads, int n_tok,
-                                 int n_sink, int window, void* out, void* stream) {
-    CacheView v;
-    MONE_TRY(cache_view(m, layer, cache, &v));
-    const DevState& s = m->s;
-    if (!Q || !out || !aligned16(Q) || !aligned16(out)) return MONE_ERR_INVALID_ARG;
-    if (n_q_heads < s.n_kv || n_q_heads % s.n_kv || n_q_heads / s.n_kv > 64) return MONE_ERR_INVALID_ARG;
-    if (n_tok < 1 || n_tok > 16 || n_sink < 0 || window < 0) return MONE_ERR_INVALID_ARG;
-    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const size_t need = cache_attention_workspace(s, v, n_q_heads, n_tok);
-    if (need == 0) return MONE_ERR_UNSUPPORTED_SHAPE;
+// The handle's workspace of the cache attentions, grown to `need` bytes.
+static mone_status cache_workspace(mone_mem* m, size_t need, const char* who, cudaStream_t st) {
     const bool grow = need > m->cws_bytes;
     if (grow || !m->cws_captured) {
         cudaStreamCaptureStatus capture;
@@ -1113,8 +1108,7 @@ mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache
         if (capture != cudaStreamCaptureStatusNone) {
             if (grow) {
                 std::snprintf(g_last_error, sizeof(g_last_error),
-                              "mone_cache_attention: a workspace of %zu bytes cannot be made during a capture; make a call of "
-                              "this size before it",
+                              "%s: a workspace of %zu bytes cannot be made during a capture; make a call of this size before it", who,
                               need);
                 return MONE_ERR_OOM;
             }
@@ -1138,6 +1132,21 @@ mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache
         m->cws = p;
         m->cws_bytes = need;
     }
+    return MONE_OK;
+}
+
+mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache, const void* Q, int n_q_heads, int n_tok,
+                                 int n_sink, int window, void* out, void* stream) {
+    CacheView v;
+    MONE_TRY(cache_view(m, layer, cache, &v));
+    const DevState& s = m->s;
+    if (!Q || !out || !aligned16(Q) || !aligned16(out)) return MONE_ERR_INVALID_ARG;
+    if (n_q_heads < s.n_kv || n_q_heads % s.n_kv || n_q_heads / s.n_kv > 64) return MONE_ERR_INVALID_ARG;
+    if (n_tok < 1 || n_tok > 16 || n_sink < 0 || window < 0) return MONE_ERR_INVALID_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const size_t need = cache_attention_workspace(s, v, n_q_heads, n_tok);
+    if (need == 0) return MONE_ERR_UNSUPPORTED_SHAPE;
+    MONE_TRY(cache_workspace(m, need, "mone_cache_attention", st));
     int kernels = 0;
     MONE_TRY(timed(m, K_CACHE, st, 0, [&] {
         return launch_cache_attention(s, v, Q, n_q_heads, n_tok, n_sink, window, out, m->cws, &kernels, st);
@@ -1146,21 +1155,222 @@ mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache
     return MONE_OK;
 }
 
+// An eviction's arguments beside its cache
+static mone_status evict_args(const float* score, const int* table, const int* lens, int page_size, int keep, int n_sink, int n_recent,
+                              const int* to_table, int to_width, const float* to_score, const int* kept, const int* lens_out) {
+    if (!score || !to_table || !to_score || !kept || to_width < 1) return MONE_ERR_INVALID_ARG;
+    if (((uintptr_t)to_table | (uintptr_t)to_score | (uintptr_t)kept | (uintptr_t)lens_out) & 3u) return MONE_ERR_INVALID_ARG;
+    if (keep < 1 || n_sink < 0 || n_recent < 0 || (long long)n_sink + n_recent > keep) return MONE_ERR_INVALID_ARG;
+    if ((long long)to_width * page_size < keep || (long long)to_width * page_size > (1ll << 30)) return MONE_ERR_INVALID_ARG;
+    if (to_table == table || to_score == score || (lens_out && lens_out == lens)) return MONE_ERR_INVALID_ARG;
+    return MONE_OK;
+}
+
 mone_status mone_cache_evict(mone_mem* m, int layer, const mone_cache* cache, int keep, int n_sink, int n_recent,
                              const int* to_table, int to_width, float* to_score, int* kept, int* lens_out, void* stream) {
     CacheView v;
     MONE_TRY(cache_view(m, layer, cache, &v));
     const DevState& s = m->s;
-    if (!cache->score || !to_table || !to_score || !kept || to_width < 1) return MONE_ERR_INVALID_ARG;
-    if (((uintptr_t)to_table | (uintptr_t)to_score | (uintptr_t)kept | (uintptr_t)lens_out) & 3u) return MONE_ERR_INVALID_ARG;
-    if (keep < 1 || n_sink < 0 || n_recent < 0 || (long long)n_sink + n_recent > keep) return MONE_ERR_INVALID_ARG;
-    if ((long long)to_width * cache->page_size < keep || (long long)to_width * cache->page_size > (1ll << 30)) return MONE_ERR_INVALID_ARG;
-    if (to_table == cache->table || to_score == cache->score || (lens_out && lens_out == cache->lens)) return MONE_ERR_INVALID_ARG;
+    MONE_TRY(evict_args(cache->score, cache->table, cache->lens, cache->page_size, keep, n_sink, n_recent, to_table, to_width, to_score, kept, lens_out));
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const size_t off = layer == MONE_ALL_LAYERS ? 0 : (size_t)layer * s.n_kv * to_width * cache->page_size;
     return timed(m, K_CACHE, st, 2, [&] {
         return launch_cache_evict(s, v, keep, n_sink, n_recent, to_table, to_width, to_score + off, kept, lens_out, st);
     });
+}
+
+// A 4-bit cache and a layer argument, checked, as the kernels take them.
+static mone_status cache4_view(const mone_mem* m, int layer, const mone_cache4* c, Cache4View* f) {
+    if (!is_live(m) || !c) return MONE_ERR_INVALID_ARG;
+    const DevState& s = m->s;
+    const mone_cache codes = {c->K, c->V, {c->strides[0], c->strides[1], c->strides[2], c->strides[3]}, c->n_pages, c->page_size, c->table,
+                              c->table_width, c->lens, c->score};
+    MONE_TRY(pool_view(m, layer, &codes, s.hd / 2, 1, &f->v));
+    const int row = s.hd / 16;
+    if (!c->K_scale || !c->V_scale || ((uintptr_t)c->K_scale | (uintptr_t)c->V_scale) % row) return MONE_ERR_INVALID_ARG;
+    for (int i = 0; i < 4; ++i)
+        if (c->strides[i] % 16 || c->scale_strides[i] < 0 || c->scale_strides[i] % row) return MONE_ERR_INVALID_ARG;
+    if ((c->page_size > 1 && c->scale_strides[3] < row) || (c->n_pages > 1 && c->scale_strides[1] < row)) return MONE_ERR_INVALID_ARG;
+    if (c->k_exp < -64 || c->k_exp > 64 || c->v_exp < -64 || c->v_exp > 64) return MONE_ERR_INVALID_ARG;
+    const long long off = layer != MONE_ALL_LAYERS ? layer * c->scale_strides[0] : 0;
+    f->Ks = (uint8_t*)c->K_scale + off;
+    f->Vs = (uint8_t*)c->V_scale + off;
+    f->c_layer = c->scale_strides[0]; f->c_page = c->scale_strides[1]; f->c_head = c->scale_strides[2]; f->c_pos = c->scale_strides[3];
+    f->k_unit = std::ldexp(1.0f, c->k_exp);
+    f->v_unit = std::ldexp(1.0f, c->v_exp);
+    return MONE_OK;
+}
+
+mone_status mone_cache4_append(mone_mem* m, int layer, const mone_cache4* cache, const void* K, const void* V,
+                               const long long strides[4], int n_tok, const int* counts, int* lens_out, void* stream) {
+    Cache4View f;
+    MONE_TRY(cache4_view(m, layer, cache, &f));
+    const DevState& s = m->s;
+    if (!K || !V || !strides || n_tok < 1 || n_tok > (1 << 20)) return MONE_ERR_INVALID_ARG;
+    if (((uintptr_t)K | (uintptr_t)V) % elsize(s.dtype) || (((uintptr_t)counts | (uintptr_t)lens_out) & 3u)) return MONE_ERR_INVALID_ARG;
+    for (int i = 0; i < 4; ++i)
+        if (strides[i] < 0) return MONE_ERR_INVALID_ARG;
+    if (lens_out && lens_out == cache->lens) return MONE_ERR_INVALID_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    return timed(m, K_CACHE, st, 1, [&] { return launch_cache4_append(s, f, K, V, strides, n_tok, counts, lens_out, st); });
+}
+
+mone_status mone_cache4_read(mone_mem* m, int layer, const mone_cache4* cache, const int* from, int n_pos, void* K, void* V,
+                             const long long strides[4], void* stream) {
+    Cache4View f;
+    MONE_TRY(cache4_view(m, layer, cache, &f));
+    const DevState& s = m->s;
+    if (!K || !V || !strides || n_pos < 1 || n_pos > (1 << 20)) return MONE_ERR_INVALID_ARG;
+    if (((uintptr_t)K | (uintptr_t)V) % elsize(s.dtype) || ((uintptr_t)from & 3u)) return MONE_ERR_INVALID_ARG;
+    for (int i = 0; i < 4; ++i)
+        if (strides[i] < 0) return MONE_ERR_INVALID_ARG;
+    // every row of the outputs has a place of its own
+    const long long rows[4] = {m->cfg.n_ctx, f.v.L, s.n_kv, n_pos};
+    for (int i = 0; i < 4; ++i)
+        if (rows[i] > 1 && strides[i] < s.hd) return MONE_ERR_INVALID_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    return timed(m, K_CACHE, st, 1, [&] { return launch_cache4_read(s, f, from, n_pos, K, V, strides, st); });
+}
+
+mone_status mone_cache4_attention(mone_mem* m, int layer, const mone_cache4* cache, const void* Q, int n_q_heads, int n_tok,
+                                  int n_sink, int window, void* out, void* stream) {
+    Cache4View f;
+    MONE_TRY(cache4_view(m, layer, cache, &f));
+    const DevState& s = m->s;
+    if (!Q || !out || !aligned16(Q) || !aligned16(out)) return MONE_ERR_INVALID_ARG;
+    if (n_q_heads < s.n_kv || n_q_heads % s.n_kv || n_q_heads / s.n_kv > 64) return MONE_ERR_INVALID_ARG;
+    if (n_tok < 1 || n_tok > 16 || n_sink < 0 || window < 0) return MONE_ERR_INVALID_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const size_t need = cache4_attention_workspace(s, f, n_q_heads, n_tok);
+    if (need == 0) return MONE_ERR_UNSUPPORTED_SHAPE;
+    MONE_TRY(cache_workspace(m, need, "mone_cache4_attention", st));
+    int kernels = 0;
+    MONE_TRY(timed(m, K_CACHE, st, 0, [&] {
+        return launch_cache4_attention(s, f, Q, n_q_heads, n_tok, n_sink, window, out, m->cws, &kernels, st);
+    }));
+    m->launches += kernels;
+    return MONE_OK;
+}
+
+mone_status mone_cache4_evict(mone_mem* m, int layer, const mone_cache4* cache, int keep, int n_sink, int n_recent,
+                              const int* to_table, int to_width, float* to_score, int* kept, int* lens_out, void* stream) {
+    Cache4View f;
+    MONE_TRY(cache4_view(m, layer, cache, &f));
+    const DevState& s = m->s;
+    MONE_TRY(evict_args(cache->score, cache->table, cache->lens, cache->page_size, keep, n_sink, n_recent, to_table, to_width, to_score, kept, lens_out));
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const size_t off = layer == MONE_ALL_LAYERS ? 0 : (size_t)layer * s.n_kv * to_width * cache->page_size;
+    return timed(m, K_CACHE, st, 2, [&] {
+        return launch_cache4_evict(s, f, keep, n_sink, n_recent, to_table, to_width, to_score + off, kept, lens_out, st);
+    });
+}
+
+// Lists and tables of pages, checked, as the kernels take them.
+static mone_status pages_view(const mone_mem* m, const mone_pages* p, const int* lens_out, const int* n_free_out, PagesView* v) {
+    if (!is_live(m) || !p || !p->free || !p->n_free || !p->table || !p->lens || !n_free_out) return MONE_ERR_INVALID_ARG;
+    if (((uintptr_t)p->free | (uintptr_t)p->n_free | (uintptr_t)p->table | (uintptr_t)p->lens | (uintptr_t)lens_out | (uintptr_t)n_free_out) & 3u)
+        return MONE_ERR_INVALID_ARG;
+    if (p->n_pages < 1 || p->page_size < 1 || p->table_width < 1) return MONE_ERR_INVALID_ARG;
+    if ((p->page_size & (p->page_size - 1)) || p->page_size > 1024) return MONE_ERR_UNSUPPORTED_SHAPE;
+    if ((long long)p->table_width * p->page_size > (1ll << 30)) return MONE_ERR_INVALID_ARG;
+    if (n_free_out == p->n_free || (lens_out && lens_out == p->lens)) return MONE_ERR_INVALID_ARG;
+    v->free = p->free;
+    v->n_free = p->n_free;
+    v->n_pages = p->n_pages;
+    v->page_log2 = 0;
+    while ((1 << v->page_log2) < p->page_size) ++v->page_log2;
+    v->table = p->table;
+    v->width = p->table_width;
+    v->lens = p->lens;
+    v->cap = (long long)p->table_width * p->page_size;
+    v->n_ctx = m->cfg.n_ctx;
+    v->status = m->s.status;
+    return MONE_OK;
+}
+
+mone_status mone_cache_reserve(mone_mem* m, const mone_pages* pages, int n_tok, const int* counts, int* granted, long long* slots,
+                               int* lens_out, int* n_free_out, void* stream) {
+    PagesView v;
+    MONE_TRY(pages_view(m, pages, lens_out, n_free_out, &v));
+    if (n_tok < 1 || n_tok > (1 << 20) || (((uintptr_t)counts | (uintptr_t)granted) & 3u) || ((uintptr_t)slots & 7u)) return MONE_ERR_INVALID_ARG;
+    if (granted && (granted == counts || granted == pages->lens || granted == lens_out)) return MONE_ERR_INVALID_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    return timed(m, K_CACHE, st, 1, [&] { return launch_cache_reserve(v, n_tok, counts, granted, slots, lens_out, n_free_out, st); });
+}
+
+mone_status mone_cache_release(mone_mem* m, const mone_pages* pages, const int* keep, int* lens_out, int* n_free_out, void* stream) {
+    PagesView v;
+    MONE_TRY(pages_view(m, pages, lens_out, n_free_out, &v));
+    if (((uintptr_t)keep & 3u) || (lens_out && lens_out == keep)) return MONE_ERR_INVALID_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    return timed(m, K_CACHE, st, 1, [&] { return launch_cache_release(v, keep, lens_out, n_free_out, st); });
+}
+
+mone_status mone_rotary_make(mone_rotary* r, int rot_dim, int pairing, const double* freq, double base, int period, float eps) {
+    if (!r || rot_dim < 0 || rot_dim > 128 || rot_dim % 16 || period < 0 || !(eps >= 0.0f) || !std::isfinite(eps)) return MONE_ERR_INVALID_ARG;
+    if (pairing != MONE_ROTATE_HALVES && pairing != MONE_ROTATE_NEIGHBOURS) return MONE_ERR_INVALID_ARG;
+    if (!freq && rot_dim && !(base > 0.0 && std::isfinite(base))) return MONE_ERR_INVALID_ARG;
+    mone_rotary made = {};
+    made.rot_dim = rot_dim;
+    made.pairing = pairing;
+    made.period = period;
+    made.eps = eps;
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        const double f = freq ? freq[i] : std::pow(base, -2.0 * i / rot_dim);
+        if (!(std::fabs(f) < 0x1p31)) return MONE_ERR_INVALID_ARG;
+        // |f| / (2 pi), 1 / (2 pi) in two doubles: the product and what its rounding left off, both as 64-bit fractions
+        const double inv = 0x1.45f306dc9c883p-3, rest = -0x1.6b01ec5417056p-57, a = std::fabs(f), p = a * inv;
+        const double high = (p - std::floor(p)) * 0x1p32, left = std::fma(a, inv, -p) + a * rest;
+        unsigned long long turn = (unsigned long long)high << 32;
+        turn += (unsigned long long)((high - std::floor(high)) * 0x1p32);
+        turn += (unsigned long long)std::llrint(left * 0x1p64);
+        made.turns[i] = f < 0.0 ? 0 - turn : turn;
+    }
+    *r = made;
+    return MONE_OK;
+}
+
+mone_status mone_norm_rotate(mone_mem* m, int layer, const mone_rotary* rotary, const int* first, int n_tok, const mone_heads* q,
+                             const mone_heads* k, void* stream) {
+    if (!is_live(m) || !rotary || (!q && !k)) return MONE_ERR_INVALID_ARG;
+    const DevState& s = m->s;
+    if (layer != MONE_ALL_LAYERS && (layer < 0 || layer >= m->cfg.n_layers)) return MONE_ERR_INVALID_ARG;
+    if (rotary->rot_dim < 0 || rotary->rot_dim > s.hd || rotary->rot_dim % 16 || rotary->period < 0 || !(rotary->eps >= 0.0f) ||
+        !std::isfinite(rotary->eps) || (rotary->pairing != MONE_ROTATE_HALVES && rotary->pairing != MONE_ROTATE_NEIGHBOURS))
+        return MONE_ERR_INVALID_ARG;
+    if (n_tok < 1 || n_tok > (1 << 24) || ((uintptr_t)first & 3u)) return MONE_ERR_INVALID_ARG;
+    const bool one = layer != MONE_ALL_LAYERS;
+    RotateArgs a = {};
+    const mone_heads* sides[2] = {q, k};
+    for (int i = 0; i < 2; ++i) {
+        const mone_heads* x = sides[i];
+        if (!x) continue;
+        if (!x->x || !x->out || x->n_heads < 1 || x->n_heads > 4096) return MONE_ERR_INVALID_ARG;
+        if (((uintptr_t)x->x | (uintptr_t)x->out) % elsize(s.dtype) || ((uintptr_t)x->weight & 3u)) return MONE_ERR_INVALID_ARG;
+        bool same = true;
+        for (int d = 0; d < 4; ++d) {
+            if (x->strides[d] < 0 || x->out_strides[d] < 0) return MONE_ERR_INVALID_ARG;
+            same &= x->strides[d] == x->out_strides[d];
+        }
+        if (x->x == x->out && !same) return MONE_ERR_INVALID_ARG;
+        // every row of the output has a place of its own
+        const long long rows[4] = {m->cfg.n_ctx, one ? 1 : m->cfg.n_layers, x->n_heads, n_tok};
+        for (int d = 0; d < 4; ++d)
+            if (rows[d] > 1 && x->out_strides[d] < s.hd) return MONE_ERR_INVALID_ARG;
+        RotateSide& to = a.side[i];
+        to.x = x->x;
+        to.out = x->out;
+        to.w = x->weight ? x->weight + (one ? (size_t)layer * s.hd : 0) : nullptr;
+        for (int d = 0; d < 4; ++d) to.s[d] = x->strides[d], to.o[d] = x->out_strides[d];
+        to.heads = x->n_heads;
+    }
+    a.first = first;
+    a.n_tok = n_tok; a.n_ctx = m->cfg.n_ctx; a.L = one ? 1 : m->cfg.n_layers;
+    a.rot = rotary->rot_dim; a.neighbours = rotary->pairing == MONE_ROTATE_NEIGHBOURS; a.period = rotary->period;
+    a.eps = rotary->eps;
+    std::copy(rotary->turns, rotary->turns + 64, a.turns);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    return timed(m, K_CACHE, st, 1, [&] { return launch_norm_rotate(s, a, st); });
 }
 
 mone_status mone_mem_free(mone_mem* m) {
@@ -1224,8 +1434,8 @@ mone_status mone_mem_sync(mone_mem* m, void* stream) {
     if (flag) MONE_CUDA(cudaMemset(m->s.status, 0, sizeof(word)));
     if (flag & DEV_CHECK) {
         static const char* const sites[] = {"?", "phase A tile", "phase B tile", "read tile", "resident rows",
-                                            "TMA x coordinate", "cache page number", "cache length"};
-        const int site = word[1] >= 1 && word[1] <= 7 ? word[1] : 0;
+                                            "TMA x coordinate", "cache page number", "cache length", "number of free pages"};
+        const int site = word[1] >= 1 && word[1] < (int)(sizeof(sites) / sizeof(*sites)) ? word[1] : 0;
         std::snprintf(g_last_error, sizeof(g_last_error), "device index check failed: %s", sites[site]);
         return MONE_ERR_CHECK;
     }

@@ -20,7 +20,7 @@ enum : int { DEV_TIMEOUT = 1, DEV_NONFINITE = 2, DEV_CHECK = 4 };
 enum : int { DS_PHASE_A_TILE = 1, DS_PHASE_B_TILE = 2, DS_READ_TILE = 3, DS_RESIDENT_ROWS = 4,
              DS_TMA_X = 5,
              // the cache operators check these in every build: they come from device memory
-             DS_CACHE_PAGE = 6, DS_CACHE_LEN = 7 };
+             DS_CACHE_PAGE = 6, DS_CACHE_LEN = 7, DS_CACHE_FREE = 8 };
 
 // Device-resident state of all chains (see mone_mem_init).
 struct TcDevice;  // what the tensor-core launches need to know of a device
@@ -212,6 +212,9 @@ struct CacheView {
 };
 cudaError_t launch_cache_append(const DevState& s, const CacheView& v, const void* K, const void* V, const long long* strides,
                                 int n_tok, const int* counts, int* lens_out, cudaStream_t st);
+// Which positions stay (launch_cache_evict's first kernel)
+cudaError_t launch_cache_select(const DevState& s, const CacheView& v, int keep, int n_sink, int n_recent, int* kept, int* lens_out,
+                                cudaStream_t st);
 cudaError_t launch_cache_evict(const DevState& s, const CacheView& v, int keep, int n_sink, int n_recent, const int* to, int to_width,
                                float* to_score, int* kept, int* lens_out, cudaStream_t st);
 // Workspace of launch_cache_attention in bytes for this call (0: more blocks than it counts), and the call, which says how many
@@ -219,6 +222,60 @@ cudaError_t launch_cache_evict(const DevState& s, const CacheView& v, int keep, 
 size_t cache_attention_workspace(const DevState& s, const CacheView& v, int n_q, int n_tok);
 cudaError_t launch_cache_attention(const DevState& s, const CacheView& v, const void* Q, int n_q, int n_tok, int n_sink, int window,
                                    void* out, void* ws, int* kernels, cudaStream_t st);
+
+// ---- kernels in cache4.cu and cache4_attention.cu (paged cache in 4 bits)
+// A mone_cache4 as the kernels take it: v's pools and their strides are the codes', in bytes.
+struct Cache4View {
+    CacheView v;
+    uint8_t *Ks, *Vs;                      // scales of the call's first layer
+    long long c_layer, c_page, c_head, c_pos;
+    float k_unit, v_unit;                  // 2^k_exp, 2^v_exp
+};
+cudaError_t launch_cache4_append(const DevState& s, const Cache4View& f, const void* K, const void* V, const long long* strides, int n_tok,
+                                 const int* counts, int* lens_out, cudaStream_t st);
+cudaError_t launch_cache4_read(const DevState& s, const Cache4View& f, const int* from, int n_pos, void* K, void* V, const long long* strides,
+                               cudaStream_t st);
+cudaError_t launch_cache4_evict(const DevState& s, const Cache4View& f, int keep, int n_sink, int n_recent, const int* to, int to_width,
+                                float* to_score, int* kept, int* lens_out, cudaStream_t st);
+size_t cache4_attention_workspace(const DevState& s, const Cache4View& f, int n_q, int n_tok);
+cudaError_t launch_cache4_attention(const DevState& s, const Cache4View& f, const void* Q, int n_q, int n_tok, int n_sink, int window, void* out,
+                                    void* ws, int* kernels, cudaStream_t st);
+
+// ---- kernels in pages.cu
+// A mone_pages as the kernels take it
+struct PagesView {
+    int* free;
+    const int* n_free;
+    int n_pages, page_log2;
+    int* table;
+    int width;
+    const int* lens;
+    long long cap;
+    int n_ctx;
+    int* status;
+};
+cudaError_t launch_cache_reserve(const PagesView& v, int n_tok, const int* counts, int* granted, long long* slots, int* lens_out, int* n_free_out,
+                                 cudaStream_t st);
+cudaError_t launch_cache_release(const PagesView& v, const int* keep, int* lens_out, int* n_free_out, cudaStream_t st);
+
+// ---- kernels in norm_rotate.cu
+// A mone_heads of the call's first layer
+struct RotateSide {
+    const void* x;
+    void* out;
+    const float* w;                        // [L][hd] or null
+    long long s[4], o[4];                  // element strides (context, layer, head, token) of x and out
+    int heads;                             // 0: no such side
+};
+struct RotateArgs {
+    RotateSide side[2];
+    const int* first;
+    int n_tok, n_ctx, L;
+    int rot, neighbours, period;
+    float eps;
+    unsigned long long turns[64];
+};
+cudaError_t launch_norm_rotate(const DevState& s, const RotateArgs& a, cudaStream_t st);
 
 // ---- kernels in ttl_tc.cu (bf16 tcgen05 path)
 struct TcMaps {
