@@ -41,145 +41,419 @@ struct FourHead {
     }
 };
 
-// ---------------------------------------------------------------- CUDA cores
-// Eight lanes share a key, each with head_dim / 8 neighbouring dimensions; the four lane groups of a warp take every fourth key and
-// keep a softmax of their own, joined at the end of the piece.
-template <typename T_, int HD_>
+// ---------------------------------------------------------------- tensor cores
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&A)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(A[0]), "r"(A[1]), "r"(A[2]), "r"(A[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t mul_halves(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_halves(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void load_shared(uint32_t (&x)[N], uint32_t addr) {
+    if constexpr (N == 4)
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(addr) : "memory");
+    else if constexpr (N == 2)
+        asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(addr) : "memory");
+    else
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x[0]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t load_byte(uint32_t addr) {
+    uint32_t x;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
+    return x;
+}
+__device__ __forceinline__ uint32_t load_two_bytes(uint32_t addr) {
+    unsigned short x;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(addr) : "memory");
+    return x;
+}
+
+// A block's codes and scales come by asynchronous copies into a ring that belongs to one warp, as with the rows of 16 bits, whatever
+// the strides and pages are.  The keys are the M of m16n8k16 and the rows its N, 8 or 16 of them.  Codes become halves on the way to the
+// product (a conversion for two of them, a product with their scale, exact), in the lane that holds them as operands: S^T = K Q^T
+// with a lane's quarter of a key's dimensions, in any order that Q has too; O^T += V^T P^T with an eighth of a value's, whose
+// halves of two keys are paired by a permutation.  So nothing but the codes goes through shared memory.
+//
+// Halves hold a row of Q scaled by a power of two to 2^14 .. 2^15 at most (an element 2^-29 of the largest loses bits, 2^-39
+// of it at most), and probabilities times 2^15 (what is below 2^-29 of the row's largest loses bits).  Rows of 32 bits are two
+// halves each, 22 bits, and so are their probabilities.
+template <typename T_, int HD_, int NT>
 struct CaFour {
     using T = T_;
-    static constexpr int HD = HD_, ROWS = 4, CTAS = HD == 64 ? 3 : 2;
-    static constexpr int D = HD / 8;  // dimensions of a lane
-    static constexpr int ONE = 1, EACH = 1, FULL = 1, FEW = 1;  // blocks of a warp, see item_ctas
-    static constexpr int WARP_BYTES = 2 * Part<HD, ROWS>::FLOATS * 4;
+    static constexpr bool TWO = std::is_same<T, float>::value;
+    static constexpr int HD = HD_, ROWS = 8 * NT, CTAS = NT == 1 ? 3 : 2;
+    static constexpr int ONE = 3, EACH = 2, FULL = 16, FEW = 6;          // blocks of a warp, see item_ctas
+    static constexpr int CODES = KB * HD / 2, SCALES = KB * HD / 16, STAGE = 2 * (CODES + SCALES);
+    static constexpr int NS = HD == 64 ? 4 : 3;
+    static constexpr int WARP_BYTES = NS * STAGE;
+    static constexpr int CHUNKS = HD / 32;  // of 16 bytes, of a row's codes
+    static_assert(CTAS * (CA_WARPS * WARP_BYTES + Part<HD, ROWS>::FLOATS * 4 + 3072) <= 228 * 1024, "CTAs an SM");
+    static_assert(Part<HD, ROWS>::FLOATS * 4 <= WARP_BYTES, "a part fits in the ring");
+
     using Args = Ca4Args;
     using Maps = NoMaps;
     using Head = FourHead;
 
-    float* parts;
+    uint32_t ring;
+    float* ring_part;  // the ring as the place of the warp's last part
 
-    __device__ CaFour(const NoMaps&, uint8_t* smem, int) : parts(reinterpret_cast<float*>(smem)) {}
+    __device__ CaFour(const NoMaps&, uint8_t* smem, int) : ring(smem_u32(smem)), ring_part(reinterpret_cast<float*>(smem)) {}
+
+    // Byte of chunk c of row r: neighbouring rows, and for head_dim 128 halves of a row, change places so that neither the loads of
+    // keys (neighbouring rows) nor those of values (every other row, the same bytes of each) meet in a bank.
+    static __device__ __forceinline__ uint32_t at(int r, int c) { return (r ^ (r >> 2 & 1)) * (HD / 2) + (HD == 128 ? c ^ (r & 2) : c) * 16; }
+
+    // The copies of a warp's blocks, ahead of their reading and on through the pieces: a lane looks up a key's page a block
+    // ahead and copies its scales, neighbours copy its codes.
+    struct Feed {
+        CaWalk w;
+        int i = 0, n = 0, page;
+        __device__ Feed(const Args& a) : w(a) {}
+        __device__ __forceinline__ void look(const Args& a) {
+            while (i == n) {
+                if (!w.next(a)) {
+                    n = -1;
+                    return;
+                }
+                i = 0;
+                n = w.b1 - w.b0;
+            }
+            const int key = w.r.at(w.b0 + i) + (threadIdx.x & 31);
+            const bool in = key < w.r.n && (key < a.n_sink || key > w.r.t0 - a.window);
+            page = in ? a.v.table[(size_t)w.c * a.v.width + (key >> a.v.page_log2)] : INT_MIN;
+        }
+    };
+    __device__ __forceinline__ void feed(const Args& a, Feed& f, int s) {
+        if (f.n >= 0) {
+            const int lane = threadIdx.x & 31, place = (f.w.r.at(f.w.b0 + f.i) + lane) & ((1 << a.v.page_log2) - 1);
+            bool in = f.page != INT_MIN;
+            if (in && (unsigned)f.page >= (unsigned)a.v.n_pages) {
+                cache_fail(a.v.status, DS_CACHE_PAGE);
+                in = false;
+            }
+            const FourHead head(a, f.w.l, f.w.g);
+            const uint32_t dst = ring + s * STAGE, scales = dst + 2 * CODES + lane * (HD / 16);
+            if (in) {
+                const long long off = f.page * head.c_page + place * head.c_pos;
+                copy_async<HD / 16>(scales, head.Ks + off);
+                copy_async<HD / 16>(scales + SCALES, head.Vs + off);
+            }
+            const long long mine = in ? f.page * head.s_page + place * head.s_pos : -1;
+#pragma unroll
+            for (int x = 0; x < CHUNKS; ++x) {
+                const int r = x * (32 / CHUNKS) + lane / CHUNKS, c = lane % CHUNKS;
+                const long long off = __shfl_sync(0xffffffffu, mine, r);
+                if (off < 0) continue;
+                copy_async<16>(dst + at(r, c), head.K + off + 16 * c);
+                copy_async<16>(dst + CODES + at(r, c), head.V + off + 16 * c);
+            }
+            ++f.i;
+            f.look(a);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+
+    // A warp's rows of an item and what it has of them.  Lane 4 gq + t has a quarter of Q of row 8 i + gq, dimensions from t HD / 4; S
+    // and the sums of rows 8 i + 2 t and + 1, and of these O's dimensions gq HD / 8 + 2 m (0, 1) and + 1 (2, 3).
+    struct Rows {
+        uint32_t q[TWO ? 2 : 1][NT][HD / 16][2];
+        float o[NT][HD / 16][4];
+        float m[NT][2], l[NT][2], lx[NT][2];
+        float unit[NT][2], k2[NT][2];  // of S: the unit in which it is q k, and in base 2 with the softmax's scale
+        int vis[NT][2];
+    };
+
+    // Q of row `row` of all, this lane's quarter, and the power of two that it is to be multiplied with
+    static __device__ __forceinline__ float load_q(const Args& a, size_t row, bool live, uint32_t (&hi)[HD / 16][2], uint32_t (*lo)[2]) {
+        constexpr int D = HD / 4, PER = 16 / sizeof(T);
+        const int t = threadIdx.x & 3;
+        const T* q = static_cast<const T*>(a.Q) + row * HD + t * D;
+        float x[D], most = 0.f;
+#pragma unroll
+        for (int p = 0; p < D / PER; ++p) {
+            const uint4 u = live ? reinterpret_cast<const uint4*>(q)[p] : make_uint4(0, 0, 0, 0);
+            const T* e = reinterpret_cast<const T*>(&u);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) x[p * PER + i] = to_f<T>(e[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < D; ++i) most = fmaxf(most, isnan(x[i]) ? INFINITY : fabsf(x[i]));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        const int e = max((int)(__float_as_uint(most) >> 23), 16);
+        float scale = __uint_as_float((unsigned)(268 - e) << 23), unit = __uint_as_float((unsigned)(e - 14) << 23);
+        const bool finite = most < INFINITY;
+        if (!finite) scale = unit = 1.f;
+#pragma unroll
+        for (int i = 0; i < D; i += 2) {
+            // beside an infinity or a NaN, what is finite has no say
+            const float x0 = finite || !isfinite(x[i]) ? x[i] * scale : 0.f, x1 = finite || !isfinite(x[i + 1]) ? x[i + 1] * scale : 0.f;
+            const uint32_t h = pack_halves(x0, x1);
+            hi[i / 4][i / 2 % 2] = h;
+            if constexpr (TWO) {
+                const float2 f = halves_float2(h);
+                lo[i / 4][i / 2 % 2] = finite ? pack_halves(x0 - f.x, x1 - f.y) : 0;
+            }
+        }
+        return unit;
+    }
 
     __device__ __forceinline__ void run(const Args& a, CaNote* notes) {
-        CaWalk walk(a);
-        while (walk.next(a)) piece(a, walk, notes);
-    }
-
-    static __device__ __forceinline__ void decode(const uint8_t* codes, const uint8_t* scales, bool in, int l8, float unit, float (&f)[D]) {
-#pragma unroll
-        for (int d = 0; d < D; ++d) f[d] = 0.f;
-        if (!in) return;
-        const float s = scale_float(scales[l8 * D / 16]) * unit;
-#pragma unroll
-        for (int w = 0; w < D / 8; ++w) {
-            uint32_t h[4];
-            code_halves(*reinterpret_cast<const uint32_t*>(codes + l8 * D / 2 + 4 * w), h);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 two = halves_float2(h[i]);
-                f[8 * w + 2 * i] = two.x * s;
-                f[8 * w + 2 * i + 1] = two.y * s;
-            }
-        }
-    }
-
-    __device__ __forceinline__ void piece(const Args& a, const CaWalk& walk, CaNote* notes) {
-        const CaRange& r = walk.r;
-        const int c = walk.c, row0 = walk.rt * ROWS, rows = min(ROWS, a.R - row0);
-        const size_t kv = walk.kv(a);
-        const Head head(a, walk.l, walk.g);
-        const float k2 = a.scale * 1.4426950408889634f;
-        const int lane = threadIdx.x & 31, grp = lane >> 3, l8 = lane & 7;
-        const int* table = a.v.table + (size_t)c * a.v.width;
-        const int mask = (1 << a.v.page_log2) - 1;
-        float q[ROWS][D], o[ROWS][D], m[ROWS], l[ROWS];
-        int vis[ROWS];
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            const int row = row0 + min(i, rows - 1);
-            const T* qr = static_cast<const T*>(a.Q) + (kv * a.R + row) * HD + l8 * D;
-#pragma unroll
-            for (int d = 0; d < D; ++d) q[i][d] = i < rows ? to_f<T>(qr[d]) : 0.f;
-            vis[i] = i < rows ? r.n - a.n_tok + row % a.n_tok + 1 : 0;
-            m[i] = -INFINITY;
-            l[i] = 0.f;
-#pragma unroll
-            for (int d = 0; d < D; ++d) o[i][d] = 0.f;
-        }
-        for (int b = walk.b0; b < walk.b1; ++b) {
-            const int j0 = r.at(b);
-#pragma unroll 1
-            for (int it = 0; it < KB / 4; ++it) {
-                const int key = j0 + grp + 4 * it;
-                bool in = key < r.n && (key < a.n_sink || key > r.t0 - a.window);
-                int page = 0;
-                if (in) {
-                    page = cache_page(a.v, table, key >> a.v.page_log2);
-                    in = page >= 0;
-                }
-                float k[D], v[D];
-                const auto row = head.row(max(page, 0), key & mask);
-                decode(row.K, row.Ks, in, l8, a.k_unit, k);
-                decode(row.V, row.Vs, in, l8, a.v_unit, v);
-                float mine = 0.f;
-#pragma unroll
-                for (int i = 0; i < ROWS; ++i) {
-                    float s = 0.f;
-#pragma unroll
-                    for (int d = 0; d < D; ++d) s = fmaf(q[i][d], k[d], s);
-#pragma unroll
-                    for (int x = 4; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-                    const float z = in && key < vis[i] && (key < a.n_sink || key >= vis[i] - a.window) ? s : -INFINITY;
-                    mine = l8 == i ? z : mine;
-                    const float mn = fmaxf(m[i], z);
-                    const float corr = mn == -INFINITY ? 1.f : ca_exp2((m[i] - mn) * k2), moff = mn == -INFINITY ? 0.f : -mn * k2;
-                    m[i] = mn;
-                    const float p = ca_exp2(fmaf(z, k2, moff));
-                    l[i] = fmaf(l[i], corr, p);
-#pragma unroll
-                    for (int d = 0; d < D; ++d) o[i][d] = fmaf(p, v[d], o[i][d] * corr);
-                }
-                if (a.z2 && l8 < rows && key < r.n) a.z2[(kv * a.R + row0 + l8) * a.pitch + key] = mine * k2;
-            }
-        }
-        // the lane groups' softmaxes into one; lane group i writes row i
         using P = Part<HD, ROWS>;
-        float* part = parts + (walk.b0 == 0) * P::FLOATS;
-        if (walk.whole && lane == 0) a.info[kv * a.RT + walk.rt] = 1 << 16;
-        if (!walk.whole && lane == 0) notes[walk.b0 == 0] = {part, c, walk.l, walk.g, walk.rt, r.n, walk.first, walk.cta_whole, walk.parts};
+        const int lane = threadIdx.x & 31, gq = lane >> 2, t = lane & 3;
+        const float scale2 = a.scale * 1.4426950408889634f;
+        Feed ahead(a);
+        CaWalk w = ahead.w;
+        int slot = 0;  // of the block to be read next
+        ahead.look(a);
+        for (int s = 0; s < NS - 1; ++s) feed(a, ahead, s);
+        while (w.next(a)) {
+            const CaRange& r = w.r;
+            const int row0 = w.rt * ROWS, rows = min(ROWS, a.R - row0);
+            const size_t kv = w.kv(a);
+            Rows x;
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            float mx = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], 8));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-            const float f = m[i] == -INFINITY ? 0.f : ca_exp2((m[i] - mx) * k2);
-            l[i] *= f;
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 8);
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 16);
-            if (i >= rows) break;
+            for (int i = 0; i < NT; ++i) {
+                const bool live = 8 * i + gq < rows;
+                const float unit = load_q(a, kv * a.R + row0 + (live ? 8 * i + gq : 0), live, x.q[0][i], TWO ? x.q[TWO][i] : nullptr);
 #pragma unroll
-            for (int d = 0; d < D; d += 2) {
-                float x[2];
+                for (int k = 0; k < HD / 16; ++k) x.o[i][k][0] = x.o[i][k][1] = x.o[i][k][2] = x.o[i][k][3] = 0.f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int row = 8 * i + 2 * t + h;
+                    x.m[i][h] = -INFINITY;
+                    x.l[i][h] = x.lx[i][h] = 0.f;
+                    x.vis[i][h] = row < rows ? r.n - a.n_tok + (a.n_tok == 1 ? 0 : (row0 + row) % a.n_tok) + 1 : 0;
+                    x.unit[i][h] = __shfl_sync(0xffffffffu, unit, 4 * (2 * t + h)) * a.k_unit;
+                    x.k2[i][h] = fminf(fmaxf(scale2 * x.unit[i][h], 1e-37f), 1e38f);  // (0 and infinity would make 0 of nothing)
+                }
+            }
+            for (int b = w.b0; b < w.b1; ++b) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(NS - 2) : "memory");
+                __syncwarp();
+                step(a, ahead, r, r.at(b), slot, kv, row0, rows, x);
+                __syncwarp();  // the block has been read
+                if (++slot == NS) slot = 0;
+            }
+            // a part goes to the workspace while the ring is in use
+            float* part = w.last ? ring_part : P::of_warp(a, w.b0 == 0);
+            if (w.whole && lane == 0) a.info[kv * a.RT + w.rt] = 1 << 16;
+            if (!w.whole && lane == 0) notes[w.b0 == 0] = {part, w.c, w.l, w.g, w.rt, r.n, w.first, w.cta_whole, w.parts};
+            const Head head(a, w.l, w.g);
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float l = x.l[i][h], lx = TWO ? l : x.lx[i][h];
+#pragma unroll
+                    for (int y = 4; y < 32; y <<= 1) {
+                        l += __shfl_xor_sync(0xffffffffu, l, y);
+                        lx += __shfl_xor_sync(0xffffffffu, lx, y);
+                    }
+                    l *= 0x1p-15f;
+                    lx *= 0x1p-15f;
+                    const int row = 8 * i + 2 * t + h, d0 = gq * (HD / 8);
+                    if (row >= rows) continue;
+                    float v[HD / 8];
+#pragma unroll
+                    for (int d = 0; d < HD / 8; ++d) v[d] = x.o[i][d / 2][d % 2 * 2 + h] * 0x1p-15f * a.v_unit;
+                    const float m = x.m[i][h] * x.unit[i][h];
+                    if (w.whole) {
+                        finish_row<CaFour, HD / 8>(a, kv, w.c, r.n, row0 + row, d0, head, v, l);
+                        T* out = static_cast<T*>(a.out) + (kv * a.R + row0 + row) * HD + d0;
+                        __align__(16) T y[HD / 8];
+#pragma unroll
+                        for (int d = 0; d < HD / 8; ++d) y[d] = from_f<T>(v[d]);
+#pragma unroll
+                        for (int d = 0; d < (int)(HD / 8 * sizeof(T) / 16); ++d) reinterpret_cast<uint4*>(out)[d] = reinterpret_cast<const uint4*>(y)[d];
+                        if (gq == 0 && a.lse) a.lse[kv * a.R + row0 + row] = row_lse(m, lx, scale2);
+                    } else {
+#pragma unroll
+                        for (int d = 0; d < HD / 8; d += 4)
+                            *reinterpret_cast<float4*>(part + row * HD + d0 + d) = make_float4(v[d], v[d + 1], v[d + 2], v[d + 3]);
+                        if (gq == 0) {
+                            part[P::M + row] = m;
+                            part[P::L + row] = l;
+                            part[P::LX + row] = lx;
+                        }
+                    }
+                }
+            __syncwarp();
+        }
+    }
+
+    // One block's keys
+    __device__ __forceinline__ void step(const Args& a, Feed& ahead, const CaRange& r, int j0, int slot, size_t kv, int row0, int rows, Rows& x) {
+        const int lane = threadIdx.x & 31, gq = lane >> 2, t = lane & 3;
+        const uint32_t ks = ring + slot * STAGE, vs = ks + CODES, kc = vs + CODES, vc = kc + SCALES;
+        const bool whole = j0 + KB <= r.n - a.n_tok + 1 && (j0 + KB <= a.n_sink || j0 >= r.n - a.window);
+        float s[NT][2][4];  // of keys 16 u + gq (0, 1) and + 8 (2, 3), rows 2 t and + 1
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i) s[i][u][0] = s[i][u][1] = s[i][u][2] = s[i][u][3] = 0.f;
+            uint32_t w[2][HD / 32], sc[2][HD / 64];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const int key = 16 * u + gq + 8 * y;
+                if constexpr (HD == 128) {
+                    load_shared(w[y], ks + at(key, t));
+                    const uint32_t two = scale_halves(load_two_bytes(kc + key * 8 + 2 * t));
+                    sc[y][0] = __byte_perm(two, 0, 0x1010);
+                    sc[y][1] = __byte_perm(two, 0, 0x3232);
+                } else {
+                    load_shared(w[y], ks + at(key, 0) + 8 * t);
+                    sc[y][0] = scale_halves(load_byte(kc + key * 4 + t) * 0x101);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < HD / 32; ++k) {
+                uint32_t h[2][4];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    code_halves(w[y][k], h[y]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) h[y][e] = mul_halves(h[y][e], sc[y][k / 2]);
+                }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    x[e] = o[i][d + e] * f;
-                    x[e] += __shfl_xor_sync(0xffffffffu, x[e], 8);
-                    x[e] += __shfl_xor_sync(0xffffffffu, x[e], 16);
+                    const uint32_t A[4] = {h[0][2 * e], h[1][2 * e], h[0][2 * e + 1], h[1][2 * e + 1]};
+#pragma unroll
+                    for (int i = 0; i < NT; ++i)
+#pragma unroll
+                        for (int y = 0; y < (TWO ? 2 : 1); ++y) mma_f16(s[i][u], A, x.q[y][i][2 * k + e][0], x.q[y][i][2 * k + e][1]);
                 }
-                const int dim = l8 * D + d;
-                if (grp != i) continue;
-                if (walk.whole)
-                    write_row<CaFour>(a, kv, c, r.n, row0 + i, dim, head, x[0], x[1], l[i]);
-                else
-                    *reinterpret_cast<float2*>(part + i * HD + dim) = make_float2(x[0], x[1]);
             }
-            if (lane == 0) {
-                if (!walk.whole)
-                    part[P::M + i] = mx, part[P::L + i] = part[P::LX + i] = l[i];
-                else if (a.lse)
-                    a.lse[kv * a.R + row0 + i] = row_lse(mx, l[i], k2);
+        }
+        feed(a, ahead, slot == 0 ? NS - 1 : slot - 1);  // into the slot that was read last, while the products are under way
+        uint32_t pb[TWO ? 2 : 1][NT][2][2];  // P^T: keys 16 u + 2 t, + 1 (and + 8) of row gq
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            if (!whole) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = j0 + 16 * u + gq + 8 * (e >> 1), v = x.vis[i][e & 1];
+                        s[i][u][e] = key < v && (key < a.n_sink || key >= v - a.window) ? s[i][u][e] : -INFINITY;
+                    }
+            }
+            if (a.z2) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (8 * i + 2 * t + h < rows) {
+                        float* z = a.z2 + (kv * a.R + row0 + 8 * i + 2 * t + h) * a.pitch + j0 + gq;
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            z[16 * u] = s[i][u][h] * x.k2[i][h];
+                            z[16 * u + 8] = s[i][u][2 + h] * x.k2[i][h];
+                        }
+                    }
+            }
+            float from[2], corr[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float cm = fmaxf(fmaxf(s[i][0][h], s[i][0][2 + h]), fmaxf(s[i][1][h], s[i][1][2 + h]));
+#pragma unroll
+                for (int y = 4; y < 32; y <<= 1) cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, y));
+                const float mn = fmaxf(x.m[i][h], cm);
+                corr[h] = mn == x.m[i][h] ? 1.f : ca_exp2((x.m[i][h] - mn) * x.k2[i][h]);
+                from[h] = mn == -INFINITY ? 0.f : mn;
+                x.m[i][h] = mn;
+            }
+            if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    x.l[i][h] *= corr[h];
+                    x.lx[i][h] *= corr[h];
+#pragma unroll
+                    for (int d = 0; d < HD / 16; ++d) {
+                        x.o[i][d][h] *= corr[h];
+                        x.o[i][d][2 + h] *= corr[h];
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const float e0 = ca_exp2(fmaf(s[i][u][2 * half] - from[0], x.k2[i][0], 15.f));
+                    const float e1 = ca_exp2(fmaf(s[i][u][2 * half + 1] - from[1], x.k2[i][1], 15.f));
+                    const uint32_t p = pack_halves(e0, e1);
+                    const float2 f = halves_float2(p);
+                    pb[0][i][u][half] = ca_transpose(p);
+                    // O's sums take the probabilities that the products see, the weights' the exact ones
+                    if constexpr (TWO) {
+                        pb[TWO][i][u][half] = ca_transpose(pack_halves(e0 - f.x, e1 - f.y));
+                        x.l[i][0] += e0;
+                        x.l[i][1] += e1;
+                    } else {
+                        x.l[i][0] += f.x;
+                        x.l[i][1] += f.y;
+                        x.lx[i][0] += e0;
+                        x.lx[i][1] += e1;
+                    }
+                }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            uint32_t w[4][HD / 64], b[4], sc[2];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int key = 16 * u + 2 * t + (y & 1) + 8 * (y >> 1);
+                load_shared(w[y], vs + (HD == 128 ? at(key, gq >> 1) + 8 * (gq & 1) : at(key, 0) + 4 * gq));
+                b[y] = load_byte(vc + key * (HD / 16) + (HD == 128 ? gq : gq >> 1));
+                if (!whole) {  // a scale that no row sees is not to meet a probability of 0
+                    const int j = j0 + key;
+                    b[y] = j < r.n && (j < a.n_sink || j > r.t0 - a.window) ? b[y] : 0;
+                }
+            }
+            sc[0] = scale_halves(b[0] | b[1] << 8);
+            sc[1] = scale_halves(b[2] | b[3] << 8);
+#pragma unroll
+            for (int k = 0; k < HD / 64; ++k) {
+                uint32_t h[4][4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) code_halves(w[y][k], h[y]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t A[4];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        A[2 * y] = mul_halves(__byte_perm(h[2 * y][e], h[2 * y + 1][e], 0x5410), sc[y]);
+                        A[2 * y + 1] = mul_halves(__byte_perm(h[2 * y][e], h[2 * y + 1][e], 0x7632), sc[y]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < NT; ++i)
+#pragma unroll
+                        for (int y = 0; y < (TWO ? 2 : 1); ++y) mma_f16(x.o[i][4 * k + e], A, pb[y][i][u][0], pb[y][i][u][1]);
+                }
             }
         }
     }
 };
+
+template <int HD>
+cudaError_t launch_four(const DevState& s, const Ca4Args& a, int* kernels, cudaStream_t st) {
+    if (s.dtype == 0) return launch<CaFour<float, HD, 1>>(a, {}, s.sms, kernels, st);
+    return a.R <= 8 ? launch<CaFour<bf16, HD, 1>>(a, {}, s.sms, kernels, st) : launch<CaFour<bf16, HD, 2>>(a, {}, s.sms, kernels, st);
+}
 
 }  // namespace
 
@@ -196,8 +470,7 @@ cudaError_t launch_cache4_attention(const DevState& s, const Cache4View& f, cons
     a.Ks = f.Ks; a.Vs = f.Vs;
     a.c_layer = f.c_layer; a.c_page = f.c_page; a.c_head = f.c_head; a.c_pos = f.c_pos;
     a.k_unit = f.k_unit; a.v_unit = f.v_unit;
-    if (s.dtype == 0) return s.hd == 64 ? launch<CaFour<float, 64>>(a, {}, s.sms, kernels, st) : launch<CaFour<float, 128>>(a, {}, s.sms, kernels, st);
-    return s.hd == 64 ? launch<CaFour<bf16, 64>>(a, {}, s.sms, kernels, st) : launch<CaFour<bf16, 128>>(a, {}, s.sms, kernels, st);
+    return s.hd == 64 ? launch_four<64>(s, a, kernels, st) : launch_four<128>(s, a, kernels, st);
 }
 
 }  // namespace mone
