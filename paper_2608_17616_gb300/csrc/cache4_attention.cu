@@ -57,6 +57,12 @@ __device__ __forceinline__ uint32_t pack_halves(float lo, float hi) {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// The low half of each byte from a, the high one from b
+__device__ __forceinline__ uint32_t low_or_high(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xca;" : "=r"(r) : "r"(0x0f0f0f0fu), "r"(a), "r"(b));
+    return r;
+}
 template <int BYTES>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
     if constexpr (BYTES == 16)
@@ -91,8 +97,8 @@ __device__ __forceinline__ uint32_t load_two_bytes(uint32_t addr) {
 // halves of two keys are paired by a permutation.  So nothing but the codes goes through shared memory.
 //
 // Halves hold a row of Q scaled by a power of two to 2^14 .. 2^15 at most (an element 2^-29 of the largest loses bits, 2^-39
-// of it at most), and probabilities times 2^15 (what is below 2^-29 of the row's largest loses bits).  Rows of 32 bits are two
-// halves each, 22 bits, and so are their probabilities.
+// of it at most), and probabilities times 2^7, of a maximum that may since have grown by 2^8 (what is below 2^-21 of the row's
+// largest loses bits).  Rows of 32 bits are two halves each, 22 bits, and so are their probabilities.
 template <typename T_, int HD_, int NT>
 struct CaFour {
     using T = T_;
@@ -103,6 +109,7 @@ struct CaFour {
     static constexpr int NS = HD == 64 ? 4 : 3;
     static constexpr int WARP_BYTES = NS * STAGE;
     static constexpr int CHUNKS = HD / 32;  // of 16 bytes, of a row's codes
+    static constexpr float P_LOG2 = 7.f, P_UNIT_INV = 0x1p-7f, P_ROOM = 8.f, FROM_NONE = -3e38f;
     static_assert(CTAS * (CA_WARPS * WARP_BYTES + Part<HD, ROWS>::FLOATS * 4 + 3072) <= 228 * 1024, "CTAs an SM");
     static_assert(Part<HD, ROWS>::FLOATS * 4 <= WARP_BYTES, "a part fits in the ring");
 
@@ -112,19 +119,32 @@ struct CaFour {
 
     uint32_t ring;
     float* ring_part;  // the ring as the place of the warp's last part
-
-    __device__ CaFour(const NoMaps&, uint8_t* smem, int) : ring(smem_u32(smem)), ring_part(reinterpret_cast<float*>(smem)) {}
+    // bytes in a stage: of the codes that this lane copies, of its eighth's key, of its values 2 t and 2 t + 1, of their scales; all of
+    // the first rows, those after them at fixed distances
+    uint32_t copy_at, key_at, val_at[2], key_scale_at, val_scale_at;
 
     // Byte of chunk c of row r: neighbouring rows, and for head_dim 128 halves of a row, change places so that neither the loads of
-    // keys (neighbouring rows) nor those of values (every other row, the same bytes of each) meet in a bank.
+    // keys (neighbouring rows) nor those of values (every other row, the same bytes of each) meet in a bank.  Rows 8 further on
+    // are 8 rows of bytes further on.
     static __device__ __forceinline__ uint32_t at(int r, int c) { return (r ^ (r >> 2 & 1)) * (HD / 2) + (HD == 128 ? c ^ (r & 2) : c) * 16; }
 
-    // The copies of a warp's blocks, ahead of their reading and on through the pieces: a lane looks up a key's page a block
-    // ahead and copies its scales, neighbours copy its codes.
+    __device__ CaFour(const NoMaps&, uint8_t* smem, int) : ring(smem_u32(smem)), ring_part(reinterpret_cast<float*>(smem)) {
+        const int lane = threadIdx.x & 31, gq = lane >> 2, t = lane & 3;
+        copy_at = at(lane / CHUNKS, lane % CHUNKS);
+        key_at = HD == 128 ? at(gq, t) : at(gq, 0) + 8 * t;
+        for (int y = 0; y < 2; ++y) val_at[y] = CODES + (HD == 128 ? at(2 * t + y, gq >> 1) + 8 * (gq & 1) : at(2 * t + y, 0) + 4 * gq);
+        key_scale_at = 2 * CODES + gq * (HD / 16) + (HD == 128 ? 2 * t : t);
+        val_scale_at = 2 * CODES + SCALES + 2 * t * (HD / 16) + (HD == 128 ? gq : gq >> 1);
+    }
+
+    // The copies of a warp's blocks, ahead of their reading and on through the pieces.  A lane looks up a key's page a block ahead and
+    // copies its scales, neighbours copy its codes: 8 rows with one instruction (head_dim 128) or 16.
     struct Feed {
         CaWalk w;
         int i = 0, n = 0, page;
+        const uint8_t *K, *V, *Ks, *Vs;  // of the piece's head
         __device__ Feed(const Args& a) : w(a) {}
+        __device__ __forceinline__ int key0() const { return w.r.at(w.b0 + i); }
         __device__ __forceinline__ void look(const Args& a) {
             while (i == n) {
                 if (!w.next(a)) {
@@ -133,35 +153,50 @@ struct CaFour {
                 }
                 i = 0;
                 n = w.b1 - w.b0;
+                const FourHead head(a, w.l, w.g);
+                K = head.K, V = head.V, Ks = head.Ks, Vs = head.Vs;
             }
-            const int key = w.r.at(w.b0 + i) + (threadIdx.x & 31);
+            const int key = key0() + (threadIdx.x & 31);
             const bool in = key < w.r.n && (key < a.n_sink || key > w.r.t0 - a.window);
             page = in ? a.v.table[(size_t)w.c * a.v.width + (key >> a.v.page_log2)] : INT_MIN;
         }
     };
     __device__ __forceinline__ void feed(const Args& a, Feed& f, int s) {
+        constexpr int LOG2 = HD == 128 ? 3 : 4, R = 1 << LOG2;  // rows of an instruction
         if (f.n >= 0) {
-            const int lane = threadIdx.x & 31, place = (f.w.r.at(f.w.b0 + f.i) + lane) & ((1 << a.v.page_log2) - 1);
-            bool in = f.page != INT_MIN;
-            if (in && (unsigned)f.page >= (unsigned)a.v.n_pages) {
-                cache_fail(a.v.status, DS_CACHE_PAGE);
-                in = false;
-            }
-            const FourHead head(a, f.w.l, f.w.g);
+            const int lane = threadIdx.x & 31, j0 = f.key0(), mask = (1 << a.v.page_log2) - 1, place = (j0 + lane) & mask;
             const uint32_t dst = ring + s * STAGE, scales = dst + 2 * CODES + lane * (HD / 16);
-            if (in) {
-                const long long off = f.page * head.c_page + place * head.c_pos;
-                copy_async<HD / 16>(scales, head.Ks + off);
-                copy_async<HD / 16>(scales + SCALES, head.Vs + off);
-            }
-            const long long mine = in ? f.page * head.s_page + place * head.s_pos : -1;
+            const int r0 = lane / CHUNKS, c = lane % CHUNKS;
+            if (a.v.page_log2 >= LOG2 && __all_sync(0xffffffffu, (unsigned)f.page < (unsigned)a.v.n_pages)) {  // an instruction's rows lie in a page
+                const long long off = f.page * a.c_page + place * a.c_pos;
+                copy_async<HD / 16>(scales, f.Ks + off);
+                copy_async<HD / 16>(scales + SCALES, f.Vs + off);
 #pragma unroll
-            for (int x = 0; x < CHUNKS; ++x) {
-                const int r = x * (32 / CHUNKS) + lane / CHUNKS, c = lane % CHUNKS;
-                const long long off = __shfl_sync(0xffffffffu, mine, r);
-                if (off < 0) continue;
-                copy_async<16>(dst + at(r, c), head.K + off + 16 * c);
-                copy_async<16>(dst + CODES + at(r, c), head.V + off + 16 * c);
+                for (int x = 0; x < CHUNKS; ++x) {
+                    const int page = __shfl_sync(0xffffffffu, f.page, x * R);
+                    const long long off = page * a.v.s_page + (((j0 + x * R) & mask) + r0) * a.v.s_pos + 16 * c;
+                    copy_async<16>(dst + copy_at + x * R * (HD / 2), f.K + off);
+                    copy_async<16>(dst + copy_at + x * R * (HD / 2) + CODES, f.V + off);
+                }
+            } else {
+                bool in = f.page != INT_MIN;
+                if (in && (unsigned)f.page >= (unsigned)a.v.n_pages) {
+                    cache_fail(a.v.status, DS_CACHE_PAGE);
+                    in = false;
+                }
+                if (in) {
+                    const long long off = f.page * a.c_page + place * a.c_pos;
+                    copy_async<HD / 16>(scales, f.Ks + off);
+                    copy_async<HD / 16>(scales + SCALES, f.Vs + off);
+                }
+                const long long mine = in ? f.page * a.v.s_page + place * a.v.s_pos : -1;
+#pragma unroll 1
+                for (int x = 0; x < CHUNKS; ++x) {
+                    const long long off = __shfl_sync(0xffffffffu, mine, x * R + r0);
+                    if (off < 0) continue;
+                    copy_async<16>(dst + copy_at + x * R * (HD / 2), f.K + off + 16 * c);
+                    copy_async<16>(dst + copy_at + x * R * (HD / 2) + CODES, f.V + off + 16 * c);
+                }
             }
             ++f.i;
             f.look(a);
@@ -174,7 +209,9 @@ struct CaFour {
     struct Rows {
         uint32_t q[TWO ? 2 : 1][NT][HD / 16][2];
         float o[NT][HD / 16][4];
-        float m[NT][2], l[NT][2], lx[NT][2];
+        float l[NT][4];                // the sums of the probabilities that O's products see, in the layout of O (each twice)
+        float lx[NT][2];               // of the exact ones, this lane's
+        float from[NT][2];             // what is taken off a row's S: within 8 of its maximum in base 2, or FROM_NONE
         float unit[NT][2], k2[NT][2];  // of S: the unit in which it is q k, and in base 2 with the softmax's scale
         int vis[NT][2];
     };
@@ -237,8 +274,8 @@ struct CaFour {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int row = 8 * i + 2 * t + h;
-                    x.m[i][h] = -INFINITY;
-                    x.l[i][h] = x.lx[i][h] = 0.f;
+                    x.from[i][h] = FROM_NONE;
+                    x.l[i][h] = x.l[i][2 + h] = x.lx[i][h] = 0.f;
                     x.vis[i][h] = row < rows ? r.n - a.n_tok + (a.n_tok == 1 ? 0 : (row0 + row) % a.n_tok) + 1 : 0;
                     x.unit[i][h] = __shfl_sync(0xffffffffu, unit, 4 * (2 * t + h)) * a.k_unit;
                     x.k2[i][h] = fminf(fmaxf(scale2 * x.unit[i][h], 1e-37f), 1e38f);  // (0 and infinity would make 0 of nothing)
@@ -260,20 +297,15 @@ struct CaFour {
             for (int i = 0; i < NT; ++i)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float l = x.l[i][h], lx = TWO ? l : x.lx[i][h];
+                    float l = x.l[i][h] * P_UNIT_INV, lx = x.lx[i][h] * P_UNIT_INV;
 #pragma unroll
-                    for (int y = 4; y < 32; y <<= 1) {
-                        l += __shfl_xor_sync(0xffffffffu, l, y);
-                        lx += __shfl_xor_sync(0xffffffffu, lx, y);
-                    }
-                    l *= 0x1p-15f;
-                    lx *= 0x1p-15f;
+                    for (int y = 4; y < 32; y <<= 1) lx += __shfl_xor_sync(0xffffffffu, lx, y);
                     const int row = 8 * i + 2 * t + h, d0 = gq * (HD / 8);
                     if (row >= rows) continue;
                     float v[HD / 8];
 #pragma unroll
-                    for (int d = 0; d < HD / 8; ++d) v[d] = x.o[i][d / 2][d % 2 * 2 + h] * 0x1p-15f * a.v_unit;
-                    const float m = x.m[i][h] * x.unit[i][h];
+                    for (int d = 0; d < HD / 8; ++d) v[d] = x.o[i][d / 2][d % 2 * 2 + h] * P_UNIT_INV * a.v_unit;
+                    const float m = x.from[i][h] == FROM_NONE ? -INFINITY : x.from[i][h] * x.unit[i][h];
                     if (w.whole) {
                         finish_row<CaFour, HD / 8>(a, kv, w.c, r.n, row0 + row, d0, head, v, l);
                         T* out = static_cast<T*>(a.out) + (kv * a.R + row0 + row) * HD + d0;
@@ -301,7 +333,7 @@ struct CaFour {
     // One block's keys
     __device__ __forceinline__ void step(const Args& a, Feed& ahead, const CaRange& r, int j0, int slot, size_t kv, int row0, int rows, Rows& x) {
         const int lane = threadIdx.x & 31, gq = lane >> 2, t = lane & 3;
-        const uint32_t ks = ring + slot * STAGE, vs = ks + CODES, kc = vs + CODES, vc = kc + SCALES;
+        const uint32_t stage = ring + slot * STAGE;
         const bool whole = j0 + KB <= r.n - a.n_tok + 1 && (j0 + KB <= a.n_sink || j0 >= r.n - a.window);
         float s[NT][2][4];  // of keys 16 u + gq (0, 1) and + 8 (2, 3), rows 2 t and + 1
 #pragma unroll
@@ -311,15 +343,14 @@ struct CaFour {
             uint32_t w[2][HD / 32], sc[2][HD / 64];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                const int key = 16 * u + gq + 8 * y;
+                const int row = 16 * u + 8 * y;  // and gq
+                load_shared(w[y], stage + key_at + row * (HD / 2));
                 if constexpr (HD == 128) {
-                    load_shared(w[y], ks + at(key, t));
-                    const uint32_t two = scale_halves(load_two_bytes(kc + key * 8 + 2 * t));
+                    const uint32_t two = scale_halves(load_two_bytes(stage + key_scale_at + row * 8));
                     sc[y][0] = __byte_perm(two, 0, 0x1010);
                     sc[y][1] = __byte_perm(two, 0, 0x3232);
                 } else {
-                    load_shared(w[y], ks + at(key, 0) + 8 * t);
-                    sc[y][0] = scale_halves(load_byte(kc + key * 4 + t) * 0x101);
+                    sc[y][0] = scale_halves(load_byte(stage + key_scale_at + row * 4) * 0x101);
                 }
             }
 #pragma unroll
@@ -354,9 +385,39 @@ struct CaFour {
                         s[i][u][e] = key < v && (key < a.n_sink || key >= v - a.window) ? s[i][u][e] : -INFINITY;
                     }
             }
+            // A row whose scores have grown by more than 2^8 (its first ones) is rescaled
+            float most[2];
+            bool grown = false;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                most[h] = fmaxf(fmaxf(s[i][0][h], s[i][0][2 + h]), fmaxf(s[i][1][h], s[i][1][2 + h]));
+                grown |= (most[h] - x.from[i][h]) * x.k2[i][h] > P_ROOM;
+            }
+            if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int y = 4; y < 32; y <<= 1) most[h] = fmaxf(most[h], __shfl_xor_sync(0xffffffffu, most[h], y));
+                    const float to = fmaxf(x.from[i][h], most[h]), f = ca_exp2((x.from[i][h] - to) * x.k2[i][h]);
+                    x.from[i][h] = to;
+                    x.lx[i][h] *= f;
+                    x.l[i][h] *= f;
+#pragma unroll
+                    for (int d = 0; d < HD / 16; ++d) {
+                        x.o[i][d][h] *= f;
+                        x.o[i][d][2 + h] *= f;
+                    }
+                }
+            }
+            float e[2][4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) e[u][k] = ca_exp2(fmaf(s[i][u][k] - x.from[i][k & 1], x.k2[i][k & 1], P_LOG2));
             if (a.z2) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < 2; ++h) {
+                    x.lx[i][h] += (e[0][h] + e[0][2 + h]) + (e[1][h] + e[1][2 + h]);
                     if (8 * i + 2 * t + h < rows) {
                         float* z = a.z2 + (kv * a.R + row0 + 8 * i + 2 * t + h) * a.pitch + j0 + gq;
 #pragma unroll
@@ -365,62 +426,34 @@ struct CaFour {
                             z[16 * u + 8] = s[i][u][2 + h] * x.k2[i][h];
                         }
                     }
-            }
-            float from[2], corr[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float cm = fmaxf(fmaxf(s[i][0][h], s[i][0][2 + h]), fmaxf(s[i][1][h], s[i][1][2 + h]));
-#pragma unroll
-                for (int y = 4; y < 32; y <<= 1) cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, y));
-                const float mn = fmaxf(x.m[i][h], cm);
-                corr[h] = mn == x.m[i][h] ? 1.f : ca_exp2((x.m[i][h] - mn) * x.k2[i][h]);
-                from[h] = mn == -INFINITY ? 0.f : mn;
-                x.m[i][h] = mn;
-            }
-            if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    x.l[i][h] *= corr[h];
-                    x.lx[i][h] *= corr[h];
-#pragma unroll
-                    for (int d = 0; d < HD / 16; ++d) {
-                        x.o[i][d][h] *= corr[h];
-                        x.o[i][d][2 + h] *= corr[h];
-                    }
                 }
             }
+            const uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < 2; ++u) {
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const float e0 = ca_exp2(fmaf(s[i][u][2 * half] - from[0], x.k2[i][0], 15.f));
-                    const float e1 = ca_exp2(fmaf(s[i][u][2 * half + 1] - from[1], x.k2[i][1], 15.f));
-                    const uint32_t p = pack_halves(e0, e1);
-                    const float2 f = halves_float2(p);
+                    const uint32_t p = pack_halves(e[u][2 * half], e[u][2 * half + 1]);
                     pb[0][i][u][half] = ca_transpose(p);
-                    // O's sums take the probabilities that the products see, the weights' the exact ones
                     if constexpr (TWO) {
-                        pb[TWO][i][u][half] = ca_transpose(pack_halves(e0 - f.x, e1 - f.y));
-                        x.l[i][0] += e0;
-                        x.l[i][1] += e1;
-                    } else {
-                        x.l[i][0] += f.x;
-                        x.l[i][1] += f.y;
-                        x.lx[i][0] += e0;
-                        x.lx[i][1] += e1;
+                        const float2 f = halves_float2(p);
+                        pb[TWO][i][u][half] = ca_transpose(pack_halves(e[u][2 * half] - f.x, e[u][2 * half + 1] - f.y));
                     }
                 }
+#pragma unroll
+                for (int y = 0; y < (TWO ? 2 : 1); ++y) mma_f16(x.l[i], ones, pb[y][i][u][0], pb[y][i][u][1]);
+            }
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             uint32_t w[4][HD / 64], b[4], sc[2];
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
-                const int key = 16 * u + 2 * t + (y & 1) + 8 * (y >> 1);
-                load_shared(w[y], vs + (HD == 128 ? at(key, gq >> 1) + 8 * (gq & 1) : at(key, 0) + 4 * gq));
-                b[y] = load_byte(vc + key * (HD / 16) + (HD == 128 ? gq : gq >> 1));
+                const int row = 16 * u + 8 * (y >> 1);  // and 2 t, and 1
+                load_shared(w[y], stage + val_at[y & 1] + row * (HD / 2));
+                b[y] = load_byte(stage + val_scale_at + (row + (y & 1)) * (HD / 16));
                 if (!whole) {  // a scale that no row sees is not to meet a probability of 0
-                    const int j = j0 + key;
+                    const int j = j0 + row + 2 * t + (y & 1);
                     b[y] = j < r.n && (j < a.n_sink || j > r.t0 - a.window) ? b[y] : 0;
                 }
             }
@@ -428,17 +461,18 @@ struct CaFour {
             sc[1] = scale_halves(b[2] | b[3] << 8);
 #pragma unroll
             for (int k = 0; k < HD / 64; ++k) {
-                uint32_t h[4][4];
+                uint32_t h[2][2][4];  // of keys 2 t and + 1 (and + 8), elements 8 k + 2 e and + 1: a code of either in a byte
 #pragma unroll
-                for (int y = 0; y < 4; ++y) code_halves(w[y][k], h[y]);
+                for (int y = 0; y < 2; ++y) {
+                    const uint32_t p = w[2 * y][k], q = w[2 * y + 1][k];
+                    code_halves(low_or_high(p, q << 4), h[y][0]);
+                    code_halves(low_or_high(p >> 4, q), h[y][1]);
+                }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     uint32_t A[4];
 #pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        A[2 * y] = mul_halves(__byte_perm(h[2 * y][e], h[2 * y + 1][e], 0x5410), sc[y]);
-                        A[2 * y + 1] = mul_halves(__byte_perm(h[2 * y][e], h[2 * y + 1][e], 0x7632), sc[y]);
-                    }
+                    for (int y = 0; y < 4; ++y) A[y] = mul_halves(h[y >> 1][y & 1][e], sc[y >> 1]);
 #pragma unroll
                     for (int i = 0; i < NT; ++i)
 #pragma unroll
