@@ -10,6 +10,7 @@ struct Ca4Args : CaArgs {
     const uint8_t *Ks, *Vs;  // scales, strides in bytes
     long long c_layer, c_page, c_head, c_pos;
     float k_unit, v_unit;
+    int near;  // 8 rows (head_dim 128) or 16 lie in a page, and its strides and its rows' have 32 bits
 };
 
 struct FourHead {
@@ -98,27 +99,30 @@ __device__ __forceinline__ uint32_t load_two_bytes(uint32_t addr) {
 //
 // Halves hold a row of Q scaled by a power of two to 2^14 .. 2^15 at most (an element 2^-29 of the largest loses bits, 2^-39
 // of it at most), and probabilities times 2^7, of a maximum that may since have grown by 2^8 (what is below 2^-21 of the row's
-// largest loses bits).  Rows of 32 bits are two halves each, 22 bits, and so are their probabilities.
-template <typename T_, int HD_, int NT>
+// largest loses bits).  Rows of 32 bits are two halves each, 22 bits, and so are their probabilities: up to four rows (BESIDE) lie
+// beside their rests in the N of 8, of more both are multiplied one after the other.
+template <typename T_, int HD_, int NT, bool BESIDE>
 struct CaFour {
     using T = T_;
-    static constexpr bool TWO = std::is_same<T, float>::value;
-    static constexpr int HD = HD_, ROWS = 8 * NT, CTAS = NT == 1 ? 3 : 2;
+    static constexpr bool TWO = std::is_same<T, float>::value && !BESIDE;
+    static constexpr int HD = HD_, ROWS = BESIDE ? 4 : 8 * NT, CTAS = NT == 1 ? (TWO ? 3 : 4) : 2;
     static constexpr int ONE = 3, EACH = 2, FULL = 16, FEW = 6;          // blocks of a warp, see item_ctas
     static constexpr int CODES = KB * HD / 2, SCALES = KB * HD / 16, STAGE = 2 * (CODES + SCALES);
     static constexpr int NS = HD == 64 ? 4 : 3;
-    static constexpr int WARP_BYTES = NS * STAGE;
+    static constexpr int WALKS = NS * STAGE, WARP_BYTES = WALKS + 256, ALIGN = 128;  // the ring, the warp's walks
     static constexpr int CHUNKS = HD / 32;  // of 16 bytes, of a row's codes
     static constexpr float P_LOG2 = 7.f, P_UNIT_INV = 0x1p-7f, P_ROOM = 8.f, FROM_NONE = -3e38f;
-    static_assert(CTAS * (CA_WARPS * WARP_BYTES + Part<HD, ROWS>::FLOATS * 4 + 3072) <= 228 * 1024, "CTAs an SM");
-    static_assert(Part<HD, ROWS>::FLOATS * 4 <= WARP_BYTES, "a part fits in the ring");
+    static_assert(CTAS * (CA_WARPS * WARP_BYTES + ALIGN + 1536) <= 228 * 1024, "CTAs an SM");
+    static_assert(Part<HD, ROWS>::FLOATS * 4 <= WALKS, "a part fits in the ring");
+    static_assert(2 * sizeof(CaWalk) <= 256, "the walks");
 
     using Args = Ca4Args;
     using Maps = NoMaps;
     using Head = FourHead;
 
-    uint32_t ring;
+    uint32_t ring, lane;
     float* ring_part;  // the ring as the place of the warp's last part
+    CaWalk* walks;     // that of the copies, that of the products: not in registers while a piece's blocks go through
     // bytes in a stage: of the codes that this lane copies, of its eighth's key, of its values 2 t and 2 t + 1, of their scales; all of
     // the first rows, those after them at fixed distances
     uint32_t copy_at, key_at, val_at[2], key_scale_at, val_scale_at;
@@ -128,8 +132,11 @@ struct CaFour {
     // are 8 rows of bytes further on.
     static __device__ __forceinline__ uint32_t at(int r, int c) { return (r ^ (r >> 2 & 1)) * (HD / 2) + (HD == 128 ? c ^ (r & 2) : c) * 16; }
 
-    __device__ CaFour(const NoMaps&, uint8_t* smem, int) : ring(smem_u32(smem)), ring_part(reinterpret_cast<float*>(smem)) {
-        const int lane = threadIdx.x & 31, gq = lane >> 2, t = lane & 3;
+    __device__ CaFour(const NoMaps&, uint8_t* smem, int) : ring_part(reinterpret_cast<float*>(smem)), walks(reinterpret_cast<CaWalk*>(smem + WALKS)) {
+        // (kept in registers: found anew for every block they took 13 instructions of 750)
+        asm volatile("mov.b32 %0, %1;" : "=r"(ring) : "r"(smem_u32(smem)));
+        asm volatile("mov.u32 %0, %%laneid;" : "=r"(lane));
+        const int gq = lane >> 2, t = lane & 3;
         copy_at = at(lane / CHUNKS, lane % CHUNKS);
         key_at = HD == 128 ? at(gq, t) : at(gq, 0) + 8 * t;
         for (int y = 0; y < 2; ++y) val_at[y] = CODES + (HD == 128 ? at(2 * t + y, gq >> 1) + 8 * (gq & 1) : at(2 * t + y, 0) + 4 * gq);
@@ -140,43 +147,62 @@ struct CaFour {
     // The copies of a warp's blocks, ahead of their reading and on through the pieces.  A lane looks up a key's page a block ahead and
     // copies its scales, neighbours copy its codes: 8 rows with one instruction (head_dim 128) or 16.
     struct Feed {
-        CaWalk w;
-        int i = 0, n = 0, page;
-        const uint8_t *K, *V, *Ks, *Vs;  // of the piece's head
-        __device__ Feed(const Args& a) : w(a) {}
-        __device__ __forceinline__ int key0() const { return w.r.at(w.b0 + i); }
-        __device__ __forceinline__ void look(const Args& a) {
-            while (i == n) {
-                if (!w.next(a)) {
-                    n = -1;
+        int left = 0, j0, page;  // blocks of the piece (-1: no more pieces); the first key of the next, the lane's key's page
+        int n, t0, gap, lo;      // of the piece's range: positions, the oldest token's; the first positions' end, the first after them
+        const uint8_t *K, *Ks;   // of the piece's head, chunk lane % CHUNKS; V is as far from K in every head
+        const int* table;
+    };
+    // The next piece of a walk
+    __device__ __forceinline__ bool next(const Args& a, CaWalk* at, CaWalk& w) const {
+        w = *at;
+        __syncwarp();
+        if (!w.next(a)) return false;
+        if (lane == 0) *at = w;
+        __syncwarp();
+        return true;
+    }
+    __device__ __forceinline__ void look(const Args& a, Feed& f) {
+        if (f.left) {
+            f.j0 += KB;
+            if (f.j0 == f.gap) f.j0 = f.lo;
+        } else {
+            CaWalk w;
+            do {
+                if (!next(a, walks, w)) {
+                    f.left = -1;
                     return;
                 }
-                i = 0;
-                n = w.b1 - w.b0;
-                const FourHead head(a, w.l, w.g);
-                K = head.K, V = head.V, Ks = head.Ks, Vs = head.Vs;
-            }
-            const int key = key0() + (threadIdx.x & 31);
-            const bool in = key < w.r.n && (key < a.n_sink || key > w.r.t0 - a.window);
-            page = in ? a.v.table[(size_t)w.c * a.v.width + (key >> a.v.page_log2)] : INT_MIN;
+                f.left = w.b1 - w.b0;
+            } while (f.left == 0);
+            f.n = w.r.n, f.t0 = w.r.t0, f.gap = w.r.ns * KB, f.lo = w.r.lo;
+            f.j0 = w.r.at(w.b0);
+            const FourHead head(a, w.l, w.g);
+            f.K = head.K + 16 * (lane % CHUNKS), f.Ks = head.Ks;
+            f.table = a.v.table + (size_t)w.c * a.v.width;
         }
-    };
+        const int key = f.j0 + lane;
+        const bool in = key < f.n && (key < a.n_sink || key > f.t0 - a.window);
+        f.page = in ? f.table[key >> a.v.page_log2] : INT_MIN;
+    }
     __device__ __forceinline__ void feed(const Args& a, Feed& f, int s) {
-        constexpr int LOG2 = HD == 128 ? 3 : 4, R = 1 << LOG2;  // rows of an instruction
-        if (f.n >= 0) {
-            const int lane = threadIdx.x & 31, j0 = f.key0(), mask = (1 << a.v.page_log2) - 1, place = (j0 + lane) & mask;
-            const uint32_t dst = ring + s * STAGE, scales = dst + 2 * CODES + lane * (HD / 16);
-            const int r0 = lane / CHUNKS, c = lane % CHUNKS;
-            if (a.v.page_log2 >= LOG2 && __all_sync(0xffffffffu, (unsigned)f.page < (unsigned)a.v.n_pages)) {  // an instruction's rows lie in a page
-                const long long off = f.page * a.c_page + place * a.c_pos;
+        constexpr int R = 32 / CHUNKS;  // rows of an instruction
+        if (f.left >= 0) {
+            const int mask = (1 << a.v.page_log2) - 1, r0 = lane / CHUNKS;
+            const long long to_v = static_cast<const uint8_t*>(a.v.V) - static_cast<const uint8_t*>(a.v.K), to_vs = a.Vs - a.Ks;
+            const uint32_t dst = ring + s * STAGE + copy_at, scales = ring + s * STAGE + 2 * CODES + lane * (HD / 16);
+            // All are there, an instruction's rows lie in a page, and strides have 32 bits
+            if (__builtin_expect(a.near && __all_sync(0xffffffffu, (unsigned)f.page < (unsigned)a.v.n_pages), 1)) {
+                auto place = [&](unsigned page, unsigned row, long long s_page, long long s_pos) {
+                    return (unsigned long long)page * (unsigned)s_page + (unsigned long long)row * (unsigned)s_pos;
+                };
+                const unsigned long long off = place(f.page, (f.j0 + lane) & mask, a.c_page, a.c_pos);
                 copy_async<HD / 16>(scales, f.Ks + off);
-                copy_async<HD / 16>(scales + SCALES, f.Vs + off);
+                copy_async<HD / 16>(scales + SCALES, f.Ks + off + to_vs);
 #pragma unroll
                 for (int x = 0; x < CHUNKS; ++x) {
-                    const int page = __shfl_sync(0xffffffffu, f.page, x * R);
-                    const long long off = page * a.v.s_page + (((j0 + x * R) & mask) + r0) * a.v.s_pos + 16 * c;
-                    copy_async<16>(dst + copy_at + x * R * (HD / 2), f.K + off);
-                    copy_async<16>(dst + copy_at + x * R * (HD / 2) + CODES, f.V + off);
+                    const unsigned long long off = place(__shfl_sync(0xffffffffu, f.page, x * R), ((f.j0 + x * R) & mask) + r0, a.v.s_page, a.v.s_pos);
+                    copy_async<16>(dst + x * R * (HD / 2), f.K + off);
+                    copy_async<16>(dst + x * R * (HD / 2) + CODES, f.K + off + to_v);
                 }
             } else {
                 bool in = f.page != INT_MIN;
@@ -184,42 +210,47 @@ struct CaFour {
                     cache_fail(a.v.status, DS_CACHE_PAGE);
                     in = false;
                 }
+                const int row = (f.j0 + lane) & mask;
                 if (in) {
-                    const long long off = f.page * a.c_page + place * a.c_pos;
+                    const long long off = f.page * a.c_page + row * a.c_pos;
                     copy_async<HD / 16>(scales, f.Ks + off);
-                    copy_async<HD / 16>(scales + SCALES, f.Vs + off);
+                    copy_async<HD / 16>(scales + SCALES, f.Ks + off + to_vs);
                 }
-                const long long mine = in ? f.page * a.v.s_page + place * a.v.s_pos : -1;
+                const long long mine = in ? f.page * a.v.s_page + row * a.v.s_pos : -1;
 #pragma unroll 1
                 for (int x = 0; x < CHUNKS; ++x) {
                     const long long off = __shfl_sync(0xffffffffu, mine, x * R + r0);
                     if (off < 0) continue;
-                    copy_async<16>(dst + copy_at + x * R * (HD / 2), f.K + off + 16 * c);
-                    copy_async<16>(dst + copy_at + x * R * (HD / 2) + CODES, f.V + off + 16 * c);
+                    copy_async<16>(dst + x * R * (HD / 2), f.K + off);
+                    copy_async<16>(dst + x * R * (HD / 2) + CODES, f.K + off + to_v);
                 }
             }
-            ++f.i;
-            f.look(a);
+            --f.left;
+            look(a, f);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
 
     // A warp's rows of an item and what it has of them.  Lane 4 gq + t has a quarter of Q of row 8 i + gq, dimensions from t HD / 4; S
-    // and the sums of rows 8 i + 2 t and + 1, and of these O's dimensions gq HD / 8 + 2 m (0, 1) and + 1 (2, 3).
+    // and the sums of rows 8 i + 2 t and + 1, and of these O's dimensions gq HD / 8 + 2 m (0, 1) and + 1 (2, 3).  (BESIDE: of row
+    // gq % 4, if gq >= 4 its rest; of rows 2 (t % 2) and + 1, if t >= 2 what their rests give to O.)
     struct Rows {
         uint32_t q[TWO ? 2 : 1][NT][HD / 16][2];
         float o[NT][HD / 16][4];
         float l[NT][4];                // the sums of the probabilities that O's products see, in the layout of O (each twice)
         float lx[NT][2];               // of the exact ones, this lane's
         float from[NT][2];             // what is taken off a row's S: within 8 of its maximum in base 2, or FROM_NONE
-        float unit[NT][2], k2[NT][2];  // of S: the unit in which it is q k, and in base 2 with the softmax's scale
+        float unit[NT], k2[NT][2];     // of S: the unit in which it is q k (of row 8 i + gq), and in base 2 with the softmax's scale
         int vis[NT][2];
     };
 
+    // the row of h = 0, 1
+    __device__ __forceinline__ int row_of(int i, int h) const { return BESIDE ? 2 * (lane & 1) + h : 8 * i + 2 * (lane & 3) + h; }
+
     // Q of row `row` of all, this lane's quarter, and the power of two that it is to be multiplied with
-    static __device__ __forceinline__ float load_q(const Args& a, size_t row, bool live, uint32_t (&hi)[HD / 16][2], uint32_t (*lo)[2]) {
+    __device__ __forceinline__ float load_q(const Args& a, size_t row, bool live, uint32_t (&hi)[HD / 16][2], uint32_t (*lo)[2]) const {
         constexpr int D = HD / 4, PER = 16 / sizeof(T);
-        const int t = threadIdx.x & 3;
+        const int t = lane & 3;
         const T* q = static_cast<const T*>(a.Q) + row * HD + t * D;
         float x[D], most = 0.f;
 #pragma unroll
@@ -243,9 +274,13 @@ struct CaFour {
             const float x0 = finite || !isfinite(x[i]) ? x[i] * scale : 0.f, x1 = finite || !isfinite(x[i + 1]) ? x[i + 1] * scale : 0.f;
             const uint32_t h = pack_halves(x0, x1);
             hi[i / 4][i / 2 % 2] = h;
-            if constexpr (TWO) {
+            if constexpr (TWO || BESIDE) {
                 const float2 f = halves_float2(h);
-                lo[i / 4][i / 2 % 2] = finite ? pack_halves(x0 - f.x, x1 - f.y) : 0;
+                const uint32_t rest = finite ? pack_halves(x0 - f.x, x1 - f.y) : 0;
+                if constexpr (TWO)
+                    lo[i / 4][i / 2 % 2] = rest;
+                else if (lane >= 16)
+                    hi[i / 4][i / 2 % 2] = rest;
             }
         }
         return unit;
@@ -253,45 +288,58 @@ struct CaFour {
 
     __device__ __forceinline__ void run(const Args& a, CaNote* notes) {
         using P = Part<HD, ROWS>;
-        const int lane = threadIdx.x & 31, gq = lane >> 2, t = lane & 3;
+        const int gq = lane >> 2, t = lane & 3;
         const float scale2 = a.scale * 1.4426950408889634f;
-        Feed ahead(a);
-        CaWalk w = ahead.w;
+        CaWalk w(a);
+        if (lane == 0) walks[0] = walks[1] = w;
+        __syncwarp();
+        Feed ahead;
         int slot = 0;  // of the block to be read next
-        ahead.look(a);
+        look(a, ahead);
         for (int s = 0; s < NS - 1; ++s) feed(a, ahead, s);
-        while (w.next(a)) {
-            const CaRange& r = w.r;
+        while (next(a, walks + 1, w)) {
             const int row0 = w.rt * ROWS, rows = min(ROWS, a.R - row0);
-            const size_t kv = w.kv(a);
+            const CaRange r = w.r;
             Rows x;
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
-                const bool live = 8 * i + gq < rows;
-                const float unit = load_q(a, kv * a.R + row0 + (live ? 8 * i + gq : 0), live, x.q[0][i], TWO ? x.q[TWO][i] : nullptr);
+                const int q_row = BESIDE ? gq & 3 : 8 * i + gq;
+                const bool live = q_row < rows;
+                x.unit[i] = load_q(a, w.kv(a) * a.R + row0 + (live ? q_row : 0), live, x.q[0][i], TWO ? x.q[TWO][i] : nullptr) * a.k_unit;
 #pragma unroll
                 for (int k = 0; k < HD / 16; ++k) x.o[i][k][0] = x.o[i][k][1] = x.o[i][k][2] = x.o[i][k][3] = 0.f;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int row = 8 * i + 2 * t + h;
+                    const int row = row_of(i, h);
                     x.from[i][h] = FROM_NONE;
                     x.l[i][h] = x.l[i][2 + h] = x.lx[i][h] = 0.f;
                     x.vis[i][h] = row < rows ? r.n - a.n_tok + (a.n_tok == 1 ? 0 : (row0 + row) % a.n_tok) + 1 : 0;
-                    x.unit[i][h] = __shfl_sync(0xffffffffu, unit, 4 * (2 * t + h)) * a.k_unit;
-                    x.k2[i][h] = fminf(fmaxf(scale2 * x.unit[i][h], 1e-37f), 1e38f);  // (0 and infinity would make 0 of nothing)
+                    const float k2 = scale2 * __shfl_sync(0xffffffffu, x.unit[i], 4 * (row - 8 * i));
+                    x.k2[i][h] = fminf(fmaxf(k2, 1e-37f), 1e38f);  // (0 and infinity would make 0 of nothing)
                 }
             }
-            for (int b = w.b0; b < w.b1; ++b) {
+            int j0 = r.at(w.b0);
+            float* z = a.z2 ? a.z2 + (w.kv(a) * a.R + row0) * a.pitch + gq : nullptr;
+#pragma unroll 1
+            for (int left = w.b1 - w.b0; left > 0; --left) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(NS - 2) : "memory");
                 __syncwarp();
-                step(a, ahead, r, r.at(b), slot, kv, row0, rows, x);
+                feed(a, ahead, slot == 0 ? NS - 1 : slot - 1);  // into the slot that was read last
+                if (__builtin_expect(j0 + KB <= r.n - a.n_tok + 1 && (j0 + KB <= a.n_sink || j0 >= r.n - a.window), 1))
+                    step<true>(a, r, j0, slot, z, rows, x);
+                else
+                    step<false>(a, r, j0, slot, z, rows, x);
                 __syncwarp();  // the block has been read
                 if (++slot == NS) slot = 0;
+                j0 += KB;
+                if (j0 == r.ns * KB) j0 = r.lo;
             }
+            w = walks[1];
+            const size_t kv = w.kv(a);
             // a part goes to the workspace while the ring is in use
             float* part = w.last ? ring_part : P::of_warp(a, w.b0 == 0);
             if (w.whole && lane == 0) a.info[kv * a.RT + w.rt] = 1 << 16;
-            if (!w.whole && lane == 0) notes[w.b0 == 0] = {part, w.c, w.l, w.g, w.rt, r.n, w.first, w.cta_whole, w.parts};
+            if (!w.whole && lane == 0) notes[w.b0 == 0] = {part, w.c, w.l, w.g, w.rt, w.r.n, w.first, w.cta_whole, w.parts};
             const Head head(a, w.l, w.g);
 #pragma unroll
             for (int i = 0; i < NT; ++i)
@@ -300,21 +348,29 @@ struct CaFour {
                     float l = x.l[i][h] * P_UNIT_INV, lx = x.lx[i][h] * P_UNIT_INV;
 #pragma unroll
                     for (int y = 4; y < 32; y <<= 1) lx += __shfl_xor_sync(0xffffffffu, lx, y);
-                    const int row = 8 * i + 2 * t + h, d0 = gq * (HD / 8);
-                    if (row >= rows) continue;
+                    const int row = row_of(i, h), d0 = gq * (HD / 8);
+                    const float unit = __shfl_sync(0xffffffffu, x.unit[i], 4 * (row - 8 * i));
                     float v[HD / 8];
 #pragma unroll
-                    for (int d = 0; d < HD / 8; ++d) v[d] = x.o[i][d / 2][d % 2 * 2 + h] * P_UNIT_INV * a.v_unit;
-                    const float m = x.from[i][h] == FROM_NONE ? -INFINITY : x.from[i][h] * x.unit[i][h];
+                    for (int d = 0; d < HD / 8; ++d) v[d] = x.o[i][d / 2][d % 2 * 2 + h] * P_UNIT_INV;
+                    if constexpr (BESIDE) {
+                        l += __shfl_xor_sync(0xffffffffu, l, 2);
+#pragma unroll
+                        for (int d = 0; d < HD / 8; ++d) v[d] += __shfl_xor_sync(0xffffffffu, v[d], 2);
+                    }
+                    if (row >= rows || (BESIDE && t >= 2)) continue;
+#pragma unroll
+                    for (int d = 0; d < HD / 8; ++d) v[d] *= a.v_unit;
+                    const float m = x.from[i][h] == FROM_NONE ? -INFINITY : x.from[i][h] * unit;
                     if (w.whole) {
-                        finish_row<CaFour, HD / 8>(a, kv, w.c, r.n, row0 + row, d0, head, v, l);
-                        T* out = static_cast<T*>(a.out) + (kv * a.R + row0 + row) * HD + d0;
+                        finish_row<CaFour, HD / 8>(a, kv, w.c, w.r.n, w.rt * ROWS + row, d0, head, v, l);
+                        T* out = static_cast<T*>(a.out) + (kv * a.R + w.rt * ROWS + row) * HD + d0;
                         __align__(16) T y[HD / 8];
 #pragma unroll
                         for (int d = 0; d < HD / 8; ++d) y[d] = from_f<T>(v[d]);
 #pragma unroll
                         for (int d = 0; d < (int)(HD / 8 * sizeof(T) / 16); ++d) reinterpret_cast<uint4*>(out)[d] = reinterpret_cast<const uint4*>(y)[d];
-                        if (gq == 0 && a.lse) a.lse[kv * a.R + row0 + row] = row_lse(m, lx, scale2);
+                        if (gq == 0 && a.lse) a.lse[kv * a.R + w.rt * ROWS + row] = row_lse(m, lx, scale2);
                     } else {
 #pragma unroll
                         for (int d = 0; d < HD / 8; d += 4)
@@ -330,11 +386,11 @@ struct CaFour {
         }
     }
 
-    // One block's keys
-    __device__ __forceinline__ void step(const Args& a, Feed& ahead, const CaRange& r, int j0, int slot, size_t kv, int row0, int rows, Rows& x) {
-        const int lane = threadIdx.x & 31, gq = lane >> 2, t = lane & 3;
+    // One block's keys; WHOLE: every row sees all of them
+    template <bool WHOLE>
+    __device__ __forceinline__ void step(const Args& a, const CaRange& r, int j0, int slot, float* z2, int rows, Rows& x) {
+        const int gq = lane >> 2, t = lane & 3;
         const uint32_t stage = ring + slot * STAGE;
-        const bool whole = j0 + KB <= r.n - a.n_tok + 1 && (j0 + KB <= a.n_sink || j0 >= r.n - a.window);
         float s[NT][2][4];  // of keys 16 u + gq (0, 1) and + 8 (2, 3), rows 2 t and + 1
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -372,11 +428,16 @@ struct CaFour {
                 }
             }
         }
-        feed(a, ahead, slot == 0 ? NS - 1 : slot - 1);  // into the slot that was read last, while the products are under way
+        if constexpr (BESIDE) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[0][u][e] += __shfl_xor_sync(0xffffffffu, s[0][u][e], 2);
+        }
         uint32_t pb[TWO ? 2 : 1][NT][2][2];  // P^T: keys 16 u + 2 t, + 1 (and + 8) of row gq
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-            if (!whole) {
+            if (!WHOLE) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -414,12 +475,12 @@ struct CaFour {
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) e[u][k] = ca_exp2(fmaf(s[i][u][k] - x.from[i][k & 1], x.k2[i][k & 1], P_LOG2));
-            if (a.z2) {
+            if (z2) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     x.lx[i][h] += (e[0][h] + e[0][2 + h]) + (e[1][h] + e[1][2 + h]);
-                    if (8 * i + 2 * t + h < rows) {
-                        float* z = a.z2 + (kv * a.R + row0 + 8 * i + 2 * t + h) * a.pitch + j0 + gq;
+                    if (row_of(i, h) < rows && !(BESIDE && t >= 2)) {
+                        float* z = z2 + row_of(i, h) * a.pitch + j0;
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
                             z[16 * u] = s[i][u][h] * x.k2[i][h];
@@ -433,7 +494,12 @@ struct CaFour {
             for (int u = 0; u < 2; ++u) {
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const uint32_t p = pack_halves(e[u][2 * half], e[u][2 * half + 1]);
+                    uint32_t p = pack_halves(e[u][2 * half], e[u][2 * half + 1]);
+                    if constexpr (BESIDE) {
+                        const float2 f = halves_float2(p);
+                        const uint32_t rest = pack_halves(e[u][2 * half] - f.x, e[u][2 * half + 1] - f.y);
+                        p = t >= 2 ? rest : p;
+                    }
                     pb[0][i][u][half] = ca_transpose(p);
                     if constexpr (TWO) {
                         const float2 f = halves_float2(p);
@@ -452,7 +518,7 @@ struct CaFour {
                 const int row = 16 * u + 8 * (y >> 1);  // and 2 t, and 1
                 load_shared(w[y], stage + val_at[y & 1] + row * (HD / 2));
                 b[y] = load_byte(stage + val_scale_at + (row + (y & 1)) * (HD / 16));
-                if (!whole) {  // a scale that no row sees is not to meet a probability of 0
+                if (!WHOLE) {  // a scale that no row sees is not to meet a probability of 0
                     const int j = j0 + row + 2 * t + (y & 1);
                     b[y] = j < r.n && (j < a.n_sink || j > r.t0 - a.window) ? b[y] : 0;
                 }
@@ -485,8 +551,9 @@ struct CaFour {
 
 template <int HD>
 cudaError_t launch_four(const DevState& s, const Ca4Args& a, int* kernels, cudaStream_t st) {
-    if (s.dtype == 0) return launch<CaFour<float, HD, 1>>(a, {}, s.sms, kernels, st);
-    return a.R <= 8 ? launch<CaFour<bf16, HD, 1>>(a, {}, s.sms, kernels, st) : launch<CaFour<bf16, HD, 2>>(a, {}, s.sms, kernels, st);
+    if (s.dtype == 0)
+        return a.R <= 4 ? launch<CaFour<float, HD, 1, true>>(a, {}, s.sms, kernels, st) : launch<CaFour<float, HD, 1, false>>(a, {}, s.sms, kernels, st);
+    return a.R <= 8 ? launch<CaFour<bf16, HD, 1, false>>(a, {}, s.sms, kernels, st) : launch<CaFour<bf16, HD, 2, false>>(a, {}, s.sms, kernels, st);
 }
 
 }  // namespace
@@ -504,6 +571,7 @@ cudaError_t launch_cache4_attention(const DevState& s, const Cache4View& f, cons
     a.Ks = f.Ks; a.Vs = f.Vs;
     a.c_layer = f.c_layer; a.c_page = f.c_page; a.c_head = f.c_head; a.c_pos = f.c_pos;
     a.k_unit = f.k_unit; a.v_unit = f.v_unit;
+    a.near = f.v.page_log2 >= (s.hd == 64 ? 4 : 3) && std::max({f.v.s_page, f.v.s_pos, f.c_page, f.c_pos}) < 1ll << 32;
     return s.hd == 64 ? launch_four<64>(s, a, kernels, st) : launch_four<128>(s, a, kernels, st);
 }
 

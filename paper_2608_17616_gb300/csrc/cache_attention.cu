@@ -15,7 +15,7 @@ struct CaCores {
     static constexpr int VE = 16 / sizeof(T), D = HD / 8, NP = D / VE;  // elements of 16 bytes; dimensions and 16-byte pieces of a lane
     static constexpr int U = 2;                                         // keys of a lane group at a time
     static constexpr int ONE = 1, EACH = 1, FULL = 1, FEW = 1;          // blocks of a warp, see item_ctas
-    static constexpr int WARP_BYTES = 2 * Part<HD, ROWS>::FLOATS * 4;
+    static constexpr int WARP_BYTES = 2 * Part<HD, ROWS>::FLOATS * 4, ALIGN = 16;
 
     using Args = CaArgs;
     using Maps = NoMaps;
@@ -222,7 +222,7 @@ struct CaTensor {
     static constexpr int ONE = 3, EACH = 2, FULL = 16, FEW = 6 / SPB;                // blocks of a warp, see item_ctas
     static constexpr int SLAB = SK * 128, TILE = HD / 64 * SLAB, STAGE = 2 * TILE;  // 64 dimensions of the keys; keys; both
     static constexpr int NS = 3;
-    static constexpr int BAR = NS * STAGE, WARP_BYTES = BAR + 1024;  // the ring, its barriers
+    static constexpr int BAR = NS * STAGE, WARP_BYTES = BAR + 1024, ALIGN = 1024;  // the ring, its barriers
     static_assert(CTAS * (CA_WARPS * WARP_BYTES + 3072) <= 228 * 1024, "CTAs an SM");
     static_assert(Part<HD, ROWS>::FLOATS * 4 <= BAR, "a part fits in the ring");
 

@@ -129,6 +129,7 @@ struct CaWalk {
     bool whole, cta_whole;    // the warp has the item whole, the CTA has
     bool first, last;         // the item begins in the CTA's share; the warp's last piece
     int cta0, cta1;           // the CTA's units
+    __device__ CaWalk() {}
     __device__ CaWalk(const CaArgs& a) {
         const int warp = threadIdx.x >> 5;
         auto share_out = [&]() {
@@ -186,7 +187,7 @@ struct CaWalk {
     __device__ size_t kv(const CaArgs& a) const { return ((size_t)c * a.v.L + l) * a.v.n_kv + g; }
 };
 
-// What a form is, beside its kernel code: Args, a CaArgs with what else it takes; Maps, the tensor maps it takes; Head, the rows
+// What a form is, beside its kernel code: WARP_BYTES of shared memory a warp, the first ALIGN-ed; Args, a CaArgs with what else it takes; Maps, the tensor maps it takes; Head, the rows
 // of a layer's KV head in the pools; T, the type of queries and outputs.
 struct NoMaps {};
 
@@ -462,7 +463,7 @@ cache_attention_kernel(const __grid_constant__ typename Form::Maps maps, const t
     using P = Part<HD, ROWS>;
     extern __shared__ uint8_t ca_raw[];
     __shared__ CaNote notes[2 * CA_WARPS];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ca_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ca_raw) + Form::ALIGN - 1) & ~uintptr_t(Form::ALIGN - 1));
     const int warp = threadIdx.x >> 5;
     if ((threadIdx.x & 31) < 2) notes[2 * warp + (threadIdx.x & 31)].part = nullptr;
     __syncwarp();
@@ -665,7 +666,7 @@ int item_ctas(const CaArgs& a, int sms) {
 template <typename Form>
 cudaError_t launch(typename Form::Args a, const typename Form::Maps& maps, int sms, int* kernels, cudaStream_t st) {
     static_assert(Form::CTAS * Form::ROWS <= CA_SM_ROWS, "the workspace's parts");
-    constexpr size_t smem = CA_WARPS * Form::WARP_BYTES + 1024, smem_items = smem + Part<Form::HD, Form::ROWS>::FLOATS * sizeof(float);
+    constexpr size_t smem = CA_WARPS * Form::WARP_BYTES + Form::ALIGN, smem_items = smem + Part<Form::HD, Form::ROWS>::FLOATS * sizeof(float);
     static PerDevice<SmemOptIn> once, once_items;
     a.RT = (a.R + Form::ROWS - 1) / Form::ROWS;
     a.per = a.v.L * a.v.n_kv * a.RT;
