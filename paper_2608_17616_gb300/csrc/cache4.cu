@@ -33,75 +33,103 @@ struct Append4Args {
     Cache4View f;
     const void *K, *V;
     long long s0, s1, s2, s3;  // element strides (context, layer, head, token)
-    int n_tok, groups;         // of a row
+    int n_tok;
     float k_inv, v_inv;        // 2^-exp
     const int* counts;
     int* lens_out;
 };
 
-// 16 neighbours
+// 16 neighbours as they are
 template <typename T, bool VEC>
-__device__ __forceinline__ void load16(const T* p, float (&x)[16]) {
-    if constexpr (VEC) {
-        constexpr int PER = 16 / sizeof(T);
-        uint4 u[16 / PER];
+struct Group {
+    static constexpr int WORDS = 16 * sizeof(T) / 4;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ explicit Group(const T* p) {
+        if constexpr (VEC) {
 #pragma unroll
-        for (int i = 0; i < 16 / PER; ++i) u[i] = reinterpret_cast<const uint4*>(p)[i];
+            for (int i = 0; i < WORDS; i += 8)
+                asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                             : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]), "=r"(w[i + 4]), "=r"(w[i + 5]), "=r"(w[i + 6]), "=r"(w[i + 7])
+                             : "l"(reinterpret_cast<const uint32_t*>(p) + i));
+        } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = to_f<T>(reinterpret_cast<const T*>(&u[i / PER])[i % PER]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = to_f<T>(p[i]);
+            for (int i = 0; i < 16; ++i) reinterpret_cast<T*>(w)[i] = p[i];
+        }
     }
-}
+};
 
-// A group's 16 codes (two words) and its scale
-__device__ __forceinline__ uint32_t encode16(const float (&x)[16], float unit_inv, uint2& codes) {
-    float most = 0.f;
+// A group's 16 codes (two words) and its scale.  Of 32-bit values the codes are those of the quotients rounded so that no tie is made or lost.
+template <bool VEC>
+__device__ __forceinline__ uint32_t encode16(const Group<float, VEC>& x, float unit_inv, uint2& codes) {
+    float most = 0.f, v[16];
     bool nan = false;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        most = fmaxf(most, fabsf(x[i]));
-        nan |= isnan(x[i]);
+        v[i] = __uint_as_float(x.w[i]) * unit_inv;
+        most = fmaxf(most, fabsf(v[i]));
+        nan |= isnan(v[i]);
     }
-    const uint32_t scale = nan ? 0x7fu : encode_scale(most * unit_inv);
-    const float s = scale_float(scale), inv = __frcp_rn(s);
+    const uint32_t scale = nan ? 0x7fu : encode_scale(most);
     codes = make_uint2(0u, 0u);
     if (scale == 0 || nan) return scale;
+    const float s = scale_float(scale), inv = __frcp_rn(s);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        codes.x |= encode_two(x[2 * i] * unit_inv, x[2 * i + 1] * unit_inv, s, inv) << (8 * i);
-        codes.y |= encode_two(x[8 + 2 * i] * unit_inv, x[9 + 2 * i] * unit_inv, s, inv) << (8 * i);
+        codes.x |= encode_two(v[2 * i], v[2 * i + 1], s, inv) << (8 * i);
+        codes.y |= encode_two(v[8 + 2 * i], v[9 + 2 * i], s, inv) << (8 * i);
     }
     return scale;
 }
+// Of bf16 values, 8 bits, and a scale of 4 bits, a quotient that is no tie (of 3 bits) is 2^-9 of itself away from one at least, so its rounding to a
+// grid of 2^-13, by a sum with 1.5 x 2^10, gives ties where there are any and moves nothing over one: 3 instructions a value for 9.
+template <bool VEC>
+__device__ __forceinline__ uint32_t encode16(const Group<bf16, VEC>& x, float unit_inv, uint2& codes) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = __vmaxu2(most, x.w[i] & 0x7fff7fffu);
+    most = max(most & 0xffffu, most >> 16);
+    const bool nan = most > 0x7f80u;
+    const uint32_t scale = nan ? 0x7fu : encode_scale(__uint_as_float(most << 16) * unit_inv);
+    codes = make_uint2(0u, 0u);
+    if (scale == 0 || nan) return scale;
+    const float inv = __frcp_rn(scale_float(scale)) * unit_inv;
+    uint32_t c[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float2 v = make_float2(__uint_as_float(x.w[i] << 16), __uint_as_float(x.w[i] & 0xffff0000u));
+        const float2 q = add2(fma2(v, make_float2(inv, inv), make_float2(1536.f, 1536.f)), make_float2(-1536.f, -1536.f));
+        c[i] = code_two(copysignf(q.x, v.x), copysignf(q.y, v.y));
+    }
+    codes = make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410),
+                       __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410));
+    return scale;
+}
 
-// A thread encodes a group of a token's key row and the same of its value row.
-template <typename T, bool VEC>
+// A thread encodes a group of a token's key row and the same of its value row.  Bound by instructions, about 270 for the two; one token a
+// context by the launch and two dependent loads.
+template <typename T, int HD, bool VEC>
 __global__ void __launch_bounds__(C4_THREADS) cache4_append_kernel(const Append4Args a) {
+    constexpr int GROUPS = HD / 16;
     const CacheView& v = a.f.v;
     const int chain = blockIdx.z, g = blockIdx.y, c = chain / v.L, l = chain % v.L;
     pdl_wait();
     const int len = cache_len(v, c);
     const int n = a.counts ? min(max(a.counts[c], 0), a.n_tok) : a.n_tok;
     if (a.lens_out && blockIdx.x == 0 && g == 0 && l == 0 && threadIdx.x == 0) a.lens_out[c] = (int)min((long long)len + n, v.cap);
-    const long long e = (long long)blockIdx.x * C4_THREADS + threadIdx.x;
-    const int i = (int)(e / a.groups), u = (int)(e % a.groups);
+    const int i = blockIdx.x * (C4_THREADS / GROUPS) + threadIdx.x / GROUPS, u = threadIdx.x % GROUPS;
     if (i >= n) return;
-    const long long pos = (long long)len + i;
+    const int pos = len + i;  // at most 2^30 + 2^20
     if (pos >= v.cap) {
         cache_fail(v.status, DS_CACHE_LEN);
         return;
     }
     if (u == 0 && v.score) v.score[(((size_t)c * v.Lh + l) * v.n_kv + g) * v.cap + pos] = 0.f;
-    const int page = cache_page(v, v.table + (size_t)c * v.width, (int)(pos >> v.page_log2));
-    if (page < 0) return;
     const long long src = c * a.s0 + l * a.s1 + g * a.s2 + i * a.s3 + 16 * u;
-    float k[16], w[16];
-    load16<T, VEC>(static_cast<const T*>(a.K) + src, k);
-    load16<T, VEC>(static_cast<const T*>(a.V) + src, w);
+    const Group<T, VEC> k(static_cast<const T*>(a.K) + src), w(static_cast<const T*>(a.V) + src);
+    const int page = cache_page(v, v.table + (size_t)c * v.width, pos >> v.page_log2);
+    if (page < 0) return;
     const FourRows rows(a.f, l, g);
-    const long long code = rows.code(page, (int)pos) + 8 * u, scale = rows.scale(page, (int)pos) + u;
+    const long long code = rows.code(page, pos) + 8 * u, scale = rows.scale(page, pos) + u;
     uint2 q;
     rows.Ks[scale] = (uint8_t)encode16(k, a.k_inv, q);
     *reinterpret_cast<uint2*>(rows.K + code) = q;
@@ -109,10 +137,12 @@ __global__ void __launch_bounds__(C4_THREADS) cache4_append_kernel(const Append4
     *reinterpret_cast<uint2*>(rows.V + code) = q;
 }
 
-template <typename T, bool VEC>
-cudaError_t append(const Append4Args& a, cudaStream_t st) {
-    const dim3 grid((unsigned)(((long long)a.n_tok * a.groups + C4_THREADS - 1) / C4_THREADS), a.f.v.n_kv, a.f.v.n_ctx * a.f.v.L);
-    return launch_kernel(cache4_append_kernel<T, VEC>, grid, dim3(C4_THREADS), 0, st, true, 1, a);
+template <typename T, int HD>
+cudaError_t append(const Append4Args& a, bool vec, cudaStream_t st) {
+    const int tokens = C4_THREADS / (HD / 16);
+    const dim3 grid((unsigned)((a.n_tok + tokens - 1) / tokens), a.f.v.n_kv, a.f.v.n_ctx * a.f.v.L);
+    return vec ? launch_kernel(cache4_append_kernel<T, HD, true>, grid, dim3(C4_THREADS), 0, st, true, 1, a)
+               : launch_kernel(cache4_append_kernel<T, HD, false>, grid, dim3(C4_THREADS), 0, st, true, 1, a);
 }
 
 // ---------------------------------------------------------------- read
@@ -120,63 +150,64 @@ struct Read4Args {
     Cache4View f;
     void *K, *V;
     long long s0, s1, s2, s3;  // element strides (context, layer, head, place)
-    int n_pos, units;          // eights of a row
+    int n_pos;
     const int* from;
 };
 
+// 16 values of their codes and scale.  A code's product with its scale is exact in a half, and that times 2^exp in T but where it leaves T's range.
 template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
+__device__ __forceinline__ void decode16(T* p, uint2 codes, uint32_t scale, float unit) {
+    uint32_t h[8];
+    code_halves(codes.x, *reinterpret_cast<uint32_t(*)[4]>(h));
+    code_halves(codes.y, *reinterpret_cast<uint32_t(*)[4]>(h + 4));
+    const uint32_t s = scale_halves(scale * 0x101u);
+    __align__(16) T t[16];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float2 x = mul2(halves_float2(mul_halves(h[i], s)), make_float2(unit, unit));
+        if constexpr (sizeof(T) == 2) {
+            reinterpret_cast<uint32_t*>(t)[i] = pack_bf16(x.x, x.y);
+        } else {
+            t[2 * i] = x.x;
+            t[2 * i + 1] = x.y;
+        }
+    }
     if constexpr (VEC) {
-        T t[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = from_f<T>(x[i]);
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(t)[i];
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) st_32b(reinterpret_cast<bf16*>(p) + 16 * i, reinterpret_cast<const uint32_t*>(t) + 8 * i);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = from_f<T>(x[i]);
-    }
-}
-__device__ __forceinline__ void decode8(uint32_t codes, float scale, float (&x)[8]) {
-    uint32_t h[4];
-    code_halves(codes, h);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 two = halves_float2(h[i]);
-        x[2 * i] = two.x * scale;
-        x[2 * i + 1] = two.y * scale;
+        for (int i = 0; i < 16; ++i) p[i] = t[i];
     }
 }
 
-// A thread decodes eight elements of a position's key row and the same of its value row.
-template <typename T, bool VEC>
+// A thread decodes a group of a position's key row and the same of its value row.  Bound by HBM.
+template <typename T, int HD, bool VEC>
 __global__ void __launch_bounds__(C4_THREADS) cache4_read_kernel(const Read4Args a) {
+    constexpr int GROUPS = HD / 16;
     const CacheView& v = a.f.v;
     const int chain = blockIdx.z, g = blockIdx.y, c = chain / v.L, l = chain % v.L;
     pdl_wait();
-    const long long e = (long long)blockIdx.x * C4_THREADS + threadIdx.x;
-    const int i = (int)(e / a.units), u = (int)(e % a.units);
-    if (i >= a.n_pos) return;
-    const long long pos = (long long)(a.from ? max(a.from[c], 0) : 0) + i;
-    if (pos >= cache_len(v, c)) return;
-    const int page = cache_page(v, v.table + (size_t)c * v.width, (int)(pos >> v.page_log2));
+    const int i = blockIdx.x * (C4_THREADS / GROUPS) + threadIdx.x / GROUPS, u = threadIdx.x % GROUPS;
+    const long long at = (long long)(a.from ? max(a.from[c], 0) : 0) + i;
+    if (i >= a.n_pos || at >= cache_len(v, c)) return;
+    const int pos = (int)at, page = cache_page(v, v.table + (size_t)c * v.width, pos >> v.page_log2);
     if (page < 0) return;
     const FourRows rows(a.f, l, g);
-    const long long code = rows.code(page, (int)pos) + 4 * u, scale = rows.scale(page, (int)pos) + (u >> 1);
-    const uint32_t kc = *reinterpret_cast<const uint32_t*>(rows.K + code), vc = *reinterpret_cast<const uint32_t*>(rows.V + code);
-    const float ks = scale_float(rows.Ks[scale]) * a.f.k_unit, vs = scale_float(rows.Vs[scale]) * a.f.v_unit;
-    const long long dst = c * a.s0 + l * a.s1 + g * a.s2 + i * a.s3 + 8 * u;
-    float x[8];
-    decode8(kc, ks, x);
-    store8<T, VEC>(static_cast<T*>(a.K) + dst, x);
-    decode8(vc, vs, x);
-    store8<T, VEC>(static_cast<T*>(a.V) + dst, x);
+    const long long code = rows.code(page, pos) + 8 * u, scale = rows.scale(page, pos) + u;
+    const uint2 kc = *reinterpret_cast<const uint2*>(rows.K + code), vc = *reinterpret_cast<const uint2*>(rows.V + code);
+    const uint32_t ks = rows.Ks[scale], vs = rows.Vs[scale];
+    const long long dst = c * a.s0 + l * a.s1 + g * a.s2 + i * a.s3 + 16 * u;
+    decode16<T, VEC>(static_cast<T*>(a.K) + dst, kc, ks, a.f.k_unit);
+    decode16<T, VEC>(static_cast<T*>(a.V) + dst, vc, vs, a.f.v_unit);
 }
 
-template <typename T, bool VEC>
-cudaError_t read(const Read4Args& a, cudaStream_t st) {
-    const dim3 grid((unsigned)(((long long)a.n_pos * a.units + C4_THREADS - 1) / C4_THREADS), a.f.v.n_kv, a.f.v.n_ctx * a.f.v.L);
-    return launch_kernel(cache4_read_kernel<T, VEC>, grid, dim3(C4_THREADS), 0, st, true, 1, a);
+template <typename T, int HD>
+cudaError_t read(const Read4Args& a, bool vec, cudaStream_t st) {
+    const int places = C4_THREADS / (HD / 16);
+    const dim3 grid((unsigned)((a.n_pos + places - 1) / places), a.f.v.n_kv, a.f.v.n_ctx * a.f.v.L);
+    return vec ? launch_kernel(cache4_read_kernel<T, HD, true>, grid, dim3(C4_THREADS), 0, st, true, 1, a)
+               : launch_kernel(cache4_read_kernel<T, HD, false>, grid, dim3(C4_THREADS), 0, st, true, 1, a);
 }
 
 // ---------------------------------------------------------------- eviction: the survivors' rows
@@ -189,77 +220,87 @@ struct Evict4Args {
     float* to_score;
     const int* kept;
 };
-constexpr int CM4_SLOTS = 8;
 
-// A warp takes CM4_SLOTS survivors: a lane looks up where one comes from and goes to and moves its scales, then all move 16 bytes of codes each.
+// A warp takes 32 survivors: a lane looks up where one comes from and goes to and moves its scales, then all move 16 bytes of codes each, four under
+// way at a time.
 template <int HD>
 __global__ void __launch_bounds__(C4_THREADS) cache4_compact_kernel(const Evict4Args a) {
-    constexpr int UNITS = HD / 32;  // of 16 bytes, of a row's codes
+    constexpr int UNITS = HD / 32, AHEAD = 4;  // 16 bytes of a row's codes; loads under way
     using Scales = typename std::conditional<HD == 64, uint32_t, uint2>::type;
     const CacheView& v = a.f.v;
     const int chain = blockIdx.z, g = blockIdx.y, c = chain / v.L, l = chain % v.L, lane = threadIdx.x & 31;
-    const int i0 = (blockIdx.x * (C4_THREADS / 32) + (threadIdx.x >> 5)) * CM4_SLOTS;
+    const int i0 = blockIdx.x * C4_THREADS + (threadIdx.x & ~31), i = i0 + lane;
     pdl_wait();
     if (i0 >= a.keep) return;
     const FourRows rows(a.f, l, g);
     long long src = -1, dst = -1;
-    const int i = i0 + lane;
-    if (lane < CM4_SLOTS && i < a.keep) {
-        const int from = a.kept[((size_t)chain * v.n_kv + g) * a.keep + i];
-        if (from >= 0) {  // (past the survivors, an entry of the target's table need not name a page)
-            const int p1 = cache_page(v, a.to + (size_t)c * a.to_width, i >> v.page_log2);
-            const size_t row = ((size_t)c * v.Lh + l) * v.n_kv + g;
-            const int p0 = cache_page(v, v.table + (size_t)c * v.width, from >> v.page_log2);
-            a.to_score[row * a.to_cap + i] = v.score[row * v.cap + from];
-            if (p0 >= 0 && p1 >= 0) {
-                src = rows.code(p0, from);
-                dst = rows.code(p1, i);
-                const long long s = rows.scale(p0, from), d = rows.scale(p1, i);
-                const Scales ks = *reinterpret_cast<const Scales*>(rows.Ks + s), vs = *reinterpret_cast<const Scales*>(rows.Vs + s);
-                *reinterpret_cast<Scales*>(rows.Ks + d) = ks;
-                *reinterpret_cast<Scales*>(rows.Vs + d) = vs;
-            }
+    const int from = i < a.keep ? a.kept[((size_t)chain * v.n_kv + g) * a.keep + i] : -1;
+    if (from >= 0) {  // (past the survivors, an entry of the target's table need not name a page)
+        const int p1 = cache_page(v, a.to + (size_t)c * a.to_width, i >> v.page_log2);
+        const size_t row = ((size_t)c * v.Lh + l) * v.n_kv + g;
+        const int p0 = cache_page(v, v.table + (size_t)c * v.width, from >> v.page_log2);
+        a.to_score[row * a.to_cap + i] = v.score[row * v.cap + from];
+        if (p0 >= 0 && p1 >= 0) {
+            src = rows.code(p0, from);
+            dst = rows.code(p1, i);
+            const long long s = rows.scale(p0, from), d = rows.scale(p1, i);
+            const Scales ks = *reinterpret_cast<const Scales*>(rows.Ks + s), vs = *reinterpret_cast<const Scales*>(rows.Vs + s);
+            *reinterpret_cast<Scales*>(rows.Ks + d) = ks;
+            *reinterpret_cast<Scales*>(rows.Vs + d) = vs;
         }
     }
-    // of a slot its key row's units, then its value row's
-    for (int e = lane; e < CM4_SLOTS * 2 * UNITS; e += 32) {
-        const int slot = e / (2 * UNITS), o = 16 * (e % UNITS);
-        const long long s = __shfl_sync(0xffffffffu, src, slot), d = __shfl_sync(0xffffffffu, dst, slot);
-        uint8_t* const p = e / UNITS & 1 ? rows.V : rows.K;
-        if (s >= 0) *reinterpret_cast<uint4*>(p + d + o) = *reinterpret_cast<const uint4*>(p + s + o);
+    // of a slot its key row's units, then its value row's: a lane the same unit of every slot that it moves
+    const int o = 16 * (lane % UNITS), slot0 = lane / (2 * UNITS);
+    uint8_t* const p = (lane / UNITS & 1 ? rows.V : rows.K) + o;
+#pragma unroll 1
+    for (int x = 0; x < 2 * UNITS; x += AHEAD) {
+        uint4 moved[AHEAD];
+        long long d[AHEAD];
+#pragma unroll
+        for (int y = 0; y < AHEAD; ++y) {
+            const int slot = (x + y) * (16 / UNITS) + slot0;
+            const long long s = __shfl_sync(0xffffffffu, src, slot);
+            d[y] = __shfl_sync(0xffffffffu, dst, slot);
+            if (s < 0)
+                d[y] = -1;
+            else
+                moved[y] = *reinterpret_cast<const uint4*>(p + s);
+        }
+#pragma unroll
+        for (int y = 0; y < AHEAD; ++y)
+            if (d[y] >= 0) *reinterpret_cast<uint4*>(p + d[y]) = moved[y];
     }
 }
 
 template <int HD>
 cudaError_t compact(const Evict4Args& a, cudaStream_t st) {
-    const int slots = CM4_SLOTS * C4_THREADS / 32;
-    const dim3 grid((unsigned)((a.keep + slots - 1) / slots), a.f.v.n_kv, a.f.v.n_ctx * a.f.v.L);
+    const dim3 grid((unsigned)((a.keep + C4_THREADS - 1) / C4_THREADS), a.f.v.n_kv, a.f.v.n_ctx * a.f.v.L);
     return launch_kernel(cache4_compact_kernel<HD>, grid, dim3(C4_THREADS), 0, st, true, 1, a);
 }
 
-// Whether rows of T at p with these element strides start on 16-byte boundaries
+// Whether rows of T at p with these element strides start on 32-byte boundaries
 bool vec_rows(const void* K, const void* V, const long long* strides, int el) {
     uintptr_t all = (uintptr_t)K | (uintptr_t)V;
     for (int i = 0; i < 4; ++i) all |= (uintptr_t)(strides[i] * el);
-    return (all & 15u) == 0;
+    return (all & 31u) == 0;
 }
 
 }  // namespace
 
 cudaError_t launch_cache4_append(const DevState& s, const Cache4View& f, const void* K, const void* V, const long long* strides, int n_tok,
                                  const int* counts, int* lens_out, cudaStream_t st) {
-    const Append4Args a{f, K, V, strides[0], strides[1], strides[2], strides[3], n_tok, s.hd / 16, 1.f / f.k_unit, 1.f / f.v_unit, counts, lens_out};
+    const Append4Args a{f, K, V, strides[0], strides[1], strides[2], strides[3], n_tok, 1.f / f.k_unit, 1.f / f.v_unit, counts, lens_out};
     const bool vec = vec_rows(K, V, strides, s.dtype == 0 ? 4 : 2);
-    if (s.dtype == 0) return vec ? append<float, true>(a, st) : append<float, false>(a, st);
-    return vec ? append<bf16, true>(a, st) : append<bf16, false>(a, st);
+    if (s.dtype == 0) return s.hd == 64 ? append<float, 64>(a, vec, st) : append<float, 128>(a, vec, st);
+    return s.hd == 64 ? append<bf16, 64>(a, vec, st) : append<bf16, 128>(a, vec, st);
 }
 
 cudaError_t launch_cache4_read(const DevState& s, const Cache4View& f, const int* from, int n_pos, void* K, void* V, const long long* strides,
                                cudaStream_t st) {
-    const Read4Args a{f, K, V, strides[0], strides[1], strides[2], strides[3], n_pos, s.hd / 8, from};
+    const Read4Args a{f, K, V, strides[0], strides[1], strides[2], strides[3], n_pos, from};
     const bool vec = vec_rows(K, V, strides, s.dtype == 0 ? 4 : 2);
-    if (s.dtype == 0) return vec ? read<float, true>(a, st) : read<float, false>(a, st);
-    return vec ? read<bf16, true>(a, st) : read<bf16, false>(a, st);
+    if (s.dtype == 0) return s.hd == 64 ? read<float, 64>(a, vec, st) : read<float, 128>(a, vec, st);
+    return s.hd == 64 ? read<bf16, 64>(a, vec, st) : read<bf16, 128>(a, vec, st);
 }
 
 cudaError_t launch_cache4_evict(const DevState& s, const Cache4View& f, int keep, int n_sink, int n_recent, const int* to, int to_width,

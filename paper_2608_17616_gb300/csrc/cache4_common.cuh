@@ -45,13 +45,21 @@ __device__ __forceinline__ uint32_t encode_scale(float most) {
     asm("{\n\t.reg .b16 s;\n\tcvt.rn.satfinite.e4m3x2.f32 s, %1, %1;\n\tcvt.u32.u16 %0, s;\n\t}" : "=r"(s) : "f"(q));
     return s & 0xff;
 }
-// Two codes of x0 (low) and x1 under scale `s` > 0, inv the rounded 1 / s
-__device__ __forceinline__ uint32_t encode_two(float x0, float x1, float s, float inv) {
-    const float q0 = copysignf(quotient_sticky(fminf(fabsf(x0), 8.f * s), s, inv), x0);
-    const float q1 = copysignf(quotient_sticky(fminf(fabsf(x1), 8.f * s), s, inv), x1);
+// Two codes, of x0 low
+__device__ __forceinline__ uint32_t code_two(float x0, float x1) {
     uint32_t c;
-    asm("{\n\t.reg .b8 c;\n\tcvt.rn.satfinite.e2m1x2.f32 c, %2, %1;\n\tcvt.u32.u8 %0, c;\n\t}" : "=r"(c) : "f"(q0), "f"(q1));
+    asm("{\n\t.reg .b8 c;\n\tcvt.rn.satfinite.e2m1x2.f32 c, %2, %1;\n\tcvt.u32.u8 %0, c;\n\t}" : "=r"(c) : "f"(x0), "f"(x1));
     return c;
+}
+// of x0 (low) and x1 under scale `s` > 0, inv the rounded 1 / s
+__device__ __forceinline__ uint32_t encode_two(float x0, float x1, float s, float inv) {
+    return code_two(copysignf(quotient_sticky(fminf(fabsf(x0), 8.f * s), s, inv), x0), copysignf(quotient_sticky(fminf(fabsf(x1), 8.f * s), s, inv), x1));
+}
+
+__device__ __forceinline__ uint32_t mul_halves(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
 }
 
 }  // namespace mone

@@ -8,7 +8,11 @@ namespace mone {
 
 namespace {
 
-constexpr int NR_THREADS = 128;
+#ifndef NR_CHUNK
+#define NR_CHUNK 16
+#endif
+constexpr int NR_DEPTH = 4;  // rows under way, one of them being computed
+constexpr int NR_THREADS = 128, NR_FILL = 152 * 1024;
 
 struct NormRotateArgs {
     RotateArgs r;
@@ -32,130 +36,210 @@ __device__ __forceinline__ void cos_sin(unsigned long long turn, float& c, float
     }
 }
 
-// 8 neighbours
+// Rows under way: a lane's pieces, two of eight elements of each, in shared memory at a place of its own, so that it waits for nobody else.
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, float* x) {
-    if constexpr (VEC) {
-        constexpr int PER = 16 / sizeof(T);
-        uint4 u[8 / PER];
+struct Ring {
+    static constexpr int PER = 8 * sizeof(T) / 16;  // 16 bytes of a piece
+    static constexpr int BYTES = NR_DEPTH * 2 * PER * 16 * NR_THREADS;
+    uint8_t* at;
+    __device__ __forceinline__ explicit Ring(uint8_t* smem) : at(smem + 16 * threadIdx.x) {}
+    __device__ __forceinline__ uint4* place(int slot, int i) const { return reinterpret_cast<uint4*>(at + (slot * 2 * PER + i) * 16 * NR_THREADS); }
+    __device__ __forceinline__ void copy(int slot, const T* p0, const T* p1) const {
+        if constexpr (VEC) {
 #pragma unroll
-        for (int i = 0; i < 8 / PER; ++i) u[i] = reinterpret_cast<const uint4*>(p)[i];
+            for (int i = 0; i < 2 * PER; ++i)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(place(slot, i))),
+                             "l"(reinterpret_cast<const uint4*>(i < PER ? p0 : p1) + i % PER)
+                             : "memory");
+        } else {
+            __align__(16) T t[16];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = to_f<T>(reinterpret_cast<const T*>(&u[i / PER])[i % PER]);
-    } else {
+            for (int i = 0; i < 8; ++i) t[i] = p0[i], t[8 + i] = p1[i];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = to_f<T>(p[i]);
+            for (int i = 0; i < 2 * PER; ++i) *place(slot, i) = reinterpret_cast<const uint4*>(t)[i];
+        }
     }
-}
+    // as pairs: 0 .. 3 of the first piece, 4 .. 7 of the second
+    __device__ __forceinline__ void read(int slot, float2 (&x)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 2 * PER; ++i) {
+            const uint4 u = *place(slot, i);
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (sizeof(T) == 2)
+                    x[4 * i + k] = make_float2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u));
+                else if (k % 2 == 0)
+                    x[2 * i + k / 2] = make_float2(__uint_as_float(w[k]), __uint_as_float(w[k + 1]));
+            }
+        }
+    }
+};
 template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T* p, const float* x) {
+__device__ __forceinline__ void store8(T* p, const float2* x) {
     if constexpr (VEC) {
         __align__(16) T t[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = from_f<T>(x[i]);
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 2) {
+                reinterpret_cast<uint32_t*>(t)[i] = pack_bf16(x[i].x, x[i].y);
+            } else {
+                t[2 * i] = x[i].x;
+                t[2 * i + 1] = x[i].y;
+            }
+        }
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(t)[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = from_f<T>(x[i]);
+        for (int i = 0; i < 4; ++i) {
+            p[2 * i] = from_f<T>(x[i].x);
+            p[2 * i + 1] = from_f<T>(x[i].y);
+        }
     }
 }
+
+// Rows of a token, one after the other: queries of a layer, its keys, the next layer's.  Those of a side and layer lie one stride apart.
+struct RowWalk {
+    const RotateArgs& r;
+    int heads, layer, h;
+    long long at, step;  // element offset of the row, within its side
+    __device__ RowWalk(const RotateArgs& r, int row) : r(r), heads(r.side[0].heads + r.side[1].heads), layer(row / heads), h(row - layer * heads) {}
+    __device__ __forceinline__ bool second() const { return h >= r.side[0].heads; }
+    // OUT: of the outputs; c, i: the token
+    template <bool OUT>
+    __device__ __forceinline__ void place(int c, int i) {
+        const RotateSide& s = r.side[second()];
+        const long long* d = OUT ? s.o : s.s;
+        at = c * d[0] + layer * d[1] + (second() ? h - r.side[0].heads : h) * d[2] + i * d[3];
+        step = d[2];
+    }
+    template <bool OUT>
+    __device__ __forceinline__ void next(int c, int i) {
+        ++h;
+        if (h == heads || h == r.side[0].heads) {
+            if (h == heads) h = 0, ++layer;
+            place<OUT>(c, i);
+        } else {
+            at += step;
+        }
+    }
+};
 
 // HD / 16 lanes take a job: some rows of one token, whose angles they compute once.  A lane has two pieces of eight elements of each row, for
 // halves those that are paired, so that a row takes no exchange but its sum of squares.
 template <typename T, int HD, bool VEC>
 __global__ void __launch_bounds__(NR_THREADS) norm_rotate_kernel(const __grid_constant__ NormRotateArgs a) {
     constexpr int LANES = HD / 16;
+    extern __shared__ __align__(16) uint8_t nr_smem[];
+    const Ring<T, VEC> ring(nr_smem);
     const RotateArgs& r = a.r;
     pdl_wait();
     const long long job = ((long long)blockIdx.x * NR_THREADS + threadIdx.x) / LANES;
     const int l = threadIdx.x % LANES;
-    const bool live = job < a.jobs;
     const long long tokens = (long long)r.n_ctx * r.n_tok;
+    const bool live = job < a.jobs;
     const long long part = live ? job / tokens : 0, ct = live ? job - part * tokens : 0;
     const int c = (int)(ct / r.n_tok), i = (int)(ct - (long long)c * r.n_tok);
-    const int n_rot = r.rot / 16;
-    const bool turns = l < n_rot;
+    const bool turns = l < r.rot / 16;
     const int d0 = 8 * (turns && !r.neighbours ? l : 2 * l), d1 = turns && !r.neighbours ? d0 + r.rot / 2 : d0 + 8;
-    float co[8], si[8];
+    const int row0 = (int)part * a.chunk, rows = live ? min(a.chunk, a.rows - row0) : 0;
+    RowWalk in(r, row0), out(r, row0);
+    in.place<false>(c, i);
+    out.place<true>(c, i);
+    auto copy = [&](int n) {
+        if (n < rows) {
+            const T* x = static_cast<const T*>(r.side[in.second()].x) + in.at;
+            ring.copy(n % NR_DEPTH, x + d0, x + d1);
+            in.next<false>(c, i);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int n = 0; n < NR_DEPTH - 1; ++n) copy(n);
+    float2 co[4], si[4];  // of pairs 2 e and 2 e + 1
     {
         unsigned p = (unsigned)((r.first ? r.first[c] : 0) + i);
         if (r.period) p %= (unsigned)r.period;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            co[e] = 1.f;
-            si[e] = 0.f;
-            if (turns) cos_sin(r.turns[8 * l + e] * p, co[e], si[e]);
+        for (int e = 0; e < 4; ++e) {
+            co[e] = make_float2(1.f, 1.f);
+            si[e] = make_float2(0.f, 0.f);
+            if (turns) {
+                cos_sin(r.turns[8 * l + 2 * e] * p, co[e].x, si[e].x);
+                cos_sin(r.turns[8 * l + 2 * e + 1] * p, co[e].y, si[e].y);
+            }
         }
     }
-    const int heads = r.side[0].heads + r.side[1].heads;
-    const int row0 = (int)part * a.chunk, row1 = live ? min(row0 + a.chunk, a.rows) : row0;
+    float2 w[8];
+    const float* loaded = nullptr;
+#pragma unroll 1
     for (int n = 0; n < a.chunk; ++n) {
-        const int row = min(row0 + n, a.rows - 1), layer = row / heads, h = row - layer * heads;
-        const bool second = h >= r.side[0].heads, on = row0 + n < row1;
-        const RotateSide& s = r.side[second];
-        const int head = second ? h - r.side[0].heads : h;
-        float x[16], ss;
-        const T* from = static_cast<const T*>(s.x) + c * s.s[0] + layer * s.s[1] + head * s.s[2] + i * s.s[3];
-        if (on) {
-            load8<T, VEC>(from + d0, x);
-            load8<T, VEC>(from + d1, x + 8);
-        } else {
+        const bool on = n < rows;
+        if (!__any_sync(0xffffffffu, on)) break;
+        copy(n + NR_DEPTH - 1);
+        const RotateSide& s = r.side[out.second()];
+        const bool scaled = on && s.w;
+        const float* weight = s.w + (size_t)out.layer * HD;
+        if (scaled && weight != loaded) {  // a layer's, of a side
+            loaded = weight;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = 0.f;
-        }
-        auto squares = [&]() {
-            ss = 0.f;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) ss = fmaf(x[e], x[e], ss);
-#pragma unroll
-            for (int o = 1; o < LANES; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        };
-        squares();
-        float mean = ss / HD + r.eps;
-        const bool out_of_range = s.w && !(mean > 1e-30f && mean < 1e37f);
-        if (__any_sync(0xffffffffu, out_of_range)) {  // squares that 32 bits do not hold: of the row scaled by a power of two
-            if (out_of_range) {
-                const float scale = mean <= 1e-30f ? 0x1p80f : 0x1p-70f;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] *= scale;
-                mean = r.eps * scale * scale;
-            } else {
-                mean = r.eps;
+            for (int e = 0; e < 4; ++e) {
+                w[e] = make_float2(weight[d0 + 2 * e], weight[d0 + 2 * e + 1]);
+                w[4 + e] = make_float2(weight[d1 + 2 * e], weight[d1 + 2 * e + 1]);
             }
-            squares();
-            mean += ss / HD;
         }
-        if (s.w) {
-            const float inv = rsqrtf(mean);
-            const float* w = s.w + (size_t)layer * HD;
+        asm volatile("cp.async.wait_group %0;" ::"n"(NR_DEPTH - 1) : "memory");
+        float2 x[8];
+        ring.read(n % NR_DEPTH, x);
+        if (__any_sync(0xffffffffu, scaled)) {
+            auto squares = [&]() {
+                float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s = fma2(x[e], x[e], s);
+                float ss = s.x + s.y;
+#pragma unroll
+                for (int o = 1; o < LANES; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+                return ss;
+            };
+            float mean = squares() / HD + r.eps;
+            const bool out_of_range = scaled && !(mean > 1e-30f && mean < 1e37f);
+            if (__any_sync(0xffffffffu, out_of_range)) {  // squares that 32 bits do not hold: of the row scaled by a power of two
+                if (out_of_range) {
+                    const float scale = mean <= 1e-30f ? 0x1p80f : 0x1p-70f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = mul2(x[e], make_float2(scale, scale));
+                    mean = r.eps * scale * scale;
+                } else {
+                    mean = r.eps;
+                }
+                mean += squares() / HD;
+            }
+            if (scaled) {
+                const float inv = rsqrtf(mean);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = mul2(x[e], mul2(w[e], make_float2(inv, inv)));
+            }
+        }
+        if (r.neighbours) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                x[e] *= inv * w[d0 + e];
-                x[8 + e] *= inv * w[d1 + e];
+                const float co1 = e & 1 ? co[e / 2].y : co[e / 2].x, si1 = e & 1 ? si[e / 2].y : si[e / 2].x;
+                x[e] = make_float2(x[e].x * co1 - x[e].y * si1, x[e].y * co1 + x[e].x * si1);
             }
-        }
-        if (turns) {
-            if (r.neighbours) {
+        } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float p = x[2 * e], q = x[2 * e + 1];
-                    x[2 * e] = p * co[e] - q * si[e];
-                    x[2 * e + 1] = q * co[e] + p * si[e];
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float p = x[e], q = x[8 + e];
-                    x[e] = p * co[e] - q * si[e];
-                    x[8 + e] = q * co[e] + p * si[e];
-                }
+            for (int e = 0; e < 4; ++e) {
+                const float2 p = x[e], q = x[4 + e];
+                x[e] = fma2(p, co[e], mul2(q, make_float2(-si[e].x, -si[e].y)));
+                x[4 + e] = fma2(q, co[e], mul2(p, si[e]));
             }
         }
         if (on) {
-            T* to = static_cast<T*>(s.out) + c * s.o[0] + layer * s.o[1] + head * s.o[2] + i * s.o[3];
+            T* to = static_cast<T*>(s.out) + out.at;
             store8<T, VEC>(to + d0, x);
-            store8<T, VEC>(to + d1, x + 8);
+            store8<T, VEC>(to + d1, x + 4);
+            out.next<true>(c, i);
         }
     }
 }
@@ -163,7 +247,8 @@ __global__ void __launch_bounds__(NR_THREADS) norm_rotate_kernel(const __grid_co
 template <typename T, int HD, bool VEC>
 cudaError_t launch(const NormRotateArgs& a, cudaStream_t st) {
     const long long threads = a.jobs * (HD / 16);
-    return launch_kernel(norm_rotate_kernel<T, HD, VEC>, dim3((unsigned)((threads + NR_THREADS - 1) / NR_THREADS)), dim3(NR_THREADS), 0, st, true, 1, a);
+    return launch_kernel(norm_rotate_kernel<T, HD, VEC>, dim3((unsigned)((threads + NR_THREADS - 1) / NR_THREADS)), dim3(NR_THREADS), Ring<T, VEC>::BYTES, st,
+                         true, 1, a);
 }
 template <typename T, int HD>
 cudaError_t launch(const NormRotateArgs& a, bool vec, cudaStream_t st) {
@@ -175,7 +260,7 @@ cudaError_t launch(const NormRotateArgs& a, bool vec, cudaStream_t st) {
 cudaError_t launch_norm_rotate(const DevState& s, const RotateArgs& r, cudaStream_t st) {
     NormRotateArgs a{r, r.L * (r.side[0].heads + r.side[1].heads), 1, 0};
     const long long tokens = (long long)r.n_ctx * r.n_tok;
-    while (a.chunk < 8 && 2 * a.chunk <= a.rows && tokens * a.rows / (2 * a.chunk) >= 16384) a.chunk *= 2;
+    while (a.chunk < NR_CHUNK && 2 * a.chunk <= a.rows && tokens * a.rows / (2 * a.chunk) * (s.hd / 16) >= NR_FILL) a.chunk *= 2;
     a.jobs = tokens * ((a.rows + a.chunk - 1) / a.chunk);
     if (a.jobs * (s.hd / 16) > (long long)INT_MAX * NR_THREADS) return cudaErrorInvalidValue;  // (more rows than any memory has)
     uintptr_t all = 0;
