@@ -98,6 +98,7 @@ class mone_heads(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("strides", _LL4),
                 ("out_strides", _LL4), ("n_heads", ctypes.c_int)]
     _of = None  # make_heads': contexts, layers, tokens, head_dim, dtype, layers of its weight
+    _fits = None  # the handle's, whether all layers, and the tokens that they were found to do for
 
 
 _lib = None
@@ -159,9 +160,7 @@ def lib(path: Optional[str] = None) -> ctypes.CDLL:
 
 
 def _ptr(x) -> Optional[int]:
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or x.__class__ is int:
         return x
     return x.data_ptr()
 
@@ -296,6 +295,15 @@ def _buffer(name: str, t, dtype: str, at_least: int, shape: str):
         want = _types[dtype] = getattr(torch, dtype)
     if t.dtype is not want or not t.is_contiguous() or t.numel() < at_least:
         raise ValueError(f"{name}: a contiguous {dtype} tensor {shape}, not {tuple(t.shape)}, {t.dtype}")
+
+
+def _vector(name: str, t, dtype: str, at_least: int, shape: str) -> Optional[int]:
+    """The address of a tensor that _buffer takes; None and addresses as they are."""
+    if t is None or t.__class__ is int:
+        return t
+    if t.dtype is not _types.get(dtype) or t.numel() < at_least or not t.is_contiguous():
+        _buffer(name, t, dtype, at_least, shape)
+    return t.data_ptr()
 
 
 def _tables(table, lens, score, page: int):
@@ -442,34 +450,35 @@ def make_pages(free, n_free, table, lens, page_size: int) -> mone_pages:
     return p
 
 
-def _pages(h: int, pages: mone_pages):
+def _pages(h: int, pages: mone_pages) -> int:
+    """Checks the pages' contexts; the handle's."""
     need = _handles.get(h)
-    if None not in (pages._of, need) and pages._of < need[1]:
+    if need is None:
+        return 1
+    if pages._of is not None and pages._of < need[1]:
         raise ValueError(f"pages of {pages._of} contexts, the handle has {need[1]}")
-    return ctypes.byref(pages), need[1] if need else 1
+    return need[1]
 
 
 def mone_cache_reserve(h: int, pages: mone_pages, n_tok: int, n_free_out, lens_out=None, granted=None, slots=None, counts=None,
                        stream=None):
     """Pages for each context's next n_tok (or counts) tokens from the free list, and the tokens' slots [contexts, n_tok] int64."""
-    ref, n_ctx = _pages(h, pages)
-    for name, t, dtype, n, shape in (("n_free_out", n_free_out, "int32", 1, "[1]"), ("lens_out", lens_out, "int32", n_ctx, "[contexts]"),
-                                     ("granted", granted, "int32", n_ctx, "[contexts]"), ("counts", counts, "int32", n_ctx, "[contexts]"),
-                                     ("slots", slots, "int64", n_ctx * n_tok, "[contexts, n_tok]")):
-        if t is not None:
-            _buffer(name, t, dtype, n, shape)
-    _check("mone_cache_reserve", lib().mone_cache_reserve(h, ref, n_tok, _ptr(counts), _ptr(granted), _ptr(slots), _ptr(lens_out),
-                                                          _ptr(n_free_out), _stream(stream)))
+    n = _pages(h, pages)
+    rc = lib().mone_cache_reserve(h, ctypes.byref(pages), n_tok, _vector("counts", counts, "int32", n, "[contexts]"),
+                                  _vector("granted", granted, "int32", n, "[contexts]"),
+                                  _vector("slots", slots, "int64", n * n_tok, "[contexts, n_tok]"),
+                                  _vector("lens_out", lens_out, "int32", n, "[contexts]"), _vector("n_free_out", n_free_out, "int32", 1, "[1]"),
+                                  _stream(stream))
+    _check("mone_cache_reserve", rc)
 
 
 def mone_cache_release(h: int, pages: mone_pages, n_free_out, keep=None, lens_out=None, stream=None):
     """The pages that hold no position below keep (None: 0) back to the free list."""
-    ref, n_ctx = _pages(h, pages)
-    for name, t, n, shape in (("n_free_out", n_free_out, 1, "[1]"), ("lens_out", lens_out, n_ctx, "[contexts]"),
-                              ("keep", keep, n_ctx, "[contexts]")):
-        if t is not None:
-            _buffer(name, t, "int32", n, shape)
-    _check("mone_cache_release", lib().mone_cache_release(h, ref, _ptr(keep), _ptr(lens_out), _ptr(n_free_out), _stream(stream)))
+    n = _pages(h, pages)
+    rc = lib().mone_cache_release(h, ctypes.byref(pages), _vector("keep", keep, "int32", n, "[contexts]"),
+                                  _vector("lens_out", lens_out, "int32", n, "[contexts]"), _vector("n_free_out", n_free_out, "int32", 1, "[1]"),
+                                  _stream(stream))
+    _check("mone_cache_release", rc)
 
 
 def make_rotary(rot_dim: int, pairing: int = MONE_ROTATE_HALVES, base: float = 10000.0, freq: Optional[Sequence[float]] = None,
@@ -503,19 +512,27 @@ def make_heads(x, out, weight=None) -> mone_heads:
 def mone_norm_rotate(h: int, layer: int, rotary: mone_rotary, first, n_tok: int, q: Optional[mone_heads], k: Optional[mone_heads],
                      stream=None):
     """Queries and keys normalised by head and rotated by position; first [contexts] int32: the first token's (None: 0)."""
+    rc = lib().mone_norm_rotate(h, layer, ctypes.byref(rotary), _heads(h, layer, n_tok, q, k, first), n_tok,
+                                None if q is None else ctypes.byref(q), None if k is None else ctypes.byref(k), _stream(stream))
+    _check("mone_norm_rotate", rc)
+
+
+def _heads(h: int, layer: int, n_tok: int, q: Optional[mone_heads], k: Optional[mone_heads], first) -> Optional[int]:
+    """Checks the sides against the handle; the address of first."""
     need = _handles.get(h)
-    if need is not None:
-        for side in (q, k):
-            of = side._of if side is not None else None
-            if of is not None and (of[0] < need[1] or of[1] < (need[0] if layer == MONE_ALL_LAYERS else 1) or of[2] < n_tok or
-                                   of[3:5] != need[3:5] or (of[5] is not None and of[5] < need[0])):
-                raise ValueError(f"contexts, layers, tokens, head_dim, dtype (and the weight's layers) are {of}, the handle's layers, contexts, "
-                                 f"KV heads, head_dim, dtype {need}")
-        if first is not None:
-            _buffer("first", first, "int32", need[1], "[contexts]")
-    _check("mone_norm_rotate", lib().mone_norm_rotate(h, layer, ctypes.byref(rotary), _ptr(first), n_tok,
-                                                      None if q is None else ctypes.byref(q), None if k is None else ctypes.byref(k),
-                                                      _stream(stream)))
+    if need is None:
+        return _ptr(first)
+    call = need, layer < 0, n_tok
+    for side in (q, k):
+        if side is None or side._of is None or side._fits == call:
+            continue
+        of = side._of
+        if (of[0] < need[1] or of[1] < (need[0] if layer == MONE_ALL_LAYERS else 1) or of[2] < n_tok or of[3:5] != need[3:5] or
+                (of[5] is not None and of[5] < need[0])):
+            raise ValueError(f"contexts, layers, tokens, head_dim, dtype (and the weight's layers) are {of}, the handle's layers, contexts, "
+                             f"KV heads, head_dim, dtype {need}")
+        side._fits = call
+    return _vector("first", first, "int32", need[1], "[contexts]")
 
 
 def mone_mem_free(h: int):
