@@ -10,7 +10,10 @@ struct Ca4Args : CaArgs {
     const uint8_t *Ks, *Vs;  // scales, strides in bytes
     long long c_layer, c_page, c_head, c_pos;
     float k_unit, v_unit;
-    int near;  // 8 rows (head_dim 128) or 16 lie in a page, and its strides and its rows' have 32 bits
+    int near;                // 8 rows (head_dim 128) or 16 lie in a page, and its strides and its rows' have 32 bits
+    int one_page;            // and a block in a page, a head's rows of it side by side
+    int mask;                // of a place in its page
+    long long to_v, to_vs;   // from keys to values, codes and scales
 };
 
 struct FourHead {
@@ -182,22 +185,32 @@ struct CaFour {
     __device__ __forceinline__ void feed(const Args& a, Feed& f, int s) {
         constexpr int R = 32 / CHUNKS;  // rows of an instruction
         if (f.left >= 0) {
-            const int mask = (1 << a.v.page_log2) - 1, r0 = lane / CHUNKS;
-            const long long to_v = static_cast<const uint8_t*>(a.v.V) - static_cast<const uint8_t*>(a.v.K), to_vs = a.Vs - a.Ks;
             const uint32_t dst = ring + s * STAGE + copy_at, scales = ring + s * STAGE + 2 * CODES + lane * (HD / 16);
-            // All are there, an instruction's rows lie in a page, and strides have 32 bits
-            if (__builtin_expect(a.near && __all_sync(0xffffffffu, (unsigned)f.page < (unsigned)a.v.n_pages), 1)) {
-                auto place = [&](unsigned page, unsigned row, long long s_page, long long s_pos) {
-                    return (unsigned long long)page * (unsigned)s_page + (unsigned long long)row * (unsigned)s_pos;
-                };
-                const unsigned long long off = place(f.page, (f.j0 + lane) & mask, a.c_page, a.c_pos);
-                copy_async<HD / 16>(scales, f.Ks + off);
-                copy_async<HD / 16>(scales + SCALES, f.Ks + off + to_vs);
+            if (__builtin_expect(a.near && __all_sync(0xffffffffu, (unsigned)f.page < (unsigned)a.v.n_pages), 1)) {  // all are there
+                if (a.one_page) {  // (35 instructions of a block's 600 for 75)
+                    const unsigned row = f.j0 & a.mask;
+                    const uint8_t* ks = f.Ks + (unsigned long long)f.page * (unsigned)a.c_page + (row + lane) * (HD / 16);
+                    copy_async<HD / 16>(scales, ks);
+                    copy_async<HD / 16>(scales + SCALES, ks + a.to_vs);
+                    const uint8_t *k = f.K + (unsigned long long)f.page * (unsigned)a.v.s_page + (row * (HD / 2) + lane / CHUNKS * (HD / 2)), *v = k + a.to_v;
 #pragma unroll
-                for (int x = 0; x < CHUNKS; ++x) {
-                    const unsigned long long off = place(__shfl_sync(0xffffffffu, f.page, x * R), ((f.j0 + x * R) & mask) + r0, a.v.s_page, a.v.s_pos);
-                    copy_async<16>(dst + x * R * (HD / 2), f.K + off);
-                    copy_async<16>(dst + x * R * (HD / 2) + CODES, f.K + off + to_v);
+                    for (int x = 0; x < CHUNKS; ++x) {
+                        copy_async<16>(dst + x * R * (HD / 2), k + x * R * (HD / 2));
+                        copy_async<16>(dst + x * R * (HD / 2) + CODES, v + x * R * (HD / 2));
+                    }
+                } else {
+                    auto place = [&](unsigned page, unsigned row, long long s_page, long long s_pos) {
+                        return (unsigned long long)page * (unsigned)s_page + (unsigned long long)row * (unsigned)s_pos;
+                    };
+                    const uint8_t* ks = f.Ks + place(f.page, (f.j0 + lane) & a.mask, a.c_page, a.c_pos);
+                    copy_async<HD / 16>(scales, ks);
+                    copy_async<HD / 16>(scales + SCALES, ks + a.to_vs);
+#pragma unroll
+                    for (int x = 0; x < CHUNKS; ++x) {
+                        const uint8_t* k = f.K + place(__shfl_sync(0xffffffffu, f.page, x * R), ((f.j0 + x * R) & a.mask) + lane / CHUNKS, a.v.s_page, a.v.s_pos);
+                        copy_async<16>(dst + x * R * (HD / 2), k);
+                        copy_async<16>(dst + x * R * (HD / 2) + CODES, k + a.to_v);
+                    }
                 }
             } else {
                 bool in = f.page != INT_MIN;
@@ -205,19 +218,19 @@ struct CaFour {
                     cache_fail(a.v.status, DS_CACHE_PAGE);
                     in = false;
                 }
-                const int row = (f.j0 + lane) & mask;
+                const int row = (f.j0 + lane) & a.mask;
                 if (in) {
-                    const long long off = f.page * a.c_page + row * a.c_pos;
-                    copy_async<HD / 16>(scales, f.Ks + off);
-                    copy_async<HD / 16>(scales + SCALES, f.Ks + off + to_vs);
+                    const uint8_t* ks = f.Ks + (f.page * a.c_page + row * a.c_pos);
+                    copy_async<HD / 16>(scales, ks);
+                    copy_async<HD / 16>(scales + SCALES, ks + a.to_vs);
                 }
                 const long long mine = in ? f.page * a.v.s_page + row * a.v.s_pos : -1;
 #pragma unroll 1
                 for (int x = 0; x < CHUNKS; ++x) {
-                    const long long off = __shfl_sync(0xffffffffu, mine, x * R + r0);
+                    const long long off = __shfl_sync(0xffffffffu, mine, x * R + lane / CHUNKS);
                     if (off < 0) continue;
                     copy_async<16>(dst + x * R * (HD / 2), f.K + off);
-                    copy_async<16>(dst + x * R * (HD / 2) + CODES, f.K + off + to_v);
+                    copy_async<16>(dst + x * R * (HD / 2) + CODES, f.K + off + a.to_v);
                 }
             }
             --f.left;
@@ -314,13 +327,15 @@ struct CaFour {
                 }
             }
             int j0 = r.at(w.b0);
+            // blocks that every row sees whole: from here on, and within the first positions, up to there
+            const int whole0 = r.n - a.window, whole1 = r.n - a.n_tok + 1 - KB;
             float* z = a.z2 ? a.z2 + (w.kv(a) * a.R + row0) * a.pitch + gq : nullptr;
 #pragma unroll 1
             for (int left = w.b1 - w.b0; left > 0; --left) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(NS - 2) : "memory");
                 __syncwarp();
                 feed(a, ahead, slot == 0 ? NS - 1 : slot - 1);  // into the slot that was read last
-                if (__builtin_expect(j0 + KB <= r.n - a.n_tok + 1 && (j0 + KB <= a.n_sink || j0 >= r.n - a.window), 1))
+                if (__builtin_expect(j0 <= whole1 && (j0 >= whole0 || j0 + KB <= a.n_sink), 1))
                     step<true>(a, r, j0, slot, z, rows, x);
                 else
                     step<false>(a, r, j0, slot, z, rows, x);
@@ -567,6 +582,10 @@ cudaError_t launch_cache4_attention(const DevState& s, const Cache4View& f, cons
     a.c_layer = f.c_layer; a.c_page = f.c_page; a.c_head = f.c_head; a.c_pos = f.c_pos;
     a.k_unit = f.k_unit; a.v_unit = f.v_unit;
     a.near = f.v.page_log2 >= (s.hd == 64 ? 4 : 3) && std::max({f.v.s_page, f.v.s_pos, f.c_page, f.c_pos}) < 1ll << 32;
+    a.one_page = a.near && f.v.page_log2 >= 5 && f.v.s_pos == s.hd / 2 && f.c_pos == s.hd / 16;
+    a.mask = (1 << f.v.page_log2) - 1;
+    a.to_v = static_cast<const uint8_t*>(f.v.V) - static_cast<const uint8_t*>(f.v.K);
+    a.to_vs = f.Vs - f.Ks;
     return s.hd == 64 ? launch_four<64>(s, a, kernels, st) : launch_four<128>(s, a, kernels, st);
 }
 
