@@ -107,12 +107,14 @@ struct CaFour {
     static constexpr int ONE = 3, EACH = 2, FULL = 16, FEW = 6;          // blocks of a warp, see item_ctas
     static constexpr int CODES = KB * HD / 2, SCALES = KB * HD / 16, STAGE = 2 * (CODES + SCALES);
     static constexpr int NS = HD == 64 ? 4 : 3;
-    static constexpr int WALKS = NS * STAGE, WARP_BYTES = WALKS + 256, ALIGN = 128;  // the ring, the warp's walks
+    // The ring, and what is not in registers while a piece's blocks go through: the walk of the copies, that of the products, the place of
+    // the piece's scores
+    static constexpr int AHEAD = NS * STAGE, NOW = AHEAD + sizeof(CaWalk), SCORES = NOW + sizeof(CaWalk), WARP_BYTES = AHEAD + 256, ALIGN = 128;
     static constexpr int CHUNKS = HD / 32;  // of 16 bytes, of a row's codes
     static constexpr float P_LOG2 = 7.f, P_UNIT_INV = 0x1p-7f, P_ROOM = 8.f, FROM_NONE = -3e38f;
     static_assert(CTAS * (CA_WARPS * WARP_BYTES + ALIGN + 1536) <= 228 * 1024, "CTAs an SM");
-    static_assert(Part<HD, ROWS>::FLOATS * 4 <= WALKS, "a part fits in the ring");
-    static_assert(2 * sizeof(CaWalk) <= 256, "the walks");
+    static_assert(Part<HD, ROWS>::FLOATS * 4 <= AHEAD, "a part fits in the ring");
+    static_assert(sizeof(CaWalk) % 16 == 0 && SCORES + 8 <= WARP_BYTES, "what is put aside");
 
     using Args = Ca4Args;
     using Maps = NoMaps;
@@ -120,7 +122,6 @@ struct CaFour {
 
     uint32_t ring, lane;
     float* ring_part;  // the ring as the place of the warp's last part
-    CaWalk* walks;     // that of the copies, that of the products: not in registers while a piece's blocks go through
     // bytes in a stage: of the codes that this lane copies, of its eighth's key, of its values 2 t and 2 t + 1, of their scales; all of
     // the first rows, those after them at fixed distances
     uint32_t copy_at, key_at, val_at[2], key_scale_at, val_scale_at;
@@ -130,7 +131,7 @@ struct CaFour {
     // are 8 rows of bytes further on.
     static __device__ __forceinline__ uint32_t at(int r, int c) { return (r ^ (r >> 2 & 1)) * (HD / 2) + (HD == 128 ? c ^ (r & 2) : c) * 16; }
 
-    __device__ CaFour(const NoMaps&, uint8_t* smem, int) : ring_part(reinterpret_cast<float*>(smem)), walks(reinterpret_cast<CaWalk*>(smem + WALKS)) {
+    __device__ CaFour(const NoMaps&, uint8_t* smem, int) : ring_part(reinterpret_cast<float*>(smem)) {
         // (kept in registers: found anew for every block they took 13 instructions of 750)
         asm volatile("mov.b32 %0, %1;" : "=r"(ring) : "r"(smem_u32(smem)));
         asm volatile("mov.u32 %0, %%laneid;" : "=r"(lane));
@@ -146,41 +147,62 @@ struct CaFour {
     // copies its scales, neighbours copy its codes: 8 rows with one instruction (head_dim 128) or 16.
     struct Feed {
         int left = 0, j0, page;  // blocks of the piece (-1: no more pieces); the first key of the next, the lane's key's page
-        int n, t0, gap, lo;      // of the piece's range: positions, the oldest token's; the first positions' end, the first after them
+        int gap;                 // the end of the first positions' blocks
         const uint8_t *K, *Ks;   // of the piece's head, chunk lane % CHUNKS; V is as far from K in every head
         const int* table;
     };
-    // The next piece of a walk
-    __device__ __forceinline__ bool next(const Args& a, CaWalk* at, CaWalk& w) const {
-        w = *at;
-        __syncwarp();
-        if (!w.next(a)) return false;
-        if (lane == 0) *at = w;
-        __syncwarp();
-        return true;
+    // A walk put aside, by every lane the same, and back
+    __device__ __forceinline__ void put(int at, const CaWalk& w) const {
+        const uint4* u = reinterpret_cast<const uint4*>(&w);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(CaWalk) / 16; ++i)
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(ring + at + 16 * i), "r"(u[i].x), "r"(u[i].y), "r"(u[i].z), "r"(u[i].w) : "memory");
     }
-    __device__ __forceinline__ void look(const Args& a, Feed& f) {
+    __device__ __forceinline__ void get(int at, CaWalk& w) const {
+        uint4* u = reinterpret_cast<uint4*>(&w);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(CaWalk) / 16; ++i)
+            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(u[i].x), "=r"(u[i].y), "=r"(u[i].z), "=r"(u[i].w) : "r"(ring + at + 16 * i) : "memory");
+    }
+    __device__ __forceinline__ int aside(int at) const {
+        int x;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(ring + at) : "memory");
+        return x;
+    }
+    static constexpr int R_N = offsetof(CaWalk, r) + offsetof(CaRange, n), R_T0 = offsetof(CaWalk, r) + offsetof(CaRange, t0),
+                         R_LO = offsetof(CaWalk, r) + offsetof(CaRange, lo);
+    // The first block of a walk's next piece that has any
+    __device__ __forceinline__ void begin(const Args& a, Feed& f, CaWalk& w) const {
+        do {
+            if (!w.next(a)) {
+                f.left = -1;
+                return;
+            }
+            f.left = w.b1 - w.b0;
+        } while (f.left == 0);
+        put(AHEAD, w);
+        f.gap = w.r.ns * KB;
+        f.j0 = w.r.at(w.b0);
+        const FourHead head(a, w.l, w.g);
+        f.K = head.K + 16 * (lane % CHUNKS), f.Ks = head.Ks;
+        f.table = a.v.table + (size_t)w.c * a.v.width;
+        page(a, f, w.r.n, w.r.t0);
+    }
+    __device__ __forceinline__ void page(const Args& a, Feed& f, int n, int t0) const {
+        const int key = f.j0 + lane;
+        f.page = key < n && (key < a.n_sink || key > t0 - a.window) ? f.table[key >> a.v.page_log2] : INT_MIN;
+    }
+    __device__ __forceinline__ void look(const Args& a, Feed& f) const {
         if (f.left) {
             f.j0 += KB;
-            if (f.j0 == f.gap) f.j0 = f.lo;
+            if (f.j0 == f.gap) f.j0 = aside(AHEAD + R_LO);
+            page(a, f, aside(AHEAD + R_N), aside(AHEAD + R_T0));
         } else {
             CaWalk w;
-            do {
-                if (!next(a, walks, w)) {
-                    f.left = -1;
-                    return;
-                }
-                f.left = w.b1 - w.b0;
-            } while (f.left == 0);
-            f.n = w.r.n, f.t0 = w.r.t0, f.gap = w.r.ns * KB, f.lo = w.r.lo;
-            f.j0 = w.r.at(w.b0);
-            const FourHead head(a, w.l, w.g);
-            f.K = head.K + 16 * (lane % CHUNKS), f.Ks = head.Ks;
-            f.table = a.v.table + (size_t)w.c * a.v.width;
+            get(AHEAD, w);
+            __syncwarp();
+            begin(a, f, w);
         }
-        const int key = f.j0 + lane;
-        const bool in = key < f.n && (key < a.n_sink || key > f.t0 - a.window);
-        f.page = in ? f.table[key >> a.v.page_log2] : INT_MIN;
     }
     __device__ __forceinline__ void feed(const Args& a, Feed& f, int s) {
         constexpr int R = 32 / CHUNKS;  // rows of an instruction
@@ -249,7 +271,6 @@ struct CaFour {
         float lx[NT][2];               // of the exact ones, this lane's
         float from[NT][2];             // what is taken off a row's S: within 8 of its maximum in base 2, or FROM_NONE
         float unit[NT], k2[NT][2];     // of S: the unit in which it is q k (of row 8 i + gq), and in base 2 with the softmax's scale
-        int vis[NT][2];
     };
 
     // the row of h = 0, 1
@@ -299,15 +320,17 @@ struct CaFour {
         const int gq = lane >> 2, t = lane & 3;
         const float scale2 = a.scale * 1.4426950408889634f;
         CaWalk w(a);
-        if (lane == 0) walks[0] = walks[1] = w;
-        __syncwarp();
         Feed ahead;
         int slot = 0;  // of the block to be read next
-        look(a, ahead);
+        {
+            CaWalk first = w;
+            begin(a, ahead, first);
+        }
         for (int s = 0; s < NS - 1; ++s) feed(a, ahead, s);
-        while (next(a, walks + 1, w)) {
+        while (w.next(a)) {
             const int row0 = w.rt * ROWS, rows = min(ROWS, a.R - row0);
-            const CaRange r = w.r;
+            put(NOW, w);
+            if (a.z2) asm volatile("st.shared.b64 [%0], %1;" ::"r"(ring + SCORES), "l"(a.z2 + (w.kv(a) * a.R + row0) * a.pitch) : "memory");
             Rows x;
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
@@ -321,30 +344,30 @@ struct CaFour {
                     const int row = row_of(i, h);
                     x.from[i][h] = FROM_NONE;
                     x.l[i][h] = x.l[i][2 + h] = x.lx[i][h] = 0.f;
-                    x.vis[i][h] = row < rows ? r.n - a.n_tok + (a.n_tok == 1 ? 0 : (row0 + row) % a.n_tok) + 1 : 0;
                     const float k2 = scale2 * __shfl_sync(0xffffffffu, x.unit[i], 4 * (row - 8 * i));
                     x.k2[i][h] = fminf(fmaxf(k2, 1e-37f), 1e38f);  // (0 and infinity would make 0 of nothing)
                 }
             }
-            int j0 = r.at(w.b0);
+            int j0 = w.r.at(w.b0);
+            const int gap = w.r.ns * KB;
             // blocks that every row sees whole: from here on, and within the first positions, up to there
-            const int whole0 = r.n - a.window, whole1 = r.n - a.n_tok + 1 - KB;
-            float* z = a.z2 ? a.z2 + (w.kv(a) * a.R + row0) * a.pitch + gq : nullptr;
+            const int whole0 = w.r.n - a.window, whole1 = w.r.n - a.n_tok + 1 - KB;
 #pragma unroll 1
             for (int left = w.b1 - w.b0; left > 0; --left) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(NS - 2) : "memory");
                 __syncwarp();
                 feed(a, ahead, slot == 0 ? NS - 1 : slot - 1);  // into the slot that was read last
                 if (__builtin_expect(j0 <= whole1 && (j0 >= whole0 || j0 + KB <= a.n_sink), 1))
-                    step<true>(a, r, j0, slot, z, rows, x);
+                    step<true>(a, j0, slot, rows, x);
                 else
-                    step<false>(a, r, j0, slot, z, rows, x);
+                    step<false>(a, j0, slot, rows, x);
                 __syncwarp();  // the block has been read
                 if (++slot == NS) slot = 0;
                 j0 += KB;
-                if (j0 == r.ns * KB) j0 = r.lo;
+                if (j0 == gap) j0 = aside(NOW + R_LO);
             }
-            w = walks[1];
+            get(NOW, w);
+            __syncwarp();
             const size_t kv = w.kv(a);
             // a part goes to the workspace while the ring is in use
             float* part = w.last ? ring_part : P::of_warp(a, w.b0 == 0);
@@ -398,9 +421,10 @@ struct CaFour {
 
     // One block's keys; WHOLE: every row sees all of them
     template <bool WHOLE>
-    __device__ __forceinline__ void step(const Args& a, const CaRange& r, int j0, int slot, float* z2, int rows, Rows& x) {
+    __device__ __forceinline__ void step(const Args& a, int j0, int slot, int rows, Rows& x) {
         const int gq = lane >> 2, t = lane & 3;
         const uint32_t stage = ring + slot * STAGE;
+        const int n = WHOLE ? 0 : aside(NOW + R_N), t0 = WHOLE ? 0 : aside(NOW + R_T0);
         float s[NT][2][4];  // of keys 16 u + gq (0, 1) and + 8 (2, 3), rows 2 t and + 1
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -449,12 +473,16 @@ struct CaFour {
         for (int i = 0; i < NT; ++i) {
             if (!WHOLE) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int h = 0; h < 2; ++h) {
+                    const int row = row_of(i, h), vis = n - a.n_tok + (a.n_tok == 1 ? 0 : (aside(NOW + offsetof(CaWalk, rt)) * ROWS + row) % a.n_tok) + 1;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = j0 + 16 * u + gq + 8 * (e >> 1), v = x.vis[i][e & 1];
-                        s[i][u][e] = key < v && (key < a.n_sink || key >= v - a.window) ? s[i][u][e] : -INFINITY;
-                    }
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int e = h; e < 4; e += 2) {
+                            const int key = j0 + 16 * u + gq + 8 * (e >> 1);
+                            s[i][u][e] = row < rows && key < vis && (key < a.n_sink || key >= vis - a.window) ? s[i][u][e] : -INFINITY;
+                        }
+                }
             }
             // A row whose scores have grown by more than 2^8 (its first ones) is rescaled
             float most[2];
@@ -485,12 +513,15 @@ struct CaFour {
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) e[u][k] = ca_exp2(fmaf(s[i][u][k] - x.from[i][k & 1], x.k2[i][k & 1], P_LOG2));
-            if (z2) {
+            if (a.z2) {
+                float* z0;
+                asm volatile("ld.shared.b64 %0, [%1];" : "=l"(z0) : "r"(ring + SCORES) : "memory");
+                z0 += j0 + gq;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     x.lx[i][h] += (e[0][h] + e[0][2 + h]) + (e[1][h] + e[1][2 + h]);
                     if (row_of(i, h) < rows && !(BESIDE && t >= 2)) {
-                        float* z = z2 + row_of(i, h) * a.pitch + j0;
+                        float* z = z0 + row_of(i, h) * a.pitch;
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
                             z[16 * u] = s[i][u][h] * x.k2[i][h];
@@ -530,7 +561,7 @@ struct CaFour {
                 b[y] = load_byte(stage + val_scale_at + (row + (y & 1)) * (HD / 16));
                 if (!WHOLE) {  // a scale that no row sees is not to meet a probability of 0
                     const int j = j0 + row + 2 * t + (y & 1);
-                    b[y] = j < r.n && (j < a.n_sink || j > r.t0 - a.window) ? b[y] : 0;
+                    b[y] = j < n && (j < a.n_sink || j > t0 - a.window) ? b[y] : 0;
                 }
             }
             sc[0] = scale_halves(b[0] | b[1] << 8);

@@ -19,6 +19,7 @@
 
 #include <algorithm>
 #include <climits>
+#include <cstddef>
 #include <type_traits>
 
 #include "cache_common.cuh"
@@ -121,7 +122,7 @@ struct CaDeal {
 };
 
 // The pieces of a warp, one after the other: blocks [b0, b1) of an item
-struct CaWalk {
+struct alignas(16) CaWalk {
     int u, end, ctx0, c, units;
     CaRange r;
     int l, g, rt, b0, b1;
