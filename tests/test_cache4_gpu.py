@@ -161,6 +161,12 @@ def attend(x, group, n_tok, n_sink, window, layer=-1, scale=1.0, k=None, v=None)
     ([90, 10], 2, 1, 64, 16, 1000, 3),            # more first positions than there are
     ([300, 77], 4, 1, 64, 1, 0, ALL),              # pages of one position
     ([300, 2100], 4, 2, 64, 1024, 8, 999),          # pages of 1024
+    ([130, 61], 4, 1, 128, 4, 3, 40),              # pages that an instruction's rows do not fit
+    ([130, 61], 4, 1, 64, 8, 0, ALL),
+    ([200, 64, 5], 1, 4, 128, 32, 0, ALL),          # four rows
+    ([200, 64, 5], 4, 2, 64, 16, 70, 20),           # eight; first positions that end inside a block
+    ([500, 96], 8, 2, 128, 32, 32, 64),             # sixteen; a window that begins where a block does
+    ([97], 3, 3, 64, 2, 32, 1),                    # nine
 ])
 def test_attention(lens, group, n_tok, hd, page, n_sink, window, dtype):
     x = Cache4(lens, hd=hd, page=page, dtype=dtype, seed=sum(lens) + group)
