@@ -448,7 +448,7 @@ mone_status mone_cache4_evict(mone_mem* m, int layer, const mone_cache4* cache, 
  * can serve contexts that grow into new pages.
  *   free    [n_pages] (room for every page): the free pages are its first *n_free entries
  *   table   [n_ctx][table_width] as in mone_cache, for every layer; n_pages and page_size too
- *   lens    [n_ctx] positions that each context holds: it has the pages of those
+ *   lens    [n_ctx] positions that each context holds: it has the pages of those, and nobody else has them
  * Calls that share a list or a table are ordered by the caller (one stream, say).
  */
 typedef struct {

@@ -8,11 +8,10 @@ namespace mone {
 
 namespace {
 
-#ifndef NR_CHUNK
-#define NR_CHUNK 16
-#endif
-constexpr int NR_DEPTH = 4;  // rows under way, one of them being computed
-constexpr int NR_THREADS = 128, NR_FILL = 152 * 1024;
+constexpr int NR_THREADS = 128;
+constexpr int NR_DEPTH = 4;           // rows under way, one of them being computed
+constexpr int NR_CHUNK = 16;          // rows of a job, at most
+constexpr int NR_FILL = 152 * 1024;   // threads that a launch keeps, if it has them
 
 struct NormRotateArgs {
     RotateArgs r;
