@@ -114,7 +114,7 @@ struct CaFour {
     static constexpr float P_LOG2 = 7.f, P_UNIT_INV = 0x1p-7f, P_ROOM = 8.f, FROM_NONE = -3e38f;
     static_assert(CTAS * (CA_WARPS * WARP_BYTES + ALIGN + 1536) <= 228 * 1024, "CTAs an SM");
     static_assert(Part<HD, ROWS>::FLOATS * 4 <= AHEAD, "a part fits in the ring");
-    static_assert(sizeof(CaWalk) % 16 == 0 && SCORES + 8 <= WARP_BYTES, "what is put aside");
+    static_assert(sizeof(CaWalk) % 16 == 0 && SCORES + 32 <= WARP_BYTES, "what is put aside");
 
     using Args = Ca4Args;
     using Maps = NoMaps;
@@ -148,8 +148,6 @@ struct CaFour {
     struct Feed {
         int left = 0, j0, page;  // blocks of the piece (-1: no more pieces); the first key of the next, the lane's key's page
         int gap;                 // the end of the first positions' blocks
-        const uint8_t *K, *Ks;   // of the piece's head, chunk lane % CHUNKS; V is as far from K in every head
-        const int* table;
     };
     // A walk put aside, by every lane the same, and back
     __device__ __forceinline__ void put(int at, const CaWalk& w) const {
@@ -169,6 +167,13 @@ struct CaFour {
         asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(ring + at) : "memory");
         return x;
     }
+    __device__ __forceinline__ void put_pointer(int at, const void* p) const { asm volatile("st.shared.b64 [%0], %1;" ::"r"(ring + at), "l"(p) : "memory"); }
+    template <typename P>
+    __device__ __forceinline__ const P* pointer(int at) const {
+        const P* p;
+        asm volatile("ld.shared.b64 %0, [%1];" : "=l"(p) : "r"(ring + at) : "memory");
+        return p;
+    }
     static constexpr int R_N = offsetof(CaWalk, r) + offsetof(CaRange, n), R_T0 = offsetof(CaWalk, r) + offsetof(CaRange, t0),
                          R_LO = offsetof(CaWalk, r) + offsetof(CaRange, lo);
     // The first block of a walk's next piece that has any
@@ -184,13 +189,15 @@ struct CaFour {
         f.gap = w.r.ns * KB;
         f.j0 = w.r.at(w.b0);
         const FourHead head(a, w.l, w.g);
-        f.K = head.K + 16 * (lane % CHUNKS), f.Ks = head.Ks;
-        f.table = a.v.table + (size_t)w.c * a.v.width;
+        // (V is as far from K in every head)
+        put_pointer(SCORES + 8, head.K);
+        put_pointer(SCORES + 16, head.Ks);
+        put_pointer(SCORES + 24, a.v.table + (size_t)w.c * a.v.width);
         page(a, f, w.r.n, w.r.t0);
     }
     __device__ __forceinline__ void page(const Args& a, Feed& f, int n, int t0) const {
         const int key = f.j0 + lane;
-        f.page = key < n && (key < a.n_sink || key > t0 - a.window) ? f.table[key >> a.v.page_log2] : INT_MIN;
+        f.page = key < n && (key < a.n_sink || key > t0 - a.window) ? pointer<int>(SCORES + 24)[key >> a.v.page_log2] : INT_MIN;
     }
     __device__ __forceinline__ void look(const Args& a, Feed& f) const {
         if (f.left) {
@@ -207,14 +214,15 @@ struct CaFour {
     __device__ __forceinline__ void feed(const Args& a, Feed& f, int s) {
         constexpr int R = 32 / CHUNKS;  // rows of an instruction
         if (f.left >= 0) {
+            const uint8_t *K = pointer<uint8_t>(SCORES + 8) + 16 * (lane % CHUNKS), *Ks = pointer<uint8_t>(SCORES + 16);
             const uint32_t dst = ring + s * STAGE + copy_at, scales = ring + s * STAGE + 2 * CODES + lane * (HD / 16);
             if (__builtin_expect(a.near && __all_sync(0xffffffffu, (unsigned)f.page < (unsigned)a.v.n_pages), 1)) {  // all are there
                 if (a.one_page) {  // (35 instructions of a block's 600 for 75)
                     const unsigned row = f.j0 & a.mask;
-                    const uint8_t* ks = f.Ks + (unsigned long long)f.page * (unsigned)a.c_page + (row + lane) * (HD / 16);
+                    const uint8_t* ks = Ks + (unsigned long long)f.page * (unsigned)a.c_page + (row + lane) * (HD / 16);
                     copy_async<HD / 16>(scales, ks);
                     copy_async<HD / 16>(scales + SCALES, ks + a.to_vs);
-                    const uint8_t *k = f.K + (unsigned long long)f.page * (unsigned)a.v.s_page + (row * (HD / 2) + lane / CHUNKS * (HD / 2)), *v = k + a.to_v;
+                    const uint8_t *k = K + (unsigned long long)f.page * (unsigned)a.v.s_page + (row * (HD / 2) + lane / CHUNKS * (HD / 2)), *v = k + a.to_v;
 #pragma unroll
                     for (int x = 0; x < CHUNKS; ++x) {
                         copy_async<16>(dst + x * R * (HD / 2), k + x * R * (HD / 2));
@@ -224,12 +232,12 @@ struct CaFour {
                     auto place = [&](unsigned page, unsigned row, long long s_page, long long s_pos) {
                         return (unsigned long long)page * (unsigned)s_page + (unsigned long long)row * (unsigned)s_pos;
                     };
-                    const uint8_t* ks = f.Ks + place(f.page, (f.j0 + lane) & a.mask, a.c_page, a.c_pos);
+                    const uint8_t* ks = Ks + place(f.page, (f.j0 + lane) & a.mask, a.c_page, a.c_pos);
                     copy_async<HD / 16>(scales, ks);
                     copy_async<HD / 16>(scales + SCALES, ks + a.to_vs);
 #pragma unroll
                     for (int x = 0; x < CHUNKS; ++x) {
-                        const uint8_t* k = f.K + place(__shfl_sync(0xffffffffu, f.page, x * R), ((f.j0 + x * R) & a.mask) + lane / CHUNKS, a.v.s_page, a.v.s_pos);
+                        const uint8_t* k = K + place(__shfl_sync(0xffffffffu, f.page, x * R), ((f.j0 + x * R) & a.mask) + lane / CHUNKS, a.v.s_page, a.v.s_pos);
                         copy_async<16>(dst + x * R * (HD / 2), k);
                         copy_async<16>(dst + x * R * (HD / 2) + CODES, k + a.to_v);
                     }
@@ -242,7 +250,7 @@ struct CaFour {
                 }
                 const int row = (f.j0 + lane) & a.mask;
                 if (in) {
-                    const uint8_t* ks = f.Ks + (f.page * a.c_page + row * a.c_pos);
+                    const uint8_t* ks = Ks + (f.page * a.c_page + row * a.c_pos);
                     copy_async<HD / 16>(scales, ks);
                     copy_async<HD / 16>(scales + SCALES, ks + a.to_vs);
                 }
@@ -251,8 +259,8 @@ struct CaFour {
                 for (int x = 0; x < CHUNKS; ++x) {
                     const long long off = __shfl_sync(0xffffffffu, mine, x * R + lane / CHUNKS);
                     if (off < 0) continue;
-                    copy_async<16>(dst + x * R * (HD / 2), f.K + off);
-                    copy_async<16>(dst + x * R * (HD / 2) + CODES, f.K + off + a.to_v);
+                    copy_async<16>(dst + x * R * (HD / 2), K + off);
+                    copy_async<16>(dst + x * R * (HD / 2) + CODES, K + off + a.to_v);
                 }
             }
             --f.left;
