@@ -376,6 +376,62 @@ def test_pages_and_lengths_out_of_range_are_latched_and_skipped():
     fails("length", lambda: mone.mone_cache4_append(x.h, -1, x.c, k, k, k.stride()[:4], 200))  # past the table's end
 
 
+def test_calls_of_changing_sizes_and_of_both_caches_share_a_workspace_and_repeat_bit_for_bit():
+    x = Cache4([5000, 130, 1], n_layers=1, score=False)
+    P, width = x.pools[0].shape[1], x.tbl.shape[1]
+    dense = [torch.randn(1, P, 2, 16, 64, generator=x.g, device="cuda").bfloat16() for _ in range(2)]
+    score = torch.zeros(3, 1, 2, width * 16, device="cuda")
+    both = mone.make_cache(*dense, x.tbl, x.len_t, score)
+    q1, q2 = (torch.randn(3, 1, 8, n, 64, generator=x.g, device="cuda").bfloat16() for n in (1, 5))
+    outs = [[], [], []]
+    for _ in range(4):
+        for q, o in ((q1, outs[0]), (q2, outs[1])):
+            o.append(torch.empty_like(q))
+            mone.mone_cache4_attention(x.h, 0, x.c, q, 8, q.shape[3], 0, ALL, o[-1])
+            outs[2].append(torch.empty_like(q1))
+            mone.mone_cache_attention(x.h, 0, both, q1, 8, 1, 0, ALL, outs[2][-1])
+    x.done()
+    for o in outs:
+        assert all(torch.equal(o[0], y) for y in o[1:])
+    ref, _ = O.window_attention(q1[0, 0].float().cpu(), x.k[0][0], x.v[0][0], 4999, 0, ALL)
+    assert rel_fro(outs[0][0][0, 0].float().cpu(), ref) <= TOL[torch.bfloat16]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_graph_is_replayed_after_larger_calls(dtype):
+    """The workspace that a graph holds stays when the handle's grows; two graphs of one handle, replayed in turn, do not disturb each other."""
+    x = Cache4([300, 40], spare=40, seed=6, dtype=dtype)
+    rn = lambda n_tok: torch.randn(2, 2, 8, n_tok, 64, generator=x.g, device="cuda").to(dtype)  # noqa: E731
+    qs, big = [rn(1), rn(4)], rn(16)
+    outs, want, graphs, score = [torch.empty_like(q) for q in qs], [], [], x.score.clone()
+    for q in qs:
+        want.append(torch.empty_like(q))
+        mone.mone_cache4_attention(x.h, -1, x.c, q, 8, q.shape[3], 2, 100, want[-1])
+    want_score = x.score.clone()
+    torch.cuda.synchronize()
+    for q, o in zip(qs, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            mone.mone_cache4_attention(x.h, -1, x.c, q, 8, q.shape[3], 2, 100, o)
+    mone.mone_cache4_attention(x.h, -1, x.c, big, 8, 16, 2, 100, torch.empty_like(big))
+    junk = [torch.full((1 << 22,), float("nan"), device="cuda") for _ in range(8)]  # what would lie where the old one was
+    for _ in range(3):
+        x.score.copy_(score)
+        for g, o in zip(graphs, outs):
+            o.zero_()
+            g.replay()
+    x.done()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want)) and torch.equal(x.score, want_score) and all(j.isnan().all() for j in junk)
+
+
+def test_on_another_stream():
+    x = Cache4([900, 40])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        attend(x, 4, 1, 0, ALL)
+
+
 # ----------------------------------------------------------------- append and read
 
 def rows_for_rounding(shape, g, exp):
