@@ -105,8 +105,9 @@ __device__ __forceinline__ uint32_t encode16(const Group<bf16, VEC>& x, float un
     return scale;
 }
 
-// A thread encodes a group of a token's key row and the same of its value row.  Bound by instructions, about 270 for the two; one token a
-// context by the launch and two dependent loads.
+// A thread encodes a group of a token's key row and the same of its value row.  Bound by instructions, 430 for the two (69% of the issue slots):
+// 2048 tokens of 16 layers, 8 heads of 64, in 20 us, 86 MB at 4.3 TB/s; 31 with quotients as for 32 bits.  One token a context by the launch and
+// two dependent loads.
 template <typename T, int HD, bool VEC>
 __global__ void __launch_bounds__(C4_THREADS) cache4_append_kernel(const Append4Args a) {
     constexpr int GROUPS = HD / 16;
@@ -181,7 +182,8 @@ __device__ __forceinline__ void decode16(T* p, uint2 codes, uint32_t scale, floa
     }
 }
 
-// A thread decodes a group of a position's key row and the same of its value row.  Bound by HBM.
+// A thread decodes a group of a position's key row and the same of its value row: 385 thousand rows of 128 twice in 41 us, 252 MB at 6.1 TB/s.
+// (Eight elements a thread in stores of 16 bytes were bound by instructions, 61 us.)
 template <typename T, int HD, bool VEC>
 __global__ void __launch_bounds__(C4_THREADS) cache4_read_kernel(const Read4Args a) {
     constexpr int GROUPS = HD / 16;
@@ -222,7 +224,7 @@ struct Evict4Args {
 };
 
 // A warp takes 32 survivors: a lane looks up where one comes from and goes to and moves its scales, then all move 16 bytes of codes each, four under
-// way at a time.
+// way at a time.  385 thousand rows of 72 bytes twice, read and written, in 22 us, 5 TB/s (8 survivors a warp: 31).
 template <int HD>
 __global__ void __launch_bounds__(C4_THREADS) cache4_compact_kernel(const Evict4Args a) {
     constexpr int UNITS = HD / 32, AHEAD = 4;  // 16 bytes of a row's codes; loads under way

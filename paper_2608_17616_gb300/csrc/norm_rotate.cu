@@ -127,6 +127,10 @@ struct RowWalk {
 
 // HD / 16 lanes take a job: some rows of one token, whose angles they compute once.  A lane has two pieces of eight elements of each row, for
 // halves those that are paired, so that a row takes no exchange but its sum of squares.
+// Bound by HBM: 2048 tokens of 16 layers, 40 heads of 64 in bf16, in 57 us, 336 MB at 5.9 TB/s (87% of what a copy reaches), with 61% of
+// the issue slots (fp32 two at a time; an angle's cosine and sine, 45 instructions, once for 16 rows).  The ring is what keeps enough
+// bytes under way: a row at a time took 79 us, the next row's pieces in registers 90 (104 of them, 14 warps an SM); rings of 3 and 6 rows 59 and
+// 56, jobs of 8 and 32 rows 58.  One token is bound by its launch and three dependent loads.
 template <typename T, int HD, bool VEC>
 __global__ void __launch_bounds__(NR_THREADS) norm_rotate_kernel(const __grid_constant__ NormRotateArgs a) {
     constexpr int LANES = HD / 16;
