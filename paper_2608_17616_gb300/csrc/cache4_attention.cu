@@ -388,7 +388,6 @@ struct CaFour {
             float* part = w.last ? ring_part : P::of_warp(a, w.b0 == 0);
             if (w.whole && lane == 0) a.info[kv * a.RT + w.rt] = 1 << 16;
             if (!w.whole && lane == 0) notes[w.b0 == 0] = {part, w.c, w.l, w.g, w.rt, w.r.n, w.first, w.cta_whole, w.parts};
-            const Head head(a, w.l, w.g);
 #pragma unroll
             for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -411,7 +410,7 @@ struct CaFour {
                     for (int d = 0; d < HD / 8; ++d) v[d] *= a.v_unit;
                     const float m = x.from[i][h] == FROM_NONE ? -INFINITY : x.from[i][h] * unit;
                     if (w.whole) {
-                        finish_row<CaFour, HD / 8>(a, kv, w.c, w.r.n, w.rt * ROWS + row, d0, head, v, l);
+                        finish_row<CaFour, HD / 8>(a, kv, w.c, w.l, w.g, w.r.n, w.rt * ROWS + row, d0, v, l);
                         T* out = static_cast<T*>(a.out) + (kv * a.R + w.rt * ROWS + row) * HD + d0;
                         __align__(16) T y[HD / 8];
 #pragma unroll

@@ -162,7 +162,7 @@ struct CaCores {
                 const int dim = d / VE * 8 * VE + l8 * VE + d % VE;
                 if (grp != i) continue;
                 if (walk.whole)
-                    write_row<CaCores>(a, kv, c, r.n, row0 + i, dim, Head(a, walk.l, walk.g), x[0], x[1], l[i]);
+                    write_row<CaCores>(a, kv, c, walk.l, walk.g, r.n, row0 + i, dim, x[0], x[1], l[i]);
                 else
                     *reinterpret_cast<float2*>(part + i * HD + dim) = make_float2(x[0], x[1]);
             }
@@ -370,7 +370,6 @@ struct CaTensor {
             float* part = w.last && ok ? ring_part : P::of_warp(a, w.b0 == 0);
             if (w.whole && lane == 0) a.info[kv * a.RT + w.rt] = 1 << 16;
             if (!w.whole && lane == 0) notes[w.b0 == 0] = {part, w.c, w.l, w.g, w.rt, r.n, w.first, w.cta_whole, w.parts};
-            const Head head(a, w.l, w.g);
 #pragma unroll
             for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -388,7 +387,7 @@ struct CaTensor {
 #pragma unroll
                         for (int d = 0; d < HD / 8; ++d) {
                             float v[1] = {x.o[i][d / 2][d % 2 * 2 + h]};
-                            finish_row<CaTensor, 1>(a, kv, w.c, r.n, row0 + row, 8 * d + gq, head, v, l);
+                            finish_row<CaTensor, 1>(a, kv, w.c, w.l, w.g, r.n, row0 + row, 8 * d + gq, v, l);
                             out[8 * d + gq] = __float2bfloat16_rn(v[0]);
                         }
                         if (gq == 0 && a.lse) a.lse[kv * a.R + row0 + row] = row_lse(x.m[i][h], lx, k2);

@@ -188,8 +188,8 @@ struct alignas(16) CaWalk {
     __device__ size_t kv(const CaArgs& a) const { return ((size_t)c * a.v.L + l) * a.v.n_kv + g; }
 };
 
-// What a form is, beside its kernel code: WARP_BYTES of shared memory a warp, the first ALIGN-ed; Args, a CaArgs with what else it takes; Maps, the tensor maps it takes; Head, the rows
-// of a layer's KV head in the pools; T, the type of queries and outputs.
+// What a form is, beside its kernel code: WARP_BYTES of shared memory a warp, the first ALIGN-ed; Args, a CaArgs with what else it takes;
+// Maps, the tensor maps it takes; Head, the rows of a layer's KV head in the pools; T, the type of queries and outputs.
 struct NoMaps {};
 
 // Rows of type T_
@@ -217,10 +217,11 @@ struct DenseHead {
 // value row times a probability of 0 for the rows that do not see it, which is NaN where the value is not finite; only
 // with several tokens do the rows of an item differ in what they see.  Reached by non-finite inputs only.
 template <typename Form, int N>
-__device__ __noinline__ void row_again(const typename Form::Args& a, const typename Form::T* q, const typename Form::Head& head, const int* table,
+__device__ __noinline__ void row_again(const typename Form::Args& a, const typename Form::T* q, int layer, int g, const int* table,
                                        int vis, int d0, float* o) {
     using T = typename Form::T;
     constexpr int HD = Form::HD;
+    const typename Form::Head head(a, layer, g);
     float m = -INFINITY, l = 0.f;
     for (int d = 0; d < N; ++d) o[d] = 0.f;
     for (int j = a.n_sink > 0 ? 0 : max(0, vis - a.window); j < vis; ++j) {
@@ -268,7 +269,7 @@ struct CaNote {
 
 // N dimensions from d of a row, from its O and sum, ready to be stored
 template <typename Form, int N>
-__device__ __forceinline__ void finish_row(const typename Form::Args& a, size_t kv, int c, int n, int row, int d, const typename Form::Head& head,
+__device__ __forceinline__ void finish_row(const typename Form::Args& a, size_t kv, int c, int layer, int g, int n, int row, int d,
                                            float (&o)[N], float l) {
     const float inv = l == 0.f ? 0.f : 1.f / l;  // no key that counts: 0
     bool bad = false;
@@ -279,18 +280,18 @@ __device__ __forceinline__ void finish_row(const typename Form::Args& a, size_t 
     }
     if (a.n_tok > 1 && bad) {
         float w[N];
-        row_again<Form, N>(a, static_cast<const typename Form::T*>(a.Q) + (kv * a.R + row) * Form::HD, head, a.v.table + (size_t)c * a.v.width,
+        row_again<Form, N>(a, static_cast<const typename Form::T*>(a.Q) + (kv * a.R + row) * Form::HD, layer, g, a.v.table + (size_t)c * a.v.width,
                            n - a.n_tok + row % a.n_tok + 1, d, w);
 #pragma unroll
         for (int i = 0; i < N; ++i) o[i] = w[i];
     }
 }
 template <typename Form>
-__device__ __forceinline__ void write_row(const typename Form::Args& a, size_t kv, int c, int n, int row, int d, const typename Form::Head& head,
+__device__ __forceinline__ void write_row(const typename Form::Args& a, size_t kv, int c, int layer, int g, int n, int row, int d,
                                           float o0, float o1, float l) {
     using T = typename Form::T;
     float o[2] = {o0, o1};
-    finish_row<Form, 2>(a, kv, c, n, row, d, head, o, l);
+    finish_row<Form, 2>(a, kv, c, layer, g, n, row, d, o, l);
     store2<T>(static_cast<T*>(a.out) + (kv * a.R + row) * Form::HD + d, o[0], o[1]);
 }
 
@@ -357,8 +358,7 @@ __device__ __forceinline__ void cluster_end(const typename Form::Args& a, const 
     const bool split = S > 1 && units > 1;
     bool nans = false;  // some row's sum
     if (units > 1) {    // else one warp has written the item
-        const typename Form::Head head(a, l, g);
-        auto write = [&](int row, int d, float o0, float o1, float l) { write_row<Form>(a, kv, c, r.n, row0 + row, d, head, o0, o1, l); };
+        auto write = [&](int row, int d, float o0, float o1, float sum) { write_row<Form>(a, kv, c, l, g, r.n, row0 + row, d, o0, o1, sum); };
         const float* ps[CA_WARPS];
 #pragma unroll
         for (int k = 0; k < CA_WARPS; ++k) ps[k] = notes[2 * k].part ? notes[2 * k].part : notes[2 * k + 1].part;
@@ -497,7 +497,6 @@ cache_attention_kernel(const __grid_constant__ typename Form::Maps maps, const t
         }
         const int row0 = it.rt * ROWS, rows = min(ROWS, a.R - row0);
         const size_t kv = ((size_t)it.c * a.v.L + it.l) * a.v.n_kv + it.g;
-        const typename Form::Head head(a, it.l, it.g);
         if (threadIdx.x == 0 && it.first) a.info[kv * a.RT + it.rt] = blockIdx.x | it.parts << 16;
         float* to = it.whole ? nullptr : P::of_cta(a, blockIdx.x, it.first);
         for (int e = 2 * threadIdx.x; e < rows * HD; e += 2 * CA_THREADS) {
@@ -507,7 +506,7 @@ cache_attention_kernel(const __grid_constant__ typename Form::Maps maps, const t
                 *reinterpret_cast<float2*>(to + e) = make_float2(x.o0, x.o1);
                 if (d == 0) to[P::M + row] = x.mx, to[P::L + row] = x.l, to[P::LX + row] = x.lx;
             } else {
-                write_row<Form>(a, kv, it.c, it.n, row0 + row, d, head, x.o0, x.o1, x.l);
+                write_row<Form>(a, kv, it.c, it.l, it.g, it.n, row0 + row, d, x.o0, x.o1, x.l);
                 if (d == 0 && a.lse) a.lse[kv * a.R + row0 + row] = row_lse(x.mx, x.lx, k2);
             }
         }
@@ -528,7 +527,7 @@ constexpr int FIN_TILE = 4 * FIN_THREADS, FIN_TILES = 4, FIN_POS = FIN_TILES * F
 // One row of a split item from its parts, of CTAs first .. first + n - 1.  A thread has two dimensions of every G-th part;
 // the G sums are added in order.
 template <typename Form>
-__device__ __forceinline__ void join_row(const typename Form::Args& a, int c, int row, size_t kv, const typename Form::Head& head, int n_pos,
+__device__ __forceinline__ void join_row(const typename Form::Args& a, int c, int layer, int g, int row, size_t kv, int n_pos,
                                          int first, int n, float k2) {
     constexpr int HD = Form::HD, ROWS = Form::ROWS;
     using P = Part<HD, ROWS>;
@@ -560,7 +559,7 @@ __device__ __forceinline__ void join_row(const typename Form::Args& a, int c, in
         o.x += os[k][col].x;
         o.y += os[k][col].y;
     }
-    write_row<Form>(a, kv, c, n_pos, row, 2 * col, head, o.x, o.y, l);
+    write_row<Form>(a, kv, c, layer, g, n_pos, row, 2 * col, o.x, o.y, l);
 }
 
 // The first R blocks of a KV head join its rows' parts; the others, if the cache has weights, add those of FIN_POS positions
@@ -579,7 +578,7 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) cache_finish_kernel(const type
     if ((int)blockIdx.x < a.R) {
         const int row = blockIdx.x, info = a.info[kv * a.RT + row / ROWS], first = info & 0xffff, n = info >> 16;
         if (n == 1) return;
-        join_row<Form>(a, c, row, kv, typename Form::Head(a, l, g), r.n, first, n, k2);
+        join_row<Form>(a, c, l, g, row, kv, r.n, first, n, k2);
         return;
     }
     float* score = a.v.score + (((size_t)c * a.v.Lh + l) * a.v.n_kv + g) * a.v.cap;
