@@ -28,20 +28,21 @@ __device__ __forceinline__ uint32_t scale_halves(uint32_t two) {
 __device__ __forceinline__ float scale_float(uint32_t one) { return __low2float(__halves2half2(__ushort_as_half((unsigned short)scale_halves(one & 0xff)), __half())); }
 __device__ __forceinline__ float2 halves_float2(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
 
-// a / b rounded so that no rounding after it, to far fewer bits, goes another way than a / b itself would: the quotient to the nearest, then a
-// step of its last place toward a / b if it is not exact (a >= 0, b > 0, inv the rounded 1 / b; a below 2^100 and normal where
-// it matters).  (The remainder of a quotient rounded to the nearest is exact in a fused multiply-add.)
-__device__ __forceinline__ float quotient_sticky(float a, float b, float inv) {
+// a / b rounded to odd: the next quotient toward zero, its last bit set if it is not exact, so that no rounding after it, to far fewer bits,
+// goes another way than a / b itself would (a >= 0, b > 0, inv the rounded 1 / b; a below 2^100 and normal where it matters).  (The
+// remainder of a quotient rounded to the nearest is exact in a fused multiply-add.)
+__device__ __forceinline__ float quotient_odd(float a, float b, float inv) {
     float q = a * inv;
     q = fmaf(fmaf(-q, b, a), inv, q);
     const float rem = fmaf(-q, b, a);
-    return rem == 0.f ? q : __int_as_float(__float_as_int(q) + (rem > 0.f ? 1 : -1));
+    const int down = __float_as_int(q) - (rem < 0.f);
+    return __int_as_float(rem == 0.f ? down : down | 1);
 }
 
 // The scale of a group whose largest |x| / 2^exp is `most`
 __device__ __forceinline__ uint32_t encode_scale(float most) {
     uint32_t s;
-    const float q = quotient_sticky(fminf(most, 2688.f), 6.f, 1.f / 6.f);
+    const float q = quotient_odd(fminf(most, 2688.f), 6.f, 1.f / 6.f);
     asm("{\n\t.reg .b16 s;\n\tcvt.rn.satfinite.e4m3x2.f32 s, %1, %1;\n\tcvt.u32.u16 %0, s;\n\t}" : "=r"(s) : "f"(q));
     return s & 0xff;
 }
@@ -53,7 +54,7 @@ __device__ __forceinline__ uint32_t code_two(float x0, float x1) {
 }
 // of x0 (low) and x1 under scale `s` > 0, inv the rounded 1 / s
 __device__ __forceinline__ uint32_t encode_two(float x0, float x1, float s, float inv) {
-    return code_two(copysignf(quotient_sticky(fminf(fabsf(x0), 8.f * s), s, inv), x0), copysignf(quotient_sticky(fminf(fabsf(x1), 8.f * s), s, inv), x1));
+    return code_two(copysignf(quotient_odd(fminf(fabsf(x0), 8.f * s), s, inv), x0), copysignf(quotient_odd(fminf(fabsf(x1), 8.f * s), s, inv), x1));
 }
 
 __device__ __forceinline__ uint32_t mul_halves(uint32_t a, uint32_t b) {

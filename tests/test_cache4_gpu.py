@@ -508,6 +508,45 @@ def test_append_and_read(lens, n_tok, page, order, pad, counts, layer, hd, exps,
             assert (g[:, :, m:] == 7.0).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rounding_next_to_every_tie(dtype):
+    """Of every scale: groups whose largest element makes it, and elements on the ties between codes and up to three steps of the type beside
+    them; and groups whose largest element lies on the ties between two scales and beside them."""
+    ties = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0])
+    info, bits = (np.int32, 0) if dtype is torch.float32 else (np.int32, 16)
+
+    def steps(v, k):  # k steps of the type away from zero
+        return (v.astype(np.float32).view(info) + (k << bits)).view(np.float32)
+
+    rows = []
+    for s in O.E4M3[1:]:
+        for k in range(-3, 4):
+            for sign in (1.0, -1.0):
+                g = np.full(16, 6.0 * s, dtype=np.float32)
+                g[1:8], g[8:15] = steps(ties * s, k), steps(ties * s, -k)
+                rows.append(np.float32(sign) * g)
+    for lo, hi in zip(O.E4M3[1:], O.E4M3[2:]):
+        for k in range(-3, 4):
+            rows.append(np.full(16, 1.0, dtype=np.float32) * steps(np.array([6 * (lo + hi) / 2]), k))
+    x = np.concatenate(rows)
+    n = len(x) // 64
+    x = x[:n * 64].reshape(1, 1, 1, n, 64)
+    h = handle(1, 1, 2, 64, dtype)
+    pages = -(-n // 16)
+    pools = [torch.zeros(1, pages, 2, 16, w, dtype=torch.uint8, device="cuda") for w in (32, 32, 4, 4)]
+    table, lens = torch.arange(pages, dtype=torch.int32, device="cuda")[None], torch.zeros(1, dtype=torch.int32, device="cuda")
+    k = torch.from_numpy(x.copy()).cuda().to(dtype).expand(1, 1, 2, n, 64).contiguous()
+    v = -k.flip(-1)
+    mone.mone_cache4_append(h, -1, mone.make_cache4(*pools, table, lens), k, v, k.stride()[:4], n)
+    mone.mone_mem_sync(h)
+    mone.mone_mem_free(h)
+    for i, t in enumerate((k, v)):
+        code, scale = O.four_bits(t[0, 0].double().cpu().numpy())
+        for pool, want in ((pools[i], packed(code)), (pools[i + 2], scale)):
+            got = pool[0].transpose(0, 1).reshape(2, pages * 16, -1)[:, :n].cpu().numpy()
+            assert np.array_equal(got, want), np.argwhere(got != want)[:5]
+
+
 def test_read_of_everything_and_of_nothing():
     x = Cache4([90, 0, 33], n_layers=3)
     K, V = (torch.full((3, 3, 2, 100, 64), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
