@@ -113,7 +113,7 @@ struct CaFour {
     static constexpr int HD = HD_, ROWS = BESIDE ? 4 : 8 * NT, CTAS = NT == 1 ? (TWO ? 3 : 4) : 2;
     static constexpr int ONE = 3, EACH = 2, FULL = 16, FEW = 6;          // blocks of a warp, see item_ctas
     static constexpr int CODES = KB * HD / 2, SCALES = KB * HD / 16, STAGE = 2 * (CODES + SCALES);
-    static constexpr int NS = HD == 64 ? 4 : 3;
+    static constexpr int NS = HD == 64 ? 4 : 2;  // (3 for 128: 121 us for 119, with less of the L1 left)
     // The ring, and what is not in registers while a piece's blocks go through: the walk of the copies, that of the products, the place of
     // the piece's scores
     static constexpr int AHEAD = NS * STAGE, NOW = AHEAD + sizeof(CaWalk), SCORES = NOW + sizeof(CaWalk), WARP_BYTES = AHEAD + 256, ALIGN = 128;
@@ -341,6 +341,7 @@ struct CaFour {
             CaWalk first = w;
             begin(a, ahead, first);
         }
+#pragma unroll 1
         for (int s = 0; s < NS - 1; ++s) feed(a, ahead, s);
         while (w.next(a)) {
             const int row0 = w.rt * ROWS, rows = min(ROWS, a.R - row0);
