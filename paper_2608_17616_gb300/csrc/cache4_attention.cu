@@ -102,7 +102,7 @@ __device__ __forceinline__ uint32_t load_two_bytes(uint32_t addr) {
 //
 // Bound by instructions, not by HBM: 600 for a block of 32 keys of 128 (140 conversions, 128 products of halves, 34 MMAs, 32 loads from
 // shared memory, 15 for the copies of a block in one page), of which 62% of the issue slots are used, with 4 warps a scheduler and no pipe above
-// half.  Two tokens over 131072 positions of 4 layers: 122 us, 604 MB at 4.9 TB/s (the rows in 16 bits: 300).  On the way: 221 us with
+// half.  Two tokens over 131072 positions of 4 layers: 119 us, 604 MB at 5.1 TB/s (the rows in 16 bits: 300).  On the way: 221 us with
 // masks, rescaling and a sum in every block; 175 with neither, and values' codes paired before their conversion (a permutation a pair of halves
 // less); 150 with four CTAs an SM for three (128 registers a thread for 168); 136 with a piece's walk out of the registers; 132 with
 // the copies of one page.  Bulk copies of a page want uniform addresses: 705 instructions, 142 for 136.
