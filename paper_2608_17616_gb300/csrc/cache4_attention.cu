@@ -105,7 +105,8 @@ __device__ __forceinline__ uint32_t load_two_bytes(uint32_t addr) {
 // half.  Two tokens over 131072 positions of 4 layers: 119 us, 604 MB at 5.1 TB/s (the rows in 16 bits: 300).  On the way: 221 us with
 // masks, rescaling and a sum in every block; 175 with neither, and values' codes paired before their conversion (a permutation a pair of halves
 // less); 150 with four CTAs an SM for three (128 registers a thread for 168); 136 with a piece's walk out of the registers; 132 with
-// the copies of one page.  Bulk copies of a page want uniform addresses: 705 instructions, 142 for 136.
+// the copies of one page.  Bulk copies of a page want uniform addresses: 705 instructions, 142 for 136.  The next block's scores beside this one's
+// values need 168 registers: 140, as three CTAs without.
 template <typename T_, int HD_, int NT, bool BESIDE>
 struct CaFour {
     using T = T_;
