@@ -479,7 +479,8 @@ mone_status mone_cache_reserve(mone_mem* m, const mone_pages* pages, int n_tok, 
 /*
  * Pages given back: those that hold no position below `keep` any more go to the end of the free list, context after context, and
  * their table entries become -1.  (A request has ended, drafted tokens were rejected, a cache has been evicted to other
- * pages.)  After a mone_cache_reserve of the same contexts, with its lens_out as lens and its lens as keep, list and tables are as before it.
+ * pages.)  After a mone_cache_reserve of the same contexts, with its lens_out as lens and its lens as keep, the list is as before it and
+ * so are the contexts' pages.
  *   keep       NULL (0), or [n_ctx] (device): positions that each context keeps, its length at most
  *   lens_out   NULL, or [n_ctx] (not lens itself): min(lens, keep); n_free_out [1] (not n_free itself)
  * Errors as above.
