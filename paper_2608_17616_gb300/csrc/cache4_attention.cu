@@ -513,7 +513,9 @@ struct CaFour {
                 for (int h = 0; h < 2; ++h) {
 #pragma unroll
                     for (int y = 4; y < 32; y <<= 1) most[h] = fmaxf(most[h], __shfl_xor_sync(0xffffffffu, most[h], y));
-                    const float to = fmaxf(x.from[i][h], most[h]), f = ca_exp2((x.from[i][h] - to) * x.k2[i][h]);
+                    // (by its own scores alone, whatever the item's other rows are)
+                    const float to = (most[h] - x.from[i][h]) * x.k2[i][h] > P_ROOM ? most[h] : x.from[i][h];
+                    const float f = ca_exp2((x.from[i][h] - to) * x.k2[i][h]);
                     x.from[i][h] = to;
                     x.lx[i][h] *= f;
                     x.l[i][h] *= f;

@@ -321,6 +321,25 @@ def test_weights_of_tokens_whose_scores_are_not_numbers(lens, spare, n_tok, bad,
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("group,spare", [(4, 3), (8, 3), (4, 2000)])
+def test_a_row_does_not_hang_on_the_others(group, spare, dtype):
+    """The bits of a head's output and no other's sizes, nor whether they are numbers."""
+    x = Cache4([900, 77], dtype=dtype, score=False, spare=spare, seed=3)
+    Q = torch.randn(2, 2, 2 * group, 1, 64, generator=x.g, device="cuda").to(dtype)
+    other, outs = Q.clone(), []
+    other[:, :, 1] *= 100
+    other[:, :, 2] = float("nan")
+    other[:, :, group - 1] = float("inf")
+    other[:, :, group + 1] = 0
+    for q in (Q, other):
+        outs.append(torch.empty_like(q))
+        mone.mone_cache4_attention(x.h, -1, x.c, q, 2 * group, 1, 0, ALL, outs[-1])
+    x.done()
+    same = [i for i in range(2 * group) if i not in (1, 2, group - 1, group + 1)]
+    assert torch.equal(outs[0][:, :, same], outs[1][:, :, same])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_queries_that_are_not_finite(dtype):
     """A NaN's row is NaN; an infinity's is what the formula gives: NaN, or where every seen key's score is -inf, 0."""
     x = Cache4([150], n_layers=1, dtype=dtype, score=False, seed=1)
