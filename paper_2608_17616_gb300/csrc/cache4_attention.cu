@@ -112,7 +112,10 @@ struct CaFour {
     using T = T_;
     static constexpr bool TWO = std::is_same<T, float>::value && !BESIDE;
     static constexpr int HD = HD_, ROWS = BESIDE ? 4 : 8 * NT, CTAS = NT == 1 ? (TWO ? 3 : 4) : 2;
-    static constexpr int ONE = 3, EACH = 2, FULL = 16, FEW = 6;          // blocks of a warp, see item_ctas
+    // Blocks of a warp, see item_ctas.  A second block costs a warp 0.6 us (head_dim 64) or 1, a cluster 0.9 (one layer of 370 positions 6.5 us, 7.4; with
+    // three blocks a warp, two of a cluster's, 7.0 and 8.6).  With a third of the GPU's CTAs in clusters they take up to 12 blocks a warp (4 layers of
+    // 9000, hd 128: 18.3 us, dealt 22.3), with fewer 6 (one of 9000: 12.3 and 11.6), with more 16 (8 contexts of up to 9000: 14.0 and 17.1).
+    static constexpr int ONE = 2, EACH = 1, FULL = 16, SOME = 12, FEW = 6;
     static constexpr int CODES = KB * HD / 2, SCALES = KB * HD / 16, STAGE = 2 * (CODES + SCALES);
     static constexpr int NS = HD == 64 ? 4 : 2;  // (3 for 128: 121 us for 119, with less of the L1 left)
     // The ring, and what is not in registers while a piece's blocks go through: the walk of the copies, that of the products, the place of

@@ -14,7 +14,7 @@ struct CaCores {
     static constexpr int HD = HD_, ROWS = 4, CTAS = HD == 64 ? 3 : 2;
     static constexpr int VE = 16 / sizeof(T), D = HD / 8, NP = D / VE;  // elements of 16 bytes; dimensions and 16-byte pieces of a lane
     static constexpr int U = 2;                                         // keys of a lane group at a time
-    static constexpr int ONE = 1, EACH = 1, FULL = 1, FEW = 1;          // blocks of a warp, see item_ctas
+    static constexpr int ONE = 1, EACH = 1, FULL = 1, SOME = 1, FEW = 1;          // blocks of a warp, see item_ctas
     static constexpr int WARP_BYTES = 2 * Part<HD, ROWS>::FLOATS * 4, ALIGN = 16;
 
     using Args = CaArgs;
@@ -219,7 +219,7 @@ struct CaTensor {
     using T = bf16;
     static constexpr int HD = HD_, ROWS = 8 * NT, CTAS = 2;
     static constexpr int SK = HD == 64 ? 32 : 16, SPB = KB / SK;  // keys of a stage, stages of a block
-    static constexpr int ONE = 3, EACH = 2, FULL = 16, FEW = 6 / SPB;                // blocks of a warp, see item_ctas
+    static constexpr int ONE = 3, EACH = 2, FULL = 16, SOME = 6 / SPB, FEW = 6 / SPB;                // blocks of a warp, see item_ctas
     static constexpr int SLAB = SK * 128, TILE = HD / 64 * SLAB, STAGE = 2 * TILE;  // 64 dimensions of the keys; keys; both
     static constexpr int NS = 3;
     static constexpr int BAR = NS * STAGE, WARP_BYTES = BAR + 1024, ALIGN = 1024;  // the ring, its barriers

@@ -649,6 +649,7 @@ inline long long seen_blocks(const CaArgs& a) {
 // 9.8, 12.1 and 12.5, 15.4; 20000: 97, 121 and 106, 124; 32 of 1151: 15.6, 17.5 and 22.6, 25.5.  hd 128, 4 layers of 131072, two tokens:
 // 297 and 318; 1 of 4500: 13.7, 17.6 and 12.2, 15.7.  The CUDA cores take 6 us a block, so it is theirs for one a warp: fp32, 500: 12.0,
 // 13.7 and 27.8, 30.8; 1151: 17.5, 20.0 and 14.7, 17.1.)
+// (The 4-bit form has its own numbers, at its constants.)
 // The lengths are on the device, so the rule goes by what the table and the window allow: a context that is short for its table is
 // dealt out (150 positions of one layer in a table of their own 5.6, with weights 6.2; in one for 8K or 32K 8.0 and 9.5).
 template <typename Form>
@@ -660,7 +661,7 @@ int item_ctas(const CaArgs& a, int sms) {
         while (S < 8 && 2 * S * items <= slots && blocks > Form::EACH * S * CA_WARPS) S *= 2;
     const bool full = 2 * S * items > slots;
     if (full && a.v.n_ctx == 1 && Form::FULL > 1) return S;
-    return blocks <= S * CA_WARPS * (full ? Form::FULL : Form::FEW) ? S : 0;
+    return blocks <= S * CA_WARPS * (full ? Form::FULL : 3 * S * items > slots ? Form::SOME : Form::FEW) ? S : 0;
 }
 
 template <typename Form>
