@@ -1,6 +1,7 @@
 // Queries and keys normalised by head and rotated by position, in one pass (mone_norm_rotate).
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "mone_common.cuh"
 
@@ -35,66 +36,69 @@ __device__ __forceinline__ void cos_sin(unsigned long long turn, float& c, float
     }
 }
 
-// Rows under way: a lane's pieces, two of eight elements of each, in shared memory at a place of its own, so that it waits for nobody else.
+// What a lane has of a row, 16 elements: NP chunks of 16 bytes, neighbouring lanes' beside one another
+template <typename T>
+struct Chunks {
+    static constexpr int E = 16 / sizeof(T), NP = 16 / E, H = NP / 2, F = E / 2;  // elements; chunks, half of them; pairs of elements of a chunk
+};
+
+// Rows under way: a lane's chunks, in shared memory at a place of its own, so that it waits for nobody else.
 template <typename T, bool VEC>
-struct Ring {
-    static constexpr int PER = 8 * sizeof(T) / 16;  // 16 bytes of a piece
-    static constexpr int BYTES = NR_DEPTH * 2 * PER * 16 * NR_THREADS;
+struct Ring : Chunks<T> {
+    using Chunks<T>::E;
+    using Chunks<T>::NP;
+    using Chunks<T>::F;
+    static constexpr int BYTES = NR_DEPTH * NP * 16 * NR_THREADS;
     uint8_t* at;
     __device__ __forceinline__ explicit Ring(uint8_t* smem) : at(smem + 16 * threadIdx.x) {}
-    __device__ __forceinline__ uint4* place(int slot, int i) const { return reinterpret_cast<uint4*>(at + (slot * 2 * PER + i) * 16 * NR_THREADS); }
-    __device__ __forceinline__ void copy(int slot, const T* p0, const T* p1) const {
-        if constexpr (VEC) {
+    __device__ __forceinline__ uint4* place(int slot, int k) const { return reinterpret_cast<uint4*>(at + (slot * NP + k) * 16 * NR_THREADS); }
+    __device__ __forceinline__ void copy(int slot, const T* row, const int (&d)[NP]) const {
 #pragma unroll
-            for (int i = 0; i < 2 * PER; ++i)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(place(slot, i))),
-                             "l"(reinterpret_cast<const uint4*>(i < PER ? p0 : p1) + i % PER)
-                             : "memory");
-        } else {
-            __align__(16) T t[16];
+        for (int k = 0; k < NP; ++k) {
+            if constexpr (VEC) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(place(slot, k))), "l"(row + d[k]) : "memory");
+            } else {
+                __align__(16) T t[E];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = p0[i], t[8 + i] = p1[i];
-#pragma unroll
-            for (int i = 0; i < 2 * PER; ++i) *place(slot, i) = reinterpret_cast<const uint4*>(t)[i];
+                for (int i = 0; i < E; ++i) t[i] = row[d[k] + i];
+                *place(slot, k) = *reinterpret_cast<const uint4*>(t);
+            }
         }
     }
-    // as pairs: 0 .. 3 of the first piece, 4 .. 7 of the second
+    // in pairs, chunk after chunk
     __device__ __forceinline__ void read(int slot, float2 (&x)[8]) const {
 #pragma unroll
-        for (int i = 0; i < 2 * PER; ++i) {
-            const uint4 u = *place(slot, i);
+        for (int k = 0; k < NP; ++k) {
+            const uint4 u = *place(slot, k);
             const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int j = 0; j < F; ++j) {
                 if constexpr (sizeof(T) == 2)
-                    x[4 * i + k] = make_float2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u));
-                else if (k % 2 == 0)
-                    x[2 * i + k / 2] = make_float2(__uint_as_float(w[k]), __uint_as_float(w[k + 1]));
+                    x[k * F + j] = make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
+                else
+                    x[k * F + j] = make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
             }
         }
     }
 };
 template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T* p, const float2* x) {
-    if constexpr (VEC) {
-        __align__(16) T t[8];
+__device__ __forceinline__ void store_chunk(T* p, const float2* x) {
+    constexpr int E = Chunks<T>::E;
+    __align__(16) T t[E];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(T) == 2) {
-                reinterpret_cast<uint32_t*>(t)[i] = pack_bf16(x[i].x, x[i].y);
-            } else {
-                t[2 * i] = x[i].x;
-                t[2 * i + 1] = x[i].y;
-            }
+    for (int j = 0; j < E / 2; ++j) {
+        if constexpr (sizeof(T) == 2) {
+            reinterpret_cast<uint32_t*>(t)[j] = pack_bf16(x[j].x, x[j].y);
+        } else {
+            t[2 * j] = x[j].x;
+            t[2 * j + 1] = x[j].y;
         }
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(t)[i];
+    }
+    if constexpr (VEC) {
+        *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(t);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            p[2 * i] = from_f<T>(x[i].x);
-            p[2 * i + 1] = from_f<T>(x[i].y);
-        }
+        for (int i = 0; i < E; ++i) p[i] = t[i];
     }
 }
 
@@ -125,15 +129,17 @@ struct RowWalk {
     }
 };
 
-// HD / 16 lanes take a job: some rows of one token, whose angles they compute once.  A lane has two pieces of eight elements of each row, for
-// halves those that are paired, so that a row takes no exchange but its sum of squares.
-// Bound by HBM: 2048 tokens of 16 layers, 40 heads of 64 in bf16, in 57 us, 336 MB at 5.9 TB/s (87% of what a copy reaches), with 61% of
-// the issue slots (fp32 two at a time; an angle's cosine and sine, 45 instructions, once for 16 rows).  The ring is what keeps enough
-// bytes under way: a row at a time took 79 us, the next row's pieces in registers 90 (104 of them, 14 warps an SM); rings of 3 and 6 rows 59 and
-// 56, jobs of 8 and 32 rows 58.  One token is bound by its launch and three dependent loads.
+// HD / 16 lanes take a job: some rows of one token, whose angles they compute once.  A lane has 16 elements of each row, with both of a pair, so that
+// a row takes no exchange but its sum of squares.
+// Bound by HBM and, in bf16, nearly by instructions (62% of the issue slots; fp32 two at a time; an angle's cosine and sine, 45 of them, once for 16
+// rows): 2048 tokens of 16 layers, 40 heads of 64 in 59 us, 336 MB at 5.7 TB/s, of 128 in 106 (6.3); in fp32 105 and 200 (6.4, 6.7; a copy
+// reaches 6.8).  The ring is what keeps enough bytes under way: a row at a time took 79 us, the next row's chunks in registers 90 (104 of
+// them, 14 warps an SM); a ring of 6 rows or jobs of 32 the same to 3% more.  Chunks of neighbouring lanes lie beside one another, so that an
+// instruction takes whole sectors: with two chunks of a lane beside one another fp32 took 139, neighbouring pairs 74 for 60.  Five
+// CTAs an SM (102 registers) for four: 59 for 63.  One token is bound by its launch and three dependent loads.
 template <typename T, int HD, bool VEC>
-__global__ void __launch_bounds__(NR_THREADS) norm_rotate_kernel(const __grid_constant__ NormRotateArgs a) {
-    constexpr int LANES = HD / 16;
+__global__ void __launch_bounds__(NR_THREADS, 5) norm_rotate_kernel(const __grid_constant__ NormRotateArgs a) {
+    constexpr int LANES = HD / 16, E = Chunks<T>::E, NP = Chunks<T>::NP, H = Chunks<T>::H, F = Chunks<T>::F;
     extern __shared__ __align__(16) uint8_t nr_smem[];
     const Ring<T, VEC> ring(nr_smem);
     const RotateArgs& r = a.r;
@@ -144,8 +150,18 @@ __global__ void __launch_bounds__(NR_THREADS) norm_rotate_kernel(const __grid_co
     const bool live = job < a.jobs;
     const long long part = live ? job / tokens : 0, ct = live ? job - part * tokens : 0;
     const int c = (int)(ct / r.n_tok), i = (int)(ct - (long long)c * r.n_tok);
-    const bool turns = l < r.rot / 16;
-    const int d0 = 8 * (turns && !r.neighbours ? l : 2 * l), d1 = turns && !r.neighbours ? d0 + r.rot / 2 : d0 + 8;
+    // The chunks: those of neighbours in order; of halves H of each half, first those that turn, then those of the halves of what does not
+    int d[NP];
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+        const int t = (r.neighbours ? k : k % H) * LANES + l, over = t * E - r.rot / 2;  // of the first half
+        if (r.neighbours)
+            d[k] = t * E;
+        else if (over < 0)
+            d[k] = t * E + k / H * (r.rot / 2);
+        else
+            d[k] = r.rot + over + k / H * ((HD - r.rot) / 2);
+    }
     const int row0 = (int)part * a.chunk, rows = live ? min(a.chunk, a.rows - row0) : 0;
     RowWalk in(r, row0), out(r, row0);
     in.place<false>(c, i);
@@ -153,25 +169,28 @@ __global__ void __launch_bounds__(NR_THREADS) norm_rotate_kernel(const __grid_co
     auto copy = [&](int n) {
         if (n < rows) {
             const T* x = static_cast<const T*>(r.side[in.second()].x) + in.at;
-            ring.copy(n % NR_DEPTH, x + d0, x + d1);
+            ring.copy(n % NR_DEPTH, x, d);
             in.next<false>(c, i);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll
     for (int n = 0; n < NR_DEPTH - 1; ++n) copy(n);
-    float2 co[4], si[4];  // of pairs 2 e and 2 e + 1
+    float2 co[4], si[4];  // of this lane's pairs 2 e and 2 e + 1
+    unsigned turns = 0;   // which of them turn
     {
         unsigned p = (unsigned)((r.first ? r.first[c] : 0) + i);
         if (r.period) p %= (unsigned)r.period;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            co[e] = make_float2(1.f, 1.f);
-            si[e] = make_float2(0.f, 0.f);
-            if (turns) {
-                cos_sin(r.turns[8 * l + 2 * e] * p, co[e].x, si[e].x);
-                cos_sin(r.turns[8 * l + 2 * e + 1] * p, co[e].y, si[e].y);
+        for (int e = 0; e < 8; ++e) {
+            const int pair = r.neighbours ? (e / F * LANES + l) * F + e % F : (e / E * LANES + l) * E + e % E;
+            float x = 1.f, y = 0.f;
+            if (pair < r.rot / 2) {
+                turns |= 1u << e;
+                cos_sin(r.turns[pair] * p, x, y);
             }
+            (e & 1 ? co[e / 2].y : co[e / 2].x) = x;
+            (e & 1 ? si[e / 2].y : si[e / 2].x) = y;
         }
     }
     float2 w[8];
@@ -187,10 +206,7 @@ __global__ void __launch_bounds__(NR_THREADS) norm_rotate_kernel(const __grid_co
         if (scaled && weight != loaded) {  // a layer's, of a side
             loaded = weight;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                w[e] = make_float2(weight[d0 + 2 * e], weight[d0 + 2 * e + 1]);
-                w[4 + e] = make_float2(weight[d1 + 2 * e], weight[d1 + 2 * e + 1]);
-            }
+            for (int e = 0; e < 8; ++e) w[e] = make_float2(weight[d[e / F] + 2 * (e % F)], weight[d[e / F] + 2 * (e % F) + 1]);
         }
         asm volatile("cp.async.wait_group %0;" ::"n"(NR_DEPTH - 1) : "memory");
         float2 x[8];
@@ -224,24 +240,30 @@ __global__ void __launch_bounds__(NR_THREADS) norm_rotate_kernel(const __grid_co
                 for (int e = 0; e < 8; ++e) x[e] = mul2(x[e], mul2(w[e], make_float2(inv, inv)));
             }
         }
-        if (r.neighbours) {
+        auto rotate = [&](auto every) {  // what does not turn is left alone: 0 times an infinity is not 0
+            constexpr bool EVERY = decltype(every)::value;
+            if (r.neighbours) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float co1 = e & 1 ? co[e / 2].y : co[e / 2].x, si1 = e & 1 ? si[e / 2].y : si[e / 2].x;
-                x[e] = make_float2(x[e].x * co1 - x[e].y * si1, x[e].y * co1 + x[e].x * si1);
-            }
-        } else {
+                for (int e = 0; e < 8; ++e) {
+                    const float co1 = e & 1 ? co[e / 2].y : co[e / 2].x, si1 = e & 1 ? si[e / 2].y : si[e / 2].x;
+                    if (EVERY || (turns >> e & 1)) x[e] = make_float2(x[e].x * co1 - x[e].y * si1, x[e].y * co1 + x[e].x * si1);
+                }
+            } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 p = x[e], q = x[4 + e];
-                x[e] = fma2(p, co[e], mul2(q, make_float2(-si[e].x, -si[e].y)));
-                x[4 + e] = fma2(q, co[e], mul2(p, si[e]));
+                for (int e = 0; e < 4; ++e) {
+                    const float2 p = x[e], q = x[4 + e];
+                    if (EVERY || (turns >> (2 * e) & 1)) {
+                        x[e] = fma2(p, co[e], mul2(q, make_float2(-si[e].x, -si[e].y)));
+                        x[4 + e] = fma2(q, co[e], mul2(p, si[e]));
+                    }
+                }
             }
-        }
+        };
+        r.rot == HD ? rotate(std::true_type()) : rotate(std::false_type());
         if (on) {
             T* to = static_cast<T*>(s.out) + out.at;
-            store8<T, VEC>(to + d0, x);
-            store8<T, VEC>(to + d1, x + 4);
+#pragma unroll
+            for (int k = 0; k < NP; ++k) store_chunk<T, VEC>(to + d[k], x + k * F);
             out.next<true>(c, i);
         }
     }

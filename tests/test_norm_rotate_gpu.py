@@ -123,6 +123,33 @@ def test_rows_whose_squares_leave_the_range(dtype):
         check(out[0, 0, a, i:i + 1], x[0, 0, a, i:i + 1], np.ones(64), [i], [10000.0 ** (-2.0 * j / 64) for j in range(32)], True, 1e-6)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("halves", [True, False])
+@pytest.mark.parametrize("rot", [0, 16, 48, 64, 112])
+def test_what_is_not_finite_reaches_its_pair_alone(rot, halves, dtype):
+    """Without a norm, an element is turned with its partner or left as it is, whatever the others of its row are."""
+    h, hd, n_tok = handle(1, 1, 1, 128, dtype), 128, 128
+    x = torch.randn(1, 1, 1, n_tok, hd, device="cuda").to(dtype)
+    for t in range(n_tok):
+        x[0, 0, 0, t, t] = [float("inf"), -float("inf"), float("nan")][t % 3]
+    out = torch.empty_like(x)
+    rotary = mone.make_rotary(rot, mone.MONE_ROTATE_HALVES if halves else mone.MONE_ROTATE_NEIGHBOURS, base=100.0)
+    mone.mone_norm_rotate(h, -1, rotary, None, n_tok, None, mone.make_heads(x, out))
+    mone.mone_mem_sync(h)
+    mone.mone_mem_free(h)
+    fine = x.clone()
+    fine[~x.isfinite()] = 1.0
+    ref = O.norm_rotate(fine[0, 0, 0].double().cpu().numpy(), None, np.arange(n_tok), [100.0 ** (-2.0 * i / max(rot, 1)) for i in range(rot // 2)], halves, 0.0)
+    got = out[0, 0, 0].double().cpu().numpy()
+    for t in range(n_tok):
+        mate = t if t >= rot else (t + rot // 2) % rot if halves else t ^ 1
+        if t >= rot:
+            assert np.array_equal(got[t, t], x[0, 0, 0, t, t].item(), equal_nan=True)
+        rest = np.array([i not in (t, mate) for i in range(hd)])
+        tol = TOL * np.abs(ref[t]).max() + (2.0 ** -8 * np.abs(ref[t]) if dtype is torch.bfloat16 else 0)
+        assert (np.abs(got[t] - ref[t]) <= tol * 1.01)[rest].all()
+
+
 def test_a_layer_by_itself():
     """One layer's tensors, as a backbone that runs layer by layer has them, and the weights of all."""
     B, L, n_tok = 2, 3, 4
