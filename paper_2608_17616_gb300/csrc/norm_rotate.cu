@@ -132,11 +132,12 @@ struct RowWalk {
 // HD / 16 lanes take a job: some rows of one token, whose angles they compute once.  A lane has 16 elements of each row, with both of a pair, so that
 // a row takes no exchange but its sum of squares.
 // Bound by HBM and, in bf16, nearly by instructions (62% of the issue slots; fp32 two at a time; an angle's cosine and sine, 45 of them, once for 16
-// rows): 2048 tokens of 16 layers, 40 heads of 64 in 59 us, 336 MB at 5.7 TB/s, of 128 in 106 (6.3); in fp32 105 and 200 (6.4, 6.7; a copy
+// rows): 2048 tokens of 16 layers, 40 heads of 64 in 57 us, 336 MB at 5.8 TB/s, of 128 in 104 (6.4); in fp32 104 and 199 (6.5, 6.7; a copy
 // reaches 6.8).  The ring is what keeps enough bytes under way: a row at a time took 79 us, the next row's chunks in registers 90 (104 of
 // them, 14 warps an SM); a ring of 6 rows or jobs of 32 the same to 3% more.  Chunks of neighbouring lanes lie beside one another, so that an
-// instruction takes whole sectors: with two chunks of a lane beside one another fp32 took 139, neighbouring pairs 74 for 60.  Five
-// CTAs an SM (102 registers) for four: 59 for 63.  One token is bound by its launch and three dependent loads.
+// instruction takes whole sectors: with two chunks of a lane beside one another fp32 took 139, neighbouring pairs 74 for 59.  Five
+// CTAs an SM (102 registers) for four: 59 for 63.  One token is bound by its launch and three dependent loads (2.5 us in a graph; with a branch
+// for each pair that may not turn 3.0).
 template <typename T, int HD, bool VEC>
 __global__ void __launch_bounds__(NR_THREADS, 5) norm_rotate_kernel(const __grid_constant__ NormRotateArgs a) {
     constexpr int LANES = HD / 16, E = Chunks<T>::E, NP = Chunks<T>::NP, H = Chunks<T>::H, F = Chunks<T>::F;
@@ -184,11 +185,10 @@ __global__ void __launch_bounds__(NR_THREADS, 5) norm_rotate_kernel(const __grid
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int pair = r.neighbours ? (e / F * LANES + l) * F + e % F : (e / E * LANES + l) * E + e % E;
-            float x = 1.f, y = 0.f;
-            if (pair < r.rot / 2) {
-                turns |= 1u << e;
-                cos_sin(r.turns[pair] * p, x, y);
-            }
+            const bool on = pair < r.rot / 2;  // (below 64 in any case, what the table has)
+            float x, y;
+            cos_sin(on ? r.turns[pair] * p : 0, x, y);
+            turns |= on << e;
             (e & 1 ? co[e / 2].y : co[e / 2].x) = x;
             (e & 1 ? si[e / 2].y : si[e / 2].x) = y;
         }
