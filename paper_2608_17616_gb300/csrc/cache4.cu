@@ -44,7 +44,7 @@ template <typename T, bool VEC>
 struct Group {
     static constexpr int WORDS = 16 * sizeof(T) / 4;
     uint32_t w[WORDS];
-    __device__ __forceinline__ explicit Group(const T* p) {
+    __device__ __forceinline__ void load(const T* p) {
         if constexpr (VEC) {
 #pragma unroll
             for (int i = 0; i < WORDS; i += 8)
@@ -105,19 +105,22 @@ __device__ __forceinline__ uint32_t encode16(const Group<bf16, VEC>& x, float un
     return scale;
 }
 
-// A thread encodes a group of a token's key row and the same of its value row.  Bound by instructions, 430 for the two (69% of the issue slots):
-// 2048 tokens of 16 layers, 8 heads of 64, in 20 us, 86 MB at 4.3 TB/s; 31 with quotients as for 32 bits.  One token a context by the launch and
-// two dependent loads.
-template <typename T, int HD, bool VEC>
+// A thread encodes PER groups of a token's key row and the same of its value row.  Bound by instructions where there are many tokens, 430 a group of
+// both: 2048 tokens of 16 layers, 8 heads of 64, in 20.2 us, 86 MB at 4.3 TB/s (31 with quotients as for 32 bits); two groups of bf16
+// values a thread, which share the addresses, 345 and 19.7.  A token a context is bound by the launch and two dependent loads: with its read 3.6 us in a
+// graph, by two groups a thread 4.0.
+template <typename T, int HD, bool VEC, int PER>
 __global__ void __launch_bounds__(C4_THREADS) cache4_append_kernel(const Append4Args a) {
-    constexpr int GROUPS = HD / 16;
+    constexpr int EACH = HD / (16 * PER);  // threads of a row
+    using Codes = typename std::conditional<PER == 2, uint4, uint2>::type;
+    using Scales = typename std::conditional<PER == 2, uint16_t, uint8_t>::type;
     const CacheView& v = a.f.v;
     const int chain = blockIdx.z, g = blockIdx.y, c = chain / v.L, l = chain % v.L;
     pdl_wait();
     const int len = cache_len(v, c);
     const int n = a.counts ? min(max(a.counts[c], 0), a.n_tok) : a.n_tok;
     if (a.lens_out && blockIdx.x == 0 && g == 0 && l == 0 && threadIdx.x == 0) a.lens_out[c] = (int)min((long long)len + n, v.cap);
-    const int i = blockIdx.x * (C4_THREADS / GROUPS) + threadIdx.x / GROUPS, u = threadIdx.x % GROUPS;
+    const int i = blockIdx.x * (C4_THREADS / EACH) + threadIdx.x / EACH, u = threadIdx.x % EACH;
     if (i >= n) return;
     const int pos = len + i;  // at most 2^30 + 2^20
     if (pos >= v.cap) {
@@ -125,25 +128,43 @@ __global__ void __launch_bounds__(C4_THREADS) cache4_append_kernel(const Append4
         return;
     }
     if (u == 0 && v.score) v.score[(((size_t)c * v.Lh + l) * v.n_kv + g) * v.cap + pos] = 0.f;
-    const long long src = c * a.s0 + l * a.s1 + g * a.s2 + i * a.s3 + 16 * u;
-    const Group<T, VEC> k(static_cast<const T*>(a.K) + src), w(static_cast<const T*>(a.V) + src);
+    const long long src = c * a.s0 + l * a.s1 + g * a.s2 + i * a.s3 + 16 * PER * u;
+    Group<T, VEC> k[PER], w[PER];
+#pragma unroll
+    for (int y = 0; y < PER; ++y) {
+        k[y].load(static_cast<const T*>(a.K) + src + 16 * y);
+        w[y].load(static_cast<const T*>(a.V) + src + 16 * y);
+    }
     const int page = cache_page(v, v.table + (size_t)c * v.width, pos >> v.page_log2);
     if (page < 0) return;
     const FourRows rows(a.f, l, g);
-    const long long code = rows.code(page, pos) + 8 * u, scale = rows.scale(page, pos) + u;
-    uint2 q;
-    rows.Ks[scale] = (uint8_t)encode16(k, a.k_inv, q);
-    *reinterpret_cast<uint2*>(rows.K + code) = q;
-    rows.Vs[scale] = (uint8_t)encode16(w, a.v_inv, q);
-    *reinterpret_cast<uint2*>(rows.V + code) = q;
+    const long long code = rows.code(page, pos) + 8 * PER * u, scale = rows.scale(page, pos) + PER * u;
+    auto put = [&](const Group<T, VEC>(&x)[PER], float unit_inv, uint8_t* codes, uint8_t* scales) {
+        __align__(16) uint2 q[PER];
+        uint32_t s = 0;
+#pragma unroll
+        for (int y = 0; y < PER; ++y) s |= encode16(x[y], unit_inv, q[y]) << (8 * y);
+        *reinterpret_cast<Scales*>(scales) = (Scales)s;
+        *reinterpret_cast<Codes*>(codes) = *reinterpret_cast<const Codes*>(q);
+    };
+    put(k, a.k_inv, rows.K + code, rows.Ks + scale);
+    put(w, a.v_inv, rows.V + code, rows.Vs + scale);
 }
 
-template <typename T, int HD>
+template <typename T, int HD, int PER>
 cudaError_t append(const Append4Args& a, bool vec, cudaStream_t st) {
-    const int tokens = C4_THREADS / (HD / 16);
+    const int tokens = C4_THREADS / (HD / 16) * PER;
     const dim3 grid((unsigned)((a.n_tok + tokens - 1) / tokens), a.f.v.n_kv, a.f.v.n_ctx * a.f.v.L);
-    return vec ? launch_kernel(cache4_append_kernel<T, HD, true>, grid, dim3(C4_THREADS), 0, st, true, 1, a)
-               : launch_kernel(cache4_append_kernel<T, HD, false>, grid, dim3(C4_THREADS), 0, st, true, 1, a);
+    return vec ? launch_kernel(cache4_append_kernel<T, HD, true, PER>, grid, dim3(C4_THREADS), 0, st, true, 1, a)
+               : launch_kernel(cache4_append_kernel<T, HD, false, PER>, grid, dim3(C4_THREADS), 0, st, true, 1, a);
+}
+template <typename T, int HD>
+cudaError_t append(const Append4Args& a, bool vec, int sms, cudaStream_t st) {
+    if constexpr (sizeof(T) == 2) {  // two groups a thread where that leaves every SM its threads
+        const long long threads = (long long)a.n_tok * a.f.v.n_kv * a.f.v.n_ctx * a.f.v.L * (HD / 32);
+        if (threads >= 2048ll * sms) return append<T, HD, 2>(a, vec, st);
+    }
+    return append<T, HD, 1>(a, vec, st);
 }
 
 // ---------------------------------------------------------------- read
@@ -293,8 +314,8 @@ cudaError_t launch_cache4_append(const DevState& s, const Cache4View& f, const v
                                  const int* counts, int* lens_out, cudaStream_t st) {
     const Append4Args a{f, K, V, strides[0], strides[1], strides[2], strides[3], n_tok, 1.f / f.k_unit, 1.f / f.v_unit, counts, lens_out};
     const bool vec = vec_rows(K, V, strides, s.dtype == 0 ? 4 : 2);
-    if (s.dtype == 0) return s.hd == 64 ? append<float, 64>(a, vec, st) : append<float, 128>(a, vec, st);
-    return s.hd == 64 ? append<bf16, 64>(a, vec, st) : append<bf16, 128>(a, vec, st);
+    if (s.dtype == 0) return s.hd == 64 ? append<float, 64>(a, vec, s.sms, st) : append<float, 128>(a, vec, s.sms, st);
+    return s.hd == 64 ? append<bf16, 64>(a, vec, s.sms, st) : append<bf16, 128>(a, vec, s.sms, st);
 }
 
 cudaError_t launch_cache4_read(const DevState& s, const Cache4View& f, const int* from, int n_pos, void* K, void* V, const long long* strides,

@@ -476,6 +476,7 @@ def rows_for_rounding(shape, g, exp):
     ([15, 16, 17, 0], 1, 16, "head", 0, None, -1, 128, (0, 0)),
     ([15, 16, 17, 0], 33, 16, "position", 0, None, 1, 64, (3, -5)),
     ([100, 7], 500, 64, "head", 0, [500, 0], -1, 64, (0, 0)),       # a prompt for one context, nothing for the other
+    ([9, 30], 10001, 64, "head", 0, [10001, 9000], -1, 128, (0, 2)),  # many
     ([100, 7, 9], 5, 1, "head", 0, [2, 9, -3], -1, 64, (0, 64)),      # counts past the tokens that there are, pages of one
     ([100, 7], 20, 16, "head", 3, None, -1, 128, (-64, 0)),
     ([3], 20, 8, "layers inner", 1, None, 0, 64, (0, 0)),
