@@ -176,7 +176,7 @@ struct Read4Args {
     const int* from;
 };
 
-// 16 values of their codes and scale.  A code's product with its scale is exact in a half, and that times 2^exp in T but where it leaves T's range.
+// 16 values of their codes and scale.  A code's product with its scale is exact in a half, and that times 2^exp in T.
 template <typename T, bool VEC>
 __device__ __forceinline__ void decode16(T* p, uint2 codes, uint32_t scale, float unit) {
     uint32_t h[8];
