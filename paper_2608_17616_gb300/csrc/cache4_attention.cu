@@ -101,7 +101,7 @@ __device__ __forceinline__ uint32_t load_two_bytes(uint32_t addr) {
 // beside their rests in the N of 8, of more both are multiplied one after the other.
 //
 // Bound by instructions, not by HBM: 600 for a block of 32 keys of 128 (140 conversions, 128 products of halves, 34 MMAs, 32 loads from
-// shared memory, 15 for the copies of a block in one page), of which 62% of the issue slots are used, with 4 warps a scheduler and no pipe above
+// shared memory, 35 for the copies of a block in one page), of which 62% of the issue slots are used, with 4 warps a scheduler and no pipe above
 // half.  Two tokens over 131072 positions of 4 layers: 119 us, 604 MB at 5.1 TB/s (the rows in 16 bits: 300).  On the way: 221 us with
 // masks, rescaling and a sum in every block; 175 with neither, and values' codes paired before their conversion (a permutation a pair of halves
 // less); 150 with four CTAs an SM for three (128 registers a thread for 168); 136 with a piece's walk out of the registers; 132 with
@@ -119,7 +119,7 @@ struct CaFour {
     static constexpr int CODES = KB * HD / 2, SCALES = KB * HD / 16, STAGE = 2 * (CODES + SCALES);
     static constexpr int NS = HD == 64 ? 4 : 2;  // (3 for 128: 121 us for 119, with less of the L1 left)
     // The ring, and what is not in registers while a piece's blocks go through: the walk of the copies, that of the products, the place of
-    // the piece's scores
+    // the piece's scores and its head's addresses
     static constexpr int AHEAD = NS * STAGE, NOW = AHEAD + sizeof(CaWalk), SCORES = NOW + sizeof(CaWalk), WARP_BYTES = AHEAD + 256, ALIGN = 128;
     static constexpr int CHUNKS = HD / 32;  // of 16 bytes, of a row's codes
     static constexpr float P_LOG2 = 7.f, P_UNIT_INV = 0x1p-7f, P_ROOM = 8.f, FROM_NONE = -3e38f;
@@ -133,8 +133,8 @@ struct CaFour {
 
     uint32_t ring, lane;
     float* ring_part;  // the ring as the place of the warp's last part
-    // bytes in a stage: of the codes that this lane copies, of its eighth's key, of its values 2 t and 2 t + 1, of their scales; all of
-    // the first rows, those after them at fixed distances
+    // Places in a stage: of the codes that this lane copies, of its quarter of key gq, its eighth of values 2 t and 2 t + 1, and their
+    // scales.  (Of the first eight rows; the others are at fixed distances.)
     uint32_t copy_at, key_at, val_at[2], key_scale_at, val_scale_at;
 
     // Byte of chunk c of row r: neighbouring rows, and for head_dim 128 halves of a row, change places so that neither the loads of
