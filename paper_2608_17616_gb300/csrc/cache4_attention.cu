@@ -115,17 +115,19 @@ struct CaFour {
     // Blocks of a warp, see item_ctas.  A second block costs a warp 0.6 us (head_dim 64) or 1, a cluster 0.9 (one layer of 370 positions 6.5 us, 7.4; with
     // three blocks a warp, two of a cluster's, 7.0 and 8.6).  With a third of the GPU's CTAs in clusters they take up to 12 blocks a warp (4 layers of
     // 9000, hd 128: 18.3 us, dealt 22.3), with fewer 6 (one of 9000: 12.3 and 11.6), with more 16 (8 contexts of up to 9000: 14.0 and 17.1).
+    static constexpr bool IN_STEP = true;
+    using Walk = CaWalk<IN_STEP>;
     static constexpr int ONE = 2, EACH = 1, FULL = 16, SOME = 12, FEW = 6;
     static constexpr int CODES = KB * HD / 2, SCALES = KB * HD / 16, STAGE = 2 * (CODES + SCALES);
     static constexpr int NS = HD == 64 ? 4 : 2;  // (3 for 128: 121 us for 119, with less of the L1 left)
     // The ring, and what is not in registers while a piece's blocks go through: the walk of the copies, that of the products, the place of
     // the piece's scores and its head's addresses
-    static constexpr int AHEAD = NS * STAGE, NOW = AHEAD + sizeof(CaWalk), SCORES = NOW + sizeof(CaWalk), WARP_BYTES = AHEAD + 256, ALIGN = 128;
+    static constexpr int AHEAD = NS * STAGE, NOW = AHEAD + sizeof(Walk), SCORES = NOW + sizeof(Walk), WARP_BYTES = AHEAD + 256, ALIGN = 128;
     static constexpr int CHUNKS = HD / 32;  // of 16 bytes, of a row's codes
     static constexpr float P_LOG2 = 7.f, P_UNIT_INV = 0x1p-7f, P_ROOM = 8.f, FROM_NONE = -3e38f;
     static_assert(CTAS * (CA_WARPS * WARP_BYTES + ALIGN + 1536) <= 228 * 1024, "CTAs an SM");
     static_assert(Part<HD, ROWS>::FLOATS * 4 <= AHEAD, "a part fits in the ring");
-    static_assert(sizeof(CaWalk) % 16 == 0 && SCORES + 32 <= WARP_BYTES, "what is put aside");
+    static_assert(sizeof(Walk) % 16 == 0 && SCORES + 32 <= WARP_BYTES, "what is put aside");
 
     using Args = Ca4Args;
     using Maps = NoMaps;
@@ -161,16 +163,16 @@ struct CaFour {
         int gap;                 // the end of the first positions' blocks
     };
     // A walk put aside, by every lane the same, and back
-    __device__ __forceinline__ void put(int at, const CaWalk& w) const {
+    __device__ __forceinline__ void put(int at, const Walk& w) const {
         const uint4* u = reinterpret_cast<const uint4*>(&w);
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(CaWalk) / 16; ++i)
+        for (int i = 0; i < (int)sizeof(Walk) / 16; ++i)
             asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(ring + at + 16 * i), "r"(u[i].x), "r"(u[i].y), "r"(u[i].z), "r"(u[i].w) : "memory");
     }
-    __device__ __forceinline__ void get(int at, CaWalk& w) const {
+    __device__ __forceinline__ void get(int at, Walk& w) const {
         uint4* u = reinterpret_cast<uint4*>(&w);
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(CaWalk) / 16; ++i)
+        for (int i = 0; i < (int)sizeof(Walk) / 16; ++i)
             asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(u[i].x), "=r"(u[i].y), "=r"(u[i].z), "=r"(u[i].w) : "r"(ring + at + 16 * i) : "memory");
     }
     __device__ __forceinline__ int aside(int at) const {
@@ -185,10 +187,10 @@ struct CaFour {
         asm volatile("ld.shared.b64 %0, [%1];" : "=l"(p) : "r"(ring + at) : "memory");
         return p;
     }
-    static constexpr int R_N = offsetof(CaWalk, r) + offsetof(CaRange, n), R_T0 = offsetof(CaWalk, r) + offsetof(CaRange, t0),
-                         R_LO = offsetof(CaWalk, r) + offsetof(CaRange, lo);
+    static constexpr int R_N = offsetof(Walk, r) + offsetof(CaRange, n), R_T0 = offsetof(Walk, r) + offsetof(CaRange, t0),
+                         R_LO = offsetof(Walk, r) + offsetof(CaRange, lo);
     // The first block of a walk's next piece that has any
-    __device__ __forceinline__ void begin(const Args& a, Feed& f, CaWalk& w) const {
+    __device__ __forceinline__ void begin(const Args& a, Feed& f, Walk& w) const {
         do {
             if (!w.next(a)) {
                 f.left = -1;
@@ -216,7 +218,7 @@ struct CaFour {
             if (f.j0 == f.gap) f.j0 = aside(AHEAD + R_LO);
             page(a, f, aside(AHEAD + R_N), aside(AHEAD + R_T0));
         } else {
-            CaWalk w;
+            Walk w;
             get(AHEAD, w);
             __syncwarp();
             begin(a, f, w);
@@ -338,11 +340,11 @@ struct CaFour {
         using P = Part<HD, ROWS>;
         const int gq = lane >> 2, t = lane & 3;
         const float scale2 = a.scale * 1.4426950408889634f;
-        CaWalk w(a);
+        Walk w(a);
         Feed ahead;
         int slot = 0;  // of the block to be read next
         {
-            CaWalk first = w;
+            Walk first = w;
             begin(a, ahead, first);
         }
 #pragma unroll 1
@@ -493,7 +495,7 @@ struct CaFour {
             if (!WHOLE) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int row = row_of(i, h), vis = n - a.n_tok + (a.n_tok == 1 ? 0 : (aside(NOW + offsetof(CaWalk, rt)) * ROWS + row) % a.n_tok) + 1;
+                    const int row = row_of(i, h), vis = n - a.n_tok + (a.n_tok == 1 ? 0 : (aside(NOW + offsetof(Walk, rt)) * ROWS + row) % a.n_tok) + 1;
 #pragma unroll
                     for (int u = 0; u < 2; ++u)
 #pragma unroll

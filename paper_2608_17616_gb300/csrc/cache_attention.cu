@@ -14,6 +14,8 @@ struct CaCores {
     static constexpr int HD = HD_, ROWS = 4, CTAS = HD == 64 ? 3 : 2;
     static constexpr int VE = 16 / sizeof(T), D = HD / 8, NP = D / VE;  // elements of 16 bytes; dimensions and 16-byte pieces of a lane
     static constexpr int U = 2;                                         // keys of a lane group at a time
+    static constexpr bool IN_STEP = false;
+    using Walk = CaWalk<IN_STEP>;
     static constexpr int ONE = 1, EACH = 1, FULL = 1, SOME = 1, FEW = 1;          // blocks of a warp, see item_ctas
     static constexpr int WARP_BYTES = 2 * Part<HD, ROWS>::FLOATS * 4, ALIGN = 16;
 
@@ -26,7 +28,7 @@ struct CaCores {
     __device__ CaCores(const NoMaps&, uint8_t* smem, int) : parts(reinterpret_cast<float*>(smem)) {}
 
     __device__ __forceinline__ void run(const CaArgs& a, CaNote* notes) {
-        CaWalk walk(a);
+        Walk walk(a);
         while (walk.next(a)) piece(a, walk, notes);
     }
 
@@ -49,7 +51,7 @@ struct CaCores {
         }
     }
 
-    __device__ __forceinline__ void piece(const CaArgs& a, const CaWalk& walk, CaNote* notes) {
+    __device__ __forceinline__ void piece(const CaArgs& a, const Walk& walk, CaNote* notes) {
         const CaRange& r = walk.r;
         const int c = walk.c, row0 = walk.rt * ROWS, rows = min(ROWS, a.R - row0);
         const size_t kv = walk.kv(a);
@@ -219,6 +221,8 @@ struct CaTensor {
     using T = bf16;
     static constexpr int HD = HD_, ROWS = 8 * NT, CTAS = 2;
     static constexpr int SK = HD == 64 ? 32 : 16, SPB = KB / SK;  // keys of a stage, stages of a block
+    static constexpr bool IN_STEP = false;
+    using Walk = CaWalk<IN_STEP>;
     static constexpr int ONE = 3, EACH = 2, FULL = 16, SOME = 6 / SPB, FEW = 6 / SPB;                // blocks of a warp, see item_ctas
     static constexpr int SLAB = SK * 128, TILE = HD / 64 * SLAB, STAGE = 2 * TILE;  // 64 dimensions of the keys; keys; both
     static constexpr int NS = 3;
@@ -261,16 +265,16 @@ struct CaTensor {
         return (chunk >> 3) * SLAB + row * 128 + (((chunk ^ row) & 7) << 4);
     }
     // stages of a piece, and the first key of one (the last block may end in its first half)
-    static __device__ __forceinline__ int stages(const CaWalk& w) {
+    static __device__ __forceinline__ int stages(const Walk& w) {
         const int n = (w.b1 - w.b0) * SPB;
         return SPB == 2 && n && w.r.at(w.b1 - 1) + SK >= w.r.n ? n - 1 : n;
     }
-    static __device__ __forceinline__ int key0(const CaWalk& w, int i) { return w.r.at(w.b0 + i / SPB) + i % SPB * SK; }
+    static __device__ __forceinline__ int key0(const Walk& w, int i) { return w.r.at(w.b0 + i / SPB) + i % SPB * SK; }
 
     // The copies of a warp's stages, ahead of their reading and on through the pieces.  Lane n holds the page of copy n of the
     // piece's next 32.
     struct Feed {
-        CaWalk w;
+        Walk w;
         int box_log2, copies;  // positions of a copy, copies of a stage
         int i = 0, n = 0, batch = 0, page = 0;
         __device__ Feed(const CaArgs& a) : w(a) {
@@ -328,7 +332,7 @@ struct CaTensor {
         const int lane = threadIdx.x & 31, gq = lane >> 2, t = lane & 3;
         const float k2 = a.scale * 1.4426950408889634f;
         Feed ahead(a);
-        CaWalk w = ahead.w;
+        Walk w = ahead.w;
         int slot = 0, phase = 0;  // of the stage to be read next
         for (int s = 0; s < NS - 1; ++s) feed(a, ahead, s);
         bool ok = true;

@@ -13,6 +13,8 @@
 // shares of the item's blocks, and at the end they join their parts through distributed shared memory, without a second
 // kernel.
 //
+// With IN_STEP the items are dealt out in groups, the CTAs in as many.
+//
 // For the weights the scores go to the workspace as well (4 bytes a row and position beside the 4 head_dim, in bf16, of its
 // key and value), and the second kernel, or the cluster's end, adds exp(z - max) / sum over the rows of a KV head.
 #pragma once
@@ -46,6 +48,7 @@ struct CaArgs {
     float scale;
     int ctas;                  // that the blocks are dealt out to
     int split;                 // CTAs of an item, or 0: dealt out
+    int groups;                // of items, each dealt out to as many CTAs: every groups-th item of a context is of the same
     float* part;               // [ctas + 4 ctas][2][ROWS][hd + 3]: the CTAs' parts, and those that their warps put here
     int* info;                 // [chains][n_kv][RT] of an item, the CTA that has its first part and their number (<< 16)
     float* lse;                // [chains][n_kv][R] log2 of the sum of exp of items that one CTA has whole, with the weights
@@ -79,19 +82,24 @@ __device__ __forceinline__ int udiv(int a, int b) { return (int)((unsigned)a / (
 
 // How the units of all items, one item after the other, are dealt out: `share` to each CTA.  A boundary within an item of
 // up to CA_WHOLE units moves to the item's start.
+template <bool IN_STEP>
 struct CaDeal {
-    int total, share;
+    // items of a context and CTAs that are dealt out together
+    static __device__ __forceinline__ int items(const CaArgs& a) { return IN_STEP ? udiv(a.per, a.groups) : a.per; }
+    static __device__ __forceinline__ int ctas(const CaArgs& a) { return IN_STEP ? udiv(a.ctas, a.groups) : a.ctas; }
+    int total, share, per;
     int units, mine, incl;  // of context c0 + lane, of those scanned last: units of an item, of its items, up to its last
-    __device__ CaDeal(const CaArgs& a) {
+    __device__ CaDeal(const CaArgs& a) : per(items(a)) {
         total = 0;
         for (int c0 = 0; c0 < a.v.n_ctx; c0 += 32) total = scan(a, c0, total);
-        share = max(udiv(total + a.ctas - 1, a.ctas), CA_SHARE);
+        const int n = ctas(a);
+        share = max(udiv(total + n - 1, n), CA_SHARE);
     }
     // with `before` units ahead of them; returns the units up to the last
     __device__ int scan(const CaArgs& a, int c0, int before) {
         const int lane = threadIdx.x & 31;
         units = c0 + lane < a.v.n_ctx ? CaRange(a, c0 + lane).units() : 0;
-        mine = units * a.per;
+        mine = units * per;
         incl = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -111,7 +119,7 @@ struct CaDeal {
         base = __shfl_sync(0xffffffffu, incl - mine, k);
         return __shfl_sync(0xffffffffu, units, k);
     }
-    // the first unit of CTA w
+    // the first unit of CTA w of them
     __device__ int start(const CaArgs& a, int w) {
         const int u = w * share;  // below 2^30 + ctas share
         if (u >= total) return total;
@@ -122,7 +130,9 @@ struct CaDeal {
 };
 
 // The pieces of a warp, one after the other: blocks [b0, b1) of an item
+template <bool IN_STEP>
 struct alignas(16) CaWalk {
+    using Deal = CaDeal<IN_STEP>;
     int u, end, ctx0, c, units;
     CaRange r;
     int l, g, rt, b0, b1;
@@ -151,10 +161,11 @@ struct alignas(16) CaWalk {
             share_out();
             return;
         }
-        CaDeal deal(a);
+        Deal deal(a);
         share = deal.share;
-        cta0 = deal.start(a, blockIdx.x);
-        cta1 = deal.start(a, blockIdx.x + 1);
+        const int n = Deal::ctas(a), rank = IN_STEP ? blockIdx.x - udiv(blockIdx.x, n) * n : blockIdx.x;
+        cta0 = deal.start(a, rank);
+        cta1 = deal.start(a, rank + 1);
         share_out();
         if (u < end) {
             units = deal.locate(a, u, ctx0, c);
@@ -163,13 +174,15 @@ struct alignas(16) CaWalk {
     }
     __device__ bool next(const CaArgs& a) {
         if (u >= end) return false;
-        while (u - ctx0 >= units * a.per) {
-            ctx0 += units * a.per;
+        while (u - ctx0 >= units * Deal::items(a)) {
+            ctx0 += units * Deal::items(a);
             r = CaRange(a, ++c);
             units = r.units();
         }
-        const int in_ctx = udiv(u - ctx0, units), lg = a.RT == 1 ? in_ctx : udiv(in_ctx, a.RT);
+        int in_ctx = udiv(u - ctx0, units);
         b0 = u - ctx0 - in_ctx * units;
+        if (IN_STEP && a.groups > 1) in_ctx = in_ctx * a.groups + udiv(blockIdx.x, Deal::ctas(a));
+        const int lg = a.RT == 1 ? in_ctx : udiv(in_ctx, a.RT);
         const int e = min(units, b0 + end - u);
         whole = b0 == 0 && e == units;
         const int u0 = u - b0;
@@ -673,12 +686,20 @@ cudaError_t launch(typename Form::Args a, const typename Form::Maps& maps, int s
     a.per = a.v.L * a.v.n_kv * a.RT;
     a.ctas = Form::CTAS * sms;
     a.split = item_ctas<Form>(a, sms);
+    a.groups = 1;
     if (a.split) {
         *kernels = 1;
         a.ctas = a.split * a.per * a.v.n_ctx;
         cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(cache_attention_kernel<Form, true>), smem_items, once_items);
         if (e != cudaSuccess) return e;
         return launch_kernel(cache_attention_kernel<Form, true>, dim3(a.ctas), dim3(CA_THREADS), smem_items, st, true, a.split, maps, a);
+    }
+    if (Form::IN_STEP) {
+        const int heads = a.v.n_kv * a.RT, all = a.ctas;
+        for (int k = a.v.L; k > 0 && a.groups == 1; --k) {
+            const int groups = k * heads, ctas = all / std::max(groups, 1) * groups;
+            if (a.v.L % k == 0 && 16 * ctas >= 15 * all) a.groups = groups, a.ctas = ctas;
+        }
     }
     cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(cache_attention_kernel<Form, false>), smem, once);
     if (e != cudaSuccess) return e;
