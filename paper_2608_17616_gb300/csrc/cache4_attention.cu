@@ -102,9 +102,9 @@ __device__ __forceinline__ uint32_t load_two_bytes(uint32_t addr) {
 //
 // Bound by instructions, not by HBM: 600 for a block of 32 keys of 128 (140 conversions, 128 products of halves, 34 MMAs, 32 loads from
 // shared memory, 35 for the copies of a block in one page), of which 62% of the issue slots are used, with 4 warps a scheduler and no pipe above
-// half.  Two tokens over 131072 positions of 4 layers: 119 us, 604 MB at 5.1 TB/s (the rows in 16 bits: 300).  On the way: 221 us with
+// half.  Two tokens over 131072 positions of 4 layers: 112 us, 604 MB at 5.4 TB/s (the rows in 16 bits: 300).  On the way: 221 us with
 // masks, rescaling and a sum in every block; 175 with neither, and values' codes paired before their conversion (a permutation a pair of halves
-// less); 150 with four CTAs an SM for three (128 registers a thread for 168); 136 with a piece's walk out of the registers; 132 with
+// less); 150 with four CTAs an SM for three (128 registers a thread for 168); 136 with a piece's walk out of the registers; 119 with
 // the copies of one page.  Bulk copies of a page want uniform addresses: 705 instructions, 142 for 136.  The next block's scores beside this one's
 // values need 168 registers: 140, as three CTAs without.
 template <typename T_, int HD_, int NT, bool BESIDE>
@@ -115,6 +115,9 @@ struct CaFour {
     // Blocks of a warp, see item_ctas.  A second block costs a warp 0.6 us (head_dim 64) or 1, a cluster 0.9 (one layer of 370 positions 6.5 us, 7.4; with
     // three blocks a warp, two of a cluster's, 7.0 and 8.6).  With a third of the GPU's CTAs in clusters they take up to 12 blocks a warp (4 layers of
     // 9000, hd 128: 18.3 us, dealt 22.3), with fewer 6 (one of 9000: 12.3 and 11.6), with more 16 (8 contexts of up to 9000: 14.0 and 17.1).
+    // A row's scales are 4 or 8 bytes of a sector of 32.  Two tokens over 131072 positions of 4 layers, heads and layers in step, heads only, neither: 112 us,
+    // 117, 120; of pools whose heads lie inside positions 122, 151, 231 (1.46 GB read); head_dim 64 78, 81, 83, inside positions 87, 92, 197; 16 contexts
+    // of 32K in fp32 73, 73, 80.
     static constexpr bool IN_STEP = true;
     using Walk = CaWalk<IN_STEP>;
     static constexpr int ONE = 2, EACH = 1, FULL = 16, SOME = 12, FEW = 6;

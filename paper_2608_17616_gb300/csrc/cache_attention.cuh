@@ -13,7 +13,9 @@
 // shares of the item's blocks, and at the end they join their parts through distributed shared memory, without a second
 // kernel.
 //
-// With IN_STEP the items are dealt out in groups, the CTAs in as many.
+// Of a form IN_STEP the items are dealt out in groups, to as many CTAs each: heads of a layer, if they can, heads and layers.  Heads of a context, and
+// row tiles of a head, are then read at the same positions at about the same time, so what they share (a sector of HBM where a position's heads
+// lie beside one another, a tile's keys) is read once.
 //
 // For the weights the scores go to the workspace as well (4 bytes a row and position beside the 4 head_dim, in bf16, of its
 // key and value), and the second kernel, or the cluster's end, adds exp(z - max) / sum over the rows of a KV head.
@@ -48,7 +50,7 @@ struct CaArgs {
     float scale;
     int ctas;                  // that the blocks are dealt out to
     int split;                 // CTAs of an item, or 0: dealt out
-    int groups;                // of items, each dealt out to as many CTAs: every groups-th item of a context is of the same
+    int groups;                // of items, each dealt out to ctas / groups CTAs: a context's items g, g + groups, .. are group g's
     float* part;               // [ctas + 4 ctas][2][ROWS][hd + 3]: the CTAs' parts, and those that their warps put here
     int* info;                 // [chains][n_kv][RT] of an item, the CTA that has its first part and their number (<< 16)
     float* lse;                // [chains][n_kv][R] log2 of the sum of exp of items that one CTA has whole, with the weights
@@ -673,7 +675,13 @@ int item_ctas(const CaArgs& a, int sms) {
     if (blocks > Form::ONE * CA_WARPS)
         while (S < 8 && 2 * S * items <= slots && blocks > Form::EACH * S * CA_WARPS) S *= 2;
     const bool full = 2 * S * items > slots;
-    if (full && a.v.n_ctx == 1 && Form::FULL > 1) return S;
+    // Dealt out in groups, long items gain more from the CTAs that clusters would leave idle than the second kernel takes: from 8 blocks a warp times
+    // the idle share on, or 10 and 20 with clusters of 4 and 2, whose more items take longer to join.  (4-bit rows, 32 heads over 8, hd 128, two
+    // tokens, us in clusters and dealt: 5 layers, 8 a cluster, half idle, 8192 positions 21.1 and 20.9, 131072 189 and 137; 6 layers, 16384
+    // 33.5 and 35.0, 32768 56.1 and 54.1; 16 layers, 4 a cluster, a sixth idle, 16384 69.8 and 72.4, 65536 239 and 222; fp32, 2 a cluster, nearly half
+    // idle, 8192 50.1 and 53.8, 16384 89.2 and 84.4.)
+    const bool idle = Form::IN_STEP && (slots - S * items) * blocks >= (long long)std::max(8, 40 / S) * slots * S * CA_WARPS;
+    if (full && a.v.n_ctx == 1 && Form::FULL > 1 && !idle) return S;
     return blocks <= S * CA_WARPS * (full ? Form::FULL : 3 * S * items > slots ? Form::SOME : Form::FEW) ? S : 0;
 }
 
@@ -694,10 +702,10 @@ cudaError_t launch(typename Form::Args a, const typename Form::Maps& maps, int s
         if (e != cudaSuccess) return e;
         return launch_kernel(cache_attention_kernel<Form, true>, dim3(a.ctas), dim3(CA_THREADS), smem_items, st, true, a.split, maps, a);
     }
-    if (Form::IN_STEP) {
+    if (Form::IN_STEP) {  // the most groups, of all heads of one layer or more, that leave out at most a sixteenth of the CTAs
         const int heads = a.v.n_kv * a.RT, all = a.ctas;
         for (int k = a.v.L; k > 0 && a.groups == 1; --k) {
-            const int groups = k * heads, ctas = all / std::max(groups, 1) * groups;
+            const int groups = k * heads, ctas = all / groups * groups;
             if (a.v.L % k == 0 && 16 * ctas >= 15 * all) a.groups = groups, a.ctas = ctas;
         }
     }

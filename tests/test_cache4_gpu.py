@@ -197,6 +197,26 @@ def test_attention_by_clusters_of_every_size(n_layers, lens, group, n_tok, hd, n
     attend(Cache4(lens, n_layers=n_layers, hd=hd, page=32, seed=n_layers), group, n_tok, n_sink, window)
 
 
+@pytest.mark.parametrize("n_layers,n_kv,lens,group,n_tok,page,spare", [
+    (16, 8, [700, 3, 33, 0, 1, 200], 4, 1, 16, 0),     # two layers a group
+    (7, 6, [700, 2100], 4, 1, 16, 600),                # an item a group
+    (25, 10, [90, 600, 5], 2, 1, 32, 0),               # five layers a group
+    (2, 6, [1200, 0, 31], 3, 7, 16, 1000),             # row tiles
+    (1, 8, [300], 20, 16, 16, 2000),                   # more row tiles than a group could have a CTA each
+    (19, 4, [40] * 5 + [0] * 9 + [1500], 4, 2, 64, 0),
+])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("order", ["head", "position"])
+def test_attention_dealt_out_in_groups(n_layers, n_kv, lens, group, n_tok, page, spare, order, dtype):
+    attend(Cache4(lens, n_layers=n_layers, n_kv=n_kv, hd=64, page=page, dtype=dtype, order=order, spare=spare, seed=n_kv), group, n_tok, 0, ALL)
+
+
+@pytest.mark.parametrize("length,window", [(17000, ALL), (17000, 16500), (300, ALL)])
+@pytest.mark.parametrize("dtype,n_tok", [(torch.bfloat16, 1), (torch.bfloat16, 4), (torch.float32, 2)])
+def test_one_context_whose_clusters_would_leave_the_gpu_idle(length, window, dtype, n_tok):
+    attend(Cache4([length], n_layers=5, n_kv=8, hd=64, page=64, dtype=dtype, spare=(17000 - length) // 64, score=n_tok != 4), 2, n_tok, 5, window)
+
+
 @pytest.mark.parametrize("order,pad", [("position", 0), ("layers inner", 0), ("head", 1), ("position", 3)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("hd", [64, 128])
