@@ -165,7 +165,8 @@ struct alignas(16) CaWalk {
         }
         Deal deal(a);
         share = deal.share;
-        const int n = Deal::ctas(a), rank = IN_STEP ? blockIdx.x - udiv(blockIdx.x, n) * n : blockIdx.x;
+        // CTAs behind the last group's have no unit
+        const int n = Deal::ctas(a), rank = IN_STEP ? blockIdx.x - min(udiv(blockIdx.x, n), a.groups - 1) * n : blockIdx.x;
         cta0 = deal.start(a, rank);
         cta1 = deal.start(a, rank + 1);
         share_out();
@@ -705,8 +706,8 @@ cudaError_t launch(typename Form::Args a, const typename Form::Maps& maps, int s
     if (Form::IN_STEP) {  // the most groups, of all heads of one layer or more, that leave out at most a sixteenth of the CTAs
         const int heads = a.v.n_kv * a.RT, all = a.ctas;
         for (int k = a.v.L; k > 0 && a.groups == 1; --k) {
-            const int groups = k * heads, ctas = all / groups * groups;
-            if (a.v.L % k == 0 && 16 * ctas >= 15 * all) a.groups = groups, a.ctas = ctas;
+            const int groups = k * heads;
+            if (a.v.L % k == 0 && 16 * (all / groups * groups) >= 15 * all) a.groups = groups;
         }
     }
     cudaError_t e = smem_opt_in(reinterpret_cast<const void*>(cache_attention_kernel<Form, false>), smem, once);
