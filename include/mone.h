@@ -449,7 +449,8 @@ mone_status mone_cache4_evict(mone_mem* m, int layer, const mone_cache4* cache, 
  *   free    [n_pages] (room for every page): the free pages are its first *n_free entries
  *   table   [n_ctx][table_width] as in mone_cache, for every layer; n_pages and page_size too
  *   lens    [n_ctx] positions that each context holds: it has the pages of those, and nobody else has them
- * Calls that share a list or a table are ordered by the caller (one stream, say).
+ * Calls that share a list or a table are ordered by the caller (one stream, say).  No output of a call may overlap another of its arrays:
+ * each context is served beside the others, by the arrays as they were.
  */
 typedef struct {
     int* free;

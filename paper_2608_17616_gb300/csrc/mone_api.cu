@@ -137,6 +137,20 @@ bool is_live(const mone_mem* m) {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+struct Range {
+    const void* p;
+    size_t bytes;
+};
+// Whether any of these, from the one at `writes` on, shares a byte with one before it (null: none)
+bool overlap(const Range* r, int writes, int n) {
+    for (int i = writes; i < n; ++i)
+        for (int j = 0; j < i; ++j) {
+            const uintptr_t a = (uintptr_t)r[i].p, b = (uintptr_t)r[j].p;
+            if (a && b && a < b + r[j].bytes && b < a + r[i].bytes) return true;
+        }
+    return false;
+}
+
 mone_status validate_config(const mone_config* c) {
     if (!c) return MONE_ERR_INVALID_ARG;
     if (c->n_ctx < 1 || c->n_layers < 1 || c->d_in < 1 || c->d_hid < 1 || c->d_out < 2 || c->n_kv_heads < 1 ||
@@ -1085,6 +1099,13 @@ static mone_status cache_view(const mone_mem* m, int layer, const mone_cache* c,
     return pool_view(m, layer, c, m->s.hd, elsize(m->s.dtype), v);
 }
 
+// Whether a call's new lengths lie in what its other CTAs read of other contexts
+static bool lens_taken(const int* lens_out, const CacheView& v, const int* counts) {
+    const size_t n = v.n_ctx * sizeof(int);
+    const Range r[] = {{v.lens, n}, {counts, n}, {v.table, n * v.width}, {lens_out, n}};
+    return overlap(r, 3, 4);
+}
+
 mone_status mone_cache_append(mone_mem* m, int layer, const mone_cache* cache, const void* K, const void* V,
                               const long long strides[4], int n_tok, const int* counts, int* lens_out, void* stream) {
     CacheView v;
@@ -1094,7 +1115,7 @@ mone_status mone_cache_append(mone_mem* m, int layer, const mone_cache* cache, c
     if (((uintptr_t)K | (uintptr_t)V) % elsize(s.dtype) || (((uintptr_t)counts | (uintptr_t)lens_out) & 3u)) return MONE_ERR_INVALID_ARG;
     for (int i = 0; i < 4; ++i)
         if (strides[i] < 0) return MONE_ERR_INVALID_ARG;
-    if (lens_out && lens_out == cache->lens) return MONE_ERR_INVALID_ARG;
+    if (lens_taken(lens_out, v, counts)) return MONE_ERR_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     return timed(m, K_CACHE, st, 1, [&] { return launch_cache_append(s, v, K, V, strides, n_tok, counts, lens_out, st); });
 }
@@ -1156,13 +1177,13 @@ mone_status mone_cache_attention(mone_mem* m, int layer, const mone_cache* cache
 }
 
 // An eviction's arguments beside its cache
-static mone_status evict_args(const float* score, const int* table, const int* lens, int page_size, int keep, int n_sink, int n_recent,
-                              const int* to_table, int to_width, const float* to_score, const int* kept, const int* lens_out) {
+static mone_status evict_args(const float* score, const CacheView& v, int page_size, int keep, int n_sink, int n_recent, const int* to_table,
+                              int to_width, const float* to_score, const int* kept, const int* lens_out) {
     if (!score || !to_table || !to_score || !kept || to_width < 1) return MONE_ERR_INVALID_ARG;
     if (((uintptr_t)to_table | (uintptr_t)to_score | (uintptr_t)kept | (uintptr_t)lens_out) & 3u) return MONE_ERR_INVALID_ARG;
     if (keep < 1 || n_sink < 0 || n_recent < 0 || (long long)n_sink + n_recent > keep) return MONE_ERR_INVALID_ARG;
     if ((long long)to_width * page_size < keep || (long long)to_width * page_size > (1ll << 30)) return MONE_ERR_INVALID_ARG;
-    if (to_table == table || to_score == score || (lens_out && lens_out == lens)) return MONE_ERR_INVALID_ARG;
+    if (to_table == v.table || to_score == score || lens_taken(lens_out, v, nullptr)) return MONE_ERR_INVALID_ARG;
     return MONE_OK;
 }
 
@@ -1171,7 +1192,7 @@ mone_status mone_cache_evict(mone_mem* m, int layer, const mone_cache* cache, in
     CacheView v;
     MONE_TRY(cache_view(m, layer, cache, &v));
     const DevState& s = m->s;
-    MONE_TRY(evict_args(cache->score, cache->table, cache->lens, cache->page_size, keep, n_sink, n_recent, to_table, to_width, to_score, kept, lens_out));
+    MONE_TRY(evict_args(cache->score, v, cache->page_size, keep, n_sink, n_recent, to_table, to_width, to_score, kept, lens_out));
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const size_t off = layer == MONE_ALL_LAYERS ? 0 : (size_t)layer * s.n_kv * to_width * cache->page_size;
     return timed(m, K_CACHE, st, 2, [&] {
@@ -1210,7 +1231,7 @@ mone_status mone_cache4_append(mone_mem* m, int layer, const mone_cache4* cache,
     if (((uintptr_t)K | (uintptr_t)V) % elsize(s.dtype) || (((uintptr_t)counts | (uintptr_t)lens_out) & 3u)) return MONE_ERR_INVALID_ARG;
     for (int i = 0; i < 4; ++i)
         if (strides[i] < 0) return MONE_ERR_INVALID_ARG;
-    if (lens_out && lens_out == cache->lens) return MONE_ERR_INVALID_ARG;
+    if (lens_taken(lens_out, f.v, counts)) return MONE_ERR_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     return timed(m, K_CACHE, st, 1, [&] { return launch_cache4_append(s, f, K, V, strides, n_tok, counts, lens_out, st); });
 }
@@ -1257,7 +1278,7 @@ mone_status mone_cache4_evict(mone_mem* m, int layer, const mone_cache4* cache, 
     Cache4View f;
     MONE_TRY(cache4_view(m, layer, cache, &f));
     const DevState& s = m->s;
-    MONE_TRY(evict_args(cache->score, cache->table, cache->lens, cache->page_size, keep, n_sink, n_recent, to_table, to_width, to_score, kept, lens_out));
+    MONE_TRY(evict_args(cache->score, f.v, cache->page_size, keep, n_sink, n_recent, to_table, to_width, to_score, kept, lens_out));
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const size_t off = layer == MONE_ALL_LAYERS ? 0 : (size_t)layer * s.n_kv * to_width * cache->page_size;
     return timed(m, K_CACHE, st, 2, [&] {
@@ -1273,7 +1294,6 @@ static mone_status pages_view(const mone_mem* m, const mone_pages* p, const int*
     if (p->n_pages < 1 || p->page_size < 1 || p->table_width < 1) return MONE_ERR_INVALID_ARG;
     if ((p->page_size & (p->page_size - 1)) || p->page_size > 1024) return MONE_ERR_UNSUPPORTED_SHAPE;
     if ((long long)p->table_width * p->page_size > (1ll << 30)) return MONE_ERR_INVALID_ARG;
-    if (n_free_out == p->n_free || (lens_out && lens_out == p->lens)) return MONE_ERR_INVALID_ARG;
     v->free = p->free;
     v->n_free = p->n_free;
     v->n_pages = p->n_pages;
@@ -1293,7 +1313,10 @@ mone_status mone_cache_reserve(mone_mem* m, const mone_pages* pages, int n_tok, 
     PagesView v;
     MONE_TRY(pages_view(m, pages, lens_out, n_free_out, &v));
     if (n_tok < 1 || n_tok > (1 << 20) || (((uintptr_t)counts | (uintptr_t)granted) & 3u) || ((uintptr_t)slots & 7u)) return MONE_ERR_INVALID_ARG;
-    if (granted && (granted == counts || granted == pages->lens || granted == lens_out)) return MONE_ERR_INVALID_ARG;
+    // every CTA adds up what the contexts before its own ask for, and no CTA waits for another
+    const size_t n = v.n_ctx * sizeof(int);
+    const Range r[] = {{v.n_free, sizeof(int)}, {v.lens, n}, {counts, n}, {lens_out, n}, {granted, n}, {slots, (size_t)v.n_ctx * n_tok * 8}, {n_free_out, sizeof(int)}};
+    if (overlap(r, 3, 7)) return MONE_ERR_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     return timed(m, K_CACHE, st, 1, [&] { return launch_cache_reserve(v, n_tok, counts, granted, slots, lens_out, n_free_out, st); });
 }
@@ -1301,7 +1324,10 @@ mone_status mone_cache_reserve(mone_mem* m, const mone_pages* pages, int n_tok, 
 mone_status mone_cache_release(mone_mem* m, const mone_pages* pages, const int* keep, int* lens_out, int* n_free_out, void* stream) {
     PagesView v;
     MONE_TRY(pages_view(m, pages, lens_out, n_free_out, &v));
-    if (((uintptr_t)keep & 3u) || (lens_out && lens_out == keep)) return MONE_ERR_INVALID_ARG;
+    if ((uintptr_t)keep & 3u) return MONE_ERR_INVALID_ARG;
+    const size_t n = v.n_ctx * sizeof(int);
+    const Range r[] = {{v.n_free, sizeof(int)}, {v.lens, n}, {keep, n}, {lens_out, n}, {n_free_out, sizeof(int)}};
+    if (overlap(r, 3, 5)) return MONE_ERR_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     return timed(m, K_CACHE, st, 1, [&] { return launch_cache_release(v, keep, lens_out, n_free_out, st); });
 }

@@ -327,3 +327,16 @@ def test_evict_refuses_targets_that_are_too_small_or_lie_otherwise(fake):
         with pytest.raises(ValueError):
             mone.mone_cache_evict(h, -1, c, 50, 2, 3, *[bad if k == i else x for k, x in enumerate(good)], stream=0)
     assert mone.mone_mem_launch_count(h) == n0
+
+
+def test_lengths_that_overlap_what_a_call_reads_are_refused(fake):
+    h, c = init(), cache()
+    n0, a, lens = mone.mone_mem_launch_count(h), P + (1 << 16), P + 4096
+    to = type("T", (), dict(shape=(2, 10), data_ptr=lambda self: P + 64))()
+    for d in (-4, 0, 4):
+        refused(1, mone.mone_cache_append, h, -1, c, P, P, ST, 3, a + d, a)  # lens_out on counts, of two contexts' 8 bytes
+        refused(1, mone.mone_cache_append, h, -1, c, P, P, ST, 3, lens + d)
+        refused(1, mone.mone_cache_evict, h, -1, c, 50, 2, 3, to, P + 128, P, lens + d)
+    refused(1, mone.mone_cache_append, h, -1, c, P, P, ST, 3, P + 76)         # the last entry of the table
+    assert mone.mone_mem_launch_count(h) == n0
+    mone.mone_cache_append(h, -1, c, P, P, ST, 3, a, a + 8, stream=0)

@@ -350,3 +350,38 @@ def test_pages_and_heads_of_tensors(fake):
                 mone.mone_norm_rotate(h, -1, r, None, 5, q, k, stream=0)
     with pytest.raises(ValueError):
         mone.mone_norm_rotate(h, -1, r, z(1), 5, s, None, stream=0)
+
+
+def test_outputs_that_overlap_what_a_call_reads_are_refused(fake):
+    """A call's CTAs read the lengths and counts of other contexts than their own, and write without waiting for one another."""
+    h, c, p = init(), cache(), pages()
+    n0, a, lens, n_free = mone.mone_mem_launch_count(h), P + (1 << 16), P + 4096, P + 64
+    for d in (-4, 0, 4):  # of two contexts' 8 bytes
+        refused(1, mone.mone_cache_reserve, h, p, 3, P + 8, a + d, None, None, a)          # lens_out on counts
+        refused(1, mone.mone_cache_reserve, h, p, 3, P + 8, lens + d)                      # on lens
+        refused(1, mone.mone_cache_reserve, h, p, 3, P + 8, None, a + d, None, a)          # granted on counts
+        refused(1, mone.mone_cache_reserve, h, p, 3, P + 8, None, lens + d)
+        refused(1, mone.mone_cache_reserve, h, p, 3, P + 8, a + d, a)                      # on lens_out
+        refused(1, mone.mone_cache_release, h, p, P + 8, a, a + d)                         # lens_out on keep
+        refused(1, mone.mone_cache_release, h, p, P + 8, None, lens + d)
+        refused(1, mone.mone_cache4_append, h, -1, c, P, P, ST, 3, a + d, a)
+        refused(1, mone.mone_cache4_append, h, -1, c, P, P, ST, 3, lens + d)
+        refused(1, mone.mone_cache4_evict, h, -1, c, 50, 2, 3, tensor(P + 64, 2, 10), P + 128, P, lens + d)
+    for d in (0, 4):
+        refused(1, mone.mone_cache_reserve, h, p, 3, a + d, None, None, None, a)           # n_free_out in counts
+        refused(1, mone.mone_cache_reserve, h, p, 3, lens + d)
+        refused(1, mone.mone_cache_reserve, h, p, 3, a + d, a)
+        refused(1, mone.mone_cache_reserve, h, p, 3, a + d, None, a)
+        refused(1, mone.mone_cache_release, h, p, a + d, a)
+        refused(1, mone.mone_cache_release, h, p, lens + d)
+    for d in (-40, 0):  # two contexts' three slots of 8 bytes each
+        refused(1, mone.mone_cache_reserve, h, p, 3, P + 8, None, None, a + d, a)
+        refused(1, mone.mone_cache_reserve, h, p, 3, P + 8, a, None, a + d)
+        refused(1, mone.mone_cache_reserve, h, p, 3, a, None, None, a + d)
+    refused(1, mone.mone_cache_reserve, h, p, 3, P + 8, n_free)
+    refused(1, mone.mone_cache4_append, h, -1, c, P, P, ST, 3, P + 76)                     # the last entry of the table
+    assert mone.mone_mem_launch_count(h) == n0
+    mone.mone_cache_reserve(h, p, 3, P + 8, a, a + 8, a + 16, a + 64, stream=0)            # side by side
+    mone.mone_cache_release(h, p, P + 8, a, a + 8, stream=0)
+    mone.mone_cache4_append(h, -1, c, P, P, ST, 3, a, a + 8, stream=0)
+    assert mone.mone_mem_launch_count(h) == n0 + 3
