@@ -339,6 +339,19 @@ def make_cache(K, V, table, lens, score=None) -> mone_cache:
     return c
 
 
+def _struct(x, cls) -> int:
+    """The address of a struct of this class: it goes to the library untyped."""
+    if x.__class__ is not cls and not isinstance(x, cls):
+        raise ctypes.ArgumentError(f"expected a {cls.__name__}, not a {type(x).__name__}")
+    return _address(x)
+
+
+def _cache4(h: int, cache) -> int:
+    if cache.__class__ is not mone_cache4:
+        _struct(cache, mone_cache4)
+    return _address(_fitting(h, cache))
+
+
 def _fitting(h: int, cache):
     need = _handles.get(h)
     if cache._fits is not need:
@@ -415,7 +428,7 @@ def make_cache4(K, V, K_scale, V_scale, table, lens, score=None, k_exp=0, v_exp=
 def mone_cache4_append(h: int, layer: int, cache: mone_cache4, K, V, strides: Sequence[int], n_tok: int, lens_out=None, counts=None,
                        stream=None):
     """New tokens' keys and values, rounded to 4 bits, after each context's positions."""
-    rc = (_lib or lib()).mone_cache4_append(h, layer, _address(_fitting(h, cache)), _ptr(K), _ptr(V), _strides(strides), n_tok, _ptr(counts),
+    rc = (_lib or lib()).mone_cache4_append(h, layer, _cache4(h, cache), _ptr(K), _ptr(V), _strides(strides), n_tok, _ptr(counts),
                                             _ptr(lens_out), _stream(stream))
     if rc:
         _check("mone_cache4_append", rc)
@@ -423,7 +436,7 @@ def mone_cache4_append(h: int, layer: int, cache: mone_cache4, K, V, strides: Se
 
 def mone_cache4_read(h: int, layer: int, cache: mone_cache4, first, n_pos: int, K, V, strides: Sequence[int], stream=None):
     """Positions first[c] .. first[c] + n_pos - 1 (None: from 0) of each context as dense keys and values."""
-    rc = (_lib or lib()).mone_cache4_read(h, layer, _address(_fitting(h, cache)), _ptr(first), n_pos, _ptr(K), _ptr(V), _strides(strides),
+    rc = (_lib or lib()).mone_cache4_read(h, layer, _cache4(h, cache), _ptr(first), n_pos, _ptr(K), _ptr(V), _strides(strides),
                                           _stream(stream))
     if rc:
         _check("mone_cache4_read", rc)
@@ -432,7 +445,7 @@ def mone_cache4_read(h: int, layer: int, cache: mone_cache4, first, n_pos: int, 
 def mone_cache4_attention(h: int, layer: int, cache: mone_cache4, Q, n_q_heads: int, n_tok: int, n_sink: int, window: int, out,
                           stream=None):
     """mone_cache_attention over a 4-bit cache."""
-    rc = (_lib or lib()).mone_cache4_attention(h, layer, _address(_fitting(h, cache)), _ptr(Q), n_q_heads, n_tok, n_sink, window, _ptr(out),
+    rc = (_lib or lib()).mone_cache4_attention(h, layer, _cache4(h, cache), _ptr(Q), n_q_heads, n_tok, n_sink, window, _ptr(out),
                                                _stream(stream))
     if rc:
         _check("mone_cache4_attention", rc)
@@ -442,7 +455,7 @@ def mone_cache4_evict(h: int, layer: int, cache: mone_cache4, keep: int, n_sink:
                       lens_out=None, stream=None):
     """mone_cache_evict of a 4-bit cache."""
     width = _targets(h, layer, cache.page_size, keep, to_table, to_score, kept)
-    rc = (_lib or lib()).mone_cache4_evict(h, layer, _address(_fitting(h, cache)), keep, n_sink, n_recent, _ptr(to_table), width, _ptr(to_score),
+    rc = (_lib or lib()).mone_cache4_evict(h, layer, _cache4(h, cache), keep, n_sink, n_recent, _ptr(to_table), width, _ptr(to_score),
                                            _ptr(kept), _ptr(lens_out), _stream(stream))
     if rc:
         _check("mone_cache4_evict", rc)
@@ -462,21 +475,21 @@ def make_pages(free, n_free, table, lens, page_size: int) -> mone_pages:
     return p
 
 
-def _pages(h: int, pages: mone_pages) -> int:
-    """Checks the pages' contexts; the handle's."""
-    need = _handles.get(h)
+def _pages(h: int, pages: mone_pages):
+    """Checks the pages' contexts; their address and the handle's contexts."""
+    at, need = _struct(pages, mone_pages), _handles.get(h)
     if need is None:
-        return 1
+        return at, 1
     if pages._of is not None and pages._of < need[1]:
         raise ValueError(f"pages of {pages._of} contexts, the handle has {need[1]}")
-    return need[1]
+    return at, need[1]
 
 
 def mone_cache_reserve(h: int, pages: mone_pages, n_tok: int, n_free_out, lens_out=None, granted=None, slots=None, counts=None,
                        stream=None):
     """Pages for each context's next n_tok (or counts) tokens from the free list, and the tokens' slots [contexts, n_tok] int64."""
-    n = _pages(h, pages)
-    rc = (_lib or lib()).mone_cache_reserve(h, _address(pages), n_tok, _vector("counts", counts, "int32", n, "[contexts]"),
+    at, n = _pages(h, pages)
+    rc = (_lib or lib()).mone_cache_reserve(h, at, n_tok, _vector("counts", counts, "int32", n, "[contexts]"),
                                   _vector("granted", granted, "int32", n, "[contexts]"),
                                   _vector("slots", slots, "int64", n * n_tok, "[contexts, n_tok]"),
                                   _vector("lens_out", lens_out, "int32", n, "[contexts]"), _vector("n_free_out", n_free_out, "int32", 1, "[1]"),
@@ -487,8 +500,8 @@ def mone_cache_reserve(h: int, pages: mone_pages, n_tok: int, n_free_out, lens_o
 
 def mone_cache_release(h: int, pages: mone_pages, n_free_out, keep=None, lens_out=None, stream=None):
     """The pages that hold no position below keep (None: 0) back to the free list."""
-    n = _pages(h, pages)
-    rc = (_lib or lib()).mone_cache_release(h, _address(pages), _vector("keep", keep, "int32", n, "[contexts]"),
+    at, n = _pages(h, pages)
+    rc = (_lib or lib()).mone_cache_release(h, at, _vector("keep", keep, "int32", n, "[contexts]"),
                                   _vector("lens_out", lens_out, "int32", n, "[contexts]"), _vector("n_free_out", n_free_out, "int32", 1, "[1]"),
                                   _stream(stream))
     if rc:
@@ -526,7 +539,7 @@ def make_heads(x, out, weight=None) -> mone_heads:
 def mone_norm_rotate(h: int, layer: int, rotary: mone_rotary, first, n_tok: int, q: Optional[mone_heads], k: Optional[mone_heads],
                      stream=None):
     """Queries and keys normalised by head and rotated by position; first [contexts] int32: the first token's (None: 0)."""
-    rc = (_lib or lib()).mone_norm_rotate(h, layer, _address(rotary), _heads(h, layer, n_tok, q, k, first), n_tok,
+    rc = (_lib or lib()).mone_norm_rotate(h, layer, _struct(rotary, mone_rotary), _heads(h, layer, n_tok, q, k, first), n_tok,
                                           None if q is None else _address(q), None if k is None else _address(k), _stream(stream))
     if rc:
         _check("mone_norm_rotate", rc)
@@ -534,6 +547,9 @@ def mone_norm_rotate(h: int, layer: int, rotary: mone_rotary, first, n_tok: int,
 
 def _heads(h: int, layer: int, n_tok: int, q: Optional[mone_heads], k: Optional[mone_heads], first) -> Optional[int]:
     """Checks the sides against the handle; the address of first."""
+    for side in (q, k):
+        if side is not None and side.__class__ is not mone_heads:
+            _struct(side, mone_heads)
     need = _handles.get(h)
     if need is None:
         return _ptr(first)

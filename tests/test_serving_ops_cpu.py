@@ -385,3 +385,31 @@ def test_outputs_that_overlap_what_a_call_reads_are_refused(fake):
     mone.mone_cache_release(h, p, P + 8, a, a + 8, stream=0)
     mone.mone_cache4_append(h, -1, c, P, P, ST, 3, a, a + 8, stream=0)
     assert mone.mone_mem_launch_count(h) == n0 + 3
+
+
+def test_structs_of_another_kind_are_refused(fake):
+    """They go to the library by address, which would read past the end of a smaller one."""
+    dense = mone.mone_cache(P, P, strides(10 ** 5, 2048, 1024, 64), 40, 16, P, 10, P + 4096, P)
+    h, r, s = init(), mone.make_rotary(64), heads()
+    n0 = mone.mone_mem_launch_count(h)
+    others = [dense, cache(), pages(), r, s, ctypes.byref(cache()), ctypes.addressof(cache()), (ctypes.c_char * 8)()]
+    calls = {mone.mone_cache4: [lambda x: mone.mone_cache4_append(h, -1, x, P, P, ST, 3, stream=0),
+                                lambda x: mone.mone_cache4_read(h, -1, x, None, 3, P, P, ST, stream=0),
+                                lambda x: mone.mone_cache4_attention(h, -1, x, P, 4, 2, 1, 100, P, stream=0),
+                                lambda x: mone.mone_cache4_evict(h, -1, x, 50, 2, 3, tensor(P + 64, 2, 10), P + 128, P, stream=0)],
+             mone.mone_pages: [lambda x: mone.mone_cache_reserve(h, x, 3, P + 8, stream=0), lambda x: mone.mone_cache_release(h, x, P + 8, stream=0)],
+             mone.mone_rotary: [lambda x: mone.mone_norm_rotate(h, -1, x, P, 3, s, None, stream=0)],
+             mone.mone_heads: [lambda x: mone.mone_norm_rotate(h, -1, r, P, 3, x, None, stream=0), lambda x: mone.mone_norm_rotate(h, -1, r, P, 3, s, x, stream=0)],
+             mone.mone_cache: [lambda x: mone.mone_cache_append(h, -1, x, P, P, ST, 3, stream=0),
+                               lambda x: mone.mone_cache_attention(h, -1, x, P, 4, 2, 1, 100, P, stream=0)]}
+    for cls, fns in calls.items():
+        for x in others:
+            for call in fns if not isinstance(x, cls) else ():
+                with pytest.raises((ctypes.ArgumentError, AttributeError)):
+                    call(x)
+    assert mone.mone_mem_launch_count(h) == n0
+    with pytest.raises(ctypes.ArgumentError, match="mone_cache4"):
+        mone.mone_cache4_attention(h, -1, dense, P, 4, 2, 1, 100, P, stream=0)
+    mine = type("mine", (mone.mone_cache4,), {})
+    mone.mone_cache4_append(h, -1, mine.from_buffer_copy(cache()), P, P, ST, 3, stream=0)
+    assert mone.mone_mem_launch_count(h) == n0 + 1
