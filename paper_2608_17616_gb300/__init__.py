@@ -161,7 +161,7 @@ def lib(path: Optional[str] = None) -> ctypes.CDLL:
 
 
 def _ptr(x) -> Optional[int]:
-    if x is None or x.__class__ is int:
+    if x is None or isinstance(x, int):
         return x
     return x.data_ptr()
 
@@ -301,7 +301,7 @@ def _buffer(name: str, t, dtype: str, at_least: int, shape: str):
 
 def _vector(name: str, t, dtype: str, at_least: int, shape: str) -> Optional[int]:
     """The address of a tensor that _buffer takes; None and addresses as they are."""
-    if t is None or t.__class__ is int:
+    if t is None or isinstance(t, int):
         return t
     if t.dtype is not _types.get(dtype) or t.numel() < at_least or not t.is_contiguous():
         _buffer(name, t, dtype, at_least, shape)

@@ -413,3 +413,18 @@ def test_structs_of_another_kind_are_refused(fake):
     mine = type("mine", (mone.mone_cache4,), {})
     mone.mone_cache4_append(h, -1, mine.from_buffer_copy(cache()), P, P, ST, 3, stream=0)
     assert mone.mone_mem_launch_count(h) == n0 + 1
+
+
+def test_addresses_of_any_integer_class(fake):
+    class Address(int):
+        pass
+
+    at, h = Address(P), init()
+    n0 = mone.mone_mem_launch_count(h)
+    mone.mone_cache4_append(h, -1, cache(), at, at, ST, 3, Address(P + 65536), Address(P + 65600), stream=0)
+    mone.mone_cache4_attention(h, -1, cache(), at, 4, 2, 1, 100, at, stream=0)
+    mone.mone_cache_reserve(h, pages(), 3, Address(P + 8), Address(P + 65536), stream=0)
+    mone.mone_norm_rotate(h, -1, mone.make_rotary(64), at, 3, heads(), None, stream=0)
+    dense = mone.mone_cache(P, P, strides(10 ** 5, 2048, 1024, 64), 40, 16, P, 10, P + 4096, P)
+    mone.mone_cache_attention(h, -1, dense, at, 4, 2, 1, 100, at, stream=0)
+    assert mone.mone_mem_launch_count(h) == n0 + 5
