@@ -20,14 +20,16 @@ struct NormRotateArgs {
     long long jobs;
 };
 
-// cos and sin of an angle of `turn` 2^-64ths of a whole turn.  The nearest quarter turn is taken off exactly, so that the angle that is left,
-// an eighth of a turn at most, is rounded to 24 bits of itself.
+// cos and sin of an angle of `turn` 2^-64ths of a whole turn.  The nearest quarter turn is taken off exactly; the angle that is left,
+// an eighth of a turn at most, is off by 2^-23 of itself at most, however small it is: the nearest multiple of 2^-32 turns and what is left to it, of
+// either sign, are each rounded to 24 bits.
 __device__ __forceinline__ void cos_sin(unsigned long long turn, float& c, float& s) {
-    const uint32_t hi = (uint32_t)(turn >> 32);
+    const int32_t lo = (int32_t)(uint32_t)turn;
+    const uint32_t hi = (uint32_t)(turn >> 32) + ((uint32_t)turn >> 31);
     const uint32_t quarter = (hi + 0x20000000u) >> 30;
     const int32_t rest = (int32_t)(hi - (quarter << 30));
     float x, y;
-    sincospif((float)rest * 0x1p-31f, &y, &x);
+    sincospif(fmaf((float)lo, 0x1p-63f, (float)rest * 0x1p-31f), &y, &x);
     c = quarter & 1 ? -y : x;
     s = quarter & 1 ? x : y;
     if (quarter & 2) {

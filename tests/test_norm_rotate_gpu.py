@@ -179,3 +179,27 @@ def test_offsets_past_32_bits():
     mone.mone_mem_free(h)
     for a in range(2):
         check(x[0, 0, a], before[0, 0, a], None, np.arange(n_tok), [10000.0 ** (-i / 32) for i in range(32)], True, 1e-6)
+
+
+@pytest.mark.parametrize("halves", [True, False])
+@pytest.mark.parametrize("base,rot", [(500000.0, 128), (1000000.0, 128), (10000.0, 64)])
+def test_slow_pairs_turn_by_angles_of_full_precision(base, rot, halves):
+    """(0, 1) becomes (-sin, cos), each to bits of its own however small the angle is.  The angle is off by 2^-23 of itself at most, and sine and
+    cosine by 2^-22 of themselves: 2^-21 in all."""
+    hd, first = rot, [1, 1000]
+    h, n_tok = handle(2, 1, 2, hd, torch.float32), 9
+    x = torch.zeros(2, 1, 2, n_tok, hd, device="cuda")
+    b = slice(rot // 2, rot) if halves else slice(1, rot, 2)
+    a = slice(0, rot // 2) if halves else slice(0, rot, 2)
+    x[..., b] = 1.0
+    out = torch.empty_like(x)
+    freq = [base ** (-2.0 * i / rot) for i in range(rot // 2)]
+    rotary = mone.make_rotary(rot, mone.MONE_ROTATE_HALVES if halves else mone.MONE_ROTATE_NEIGHBOURS, freq=freq)
+    mone.mone_norm_rotate(h, -1, rotary, torch.tensor(first, dtype=torch.int32, device="cuda"), n_tok, None, mone.make_heads(x, out))
+    mone.mone_mem_sync(h)
+    mone.mone_mem_free(h)
+    for c in range(2):
+        angle = (first[c] + np.arange(n_tok))[:, None] * np.array(freq)
+        for got, ref in ((out[c, 0, :, :, a], -np.sin(angle)), (out[c, 0, :, :, b], np.cos(angle))):
+            err = np.abs(got.double().cpu().numpy() - ref) / np.abs(ref)
+            assert err.max() <= 2.0 ** -21, err.max()
