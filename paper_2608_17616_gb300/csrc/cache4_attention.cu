@@ -98,7 +98,11 @@ __device__ __forceinline__ uint32_t load_two_bytes(uint32_t addr) {
 // Halves hold a row of Q scaled by a power of two to 2^14 .. 2^15 at most (an element 2^-29 of the largest loses bits, 2^-39
 // of it at most), and probabilities times 2^7, of a maximum that may since have grown by 2^8 (what is below 2^-21 of the row's
 // largest loses bits).  Rows of 32 bits are two halves each, 22 bits, and so are their probabilities: up to four rows (BESIDE) lie
-// beside their rests in the N of 8, of more both are multiplied one after the other.
+// beside their rests in the N of 8, of more (TWO) both are multiplied one after the other.
+// The tensor cores cut an addend off at 2^-24 of the sum and do not round it, so values of one sign came out too small by 2^-24 a product at least: 1.2e-4 after
+// 65536 positions of a warp.  Of rows of 32 bits a block's products add up by themselves and then to the others', rounded, and the sum of
+// the probabilities is one of what they are before their rounding.  Of rows of 16 bits, whose last bit is 2^-8, they add up in the accumulators
+// (111.5 us for 123 over 131072 positions of 4 layers): less than 1e-4 of that length.
 //
 // Bound by instructions, not by HBM: 600 for a block of 32 keys of 128 (140 conversions, 128 products of halves, 34 MMAs, 32 loads from
 // shared memory, 35 for the copies of a block in one page), of which 62% of the issue slots are used, with 4 warps a scheduler and no pipe above
@@ -110,7 +114,7 @@ __device__ __forceinline__ uint32_t load_two_bytes(uint32_t addr) {
 template <typename T_, int HD_, int NT, bool BESIDE>
 struct CaFour {
     using T = T_;
-    static constexpr bool TWO = std::is_same<T, float>::value && !BESIDE;
+    static constexpr bool F32 = std::is_same<T, float>::value, TWO = F32 && !BESIDE;
     static constexpr int HD = HD_, ROWS = BESIDE ? 4 : 8 * NT, CTAS = NT == 1 ? (TWO ? 3 : 4) : 2;
     // Blocks of a warp, see item_ctas.  A second block costs a warp 0.6 us (head_dim 64) or 1, a cluster 0.9 (one layer of 370 positions 6.5 us, 7.4; with
     // three blocks a warp, two of a cluster's, 7.0 and 8.6).  With a third of the GPU's CTAs in clusters they take up to 12 blocks a warp (4 layers of
@@ -291,11 +295,20 @@ struct CaFour {
     struct Rows {
         uint32_t q[TWO ? 2 : 1][NT][HD / 16][2];
         float o[NT][HD / 16][4];
-        float l[NT][4];                // the sums of the probabilities that O's products see, in the layout of O (each twice)
-        float lx[NT][2];               // of the exact ones, this lane's
-        float from[NT][2];             // what is taken off a row's S: within 8 of its maximum in base 2, or FROM_NONE
+        float l[F32 ? 1 : NT][4];      // the sums of the probabilities that O's products see, in the layout of O (each twice); not F32
+        float lx[NT][2];               // of the exact ones, this lane's: F32, or with scores
+        float from[NT][2];             // what is taken off a row's S: within P_ROOM of its maximum in base 2, or FROM_NONE
         float unit[NT], k2[NT][2];     // of S: the unit in which it is q k (of row 8 i + gq), and in base 2 with the softmax's scale
     };
+
+    static __device__ __forceinline__ void add(float (&d)[4], const float (&x)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            const float2 s = add2(make_float2(x[i], x[i + 1]), make_float2(d[i], d[i + 1]));
+            d[i] = s.x;
+            d[i + 1] = s.y;
+        }
+    }
 
     // the row of h = 0, 1
     __device__ __forceinline__ int row_of(int i, int h) const { return BESIDE ? 2 * (lane & 1) + h : 8 * i + 2 * (lane & 3) + h; }
@@ -368,7 +381,8 @@ struct CaFour {
                 for (int h = 0; h < 2; ++h) {
                     const int row = row_of(i, h);
                     x.from[i][h] = FROM_NONE;
-                    x.l[i][h] = x.l[i][2 + h] = x.lx[i][h] = 0.f;
+                    if constexpr (!F32) x.l[i][h] = x.l[i][2 + h] = 0.f;
+                    x.lx[i][h] = 0.f;
                     const float k2 = scale2 * __shfl_sync(0xffffffffu, x.unit[i], 4 * (row - 8 * i));
                     x.k2[i][h] = fminf(fmaxf(k2, 1e-37f), 1e38f);  // (0 and infinity would make 0 of nothing)
                 }
@@ -402,16 +416,16 @@ struct CaFour {
             for (int i = 0; i < NT; ++i)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float l = x.l[i][h] * P_UNIT_INV, lx = x.lx[i][h] * P_UNIT_INV;
+                    float lx = x.lx[i][h] * P_UNIT_INV;
 #pragma unroll
                     for (int y = 4; y < 32; y <<= 1) lx += __shfl_xor_sync(0xffffffffu, lx, y);
+                    const float l = F32 ? lx : x.l[i][h] * P_UNIT_INV;
                     const int row = row_of(i, h), d0 = gq * (HD / 8);
                     const float unit = __shfl_sync(0xffffffffu, x.unit[i], 4 * (row - 8 * i));
                     float v[HD / 8];
 #pragma unroll
                     for (int d = 0; d < HD / 8; ++d) v[d] = x.o[i][d / 2][d % 2 * 2 + h] * P_UNIT_INV;
                     if constexpr (BESIDE) {
-                        l += __shfl_xor_sync(0xffffffffu, l, 2);
 #pragma unroll
                         for (int d = 0; d < HD / 8; ++d) v[d] += __shfl_xor_sync(0xffffffffu, v[d], 2);
                     }
@@ -526,7 +540,7 @@ struct CaFour {
                     const float f = ca_exp2((x.from[i][h] - to) * x.k2[i][h]);
                     x.from[i][h] = to;
                     x.lx[i][h] *= f;
-                    x.l[i][h] *= f;
+                    if constexpr (!F32) x.l[i][h] *= f;
 #pragma unroll
                     for (int d = 0; d < HD / 16; ++d) {
                         x.o[i][d][h] *= f;
@@ -539,13 +553,16 @@ struct CaFour {
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) e[u][k] = ca_exp2(fmaf(s[i][u][k] - x.from[i][k & 1], x.k2[i][k & 1], P_LOG2));
+            if (F32 || a.z2) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) x.lx[i][h] += (e[0][h] + e[0][2 + h]) + (e[1][h] + e[1][2 + h]);
+            }
             if (a.z2) {
                 float* z0;
                 asm volatile("ld.shared.b64 %0, [%1];" : "=l"(z0) : "r"(ring + SCORES) : "memory");
                 z0 += j0 + gq;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    x.lx[i][h] += (e[0][h] + e[0][2 + h]) + (e[1][h] + e[1][2 + h]);
                     if (row_of(i, h) < rows && !(BESIDE && t >= 2)) {
                         float* z = z0 + row_of(i, h) * a.pitch;
 #pragma unroll
@@ -562,24 +579,22 @@ struct CaFour {
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     uint32_t p = pack_halves(e[u][2 * half], e[u][2 * half + 1]);
-                    if constexpr (BESIDE) {
+                    if constexpr (F32) {
                         const float2 f = halves_float2(p);
                         const uint32_t rest = pack_halves(e[u][2 * half] - f.x, e[u][2 * half + 1] - f.y);
-                        p = t >= 2 ? rest : p;
+                        if constexpr (TWO)
+                            pb[TWO][i][u][half] = ca_transpose(rest);
+                        else
+                            p = t >= 2 ? rest : p;
                     }
                     pb[0][i][u][half] = ca_transpose(p);
-                    if constexpr (TWO) {
-                        const float2 f = halves_float2(p);
-                        pb[TWO][i][u][half] = ca_transpose(pack_halves(e[u][2 * half] - f.x, e[u][2 * half + 1] - f.y));
-                    }
                 }
-#pragma unroll
-                for (int y = 0; y < (TWO ? 2 : 1); ++y) mma_f16(x.l[i], ones, pb[y][i][u][0], pb[y][i][u][1]);
+                if constexpr (!F32) mma_f16(x.l[i], ones, pb[0][i][u][0], pb[0][i][u][1]);
             }
         }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            uint32_t w[4][HD / 64], b[4], sc[2];
+        uint32_t w[F32 ? 2 : 1][4][HD / 64], sc[F32 ? 2 : 1][2];
+        auto load = [&](int u, uint32_t (&w)[4][HD / 64], uint32_t (&sc)[2]) {
+            uint32_t b[4];
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
                 const int row = 16 * u + 8 * (y >> 1);  // and 2 t, and 1
@@ -592,25 +607,43 @@ struct CaFour {
             }
             sc[0] = scale_halves(b[0] | b[1] << 8);
             sc[1] = scale_halves(b[2] | b[3] << 8);
+        };
+        auto product = [&](int u, int k, const uint32_t (&w)[4][HD / 64], const uint32_t (&sc)[2], float (&sum)[F32 ? 4 : 1][4]) {
+            uint32_t h[2][2][4];  // of keys 2 t and + 1 (and + 8), elements 8 k + 2 e and + 1: a code of either in a byte
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const uint32_t p = w[2 * y][k], q = w[2 * y + 1][k];
+                code_halves(low_or_high(p, q << 4), h[y][0]);
+                code_halves(low_or_high(p >> 4, q), h[y][1]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t A[4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) A[y] = mul_halves(h[y >> 1][y & 1][e], sc[y >> 1]);
+#pragma unroll
+                for (int i = 0; i < NT; ++i) mma_f16(F32 ? sum[F32 ? e : 0] : x.o[i][4 * k + e], A, pb[0][i][u][0], pb[0][i][u][1]);
+                if constexpr (TWO) mma_f16(sum[e], A, pb[TWO][0][u][0], pb[TWO][0][u][1]);
+            }
+        };
+        if constexpr (F32) {
+            load(0, w[0], sc[0]);
+            load(1, w[F32], sc[F32]);
 #pragma unroll
             for (int k = 0; k < HD / 64; ++k) {
-                uint32_t h[2][2][4];  // of keys 2 t and + 1 (and + 8), elements 8 k + 2 e and + 1: a code of either in a byte
+                float sum[4][4] = {};
+                product(0, k, w[0], sc[0], sum);
+                product(1, k, w[F32], sc[F32], sum);
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const uint32_t p = w[2 * y][k], q = w[2 * y + 1][k];
-                    code_halves(low_or_high(p, q << 4), h[y][0]);
-                    code_halves(low_or_high(p >> 4, q), h[y][1]);
-                }
+                for (int e = 0; e < 4; ++e) add(x.o[0][4 * k + e], sum[e]);
+            }
+        } else {
+            float none[1][4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint32_t A[4];
+            for (int u = 0; u < 2; ++u) {
+                load(u, w[0], sc[0]);
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) A[y] = mul_halves(h[y >> 1][y & 1][e], sc[y >> 1]);
-#pragma unroll
-                    for (int i = 0; i < NT; ++i)
-#pragma unroll
-                        for (int y = 0; y < (TWO ? 2 : 1); ++y) mma_f16(x.o[i][4 * k + e], A, pb[y][i][u][0], pb[y][i][u][1]);
-                }
+                for (int k = 0; k < HD / 64; ++k) product(u, k, w[0], sc[0], none);
             }
         }
     }

@@ -672,3 +672,30 @@ def test_pools_and_offsets_past_32_bits(hd):
         at = O.cache_keep(score[0, 0, a, :n].cpu(), 100, 4, 20)
         assert kept[0, 0, a].tolist() == at.tolist()
         assert np.array_equal(K[0, 0, a].double().cpu().numpy(), kq[a, at]) and np.array_equal(V[0, 0, a].double().cpu().numpy(), vq[a, at])
+
+
+@pytest.mark.parametrize("group", [4, 8])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_sums_of_one_sign_over_a_long_walk(hd, group):
+    """More items than warps and values of one sign, so that a sum that is cut off rather than rounded shows: 512 blocks of a warp, each of 2^-20 of itself at
+    most, added up with a rounding of 2^-24 of either sign each, 1.4e-6 of the sum; weights as above."""
+    n, B, L, n_kv, page = 16384, 64, 20, 2, 32
+    g = np.random.default_rng(hd + group)
+    codes, values = [], []
+    for t in (g.standard_normal((1, n, hd)), 0.5 + np.abs(g.standard_normal((1, n, hd)))):
+        code, scale = O.four_bits(t)
+        values.append(O.four_bit_values(code, scale))
+        codes.append([torch.from_numpy(x).cuda().view(n // page, 1, page, -1).expand(L, -1, n_kv, -1, -1) for x in (packed(code), scale.astype(np.uint8))])
+    (K, Ks), (V, Vs) = codes
+    table = torch.arange(n // page, dtype=torch.int32, device="cuda").repeat(B, 1)
+    lens = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    Q = torch.from_numpy(g.standard_normal((n_kv * group, 1, hd))).float().cuda().expand(B, L, -1, -1, -1).contiguous()
+    h, out = handle(B, L, n_kv, hd, torch.float32), torch.full_like(Q, 7.0)
+    mone.mone_cache4_attention(h, -1, mone.make_cache4(K, V, Ks, Vs, table, lens), Q, n_kv * group, 1, 0, ALL, out)
+    mone.mone_mem_sync(h)
+    mone.mone_mem_free(h)
+    ref, _ = O.window_attention(Q[0, 0].double().cpu(), *values, n - 1, 0, ALL)
+    ref = torch.from_numpy(ref).cuda()
+    err = ((out.double() - ref).square().sum((-1, -2, -3)) / ref.square().sum()).sqrt().max().item()
+    record("cache4 attention", f"long walk hd {hd} group {group}", err, TOL[torch.float32])
+    assert err <= TOL[torch.float32]
