@@ -433,9 +433,10 @@ mone_status mone_cache4_read(mone_mem* m, int layer, const mone_cache4* cache, c
 
 /*
  * mone_cache_attention over a 4-bit cache: the same arguments, masks, weights, workspace and constraints, errors too.  Sums and
- * softmax are held in 32 bits; with a bf16 handle the probabilities are rounded to 11 bits for their product with the values, with an
- * fp32 handle queries and probabilities to 22.  An fp32 handle's sums are rounded; a bf16 handle's outputs are sums of which each product is cut
- * off at 2^-24, less than 2^-13 of values of one sign over 65536 positions.
+ * softmax are held in 32 bits; with a bf16 handle the probabilities are rounded to 11 bits for their product with the values (or to 2^-36 of the
+ * row's largest), with an fp32 handle to 22 (or 2^-47), and so are the queries (or to 2^-39 of the row's largest element).  An fp32 handle's
+ * sums are rounded; a bf16 handle's outputs are sums of which each product is cut off at 2^-24, less than 2^-13 of values of one sign
+ * over 65536 positions.
  */
 mone_status mone_cache4_attention(mone_mem* m, int layer, const mone_cache4* cache, const void* Q, int n_q_heads, int n_tok,
                                   int n_sink, int window, void* out, void* stream);

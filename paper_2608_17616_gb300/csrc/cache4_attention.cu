@@ -96,13 +96,15 @@ __device__ __forceinline__ uint32_t load_two_bytes(uint32_t addr) {
 // halves of two keys are paired by a permutation.  So nothing but the codes goes through shared memory.
 //
 // Halves hold a row of Q scaled by a power of two to 2^14 .. 2^15 at most (an element 2^-29 of the largest loses bits, 2^-39
-// of it at most), and probabilities times 2^7, of a maximum that may since have grown by 2^8 (what is below 2^-21 of the row's
-// largest loses bits).  Rows of 32 bits are two halves each, 22 bits, and so are their probabilities: up to four rows (BESIDE) lie
-// beside their rests in the N of 8, of more (TWO) both are multiplied one after the other.
+// of it at most), and probabilities times 2^11, of a maximum that may since have grown by 2^4 (what is below 2^-25 of the row's
+// largest loses bits, 2^-36 of it at most).  Rows of 32 bits are two halves each, 22 bits, and so are their probabilities: up to four rows (BESIDE) lie
+// beside their rests in the N of 8, of more (TWO) both are multiplied one after the other.  A probability's rest is held 2^11 larger and its products add up
+// apart, so that bits are lost below 2^-24 of the largest, 2^-47 of it at most (at the scale of the first halves from 2^-10 on: a row behind a large
+// weight of value 0 was 2e-4 off).
 // The tensor cores cut an addend off at 2^-24 of the sum and do not round it, so values of one sign came out too small by 2^-24 a product at least: 1.2e-4 after
 // 65536 positions of a warp.  Of rows of 32 bits a block's products add up by themselves and then to the others', rounded, and the sum of
-// the probabilities is one of what they are before their rounding.  Of rows of 16 bits, whose last bit is 2^-8, they add up in the accumulators
-// (111.5 us for 123 over 131072 positions of 4 layers): less than 1e-4 of that length.
+// the probabilities is one of what they are before their rounding (with the rests' scale, 4 layers of 131072: 118.8 us, 126.0; of more than four rows 139.1,
+// 151.5).  Of rows of 16 bits, whose last bit is 2^-8, they add up in the accumulators (112.1 us for 123.6): less than 1e-4 of that length.
 //
 // Bound by instructions, not by HBM: 600 for a block of 32 keys of 128 (140 conversions, 128 products of halves, 34 MMAs, 32 loads from
 // shared memory, 35 for the copies of a block in one page), of which 62% of the issue slots are used, with 4 warps a scheduler and no pipe above
@@ -131,7 +133,8 @@ struct CaFour {
     // the piece's scores and its head's addresses
     static constexpr int AHEAD = NS * STAGE, NOW = AHEAD + sizeof(Walk), SCORES = NOW + sizeof(Walk), WARP_BYTES = AHEAD + 256, ALIGN = 128;
     static constexpr int CHUNKS = HD / 32;  // of 16 bytes, of a row's codes
-    static constexpr float P_LOG2 = 7.f, P_UNIT_INV = 0x1p-7f, P_ROOM = 8.f, FROM_NONE = -3e38f;
+    // Of the probabilities and their rests (the growth that is let pass: with 2^8, and 2^7 for 2^11, 111.5 us for 112.1 and bits lost from 2^-21 on)
+    static constexpr float P_LOG2 = 11.f, P_UNIT_INV = 0x1p-11f, P_ROOM = 4.f, REST = 0x1p11f, REST_INV = 0x1p-11f, FROM_NONE = -3e38f;
     static_assert(CTAS * (CA_WARPS * WARP_BYTES + ALIGN + 1536) <= 228 * 1024, "CTAs an SM");
     static_assert(Part<HD, ROWS>::FLOATS * 4 <= AHEAD, "a part fits in the ring");
     static_assert(sizeof(Walk) % 16 == 0 && SCORES + 32 <= WARP_BYTES, "what is put aside");
@@ -301,10 +304,11 @@ struct CaFour {
         float unit[NT], k2[NT][2];     // of S: the unit in which it is q k (of row 8 i + gq), and in base 2 with the softmax's scale
     };
 
-    static __device__ __forceinline__ void add(float (&d)[4], const float (&x)[4]) {
+    static __device__ __forceinline__ void add(float (&d)[4], const float (&x)[4], float unit) {
 #pragma unroll
         for (int i = 0; i < 4; i += 2) {
-            const float2 s = add2(make_float2(x[i], x[i + 1]), make_float2(d[i], d[i + 1]));
+            const float2 a = make_float2(x[i], x[i + 1]), b = make_float2(d[i], d[i + 1]);
+            const float2 s = unit == 1.f ? add2(a, b) : fma2(a, make_float2(unit, unit), b);
             d[i] = s.x;
             d[i + 1] = s.y;
         }
@@ -427,7 +431,7 @@ struct CaFour {
                     for (int d = 0; d < HD / 8; ++d) v[d] = x.o[i][d / 2][d % 2 * 2 + h] * P_UNIT_INV;
                     if constexpr (BESIDE) {
 #pragma unroll
-                        for (int d = 0; d < HD / 8; ++d) v[d] += __shfl_xor_sync(0xffffffffu, v[d], 2);
+                        for (int d = 0; d < HD / 8; ++d) v[d] = fmaf(__shfl_xor_sync(0xffffffffu, v[d], 2), REST_INV, v[d]);
                     }
                     if (row >= rows || (BESIDE && t >= 2)) continue;
 #pragma unroll
@@ -580,8 +584,9 @@ struct CaFour {
                 for (int half = 0; half < 2; ++half) {
                     uint32_t p = pack_halves(e[u][2 * half], e[u][2 * half + 1]);
                     if constexpr (F32) {
-                        const float2 f = halves_float2(p);
-                        const uint32_t rest = pack_halves(e[u][2 * half] - f.x, e[u][2 * half + 1] - f.y);
+                        const float2 f = fma2(halves_float2(p), make_float2(-REST, -REST),
+                                              mul2(make_float2(e[u][2 * half], e[u][2 * half + 1]), make_float2(REST, REST)));
+                        const uint32_t rest = pack_halves(f.x, f.y);
                         if constexpr (TWO)
                             pb[TWO][i][u][half] = ca_transpose(rest);
                         else
@@ -608,7 +613,7 @@ struct CaFour {
             sc[0] = scale_halves(b[0] | b[1] << 8);
             sc[1] = scale_halves(b[2] | b[3] << 8);
         };
-        auto product = [&](int u, int k, const uint32_t (&w)[4][HD / 64], const uint32_t (&sc)[2], float (&sum)[F32 ? 4 : 1][4]) {
+        auto product = [&](int u, int k, const uint32_t (&w)[4][HD / 64], const uint32_t (&sc)[2], float (&sum)[F32 ? 4 : 1][4], float (&rest)[TWO ? 4 : 1][4]) {
             uint32_t h[2][2][4];  // of keys 2 t and + 1 (and + 8), elements 8 k + 2 e and + 1: a code of either in a byte
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
@@ -623,7 +628,7 @@ struct CaFour {
                 for (int y = 0; y < 4; ++y) A[y] = mul_halves(h[y >> 1][y & 1][e], sc[y >> 1]);
 #pragma unroll
                 for (int i = 0; i < NT; ++i) mma_f16(F32 ? sum[F32 ? e : 0] : x.o[i][4 * k + e], A, pb[0][i][u][0], pb[0][i][u][1]);
-                if constexpr (TWO) mma_f16(sum[e], A, pb[TWO][0][u][0], pb[TWO][0][u][1]);
+                if constexpr (TWO) mma_f16(rest[e], A, pb[TWO][0][u][0], pb[TWO][0][u][1]);
             }
         };
         if constexpr (F32) {
@@ -631,11 +636,14 @@ struct CaFour {
             load(1, w[F32], sc[F32]);
 #pragma unroll
             for (int k = 0; k < HD / 64; ++k) {
-                float sum[4][4] = {};
-                product(0, k, w[0], sc[0], sum);
-                product(1, k, w[F32], sc[F32], sum);
+                float sum[4][4] = {}, rest[TWO ? 4 : 1][4] = {};
+                product(0, k, w[0], sc[0], sum, rest);
+                product(1, k, w[F32], sc[F32], sum, rest);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) add(x.o[0][4 * k + e], sum[e]);
+                for (int e = 0; e < 4; ++e) {
+                    add(x.o[0][4 * k + e], sum[e], 1.f);
+                    if constexpr (TWO) add(x.o[0][4 * k + e], rest[e], REST_INV);
+                }
             }
         } else {
             float none[1][4];
@@ -643,7 +651,7 @@ struct CaFour {
             for (int u = 0; u < 2; ++u) {
                 load(u, w[0], sc[0]);
 #pragma unroll
-                for (int k = 0; k < HD / 64; ++k) product(u, k, w[0], sc[0], none);
+                for (int k = 0; k < HD / 64; ++k) product(u, k, w[0], sc[0], none, none);
             }
         }
     }

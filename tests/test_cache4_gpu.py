@@ -674,6 +674,39 @@ def test_pools_and_offsets_past_32_bits(hd):
         assert np.array_equal(K[0, 0, a].double().cpu().numpy(), kq[a, at]) and np.array_equal(V[0, 0, a].double().cpu().numpy(), vq[a, at])
 
 
+@pytest.mark.parametrize("dtype,group", [(torch.float32, 4), (torch.float32, 8), (torch.float32, 12), (torch.bfloat16, 4), (torch.bfloat16, 8), (torch.bfloat16, 16)])
+def test_small_weights_behind_a_large_one_of_value_zero(dtype, group):
+    """More items than warps, so that a warp goes through most of a context behind its first key, whose value is 0: the output is what the small
+    weights give, 2^-14 to 2^-28 of the largest (2^-24 with a bf16 handle).  The queries are exact in 8 bits.  fp32: scores of up to 20, each three roundings
+    of 2^-24 off, 3.6e-6 of a weight; the exponential 2^-22; a probability 2^-47 of the largest, 2^-19 of the smallest here: 5.8e-6.  bf16: as above."""
+    n, B, L, n_kv, hd, page = 2048, 64, 20, 2, 64, 32
+    key, val = np.zeros((1, n, hd)), np.zeros((1, n, hd))
+    key[0, 0, 0] = 6.0
+    val[0, 1:] = 6.0 * np.sign(np.arange(hd) - 20.5)
+    pools = []
+    for t in (key, val):
+        code, scale = O.four_bits(t)
+        assert np.array_equal(O.four_bit_values(code, scale), t)
+        pools.append([torch.from_numpy(x).cuda().view(n // page, 1, page, -1).expand(L, -1, n_kv, -1, -1) for x in (packed(code), scale.astype(np.uint8))])
+    (K, Ks), (V, Vs) = pools
+    table = torch.arange(n // page, dtype=torch.int32, device="cuda").repeat(B, 1)  # the contexts share their pages, layers and heads their rows
+    lens = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    z = [13.25, 18.5, 22.25, 26.0 if dtype is torch.float32 else 20.0]  # 8 / 6 of the largest score: weights of 2^-14.3, 2^-20.0, 2^-24.1 and 2^-28.1
+    Q = torch.zeros(B, L, n_kv * group, 1, hd, device="cuda")
+    Q[:, :, :, 0, 0] = torch.tensor([z[i % 4] for i in range(n_kv * group)], device="cuda")
+    Q = Q.to(dtype)
+    h, out = handle(B, L, n_kv, hd, dtype), torch.full_like(Q, 7.0)
+    mone.mone_cache4_attention(h, -1, mone.make_cache4(K, V, Ks, Vs, table, lens), Q, n_kv * group, 1, 0, ALL, out)
+    mone.mone_mem_sync(h)
+    mone.mone_mem_free(h)
+    for i in range(4):
+        ref, _ = O.window_attention(Q[0, 0, i:i + 1].double().cpu(), key, val, n - 1, 0, ALL)
+        got = out[:, :, i::4, 0].double().cpu()
+        err = max(rel_fro(x, ref[0, 0]) for x in got.reshape(-1, hd).unique(dim=0))
+        record("cache4 attention", f"weights of 2^-{z[i] * 0.75 / np.log(2):.0f} {str(dtype)[6:]} group {group}", err, TOL[dtype])
+        assert err <= TOL[dtype], (i, err)
+
+
 @pytest.mark.parametrize("group", [4, 8])
 @pytest.mark.parametrize("hd", [64, 128])
 def test_sums_of_one_sign_over_a_long_walk(hd, group):
