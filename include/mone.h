@@ -435,8 +435,8 @@ mone_status mone_cache4_read(mone_mem* m, int layer, const mone_cache4* cache, c
  * mone_cache_attention over a 4-bit cache: the same arguments, masks, weights, workspace and constraints, errors too.  Sums and
  * softmax are held in 32 bits; with a bf16 handle the probabilities are rounded to 11 bits for their product with the values (or to 2^-36 of the
  * row's largest), with an fp32 handle to 22 (or 2^-47), and so are the queries (or to 2^-39 of the row's largest element).  An fp32 handle's
- * sums are rounded; a bf16 handle's outputs are sums of which each product is cut off at 2^-24, less than 2^-13 of values of one sign
- * over 65536 positions.
+ * sums are rounded; of a bf16 handle's each product is cut off at 2^-24 of the sum so far, which over 2^18 positions is less than
+ * the output's own rounding.
  */
 mone_status mone_cache4_attention(mone_mem* m, int layer, const mone_cache4* cache, const void* Q, int n_q_heads, int n_tok,
                                   int n_sink, int window, void* out, void* stream);
@@ -526,7 +526,8 @@ typedef struct {
 /*
  *   q, k    one of them may be NULL
  *   first   NULL (0), or [n_ctx] (device, >= 0): the position of each context's first token (its length in a cache, say)
- * Sums of squares and rotations are in 32 bits and rounded once.  Constraints: rot_dim <= head_dim; 1 <= n_tok <= 2^24; n_heads <= 4096.
+ * Sums of squares and rotations are in 32 bits and rounded once, cosines and sines of an angle that is off by 2^-23 of itself at most (less its
+ * quarter turns).  Constraints: rot_dim <= head_dim; 1 <= n_tok <= 2^24; n_heads <= 4096.
  * Errors: INVALID_ARG.  Asynchronous on stream.
  */
 mone_status mone_norm_rotate(mone_mem* m, int layer, const mone_rotary* rotary, const int* first, int n_tok, const mone_heads* q,

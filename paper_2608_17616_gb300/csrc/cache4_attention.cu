@@ -107,7 +107,7 @@ __device__ __forceinline__ uint32_t load_two_bytes(uint32_t addr) {
 // 151.5).  Of rows of 16 bits, whose last bit is 2^-8, they add up in the accumulators (112.1 us for 123.6): less than 1e-4 of that length.
 //
 // Bound by instructions, not by HBM: 600 for a block of 32 keys of 128 (140 conversions, 128 products of halves, 34 MMAs, 32 loads from
-// shared memory, 35 for the copies of a block in one page), of which 62% of the issue slots are used, with 4 warps a scheduler and no pipe above
+// shared memory, 35 for the copies of a block in one page; fp32 710, with more than four rows 723; of 64 417), of which 62% of the issue slots are used, with 4 warps a scheduler and no pipe above
 // half.  Two tokens over 131072 positions of 4 layers: 112 us, 604 MB at 5.4 TB/s (the rows in 16 bits: 300).  On the way: 221 us with
 // masks, rescaling and a sum in every block; 175 with neither, and values' codes paired before their conversion (a permutation a pair of halves
 // less); 150 with four CTAs an SM for three (128 registers a thread for 168); 136 with a piece's walk out of the registers; 119 with
@@ -123,7 +123,7 @@ struct CaFour {
     // 9000, hd 128: 18.3 us, dealt 22.3), with fewer 6 (one of 9000: 12.3 and 11.6), with more 16 (8 contexts of up to 9000: 14.0 and 17.1).
     // A row's scales are 4 or 8 bytes of a sector of 32.  Two tokens over 131072 positions of 4 layers, heads and layers in step, heads only, neither: 112 us,
     // 117, 120; of pools whose heads lie inside positions 122, 151, 231 (1.46 GB read); head_dim 64 78, 81, 83, inside positions 87, 92, 197; 16 contexts
-    // of 32K in fp32 73, 73, 80.
+    // of 32K in fp32 73, 73, 80 (74 since its sums are rounded).
     static constexpr bool IN_STEP = true;
     using Walk = CaWalk<IN_STEP>;
     static constexpr int ONE = 2, EACH = 1, FULL = 16, SOME = 12, FEW = 6;

@@ -680,7 +680,8 @@ int item_ctas(const CaArgs& a, int sms) {
     // the idle share on, or 10 and 20 with clusters of 4 and 2, whose more items take longer to join.  (4-bit rows, 32 heads over 8, hd 128, two
     // tokens, us in clusters and dealt: 5 layers, 8 a cluster, half idle, 8192 positions 21.1 and 20.9, 131072 189 and 137; 6 layers, 16384
     // 33.5 and 35.0, 32768 56.1 and 54.1; 16 layers, 4 a cluster, a sixth idle, 16384 69.8 and 72.4, 65536 239 and 222; fp32, 2 a cluster, nearly half
-    // idle, 8192 50.1 and 53.8, 16384 89.2 and 84.4.)
+    // idle, 8192 53.3 and 56.5, 16384 97.1 and 90.5.  With one a cluster it could be sooner: 10 layers of 32 KV heads, nearly half idle, 4096 52.8 and 52.0, 8192 97
+    // and 83, 16384 186 and 146; 15, a fifth idle, 4096 66 and 70, 8192 123 and 117, 16384 235 and 210.)
     const bool idle = Form::IN_STEP && (slots - S * items) * blocks >= (long long)std::max(8, 40 / S) * slots * S * CA_WARPS;
     if (full && a.v.n_ctx == 1 && Form::FULL > 1 && !idle) return S;
     return blocks <= S * CA_WARPS * (full ? Form::FULL : 3 * S * items > slots ? Form::SOME : Form::FEW) ? S : 0;

@@ -133,7 +133,7 @@ struct RowWalk {
 
 // HD / 16 lanes take a job: some rows of one token, whose angles they compute once.  A lane has 16 elements of each row, with both of a pair, so that
 // a row takes no exchange but its sum of squares.
-// Bound by HBM and, in bf16, nearly by instructions (62% of the issue slots; fp32 two at a time; an angle's cosine and sine, 45 of them, once for 16
+// Bound by HBM and, in bf16, nearly by instructions (67% of the issue slots; fp32 two at a time; an angle's cosine and sine, 45 of them, once for 16
 // rows): 2048 tokens of 16 layers, 40 heads of 64 in 57 us, 336 MB at 5.8 TB/s, of 128 in 104 (6.4); in fp32 104 and 199 (6.5, 6.7; a copy
 // reaches 6.8).  The ring is what keeps enough bytes under way: a row at a time took 79 us, the next row's chunks in registers 90 (104 of
 // them, 14 warps an SM); a ring of 6 rows or jobs of 32 the same to 3% more.  Chunks of neighbouring lanes lie beside one another, so that an
